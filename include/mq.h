@@ -455,6 +455,119 @@ int mq_aifs_attention(const void* Q, int64_t ldq, const void* K, int64_t ldk, co
                       const int32_t* perm, const uint8_t* pad_u, int32_t L, int32_t n_q_heads, int32_t n_kv_heads,
                       int32_t head_dim, void* O, int64_t ldo, void* ws, size_t ws_bytes, int32_t* status, void* stream);
 
+/* ---- Paged key/value cache: store, attention, accumulated weights, eviction --------------------
+ *
+ * What a decoder block needs to go on after its prompt: the keys and values of a sequence live in pages of
+ * page_size tokens, page_table[b][p] names the page that holds keys p * page_size .. of sequence b, and the new
+ * tokens of a step (one per sequence, a few, or a long chunk) attend everything cached before them.
+ *
+ * mq_kv_cache describes the pages.  Key s of page p, head g is the row of head_dim contiguous elements at
+ * K + p * page_stride + g * head_stride + s * slot_stride (elements), and V alike: both page layouts in use,
+ * [page][head][slot][dim] and [page][slot][head][dim], are strides of this form.  Rows must start on 16-byte
+ * boundaries (MQ_ERR_ALIGNMENT).  head_dim 64 or 128, page_size a power of two from 16 to 256
+ * (MQ_ERR_UNSUPPORTED).  Elements are bf16 or, with MQ_KV_INT8, int8 codes with one static scale per
+ * key/value head and tensor (Eq. 2: value = code * scale), k_scale / v_scale device float32 [n_kv_heads].
+ *
+ * mq_kv_batch describes the new tokens: rows cu_q[b] .. cu_q[b + 1] - 1 of the query matrix belong to sequence b,
+ * kv_len[b] counts its keys INCLUDING the new ones (they are already in the cache, at its end).  All four arrays are
+ * device memory, so lengths may change between replays of a captured graph; total_q (rows), max_q (the most rows of
+ * one sequence) and max_pages (the table's row length) are host bounds.  Lengths are clamped to those bounds;
+ * table entries behind a sequence's last key are never read as pages.  A page number outside [0, n_pages) is
+ * never followed: its keys and values read as zeros.  n_seq <= 4096.
+ *   perm  NULL: row i of a chunk sees the cached context and the chunk's rows 0 .. i.  Else device int32
+ *         [total_q]: the chunk stands in AIFS order, perm[cu_q[b] + i] is the original index of its row i
+ *         (mq_aifs_reorder's output), and row i sees the context and the chunk's rows j with perm[j] <= perm[i]
+ *         (Eq. 5 behind a context).
+ * A row that sees no key (kv_len shorter than the chunk) gives zeros, and a log-sum-exp of -infinity.
+ */
+#define MQ_KV_INT8 1u    /* mq_kv_cache.flags: int8 codes with static scales */
+#define MQ_ROPE_HALF 1u  /* mq_qk_norm_rope flags: rotate channels (i, i + head_dim / 2) instead of (2i, 2i + 1) */
+
+typedef struct mq_kv_cache {
+  void* K; /* device, NULL only when n_pages is 0 */
+  void* V;
+  int64_t page_stride, head_stride, slot_stride; /* elements, of K and of V */
+  int32_t n_pages, page_size, n_kv_heads, head_dim;
+  uint32_t flags;
+  const float* k_scale; /* device float32 [n_kv_heads]: MQ_KV_INT8 only, else NULL */
+  const float* v_scale;
+} mq_kv_cache;
+
+typedef struct mq_kv_batch {
+  int32_t n_seq, total_q, max_q, max_pages;
+  const int32_t* cu_q;       /* device int32 [n_seq + 1], non-decreasing from 0 to total_q */
+  const int32_t* kv_len;     /* device int32 [n_seq] */
+  const int32_t* page_table; /* device int32 [n_seq][max_pages] */
+  const int32_t* perm;       /* device int32 [total_q] or NULL */
+} mq_kv_batch;
+
+/*
+ * Norm of every query and key head, rotary embedding on the ORIGINAL positions (App. A.2) and the store into the
+ * cache, in one pass over the projections' outputs:
+ *   x  = bf16 head of Q or K;  n = x / sqrt(mean(x^2) + eps) * gain   (a NULL gain skips that norm);
+ *   y  = n rotated by pos[t] * base^(-2i / head_dim) over its channel pairs (2i, 2i + 1), or (i, i + head_dim / 2)
+ *        with MQ_ROPE_HALF; the angle is reduced in double precision, so far positions lose nothing.
+ * Q_out (may be Q) receives the query heads and K_out (may be K, or NULL) the key heads, rounded once to bf16.
+ * With a cache, key and value row t go to slot slots[t] = page * page_size + slot of it: bf16, or
+ * sat_int8(round_half_even(y * (1 / scale))) of the unrounded y and of V.  Rows whose slot is outside the cache
+ * (padding: -1) are not stored.  Two rows with one slot leave either of them there.
+ *   Q [T, n_q_heads * head_dim], K, V [T, n_kv_heads * head_dim] (leading dimensions in elements, 16-byte rows)
+ *   gain_q, gain_k  device float32 [head_dim] or NULL, 16-byte aligned;  pos device int32 [T]
+ *   cache NULL: V and slots are ignored and K_out is required.  cache->head_dim / n_kv_heads must match.
+ * T = 0 is a successful no-op.
+ */
+int mq_qk_norm_rope(const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V, int64_t ldv, int32_t T,
+                    int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, const float* gain_q, const float* gain_k,
+                    float eps, const int32_t* pos, float base, uint32_t flags, void* Q_out, int64_t ldqo, void* K_out,
+                    int64_t ldko, const mq_kv_cache* cache, const int64_t* slots, void* stream);
+
+/*
+ * Attention of the new tokens over the paged cache:
+ *   O[i, h] = sum_j P[i, j] V[j, g(h)],  P[i, :] = softmax over the keys j that row i sees of scale * Q[i, h] . K[j, g(h)],
+ *   lse[i, h] = log of the softmax's denominator: log sum_j exp(scale * Q . K)     (optional, float32 [total_q, n_q_heads])
+ * with g(h) = h / (n_q_heads / n_kv_heads).  Q, O bf16 [total_q, n_q_heads * head_dim].  scale is finite and > 0.
+ * Scores, statistics and sums are float32; the probabilities enter the second product rounded to bf16 (bf16 cache)
+ * or fp16 (int8 cache).  Rows of O and lse that belong to no sequence are left as they were.
+ * ws: mq_kv_attention_workspace_bytes() bytes, 256-byte aligned, its status word reset once by
+ * mq_reset_device_status; calls that may overlap need workspaces of their own.  The status word receives
+ * MQ_ERR_INVALID_ARG if a page number of a cached key was outside the cache, MQ_ERR_TIMEOUT if a bounded wait expired.
+ */
+size_t mq_kv_attention_workspace_bytes(const mq_kv_batch* batch, const mq_kv_cache* cache, int32_t n_q_heads);
+int mq_kv_attention(const void* Q, int64_t ldq, const mq_kv_batch* batch, const mq_kv_cache* cache, int32_t n_q_heads,
+                    float scale, void* O, int64_t ldo, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * The softmax weight that every key received from this call's rows, added to what it had:
+ *   W_out[b, g, j] = (W_in[b, g, j] if key j was cached before this chunk, else 0)
+ *                    + sum over the chunk's rows i that see j and the query heads h of g of exp(scale * Q[i, h] . K[j, g] - lse[i, h])
+ * for j < kv_len[b]; other entries of W_out are left as they were.  lse is mq_kv_attention's output for the same
+ * call.  W_in NULL counts as zeros; W_in == W_out accumulates in place.  float32 throughout, and every sum is
+ * taken in a fixed order (no atomics).  w_seq_stride, w_head_stride: elements between sequences and heads
+ * (w_head_stride at least the longest kv_len; for both arrays).
+ */
+int mq_kv_weights(const void* Q, int64_t ldq, const mq_kv_batch* batch, const mq_kv_cache* cache, int32_t n_q_heads,
+                  float scale, const float* lse, const float* W_in, float* W_out, int64_t w_seq_stride,
+                  int64_t w_head_stride, void* stream);
+
+/*
+ * Eviction: cuts every sequence to at most `budget` keys per key/value head and copies them, in their order, to fresh
+ * pages.  Of sequence b with n = kv_len[b] keys, a head keeps
+ *   all of them if n <= budget; else the first n_first and the last n_last keys and, of the others, the
+ *   budget - n_first - n_last with the largest W[b, g, j] (of equal ones the lowest j; a NaN counts as lowest).
+ *   kept     int32 [n_seq, n_kv_heads, budget]: the kept keys' indices, ascending; entries behind them are left as they were
+ *   new_len  int32 [n_seq]: min(n, budget)
+ *   W_out    optional float32 [n_seq, n_kv_heads, budget]: the kept keys' weights (same order)
+ *   dst, dst_table [n_seq][dst_max_pages]: where the kept rows go, row i to slot i of the sequence's new pages; dst
+ *            has the type, heads and head_dim of `cache`, and may be the same cache as long as no destination page
+ *            is a source page of any sequence.  dst_max_pages * page_size must reach the budget.
+ * W: float32 with the strides of mq_kv_weights.  n_first + n_last <= budget (MQ_ERR_INVALID_ARG).  A page number outside
+ * the cache reads as zeros, and is not written to.  The page table's max_pages bounds kv_len.
+ */
+int mq_kv_evict(const mq_kv_cache* cache, const int32_t* page_table, int32_t max_pages, const int32_t* kv_len,
+                int32_t n_seq, const float* W, int64_t w_seq_stride, int64_t w_head_stride, int32_t budget,
+                int32_t n_first, int32_t n_last, const mq_kv_cache* dst, const int32_t* dst_table,
+                int32_t dst_max_pages, int32_t* kept, int32_t* new_len, float* W_out, void* stream);
+
 /* ---- Measurement and self-test aids (the paper has no counterpart) ------------------------- */
 
 /*

@@ -25,6 +25,8 @@ MQ_FLAG_Y_IS_F32 = 2
 MQ_FLAG_A4 = 4
 MQ_FLAG_W8 = 8
 MQ_NOALLOC_WS_BYTES = 4 << 20
+MQ_KV_INT8 = 1
+MQ_ROPE_HALF = 1
 MQ_W_TILE_N, MQ_W_TILE_K = 128, 128
 TEXT, VISUAL = 0, 1
 
@@ -47,6 +49,17 @@ class mq_linear_desc(C.Structure):
                 ("group_size", C.c_int32), ("flags", C.c_uint32)]
 
 
+class mq_kv_cache(C.Structure):
+    _fields_ = [("K", C.c_void_p), ("V", C.c_void_p), ("page_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("slot_stride", C.c_int64), ("n_pages", C.c_int32), ("page_size", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("flags", C.c_uint32), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+
+
+class mq_kv_batch(C.Structure):
+    _fields_ = [("n_seq", C.c_int32), ("total_q", C.c_int32), ("max_q", C.c_int32), ("max_pages", C.c_int32),
+                ("cu_q", C.c_void_p), ("kv_len", C.c_void_p), ("page_table", C.c_void_p), ("perm", C.c_void_p)]
+
+
 def lib_path() -> str:
     return os.path.join(os.path.dirname(os.path.abspath(__file__)), _LIB_NAME)
 
@@ -66,6 +79,7 @@ def load(build_if_missing: bool = False):
     lib = C.CDLL(path)
     vp, i32, i64, f32, sz = C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_size_t
     segp, descp = C.POINTER(mq_segments), C.POINTER(mq_linear_desc)
+    kvcp, kvbp = C.POINTER(mq_kv_cache), C.POINTER(mq_kv_batch)
     sigs = {
         "mq_version": (C.c_int, []),
         "mq_status_string": (C.c_char_p, [C.c_int]),
@@ -84,6 +98,12 @@ def load(build_if_missing: bool = False):
         "mq_glue_residual_add": (C.c_int, [vp, i64, vp, i64, i32, i32, vp, i64, vp]),
         "mq_aifs_attention_workspace_bytes": (sz, [i32, i32, i32]),
         "mq_aifs_attention": (C.c_int, [vp, i64, vp, i64, vp, i64, vp, vp, i32, i32, i32, i32, vp, i64, vp, sz, vp, vp]),
+        "mq_qk_norm_rope": (C.c_int, [vp, i64, vp, i64, vp, i64, i32, i32, i32, i32, vp, vp, f32, vp, f32, C.c_uint32, vp, i64,
+                                      vp, i64, kvcp, vp, vp]),
+        "mq_kv_attention_workspace_bytes": (sz, [kvbp, kvcp, i32]),
+        "mq_kv_attention": (C.c_int, [vp, i64, kvbp, kvcp, i32, f32, vp, i64, vp, vp, sz, vp]),
+        "mq_kv_weights": (C.c_int, [vp, i64, kvbp, kvcp, i32, f32, vp, vp, vp, i64, i64, vp]),
+        "mq_kv_evict": (C.c_int, [kvcp, vp, i32, vp, i32, vp, i64, i64, i32, i32, i32, kvcp, vp, i32, vp, vp, vp, vp]),
         "mq_repack_w4": (C.c_int, [vp, i32, i32, vp, vp]),
         "mq_unpack_w4": (C.c_int, [vp, vp, i32, i32, vp, i64, vp]),
         "mq_aifs_reorder": (C.c_int, [vp, vp, i32, i32, i64, i64, vp, vp, vp, vp, vp, i32, vp]),
@@ -121,7 +141,8 @@ EXPORTED = ["mq_version", "mq_status_string", "mq_workspace_bytes", "mq_w4_layou
             "mq_w4a8_msq_linear_rms", "mq_dynamic_quant_i8", "mq_dynamic_workspace_bytes", "mq_w4a8_dynamic_linear",
             "mq_ubench_mma_i8", "mq_selftest_bounded_wait", "mq_ubench_expand", "mq_calibrate_static_scales_bits",
             "mq_w8_layout_bytes", "mq_pack_w8", "mq_fwht_quant_bits", "mq_kron_quant_i8", "mq_glue_rmsnorm", "mq_glue_rope",
-            "mq_glue_swiglu", "mq_glue_residual_add", "mq_aifs_attention_workspace_bytes", "mq_aifs_attention"]
+            "mq_glue_swiglu", "mq_glue_residual_add", "mq_aifs_attention_workspace_bytes", "mq_aifs_attention",
+            "mq_qk_norm_rope", "mq_kv_attention_workspace_bytes", "mq_kv_attention", "mq_kv_weights", "mq_kv_evict"]
 
 
 def status_string(status: int) -> str:
@@ -462,6 +483,171 @@ def mq_aifs_attention(q, k, v, perm, pad_u, n_q_heads, n_kv_heads, o, ws, status
     _check(load().mq_aifs_attention(_ptr(q), _ld(q), _ptr(k), _ld(k), _ptr(v), _ld(v), _ptr(perm), _ptr(pad_u), L,
                                     n_q_heads, n_kv_heads, head_dim, _ptr(o), _ld(o), _ptr(ws), ws.numel(), _ptr(status),
                                     _stream()), "mq_aifs_attention")
+
+
+class KVCache:
+    """Handle of a paged cache (mq_kv_cache): K, V [n_pages, n_kv_heads, page_size, head_dim], bf16 or int8, of any strides
+    with contiguous rows (a [page, slot, head, dim] pool is passed as its .permute(0, 2, 1, 3) view).  An int8 cache
+    brings float32 [n_kv_heads] scales.  The tensors are kept alive by the handle."""
+
+    def __init__(self, K, V, k_scale=None, v_scale=None):
+        assert K.dim() == 4 and K.shape == V.shape and K.dtype == V.dtype and K.device == V.device
+        assert K.dtype in (torch.bfloat16, torch.int8)
+        if K.stride() != V.stride() or K.stride(3) != 1:
+            raise ValueError("K and V must have the same strides and contiguous rows")
+        int8 = K.dtype == torch.int8
+        if int8 != (k_scale is not None) or int8 != (v_scale is not None):
+            raise ValueError("an int8 cache needs k_scale and v_scale, a bf16 cache takes none")
+        n_pages, n_kv, page, dim = K.shape
+        if int8:
+            for s in (k_scale, v_scale):
+                assert s.dtype == torch.float32 and s.shape == (n_kv,) and s.is_contiguous() and s.device == K.device
+        self.K, self.V, self.k_scale, self.v_scale = K, V, k_scale, v_scale
+        # strides of dimensions of size one are arbitrary in torch: give them the value a packed pool would have
+        slot = K.stride(2) if page > 1 else dim
+        head = K.stride(1) if n_kv > 1 else max(slot * page, dim)
+        pg = K.stride(0) if n_pages > 1 else max(head * n_kv, slot * page, dim)
+        empty = n_pages == 0
+        self.c = mq_kv_cache(None if empty else _addr(K), None if empty else _addr(V), pg, head, slot, n_pages, page, n_kv, dim,
+                             MQ_KV_INT8 if int8 else 0, _addr(k_scale), _addr(v_scale))
+        self.device = K.device
+
+    @property
+    def page_size(self):
+        return self.c.page_size
+
+    @property
+    def head_dim(self):
+        return self.c.head_dim
+
+    @property
+    def n_kv_heads(self):
+        return self.c.n_kv_heads
+
+
+def _addr(t: Optional[torch.Tensor]):
+    """Device address of t as a plain integer (NULL for None)."""
+    if t is None:
+        return None
+    if not t.is_cuda:
+        raise ValueError("tensor must live on a CUDA device (the library has no CPU path)")
+    return t.data_ptr()
+
+
+def _kv_call(device, fn, where, *args):
+    """Runs one library call on the current stream of `device`, which is made current for it if it is not."""
+    if device.index is not None and device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            _check(fn(*args, torch.cuda.current_stream().cuda_stream), where)
+    else:
+        _check(fn(*args, torch.cuda.current_stream().cuda_stream), where)
+
+
+def _same_device(device, *tensors):
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError(f"tensor on {t.device}, the cache is on {device}")
+
+
+def _kv_batch(cu_q, kv_len, page_table, total_q, max_q, perm):
+    assert cu_q.dtype == torch.int32 and kv_len.dtype == torch.int32 and page_table.dtype == torch.int32
+    n_seq = kv_len.numel()
+    assert cu_q.numel() == n_seq + 1 and page_table.dim() == 2 and page_table.shape[0] == n_seq
+    assert cu_q.is_contiguous() and kv_len.is_contiguous() and page_table.is_contiguous()
+    assert perm is None or (perm.dtype == torch.int32 and perm.numel() == total_q and perm.is_contiguous())
+    return mq_kv_batch(n_seq, total_q, max_q, page_table.shape[1], _addr(cu_q), _addr(kv_len), _addr(page_table), _addr(perm))
+
+
+def mq_qk_norm_rope(q, k, pos, n_q_heads, n_kv_heads, q_out, k_out=None, gain_q=None, gain_k=None, eps=1e-6, base=10000.0,
+                    half=False, v=None, cache: Optional[KVCache] = None, slots=None):
+    """Per-head RMSNorm (where a gain is given), rotary embedding, and the store of K and V into `cache` at `slots`
+    (int64 [T], page * page_size + slot; negative: not stored).  See include/mq.h."""
+    T, width = q.shape
+    head_dim = width // n_q_heads
+    assert q.dtype == torch.bfloat16 and k.dtype == torch.bfloat16 and q_out.dtype == torch.bfloat16
+    assert width == n_q_heads * head_dim and k.shape == (T, n_kv_heads * head_dim) and q_out.shape == q.shape
+    assert k_out is None or (k_out.dtype == torch.bfloat16 and k_out.shape == k.shape)
+    assert pos.dtype == torch.int32 and pos.shape == (T,) and pos.is_contiguous()
+    for gain in (gain_q, gain_k):
+        assert gain is None or (gain.dtype == torch.float32 and gain.shape == (head_dim,) and gain.is_contiguous())
+    if cache is not None:
+        assert v.dtype == torch.bfloat16 and v.shape == k.shape
+        assert slots.dtype == torch.int64 and slots.shape == (T,) and slots.is_contiguous()
+    else:
+        v = slots = None
+    _same_device(q.device, k, pos, q_out, k_out, gain_q, gain_k, v, slots, None if cache is None else cache.K)
+    _kv_call(q.device, load().mq_qk_norm_rope, "mq_qk_norm_rope", _addr(q), _ld(q), _addr(k), _ld(k), _addr(v),
+             _ld(v) if v is not None else 0, T, n_q_heads, n_kv_heads, head_dim, _addr(gain_q), _addr(gain_k), float(eps),
+             _addr(pos), float(base), MQ_ROPE_HALF if half else 0, _addr(q_out), _ld(q_out), _addr(k_out),
+             _ld(k_out) if k_out is not None else 0, None if cache is None else C.byref(cache.c), _addr(slots))
+
+
+def mq_kv_attention_workspace_bytes(n_seq, total_q, max_q, max_pages, n_q_heads, cache: KVCache) -> int:
+    b = mq_kv_batch(n_seq, total_q, max_q, max_pages, 1, 1, 1, None)   # the arrays are not read for the size
+    return int(load().mq_kv_attention_workspace_bytes(C.byref(b), C.byref(cache.c), n_q_heads))
+
+
+def new_kv_attention_workspace(n_seq, total_q, max_q, max_pages, n_q_heads, cache: KVCache) -> torch.Tensor:
+    """Allocates (with torch) and clears a workspace for mq_kv_attention calls up to these bounds."""
+    with torch.cuda.device(cache.device):
+        n = mq_kv_attention_workspace_bytes(n_seq, total_q, max_q, max_pages, n_q_heads, cache)
+        if n == 0:
+            raise MqError(MQ_ERR_INVALID_ARG, "mq_kv_attention_workspace_bytes")
+        ws = torch.empty(n, dtype=torch.uint8, device=cache.device)
+        _check(load().mq_reset_device_status(_ptr(ws), _stream()), "mq_reset_device_status")
+    return ws
+
+
+def mq_kv_attention(q, cu_q, kv_len, page_table, cache: KVCache, n_q_heads, max_q, o, ws, lse=None, perm=None, scale=None):
+    """Attention of the new rows q over the paged cache; see include/mq.h.  scale: 1 / sqrt(head_dim) if not given."""
+    assert q.dtype == torch.bfloat16 and o.dtype == torch.bfloat16 and q.shape == o.shape
+    total_q = q.shape[0]
+    assert q.shape[1] == n_q_heads * cache.head_dim
+    assert lse is None or (lse.dtype == torch.float32 and lse.shape == (total_q, n_q_heads) and lse.is_contiguous())
+    _same_device(cache.device, q, cu_q, kv_len, page_table, o, ws, lse, perm)
+    b = _kv_batch(cu_q, kv_len, page_table, total_q, max_q, perm)
+    scale = float(scale) if scale is not None else cache.head_dim ** -0.5
+    _kv_call(cache.device, load().mq_kv_attention, "mq_kv_attention", _addr(q), _ld(q), C.byref(b), C.byref(cache.c), n_q_heads,
+             scale, _addr(o), _ld(o), _addr(lse), _addr(ws), ws.numel())
+
+
+def _weight_strides(w, n_seq, n_kv_heads):
+    assert w.dtype == torch.float32 and w.dim() == 3 and w.shape[:2] == (n_seq, n_kv_heads) and (w.stride(2) == 1 or w.shape[2] <= 1)
+    return w.stride(0), w.stride(1)
+
+
+def mq_kv_weights(q, cu_q, kv_len, page_table, cache: KVCache, n_q_heads, max_q, lse, w_out, w_in=None, perm=None, scale=None):
+    """Adds the softmax weight every key receives from the rows q to w_in (None: zeros) and writes w_out
+    (float32 [n_seq, n_kv_heads, >= longest kv_len]; may be w_in).  lse: mq_kv_attention's output for the same rows."""
+    assert q.dtype == torch.bfloat16 and q.shape[1] == n_q_heads * cache.head_dim
+    total_q = q.shape[0]
+    assert lse.dtype == torch.float32 and lse.shape == (total_q, n_q_heads) and lse.is_contiguous()
+    _same_device(cache.device, q, cu_q, kv_len, page_table, lse, w_out, w_in, perm)
+    b = _kv_batch(cu_q, kv_len, page_table, total_q, max_q, perm)
+    strides = _weight_strides(w_out, b.n_seq, cache.n_kv_heads)
+    if w_in is not None and (w_in.shape != w_out.shape or _weight_strides(w_in, b.n_seq, cache.n_kv_heads) != strides):
+        raise ValueError("w_in and w_out must have the same shape and strides")
+    scale = float(scale) if scale is not None else cache.head_dim ** -0.5
+    _kv_call(cache.device, load().mq_kv_weights, "mq_kv_weights", _addr(q), _ld(q), C.byref(b), C.byref(cache.c), n_q_heads, scale,
+             _addr(lse), _addr(w_in), _addr(w_out), strides[0], strides[1])
+
+
+def mq_kv_evict(cache: KVCache, page_table, kv_len, w, budget, n_first, n_last, dst: KVCache, dst_table, kept, new_len, w_out=None):
+    """Cuts every sequence to `budget` keys per key/value head by the weights w and copies the kept rows to dst_table's pages
+    of `dst` (see include/mq.h).  kept int32 [n_seq, n_kv_heads, budget], new_len int32 [n_seq], w_out float32 like kept."""
+    n_seq = kv_len.numel()
+    assert kv_len.dtype == torch.int32 and page_table.dtype == torch.int32 and dst_table.dtype == torch.int32
+    assert page_table.shape[0] == n_seq and dst_table.shape[0] == n_seq
+    assert page_table.is_contiguous() and dst_table.is_contiguous() and kv_len.is_contiguous()
+    shape = (n_seq, cache.n_kv_heads, budget)
+    assert kept.dtype == torch.int32 and kept.shape == shape and kept.is_contiguous()
+    assert new_len.dtype == torch.int32 and new_len.shape == (n_seq,) and new_len.is_contiguous()
+    assert w_out is None or (w_out.dtype == torch.float32 and w_out.shape == shape and w_out.is_contiguous())
+    _same_device(cache.device, page_table, kv_len, w, dst.K, dst_table, kept, new_len, w_out)
+    strides = _weight_strides(w, n_seq, cache.n_kv_heads)
+    _kv_call(cache.device, load().mq_kv_evict, "mq_kv_evict", C.byref(cache.c), _addr(page_table), page_table.shape[1], _addr(kv_len),
+             n_seq, _addr(w), strides[0], strides[1], budget, n_first, n_last, C.byref(dst.c), _addr(dst_table), dst_table.shape[1],
+             _addr(kept), _addr(new_len), _addr(w_out))
 
 
 def mq_last_device_status(ws):

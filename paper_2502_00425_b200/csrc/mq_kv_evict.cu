@@ -1,0 +1,267 @@
+// Eviction from the paged cache by accumulated weight: per sequence and key/value head the first n_first and the last
+// n_last keys stay, and of the others those with the largest weight (equal ones: the lowest index first) until the
+// budget is full; the kept rows move, in their order, to fresh pages.
+//
+// Two kernels.  Selection: one CTA per (sequence, head) finds the weight of the last kept key exactly by a radix select
+// over the weights' order-preserving integer images (12, 10 and 10 bits; three passes that hit L2 after the first),
+// and a fourth pass writes the kept indices in order with block-wide prefix counts.  Copy: 16-byte pieces of all kept
+// rows of the batch, many in flight per thread; this is what the call's bytes are.
+#include "mq_kv.cuh"
+
+namespace mq {
+namespace {
+
+constexpr int kSelThreads = 1024;
+constexpr int kBins = 4096;
+
+struct EvictParams {
+  KvView src, dst;
+  int dim_bytes;
+  const int32_t* table;
+  int max_pages;
+  const int32_t* kv_len;
+  int n_seq;
+  const float* W;
+  int64_t w_seq, w_head;
+  int budget, n_first, n_last;
+  const int32_t* dst_table;
+  int dst_max_pages;
+  int32_t* kept;
+  int32_t* new_len;
+  float* W_out;
+};
+
+__device__ __forceinline__ int evict_len(const EvictParams& p, int b) {
+  return (int)min((int64_t)max(p.kv_len[b], 0), (int64_t)p.max_pages << p.src.page_shift);
+}
+
+// Larger weights have larger images; NaN has the smallest, and the two zeros are one.
+__device__ __forceinline__ uint32_t image(float w) {
+  if (w != w) return 0u;
+  const uint32_t u = __float_as_uint(w + 0.0f);
+  return (u & 0x80000000u) ? ~u : u | 0x80000000u;
+}
+
+// Block-wide exclusive prefix of two 16-bit counts packed in one word (a thread counts at most 4: 4096 in all).
+__device__ __forceinline__ uint32_t block_prefix(uint32_t v, uint32_t* red, uint32_t& total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint32_t inc = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t y = __shfl_up_sync(0xffffffffu, inc, o);
+    if (lane >= o) inc += y;
+  }
+  if (lane == 31) red[warp] = inc;
+  __syncthreads();
+  uint32_t w = red[lane], winc = w;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t y = __shfl_up_sync(0xffffffffu, winc, o);
+    if (lane >= o) winc += y;
+  }
+  total = __shfl_sync(0xffffffffu, winc, 31);
+  const uint32_t base = __shfl_sync(0xffffffffu, winc - w, warp);
+  __syncthreads();   // `red` may be written again
+  return base + inc - v;
+}
+
+__global__ void __launch_bounds__(kSelThreads)
+kv_select_kernel(const __grid_constant__ EvictParams p) {
+  __shared__ uint32_t hist[kBins];
+  __shared__ uint32_t red[32];
+  __shared__ uint32_t found[2];
+  pdl_launch_dependents();
+  pdl_wait();
+  const int g = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
+  const int n = evict_len(p, b), m = min(n, p.budget);
+  const float* w = p.W + (int64_t)b * p.w_seq + (int64_t)g * p.w_head;
+  const int64_t out = ((int64_t)b * p.src.n_kv_heads + g) * p.budget;
+  if (g == 0 && tid == 0) p.new_len[b] = m;
+  if (n <= p.budget) {
+    for (int j = tid; j < n; j += kSelThreads) {
+      p.kept[out + j] = j;
+      if (p.W_out) p.W_out[out + j] = w[j];
+    }
+    return;
+  }
+  const int lo = p.n_first, hi = n - p.n_last;     // the keys that compete
+  uint32_t need = (uint32_t)(p.budget - p.n_first - p.n_last);   // how many of them stay; < hi - lo
+  uint32_t prefix = 0u, known = 0u;                // the bits of the last kept image found so far
+  const int shifts[3] = {20, 10, 0}, widths[3] = {12, 10, 10};
+  if (need > 0) {
+#pragma unroll 1
+    for (int pass = 0; pass < 3; ++pass) {
+      const int shift = shifts[pass];
+      const uint32_t bins = 1u << widths[pass];
+      for (uint32_t i = tid; i < bins; i += kSelThreads) hist[i] = 0u;
+      __syncthreads();
+      for (int j0 = lo + tid; j0 < hi; j0 += 4 * kSelThreads) {
+        float v[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) v[c] = j0 + c * kSelThreads < hi ? w[j0 + c * kSelThreads] : 0.0f;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const uint32_t u = image(v[c]);
+          if (j0 + c * kSelThreads < hi && (u & known) == prefix) atomicAdd(&hist[(u >> shift) & (bins - 1u)], 1u);
+        }
+      }
+      __syncthreads();
+      // from the largest bin down: the bin in which the count reaches `need`
+      const int per = (int)bins / kSelThreads;   // 4 or 1
+      uint32_t mine = 0u;
+      for (int c = 0; c < per; ++c) mine += hist[bins - 1u - (uint32_t)(tid * per + c)];
+      // (counts may pass 16 bits: a plain 32-bit scan)
+      uint32_t inc = mine;
+      const int lane = tid & 31, warp = tid >> 5;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t y = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += y;
+      }
+      if (lane == 31) red[warp] = inc;
+      __syncthreads();
+      uint32_t before = inc - mine;
+      for (int x = 0; x < warp; ++x) before += red[x];
+      if (before < need && before + mine >= need) {
+        uint32_t acc = before;
+        for (int c = 0; c < per; ++c) {
+          const uint32_t bin = bins - 1u - (uint32_t)(tid * per + c), h = hist[bin];
+          if (acc + h >= need) {
+            found[0] = bin;
+            found[1] = need - acc;
+            break;
+          }
+          acc += h;
+        }
+      }
+      __syncthreads();
+      prefix |= found[0] << shift;
+      known |= (bins - 1u) << shift;
+      need = found[1];
+      __syncthreads();
+    }
+  }
+  // every competing key with an image above `prefix` stays, and the first `need` of those equal to it (need = 0: none do)
+  const bool any = known != 0u;
+  uint32_t above = 0u, equal = 0u;   // counts before this tile
+  for (int j0 = 0; j0 < n; j0 += 4 * kSelThreads) {
+    uint32_t cls = 0u, cnt = 0u;
+    float v[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const int j = j0 + tid * 4 + c;
+      v[c] = j < n ? w[j] : 0.0f;
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const int j = j0 + tid * 4 + c;
+      if (j >= n) continue;
+      const uint32_t u = image(v[c]);
+      if (j < lo || j >= hi || (any && u > prefix)) { cls |= 1u << (2 * c); cnt += 1u; }
+      else if (any && u == prefix) { cls |= 2u << (2 * c); cnt += 1u << 16; }
+    }
+    uint32_t total;
+    const uint32_t pre = block_prefix(cnt, red, total);
+    uint32_t a = above + (pre & 0xffffu), e = equal + (pre >> 16);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const uint32_t k = (cls >> (2 * c)) & 3u;
+      if (k == 1u || (k == 2u && e < need)) {
+        const int64_t at = out + a + min(e, need);
+        p.kept[at] = j0 + tid * 4 + c;
+        if (p.W_out) p.W_out[at] = v[c];
+      }
+      if (k == 1u) ++a;
+      if (k == 2u) ++e;
+    }
+    above += total & 0xffffu;
+    equal += total >> 16;
+  }
+}
+
+// Threads walk the 16-byte pieces of all kept rows: piece q of row i of head g of sequence b.
+constexpr int kCopyThreads = 256;
+constexpr int kCopyRows = 4;   // rows a lane has in flight
+
+template <int kRowBytes>
+__global__ void __launch_bounds__(kCopyThreads)
+kv_copy_kernel(const __grid_constant__ EvictParams p) {
+  constexpr int kPieces = kRowBytes / 16, kPerCta = kCopyThreads / kPieces;   // rows per CTA and step
+  pdl_launch_dependents();
+  pdl_wait();
+  const int b = blockIdx.z, g = blockIdx.y;
+  const int m = min(evict_len(p, b), p.budget);
+  const int pc = (int)threadIdx.x % kPieces, r = (int)threadIdx.x / kPieces;
+  const int32_t* kept = p.kept + ((int64_t)b * p.src.n_kv_heads + g) * p.budget;
+  for (int i0 = blockIdx.x * kPerCta * kCopyRows; i0 < m; i0 += gridDim.x * kPerCta * kCopyRows) {
+    uint4 k[kCopyRows], v[kCopyRows];
+    int64_t to[kCopyRows];
+#pragma unroll
+    for (int c = 0; c < kCopyRows; ++c) {
+      const int i = i0 + c * kPerCta + r;
+      k[c] = v[c] = make_uint4(0u, 0u, 0u, 0u);
+      to[c] = -1;
+      if (i >= m) continue;
+      const int j = kept[i];
+      const int from_page = p.table[(int64_t)b * p.max_pages + (j >> p.src.page_shift)];
+      const int to_page = p.dst_table[(int64_t)b * p.dst_max_pages + (i >> p.dst.page_shift)];
+      if ((unsigned)from_page < (unsigned)p.src.n_pages) {
+        const int64_t off = (int64_t)from_page * p.src.page_stride + (int64_t)g * p.src.head_stride +
+                            (int64_t)(j & ((1 << p.src.page_shift) - 1)) * p.src.slot_stride + pc * 16;
+        k[c] = *reinterpret_cast<const uint4*>(p.src.K + off);
+        v[c] = *reinterpret_cast<const uint4*>(p.src.V + off);
+      }
+      if ((unsigned)to_page < (unsigned)p.dst.n_pages)
+        to[c] = (int64_t)to_page * p.dst.page_stride + (int64_t)g * p.dst.head_stride +
+                (int64_t)(i & ((1 << p.dst.page_shift) - 1)) * p.dst.slot_stride + pc * 16;
+    }
+#pragma unroll
+    for (int c = 0; c < kCopyRows; ++c) {
+      if (to[c] < 0) continue;
+      *reinterpret_cast<uint4*>(const_cast<uint8_t*>(p.dst.K) + to[c]) = k[c];
+      *reinterpret_cast<uint4*>(const_cast<uint8_t*>(p.dst.V) + to[c]) = v[c];
+    }
+  }
+}
+
+template <int kRowBytes>
+cudaError_t launch_copy(const EvictParams& p, cudaStream_t st) {
+  constexpr int rows = kCopyThreads / (kRowBytes / 16) * kCopyRows;
+  const unsigned x = (unsigned)((p.budget + rows - 1) / rows);
+  return launch_pdl(kv_copy_kernel<kRowBytes>, dim3(x < 1024u ? x : 1024u, (unsigned)p.src.n_kv_heads, (unsigned)p.n_seq),
+                    dim3(kCopyThreads), 0, st, p);
+}
+
+}  // namespace
+}  // namespace mq
+
+using namespace mq;
+
+extern "C" int mq_kv_evict(const mq_kv_cache* cache, const int32_t* page_table, int32_t max_pages, const int32_t* kv_len,
+                           int32_t n_seq, const float* W, int64_t w_seq_stride, int64_t w_head_stride, int32_t budget,
+                           int32_t n_first, int32_t n_last, const mq_kv_cache* dst, const int32_t* dst_table,
+                           int32_t dst_max_pages, int32_t* kept, int32_t* new_len, float* W_out, void* stream) {
+  EvictParams p{};
+  int rc = check_kv_cache(cache, &p.src);
+  if (rc != MQ_OK) return rc;
+  if ((rc = check_kv_cache(dst, &p.dst)) != MQ_OK) return rc;
+  if (dst->flags != cache->flags || dst->head_dim != cache->head_dim || dst->n_kv_heads != cache->n_kv_heads) return MQ_ERR_INVALID_ARG;
+  if (n_seq < 0 || max_pages < 0 || dst_max_pages < 0 || budget < 0 || n_first < 0 || n_last < 0 || w_seq_stride < 0 || w_head_stride < 0)
+    return MQ_ERR_INVALID_ARG;
+  if ((int64_t)n_first + n_last > budget || (int64_t)dst_max_pages * dst->page_size < budget) return MQ_ERR_INVALID_ARG;
+  if (n_seq > kMaxKvSeqs || cache->n_kv_heads > 65535 || max_pages > (1 << 22) || dst_max_pages > (1 << 22)) return MQ_ERR_UNSUPPORTED;
+  if (n_seq == 0) return MQ_OK;
+  if (!kv_len || !new_len || (max_pages > 0 && (!page_table || !W)) || (budget > 0 && (!dst_table || !kept))) return MQ_ERR_INVALID_ARG;
+  p.dim_bytes = cache->head_dim * ((cache->flags & MQ_KV_INT8) ? 1 : 2);
+  p.table = page_table; p.max_pages = max_pages; p.kv_len = kv_len; p.n_seq = n_seq;
+  p.W = W; p.w_seq = w_seq_stride; p.w_head = w_head_stride;
+  p.budget = budget; p.n_first = n_first; p.n_last = n_last;
+  p.dst_table = dst_table; p.dst_max_pages = dst_max_pages;
+  p.kept = kept; p.new_len = new_len; p.W_out = W_out;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cudaError_t e = launch_pdl(kv_select_kernel, dim3((unsigned)cache->n_kv_heads, (unsigned)n_seq), dim3(kSelThreads), 0, st, p);
+  if (e == cudaSuccess && budget > 0)
+    e = p.dim_bytes == 256 ? launch_copy<256>(p, st) : p.dim_bytes == 128 ? launch_copy<128>(p, st) : launch_copy<64>(p, st);
+  if (e != cudaSuccess) return cuda_status(e);
+  return cuda_status(cudaGetLastError());
+}

@@ -1,0 +1,172 @@
+// How the attention kernels over a paged cache divide their work (mq_kv_attn.cu, mq_kv_chunk.cu).
+//
+// A UNIT is (sequence, key/value head, block of kM query rows); a query row is (token, query head of the group), token
+// major, so that the heads of a group share every key tile.  A unit walks its keys in tiles.  All tiles of all units
+// form one line, which is cut into equal contiguous ranges, one per worker (CTA): ragged batches, one long sequence
+// and many short ones are all balanced without the host knowing a length.  A worker whose range covers a unit whole
+// writes its output; otherwise it leaves a partial result (running maximum, sum, unnormalised output) in its slot and
+// the combine kernel joins the slots in the order of the keys: no atomics, the result does not depend on timing.
+#pragma once
+
+#include "mq_kv.cuh"
+
+namespace mq {
+
+struct KvSchedArgs {
+  KvBatchView b;
+  int page_shift, max_q, group, n_kv;
+  int rows;        // kM: query rows of a unit
+  int tile;        // keys of a tile
+  int min_tiles;   // a worker gets at least this many tiles (fewer workers for little work)
+};
+
+// Keys [0, end) that row block rb of a sequence may see any of, and the tiles that hold them (at least one: a unit that
+// sees nothing still has to write its zeros).
+__device__ __forceinline__ int sched_end(const KvSchedArgs& a, const KvSeq& s, int rb) {
+  if (a.b.perm) return s.n_all;
+  const int last = min((int)(((int64_t)rb * a.rows + a.rows - 1) / a.group), s.n_new - 1);
+  return max(0, min(s.n_all, s.n_all - s.n_new + last + 1));
+}
+__device__ __forceinline__ int sched_tiles(const KvSchedArgs& a, const KvSeq& s, int rb) {
+  return max(1, (sched_end(a, s, rb) + a.tile - 1) / a.tile);
+}
+__device__ __forceinline__ int sched_blocks(const KvSchedArgs& a, const KvSeq& s) {
+  return (int)(((int64_t)s.n_new * a.group + a.rows - 1) / a.rows);
+}
+
+// prefix[b] = tiles of all units before sequence b; prefix[n_seq] = all.  Called by every thread of a block of kThreads;
+// `red` is shared scratch of kThreads / 32 entries.
+template <int kThreads>
+__device__ __forceinline__ void sched_prefix(const KvSchedArgs& a, int64_t* prefix, int64_t* red) {
+  const int n = a.b.n_seq, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int per = (n + kThreads - 1) / kThreads;
+  int64_t sum = 0;
+  for (int k = 0; k < per; ++k) {
+    const int b = tid * per + k;
+    if (b >= n) break;
+    const KvSeq s = kv_seq(a.b, a.page_shift, a.max_q, b);
+    const int blocks = sched_blocks(a, s);
+    int64_t t = 0;
+    if (a.b.perm) t = (int64_t)blocks * (blocks ? sched_tiles(a, s, 0) : 0);
+    else
+      for (int rb = 0; rb < blocks; ++rb) t += sched_tiles(a, s, rb);
+    sum += t * a.n_kv;
+    prefix[b + 1] = sum;   // within this thread's run; the offset follows
+  }
+  int64_t inc = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t v = __shfl_up_sync(0xffffffffu, inc, o);
+    if (lane >= o) inc += v;
+  }
+  if (lane == 31) red[warp] = inc;
+  __syncthreads();
+  int64_t off = inc - sum;
+  for (int w = 0; w < warp; ++w) off += red[w];
+  for (int k = 0; k < per; ++k) {
+    const int b = tid * per + k;
+    if (b >= n) break;
+    prefix[b + 1] += off;
+  }
+  if (tid == 0) prefix[0] = 0;
+  __syncthreads();
+}
+
+// The unit that holds position `at` of the line, and the tile of it that `at` is.
+struct KvUnit {
+  int b, g, rb, tiles, tile;
+  KvSeq s;
+};
+__device__ __forceinline__ KvUnit sched_unit(const KvSchedArgs& a, const int64_t* prefix, int64_t at) {
+  int lo = 0, hi = a.b.n_seq;   // prefix[lo] <= at < prefix[hi]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (prefix[mid] <= at) lo = mid;
+    else hi = mid;
+  }
+  KvUnit u;
+  u.b = lo;
+  u.s = kv_seq(a.b, a.page_shift, a.max_q, lo);
+  const int64_t per_head = (prefix[lo + 1] - prefix[lo]) / a.n_kv;
+  const int64_t x = at - prefix[lo];
+  u.g = (int)(x / per_head);
+  int64_t y = x - u.g * per_head;
+  if (a.b.perm) {
+    u.tiles = sched_tiles(a, u.s, 0);
+    u.rb = (int)(y / u.tiles);
+    y -= (int64_t)u.rb * u.tiles;
+  } else {
+    u.rb = 0;
+    u.tiles = sched_tiles(a, u.s, 0);
+    while (y >= u.tiles) {
+      y -= u.tiles;
+      u.tiles = sched_tiles(a, u.s, ++u.rb);
+    }
+  }
+  u.tile = (int)y;
+  return u;
+}
+
+// Workers that take part, and the start of worker w's range (w = workers: the end of the line).
+__device__ __forceinline__ int sched_workers(const KvSchedArgs& a, int64_t total, int grid) {
+  const int64_t most = (total + a.min_tiles - 1) / a.min_tiles;
+  return (int)(most < grid ? (most > 0 ? most : 1) : grid);
+}
+__device__ __forceinline__ int64_t sched_start(int64_t total, int workers, int w) { return total * w / workers; }
+// The worker whose range holds position `at`.
+__device__ __forceinline__ int sched_owner(int64_t total, int workers, int64_t at) {
+  int w = (int)(((at + 1) * workers - 1) / total);
+  while (sched_start(total, workers, w + 1) <= at) ++w;
+  while (sched_start(total, workers, w) > at) --w;
+  return w;
+}
+
+// ---- partial results -----------------------------------------------------------------------------------
+// Worker w has two slots: 2 w for a range's first piece when it starts inside a unit, 2 w + 1 for a piece that starts
+// with its unit and does not reach its end.  Record w names the unit whose first piece is in slot 2 w + 1.
+struct KvRecord {
+  int n_parts;   // 0: this worker left no first piece; else the pieces are slots 2 w + 1, 2 (w + 1), 2 (w + 2), ...
+  int b, g, rb;
+};
+struct KvParts {
+  KvRecord* rec;   // [workers]
+  float2* ml;      // [2 workers][rows]: maximum (log2 units), sum
+  float* o;        // [2 workers][rows][D]
+};
+inline size_t kv_parts_bytes(int workers, int rows, int dim) {
+  return align_up((size_t)workers * sizeof(KvRecord), 256) + align_up((size_t)workers * 2 * rows * sizeof(float2), 256) +
+         (size_t)workers * 2 * rows * dim * sizeof(float);
+}
+inline KvParts kv_parts(uint8_t* base, int workers, int rows) {
+  KvParts p;
+  p.rec = reinterpret_cast<KvRecord*>(base);
+  base += align_up((size_t)workers * sizeof(KvRecord), 256);
+  p.ml = reinterpret_cast<float2*>(base);
+  base += align_up((size_t)workers * 2 * rows * sizeof(float2), 256);
+  p.o = reinterpret_cast<float*>(base);
+  return p;
+}
+
+struct KvOutArgs {
+  __nv_bfloat16* O;
+  int64_t ldo;
+  float* lse;
+  int n_q_heads;
+};
+
+// joins the pieces of split units; grid `workers` x (rows / 4)
+int launch_kv_combine(const KvSchedArgs& a, const KvParts& parts, const KvOutArgs& out, int workers, int dim, cudaStream_t st);
+
+// the tensor-memory form for long chunks (mq_kv_chunk.cu)
+struct KvAttnArgs {
+  const uint8_t* Q;
+  int64_t ldq;       // bytes
+  KvSchedArgs sched;
+  KvView cache;
+  KvOutArgs out;
+  KvParts parts;
+  float scale;
+  int32_t* status;
+};
+
+}  // namespace mq
