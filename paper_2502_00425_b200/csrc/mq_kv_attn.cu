@@ -22,6 +22,7 @@ constexpr int kWarps = 4;
 constexpr int kTile = 16 * kWarps; // keys of a tile: 16 per warp
 constexpr int kThreads = kWarps * 32;
 constexpr int kCtasPerSm = 3;
+constexpr int kExtra = 3;         // what a unit costs besides its tiles, in tiles
 // fp16 probabilities reach down to 2^-24 only: with the reference 14 below the maximum they run up to 2^14 instead of 1, and
 // what is lost below is 2^-39 of the largest one (a sum over them stays in float32 either way).
 constexpr float kLiftF16 = 14.0f;
@@ -60,18 +61,19 @@ kv_decode_kernel(const __grid_constant__ KvAttnArgs p) {
   const KvSchedArgs& sc = p.sched;
   sched_prefix<kThreads>(sc, prefix, red);
   const int64_t total = prefix[sc.b.n_seq];
-  const int workers = sched_workers(sc, total, gridDim.x);
+  const int64_t share = sched_share(sc, total, gridDim.x);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quad = lane >> 2, t4 = lane & 3;
   KvRecord rec{0, 0, 0, 0};
-  int64_t at = 0, stop = 0;
-  if (total > 0 && (int)blockIdx.x < workers) {
-    at = sched_start(total, workers, blockIdx.x);
-    stop = sched_start(total, workers, blockIdx.x + 1);
-  }
+  int64_t at = min(total, (int64_t)blockIdx.x * share);
+  const int64_t stop = min(total, at + share);
   const uint32_t ring = kv_smem_u32(smem) + (uint32_t)(warp * C::kRing);
   while (at < stop) {
     const KvUnit u = sched_unit(sc, prefix, at);
-    const int t0 = u.tile, t1 = (int)min((int64_t)u.tiles, (int64_t)u.tile + (stop - at));
+    const int len = (int)min((int64_t)(u.tiles + sc.extra - u.skip), stop - at);   // of this range on the line
+    const int t0 = max(0, u.skip - sc.extra), t1 = max(0, u.skip + len - sc.extra);
+    const int64_t unit_at = at - u.skip;
+    at += len;
+    if (t0 == t1) continue;   // the range ends before the unit's first tile
     const int end = sched_end(sc, u.s, u.rb), ctx = u.s.n_all - u.s.n_new;
     const int row0 = u.rb * kM, n_rows = min(kM, u.s.n_new * sc.group - row0);
     const int32_t* table = sc.b.page_table + (int64_t)u.b * sc.b.max_pages;
@@ -386,56 +388,103 @@ kv_decode_kernel(const __grid_constant__ KvAttnArgs p) {
       }
     }
     if (t0 == 0 && !whole) {
-      const int64_t unit_end = at + u.tiles;   // this piece starts with its unit
-      rec.n_parts = sched_owner(total, workers, unit_end - 1) - (int)blockIdx.x + 1;
+      // the pieces end with the worker whose range holds the unit's last tile
+      rec.n_parts = (int)((unit_at + sc.extra + u.tiles - 1) / share) - (int)blockIdx.x + 1;
       rec.b = u.b; rec.g = u.g; rec.rb = u.rb;
     }
-    at += t1 - t0;
     __syncthreads();   // the join has been read before the next range fills the rings
   }
   if (threadIdx.x == 0) p.parts.rec[blockIdx.x] = rec;
 }
 
-// One warp per row of a split unit.
+// Joins the pieces of the units that are split: four rows of a record's unit per CTA, and per row four warps that take
+// every fourth piece (a decode step of one sequence has tens of pieces per unit and few units, so the call is as long
+// as this chain of loads).
+constexpr int kJoinRows = 4, kJoinWarps = 4;
 template <int kD>
-__global__ void __launch_bounds__(128)
+__global__ void __launch_bounds__(kJoinRows * kJoinWarps * 32)
 kv_combine_kernel(const __grid_constant__ KvSchedArgs sc, const KvParts parts, const KvOutArgs out) {
+  constexpr int kPer = kD / 32;
+  __shared__ float part[kJoinRows][kJoinWarps][kD + 2];
   pdl_launch_dependents();
   pdl_wait();
-  const int w = blockIdx.x, lane = threadIdx.x & 31;
+  const int w = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rr = warp / kJoinWarps, pw = warp % kJoinWarps;
   const KvRecord rec = parts.rec[w];
   if (rec.n_parts == 0) return;
-  const int r = blockIdx.y * 4 + (threadIdx.x >> 5);
   const KvSeq s = kv_seq(sc.b, sc.page_shift, sc.max_q, rec.b);
+  const int r = blockIdx.y * kJoinRows + rr;
   const int64_t row = (int64_t)rec.rb * sc.rows + r;
-  if (row >= (int64_t)s.n_new * sc.group) return;
+  const bool live = row < (int64_t)s.n_new * sc.group;
+  if ((int64_t)rec.rb * sc.rows + blockIdx.y * kJoinRows >= (int64_t)s.n_new * sc.group) return;
   auto slot = [&](int i) { return (int64_t)(i == 0 ? 2 * w + 1 : 2 * (w + i)) * sc.rows + r; };
-  float m = -INFINITY;
-  for (int i = lane; i < rec.n_parts; i += 32) m = fmaxf(m, parts.ml[slot(i)].x);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  constexpr int kPer = kD / 32;
-  float l = 0.0f, x[kPer];
+  float m = -INFINITY, l = 0.0f, x[kPer];
 #pragma unroll
   for (int e = 0; e < kPer; ++e) x[e] = 0.0f;
-#pragma unroll 4
-  for (int i = 0; i < rec.n_parts; ++i) {
-    const int64_t at = slot(i);
-    const float2 ml = parts.ml[at];
-    float v[kPer];
-    if (kPer == 4) {
-      const float4 q = *reinterpret_cast<const float4*>(parts.o + at * kD + lane * 4);
-      v[0] = q.x; v[1] = q.y; v[2 % kPer] = q.z; v[3 % kPer] = q.w;
-    } else {
-      const float2 q = *reinterpret_cast<const float2*>(parts.o + at * kD + lane * 2);
-      v[0] = q.x; v[1] = q.y;
-    }
-    const float f = ml.x == -INFINITY ? 0.0f : kv_exp2(ml.x - m);
-    l = fmaf(f, ml.y, l);
-    if (f != 0.0f) {
+  if (live) {
+    constexpr int kBatch = 8;
+    for (int i0 = pw; i0 < rec.n_parts; i0 += kBatch * kJoinWarps) {
+      float2 ml[kBatch];
+      float v[kBatch][kPer];
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) x[e] = fmaf(f, v[e], x[e]);
+      for (int c = 0; c < kBatch; ++c) {
+        const int i = i0 + c * kJoinWarps;
+        ml[c] = make_float2(-INFINITY, 0.0f);
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) v[c][e] = 0.0f;
+        if (i < rec.n_parts) {
+          const int64_t at = slot(i);
+          ml[c] = parts.ml[at];
+          const float* src = parts.o + at * kD + lane * kPer;
+          if (kPer == 4) {
+            const float4 q = *reinterpret_cast<const float4*>(src);
+            v[c][0] = q.x; v[c][1] = q.y; v[c][2 % kPer] = q.z; v[c][3 % kPer] = q.w;
+          } else {
+            const float2 q = *reinterpret_cast<const float2*>(src);
+            v[c][0] = q.x; v[c][1] = q.y;
+          }
+        }
+      }
+      float top = m;
+#pragma unroll
+      for (int c = 0; c < kBatch; ++c) top = fmaxf(top, ml[c].x);
+      if (top == -INFINITY) continue;
+      const float back = kv_exp2(m - top);   // (0 while nothing has been seen)
+      l *= back;
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) x[e] *= back;
+#pragma unroll
+      for (int c = 0; c < kBatch; ++c) {
+        if (ml[c].x == -INFINITY) continue;
+        const float f = kv_exp2(ml[c].x - top);
+        l = fmaf(f, ml[c].y, l);
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) x[e] = fmaf(f, v[c][e], x[e]);
+      }
+      m = top;
     }
+  }
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) part[rr][pw][lane * kPer + e] = x[e];
+  if (lane == 0) {
+    part[rr][pw][kD] = m;
+    part[rr][pw][kD + 1] = l;
+  }
+  __syncthreads();
+  if (pw != 0 || !live) return;
+  m = part[rr][0][kD];
+#pragma unroll
+  for (int k = 1; k < kJoinWarps; ++k) m = fmaxf(m, part[rr][k][kD]);
+  l = 0.0f;
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) x[e] = 0.0f;
+#pragma unroll
+  for (int k = 0; k < kJoinWarps; ++k) {
+    const float mk = part[rr][k][kD];
+    if (mk == -INFINITY) continue;
+    const float f = kv_exp2(mk - m);
+    l = fmaf(f, part[rr][k][kD + 1], l);
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) x[e] = fmaf(f, part[rr][k][lane * kPer + e], x[e]);
   }
   const int tok = s.begin + (int)(row / sc.group), head = rec.g * sc.group + (int)(row % sc.group);
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
@@ -487,9 +536,9 @@ int check_attention(const mq_kv_batch* batch, const mq_kv_cache* cache, int32_t 
 }  // namespace
 
 int launch_kv_combine(const KvSchedArgs& a, const KvParts& parts, const KvOutArgs& out, int workers, int dim, cudaStream_t st) {
-  const dim3 grid((unsigned)workers, (unsigned)(a.rows / 4));
-  const cudaError_t e = dim == 128 ? launch_pdl(kv_combine_kernel<128>, grid, dim3(128), 0, st, a, parts, out)
-                                   : launch_pdl(kv_combine_kernel<64>, grid, dim3(128), 0, st, a, parts, out);
+  const dim3 grid((unsigned)workers, (unsigned)(a.rows / kJoinRows)), block(kJoinRows * kJoinWarps * 32);
+  const cudaError_t e = dim == 128 ? launch_pdl(kv_combine_kernel<128>, grid, block, 0, st, a, parts, out)
+                                   : launch_pdl(kv_combine_kernel<64>, grid, block, 0, st, a, parts, out);
   if (e != cudaSuccess) return cuda_status(e);
   return cuda_status(cudaGetLastError());
 }
@@ -527,7 +576,8 @@ extern "C" int mq_kv_attention(const void* Q, int64_t ldq, const mq_kv_batch* ba
   a.sched.n_kv = cache->n_kv_heads;
   a.sched.rows = p.rows;
   a.sched.tile = p.tile;
-  a.sched.min_tiles = 1;
+  a.sched.extra = kExtra;
+  a.sched.min_len = kExtra + 2;
   a.out.O = static_cast<__nv_bfloat16*>(O);
   a.out.ldo = ldo;
   a.out.lse = lse;

@@ -1,11 +1,13 @@
 // How the attention kernels over a paged cache divide their work (mq_kv_attn.cu, mq_kv_chunk.cu).
 //
 // A UNIT is (sequence, key/value head, block of kM query rows); a query row is (token, query head of the group), token
-// major, so that the heads of a group share every key tile.  A unit walks its keys in tiles.  All tiles of all units
-// form one line, which is cut into equal contiguous ranges, one per worker (CTA): ragged batches, one long sequence
-// and many short ones are all balanced without the host knowing a length.  A worker whose range covers a unit whole
-// writes its output; otherwise it leaves a partial result (running maximum, sum, unnormalised output) in its slot and
-// the combine kernel joins the slots in the order of the keys: no atomics, the result does not depend on timing.
+// major, so that the heads of a group share every key tile.  A unit walks its keys in tiles.  All units form one line, a
+// unit as long as its tiles plus a fixed length for what it costs besides them (queries, filling the pipeline, writing
+// the result), and the line is cut into equal contiguous ranges, one per worker (CTA): ragged batches, one long
+// sequence and many short ones are all balanced without the host knowing a length.  A worker whose range covers a
+// unit's tiles whole writes its output; otherwise it leaves a partial result (exponent reference, sum, unnormalised
+// output) in its slot and the combine kernel joins the slots in the order of the keys: no atomics, the result does
+// not depend on timing.
 #pragma once
 
 #include "mq_kv.cuh"
@@ -17,7 +19,8 @@ struct KvSchedArgs {
   int page_shift, max_q, group, n_kv;
   int rows;        // kM: query rows of a unit
   int tile;        // keys of a tile
-  int min_tiles;   // a worker gets at least this many tiles (fewer workers for little work)
+  int extra;       // a unit's cost besides its tiles, in tiles
+  int min_len;     // a worker's range is at least this long (fewer workers for little work)
 };
 
 // Keys [0, end) that row block rb of a sequence may see any of, and the tiles that hold them (at least one: a unit that
@@ -34,7 +37,7 @@ __device__ __forceinline__ int sched_blocks(const KvSchedArgs& a, const KvSeq& s
   return (int)(((int64_t)s.n_new * a.group + a.rows - 1) / a.rows);
 }
 
-// prefix[b] = tiles of all units before sequence b; prefix[n_seq] = all.  Called by every thread of a block of kThreads;
+// prefix[b] = length of all units before sequence b; prefix[n_seq] = the whole line.  Called by every thread of a block of kThreads;
 // `red` is shared scratch of kThreads / 32 entries.
 template <int kThreads>
 __device__ __forceinline__ void sched_prefix(const KvSchedArgs& a, int64_t* prefix, int64_t* red) {
@@ -47,9 +50,9 @@ __device__ __forceinline__ void sched_prefix(const KvSchedArgs& a, int64_t* pref
     const KvSeq s = kv_seq(a.b, a.page_shift, a.max_q, b);
     const int blocks = sched_blocks(a, s);
     int64_t t = 0;
-    if (a.b.perm) t = (int64_t)blocks * (blocks ? sched_tiles(a, s, 0) : 0);
+    if (a.b.perm) t = (int64_t)blocks * (blocks ? sched_tiles(a, s, 0) + a.extra : 0);
     else
-      for (int rb = 0; rb < blocks; ++rb) t += sched_tiles(a, s, rb);
+      for (int rb = 0; rb < blocks; ++rb) t += sched_tiles(a, s, rb) + a.extra;
     sum += t * a.n_kv;
     prefix[b + 1] = sum;   // within this thread's run; the offset follows
   }
@@ -72,9 +75,9 @@ __device__ __forceinline__ void sched_prefix(const KvSchedArgs& a, int64_t* pref
   __syncthreads();
 }
 
-// The unit that holds position `at` of the line, and the tile of it that `at` is.
+// The unit that holds position `at` of the line; `skip` is the place in it (0 .. extra + tiles - 1).
 struct KvUnit {
-  int b, g, rb, tiles, tile;
+  int b, g, rb, tiles, skip;
   KvSeq s;
 };
 __device__ __forceinline__ KvUnit sched_unit(const KvSchedArgs& a, const int64_t* prefix, int64_t at) {
@@ -91,34 +94,25 @@ __device__ __forceinline__ KvUnit sched_unit(const KvSchedArgs& a, const int64_t
   const int64_t x = at - prefix[lo];
   u.g = (int)(x / per_head);
   int64_t y = x - u.g * per_head;
+  u.tiles = sched_tiles(a, u.s, 0);
+  u.rb = 0;
   if (a.b.perm) {
-    u.tiles = sched_tiles(a, u.s, 0);
-    u.rb = (int)(y / u.tiles);
-    y -= (int64_t)u.rb * u.tiles;
+    u.rb = (int)(y / (u.tiles + a.extra));
+    y -= (int64_t)u.rb * (u.tiles + a.extra);
   } else {
-    u.rb = 0;
-    u.tiles = sched_tiles(a, u.s, 0);
-    while (y >= u.tiles) {
-      y -= u.tiles;
+    while (y >= u.tiles + a.extra) {
+      y -= u.tiles + a.extra;
       u.tiles = sched_tiles(a, u.s, ++u.rb);
     }
   }
-  u.tile = (int)y;
+  u.skip = (int)y;
   return u;
 }
 
-// Workers that take part, and the start of worker w's range (w = workers: the end of the line).
-__device__ __forceinline__ int sched_workers(const KvSchedArgs& a, int64_t total, int grid) {
-  const int64_t most = (total + a.min_tiles - 1) / a.min_tiles;
-  return (int)(most < grid ? (most > 0 ? most : 1) : grid);
-}
-__device__ __forceinline__ int64_t sched_start(int64_t total, int workers, int w) { return total * w / workers; }
-// The worker whose range holds position `at`.
-__device__ __forceinline__ int sched_owner(int64_t total, int workers, int64_t at) {
-  int w = (int)(((at + 1) * workers - 1) / total);
-  while (sched_start(total, workers, w + 1) <= at) ++w;
-  while (sched_start(total, workers, w) > at) --w;
-  return w;
+// Length of a worker's range: the line cut into at most `grid` equal ranges (the last one may be shorter or empty).
+__device__ __forceinline__ int64_t sched_share(const KvSchedArgs& a, int64_t total, int grid) {
+  const int64_t len = (total + grid - 1) / grid;
+  return len > a.min_len ? len : a.min_len;
 }
 
 // ---- partial results -----------------------------------------------------------------------------------
