@@ -473,7 +473,7 @@ int mq_aifs_attention(const void* Q, int64_t ldq, const void* K, int64_t ldk, co
  * device memory, so lengths may change between replays of a captured graph; total_q (rows), max_q (the most rows of
  * one sequence) and max_pages (the table's row length) are host bounds.  Lengths are clamped to those bounds;
  * table entries behind a sequence's last key are never read as pages.  A page number outside [0, n_pages) is
- * never followed: its keys and values read as zeros.  n_seq <= 4096.
+ * never followed: its keys and values read as zeros.  n_seq <= 2048.
  *   perm  NULL: row i of a chunk sees the cached context and the chunk's rows 0 .. i.  Else device int32
  *         [total_q]: the chunk stands in AIFS order, perm[cu_q[b] + i] is the original index of its row i
  *         (mq_aifs_reorder's output), and row i sees the context and the chunk's rows j with perm[j] <= perm[i]

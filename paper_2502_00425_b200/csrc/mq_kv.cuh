@@ -64,7 +64,7 @@ inline int check_kv_cache(const mq_kv_cache* c, KvView* out) {
   return MQ_OK;
 }
 
-constexpr int kMaxKvSeqs = 4096;   // sequences of one call: every CTA keeps a prefix over them in shared memory
+constexpr int kMaxKvSeqs = 2048;   // sequences of one call: every CTA keeps a prefix over them in shared memory
 
 inline int check_kv_batch(const mq_kv_batch* b, KvBatchView* out) {
   if (!b) return MQ_ERR_INVALID_ARG;

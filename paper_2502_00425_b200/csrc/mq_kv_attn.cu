@@ -508,17 +508,22 @@ int launch_decode(const KvAttnArgs& a, int workers, cudaStream_t st) {
   return cuda_status(cudaGetLastError());
 }
 
+// Which kernel, and how many workers.  Up to kFewRows query rows per key/value head (tokens x heads of the group) take the
+// kernel above in blocks of 16 rows, more take the 128-row tensor-memory kernel of mq_kv_chunk.cu.
+constexpr int kFewRows = 32;
 struct Plan {
-  int workers, rows, tile;
+  bool chunk;
+  int workers, rows, tile, extra;
 };
 Plan attn_plan(const mq_kv_batch* b, const mq_kv_cache* c, int group) {
-  Plan p;
-  p.rows = kM;
-  p.tile = kTile;
+  Plan p{};
+  p.chunk = (int64_t)b->max_q * group > kFewRows && c->n_pages > 0;
+  if (p.chunk) kv_chunk_shape(&p.rows, &p.tile, &p.extra);
+  else p.rows = kM, p.tile = kTile, p.extra = kExtra;
   const int64_t blocks = ((int64_t)b->max_q * group + p.rows - 1) / p.rows;
   const int64_t tiles = (((int64_t)b->max_pages * c->page_size) + p.tile - 1) / p.tile;
   const int64_t most = (int64_t)b->n_seq * c->n_kv_heads * blocks * (tiles > 0 ? tiles : 1);
-  const int64_t cap = (int64_t)sm_count() * kCtasPerSm;
+  const int64_t cap = (int64_t)sm_count() * (p.chunk ? 1 : kCtasPerSm);
   p.workers = (int)(most < cap ? (most > 0 ? most : 1) : cap);
   return p;
 }
@@ -576,8 +581,8 @@ extern "C" int mq_kv_attention(const void* Q, int64_t ldq, const mq_kv_batch* ba
   a.sched.n_kv = cache->n_kv_heads;
   a.sched.rows = p.rows;
   a.sched.tile = p.tile;
-  a.sched.extra = kExtra;
-  a.sched.min_len = kExtra + 2;
+  a.sched.extra = p.extra;
+  a.sched.min_len = p.extra + 2;
   a.out.O = static_cast<__nv_bfloat16*>(O);
   a.out.ldo = ldo;
   a.out.lse = lse;
@@ -588,7 +593,8 @@ extern "C" int mq_kv_attention(const void* Q, int64_t ldq, const mq_kv_batch* ba
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool i8 = (cache->flags & MQ_KV_INT8) != 0;
   int e;
-  if (cache->head_dim == 128) e = i8 ? launch_decode<128, true>(a, p.workers, st) : launch_decode<128, false>(a, p.workers, st);
+  if (p.chunk) e = launch_kv_chunk(a, cache->head_dim, i8, p.workers, st);
+  else if (cache->head_dim == 128) e = i8 ? launch_decode<128, true>(a, p.workers, st) : launch_decode<128, false>(a, p.workers, st);
   else e = i8 ? launch_decode<64, true>(a, p.workers, st) : launch_decode<64, false>(a, p.workers, st);
   if (e != MQ_OK) return e;
   return launch_kv_combine(a.sched, a.parts, a.out, p.workers, cache->head_dim, st);

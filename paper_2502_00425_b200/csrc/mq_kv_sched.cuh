@@ -163,4 +163,7 @@ struct KvAttnArgs {
   int32_t* status;
 };
 
+void kv_chunk_shape(int* rows, int* tile, int* extra);
+int launch_kv_chunk(const KvAttnArgs& a, int dim, bool i8, int workers, cudaStream_t st);
+
 }  // namespace mq

@@ -5,7 +5,7 @@ product off by half a step of its type (2^-8 bf16, 2^-11 fp16) and by its own er
 float32 sum of D exact products, at most (D + 8) 2^-23 of the sum of their magnitudes -- plus a few float32 roundings
 of the exponent's argument and of exp2 (2^-19 together); all of them are relative to sum_j p |v|.  An fp16 probability
 below fp16's normal range is off by half its smallest step, 2^-25, whatever its size; as the largest of a row is at least
-2^14 there, that is at most 2^-39 of the softmax's denominator per key, times |v|.
+2^6 there (2^14 in the kernel for few rows), that is at most 2^-31 (2^-39) of the softmax's denominator per key, times |v|.
 """
 import numpy as np
 import pytest
@@ -66,7 +66,8 @@ def _check(pg, q, new, hq, o, lse, perm=None, scale=None, seqs=None, heads=None)
                 ds = (dim + 8) * 2.0 ** -23 * mag[:, None]
                 tol = 2.0 ** -8 * np.abs(ref) + (p_step + 2 * ds + 2.0 ** -19) * abs_pv + 1e-30
                 if pg.int8:
-                    tol = tol + 2.0 ** -39 * np.abs(pg.v[b][:, g]).sum(0)
+                    few = max(new) * group <= 32
+                    tol = tol + 2.0 ** (-39 if few else -31) * np.abs(pg.v[b][:, g]).sum(0)
                 assert np.isfinite(got).all()
                 worst = max(worst, float((np.abs(got - ref) / tol).max(initial=0.0)))
                 got_l = lse[start:start + n, h]
