@@ -63,7 +63,7 @@ kv_decode_kernel(const __grid_constant__ KvAttnArgs p) {
   const int64_t total = prefix[sc.b.n_seq];
   const int64_t share = sched_share(sc, total, gridDim.x);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quad = lane >> 2, t4 = lane & 3;
-  KvRecord rec{0, 0, 0, 0};
+  KvRecord rec{};
   int64_t at = min(total, (int64_t)blockIdx.x * share);
   const int64_t stop = min(total, at + share);
   const uint32_t ring = kv_smem_u32(smem) + (uint32_t)(warp * C::kRing);
@@ -390,44 +390,42 @@ kv_decode_kernel(const __grid_constant__ KvAttnArgs p) {
     if (t0 == 0 && !whole) {
       // the pieces end with the worker whose range holds the unit's last tile
       rec.n_parts = (int)((unit_at + sc.extra + u.tiles - 1) / share) - (int)blockIdx.x + 1;
-      rec.b = u.b; rec.g = u.g; rec.rb = u.rb;
+      rec.begin = u.s.begin; rec.row0 = row0; rec.n_rows = n_rows; rec.g = u.g;
     }
     __syncthreads();   // the join has been read before the next range fills the rings
   }
   if (threadIdx.x == 0) p.parts.rec[blockIdx.x] = rec;
 }
 
-// Joins the pieces of the units that are split: four rows of a record's unit per CTA, and per row four warps that take
-// every fourth piece (a decode step of one sequence has tens of pieces per unit and few units, so the call is as long
-// as this chain of loads).
-constexpr int kJoinRows = 4, kJoinWarps = 4;
-template <int kD>
-__global__ void __launch_bounds__(kJoinRows * kJoinWarps * 32)
-kv_combine_kernel(const __grid_constant__ KvSchedArgs sc, const KvParts parts, const KvOutArgs out) {
-  constexpr int kPer = kD / 32;
-  __shared__ float part[kJoinRows][kJoinWarps][kD + 2];
+// Joins the pieces of the units that are split.  kWarps warps share a row and take every kWarps-th piece: four where
+// a unit has few rows and may have tens of pieces (a decode step of one sequence is as long as this chain of loads),
+// one where it has 128 rows and mostly two pieces.  The record holds all that is needed: one dependent load before
+// the pieces.
+constexpr int kJoinThreads = 256;
+template <int kD, int kWarpsPerRow>
+__global__ void __launch_bounds__(kJoinThreads)
+kv_combine_kernel(const int pitch, const int group, const KvParts parts, const KvOutArgs out) {
+  constexpr int kPer = kD / 32, kRows = kJoinThreads / 32 / kWarpsPerRow;
+  __shared__ float part[kRows][kWarpsPerRow][kD + 2];
   pdl_launch_dependents();
   pdl_wait();
-  const int w = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rr = warp / kJoinWarps, pw = warp % kJoinWarps;
+  const int w = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rr = warp / kWarpsPerRow, pw = warp % kWarpsPerRow;
   const KvRecord rec = parts.rec[w];
-  if (rec.n_parts == 0) return;
-  const KvSeq s = kv_seq(sc.b, sc.page_shift, sc.max_q, rec.b);
-  const int r = blockIdx.y * kJoinRows + rr;
-  const int64_t row = (int64_t)rec.rb * sc.rows + r;
-  const bool live = row < (int64_t)s.n_new * sc.group;
-  if ((int64_t)rec.rb * sc.rows + blockIdx.y * kJoinRows >= (int64_t)s.n_new * sc.group) return;
-  auto slot = [&](int i) { return (int64_t)(i == 0 ? 2 * w + 1 : 2 * (w + i)) * sc.rows + r; };
+  if ((int)blockIdx.y * kRows >= (rec.n_parts ? rec.n_rows : 0)) return;
+  const int r = blockIdx.y * kRows + rr;
+  const bool live = r < rec.n_rows;
+  auto slot = [&](int i) { return (int64_t)(i == 0 ? 2 * w + 1 : 2 * (w + i)) * pitch + r; };
   float m = -INFINITY, l = 0.0f, x[kPer];
 #pragma unroll
   for (int e = 0; e < kPer; ++e) x[e] = 0.0f;
   if (live) {
-    constexpr int kBatch = 8;
-    for (int i0 = pw; i0 < rec.n_parts; i0 += kBatch * kJoinWarps) {
+    constexpr int kBatch = kWarpsPerRow > 1 ? 8 : 3;
+    for (int i0 = pw; i0 < rec.n_parts; i0 += kBatch * kWarpsPerRow) {
       float2 ml[kBatch];
       float v[kBatch][kPer];
 #pragma unroll
       for (int c = 0; c < kBatch; ++c) {
-        const int i = i0 + c * kJoinWarps;
+        const int i = i0 + c * kWarpsPerRow;
         ml[c] = make_float2(-INFINITY, 0.0f);
 #pragma unroll
         for (int e = 0; e < kPer; ++e) v[c][e] = 0.0f;
@@ -463,30 +461,33 @@ kv_combine_kernel(const __grid_constant__ KvSchedArgs sc, const KvParts parts, c
       m = top;
     }
   }
+  if (kWarpsPerRow > 1) {
 #pragma unroll
-  for (int e = 0; e < kPer; ++e) part[rr][pw][lane * kPer + e] = x[e];
-  if (lane == 0) {
-    part[rr][pw][kD] = m;
-    part[rr][pw][kD + 1] = l;
+    for (int e = 0; e < kPer; ++e) part[rr][pw][lane * kPer + e] = x[e];
+    if (lane == 0) {
+      part[rr][pw][kD] = m;
+      part[rr][pw][kD + 1] = l;
+    }
+    __syncthreads();
+    if (pw != 0) return;
+    m = part[rr][0][kD];
+#pragma unroll
+    for (int k = 1; k < kWarpsPerRow; ++k) m = fmaxf(m, part[rr][k][kD]);
+    l = 0.0f;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) x[e] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kWarpsPerRow; ++k) {
+      const float mk = part[rr][k][kD];
+      if (mk == -INFINITY) continue;
+      const float f = kv_exp2(mk - m);
+      l = fmaf(f, part[rr][k][kD + 1], l);
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) x[e] = fmaf(f, part[rr][k][lane * kPer + e], x[e]);
+    }
   }
-  __syncthreads();
-  if (pw != 0 || !live) return;
-  m = part[rr][0][kD];
-#pragma unroll
-  for (int k = 1; k < kJoinWarps; ++k) m = fmaxf(m, part[rr][k][kD]);
-  l = 0.0f;
-#pragma unroll
-  for (int e = 0; e < kPer; ++e) x[e] = 0.0f;
-#pragma unroll
-  for (int k = 0; k < kJoinWarps; ++k) {
-    const float mk = part[rr][k][kD];
-    if (mk == -INFINITY) continue;
-    const float f = kv_exp2(mk - m);
-    l = fmaf(f, part[rr][k][kD + 1], l);
-#pragma unroll
-    for (int e = 0; e < kPer; ++e) x[e] = fmaf(f, part[rr][k][lane * kPer + e], x[e]);
-  }
-  const int tok = s.begin + (int)(row / sc.group), head = rec.g * sc.group + (int)(row % sc.group);
+  if (!live) return;
+  const int tok = rec.begin + (rec.row0 + r) / group, head = rec.g * group + (rec.row0 + r) % group;
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   __nv_bfloat16* dst = out.O + (int64_t)tok * out.ldo + (int64_t)head * kD + lane * kPer;
   if (kPer == 4)
@@ -513,13 +514,14 @@ int launch_decode(const KvAttnArgs& a, int workers, cudaStream_t st) {
 constexpr int kFewRows = 32;
 struct Plan {
   bool chunk;
-  int workers, rows, tile, extra;
+  int workers, rows, pitch, tile, extra;
 };
 Plan attn_plan(const mq_kv_batch* b, const mq_kv_cache* c, int group) {
   Plan p{};
-  p.chunk = (int64_t)b->max_q * group > kFewRows && c->n_pages > 0;
-  if (p.chunk) kv_chunk_shape(&p.rows, &p.tile, &p.extra);
-  else p.rows = kM, p.tile = kTile, p.extra = kExtra;
+  // (a token's heads have to fit into a block of that kernel, and its maps need a page)
+  p.chunk = (int64_t)b->max_q * group > kFewRows && group <= 128 && c->n_pages > 0;
+  if (p.chunk) kv_chunk_shape(group, &p.rows, &p.pitch, &p.tile, &p.extra);
+  else p.rows = p.pitch = kM, p.tile = kTile, p.extra = kExtra;
   const int64_t blocks = ((int64_t)b->max_q * group + p.rows - 1) / p.rows;
   const int64_t tiles = (((int64_t)b->max_pages * c->page_size) + p.tile - 1) / p.tile;
   const int64_t most = (int64_t)b->n_seq * c->n_kv_heads * blocks * (tiles > 0 ? tiles : 1);
@@ -540,10 +542,18 @@ int check_attention(const mq_kv_batch* batch, const mq_kv_cache* cache, int32_t 
 
 }  // namespace
 
+namespace {
+template <int kD, int kW>
+cudaError_t launch_join(const KvSchedArgs& a, const KvParts& parts, const KvOutArgs& out, int workers, cudaStream_t st) {
+  return launch_pdl(kv_combine_kernel<kD, kW>, dim3((unsigned)workers, (unsigned)(a.pitch * kW * 32 / kJoinThreads)), dim3(kJoinThreads), 0, st,
+                    a.pitch, a.group, parts, out);
+}
+}  // namespace
+
 int launch_kv_combine(const KvSchedArgs& a, const KvParts& parts, const KvOutArgs& out, int workers, int dim, cudaStream_t st) {
-  const dim3 grid((unsigned)workers, (unsigned)(a.rows / kJoinRows)), block(kJoinRows * kJoinWarps * 32);
-  const cudaError_t e = dim == 128 ? launch_pdl(kv_combine_kernel<128>, grid, block, 0, st, a, parts, out)
-                                   : launch_pdl(kv_combine_kernel<64>, grid, block, 0, st, a, parts, out);
+  const bool few = a.pitch == kM;
+  const cudaError_t e = dim == 128 ? (few ? launch_join<128, 4>(a, parts, out, workers, st) : launch_join<128, 1>(a, parts, out, workers, st))
+                                   : (few ? launch_join<64, 4>(a, parts, out, workers, st) : launch_join<64, 1>(a, parts, out, workers, st));
   if (e != cudaSuccess) return cuda_status(e);
   return cuda_status(cudaGetLastError());
 }
@@ -557,7 +567,7 @@ extern "C" size_t mq_kv_attention_workspace_bytes(const mq_kv_batch* batch, cons
   KvView cv;
   if (check_attention(batch, cache, n_q_heads, &bv, &cv) != MQ_OK) return 0;
   const Plan p = attn_plan(batch, cache, n_q_heads / cache->n_kv_heads);
-  return kStatusBytes + kv_parts_bytes(p.workers, p.rows, cache->head_dim);
+  return kStatusBytes + kv_parts_bytes(p.workers, p.pitch, cache->head_dim);
 }
 
 extern "C" int mq_kv_attention(const void* Q, int64_t ldq, const mq_kv_batch* batch, const mq_kv_cache* cache, int32_t n_q_heads,
@@ -572,7 +582,7 @@ extern "C" int mq_kv_attention(const void* Q, int64_t ldq, const mq_kv_batch* ba
   if (!Q || !O || !ws) return MQ_ERR_INVALID_ARG;
   if (!kv_aligned16(Q) || !kv_aligned16(O) || ldq % 8 || ldo % 8 || (reinterpret_cast<uintptr_t>(ws) & 255u)) return MQ_ERR_ALIGNMENT;
   const Plan p = attn_plan(batch, cache, n_q_heads / cache->n_kv_heads);
-  if (ws_bytes < kStatusBytes + kv_parts_bytes(p.workers, p.rows, cache->head_dim)) return MQ_ERR_WORKSPACE;
+  if (ws_bytes < kStatusBytes + kv_parts_bytes(p.workers, p.pitch, cache->head_dim)) return MQ_ERR_WORKSPACE;
   a.Q = static_cast<const uint8_t*>(Q);
   a.ldq = ldq * 2;
   a.sched.page_shift = a.cache.page_shift;
@@ -580,6 +590,7 @@ extern "C" int mq_kv_attention(const void* Q, int64_t ldq, const mq_kv_batch* ba
   a.sched.group = n_q_heads / cache->n_kv_heads;
   a.sched.n_kv = cache->n_kv_heads;
   a.sched.rows = p.rows;
+  a.sched.pitch = p.pitch;
   a.sched.tile = p.tile;
   a.sched.extra = p.extra;
   a.sched.min_len = p.extra + 2;
@@ -587,7 +598,7 @@ extern "C" int mq_kv_attention(const void* Q, int64_t ldq, const mq_kv_batch* ba
   a.out.ldo = ldo;
   a.out.lse = lse;
   a.out.n_q_heads = n_q_heads;
-  a.parts = kv_parts(static_cast<uint8_t*>(ws) + kStatusBytes, p.workers, p.rows);
+  a.parts = kv_parts(static_cast<uint8_t*>(ws) + kStatusBytes, p.workers, p.pitch);
   a.scale = scale;
   a.status = static_cast<int32_t*>(ws);
   cudaStream_t st = static_cast<cudaStream_t>(stream);

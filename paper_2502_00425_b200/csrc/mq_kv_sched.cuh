@@ -1,6 +1,6 @@
 // How the attention kernels over a paged cache divide their work (mq_kv_attn.cu, mq_kv_chunk.cu).
 //
-// A UNIT is (sequence, key/value head, block of kM query rows); a query row is (token, query head of the group), token
+// A UNIT is (sequence, key/value head, block of query rows); a query row is (token, query head of the group), token
 // major, so that the heads of a group share every key tile.  A unit walks its keys in tiles.  All units form one line, a
 // unit as long as its tiles plus a fixed length for what it costs besides them (queries, filling the pipeline, writing
 // the result), and the line is cut into equal contiguous ranges, one per worker (CTA): ragged batches, one long
@@ -17,7 +17,8 @@ namespace mq {
 struct KvSchedArgs {
   KvBatchView b;
   int page_shift, max_q, group, n_kv;
-  int rows;        // kM: query rows of a unit
+  int rows;        // query rows of a unit
+  int pitch;       // rows between the slots of partial results (at least `rows`)
   int tile;        // keys of a tile
   int extra;       // a unit's cost besides its tiles, in tiles
   int min_len;     // a worker's range is at least this long (fewer workers for little work)
@@ -118,25 +119,29 @@ __device__ __forceinline__ int64_t sched_share(const KvSchedArgs& a, int64_t tot
 // ---- partial results -----------------------------------------------------------------------------------
 // Worker w has two slots: 2 w for a range's first piece when it starts inside a unit, 2 w + 1 for a piece that starts
 // with its unit and does not reach its end.  Record w names the unit whose first piece is in slot 2 w + 1.
-struct KvRecord {
+struct __align__(16) KvRecord {
   int n_parts;   // 0: this worker left no first piece; else the pieces are slots 2 w + 1, 2 (w + 1), 2 (w + 2), ...
-  int b, g, rb;
+  int begin;     // first row of the sequence in Q, O and lse
+  int row0;      // the unit's first query row (token x group + head of the group) and how many it has
+  int n_rows;
+  int g;
+  int pad[3];
 };
 struct KvParts {
   KvRecord* rec;   // [workers]
-  float2* ml;      // [2 workers][rows]: maximum (log2 units), sum
-  float* o;        // [2 workers][rows][D]
+  float2* ml;      // [2 workers][pitch]: exponent reference (log2 units), sum
+  float* o;        // [2 workers][pitch][D]
 };
-inline size_t kv_parts_bytes(int workers, int rows, int dim) {
-  return align_up((size_t)workers * sizeof(KvRecord), 256) + align_up((size_t)workers * 2 * rows * sizeof(float2), 256) +
-         (size_t)workers * 2 * rows * dim * sizeof(float);
+inline size_t kv_parts_bytes(int workers, int pitch, int dim) {
+  return align_up((size_t)workers * sizeof(KvRecord), 256) + align_up((size_t)workers * 2 * pitch * sizeof(float2), 256) +
+         (size_t)workers * 2 * pitch * dim * sizeof(float);
 }
-inline KvParts kv_parts(uint8_t* base, int workers, int rows) {
+inline KvParts kv_parts(uint8_t* base, int workers, int pitch) {
   KvParts p;
   p.rec = reinterpret_cast<KvRecord*>(base);
   base += align_up((size_t)workers * sizeof(KvRecord), 256);
   p.ml = reinterpret_cast<float2*>(base);
-  base += align_up((size_t)workers * 2 * rows * sizeof(float2), 256);
+  base += align_up((size_t)workers * 2 * pitch * sizeof(float2), 256);
   p.o = reinterpret_cast<float*>(base);
   return p;
 }
@@ -148,7 +153,7 @@ struct KvOutArgs {
   int n_q_heads;
 };
 
-// joins the pieces of split units; grid `workers` x (rows / 4)
+// joins the pieces of split units
 int launch_kv_combine(const KvSchedArgs& a, const KvParts& parts, const KvOutArgs& out, int workers, int dim, cudaStream_t st);
 
 // the tensor-memory form for long chunks (mq_kv_chunk.cu)
@@ -163,7 +168,7 @@ struct KvAttnArgs {
   int32_t* status;
 };
 
-void kv_chunk_shape(int* rows, int* tile, int* extra);
+void kv_chunk_shape(int group, int* rows, int* pitch, int* tile, int* extra);
 int launch_kv_chunk(const KvAttnArgs& a, int dim, bool i8, int workers, cudaStream_t st);
 
 }  // namespace mq
