@@ -510,19 +510,9 @@ class KVCache:
         empty = n_pages == 0
         self.c = mq_kv_cache(None if empty else _addr(K), None if empty else _addr(V), pg, head, slot, n_pages, page, n_kv, dim,
                              MQ_KV_INT8 if int8 else 0, _addr(k_scale), _addr(v_scale))
-        self.device = K.device
-
-    @property
-    def page_size(self):
-        return self.c.page_size
-
-    @property
-    def head_dim(self):
-        return self.c.head_dim
-
-    @property
-    def n_kv_heads(self):
-        return self.c.n_kv_heads
+        self.device, self.index = K.device, K.get_device()
+        self.ref = C.byref(self.c)
+        self.page_size, self.head_dim, self.n_kv_heads = page, dim, n_kv
 
 
 def _addr(t: Optional[torch.Tensor]):
@@ -534,28 +524,55 @@ def _addr(t: Optional[torch.Tensor]):
     return t.data_ptr()
 
 
-def _kv_call(device, fn, where, *args):
-    """Runs one library call on the current stream of `device`, which is made current for it if it is not."""
-    if device.index is not None and device.index != torch.cuda.current_device():
-        with torch.cuda.device(device):
-            _check(fn(*args, torch.cuda.current_stream().cuda_stream), where)
+# The cache calls are made once per layer and token, so their wrappers are written for few Python steps: one look at a
+# tensor's device gives its address or the refusal, the stream comes as a bare handle, types are compared once each.
+_BF16, _F32, _I32, _I64 = torch.bfloat16, torch.float32, torch.int32, torch.int64
+
+
+def _at(t: torch.Tensor, device: int) -> int:
+    """Device address of t, which must live on CUDA device number `device`."""
+    if t.get_device() != device:
+        if not t.is_cuda:
+            raise ValueError("tensor must live on a CUDA device (the library has no CPU path)")
+        raise ValueError(f"tensor on {t.device}, expected cuda:{device}")
+    return t.data_ptr()
+
+
+def _opt(t: Optional[torch.Tensor], device: int):
+    return None if t is None else _at(t, device)
+
+
+def _kv_call(device: int, fn, where, *args):
+    """Runs one library call on the current stream of CUDA device number `device`, made current for it if it is not."""
+    if device == torch.cuda.current_device():
+        status = fn(*args, torch._C._cuda_getCurrentRawStream(device))
     else:
-        _check(fn(*args, torch.cuda.current_stream().cuda_stream), where)
+        with torch.cuda.device(device):
+            status = fn(*args, torch._C._cuda_getCurrentRawStream(device))
+    if status != MQ_OK:
+        raise MqError(status, where)
 
 
-def _same_device(device, *tensors):
-    for t in tensors:
-        if t is not None and t.device != device:
-            raise ValueError(f"tensor on {t.device}, the cache is on {device}")
+def _pitch(t: torch.Tensor) -> int:
+    """Leading dimension of a row-major matrix (a single row or column may carry any stride in torch)."""
+    rows, cols = t.shape
+    pitch, unit = t.stride()
+    if unit != 1 and cols > 1:
+        raise ValueError("rows must be contiguous")
+    return pitch if rows > 1 else max(pitch, cols)
 
 
-def _kv_batch(cu_q, kv_len, page_table, total_q, max_q, perm):
-    assert cu_q.dtype == torch.int32 and kv_len.dtype == torch.int32 and page_table.dtype == torch.int32
-    n_seq = kv_len.numel()
-    assert cu_q.numel() == n_seq + 1 and page_table.dim() == 2 and page_table.shape[0] == n_seq
-    assert cu_q.is_contiguous() and kv_len.is_contiguous() and page_table.is_contiguous()
-    assert perm is None or (perm.dtype == torch.int32 and perm.numel() == total_q and perm.is_contiguous())
-    return mq_kv_batch(n_seq, total_q, max_q, page_table.shape[1], _addr(cu_q), _addr(kv_len), _addr(page_table), _addr(perm))
+def _kv_batch(cu_q, kv_len, page_table, total_q, max_q, perm, device):
+    n_seq, width = page_table.shape
+    if not (cu_q.dtype == kv_len.dtype == page_table.dtype == _I32 and (perm is None or perm.dtype == _I32)):
+        raise ValueError("cu_q, kv_len, page_table and perm are int32")
+    if kv_len.numel() != n_seq or cu_q.numel() != n_seq + 1 or (perm is not None and perm.numel() != total_q):
+        raise ValueError("cu_q [n_seq + 1], kv_len [n_seq], page_table [n_seq, max_pages], perm [rows of q]")
+    if not (cu_q.is_contiguous() and kv_len.is_contiguous() and page_table.is_contiguous() and
+            (perm is None or perm.is_contiguous())):
+        raise ValueError("cu_q, kv_len, page_table and perm must be contiguous")
+    return mq_kv_batch(n_seq, total_q, max_q, width, _at(cu_q, device), _at(kv_len, device), _at(page_table, device),
+                       _opt(perm, device))
 
 
 def mq_qk_norm_rope(q, k, pos, n_q_heads, n_kv_heads, q_out, k_out=None, gain_q=None, gain_k=None, eps=1e-6, base=10000.0,
@@ -564,22 +581,28 @@ def mq_qk_norm_rope(q, k, pos, n_q_heads, n_kv_heads, q_out, k_out=None, gain_q=
     (int64 [T], page * page_size + slot; negative: not stored).  See include/mq.h."""
     T, width = q.shape
     head_dim = width // n_q_heads
-    assert q.dtype == torch.bfloat16 and k.dtype == torch.bfloat16 and q_out.dtype == torch.bfloat16
-    assert width == n_q_heads * head_dim and k.shape == (T, n_kv_heads * head_dim) and q_out.shape == q.shape
-    assert k_out is None or (k_out.dtype == torch.bfloat16 and k_out.shape == k.shape)
-    assert pos.dtype == torch.int32 and pos.shape == (T,) and pos.is_contiguous()
+    kv = (T, n_kv_heads * head_dim)
+    if not (q.dtype == k.dtype == q_out.dtype == _BF16 and pos.dtype == _I32):
+        raise ValueError("q, k and q_out are bf16, pos is int32")
+    if width != n_q_heads * head_dim or k.shape != kv or q_out.shape != q.shape or pos.numel() != T or not pos.is_contiguous():
+        raise ValueError("q, q_out [T, n_q_heads * head_dim], k [T, n_kv_heads * head_dim], pos [T]")
+    if k_out is not None and (k_out.dtype != _BF16 or k_out.shape != kv):
+        raise ValueError("k_out is bf16 of k's shape")
     for gain in (gain_q, gain_k):
-        assert gain is None or (gain.dtype == torch.float32 and gain.shape == (head_dim,) and gain.is_contiguous())
-    if cache is not None:
-        assert v.dtype == torch.bfloat16 and v.shape == k.shape
-        assert slots.dtype == torch.int64 and slots.shape == (T,) and slots.is_contiguous()
+        if gain is not None and (gain.dtype != _F32 or gain.numel() != head_dim or not gain.is_contiguous()):
+            raise ValueError("gains are float32 [head_dim]")
+    d = q.get_device()
+    if cache is None:
+        pv, ldv, pc, ps = None, 0, None, None
     else:
-        v = slots = None
-    _same_device(q.device, k, pos, q_out, k_out, gain_q, gain_k, v, slots, None if cache is None else cache.K)
-    _kv_call(q.device, load().mq_qk_norm_rope, "mq_qk_norm_rope", _addr(q), _ld(q), _addr(k), _ld(k), _addr(v),
-             _ld(v) if v is not None else 0, T, n_q_heads, n_kv_heads, head_dim, _addr(gain_q), _addr(gain_k), float(eps),
-             _addr(pos), float(base), MQ_ROPE_HALF if half else 0, _addr(q_out), _ld(q_out), _addr(k_out),
-             _ld(k_out) if k_out is not None else 0, None if cache is None else C.byref(cache.c), _addr(slots))
+        if v.dtype != _BF16 or v.shape != kv or slots.dtype != _I64 or slots.numel() != T or not slots.is_contiguous():
+            raise ValueError("v is bf16 of k's shape, slots int64 [T]")
+        if cache.index != d:
+            raise ValueError(f"the cache is on cuda:{cache.index}, q on {q.device}")
+        pv, ldv, pc, ps = _at(v, d), _pitch(v), cache.ref, _at(slots, d)
+    _kv_call(d, load().mq_qk_norm_rope, "mq_qk_norm_rope", _at(q, d), _pitch(q), _at(k, d), _pitch(k), pv, ldv, T, n_q_heads,
+             n_kv_heads, head_dim, _opt(gain_q, d), _opt(gain_k, d), eps, _at(pos, d), base, MQ_ROPE_HALF if half else 0,
+             _at(q_out, d), _pitch(q_out), _opt(k_out, d), 0 if k_out is None else _pitch(k_out), pc, ps)
 
 
 def mq_kv_attention_workspace_bytes(n_seq, total_q, max_q, max_pages, n_q_heads, cache: KVCache) -> int:
@@ -600,54 +623,61 @@ def new_kv_attention_workspace(n_seq, total_q, max_q, max_pages, n_q_heads, cach
 
 def mq_kv_attention(q, cu_q, kv_len, page_table, cache: KVCache, n_q_heads, max_q, o, ws, lse=None, perm=None, scale=None):
     """Attention of the new rows q over the paged cache; see include/mq.h.  scale: 1 / sqrt(head_dim) if not given."""
-    assert q.dtype == torch.bfloat16 and o.dtype == torch.bfloat16 and q.shape == o.shape
-    total_q = q.shape[0]
-    assert q.shape[1] == n_q_heads * cache.head_dim
-    assert lse is None or (lse.dtype == torch.float32 and lse.shape == (total_q, n_q_heads) and lse.is_contiguous())
-    _same_device(cache.device, q, cu_q, kv_len, page_table, o, ws, lse, perm)
-    b = _kv_batch(cu_q, kv_len, page_table, total_q, max_q, perm)
-    scale = float(scale) if scale is not None else cache.head_dim ** -0.5
-    _kv_call(cache.device, load().mq_kv_attention, "mq_kv_attention", _addr(q), _ld(q), C.byref(b), C.byref(cache.c), n_q_heads,
-             scale, _addr(o), _ld(o), _addr(lse), _addr(ws), ws.numel())
+    total_q, width = q.shape
+    if not (q.dtype == o.dtype == _BF16) or o.shape != q.shape or width != n_q_heads * cache.head_dim:
+        raise ValueError("q and o are bf16 [rows, n_q_heads * head_dim]")
+    if lse is not None and (lse.dtype != _F32 or lse.shape != (total_q, n_q_heads) or not lse.is_contiguous()):
+        raise ValueError("lse is float32 [rows, n_q_heads]")
+    d = cache.index
+    b = _kv_batch(cu_q, kv_len, page_table, total_q, max_q, perm, d)
+    _kv_call(d, load().mq_kv_attention, "mq_kv_attention", _at(q, d), _pitch(q), C.byref(b), cache.ref, n_q_heads,
+             cache.head_dim ** -0.5 if scale is None else scale, _at(o, d), _pitch(o), _opt(lse, d), _at(ws, d), ws.numel())
 
 
 def _weight_strides(w, n_seq, n_kv_heads):
-    assert w.dtype == torch.float32 and w.dim() == 3 and w.shape[:2] == (n_seq, n_kv_heads) and (w.stride(2) == 1 or w.shape[2] <= 1)
+    if w.dtype != _F32 or w.dim() != 3 or w.shape[0] != n_seq or w.shape[1] != n_kv_heads or (w.stride(2) != 1 and w.shape[2] > 1):
+        raise ValueError("weights are float32 [n_seq, n_kv_heads, keys] with contiguous rows")
     return w.stride(0), w.stride(1)
 
 
 def mq_kv_weights(q, cu_q, kv_len, page_table, cache: KVCache, n_q_heads, max_q, lse, w_out, w_in=None, perm=None, scale=None):
     """Adds the softmax weight every key receives from the rows q to w_in (None: zeros) and writes w_out
     (float32 [n_seq, n_kv_heads, >= longest kv_len]; may be w_in).  lse: mq_kv_attention's output for the same rows."""
-    assert q.dtype == torch.bfloat16 and q.shape[1] == n_q_heads * cache.head_dim
-    total_q = q.shape[0]
-    assert lse.dtype == torch.float32 and lse.shape == (total_q, n_q_heads) and lse.is_contiguous()
-    _same_device(cache.device, q, cu_q, kv_len, page_table, lse, w_out, w_in, perm)
-    b = _kv_batch(cu_q, kv_len, page_table, total_q, max_q, perm)
+    total_q, width = q.shape
+    if q.dtype != _BF16 or width != n_q_heads * cache.head_dim:
+        raise ValueError("q is bf16 [rows, n_q_heads * head_dim]")
+    if lse.dtype != _F32 or lse.shape != (total_q, n_q_heads) or not lse.is_contiguous():
+        raise ValueError("lse is float32 [rows, n_q_heads]")
+    d = cache.index
+    b = _kv_batch(cu_q, kv_len, page_table, total_q, max_q, perm, d)
     strides = _weight_strides(w_out, b.n_seq, cache.n_kv_heads)
     if w_in is not None and (w_in.shape != w_out.shape or _weight_strides(w_in, b.n_seq, cache.n_kv_heads) != strides):
         raise ValueError("w_in and w_out must have the same shape and strides")
-    scale = float(scale) if scale is not None else cache.head_dim ** -0.5
-    _kv_call(cache.device, load().mq_kv_weights, "mq_kv_weights", _addr(q), _ld(q), C.byref(b), C.byref(cache.c), n_q_heads, scale,
-             _addr(lse), _addr(w_in), _addr(w_out), strides[0], strides[1])
+    _kv_call(d, load().mq_kv_weights, "mq_kv_weights", _at(q, d), _pitch(q), C.byref(b), cache.ref, n_q_heads,
+             cache.head_dim ** -0.5 if scale is None else scale, _at(lse, d), _opt(w_in, d), _at(w_out, d), strides[0], strides[1])
 
 
 def mq_kv_evict(cache: KVCache, page_table, kv_len, w, budget, n_first, n_last, dst: KVCache, dst_table, kept, new_len, w_out=None):
     """Cuts every sequence to `budget` keys per key/value head by the weights w and copies the kept rows to dst_table's pages
     of `dst` (see include/mq.h).  kept int32 [n_seq, n_kv_heads, budget], new_len int32 [n_seq], w_out float32 like kept."""
-    n_seq = kv_len.numel()
-    assert kv_len.dtype == torch.int32 and page_table.dtype == torch.int32 and dst_table.dtype == torch.int32
-    assert page_table.shape[0] == n_seq and dst_table.shape[0] == n_seq
-    assert page_table.is_contiguous() and dst_table.is_contiguous() and kv_len.is_contiguous()
+    n_seq, width = page_table.shape
+    d = cache.index
+    if not (kv_len.dtype == page_table.dtype == dst_table.dtype == kept.dtype == new_len.dtype == _I32):
+        raise ValueError("page tables, lengths and kept indices are int32")
     shape = (n_seq, cache.n_kv_heads, budget)
-    assert kept.dtype == torch.int32 and kept.shape == shape and kept.is_contiguous()
-    assert new_len.dtype == torch.int32 and new_len.shape == (n_seq,) and new_len.is_contiguous()
-    assert w_out is None or (w_out.dtype == torch.float32 and w_out.shape == shape and w_out.is_contiguous())
-    _same_device(cache.device, page_table, kv_len, w, dst.K, dst_table, kept, new_len, w_out)
+    if kv_len.numel() != n_seq or new_len.numel() != n_seq or dst_table.shape[0] != n_seq or kept.shape != shape:
+        raise ValueError("kv_len, new_len [n_seq], dst_table [n_seq, pages], kept [n_seq, n_kv_heads, budget]")
+    if w_out is not None and (w_out.dtype != _F32 or w_out.shape != shape or not w_out.is_contiguous()):
+        raise ValueError("w_out is float32 [n_seq, n_kv_heads, budget]")
+    if not (page_table.is_contiguous() and dst_table.is_contiguous() and kv_len.is_contiguous() and kept.is_contiguous() and
+            new_len.is_contiguous()):
+        raise ValueError("page tables, lengths and kept indices must be contiguous")
+    if dst.index != d:
+        raise ValueError(f"the caches are on cuda:{d} and cuda:{dst.index}")
     strides = _weight_strides(w, n_seq, cache.n_kv_heads)
-    _kv_call(cache.device, load().mq_kv_evict, "mq_kv_evict", C.byref(cache.c), _addr(page_table), page_table.shape[1], _addr(kv_len),
-             n_seq, _addr(w), strides[0], strides[1], budget, n_first, n_last, C.byref(dst.c), _addr(dst_table), dst_table.shape[1],
-             _addr(kept), _addr(new_len), _addr(w_out))
+    _kv_call(d, load().mq_kv_evict, "mq_kv_evict", cache.ref, _at(page_table, d), width, _at(kv_len, d), n_seq, _at(w, d),
+             strides[0], strides[1], budget, n_first, n_last, dst.ref, _at(dst_table, d), dst_table.shape[1], _at(kept, d),
+             _at(new_len, d), _opt(w_out, d))
 
 
 def mq_last_device_status(ws):

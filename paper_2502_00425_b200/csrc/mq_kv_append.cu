@@ -193,8 +193,10 @@ extern "C" int mq_qk_norm_rope(const void* Q, int64_t ldq, const void* K, int64_
   p.T = T; p.n_q = n_q_heads; p.n_kv = n_kv_heads;
   p.gain_q = gain_q; p.gain_k = gain_k; p.eps = eps; p.pos = pos; p.slots = slots;
   p.has_cache = cache != nullptr;
-  for (int i = 0; i < head_dim / 2; ++i)
-    p.turns[i] = std::pow((double)base, -2.0 * i / head_dim) / 6.283185307179586476925286766559;
+  // powers of one ratio, in long double: 64 roundings of 2^-64 (one pow instead of 64, which took longer than the launch)
+  const long double ratio = powl((long double)base, -2.0L / head_dim);
+  long double turn = 1.0L / 6.283185307179586476925286766559L;
+  for (int i = 0; i < head_dim / 2; ++i, turn *= ratio) p.turns[i] = (double)turn;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool half = flags & MQ_ROPE_HALF, i8 = cache && (cache->flags & MQ_KV_INT8);
   if (head_dim == 128) {
