@@ -543,11 +543,12 @@ int mq_kv_attention(const void* Q, int64_t ldq, const mq_kv_batch* batch, const 
  * for j < kv_len[b]; other entries of W_out are left as they were.  lse is mq_kv_attention's output for the same
  * call.  W_in NULL counts as zeros; W_in == W_out accumulates in place.  float32 throughout, and every sum is
  * taken in a fixed order (no atomics).  w_seq_stride, w_head_stride: elements between sequences and heads
- * (w_head_stride at least the longest kv_len; for both arrays).
+ * (w_head_stride at least the longest kv_len; for both arrays).  status: optional device int32[2], zeroed by the caller:
+ * MQ_ERR_INVALID_ARG for a page number outside the cache, MQ_ERR_TIMEOUT and the wait's site if a bounded wait expired.
  */
 int mq_kv_weights(const void* Q, int64_t ldq, const mq_kv_batch* batch, const mq_kv_cache* cache, int32_t n_q_heads,
                   float scale, const float* lse, const float* W_in, float* W_out, int64_t w_seq_stride,
-                  int64_t w_head_stride, void* stream);
+                  int64_t w_head_stride, int32_t* status, void* stream);
 
 /*
  * Eviction: cuts every sequence to at most `budget` keys per key/value head and copies them, in their order, to fresh

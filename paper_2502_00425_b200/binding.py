@@ -102,7 +102,7 @@ def load(build_if_missing: bool = False):
                                       vp, i64, kvcp, vp, vp]),
         "mq_kv_attention_workspace_bytes": (sz, [kvbp, kvcp, i32]),
         "mq_kv_attention": (C.c_int, [vp, i64, kvbp, kvcp, i32, f32, vp, i64, vp, vp, sz, vp]),
-        "mq_kv_weights": (C.c_int, [vp, i64, kvbp, kvcp, i32, f32, vp, vp, vp, i64, i64, vp]),
+        "mq_kv_weights": (C.c_int, [vp, i64, kvbp, kvcp, i32, f32, vp, vp, vp, i64, i64, vp, vp]),
         "mq_kv_evict": (C.c_int, [kvcp, vp, i32, vp, i32, vp, i64, i64, i32, i32, i32, kvcp, vp, i32, vp, vp, vp, vp]),
         "mq_repack_w4": (C.c_int, [vp, i32, i32, vp, vp]),
         "mq_unpack_w4": (C.c_int, [vp, vp, i32, i32, vp, i64, vp]),
@@ -640,21 +640,26 @@ def _weight_strides(w, n_seq, n_kv_heads):
     return w.stride(0), w.stride(1)
 
 
-def mq_kv_weights(q, cu_q, kv_len, page_table, cache: KVCache, n_q_heads, max_q, lse, w_out, w_in=None, perm=None, scale=None):
+def mq_kv_weights(q, cu_q, kv_len, page_table, cache: KVCache, n_q_heads, max_q, lse, w_out, w_in=None, perm=None, scale=None,
+                  status=None):
     """Adds the softmax weight every key receives from the rows q to w_in (None: zeros) and writes w_out
-    (float32 [n_seq, n_kv_heads, >= longest kv_len]; may be w_in).  lse: mq_kv_attention's output for the same rows."""
+    (float32 [n_seq, n_kv_heads, >= longest kv_len]; may be w_in).  lse: mq_kv_attention's output for the same rows.
+    status: zeroed int32[2] or None."""
     total_q, width = q.shape
     if q.dtype != _BF16 or width != n_q_heads * cache.head_dim:
         raise ValueError("q is bf16 [rows, n_q_heads * head_dim]")
     if lse.dtype != _F32 or lse.shape != (total_q, n_q_heads) or not lse.is_contiguous():
         raise ValueError("lse is float32 [rows, n_q_heads]")
+    if status is not None and (status.dtype != _I32 or status.numel() < 2):
+        raise ValueError("status is int32[2]")
     d = cache.index
     b = _kv_batch(cu_q, kv_len, page_table, total_q, max_q, perm, d)
     strides = _weight_strides(w_out, b.n_seq, cache.n_kv_heads)
     if w_in is not None and (w_in.shape != w_out.shape or _weight_strides(w_in, b.n_seq, cache.n_kv_heads) != strides):
         raise ValueError("w_in and w_out must have the same shape and strides")
     _kv_call(d, load().mq_kv_weights, "mq_kv_weights", _at(q, d), _pitch(q), C.byref(b), cache.ref, n_q_heads,
-             cache.head_dim ** -0.5 if scale is None else scale, _at(lse, d), _opt(w_in, d), _at(w_out, d), strides[0], strides[1])
+             cache.head_dim ** -0.5 if scale is None else scale, _at(lse, d), _opt(w_in, d), _at(w_out, d), strides[0], strides[1],
+             _opt(status, d))
 
 
 def mq_kv_evict(cache: KVCache, page_table, kv_len, w, budget, n_first, n_last, dst: KVCache, dst_table, kept, new_len, w_out=None):

@@ -11,7 +11,7 @@ ROOT = os.path.dirname(PKG_DIR)
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libmq.so")
 SOURCES = ["mq_api.cu", "mq_fwht_quant.cu", "mq_pack.cu", "mq_aifs.cu", "mq_gemm.cu", "mq_noalloc.cu", "mq_rms.cu", "mq_gemv.cu", "mq_dynquant.cu", "mq_probe.cu", "mq_kron.cu", "mq_glue.cu", "mq_attn.cu", "mq_kv_append.cu",
-           "mq_kv_attn.cu", "mq_kv_chunk.cu", "mq_kv_weights.cu", "mq_kv_evict.cu"]
+           "mq_kv_attn.cu", "mq_kv_chunk.cu", "mq_kv_weights.cu", "mq_kv_weights_chunk.cu", "mq_kv_evict.cu"]
 
 
 def _nvcc() -> str:

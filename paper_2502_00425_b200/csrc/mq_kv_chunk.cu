@@ -23,7 +23,7 @@
 #include <cuda.h>
 
 #include "mq_kv_sched.cuh"
-#include "mq_sm100.cuh"
+#include "mq_kv_tma.cuh"
 
 namespace mq {
 namespace {
@@ -69,16 +69,6 @@ struct ChunkCfg {
   static constexpr int kSmem = 1024 + (2 + 2 * kStages) * kTileBytes + (int)sizeof(ChunkBarriers) + kRing * (int)sizeof(Piece) + 8 * 64 * 4 + 16 * 8;
 };
 
-__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
-      ::"r"(dst), "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z) : "memory");
-}
-__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, uint64_t* bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
-      ::"r"(dst), "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
-}
 // B operand whose N (64 channels per block, 128-byte swizzle) is contiguous: blocks `block_bytes` apart, 8-key groups 1024 apart
 __device__ __forceinline__ uint64_t desc_n_major(uint32_t addr, uint32_t block_bytes) {
   return (uint64_t)((addr >> 4) & 0x3FFFu) | ((uint64_t)(block_bytes >> 4) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
@@ -658,43 +648,6 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
   }
 }
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_fn() {
-  static EncodeTiledFn fn = [] {
-    void* ptr = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ptr, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess)
-      ptr = nullptr;
-    return reinterpret_cast<EncodeTiledFn>(ptr);
-  }();
-  return fn;
-}
-
-bool encode_bf16(CUtensorMap* map, int rank, const void* base, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
-  const cuuint32_t es[4] = {1, 1, 1, 1};
-  return encode_fn() && encode_fn()(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(base), dims, strides, box, es,
-                                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-// The pages as a map [page][head][slot][channel], read in boxes of 64 channels x (a page's slots, at most 128)
-bool encode_pages(CUtensorMap* map, const uint8_t* base, const KvView& c, int dim) {
-  const int page = 1 << c.page_shift;
-  const cuuint64_t dims[4] = {(cuuint64_t)dim, (cuuint64_t)page, (cuuint64_t)c.n_kv_heads, (cuuint64_t)c.n_pages};
-  const cuuint64_t strides[3] = {(cuuint64_t)c.slot_stride, (cuuint64_t)c.head_stride, (cuuint64_t)c.page_stride};
-  const cuuint32_t box[4] = {64, (cuuint32_t)(page < kTile ? page : kTile), 1, 1};
-  return encode_bf16(map, 4, base, dims, strides, box);
-}
-// The queries as a map [token][head][channel], read in boxes of 64 channels x the heads of a group x a block's tokens
-bool encode_queries(CUtensorMap* map, const KvAttnArgs& a, int dim) {
-  const cuuint64_t dims[3] = {(cuuint64_t)dim, (cuuint64_t)a.out.n_q_heads, (cuuint64_t)a.sched.b.total_q};
-  const cuuint64_t strides[2] = {(cuuint64_t)dim * 2, (cuuint64_t)a.ldq};
-  const cuuint32_t box[3] = {64, (cuuint32_t)a.sched.group, (cuuint32_t)(a.sched.rows / 2 / a.sched.group)};
-  return encode_bf16(map, 3, a.Q, dims, strides, box);
-}
-
 template <int kD, bool kI8>
 int launch(const KvAttnArgs& a, int workers, cudaStream_t st) {
   using C = ChunkCfg<kD, kI8>;
@@ -702,8 +655,8 @@ int launch(const KvAttnArgs& a, int workers, cudaStream_t st) {
   static PerDeviceTable<char> attr_set;
   if (!ensure_dynamic_smem(attr_set, kv_chunk_kernel<kD, kI8>, C::kSmem + (kMaxKvSeqs + 1) * (int)sizeof(int64_t))) return MQ_ERR_CUDA;
   CUtensorMap mq_{}, mk{}, mv{};
-  if (!encode_queries(&mq_, a, kD)) return MQ_ERR_CUDA;
-  if (!kI8 && (!encode_pages(&mk, a.cache.K, a.cache, kD) || !encode_pages(&mv, a.cache.V, a.cache, kD))) return MQ_ERR_CUDA;
+  if (!encode_queries(&mq_, a.Q, a.ldq, a.out.n_q_heads, a.sched.b.total_q, a.sched.group, a.sched.rows / 2, kD)) return MQ_ERR_CUDA;
+  if (!kI8 && (!encode_pages(&mk, a.cache.K, a.cache, kD, kTile) || !encode_pages(&mv, a.cache.V, a.cache, kD, kTile))) return MQ_ERR_CUDA;
   const cudaError_t e = launch_pdl(kv_chunk_kernel<kD, kI8>, dim3((unsigned)workers), dim3(C::kThreads),
                                    C::kSmem + ((size_t)a.sched.b.n_seq + 1) * sizeof(int64_t), st, mq_, mk, mv, a);
   if (e != cudaSuccess) return cuda_status(e);

@@ -5,8 +5,8 @@
 // The product is taken with the KEYS as the rows of the tensor-core tile: a CTA owns 128 keys of one head (16 per
 // warp), keeps them in registers as A fragments, and walks the query rows in blocks of 64; a key's sum is then over
 // columns, i.e. over registers of four neighbouring lanes, and is written once.  No atomics, one order of summation.
-// With few query rows the kernel is bound by reading K; with many by the exponentials and the products.
-#include "mq_kv.cuh"
+// This is the kernel for few query rows, bound by reading K; chunks take mq_kv_weights_chunk.cu.
+#include "mq_kv_weights.cuh"
 
 namespace mq {
 namespace {
@@ -15,19 +15,7 @@ constexpr int kWarps = 8;
 constexpr int kThreads = kWarps * 32;
 constexpr int kKeys = kWarps * 16;   // keys of a CTA's tile
 constexpr int kRowsQ = 64;           // query rows per step
-
-struct WeightParams {
-  const uint8_t* Q;
-  int64_t ldq;   // bytes
-  KvBatchView b;
-  KvView c;
-  int max_q, group, n_q_heads;
-  float scale;
-  const float* lse;
-  const float* W_in;
-  float* W_out;
-  int64_t seq_stride, head_stride;
-};
+constexpr int kFewRows = 64;         // up to here (tokens x heads of the group) this kernel, above the tensor-memory one
 
 template <int kD>
 struct Smem {
@@ -103,6 +91,7 @@ kv_weights_kernel(const __grid_constant__ WeightParams p) {
       int page = -1;
       if (key < s.n_all) page = table[key >> p.c.page_shift];
       const bool ok = (unsigned)page < (unsigned)p.c.n_pages;
+      if (!ok && key < s.n_all && p.status) atomicCAS(p.status, MQ_OK, MQ_ERR_INVALID_ARG);
       const int64_t src = ok ? (int64_t)page * p.c.page_stride + (int64_t)g * p.c.head_stride +
                                    (int64_t)(key & ((1 << p.c.page_shift) - 1)) * p.c.slot_stride + pc * 16
                              : 0;
@@ -225,7 +214,7 @@ using namespace mq;
 
 extern "C" int mq_kv_weights(const void* Q, int64_t ldq, const mq_kv_batch* batch, const mq_kv_cache* cache, int32_t n_q_heads,
                              float scale, const float* lse, const float* W_in, float* W_out, int64_t w_seq_stride,
-                             int64_t w_head_stride, void* stream) {
+                             int64_t w_head_stride, int32_t* status, void* stream) {
   WeightParams p{};
   int rc = check_kv_cache(cache, &p.c);
   if (rc != MQ_OK) return rc;
@@ -249,9 +238,13 @@ extern "C" int mq_kv_weights(const void* Q, int64_t ldq, const mq_kv_batch* batc
   p.W_out = W_out;
   p.seq_stride = w_seq_stride;
   p.head_stride = w_head_stride;
+  p.status = status;
   const int64_t most = (int64_t)batch->n_seq * cache->n_kv_heads * ((reach + kKeys - 1) / kKeys);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool i8 = (cache->flags & MQ_KV_INT8) != 0;
+  // (a token's heads have to fit into a row tile of the chunk kernel, and its maps need a page)
+  if ((int64_t)batch->max_q * p.group > kFewRows && p.group <= 128 && cache->n_pages > 0)
+    return launch_kv_weights_chunk(p, cache->head_dim, i8, most, st);
   if (cache->head_dim == 128) return i8 ? launch<128, true>(p, most, st) : launch<128, false>(p, most, st);
   return i8 ? launch<64, true>(p, most, st) : launch<64, false>(p, most, st);
 }

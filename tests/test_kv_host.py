@@ -55,7 +55,7 @@ def test_every_entry_point_refuses_a_bad_cache(lib, kw, status):
     b = _batch()
     att = lib.mq_kv_attention(A, 1024, C.byref(b), C.byref(c), 8, 0.1, A, 1024, None, A, 1 << 30, None)
     assert att == want and lib.mq_kv_attention_workspace_bytes(C.byref(b), C.byref(c), 8) == 0
-    assert lib.mq_kv_weights(A, 1024, C.byref(b), C.byref(c), 8, 0.1, A, None, A, 4096, 512, None) == want
+    assert lib.mq_kv_weights(A, 1024, C.byref(b), C.byref(c), 8, 0.1, A, None, A, 4096, 512, None, None) == want
     for src, dst in ((c, good), (good, c)):
         assert lib.mq_kv_evict(C.byref(src), A, 7, A, 2, A, 4096, 512, 64, 0, 0, C.byref(dst), A, 7, A, A, None, None) == want
     if kw.get("dim", 128) == 128 and kw.get("hkv", 4) == 4:
@@ -88,7 +88,7 @@ def test_attention_refusals(lib):
 
 def test_weights_refusals(lib):
     def call(q=A, ldq=1024, hq=8, scale=0.1, lse=A, w=A, ss=4096, hs=512, **kw):
-        return lib.mq_kv_weights(q, ldq, C.byref(_batch(**kw)), C.byref(_cache()), hq, scale, lse, None, w, ss, hs, None)
+        return lib.mq_kv_weights(q, ldq, C.byref(_batch(**kw)), C.byref(_cache()), hq, scale, lse, None, w, ss, hs, None, None)
 
     assert call(hq=6) == call(ldq=512) == call(scale=0.0) == call(ss=-1) == call(hs=-1) == B.MQ_ERR_INVALID_ARG
     assert call(q=None) == call(lse=None) == call(w=None) == B.MQ_ERR_INVALID_ARG
