@@ -99,6 +99,23 @@ __device__ __forceinline__ KvSeq kv_seq(const KvBatchView& v, int page_shift, in
   return s;
 }
 
+// Division of 0 <= n < 2^31 by a divisor known on the host: n * m >> 31 + l with l = ceil(log2 d), m = ceil(2^(31 + l) / d)
+// (m < 2^32, and the quotient is exact for n < 2^31).  A runtime division is some 40 dependent instructions, which
+// counts in kernels that last a few microseconds.
+struct FastDiv {
+  uint32_t m;
+  int32_t l, d;
+};
+inline FastDiv fast_div(int d) {
+  FastDiv f;
+  f.d = d;
+  f.l = 0;
+  while (((int64_t)1 << f.l) < d) ++f.l;
+  f.m = (uint32_t)((((uint64_t)1 << (31 + f.l)) + d - 1) / d);
+  return f;
+}
+__device__ __forceinline__ int operator/(int n, const FastDiv& f) { return (int)(((uint64_t)(uint32_t)n * f.m) >> (31 + f.l)); }
+
 // ---- instructions ---------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t kv_smem_u32(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
 // 16 bytes global -> shared, zero-filled when `bytes` is 0 (the source is then not read)
@@ -116,6 +133,12 @@ __device__ __forceinline__ void ldsm_x4(uint32_t addr, uint32_t (&r)[4]) {
 __device__ __forceinline__ void ldsm_x4_trans(uint32_t addr, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+// The transpose of an 8 x 8 matrix of 16-bit values held as two neighbouring columns per lane
+__device__ __forceinline__ uint32_t mat_transpose(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
 }
 // D (16 x 8, float32) += A (16 x 16) B (16 x 8)
 template <bool F16>

@@ -2,12 +2,15 @@
 //
 //   O[i, h] = sum_j P[i, j] V[j, g],  P = softmax_j(scale * Q[i, h] . K[j, g]),  lse = log of the denominator
 //
-// The kernel of this file is the one for few query rows (decode steps): it is bound by reading K and V once.  A unit is
-// 16 query rows (tokens x the query heads of one key/value head), so a key is read once for the whole group.
+// The kernel of this file is the one for few query rows (decode steps): it is bound by reading K and V once.  A unit is 8
+// or 16 query rows (tokens x the query heads of one key/value head), so a key is read once for the whole group.
 //   * A warp is on its own: it streams 16 keys at a time (K and V rows, 16-byte asynchronous copies straight from the
 //     pages, two or more tiles in flight) into its own ring in shared memory and runs a complete online softmax over
 //     them on mma.sync; there is no block-wide barrier until the four warps' results are joined at the end of a range.
 //     Tensor-core throughput is no concern here: at the cache's rate an SM sees 16 keys in about 190 cycles.
+//   * Both products are taken transposed, S^T = K Q^T and O^T = V^T P^T: the 16 keys, and 16 channels, are the rows of the
+//     instruction's tile and the query rows its 8 columns, so a group of up to 8 heads wastes nothing.  P^T changes from
+//     the layout of a result to that of an operand by an 8 x 8 transpose in registers.
 //   * The exponents are taken relative to the running maximum, the accumulator is rescaled only when a row's maximum moved.
 //   * An int8 cache is read as codes and widened in registers to fp16 exactly (the products' sums do not care in which
 //     order the channels come, so a thread takes contiguous codes); the scales multiply the scores and the result.
@@ -17,25 +20,32 @@
 namespace mq {
 namespace {
 
-constexpr int kM = 16;            // query rows of a unit
 constexpr int kWarps = 4;
 constexpr int kTile = 16 * kWarps; // keys of a tile: 16 per warp
 constexpr int kThreads = kWarps * 32;
-constexpr int kCtasPerSm = 3;
 constexpr int kExtra = 3;         // what a unit costs besides its tiles, in tiles
+constexpr int kMinLen = 2;        // a worker's least share of the line
 // fp16 probabilities reach down to 2^-24 only: with the reference 14 below the maximum they run up to 2^14 instead of 1, and
 // what is lost below is 2^-39 of the largest one (a sum over them stays in float32 either way).
 constexpr float kLiftF16 = 14.0f;
 
-template <int kD, bool kI8>
+// kN: query rows of a unit, in eights
+template <int kD, bool kI8, int kN>
 struct Cfg {
+  static constexpr int kRows = 8 * kN;
   static constexpr int kRow = kD * (kI8 ? 1 : 2);        // bytes of a cached row
   static constexpr int kStage = 16 * kRow * 2;           // K and V of 16 keys
-  static constexpr int kStages = kI8 ? 4 : (kD == 128 ? 2 : 4);
+  static constexpr int kCtas = kStage == 8192 ? 2 : kN == 1 ? 4 : 3;   // per SM
+  static constexpr int kStages = kStage == 2048 ? 4 : 3;
   static constexpr int kRing = kStage * kStages;
+  static constexpr int kPitch = kD + 4;                  // floats between rows of the warps' results
   static constexpr int kSmem = kWarps * kRing;
-  static_assert(kSmem >= kWarps * kM * kD * 4, "the join of the warps reuses the rings");
+  static_assert(kSmem >= kWarps * kRows * kPitch * 4, "the join of the warps reuses the rings");
 };
+constexpr int decode_ctas(int dim, bool i8, int n) {
+  return dim == 128 ? (i8 ? (n == 1 ? Cfg<128, true, 1>::kCtas : Cfg<128, true, 2>::kCtas) : (n == 1 ? Cfg<128, false, 1>::kCtas : Cfg<128, false, 2>::kCtas))
+                    : (i8 ? (n == 1 ? Cfg<64, true, 1>::kCtas : Cfg<64, true, 2>::kCtas) : (n == 1 ? Cfg<64, false, 1>::kCtas : Cfg<64, false, 2>::kCtas));
+}
 
 // Offset of 16-byte piece c of row r in a tile: pieces are exchanged within 128-byte lines so that the eight rows that
 // one load instruction touches lie in different banks.
@@ -46,14 +56,14 @@ __device__ __forceinline__ uint32_t piece(int r, int c) {
   return off ^ (key << 4);
 }
 
-template <int kD, bool kI8>
-__global__ void __launch_bounds__(kThreads, kCtasPerSm)
+template <int kD, bool kI8, int kN>
+__global__ void __launch_bounds__(kThreads, (Cfg<kD, kI8, kN>::kCtas))
 kv_decode_kernel(const __grid_constant__ KvAttnArgs p) {
-  using C = Cfg<kD, kI8>;
-  constexpr int kRow = C::kRow, kPieces = kRow / 16, kSteps = kD / 16, kOut = kD / 8;
-  constexpr float kLift = kI8 ? kLiftF16 : 0.0f;   // m0, m1: the exponents' reference, the running maximum less this
+  using C = Cfg<kD, kI8, kN>;
+  constexpr int kRow = C::kRow, kPieces = kRow / 16, kSteps = kD / 16, kRows = C::kRows;
+  constexpr float kLift = kI8 ? kLiftF16 : 0.0f;   // m: the exponents' reference, the running maximum less this
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ float ml_s[kWarps][kM][2];
+  __shared__ float ml_s[kWarps][kRows][2];
   __shared__ int64_t red[kWarps];
   int64_t* prefix = reinterpret_cast<int64_t*>(smem + C::kSmem);
   pdl_launch_dependents();
@@ -75,7 +85,7 @@ kv_decode_kernel(const __grid_constant__ KvAttnArgs p) {
     at += len;
     if (t0 == t1) continue;   // the range ends before the unit's first tile
     const int end = sched_end(sc, u.s, u.rb), ctx = u.s.n_all - u.s.n_new;
-    const int row0 = u.rb * kM, n_rows = min(kM, u.s.n_new * sc.group - row0);
+    const int row0 = u.rb * kRows, n_rows = min(kRows, u.s.n_new * sc.group.d - row0);
     const int32_t* table = sc.b.page_table + (int64_t)u.b * sc.b.max_pages;
     const int64_t head_off = (int64_t)u.g * p.cache.head_stride;
 
@@ -85,7 +95,7 @@ kv_decode_kernel(const __grid_constant__ KvAttnArgs p) {
       const int key0 = ((t0 + i) * kWarps + warp) * 16;
       return i < n_my && key0 < end ? table[key0 >> p.cache.page_shift] : -1;
     };
-    auto issue = [&](int i, int page) {
+    auto issue = [&](int i, int stage, int page) {
       if (i < n_my) {
         const int key0 = ((t0 + i) * kWarps + warp) * 16;
         int n_ok = min(max(end - key0, 0), 16);
@@ -93,19 +103,22 @@ kv_decode_kernel(const __grid_constant__ KvAttnArgs p) {
           n_ok = 0;
           if (lane == 0) atomicCAS(p.status, MQ_OK, MQ_ERR_INVALID_ARG);
         }
+        constexpr int kCopies = 16 * kPieces / 32, kStep = 32 / kPieces;   // rows of one instruction
+        const int r0 = lane / kPieces, pc = lane % kPieces;
         const int64_t off = n_ok > 0 ? (int64_t)page * p.cache.page_stride + head_off +
-                                           (int64_t)(key0 & ((1 << p.cache.page_shift) - 1)) * p.cache.slot_stride
+                                           (int64_t)((key0 & ((1 << p.cache.page_shift) - 1)) + r0) * p.cache.slot_stride + pc * 16
                                      : 0;
-        const uint32_t dst = ring + (uint32_t)((i % C::kStages) * C::kStage);
-        constexpr int kCopies = 16 * kPieces / 32;
+        const uint8_t *ks = p.cache.K + off, *vs = p.cache.V + off;
+        const uint32_t dst = ring + (uint32_t)(stage * C::kStage);
 #pragma unroll
         for (int c = 0; c < kCopies; ++c) {
-          const int idx = c * 32 + lane, r = idx / kPieces, pc = idx % kPieces;
+          const int r = c * kStep + r0;
           const bool ok = r < n_ok;
-          const int64_t src = ok ? off + (int64_t)r * p.cache.slot_stride + pc * 16 : 0;
           const uint32_t d = dst + piece<kRow>(r, pc);
-          cp_async16(d, ok ? p.cache.K + src : p.Q, ok ? 16u : 0u);
-          cp_async16(d + 16 * kRow, ok ? p.cache.V + src : p.Q, ok ? 16u : 0u);
+          cp_async16(d, ok ? ks : p.Q, ok ? 16u : 0u);
+          cp_async16(d + 16 * kRow, ok ? vs : p.Q, ok ? 16u : 0u);
+          ks += kStep * p.cache.slot_stride;
+          vs += kStep * p.cache.slot_stride;
         }
       }
       cp_async_commit();
@@ -115,194 +128,223 @@ kv_decode_kernel(const __grid_constant__ KvAttnArgs p) {
     for (int i = 0; i < C::kStages - 1; ++i) {
       const int pg = page_next;
       page_next = page_of(i + 1);
-      issue(i, pg);
+      issue(i, i, pg);
     }
 
-    // ---- query fragments (A operand): rows quad and quad + 8
-    uint32_t qf[kSteps][4];
-    float sc0, sc1;                 // scores -> log2 units, per row
-    const bool ok0 = quad < n_rows, ok1 = quad + 8 < n_rows;
-    const int i0 = (row0 + quad) / sc.group, i1 = (row0 + quad + 8) / sc.group;
-    {
-      const int h0 = u.g * sc.group + (row0 + quad) % sc.group, h1 = u.g * sc.group + (row0 + quad + 8) % sc.group;
-      const uint8_t* q0 = p.Q + (int64_t)(u.s.begin + i0) * p.ldq + (int64_t)h0 * (kD * 2);
-      const uint8_t* q1 = p.Q + (int64_t)(u.s.begin + i1) * p.ldq + (int64_t)h1 * (kD * 2);
-      sc0 = sc1 = p.scale * 1.4426950408889634f;
+    // ---- query fragments (B operand): column quad of block nt is row 8 nt + quad of the unit
+    uint32_t qf[kN][kSteps][2];
+    float fac[kN][2];               // scores -> log2 units, rows 2 t4 and 2 t4 + 1 of block nt
+    int lim[kN][2];                 // how far these rows see (below)
+    const int32_t* perm = sc.b.perm ? sc.b.perm + u.s.begin : nullptr;
+    const float base_fac = p.scale * 1.4426950408889634f * (kI8 ? p.cache.k_scale[u.g] : 1.0f);
+#pragma unroll
+    for (int nt = 0; nt < kN; ++nt) {
+      const int r = 8 * nt + quad;
+      const bool ok = r < n_rows;
+      const int tok = (row0 + r) / sc.group;
+      const uint8_t* q = p.Q + (int64_t)(u.s.begin + tok) * p.ldq + (int64_t)(u.g * sc.group.d + (row0 + r) - tok * sc.group.d) * (kD * 2);
       if (!kI8) {
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) {
           const int c = (k * 16 + 2 * t4) * 2;
-          qf[k][0] = ok0 ? *reinterpret_cast<const uint32_t*>(q0 + c) : 0u;
-          qf[k][1] = ok1 ? *reinterpret_cast<const uint32_t*>(q1 + c) : 0u;
-          qf[k][2] = ok0 ? *reinterpret_cast<const uint32_t*>(q0 + c + 16) : 0u;
-          qf[k][3] = ok1 ? *reinterpret_cast<const uint32_t*>(q1 + c + 16) : 0u;
+          qf[nt][k][0] = ok ? *reinterpret_cast<const uint32_t*>(q + c) : 0u;
+          qf[nt][k][1] = ok ? *reinterpret_cast<const uint32_t*>(q + c + 16) : 0u;
         }
+        fac[nt][0] = fac[nt][1] = base_fac;
       } else {
         // channel order of the product: step k, position (2 t4, 2 t4 + 1, 2 t4 + 8, 2 t4 + 9) is channel t4 * D/4 + 4 k + 0 .. 3
-        uint2 w0[kSteps], w1[kSteps];
-        float m0 = 0.0f, m1 = 0.0f;
+        uint2 w[kSteps];
+        float m = 0.0f;
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) {
-          const int c = (t4 * (kD / 4) + 4 * k) * 2;
-          w0[k] = ok0 ? *reinterpret_cast<const uint2*>(q0 + c) : make_uint2(0u, 0u);
-          w1[k] = ok1 ? *reinterpret_cast<const uint2*>(q1 + c) : make_uint2(0u, 0u);
-          m0 = fmaxf(m0, fmaxf(fmaxf(fabsf(kv_bf16_lo(w0[k].x)), fabsf(kv_bf16_hi(w0[k].x))),
-                               fmaxf(fabsf(kv_bf16_lo(w0[k].y)), fabsf(kv_bf16_hi(w0[k].y)))));
-          m1 = fmaxf(m1, fmaxf(fmaxf(fabsf(kv_bf16_lo(w1[k].x)), fabsf(kv_bf16_hi(w1[k].x))),
-                               fmaxf(fabsf(kv_bf16_lo(w1[k].y)), fabsf(kv_bf16_hi(w1[k].y)))));
+          w[k] = ok ? *reinterpret_cast<const uint2*>(q + (t4 * (kD / 4) + 4 * k) * 2) : make_uint2(0u, 0u);
+          m = fmaxf(m, fmaxf(fmaxf(fabsf(kv_bf16_lo(w[k].x)), fabsf(kv_bf16_hi(w[k].x))),
+                             fmaxf(fabsf(kv_bf16_lo(w[k].y)), fabsf(kv_bf16_hi(w[k].y)))));
         }
-        m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, 1)); m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, 2));
-        m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, 1)); m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, 2));
+        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
+        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
         // the power of two that brings the row's largest magnitude into [1, 2) (an infinity stays one either way)
-        const int e0 = m0 > 0.0f && m0 < INFINITY ? (int)((__float_as_uint(m0) >> 23) & 255) - 127 : 0;
-        const int e1 = m1 > 0.0f && m1 < INFINITY ? (int)((__float_as_uint(m1) >> 23) & 255) - 127 : 0;
-        const float f0 = exp2f((float)-e0), f1 = exp2f((float)-e1);
-        const float ks = p.cache.k_scale[u.g];
-        sc0 = sc0 * ks * exp2f((float)e0);
-        sc1 = sc1 * ks * exp2f((float)e1);
+        const int e = m > 0.0f && m < INFINITY ? (int)((__float_as_uint(m) >> 23) & 255) - 127 : 0;
+        const float f = exp2f((float)-e), back = base_fac * exp2f((float)e);
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) {
-          qf[k][0] = kv_pack_f16(kv_bf16_lo(w0[k].x) * f0, kv_bf16_hi(w0[k].x) * f0);
-          qf[k][2] = kv_pack_f16(kv_bf16_lo(w0[k].y) * f0, kv_bf16_hi(w0[k].y) * f0);
-          qf[k][1] = kv_pack_f16(kv_bf16_lo(w1[k].x) * f1, kv_bf16_hi(w1[k].x) * f1);
-          qf[k][3] = kv_pack_f16(kv_bf16_lo(w1[k].y) * f1, kv_bf16_hi(w1[k].y) * f1);
+          qf[nt][k][0] = kv_pack_f16(kv_bf16_lo(w[k].x) * f, kv_bf16_hi(w[k].x) * f);
+          qf[nt][k][1] = kv_pack_f16(kv_bf16_lo(w[k].y) * f, kv_bf16_hi(w[k].y) * f);
         }
+        fac[nt][0] = __shfl_sync(0xffffffffu, back, 8 * t4);
+        fac[nt][1] = __shfl_sync(0xffffffffu, back, 8 * t4 + 4);
+      }
+      // visibility: without perm, keys below lim; with it, the context and the chunk's rows whose index is not larger
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int rr = 8 * nt + 2 * t4 + e, tk = (row0 + rr) / sc.group;
+        lim[nt][e] = rr >= n_rows ? INT_MIN : perm ? perm[tk] : ctx + tk + 1;
       }
     }
-    // visibility: without perm, keys below lim; with it, the context and the chunk's rows whose index is not larger
-    const int32_t* perm = sc.b.perm ? sc.b.perm + u.s.begin : nullptr;
-    const int r_first = row0 / sc.group;
-    const int all_see = perm ? ctx : min(end, ctx + r_first + 1);   // every row of the unit sees the keys below
-    const int lim0 = ok0 ? (perm ? perm[i0] : ctx + i0 + 1) : INT_MIN, lim1 = ok1 ? (perm ? perm[i1] : ctx + i1 + 1) : INT_MIN;
-    auto sees = [&](int key, int lim, bool ok) -> bool {
-      if (key >= end || !ok) return false;
-      if (!perm) return key < lim;
-      return key < ctx || perm[key - ctx] <= lim;
+    const int all_see = perm ? ctx : min(end, ctx + row0 / sc.group + 1);   // every row of the unit sees the keys below
+    auto sees = [&](int key, int lm) -> bool {
+      if (key >= end || lm == INT_MIN) return false;
+      if (!perm) return key < lm;
+      return key < ctx || perm[key - ctx] <= lm;
     };
 
-    float o[kOut][4];
+    float o[kSteps][kN][4];    // O^T: channels 16 mt + quad (+ 8) x rows 2 t4, 2 t4 + 1 of block nt
+    float m[kN][2], l[kN][2];
 #pragma unroll
-    for (int n = 0; n < kOut; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.0f;
-    float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.0f, l1 = 0.0f;
+    for (int nt = 0; nt < kN; ++nt) {
+#pragma unroll
+      for (int mt = 0; mt < kSteps; ++mt) o[mt][nt][0] = o[mt][nt][1] = o[mt][nt][2] = o[mt][nt][3] = 0.0f;
+      m[nt][0] = m[nt][1] = -INFINITY;
+      l[nt][0] = l[nt][1] = 0.0f;
+    }
 
+    int stage = 0, fill = C::kStages - 1;   // ring positions of the tile at hand and of the one to ask for
     for (int i = 0; i < n_my; ++i) {
       const int pg = page_next;
       page_next = page_of(i + C::kStages);
-      issue(i + C::kStages - 1, pg);
+      issue(i + C::kStages - 1, fill, pg);
+      if (++fill == C::kStages) fill = 0;
       cp_async_wait<C::kStages - 1>();
       __syncwarp();
-      const uint32_t kt = ring + (uint32_t)((i % C::kStages) * C::kStage), vt = kt + 16 * kRow;
+      const uint32_t kt = ring + (uint32_t)(stage * C::kStage), vt = kt + 16 * kRow;
+      if (++stage == C::kStages) stage = 0;
       const int key0 = ((t0 + i) * kWarps + warp) * 16;
       if (key0 < end) {
-        float s[2][4] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
+        // ---- S^T (16 keys x 8 rows): two chains of products each, so that they overlap
+        float s[kN][4], s2[kN][4];
+#pragma unroll
+        for (int nt = 0; nt < kN; ++nt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[nt][e] = s2[nt][e] = 0.0f;
         if (!kI8) {
 #pragma unroll
           for (int k = 0; k < kSteps; ++k) {
-            uint32_t b[4];
-            ldsm_x4(kt + piece<kRow>((lane & 7) + ((lane >> 4) << 3), 2 * k + ((lane >> 3) & 1)), b);
-            mma_16816<false>(s[0], qf[k], b[0], b[1]);
-            mma_16816<false>(s[1], qf[k], b[2], b[3]);
+            uint32_t a[4];
+            ldsm_x4(kt + piece<kRow>(lane & 15, 2 * k + (lane >> 4)), a);
+#pragma unroll
+            for (int nt = 0; nt < kN; ++nt) mma_16816<false>((k & 1) ? s2[nt] : s[nt], a, qf[nt][k][0], qf[nt][k][1]);
           }
         } else {
           constexpr int kLoads = kD / 64;   // 16-byte loads per key row and thread
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
+          for (int c = 0; c < kLoads; ++c) {
+            uint32_t x[2][4];
 #pragma unroll
-            for (int c = 0; c < kLoads; ++c) {
-              uint32_t x[4];
+            for (int j = 0; j < 2; ++j)
               asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-                           : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(kt + piece<kRow>(quad + 8 * j, t4 * kLoads + c)));
+                           : "=r"(x[j][0]), "=r"(x[j][1]), "=r"(x[j][2]), "=r"(x[j][3]) : "r"(kt + piece<kRow>(quad + 8 * j, t4 * kLoads + c)));
 #pragma unroll
-              for (int w = 0; w < 4; ++w) {
-                uint32_t b0, b1;
-                i8x4_to_f16(x[w], b0, b1);
-                mma_16816<true>(s[j], qf[4 * c + w], b0, b1);
-              }
+            for (int w = 0; w < 4; ++w) {
+              uint32_t a[4];
+              i8x4_to_f16(x[0][w], a[0], a[2]);
+              i8x4_to_f16(x[1][w], a[1], a[3]);
+#pragma unroll
+              for (int nt = 0; nt < kN; ++nt) mma_16816<true>((w & 1) ? s2[nt] : s[nt], a, qf[nt][4 * c + w][0], qf[nt][4 * c + w][1]);
             }
           }
         }
         const bool masked = key0 + 16 > all_see;
-        unsigned seen = 0xffu;   // bit 4 j + e: score s[j][e] counts
+        unsigned seen = ~0u;   // bit 4 nt + e: score s[nt][e] counts
         if (masked) {
           seen = 0u;
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
+          for (int nt = 0; nt < kN; ++nt)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              if (sees(key0 + 8 * j + 2 * t4 + (e & 1), e < 2 ? lim0 : lim1, e < 2 ? ok0 : ok1)) seen |= 1u << (4 * j + e);
+              if (sees(key0 + quad + 8 * (e >> 1), lim[nt][e & 1])) seen |= 1u << (4 * nt + e);
         }
+        bool grown = false;
+        float top[kN][2];
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int nt = 0; nt < kN; ++nt) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            s[j][e] *= e < 2 ? sc0 : sc1;
-            if (masked && !((seen >> (4 * j + e)) & 1u)) s[j][e] = -INFINITY;
+            s[nt][e] = (s[nt][e] + s2[nt][e]) * fac[nt][e & 1];
+            if (masked && !((seen >> (4 * nt + e)) & 1u)) s[nt][e] = -INFINITY;
           }
-        float x0 = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[1][0], s[1][1])), x1 = fmaxf(fmaxf(s[0][2], s[0][3]), fmaxf(s[1][2], s[1][3]));
-        x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, 1)); x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, 2));
-        x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, 1)); x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, 2));
-        x0 -= kLift;
-        x1 -= kLift;
-        if (__any_sync(0xffffffffu, x0 > m0 || x1 > m1)) {
-          const float n0 = fmaxf(m0, x0), n1 = fmaxf(m1, x1);
-          const float f0 = m0 == -INFINITY ? 0.0f : kv_exp2(m0 - n0), f1 = m1 == -INFINITY ? 0.0f : kv_exp2(m1 - n1);
-          m0 = n0; m1 = n1;
-          l0 *= f0; l1 *= f1;
 #pragma unroll
-          for (int n = 0; n < kOut; ++n) { o[n][0] *= f0; o[n][1] *= f0; o[n][2] *= f1; o[n][3] *= f1; }
+          for (int e = 0; e < 2; ++e) {
+            float x = fmaxf(s[nt][e], s[nt][e + 2]);
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+            top[nt][e] = x - kLift;
+            grown |= top[nt][e] > m[nt][e];
+          }
         }
-        const float u0 = m0 == -INFINITY ? 0.0f : m0, u1 = m1 == -INFINITY ? 0.0f : m1;   // a row without keys yet: exp2(-inf) = 0
+        if (__any_sync(0xffffffffu, grown)) {
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          s[j][0] = kv_exp2(s[j][0] - u0); s[j][1] = kv_exp2(s[j][1] - u0);
-          s[j][2] = kv_exp2(s[j][2] - u1); s[j][3] = kv_exp2(s[j][3] - u1);
-          l0 += s[j][0] + s[j][1];
-          l1 += s[j][2] + s[j][3];
+          for (int nt = 0; nt < kN; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const float n = fmaxf(m[nt][e], top[nt][e]);
+              const float f = m[nt][e] == -INFINITY ? 0.0f : kv_exp2(m[nt][e] - n);
+              m[nt][e] = n;
+              l[nt][e] *= f;
+#pragma unroll
+              for (int mt = 0; mt < kSteps; ++mt) { o[mt][nt][e] *= f; o[mt][nt][e + 2] *= f; }
+            }
+        }
+        uint32_t pf[kN][2];
+#pragma unroll
+        for (int nt = 0; nt < kN; ++nt) {
+          // (a row without keys yet: exp2(-inf) = 0)
+          const float u0 = m[nt][0] == -INFINITY ? 0.0f : m[nt][0], u1 = m[nt][1] == -INFINITY ? 0.0f : m[nt][1];
+          s[nt][0] = kv_exp2(s[nt][0] - u0); s[nt][1] = kv_exp2(s[nt][1] - u1);
+          s[nt][2] = kv_exp2(s[nt][2] - u0); s[nt][3] = kv_exp2(s[nt][3] - u1);
+          l[nt][0] += s[nt][0] + s[nt][2];
+          l[nt][1] += s[nt][1] + s[nt][3];
+          pf[nt][0] = mat_transpose(kI8 ? kv_pack_f16(s[nt][0], s[nt][1]) : kv_pack_bf16(s[nt][0], s[nt][1]));
+          pf[nt][1] = mat_transpose(kI8 ? kv_pack_f16(s[nt][2], s[nt][3]) : kv_pack_bf16(s[nt][2], s[nt][3]));
         }
         // A value that some rows may not see must not reach them even if it is infinite or NaN (0 * inf): such a tile
         // is multiplied key by key.  Only tiles with rows of different sight can hold one.
         bool odd = false;
         if (!kI8 && masked && all_see < end) {
-          bool mine = false;
+          uint32_t big = 0u;
 #pragma unroll
           for (int c = 0; c < 16 * kPieces / 32; ++c) {
             uint32_t x[4];
             asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
                          : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(vt + (uint32_t)(c * 32 + lane) * 16u));
 #pragma unroll
-            for (int w = 0; w < 4; ++w) mine |= (x[w] & 0x7f80u) == 0x7f80u || (x[w] & 0x7f800000u) == 0x7f800000u;
+            for (int w = 0; w < 4; ++w) big = __vmaxu2(big, x[w] & 0x7fff7fffu);
           }
-          odd = __any_sync(0xffffffffu, mine);
+          odd = __any_sync(0xffffffffu, (big & 0xffffu) >= 0x7f80u || (big >> 16) >= 0x7f80u);
         }
         if (!kI8 && odd) {
-#pragma unroll
+#pragma unroll 1
           for (int key = 0; key < 16; ++key) {
-            const int from = (lane & ~3) | ((key & 7) >> 1);
-            const float p0 = __shfl_sync(0xffffffffu, s[key >> 3][key & 1], from), p1 = __shfl_sync(0xffffffffu, s[key >> 3][2 + (key & 1)], from);
-            const unsigned vis = __shfl_sync(0xffffffffu, seen, from);
-            const bool v0 = (vis >> (4 * (key >> 3) + (key & 1))) & 1u, v1 = (vis >> (4 * (key >> 3) + 2 + (key & 1))) & 1u;
+            const int from = ((key & 7) << 2) | t4;
 #pragma unroll
-            for (int n = 0; n < kOut; ++n) {
-              uint32_t x;
-              asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(vt + piece<kRow>(key, n) + (uint32_t)t4 * 4u));
-              if (v0) { o[n][0] = fmaf(p0, kv_bf16_lo(x), o[n][0]); o[n][1] = fmaf(p0, kv_bf16_hi(x), o[n][1]); }
-              if (v1) { o[n][2] = fmaf(p1, kv_bf16_lo(x), o[n][2]); o[n][3] = fmaf(p1, kv_bf16_hi(x), o[n][3]); }
+            for (int nt = 0; nt < kN; ++nt) {
+              const float a0 = __shfl_sync(0xffffffffu, s[nt][0], from), a1 = __shfl_sync(0xffffffffu, s[nt][1], from);
+              const float b0 = __shfl_sync(0xffffffffu, s[nt][2], from), b1 = __shfl_sync(0xffffffffu, s[nt][3], from);
+              const unsigned vis = __shfl_sync(0xffffffffu, seen, from) >> (4 * nt + (key < 8 ? 0 : 2));
+              const float p0 = key < 8 ? a0 : b0, p1 = key < 8 ? a1 : b1;
+#pragma unroll
+              for (int mt = 0; mt < kSteps; ++mt)
+#pragma unroll
+                for (int hh = 0; hh < 2; ++hh) {
+                  unsigned short x;
+                  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(x) : "r"(vt + piece<kRow>(key, 2 * mt + hh) + (uint32_t)quad * 2u));
+                  const float v = __uint_as_float((uint32_t)x << 16);
+                  if (vis & 1u) o[mt][nt][2 * hh] = fmaf(p0, v, o[mt][nt][2 * hh]);
+                  if (vis & 2u) o[mt][nt][2 * hh + 1] = fmaf(p1, v, o[mt][nt][2 * hh + 1]);
+                }
             }
           }
         } else if (!kI8) {
-          const uint32_t pf[4] = {kv_pack_bf16(s[0][0], s[0][1]), kv_pack_bf16(s[0][2], s[0][3]), kv_pack_bf16(s[1][0], s[1][1]),
-                                  kv_pack_bf16(s[1][2], s[1][3])};
 #pragma unroll
-          for (int n = 0; n < kOut; n += 2) {
-            uint32_t b[4];
-            ldsm_x4_trans(vt + piece<kRow>((lane & 7) + (((lane >> 3) & 1) << 3), n + (lane >> 4)), b);
-            mma_16816<false>(o[n], pf, b[0], b[1]);
-            mma_16816<false>(o[n + 1], pf, b[2], b[3]);
+          for (int mt = 0; mt < kSteps; ++mt) {
+            uint32_t a[4];
+            ldsm_x4_trans(vt + piece<kRow>((lane & 7) + ((lane >> 4) << 3), 2 * mt + ((lane >> 3) & 1)), a);
+#pragma unroll
+            for (int nt = 0; nt < kN; ++nt) mma_16816<false>(o[mt][nt], a, pf[nt][0], pf[nt][1]);
           }
         } else {
-          const uint32_t pf[4] = {kv_pack_f16(s[0][0], s[0][1]), kv_pack_f16(s[0][2], s[0][3]), kv_pack_f16(s[1][0], s[1][1]),
-                                  kv_pack_f16(s[1][2], s[1][3])};
-          // output column n of product j is channel n * D/8 + j: a thread reads D/8 contiguous codes of each of its four keys
+          // result row quad (+ 8) of product mt is channel quad * D/8 + 2 mt (+ 1): a thread reads D/8 contiguous codes of each of its
+          // four keys
           constexpr int kWords = kD / 32;
           uint32_t x[4][kWords];
 #pragma unroll
@@ -317,79 +359,85 @@ kv_decode_kernel(const __grid_constant__ KvAttnArgs p) {
           }
 #pragma unroll
           for (int w = 0; w < kWords; ++w) {
-            const uint32_t lo01 = __byte_perm(x[0][w], x[1][w], 0x5140), hi01 = __byte_perm(x[0][w], x[1][w], 0x7362);
-            const uint32_t lo23 = __byte_perm(x[2][w], x[3][w], 0x5140), hi23 = __byte_perm(x[2][w], x[3][w], 0x7362);
-            uint32_t a0, a1, b0, b1;
-            i8x4_to_f16(lo01, a0, a1);
-            i8x4_to_f16(lo23, b0, b1);
-            mma_16816<true>(o[4 * w], pf, a0, b0);
-            mma_16816<true>(o[4 * w + 1], pf, a1, b1);
-            i8x4_to_f16(hi01, a0, a1);
-            i8x4_to_f16(hi23, b0, b1);
-            mma_16816<true>(o[4 * w + 2], pf, a0, b0);
-            mma_16816<true>(o[4 * w + 3], pf, a1, b1);
+            uint32_t a[2][4];   // two products: channels 4 w, 4 w + 1 and 4 w + 2, 4 w + 3 of this thread's run
+            i8x4_to_f16(__byte_perm(x[0][w], x[1][w], 0x5140), a[0][0], a[0][1]);
+            i8x4_to_f16(__byte_perm(x[2][w], x[3][w], 0x5140), a[0][2], a[0][3]);
+            i8x4_to_f16(__byte_perm(x[0][w], x[1][w], 0x7362), a[1][0], a[1][1]);
+            i8x4_to_f16(__byte_perm(x[2][w], x[3][w], 0x7362), a[1][2], a[1][3]);
+#pragma unroll
+            for (int nt = 0; nt < kN; ++nt) {
+              mma_16816<true>(o[2 * w][nt], a[0], pf[nt][0], pf[nt][1]);
+              mma_16816<true>(o[2 * w + 1][nt], a[1], pf[nt][0], pf[nt][1]);
+            }
           }
         }
       }
       __syncwarp();   // every lane has read the tile before its slot is filled again
     }
     cp_async_wait<0>();
-    l0 += __shfl_xor_sync(0xffffffffu, l0, 1); l0 += __shfl_xor_sync(0xffffffffu, l0, 2);
-    l1 += __shfl_xor_sync(0xffffffffu, l1, 1); l1 += __shfl_xor_sync(0xffffffffu, l1, 2);
+#pragma unroll
+    for (int nt = 0; nt < kN; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        l[nt][e] += __shfl_xor_sync(0xffffffffu, l[nt][e], 4);
+        l[nt][e] += __shfl_xor_sync(0xffffffffu, l[nt][e], 8);
+        l[nt][e] += __shfl_xor_sync(0xffffffffu, l[nt][e], 16);
+      }
 
     // ---- join the warps: each ran a softmax over its own keys
     __syncthreads();   // the rings are free
-    float* join = reinterpret_cast<float*>(smem) + warp * (kM * kD);
-    if (t4 == 0) {
-      ml_s[warp][quad][0] = m0; ml_s[warp][quad][1] = l0;
-      ml_s[warp][quad + 8][0] = m1; ml_s[warp][quad + 8][1] = l1;
-    }
+    float* join = reinterpret_cast<float*>(smem) + warp * (kRows * C::kPitch);
 #pragma unroll
-    for (int n = 0; n < kOut; ++n) {
-      if (!kI8) {
-        *reinterpret_cast<float2*>(join + quad * kD + 8 * n + 2 * t4) = make_float2(o[n][0], o[n][1]);
-        *reinterpret_cast<float2*>(join + (quad + 8) * kD + 8 * n + 2 * t4) = make_float2(o[n][2], o[n][3]);
-      } else {
-        join[quad * kD + (2 * t4) * kOut + n] = o[n][0];
-        join[quad * kD + (2 * t4 + 1) * kOut + n] = o[n][1];
-        join[(quad + 8) * kD + (2 * t4) * kOut + n] = o[n][2];
-        join[(quad + 8) * kD + (2 * t4 + 1) * kOut + n] = o[n][3];
+    for (int nt = 0; nt < kN; ++nt) {
+      const int r = 8 * nt + 2 * t4;
+      if (quad == 0) {
+        ml_s[warp][r][0] = m[nt][0]; ml_s[warp][r][1] = l[nt][0];
+        ml_s[warp][r + 1][0] = m[nt][1]; ml_s[warp][r + 1][1] = l[nt][1];
+      }
+#pragma unroll
+      for (int mt = 0; mt < kSteps; ++mt) {
+        const int d0 = kI8 ? quad * (kD / 8) + 2 * mt : 16 * mt + quad, d1 = kI8 ? d0 + 1 : d0 + 8;
+        join[r * C::kPitch + d0] = o[mt][nt][0];
+        join[(r + 1) * C::kPitch + d0] = o[mt][nt][1];
+        join[r * C::kPitch + d1] = o[mt][nt][2];
+        join[(r + 1) * C::kPitch + d1] = o[mt][nt][3];
       }
     }
     __syncthreads();
     const bool whole = t0 == 0 && t1 == u.tiles;
     const int slot = 2 * (int)blockIdx.x + (t0 == 0 ? 1 : 0);
-    const float vs = kI8 ? p.cache.v_scale[u.g] : 1.0f;
+    const float vsc = kI8 ? p.cache.v_scale[u.g] : 1.0f;
     constexpr int kColThreads = kD / 2;                 // two channels per thread
     const int col = ((int)threadIdx.x % kColThreads) * 2;
     for (int r = (int)threadIdx.x / kColThreads; r < n_rows; r += kThreads / kColThreads) {
-      float m = ml_s[0][r][0];
+      float mm = ml_s[0][r][0];
 #pragma unroll
-      for (int w = 1; w < kWarps; ++w) m = fmaxf(m, ml_s[w][r][0]);
-      float l = 0.0f, x = 0.0f, y = 0.0f;
+      for (int w = 1; w < kWarps; ++w) mm = fmaxf(mm, ml_s[w][r][0]);
+      float ll = 0.0f, x = 0.0f, y = 0.0f;
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) {
         const float mw = ml_s[w][r][0];
-        const float f = mw == -INFINITY ? 0.0f : kv_exp2(mw - m);
-        l = fmaf(f, ml_s[w][r][1], l);
-        const float2 v = *reinterpret_cast<const float2*>(reinterpret_cast<const float*>(smem) + w * (kM * kD) + r * kD + col);
+        const float f = mw == -INFINITY ? 0.0f : kv_exp2(mw - mm);
+        ll = fmaf(f, ml_s[w][r][1], ll);
+        const float2 v = *reinterpret_cast<const float2*>(reinterpret_cast<const float*>(smem) + (w * kRows + r) * C::kPitch + col);
         if (f != 0.0f) { x = fmaf(f, v.x, x); y = fmaf(f, v.y, y); }
       }
       if (whole) {
-        const int tok = u.s.begin + (row0 + r) / sc.group, head = u.g * sc.group + (row0 + r) % sc.group;
-        const float inv = l == 0.0f ? 0.0f : vs / l;
+        const int tk = (row0 + r) / sc.group, tok = u.s.begin + tk, head = u.g * sc.group.d + (row0 + r) - tk * sc.group.d;
+        const float inv = ll == 0.0f ? 0.0f : vsc / ll;
         *reinterpret_cast<__nv_bfloat162*>(p.out.O + (int64_t)tok * p.out.ldo + (int64_t)head * kD + col) =
             __floats2bfloat162_rn(x * inv, y * inv);
         if (col == 0 && p.out.lse)
-          p.out.lse[(int64_t)tok * p.out.n_q_heads + head] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+          p.out.lse[(int64_t)tok * p.out.n_q_heads + head] = ll == 0.0f ? -INFINITY : (mm + log2f(ll)) * 0.6931471805599453f;
       } else {
-        if (col == 0) p.parts.ml[(int64_t)slot * kM + r] = make_float2(m, l);
-        *reinterpret_cast<float2*>(p.parts.o + ((int64_t)slot * kM + r) * kD + col) = make_float2(x * vs, y * vs);
+        if (col == 0) p.parts.ml[(int64_t)slot * kRows + r] = make_float2(mm, ll);
+        *reinterpret_cast<float2*>(p.parts.o + ((int64_t)slot * kRows + r) * kD + col) = make_float2(x * vsc, y * vsc);
       }
     }
     if (t0 == 0 && !whole) {
       // the pieces end with the worker whose range holds the unit's last tile
-      rec.n_parts = (int)((unit_at + sc.extra + u.tiles - 1) / share) - (int)blockIdx.x + 1;
+      const int64_t last = unit_at + sc.extra + u.tiles - 1;
+      rec.n_parts = (last >> 31 ? (int)(last / share) : (int)((uint32_t)last / (uint32_t)share)) - (int)blockIdx.x + 1;
       rec.begin = u.s.begin; rec.row0 = row0; rec.n_rows = n_rows; rec.g = u.g;
     }
     __syncthreads();   // the join has been read before the next range fills the rings
@@ -404,7 +452,7 @@ kv_decode_kernel(const __grid_constant__ KvAttnArgs p) {
 constexpr int kJoinThreads = 256;
 template <int kD, int kWarpsPerRow>
 __global__ void __launch_bounds__(kJoinThreads)
-kv_combine_kernel(const int pitch, const int group, const KvParts parts, const KvOutArgs out) {
+kv_combine_kernel(const int pitch, const FastDiv group, const KvParts parts, const KvOutArgs out) {
   constexpr int kPer = kD / 32, kRows = kJoinThreads / 32 / kWarpsPerRow;
   __shared__ float part[kRows][kWarpsPerRow][kD + 2];
   pdl_launch_dependents();
@@ -487,7 +535,7 @@ kv_combine_kernel(const int pitch, const int group, const KvParts parts, const K
     }
   }
   if (!live) return;
-  const int tok = rec.begin + (rec.row0 + r) / group, head = rec.g * group + (rec.row0 + r) % group;
+  const int tk = (rec.row0 + r) / group, tok = rec.begin + tk, head = rec.g * group.d + (rec.row0 + r) - tk * group.d;
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   __nv_bfloat16* dst = out.O + (int64_t)tok * out.ldo + (int64_t)head * kD + lane * kPer;
   if (kPer == 4)
@@ -498,19 +546,23 @@ kv_combine_kernel(const int pitch, const int group, const KvParts parts, const K
     out.lse[(int64_t)tok * out.n_q_heads + head] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
 }
 
-template <int kD, bool kI8>
+template <int kD, bool kI8, int kN>
 int launch_decode(const KvAttnArgs& a, int workers, cudaStream_t st) {
-  using C = Cfg<kD, kI8>;
+  using C = Cfg<kD, kI8, kN>;
   const size_t smem = C::kSmem + ((size_t)a.sched.b.n_seq + 1) * sizeof(int64_t);
   static PerDeviceTable<char> attr_set;
-  if (!ensure_dynamic_smem(attr_set, kv_decode_kernel<kD, kI8>, C::kSmem + (kMaxKvSeqs + 1) * (int)sizeof(int64_t))) return MQ_ERR_CUDA;
-  const cudaError_t e = launch_pdl(kv_decode_kernel<kD, kI8>, dim3((unsigned)workers), dim3(kThreads), smem, st, a);
+  if (!ensure_dynamic_smem(attr_set, kv_decode_kernel<kD, kI8, kN>, C::kSmem + (kMaxKvSeqs + 1) * (int)sizeof(int64_t))) return MQ_ERR_CUDA;
+  const cudaError_t e = launch_pdl(kv_decode_kernel<kD, kI8, kN>, dim3((unsigned)workers), dim3(kThreads), smem, st, a);
   if (e != cudaSuccess) return cuda_status(e);
   return cuda_status(cudaGetLastError());
 }
+template <int kD, bool kI8>
+int launch_decode(const KvAttnArgs& a, int workers, cudaStream_t st) {
+  return a.sched.rows == 8 ? launch_decode<kD, kI8, 1>(a, workers, st) : launch_decode<kD, kI8, 2>(a, workers, st);
+}
 
 // Which kernel, and how many workers.  Up to kFewRows query rows per key/value head (tokens x heads of the group) take the
-// kernel above in blocks of 16 rows, more take the 128-row tensor-memory kernel of mq_kv_chunk.cu.
+// kernel above in blocks of 8 or 16 rows, more take the 128-row tensor-memory kernel of mq_kv_chunk.cu.
 constexpr int kFewRows = 32;
 struct Plan {
   bool chunk;
@@ -521,11 +573,11 @@ Plan attn_plan(const mq_kv_batch* b, const mq_kv_cache* c, int group) {
   // (a token's heads have to fit into a block of that kernel, and its maps need a page)
   p.chunk = (int64_t)b->max_q * group > kFewRows && group <= 128 && c->n_pages > 0;
   if (p.chunk) kv_chunk_shape(group, &p.rows, &p.pitch, &p.tile, &p.extra);
-  else p.rows = p.pitch = kM, p.tile = kTile, p.extra = kExtra;
+  else p.rows = p.pitch = (int64_t)b->max_q * group <= 8 ? 8 : 16, p.tile = kTile, p.extra = kExtra;
   const int64_t blocks = ((int64_t)b->max_q * group + p.rows - 1) / p.rows;
   const int64_t tiles = (((int64_t)b->max_pages * c->page_size) + p.tile - 1) / p.tile;
   const int64_t most = (int64_t)b->n_seq * c->n_kv_heads * blocks * (tiles > 0 ? tiles : 1);
-  const int64_t cap = (int64_t)sm_count() * (p.chunk ? 1 : kCtasPerSm);
+  const int64_t cap = (int64_t)sm_count() * (p.chunk ? 1 : decode_ctas(c->head_dim, (c->flags & MQ_KV_INT8) != 0, p.rows / 8));
   p.workers = (int)(most < cap ? (most > 0 ? most : 1) : cap);
   return p;
 }
@@ -551,7 +603,7 @@ cudaError_t launch_join(const KvSchedArgs& a, const KvParts& parts, const KvOutA
 }  // namespace
 
 int launch_kv_combine(const KvSchedArgs& a, const KvParts& parts, const KvOutArgs& out, int workers, int dim, cudaStream_t st) {
-  const bool few = a.pitch == kM;
+  const bool few = a.pitch <= 16;
   const cudaError_t e = dim == 128 ? (few ? launch_join<128, 4>(a, parts, out, workers, st) : launch_join<128, 1>(a, parts, out, workers, st))
                                    : (few ? launch_join<64, 4>(a, parts, out, workers, st) : launch_join<64, 1>(a, parts, out, workers, st));
   if (e != cudaSuccess) return cuda_status(e);
@@ -587,13 +639,15 @@ extern "C" int mq_kv_attention(const void* Q, int64_t ldq, const mq_kv_batch* ba
   a.ldq = ldq * 2;
   a.sched.page_shift = a.cache.page_shift;
   a.sched.max_q = batch->max_q;
-  a.sched.group = n_q_heads / cache->n_kv_heads;
+  a.sched.group = fast_div(n_q_heads / cache->n_kv_heads);
+  a.sched.by_rows = fast_div(p.rows);
   a.sched.n_kv = cache->n_kv_heads;
   a.sched.rows = p.rows;
   a.sched.pitch = p.pitch;
   a.sched.tile = p.tile;
+  a.sched.tile_shift = 31 - __builtin_clz((unsigned)p.tile);
   a.sched.extra = p.extra;
-  a.sched.min_len = p.extra + 2;
+  a.sched.min_len = p.chunk ? p.extra + 2 : kMinLen;
   a.out.O = static_cast<__nv_bfloat16*>(O);
   a.out.ldo = ldo;
   a.out.lse = lse;

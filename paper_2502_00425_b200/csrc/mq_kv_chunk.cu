@@ -282,7 +282,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
     const int64_t share = sched_share(sc, total, gridDim.x);
     int64_t at = min(total, (int64_t)blockIdx.x * share);
     const int64_t stop = min(total, at + share);
-    const int group = sc.group, block_tokens = block_rows / group;
+    const int group = sc.group.d, block_tokens = block_rows / sc.group;
     KvRecord rec{};
     bool ok = true;
     int np = 0, nq[2] = {0, 0};
@@ -300,7 +300,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
         pc.ctx = u.s.n_all - u.s.n_new;
         pc.row0 = u.rb * sc.rows;
         pc.n_rows = min(sc.rows, u.s.n_new * group - pc.row0);
-        pc.all_see = sc.b.perm ? pc.ctx : min(pc.end, pc.ctx + pc.row0 / group + 1);
+        pc.all_see = sc.b.perm ? pc.ctx : min(pc.end, pc.ctx + pc.row0 / sc.group + 1);
         pc.b = u.b;
         pc.g = u.g;
         pc.begin = u.s.begin;
@@ -328,7 +328,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
 #pragma unroll
           for (int h = 0; h < kHalves; ++h)
             tma_load_3d(smem_u32(q_smem + k * kTileBytes + h * kHalfBytes), &tmap_q, h * 64, pc.g * group,
-                        pc.begin + pc.row0 / group + k * block_tokens, &sh->q_full[k]);
+                        pc.begin + pc.row0 / sc.group + k * block_tokens, &sh->q_full[k]);
         }
         __syncwarp();
         ++nq[k];
@@ -516,7 +516,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
       const float vsc = kI8 ? p.cache.v_scale[pc->g] : 1.0f;
       const float w = whole ? (l_run != 0.0f ? vsc / l_run : 0.0f) : vsc;
       const int64_t at_part = (int64_t)(2 * (int)blockIdx.x + (pc->t0 == 0 ? 1 : 0)) * kPitch + unit_row;
-      const int head = pc->g * sc.group + (pc->row0 + unit_row) % sc.group;
+      const int head = pc->g * sc.group.d + (pc->row0 + unit_row) - tok * sc.group.d;
       const int64_t out_row = (int64_t)(pc->begin + tok);
       const bool poison = !kI8 && *reinterpret_cast<const volatile int*>(&pc->poison) != 0;
 #pragma unroll 1
@@ -655,7 +655,7 @@ int launch(const KvAttnArgs& a, int workers, cudaStream_t st) {
   static PerDeviceTable<char> attr_set;
   if (!ensure_dynamic_smem(attr_set, kv_chunk_kernel<kD, kI8>, C::kSmem + (kMaxKvSeqs + 1) * (int)sizeof(int64_t))) return MQ_ERR_CUDA;
   CUtensorMap mq_{}, mk{}, mv{};
-  if (!encode_queries(&mq_, a.Q, a.ldq, a.out.n_q_heads, a.sched.b.total_q, a.sched.group, a.sched.rows / 2, kD)) return MQ_ERR_CUDA;
+  if (!encode_queries(&mq_, a.Q, a.ldq, a.out.n_q_heads, a.sched.b.total_q, a.sched.group.d, a.sched.rows / 2, kD)) return MQ_ERR_CUDA;
   if (!kI8 && (!encode_pages(&mk, a.cache.K, a.cache, kD, kTile) || !encode_pages(&mv, a.cache.V, a.cache, kD, kTile))) return MQ_ERR_CUDA;
   const cudaError_t e = launch_pdl(kv_chunk_kernel<kD, kI8>, dim3((unsigned)workers), dim3(C::kThreads),
                                    C::kSmem + ((size_t)a.sched.b.n_seq + 1) * sizeof(int64_t), st, mq_, mk, mv, a);

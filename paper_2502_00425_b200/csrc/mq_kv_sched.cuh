@@ -16,26 +16,28 @@ namespace mq {
 
 struct KvSchedArgs {
   KvBatchView b;
-  int page_shift, max_q, group, n_kv;
+  int page_shift, max_q, n_kv;
+  FastDiv group;   // query heads per key/value head
+  FastDiv by_rows; // `rows` as a divisor
   int rows;        // query rows of a unit
   int pitch;       // rows between the slots of partial results (at least `rows`)
-  int tile;        // keys of a tile
+  int tile, tile_shift;   // keys of a tile (a power of two)
   int extra;       // a unit's cost besides its tiles, in tiles
   int min_len;     // a worker's range is at least this long (fewer workers for little work)
 };
 
 // Keys [0, end) that row block rb of a sequence may see any of, and the tiles that hold them (at least one: a unit that
-// sees nothing still has to write its zeros).
+// sees nothing still has to write its zeros).  (Rows of a sequence, tokens x group, are below 2^30.)
 __device__ __forceinline__ int sched_end(const KvSchedArgs& a, const KvSeq& s, int rb) {
   if (a.b.perm) return s.n_all;
-  const int last = min((int)(((int64_t)rb * a.rows + a.rows - 1) / a.group), s.n_new - 1);
+  const int last = min((rb * a.rows + a.rows - 1) / a.group, s.n_new - 1);
   return max(0, min(s.n_all, s.n_all - s.n_new + last + 1));
 }
 __device__ __forceinline__ int sched_tiles(const KvSchedArgs& a, const KvSeq& s, int rb) {
-  return max(1, (sched_end(a, s, rb) + a.tile - 1) / a.tile);
+  return max(1, (sched_end(a, s, rb) + a.tile - 1) >> a.tile_shift);
 }
 __device__ __forceinline__ int sched_blocks(const KvSchedArgs& a, const KvSeq& s) {
-  return (int)(((int64_t)s.n_new * a.group + a.rows - 1) / a.rows);
+  return (s.n_new * a.group.d + a.rows - 1) / a.by_rows;
 }
 
 // prefix[b] = length of all units before sequence b; prefix[n_seq] = the whole line.  Called by every thread of a block of kThreads;
@@ -91,14 +93,21 @@ __device__ __forceinline__ KvUnit sched_unit(const KvSchedArgs& a, const int64_t
   KvUnit u;
   u.b = lo;
   u.s = kv_seq(a.b, a.page_shift, a.max_q, lo);
-  const int64_t per_head = (prefix[lo + 1] - prefix[lo]) / a.n_kv;
-  const int64_t x = at - prefix[lo];
-  u.g = (int)(x / per_head);
-  int64_t y = x - u.g * per_head;
+  const int64_t all = prefix[lo + 1] - prefix[lo], x = at - prefix[lo];
+  int64_t y;
+  if (all >> 31) {
+    const int64_t per_head = all / a.n_kv;
+    u.g = (int)(x / per_head);
+    y = x - u.g * per_head;
+  } else {   // (the usual case, in 32 bits)
+    const uint32_t per_head = (uint32_t)all / (uint32_t)a.n_kv;
+    u.g = (int)((uint32_t)x / per_head);
+    y = (uint32_t)x - (uint32_t)u.g * per_head;
+  }
   u.tiles = sched_tiles(a, u.s, 0);
   u.rb = 0;
   if (a.b.perm) {
-    u.rb = (int)(y / (u.tiles + a.extra));
+    if (y >= u.tiles + a.extra) u.rb = (int)(y / (u.tiles + a.extra));
     y -= (int64_t)u.rb * (u.tiles + a.extra);
   } else {
     while (y >= u.tiles + a.extra) {
@@ -112,8 +121,8 @@ __device__ __forceinline__ KvUnit sched_unit(const KvSchedArgs& a, const int64_t
 
 // Length of a worker's range: the line cut into at most `grid` equal ranges (the last one may be shorter or empty).
 __device__ __forceinline__ int64_t sched_share(const KvSchedArgs& a, int64_t total, int grid) {
-  const int64_t len = (total + grid - 1) / grid;
-  return len > a.min_len ? len : a.min_len;
+  if (total <= (int64_t)grid * a.min_len) return a.min_len;
+  return total >> 31 ? (total + grid - 1) / grid : (int64_t)(((uint32_t)total + (uint32_t)grid - 1u) / (uint32_t)grid);
 }
 
 // ---- partial results -----------------------------------------------------------------------------------
