@@ -1,10 +1,11 @@
 // Norm of every query and key head, rotary embedding and the store into the paged cache, in one pass:
 //   n = x / sqrt(mean(x^2) + eps) * gain;   y = n rotated by pos * base^(-2i / D);   Q_out, K_out, cache <- y, V
 // The pass is bound by its bytes (each of q, k, v read once and written once).  A head row of D channels is held by
-// D / 8 lanes (16 bytes each), so the sum of squares is a shuffle over those lanes and a row never leaves registers;
-// a warp loads all the head rows it will work on before it touches the first one.  The rotation's angle depends on
-// (token, pair) only: a lane always holds the same channels, so the sines and cosines are computed once per token and
-// warp and serve all of its heads, and the frequencies (doubles) are read once per thread.
+// D / 8 lanes, so the sum of squares is a shuffle over those lanes and a row never leaves registers; a lane's 8 channels
+// are four pairs: 16 contiguous bytes, or for pairs (i, i + D/2) two runs of 8 bytes, so that no pair crosses lanes.
+// A warp works on (a part of) a token: it loads several head rows before it touches the first one.  The rotation's angle
+// depends on (token, pair) only, and a lane always holds the same pairs: four sines and cosines per token serve all of
+// its heads (they cost as much as two head rows), and the frequencies (doubles) are read once per thread.
 // The angle in turns, pos * theta / (2 pi), is formed and reduced in double: in float32 a position of 100,000 would
 // leave an angle error of 4e-3.
 #include "mq_kv.cuh"
@@ -17,7 +18,9 @@ struct AppendParams {
   int64_t ldq, ldk, ldv;     // bytes
   uint8_t *Qo, *Ko;
   int64_t ldqo, ldko;        // bytes
-  int T, n_q, n_kv, n_items; // n_items: head-row groups per token
+  int T, n_q, n_kv;
+  int n_steps;               // steps of 32 lanes per token
+  int chunks, per_chunk;     // parts that a token's steps are cut into, and the steps of a part
   const float *gain_q, *gain_k;
   float eps;
   const int32_t* pos;
@@ -29,111 +32,131 @@ struct AppendParams {
 
 constexpr int kWarps = 8;
 
-// kD: head dimension; kHalf: pairs (i, i + D/2); kI8: int8 cache; kU: head-row groups a warp loads at once
+// kD: head dimension; kHalf: pairs (i, i + D/2); kI8: int8 cache; kU: steps of 32 lanes that a warp loads at once
 template <int kD, bool kHalf, bool kI8, int kU>
-__global__ void __launch_bounds__(kWarps * 32)
+__global__ void __launch_bounds__(kWarps * 32, kU > 1 ? 3 : 2)
 qk_norm_rope_kernel(const __grid_constant__ AppendParams p) {
   constexpr int kLanes = kD / 8;        // lanes per head row
-  constexpr int kRows = 32 / kLanes;    // head rows per warp step
-  constexpr int kAng = kHalf ? 8 : 4;   // angles a lane needs
+  constexpr int kRows = 32 / kLanes;    // head rows per step
+  // byte offsets of a lane's two runs of four channels
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int sub = lane % kLanes, sel = lane / kLanes;
-  double turns[kAng];
+  const int off0 = kHalf ? sub * 8 : sub * 16, off1 = kHalf ? kD + sub * 8 : sub * 16 + 8;
+  double turns[4];
 #pragma unroll
-  for (int e = 0; e < kAng; ++e) turns[e] = p.turns[kHalf ? (8 * sub + e) % (kD / 2) : 4 * sub + e];
+  for (int e = 0; e < 4; ++e) turns[e] = p.turns[4 * sub + e];
   pdl_wait();
-  float gq[8], gk[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    gq[e] = p.gain_q ? p.gain_q[8 * sub + e] : 1.0f;
-    gk[e] = p.gain_k ? p.gain_k[8 * sub + e] : 1.0f;
-  }
   const int n_rows = p.n_q + p.n_kv + (p.has_cache ? p.n_kv : 0);   // q heads, k heads, v heads of one token
-  const int chunks = (p.n_items + kU - 1) / kU;
-  const int64_t n_work = (int64_t)p.T * chunks;
+  const int64_t n_work = (int64_t)p.T * p.chunks;
   for (int64_t w = (int64_t)blockIdx.x * kWarps + warp; w < n_work; w += (int64_t)gridDim.x * kWarps) {
-    const int t = (int)(w / chunks), c = (int)(w % chunks);
-    uint4 x[kU];
+    const int t = p.chunks == 1 ? (int)w : (int)(w / p.chunks), part = p.chunks == 1 ? 0 : (int)(w - (int64_t)t * p.chunks);
+    const uint8_t *q_row = p.Q + (int64_t)t * p.ldq, *k_row = p.K + (int64_t)t * p.ldk, *v_row = p.V + (int64_t)t * p.ldv;
+    const int s_end = min(p.n_steps, (part + 1) * p.per_chunk);
+    float cs[4], sn[4];
+    bool stored = false;
+    int64_t row_off = 0;
+    for (int s0 = part * p.per_chunk; s0 < s_end; s0 += kU) {
+      uint2 x[kU][2];
 #pragma unroll
-    for (int u = 0; u < kU; ++u) {
-      const int h = (c * kU + u) * kRows + sel;
-      x[u] = make_uint4(0u, 0u, 0u, 0u);
-      const uint8_t* src = nullptr;
-      if (h < p.n_q) src = p.Q + (int64_t)t * p.ldq + (int64_t)h * (kD * 2);
-      else if (h < p.n_q + p.n_kv) src = p.K + (int64_t)t * p.ldk + (int64_t)(h - p.n_q) * (kD * 2);
-      else if (h < n_rows) src = p.V + (int64_t)t * p.ldv + (int64_t)(h - p.n_q - p.n_kv) * (kD * 2);
-      if (src) x[u] = *reinterpret_cast<const uint4*>(src + sub * 16);
-    }
-    const double pos = (double)p.pos[t];
-    int64_t slot = -1;
-    if (p.has_cache) slot = p.slots[t];
-    float cs[kAng], sn[kAng];
-#pragma unroll
-    for (int e = 0; e < kAng; ++e) {
-      const double rev = pos * turns[e];
-      sincospif(2.0f * (float)(rev - rint(rev)), &sn[e], &cs[e]);
-    }
-    const int64_t page = slot >> p.c.page_shift;
-    const bool stored = p.has_cache && slot >= 0 && page < p.c.n_pages;
-    const int64_t row_off = stored ? page * p.c.page_stride + (slot & ((1 << p.c.page_shift) - 1)) * p.c.slot_stride : 0;
-#pragma unroll
-    for (int u = 0; u < kU; ++u) {
-      const int h = (c * kU + u) * kRows + sel;
-      const uint32_t xw[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
-      float v[8];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) { v[2 * e] = kv_bf16_lo(xw[e]); v[2 * e + 1] = kv_bf16_hi(xw[e]); }
-      const bool is_q = h < p.n_q, is_k = !is_q && h < p.n_q + p.n_kv;
-      const bool norm = is_q ? p.gain_q != nullptr : is_k && p.gain_k != nullptr;
-      float ss = 0.0f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) ss = fmaf(v[e], v[e], ss);
-#pragma unroll
-      for (int o = kLanes / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-      if (norm) {
-        const float r = rsqrtf(ss * (1.0f / kD) + p.eps);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = v[e] * r * (is_q ? gq[e] : gk[e]);
-      }
-      float y[8];
-      if (kHalf) {
-        const bool second = sub >= kLanes / 2;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float mate = __shfl_xor_sync(0xffffffffu, v[e], kLanes / 2);
-          y[e] = second ? fmaf(mate, sn[e % kAng], v[e] * cs[e % kAng]) : fmaf(-mate, sn[e % kAng], v[e] * cs[e % kAng]);
+      for (int u = 0; u < kU; ++u) {
+        const int h = (s0 + u) * kRows + sel;
+        x[u][0] = x[u][1] = make_uint2(0u, 0u);
+        if (s0 + u < s_end && h < n_rows) {
+          const uint8_t* src = h < p.n_q ? q_row + h * (kD * 2)
+                               : h < p.n_q + p.n_kv ? k_row + (h - p.n_q) * (kD * 2) : v_row + (h - p.n_q - p.n_kv) * (kD * 2);
+          if (kHalf) {
+            x[u][0] = *reinterpret_cast<const uint2*>(src + off0);
+            x[u][1] = *reinterpret_cast<const uint2*>(src + off1);
+          } else {
+            const uint4 y = *reinterpret_cast<const uint4*>(src + off0);
+            x[u][0] = make_uint2(y.x, y.y);
+            x[u][1] = make_uint2(y.z, y.w);
+          }
         }
-      } else {
+      }
+      if (s0 == part * p.per_chunk) {   // (while the first loads are on their way)
+        const double pos = (double)p.pos[t];
+        const int64_t slot = p.has_cache ? p.slots[t] : -1;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          y[2 * e] = fmaf(-v[2 * e + 1], sn[e], v[2 * e] * cs[e]);
-          y[2 * e + 1] = fmaf(v[2 * e + 1], cs[e], v[2 * e] * sn[e]);
+          const double rev = pos * turns[e];
+          sincospif(2.0f * (float)(rev - rint(rev)), &sn[e], &cs[e]);
         }
+        const int64_t page = slot >> p.c.page_shift;
+        stored = slot >= 0 && page < p.c.n_pages;
+        row_off = stored ? page * p.c.page_stride + (slot & ((1 << p.c.page_shift) - 1)) * p.c.slot_stride : 0;
       }
-      if (!is_q && !is_k) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = v[e];
-      }
-      const uint4 o = make_uint4(kv_pack_bf16(y[0], y[1]), kv_pack_bf16(y[2], y[3]), kv_pack_bf16(y[4], y[5]), kv_pack_bf16(y[6], y[7]));
-      if (is_q) {
-        *reinterpret_cast<uint4*>(p.Qo + (int64_t)t * p.ldqo + (int64_t)h * (kD * 2) + sub * 16) = o;
-      } else if (h < n_rows) {
-        const int g = is_k ? h - p.n_q : h - p.n_q - p.n_kv;
-        if (is_k && p.Ko) *reinterpret_cast<uint4*>(p.Ko + (int64_t)t * p.ldko + (int64_t)g * (kD * 2) + sub * 16) = o;
-        if (stored) {
-          uint8_t* dst = const_cast<uint8_t*>(is_k ? p.c.K : p.c.V) + row_off + (int64_t)g * p.c.head_stride;
-          if (kI8) {
-            const float inv = 1.0f / (is_k ? p.c.k_scale[g] : p.c.v_scale[g]);
-            uint32_t q[2] = {0u, 0u};
+      for (int u = 0; u < kU; ++u) {
+        const int h = (s0 + u) * kRows + sel;
+        if (s0 + u >= s_end) continue;                       // (the same for all lanes)
+        const bool is_q = h < p.n_q, is_k = !is_q && h < p.n_q + p.n_kv;
+        float a[4], b[4];   // the pairs
+        if (kHalf) {
+          a[0] = kv_bf16_lo(x[u][0].x); a[1] = kv_bf16_hi(x[u][0].x); a[2] = kv_bf16_lo(x[u][0].y); a[3] = kv_bf16_hi(x[u][0].y);
+          b[0] = kv_bf16_lo(x[u][1].x); b[1] = kv_bf16_hi(x[u][1].x); b[2] = kv_bf16_lo(x[u][1].y); b[3] = kv_bf16_hi(x[u][1].y);
+        } else {
+          a[0] = kv_bf16_lo(x[u][0].x); b[0] = kv_bf16_hi(x[u][0].x); a[1] = kv_bf16_lo(x[u][0].y); b[1] = kv_bf16_hi(x[u][0].y);
+          a[2] = kv_bf16_lo(x[u][1].x); b[2] = kv_bf16_hi(x[u][1].x); a[3] = kv_bf16_lo(x[u][1].y); b[3] = kv_bf16_hi(x[u][1].y);
+        }
+        const float* gain = is_q ? p.gain_q : is_k ? p.gain_k : nullptr;
+        if (p.gain_q || p.gain_k) {                          // (the same for all lanes)
+          float ss = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const int code = max(-128, min(127, __float2int_rn(y[e] * inv)));
-              q[e >> 2] |= (uint32_t)(code & 255) << (8 * (e & 3));
-            }
-            *reinterpret_cast<uint2*>(dst + sub * 8) = make_uint2(q[0], q[1]);
+          for (int e = 0; e < 4; ++e) ss = fmaf(a[e], a[e], fmaf(b[e], b[e], ss));
+#pragma unroll
+          for (int o = kLanes / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+          if (gain) {
+            const float r = rsqrtf(ss * (1.0f / kD) + p.eps);
+            const float4 g0 = *reinterpret_cast<const float4*>(gain + off0 / 2), g1 = *reinterpret_cast<const float4*>(gain + off1 / 2);
+            const float ga[4] = {g0.x, kHalf ? g0.y : g0.z, kHalf ? g0.z : g1.x, kHalf ? g0.w : g1.z};
+            const float gb[4] = {kHalf ? g1.x : g0.y, kHalf ? g1.y : g0.w, kHalf ? g1.z : g1.y, g1.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { a[e] *= r * ga[e]; b[e] *= r * gb[e]; }
+          }
+        }
+        if (is_q || is_k) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float y = fmaf(-b[e], sn[e], a[e] * cs[e]);
+            b[e] = fmaf(b[e], cs[e], a[e] * sn[e]);
+            a[e] = y;
+          }
+        }
+        if (h >= n_rows) continue;
+        const uint2 o0 = kHalf ? make_uint2(kv_pack_bf16(a[0], a[1]), kv_pack_bf16(a[2], a[3])) : make_uint2(kv_pack_bf16(a[0], b[0]), kv_pack_bf16(a[1], b[1]));
+        const uint2 o1 = kHalf ? make_uint2(kv_pack_bf16(b[0], b[1]), kv_pack_bf16(b[2], b[3])) : make_uint2(kv_pack_bf16(a[2], b[2]), kv_pack_bf16(a[3], b[3]));
+        auto put = [&](uint8_t* dst) {
+          if (kHalf) {
+            *reinterpret_cast<uint2*>(dst + off0) = o0;
+            *reinterpret_cast<uint2*>(dst + off1) = o1;
           } else {
-            *reinterpret_cast<uint4*>(dst + sub * 16) = o;
+            *reinterpret_cast<uint4*>(dst + off0) = make_uint4(o0.x, o0.y, o1.x, o1.y);
+          }
+        };
+        if (is_q) {
+          put(p.Qo + (int64_t)t * p.ldqo + h * (kD * 2));
+        } else {
+          const int g = is_k ? h - p.n_q : h - p.n_q - p.n_kv;
+          if (is_k && p.Ko) put(p.Ko + (int64_t)t * p.ldko + g * (kD * 2));
+          if (stored) {
+            uint8_t* dst = const_cast<uint8_t*>(is_k ? p.c.K : p.c.V) + row_off + (int64_t)g * p.c.head_stride;
+            if (kI8) {
+              const float inv = 1.0f / (is_k ? p.c.k_scale[g] : p.c.v_scale[g]);
+              auto code = [&](float y) { return (uint32_t)max(-128, min(127, __float2int_rn(y * inv))) & 255u; };
+              uint32_t ca[4], cb[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) { ca[e] = code(a[e]); cb[e] = code(b[e]); }
+              if (kHalf) {
+                *reinterpret_cast<uint32_t*>(dst + off0 / 2) = ca[0] | ca[1] << 8 | ca[2] << 16 | ca[3] << 24;
+                *reinterpret_cast<uint32_t*>(dst + off1 / 2) = cb[0] | cb[1] << 8 | cb[2] << 16 | cb[3] << 24;
+              } else {
+                *reinterpret_cast<uint2*>(dst + off0 / 2) = make_uint2(ca[0] | cb[0] << 8 | ca[1] << 16 | cb[1] << 24, ca[2] | cb[2] << 8 | ca[3] << 16 | cb[3] << 24);
+              }
+            } else {
+              put(dst);
+            }
           }
         }
       }
@@ -145,14 +168,16 @@ template <int kD, bool kHalf, bool kI8>
 int launch(AppendParams& p, cudaStream_t st) {
   const int rows = p.n_q + p.n_kv * (p.has_cache ? 2 : 1);
   constexpr int per = 32 / (kD / 8);
-  p.n_items = (rows + per - 1) / per;
+  p.n_steps = (rows + per - 1) / per;
   const int sms = sm_count();
-  // few tokens: one head-row group per warp, so that the call is one latency long; many: six loads in flight per lane
-  const bool wide = (int64_t)p.T * p.n_items > (int64_t)sms * 64;
-  const int64_t work = (int64_t)p.T * (wide ? (p.n_items + 5) / 6 : p.n_items);
-  const int64_t blocks = (work + kWarps - 1) / kWarps;
-  const unsigned grid = (unsigned)(blocks < (int64_t)sms * 8 ? blocks : (int64_t)sms * 8);
-  const cudaError_t e = wide ? launch_pdl(qk_norm_rope_kernel<kD, kHalf, kI8, 6>, dim3(grid), dim3(kWarps * 32), 0, st, p)
+  // few tokens: one step per warp, so that the call is one latency long; many: a warp takes a token, or half of one where
+  // that leaves the last warps less to wait for, with four steps in flight
+  const bool wide = (int64_t)p.T * p.n_steps > (int64_t)sms * 64;
+  p.chunks = !wide ? p.n_steps : p.n_steps > 8 ? 2 : 1;
+  p.per_chunk = (p.n_steps + p.chunks - 1) / p.chunks;
+  const int64_t blocks = ((int64_t)p.T * p.chunks + kWarps - 1) / kWarps, most = (int64_t)sms * 3;
+  const unsigned grid = (unsigned)(!wide || blocks < most ? blocks : most);
+  const cudaError_t e = wide ? launch_pdl(qk_norm_rope_kernel<kD, kHalf, kI8, 4>, dim3(grid), dim3(kWarps * 32), 0, st, p)
                              : launch_pdl(qk_norm_rope_kernel<kD, kHalf, kI8, 1>, dim3(grid), dim3(kWarps * 32), 0, st, p);
   if (e != cudaSuccess) return cuda_status(e);
   return cuda_status(cudaGetLastError());

@@ -23,7 +23,7 @@ namespace {
 constexpr int kWarps = 4;
 constexpr int kTile = 16 * kWarps; // keys of a tile: 16 per warp
 constexpr int kThreads = kWarps * 32;
-constexpr int kExtra = 3;         // what a unit costs besides its tiles, in tiles
+constexpr int kExtra = 4;         // what a unit costs besides its tiles, in tiles
 constexpr int kMinLen = 2;        // a worker's least share of the line
 // fp16 probabilities reach down to 2^-24 only: with the reference 14 below the maximum they run up to 2^14 instead of 1, and
 // what is lost below is 2^-39 of the largest one (a sum over them stays in float32 either way).
