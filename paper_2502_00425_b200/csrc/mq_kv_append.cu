@@ -34,7 +34,7 @@ constexpr int kWarps = 8;
 
 // kD: head dimension; kHalf: pairs (i, i + D/2); kI8: int8 cache; kU: steps of 32 lanes that a warp loads at once
 template <int kD, bool kHalf, bool kI8, int kU>
-__global__ void __launch_bounds__(kWarps * 32, kU > 1 ? 3 : 2)
+__global__ void __launch_bounds__(kWarps * 32, kU > 1 ? 4 : 2)
 qk_norm_rope_kernel(const __grid_constant__ AppendParams p) {
   constexpr int kLanes = kD / 8;        // lanes per head row
   constexpr int kRows = 32 / kLanes;    // head rows per step
@@ -175,7 +175,7 @@ int launch(AppendParams& p, cudaStream_t st) {
   const bool wide = (int64_t)p.T * p.n_steps > (int64_t)sms * 64;
   p.chunks = !wide ? p.n_steps : p.n_steps > 8 ? 2 : 1;
   p.per_chunk = (p.n_steps + p.chunks - 1) / p.chunks;
-  const int64_t blocks = ((int64_t)p.T * p.chunks + kWarps - 1) / kWarps, most = (int64_t)sms * 3;
+  const int64_t blocks = ((int64_t)p.T * p.chunks + kWarps - 1) / kWarps, most = (int64_t)sms * 4;
   const unsigned grid = (unsigned)(!wide || blocks < most ? blocks : most);
   const cudaError_t e = wide ? launch_pdl(qk_norm_rope_kernel<kD, kHalf, kI8, 4>, dim3(grid), dim3(kWarps * 32), 0, st, p)
                              : launch_pdl(qk_norm_rope_kernel<kD, kHalf, kI8, 1>, dim3(grid), dim3(kWarps * 32), 0, st, p);

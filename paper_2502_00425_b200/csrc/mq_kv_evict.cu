@@ -3,8 +3,9 @@
 // budget is full; the kept rows move, in their order, to fresh pages.
 //
 // Two kernels.  Selection: one CTA per (sequence, head) finds the weight of the last kept key exactly by a radix select
-// over the weights' order-preserving integer images (12, 10 and 10 bits; three passes that hit L2 after the first),
-// and a fourth pass writes the kept indices in order with block-wide prefix counts.  Copy: 16-byte pieces of all kept
+// over the weights' order-preserving integer images (12, 10 and 10 bits), then writes the kept indices in order with
+// block-wide prefix counts.  The images of up to kHeld keys stay in shared memory (the weights are read once, and two CTAs
+// fit an SM); longer sequences are read again for each pass.  Copy: 16-byte pieces of all kept
 // rows of the batch, many in flight per thread; this is what the call's bytes are.
 #include "mq_kv.cuh"
 
@@ -12,6 +13,7 @@ namespace mq {
 namespace {
 
 constexpr int kSelThreads = 1024;
+constexpr int kSelWarps = kSelThreads / 32;
 constexpr int kBins = 4096;
 
 struct EvictParams {
@@ -53,7 +55,8 @@ __device__ __forceinline__ uint32_t block_prefix(uint32_t v, uint32_t* red, uint
   }
   if (lane == 31) red[warp] = inc;
   __syncthreads();
-  uint32_t w = red[lane], winc = w;
+  const uint32_t w = lane < kSelWarps ? red[lane] : 0u;
+  uint32_t winc = w;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const uint32_t y = __shfl_up_sync(0xffffffffu, winc, o);
@@ -65,14 +68,18 @@ __device__ __forceinline__ uint32_t block_prefix(uint32_t v, uint32_t* red, uint
   return base + inc - v;
 }
 
-__global__ void __launch_bounds__(kSelThreads)
-kv_select_kernel(const __grid_constant__ EvictParams p) {
-  __shared__ uint32_t hist[kBins];
+constexpr int kHeld = 24576;   // images kept in shared memory: 96 KB, two CTAs to an SM
+
+__global__ void __launch_bounds__(kSelThreads, 2)
+kv_select_kernel(const __grid_constant__ EvictParams p, const int held_most) {
+  extern __shared__ __align__(16) uint32_t img[];   // [held_most rounded up to 4]
+  __shared__ __align__(16) uint32_t hist[kBins];
   __shared__ uint32_t red[32];
   __shared__ uint32_t found[2];
-  pdl_launch_dependents();
+  const int g = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  reinterpret_cast<uint4*>(hist)[tid] = make_uint4(0u, 0u, 0u, 0u);
   pdl_wait();
-  const int g = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
+  pdl_launch_dependents();   // (behind the wait: the copy kernel reads lengths and tables before its own)
   const int n = evict_len(p, b), m = min(n, p.budget);
   const float* w = p.W + (int64_t)b * p.w_seq + (int64_t)g * p.w_head;
   const int64_t out = ((int64_t)b * p.src.n_kv_heads + g) * p.budget;
@@ -86,33 +93,47 @@ kv_select_kernel(const __grid_constant__ EvictParams p) {
   }
   const int lo = p.n_first, hi = n - p.n_last;     // the keys that compete
   uint32_t need = (uint32_t)(p.budget - p.n_first - p.n_last);   // how many of them stay; < hi - lo
+  const bool held = n <= held_most;
   uint32_t prefix = 0u, known = 0u;                // the bits of the last kept image found so far
-  const int shifts[3] = {20, 10, 0}, widths[3] = {12, 10, 10};
+  __syncthreads();                                 // the bins are zero
+  // the first pass counts while it reads the weights
+  for (int j0 = tid; j0 < n; j0 += 4 * kSelThreads) {
+    float v[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) v[c] = j0 + c * kSelThreads < n ? w[j0 + c * kSelThreads] : 0.0f;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const int j = j0 + c * kSelThreads;
+      if (j >= n) break;
+      const uint32_t u = image(v[c]);
+      if (held) img[j] = u;
+      if (j >= lo && j < hi) atomicAdd(&hist[u >> 20], 1u);
+    }
+  }
+  __syncthreads();
   if (need > 0) {
 #pragma unroll 1
     for (int pass = 0; pass < 3; ++pass) {
-      const int shift = shifts[pass];
-      const uint32_t bins = 1u << widths[pass];
-      for (uint32_t i = tid; i < bins; i += kSelThreads) hist[i] = 0u;
-      __syncthreads();
-      for (int j0 = lo + tid; j0 < hi; j0 += 4 * kSelThreads) {
-        float v[4];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) v[c] = j0 + c * kSelThreads < hi ? w[j0 + c * kSelThreads] : 0.0f;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const uint32_t u = image(v[c]);
-          if (j0 + c * kSelThreads < hi && (u & known) == prefix) atomicAdd(&hist[(u >> shift) & (bins - 1u)], 1u);
+      const int shift = pass == 0 ? 20 : pass == 1 ? 10 : 0;
+      const uint32_t bins = pass == 0 ? 4096u : 1024u;
+      if (pass > 0) {
+        for (int j = lo + tid; j < hi; j += kSelThreads) {
+          const uint32_t u = held ? img[j] : image(w[j]);
+          if ((u & known) == prefix) atomicAdd(&hist[(u >> shift) & 1023u], 1u);
         }
+        __syncthreads();
       }
-      __syncthreads();
-      // from the largest bin down: the bin in which the count reaches `need`
-      const int per = (int)bins / kSelThreads;   // 4 or 1
-      uint32_t mine = 0u;
-      for (int c = 0; c < per; ++c) mine += hist[bins - 1u - (uint32_t)(tid * per + c)];
-      // (counts may pass 16 bits: a plain 32-bit scan)
+      // from the largest bin down: the bin in which the count reaches `need`.  A thread has 4 bins, or 1.
+      uint32_t h[4] = {0u, 0u, 0u, 0u};
+      const uint32_t bin0 = pass == 0 ? 4095u - 4u * (uint32_t)tid : 1023u - (uint32_t)tid;   // its largest bin
+      if (pass == 0) {
+        const uint4 x = reinterpret_cast<const uint4*>(hist)[kSelThreads - 1 - tid];
+        h[0] = x.w; h[1] = x.z; h[2] = x.y; h[3] = x.x;
+      } else {
+        h[0] = hist[bin0];
+      }
+      const uint32_t mine = h[0] + h[1] + h[2] + h[3];
       uint32_t inc = mine;
-      const int lane = tid & 31, warp = tid >> 5;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const uint32_t y = __shfl_up_sync(0xffffffffu, inc, o);
@@ -120,45 +141,54 @@ kv_select_kernel(const __grid_constant__ EvictParams p) {
       }
       if (lane == 31) red[warp] = inc;
       __syncthreads();
-      uint32_t before = inc - mine;
-      for (int x = 0; x < warp; ++x) before += red[x];
+      const uint32_t sum = red[lane];            // warp sums, scanned by every warp
+      uint32_t before = sum;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t y = __shfl_up_sync(0xffffffffu, before, o);
+        if (lane >= o) before += y;
+      }
+      before = __shfl_sync(0xffffffffu, before - sum, warp) + inc - mine;
       if (before < need && before + mine >= need) {
         uint32_t acc = before;
-        for (int c = 0; c < per; ++c) {
-          const uint32_t bin = bins - 1u - (uint32_t)(tid * per + c), h = hist[bin];
-          if (acc + h >= need) {
-            found[0] = bin;
+#pragma unroll
+        for (uint32_t c = 0; c < 4u; ++c) {
+          if (acc < need && acc + h[c] >= need) {
+            found[0] = bin0 - c;
             found[1] = need - acc;
-            break;
           }
-          acc += h;
+          acc += h[c];
         }
       }
+      if (pass < 2) hist[tid] = 0u;              // (every thread has read its bins; the next pass has 1024 of them)
       __syncthreads();
       prefix |= found[0] << shift;
       known |= (bins - 1u) << shift;
       need = found[1];
-      __syncthreads();
     }
   }
   // every competing key with an image above `prefix` stays, and the first `need` of those equal to it (need = 0: none do)
   const bool any = known != 0u;
-  uint32_t above = 0u, equal = 0u;   // counts before this tile
-  for (int j0 = 0; j0 < n; j0 += 4 * kSelThreads) {
-    uint32_t cls = 0u, cnt = 0u;
-    float v[4];
+  uint32_t above = 0u, equal = 0u;   // counts before these keys
+  for (int j0 = tid * 4; j0 - tid * 4 < n; j0 += 4 * kSelThreads) {
+    uint32_t u[4] = {0u, 0u, 0u, 0u};
+    if (held) {
+      if (j0 < n) {
+        const uint4 x = *reinterpret_cast<const uint4*>(img + j0);
+        u[0] = x.x; u[1] = x.y; u[2] = x.z; u[3] = x.w;
+      }
+    } else {
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const int j = j0 + tid * 4 + c;
-      v[c] = j < n ? w[j] : 0.0f;
+      for (int c = 0; c < 4; ++c)
+        if (j0 + c < n) u[c] = image(w[j0 + c]);
     }
+    uint32_t cls = 0u, cnt = 0u;
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
-      const int j = j0 + tid * 4 + c;
+      const int j = j0 + c;
       if (j >= n) continue;
-      const uint32_t u = image(v[c]);
-      if (j < lo || j >= hi || (any && u > prefix)) { cls |= 1u << (2 * c); cnt += 1u; }
-      else if (any && u == prefix) { cls |= 2u << (2 * c); cnt += 1u << 16; }
+      if (j < lo || j >= hi || (any && u[c] > prefix)) { cls |= 1u << (2 * c); cnt += 1u; }
+      else if (any && u[c] == prefix) { cls |= 2u << (2 * c); cnt += 1u << 16; }
     }
     uint32_t total;
     const uint32_t pre = block_prefix(cnt, red, total);
@@ -168,8 +198,8 @@ kv_select_kernel(const __grid_constant__ EvictParams p) {
       const uint32_t k = (cls >> (2 * c)) & 3u;
       if (k == 1u || (k == 2u && e < need)) {
         const int64_t at = out + a + min(e, need);
-        p.kept[at] = j0 + tid * 4 + c;
-        if (p.W_out) p.W_out[at] = v[c];
+        p.kept[at] = j0 + c;
+        if (p.W_out) p.W_out[at] = w[j0 + c];
       }
       if (k == 1u) ++a;
       if (k == 2u) ++e;
@@ -187,12 +217,14 @@ template <int kRowBytes>
 __global__ void __launch_bounds__(kCopyThreads)
 kv_copy_kernel(const __grid_constant__ EvictParams p) {
   constexpr int kPieces = kRowBytes / 16, kPerCta = kCopyThreads / kPieces;   // rows per CTA and step
-  pdl_launch_dependents();
-  pdl_wait();
+  // What came before the selection is complete once this kernel runs (every CTA of the selection has passed its own wait before
+  // it lets this one start); only the kept indices have to be waited for.
   const int b = blockIdx.z, g = blockIdx.y;
   const int m = min(evict_len(p, b), p.budget);
   const int pc = (int)threadIdx.x % kPieces, r = (int)threadIdx.x / kPieces;
   const int32_t* kept = p.kept + ((int64_t)b * p.src.n_kv_heads + g) * p.budget;
+  pdl_launch_dependents();
+  pdl_wait();
   for (int i0 = blockIdx.x * kPerCta * kCopyRows; i0 < m; i0 += gridDim.x * kPerCta * kCopyRows) {
     uint4 k[kCopyRows], v[kCopyRows];
     int64_t to[kCopyRows];
@@ -259,7 +291,12 @@ extern "C" int mq_kv_evict(const mq_kv_cache* cache, const int32_t* page_table, 
   p.dst_table = dst_table; p.dst_max_pages = dst_max_pages;
   p.kept = kept; p.new_len = new_len; p.W_out = W_out;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  cudaError_t e = launch_pdl(kv_select_kernel, dim3((unsigned)cache->n_kv_heads, (unsigned)n_seq), dim3(kSelThreads), 0, st, p);
+  static PerDeviceTable<char> attr_set;
+  if (!ensure_dynamic_smem(attr_set, kv_select_kernel, kHeld * 4)) return MQ_ERR_CUDA;
+  const int64_t reach = (int64_t)max_pages * cache->page_size;
+  const int held = reach <= budget ? 0 : reach < kHeld ? (int)reach : kHeld;
+  cudaError_t e = launch_pdl(kv_select_kernel, dim3((unsigned)cache->n_kv_heads, (unsigned)n_seq), dim3(kSelThreads), (size_t)align_up(held, 4) * 4, st,
+                             p, held);
   if (e == cudaSuccess && budget > 0)
     e = p.dim_bytes == 256 ? launch_copy<256>(p, st) : p.dim_bytes == 128 ? launch_copy<128>(p, st) : launch_copy<64>(p, st);
   if (e != cudaSuccess) return cuda_status(e);
