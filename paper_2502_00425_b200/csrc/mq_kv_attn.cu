@@ -4,9 +4,9 @@
 //
 // The kernel of this file is the one for few query rows (decode steps): it is bound by reading K and V once.  A unit is 8
 // or 16 query rows (tokens x the query heads of one key/value head), so a key is read once for the whole group.
-//   * A warp is on its own: it streams 16 keys at a time (K and V rows, 16-byte asynchronous copies straight from the
-//     pages, two or more tiles in flight) into its own ring in shared memory and runs a complete online softmax over
-//     them on mma.sync; there is no block-wide barrier until the four warps' results are joined at the end of a range.
+//   * A warp is on its own: it streams 16 keys at a time (K and V rows by TMA straight from the pages, one lane asking, two or
+//     more tiles in flight) into its own ring in shared memory and runs a complete online softmax over them on
+//     mma.sync; there is no block-wide barrier until the four warps' results are joined at the end of a range.
 //     Tensor-core throughput is no concern here: at the cache's rate an SM sees 16 keys in about 190 cycles.
 //   * Both products are taken transposed, S^T = K Q^T and O^T = V^T P^T: the 16 keys, and 16 channels, are the rows of the
 //     instruction's tile and the query rows its 8 columns, so a group of up to 8 heads wastes nothing.  P^T changes from
@@ -15,14 +15,12 @@
 //   * An int8 cache is read as codes and widened in registers to fp16 exactly (the products' sums do not care in which
 //     order the channels come, so a thread takes contiguous codes); the scales multiply the scores and the result.
 //     Queries are scaled by a power of two per row so that fp16 holds them with all their bits.
-#include "mq_kv_sched.cuh"
+#include "mq_kv_warp.cuh"
 
 namespace mq {
 namespace {
 
-constexpr int kWarps = 4;
-constexpr int kTile = 16 * kWarps; // keys of a tile: 16 per warp
-constexpr int kThreads = kWarps * 32;
+constexpr int kWarps = kStreamWarps, kThreads = kStreamThreads, kTile = kStreamTile;
 constexpr int kExtra = 4;         // what a unit costs besides its tiles, in tiles
 constexpr int kMinLen = 2;        // a worker's least share of the line
 // fp16 probabilities reach down to 2^-24 only: with the reference 14 below the maximum they run up to 2^14 instead of 1, and
@@ -33,50 +31,51 @@ constexpr float kLiftF16 = 14.0f;
 template <int kD, bool kI8, int kN>
 struct Cfg {
   static constexpr int kRows = 8 * kN;
-  static constexpr int kRow = kD * (kI8 ? 1 : 2);        // bytes of a cached row
-  static constexpr int kStage = 16 * kRow * 2;           // K and V of 16 keys
+  static constexpr int kStage = 2 * KeyTile<kD, kI8>::kBytes;   // K and V of 16 keys
   static constexpr int kCtas = kStage == 8192 ? 2 : kN == 1 ? 4 : 3;   // per SM
   static constexpr int kStages = kStage == 2048 ? 4 : 3;
   static constexpr int kRing = kStage * kStages;
   static constexpr int kPitch = kD + 4;                  // floats between rows of the warps' results
-  static constexpr int kSmem = kWarps * kRing;
-  static_assert(kSmem >= kWarps * kRows * kPitch * 4, "the join of the warps reuses the rings");
+  static constexpr int kSmem = 1024 + kWarps * kRing;    // (swizzled tiles stand on 1024-byte boundaries)
+  static_assert(kWarps * kRing >= kWarps * kRows * kPitch * 4, "the join of the warps reuses the rings");
 };
 constexpr int decode_ctas(int dim, bool i8, int n) {
   return dim == 128 ? (i8 ? (n == 1 ? Cfg<128, true, 1>::kCtas : Cfg<128, true, 2>::kCtas) : (n == 1 ? Cfg<128, false, 1>::kCtas : Cfg<128, false, 2>::kCtas))
                     : (i8 ? (n == 1 ? Cfg<64, true, 1>::kCtas : Cfg<64, true, 2>::kCtas) : (n == 1 ? Cfg<64, false, 1>::kCtas : Cfg<64, false, 2>::kCtas));
 }
 
-// Offset of 16-byte piece c of row r in a tile: pieces are exchanged within 128-byte lines so that the eight rows that
-// one load instruction touches lie in different banks.
-template <int kRow>
-__device__ __forceinline__ uint32_t piece(int r, int c) {
-  const uint32_t off = (uint32_t)r * kRow + (uint32_t)c * 16u;
-  const uint32_t key = kRow >= 128 ? (uint32_t)r & 7u : ((uint32_t)r >> 1) & 7u;
-  return off ^ (key << 4);
-}
-
 template <int kD, bool kI8, int kN>
 __global__ void __launch_bounds__(kThreads, (Cfg<kD, kI8, kN>::kCtas))
-kv_decode_kernel(const __grid_constant__ KvAttnArgs p) {
+kv_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ KvAttnArgs p) {
   using C = Cfg<kD, kI8, kN>;
-  constexpr int kRow = C::kRow, kPieces = kRow / 16, kSteps = kD / 16, kRows = C::kRows;
+  using T = KeyTile<kD, kI8>;
+  constexpr int kSteps = kD / 16, kRows = C::kRows;
   constexpr float kLift = kI8 ? kLiftF16 : 0.0f;   // m: the exponents' reference, the running maximum less this
-  extern __shared__ __align__(128) uint8_t smem[];
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  __shared__ uint64_t full[kWarps][C::kStages];   // a tile has landed
+  __shared__ int abort_flag;
   __shared__ float ml_s[kWarps][kRows][2];
   __shared__ int64_t red[kWarps];
-  int64_t* prefix = reinterpret_cast<int64_t*>(smem + C::kSmem);
+  int64_t* prefix = reinterpret_cast<int64_t*>(smem + kWarps * C::kRing);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quad = lane >> 2, t4 = lane & 3;
+  if (threadIdx.x == 0) {
+    abort_flag = 0;
+    for (int i = 0; i < kWarps * C::kStages; ++i) mbar_init(&full[0][0] + i, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
   pdl_launch_dependents();
   pdl_wait();
   const KvSchedArgs& sc = p.sched;
   sched_prefix<kThreads>(sc, prefix, red);
   const int64_t total = prefix[sc.b.n_seq];
   const int64_t share = sched_share(sc, total, gridDim.x);
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quad = lane >> 2, t4 = lane & 3;
   KvRecord rec{};
   int64_t at = min(total, (int64_t)blockIdx.x * share);
   const int64_t stop = min(total, at + share);
   const uint32_t ring = kv_smem_u32(smem) + (uint32_t)(warp * C::kRing);
+  uint32_t asked = 0, taken = 0;   // tiles of this warp so far (ring positions and phases run on over units)
+  bool ok = true;
   while (at < stop) {
     const KvUnit u = sched_unit(sc, prefix, at);
     const int len = (int)min((int64_t)(u.tiles + sc.extra - u.skip), stop - at);   // of this range on the line
@@ -87,48 +86,32 @@ kv_decode_kernel(const __grid_constant__ KvAttnArgs p) {
     const int end = sched_end(sc, u.s, u.rb), ctx = u.s.n_all - u.s.n_new;
     const int row0 = u.rb * kRows, n_rows = min(kRows, u.s.n_new * sc.group.d - row0);
     const int32_t* table = sc.b.page_table + (int64_t)u.b * sc.b.max_pages;
-    const int64_t head_off = (int64_t)u.g * p.cache.head_stride;
 
-    // ---- the warp's stream of tiles: tile t holds keys (t * kWarps + warp) * 16 ..
-    const int n_my = t1 - t0;
-    auto page_of = [&](int i) -> int {   // the page of the i-th tile of this range, -1 where it holds no visible key
-      const int key0 = ((t0 + i) * kWarps + warp) * 16;
-      return i < n_my && key0 < end ? table[key0 >> p.cache.page_shift] : -1;
-    };
-    auto issue = [&](int i, int stage, int page) {
-      if (i < n_my) {
-        const int key0 = ((t0 + i) * kWarps + warp) * 16;
-        int n_ok = min(max(end - key0, 0), 16);
-        if (n_ok > 0 && (unsigned)page >= (unsigned)p.cache.n_pages) {
-          n_ok = 0;
-          if (lane == 0) atomicCAS(p.status, MQ_OK, MQ_ERR_INVALID_ARG);
+    // ---- the warp's stream of tiles: tile t holds keys (t * kWarps + warp) * 16 ..; tiles behind the last key are not asked for
+    const int first_key = (t0 * kWarps + warp) * 16;
+    const int n_my = min(t1 - t0, end > first_key ? (end - first_key + kTile - 1) / kTile : 0);
+    auto page_of = [&](int i) -> int { return i < n_my ? table[(first_key + i * kTile) >> p.cache.page_shift] : 0; };
+    auto ask = [&](int i, int page) {
+      if (i >= n_my) return;
+      if (lane == 0) {
+        if ((unsigned)page >= (unsigned)p.cache.n_pages) {
+          page = max(p.cache.n_pages, 1);   // a page number the maps do not have: zeros
+          atomicCAS(p.status, MQ_OK, MQ_ERR_INVALID_ARG);
         }
-        constexpr int kCopies = 16 * kPieces / 32, kStep = 32 / kPieces;   // rows of one instruction
-        const int r0 = lane / kPieces, pc = lane % kPieces;
-        const int64_t off = n_ok > 0 ? (int64_t)page * p.cache.page_stride + head_off +
-                                           (int64_t)((key0 & ((1 << p.cache.page_shift) - 1)) + r0) * p.cache.slot_stride + pc * 16
-                                     : 0;
-        const uint8_t *ks = p.cache.K + off, *vs = p.cache.V + off;
-        const uint32_t dst = ring + (uint32_t)(stage * C::kStage);
-#pragma unroll
-        for (int c = 0; c < kCopies; ++c) {
-          const int r = c * kStep + r0;
-          const bool ok = r < n_ok;
-          const uint32_t d = dst + piece<kRow>(r, pc);
-          cp_async16(d, ok ? ks : p.Q, ok ? 16u : 0u);
-          cp_async16(d + 16 * kRow, ok ? vs : p.Q, ok ? 16u : 0u);
-          ks += kStep * p.cache.slot_stride;
-          vs += kStep * p.cache.slot_stride;
-        }
+        const int s = (int)(asked % C::kStages), slot = (first_key + i * kTile) & ((1 << p.cache.page_shift) - 1);
+        const uint32_t dst = ring + (uint32_t)(s * C::kStage);
+        mbar_arrive_expect_tx(&full[warp][s], C::kStage);
+        T::load(dst, &tmap_k, slot, u.g, page, &full[warp][s]);
+        T::load(dst + T::kBytes, &tmap_v, slot, u.g, page, &full[warp][s]);
       }
-      cp_async_commit();
+      ++asked;
     };
     int page_next = page_of(0);
 #pragma unroll
     for (int i = 0; i < C::kStages - 1; ++i) {
       const int pg = page_next;
       page_next = page_of(i + 1);
-      issue(i, i, pg);
+      ask(i, pg);
     }
 
     // ---- query fragments (B operand): column quad of block nt is row 8 nt + quad of the unit
@@ -140,40 +123,9 @@ kv_decode_kernel(const __grid_constant__ KvAttnArgs p) {
 #pragma unroll
     for (int nt = 0; nt < kN; ++nt) {
       const int r = 8 * nt + quad;
-      const bool ok = r < n_rows;
       const int tok = (row0 + r) / sc.group;
-      const uint8_t* q = p.Q + (int64_t)(u.s.begin + tok) * p.ldq + (int64_t)(u.g * sc.group.d + (row0 + r) - tok * sc.group.d) * (kD * 2);
-      if (!kI8) {
-#pragma unroll
-        for (int k = 0; k < kSteps; ++k) {
-          const int c = (k * 16 + 2 * t4) * 2;
-          qf[nt][k][0] = ok ? *reinterpret_cast<const uint32_t*>(q + c) : 0u;
-          qf[nt][k][1] = ok ? *reinterpret_cast<const uint32_t*>(q + c + 16) : 0u;
-        }
-        fac[nt][0] = fac[nt][1] = base_fac;
-      } else {
-        // channel order of the product: step k, position (2 t4, 2 t4 + 1, 2 t4 + 8, 2 t4 + 9) is channel t4 * D/4 + 4 k + 0 .. 3
-        uint2 w[kSteps];
-        float m = 0.0f;
-#pragma unroll
-        for (int k = 0; k < kSteps; ++k) {
-          w[k] = ok ? *reinterpret_cast<const uint2*>(q + (t4 * (kD / 4) + 4 * k) * 2) : make_uint2(0u, 0u);
-          m = fmaxf(m, fmaxf(fmaxf(fabsf(kv_bf16_lo(w[k].x)), fabsf(kv_bf16_hi(w[k].x))),
-                             fmaxf(fabsf(kv_bf16_lo(w[k].y)), fabsf(kv_bf16_hi(w[k].y)))));
-        }
-        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
-        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
-        // the power of two that brings the row's largest magnitude into [1, 2) (an infinity stays one either way)
-        const int e = m > 0.0f && m < INFINITY ? (int)((__float_as_uint(m) >> 23) & 255) - 127 : 0;
-        const float f = exp2f((float)-e), back = base_fac * exp2f((float)e);
-#pragma unroll
-        for (int k = 0; k < kSteps; ++k) {
-          qf[nt][k][0] = kv_pack_f16(kv_bf16_lo(w[k].x) * f, kv_bf16_hi(w[k].x) * f);
-          qf[nt][k][1] = kv_pack_f16(kv_bf16_lo(w[k].y) * f, kv_bf16_hi(w[k].y) * f);
-        }
-        fac[nt][0] = __shfl_sync(0xffffffffu, back, 8 * t4);
-        fac[nt][1] = __shfl_sync(0xffffffffu, back, 8 * t4 + 4);
-      }
+      load_query<kD, kI8>(p.Q + (int64_t)(u.s.begin + tok) * p.ldq + (int64_t)(u.g * sc.group.d + (row0 + r) - tok * sc.group.d) * (kD * 2), r < n_rows, t4,
+                          base_fac, qf[nt], fac[nt]);
       // visibility: without perm, keys below lim; with it, the context and the chunk's rows whose index is not larger
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
@@ -198,50 +150,27 @@ kv_decode_kernel(const __grid_constant__ KvAttnArgs p) {
       l[nt][0] = l[nt][1] = 0.0f;
     }
 
-    int stage = 0, fill = C::kStages - 1;   // ring positions of the tile at hand and of the one to ask for
     for (int i = 0; i < n_my; ++i) {
       const int pg = page_next;
       page_next = page_of(i + C::kStages);
-      issue(i + C::kStages - 1, fill, pg);
-      if (++fill == C::kStages) fill = 0;
-      cp_async_wait<C::kStages - 1>();
-      __syncwarp();
-      const uint32_t kt = ring + (uint32_t)(stage * C::kStage), vt = kt + 16 * kRow;
-      if (++stage == C::kStages) stage = 0;
-      const int key0 = ((t0 + i) * kWarps + warp) * 16;
-      if (key0 < end) {
-        // ---- S^T (16 keys x 8 rows): two chains of products each, so that they overlap
-        float s[kN][4], s2[kN][4];
+      ask(i + C::kStages - 1, pg);
+      const int stage = (int)(taken % C::kStages);
+      if (!(ok = warp_all(mbar_wait(&full[warp][stage], (taken / C::kStages) & 1u, &abort_flag, p.status, 90)))) break;
+      ++taken;
+      const uint32_t kt = ring + (uint32_t)(stage * C::kStage), vt = kt + T::kBytes;
+      const int key0 = first_key + i * kTile;
+      {
+        float s[kN][4];
+        key_scores<kD, kI8, kN>(kt, lane, qf, s);
+        if (!kI8 && key0 + 16 > end) {
+          // slots behind the last key hold anything: their values must not meet the zeros of P as infinities
 #pragma unroll
-        for (int nt = 0; nt < kN; ++nt)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[nt][e] = s2[nt][e] = 0.0f;
-        if (!kI8) {
-#pragma unroll
-          for (int k = 0; k < kSteps; ++k) {
-            uint32_t a[4];
-            ldsm_x4(kt + piece<kRow>(lane & 15, 2 * k + (lane >> 4)), a);
-#pragma unroll
-            for (int nt = 0; nt < kN; ++nt) mma_16816<false>((k & 1) ? s2[nt] : s[nt], a, qf[nt][k][0], qf[nt][k][1]);
+          for (int c = 0; c < 16 * kD / 8 / 32; ++c) {
+            const int idx = c * 32 + lane, r = idx / (kD / 8), pc = idx % (kD / 8);
+            if (key0 + r >= end) asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(vt + T::piece(r, pc)), "r"(0) : "memory");
           }
-        } else {
-          constexpr int kLoads = kD / 64;   // 16-byte loads per key row and thread
-#pragma unroll
-          for (int c = 0; c < kLoads; ++c) {
-            uint32_t x[2][4];
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-              asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-                           : "=r"(x[j][0]), "=r"(x[j][1]), "=r"(x[j][2]), "=r"(x[j][3]) : "r"(kt + piece<kRow>(quad + 8 * j, t4 * kLoads + c)));
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-              uint32_t a[4];
-              i8x4_to_f16(x[0][w], a[0], a[2]);
-              i8x4_to_f16(x[1][w], a[1], a[3]);
-#pragma unroll
-              for (int nt = 0; nt < kN; ++nt) mma_16816<true>((w & 1) ? s2[nt] : s[nt], a, qf[nt][4 * c + w][0], qf[nt][4 * c + w][1]);
-            }
-          }
+          fence_proxy_async_smem();   // (the slot's next tile is written by TMA)
+          __syncwarp();
         }
         const bool masked = key0 + 16 > all_see;
         unsigned seen = ~0u;   // bit 4 nt + e: score s[nt][e] counts
@@ -259,7 +188,7 @@ kv_decode_kernel(const __grid_constant__ KvAttnArgs p) {
         for (int nt = 0; nt < kN; ++nt) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            s[nt][e] = (s[nt][e] + s2[nt][e]) * fac[nt][e & 1];
+            s[nt][e] *= fac[nt][e & 1];
             if (masked && !((seen >> (4 * nt + e)) & 1u)) s[nt][e] = -INFINITY;
           }
 #pragma unroll
@@ -303,7 +232,7 @@ kv_decode_kernel(const __grid_constant__ KvAttnArgs p) {
         if (!kI8 && masked && all_see < end) {
           uint32_t big = 0u;
 #pragma unroll
-          for (int c = 0; c < 16 * kPieces / 32; ++c) {
+          for (int c = 0; c < T::kBytes / 512; ++c) {
             uint32_t x[4];
             asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
                          : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(vt + (uint32_t)(c * 32 + lane) * 16u));
@@ -327,7 +256,7 @@ kv_decode_kernel(const __grid_constant__ KvAttnArgs p) {
 #pragma unroll
                 for (int hh = 0; hh < 2; ++hh) {
                   unsigned short x;
-                  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(x) : "r"(vt + piece<kRow>(key, 2 * mt + hh) + (uint32_t)quad * 2u));
+                  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(x) : "r"(vt + T::piece(key, 2 * mt + hh) + (uint32_t)quad * 2u));
                   const float v = __uint_as_float((uint32_t)x << 16);
                   if (vis & 1u) o[mt][nt][2 * hh] = fmaf(p0, v, o[mt][nt][2 * hh]);
                   if (vis & 2u) o[mt][nt][2 * hh + 1] = fmaf(p1, v, o[mt][nt][2 * hh + 1]);
@@ -338,7 +267,7 @@ kv_decode_kernel(const __grid_constant__ KvAttnArgs p) {
 #pragma unroll
           for (int mt = 0; mt < kSteps; ++mt) {
             uint32_t a[4];
-            ldsm_x4_trans(vt + piece<kRow>((lane & 7) + ((lane >> 4) << 3), 2 * mt + ((lane >> 3) & 1)), a);
+            ldsm_x4_trans(vt + T::piece((lane & 7) + ((lane >> 4) << 3), 2 * mt + ((lane >> 3) & 1)), a);
 #pragma unroll
             for (int nt = 0; nt < kN; ++nt) mma_16816<false>(o[mt][nt], a, pf[nt][0], pf[nt][1]);
           }
@@ -352,10 +281,10 @@ kv_decode_kernel(const __grid_constant__ KvAttnArgs p) {
             const int key = 2 * t4 + (r & 1) + 8 * (r >> 1);
             if (kD == 128)
               asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-                           : "=r"(x[r][0]), "=r"(x[r][1]), "=r"(x[r][2 % kWords]), "=r"(x[r][3 % kWords]) : "r"(vt + piece<kRow>(key, quad)));
+                           : "=r"(x[r][0]), "=r"(x[r][1]), "=r"(x[r][2 % kWords]), "=r"(x[r][3 % kWords]) : "r"(vt + T::piece(key, quad)));
             else
               asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];"
-                           : "=r"(x[r][0]), "=r"(x[r][1]) : "r"(vt + piece<kRow>(key, quad >> 1) + (uint32_t)(quad & 1) * 8u));
+                           : "=r"(x[r][0]), "=r"(x[r][1]) : "r"(vt + T::piece(key, quad >> 1) + (uint32_t)(quad & 1) * 8u));
           }
 #pragma unroll
           for (int w = 0; w < kWords; ++w) {
@@ -372,9 +301,8 @@ kv_decode_kernel(const __grid_constant__ KvAttnArgs p) {
           }
         }
       }
-      __syncwarp();   // every lane has read the tile before its slot is filled again
+      __syncwarp();   // every lane has read the tile before its slot is asked to be filled again
     }
-    cp_async_wait<0>();
 #pragma unroll
     for (int nt = 0; nt < kN; ++nt)
 #pragma unroll
@@ -385,7 +313,10 @@ kv_decode_kernel(const __grid_constant__ KvAttnArgs p) {
       }
 
     // ---- join the warps: each ran a softmax over its own keys
-    __syncthreads();   // the rings are free
+    if (__syncthreads_or(!ok)) {   // (the rings are free)
+      ok = false;
+      break;
+    }
     float* join = reinterpret_cast<float*>(smem) + warp * (kRows * C::kPitch);
 #pragma unroll
     for (int nt = 0; nt < kN; ++nt) {
@@ -440,7 +371,12 @@ kv_decode_kernel(const __grid_constant__ KvAttnArgs p) {
       rec.n_parts = (last >> 31 ? (int)(last / share) : (int)((uint32_t)last / (uint32_t)share)) - (int)blockIdx.x + 1;
       rec.begin = u.s.begin; rec.row0 = row0; rec.n_rows = n_rows; rec.g = u.g;
     }
+    fence_proxy_async_smem();   // (the rings are next written by TMA)
     __syncthreads();   // the join has been read before the next range fills the rings
+  }
+  if (!ok) {   // copies still landing in this CTA's shared memory get time to finish before it exits
+    for (; taken < asked; ++taken) mbar_wait_drain(&full[warp][taken % C::kStages], (taken / C::kStages) & 1u, 20000ull);
+    rec = KvRecord{};
   }
   if (threadIdx.x == 0) p.parts.rec[blockIdx.x] = rec;
 }
@@ -552,7 +488,9 @@ int launch_decode(const KvAttnArgs& a, int workers, cudaStream_t st) {
   const size_t smem = C::kSmem + ((size_t)a.sched.b.n_seq + 1) * sizeof(int64_t);
   static PerDeviceTable<char> attr_set;
   if (!ensure_dynamic_smem(attr_set, kv_decode_kernel<kD, kI8, kN>, C::kSmem + (kMaxKvSeqs + 1) * (int)sizeof(int64_t))) return MQ_ERR_CUDA;
-  const cudaError_t e = launch_pdl(kv_decode_kernel<kD, kI8, kN>, dim3((unsigned)workers), dim3(kThreads), smem, st, a);
+  CUtensorMap mk, mv;
+  if (!encode_key_tiles(&mk, a.cache.K, a.Q, a.cache, kD, kI8) || !encode_key_tiles(&mv, a.cache.V, a.Q, a.cache, kD, kI8)) return MQ_ERR_CUDA;
+  const cudaError_t e = launch_pdl(kv_decode_kernel<kD, kI8, kN>, dim3((unsigned)workers), dim3(kThreads), smem, st, mk, mv, a);
   if (e != cudaSuccess) return cuda_status(e);
   return cuda_status(cudaGetLastError());
 }
@@ -570,8 +508,8 @@ struct Plan {
 };
 Plan attn_plan(const mq_kv_batch* b, const mq_kv_cache* c, int group) {
   Plan p{};
-  // (a token's heads have to fit into a block of that kernel, and its maps need a page)
-  p.chunk = (int64_t)b->max_q * group > kFewRows && group <= 128 && c->n_pages > 0;
+  // (a token's heads have to fit into a block of that kernel)
+  p.chunk = (int64_t)b->max_q * group > kFewRows && group <= 128;
   if (p.chunk) kv_chunk_shape(group, &p.rows, &p.pitch, &p.tile, &p.extra);
   else p.rows = p.pitch = (int64_t)b->max_q * group <= 8 ? 8 : 16, p.tile = kTile, p.extra = kExtra;
   const int64_t blocks = ((int64_t)b->max_q * group + p.rows - 1) / p.rows;

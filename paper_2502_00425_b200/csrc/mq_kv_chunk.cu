@@ -143,14 +143,14 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
       const Piece* pc = get_piece(np, ok, 50);
       if (!(ok = warp_all(ok)) || !pc) break;
       const int32_t* table = sc.b.page_table + (int64_t)pc->b * sc.b.max_pages;
-      const int t1 = pc->t1, end = pc->end, g = pc->g;
+      const int t1 = pc->t1, end = pc->end, g = pc->g, outside = max(p.cache.n_pages, 1);   // (a page number the map does not have)
       auto page_of = [&](int tile) -> int {
         const int key = tile * kTile + lane * rows;
-        if (lane >= boxes || tile >= t1 || key >= end) return p.cache.n_pages;   // outside the map: zeros
+        if (lane >= boxes || tile >= t1 || key >= end) return outside;   // zeros
         const int pg = table[key >> shift];
         if ((unsigned)pg >= (unsigned)p.cache.n_pages) {
           bad = true;
-          return p.cache.n_pages;
+          return outside;
         }
         return pg;
       };
@@ -656,7 +656,7 @@ int launch(const KvAttnArgs& a, int workers, cudaStream_t st) {
   if (!ensure_dynamic_smem(attr_set, kv_chunk_kernel<kD, kI8>, C::kSmem + (kMaxKvSeqs + 1) * (int)sizeof(int64_t))) return MQ_ERR_CUDA;
   CUtensorMap mq_{}, mk{}, mv{};
   if (!encode_queries(&mq_, a.Q, a.ldq, a.out.n_q_heads, a.sched.b.total_q, a.sched.group.d, a.sched.rows / 2, kD)) return MQ_ERR_CUDA;
-  if (!kI8 && (!encode_pages(&mk, a.cache.K, a.cache, kD, kTile) || !encode_pages(&mv, a.cache.V, a.cache, kD, kTile))) return MQ_ERR_CUDA;
+  if (!kI8 && (!encode_pages(&mk, a.cache.K, a.Q, a.cache, kD, kTile) || !encode_pages(&mv, a.cache.V, a.Q, a.cache, kD, kTile))) return MQ_ERR_CUDA;
   const cudaError_t e = launch_pdl(kv_chunk_kernel<kD, kI8>, dim3((unsigned)workers), dim3(C::kThreads),
                                    C::kSmem + ((size_t)a.sched.b.n_seq + 1) * sizeof(int64_t), st, mq_, mk, mv, a);
   if (e != cudaSuccess) return cuda_status(e);

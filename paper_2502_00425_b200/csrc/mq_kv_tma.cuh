@@ -40,9 +40,11 @@ inline bool encode_bf16(CUtensorMap* map, int rank, const void* base, const cuui
                                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 // The pages as a map [page][head][slot][channel], read in boxes of 64 channels x (a page's slots, at most `tile`)
-inline bool encode_pages(CUtensorMap* map, const uint8_t* base, const KvView& c, int dim, int tile) {
+// (a cache without pages: a map of one page, over any memory, that no coordinate in use reaches)
+inline bool encode_pages(CUtensorMap* map, const void* base, const void* any, const KvView& c, int dim, int tile) {
   const int page = 1 << c.page_shift;
-  const cuuint64_t dims[4] = {(cuuint64_t)dim, (cuuint64_t)page, (cuuint64_t)c.n_kv_heads, (cuuint64_t)c.n_pages};
+  if (c.n_pages == 0) base = any;
+  const cuuint64_t dims[4] = {(cuuint64_t)dim, (cuuint64_t)page, (cuuint64_t)c.n_kv_heads, (cuuint64_t)(c.n_pages > 0 ? c.n_pages : 1)};
   const cuuint64_t strides[3] = {(cuuint64_t)c.slot_stride, (cuuint64_t)c.head_stride, (cuuint64_t)c.page_stride};
   const cuuint32_t box[4] = {64, (cuuint32_t)(page < tile ? page : tile), 1, 1};
   return encode_bf16(map, 4, base, dims, strides, box);

@@ -2,207 +2,215 @@
 //   W_out[b, g, j] = W_in[b, g, j] + sum over rows i and heads h that see j of exp(scale * Q[i, h] . K[j, g] - lse[i, h])
 // lse (the log of every row's softmax denominator) comes from the attention call, so one pass over K suffices.
 //
-// The product is taken with the KEYS as the rows of the tensor-core tile: a CTA owns 128 keys of one head (16 per
-// warp), keeps them in registers as A fragments, and walks the query rows in blocks of 64; a key's sum is then over
-// columns, i.e. over registers of four neighbouring lanes, and is written once.  No atomics, one order of summation.
-// This is the kernel for few query rows, bound by reading K; chunks take mq_kv_weights_chunk.cu.
+// This is the kernel for few query rows (decode steps), bound by reading K; chunks take mq_kv_weights_chunk.cu.  Like the
+// decode attention it lets every warp stream 16 keys at a time into a ring of its own and multiply them as the rows of
+// the instruction's tile: a key's sum is over the columns, registers of four neighbouring lanes, and is written once.
+// The work line is the sequences' key tiles, cut into equal ranges; nothing has to be joined.  No atomics, one order of
+// summation.  More than 8 kN rows (only where a group does not fit the chunk kernel) are walked in blocks per key tile.
+#include "mq_kv_warp.cuh"
 #include "mq_kv_weights.cuh"
 
 namespace mq {
 namespace {
 
-constexpr int kWarps = 8;
-constexpr int kThreads = kWarps * 32;
-constexpr int kKeys = kWarps * 16;   // keys of a CTA's tile
-constexpr int kRowsQ = 64;           // query rows per step
-constexpr int kFewRows = 64;         // up to here (tokens x heads of the group) this kernel, above the tensor-memory one
+constexpr int kWarps = kStreamWarps, kThreads = kStreamThreads, kTile = kStreamTile;
+constexpr int kFewRows = 16;   // query rows per key/value head (tokens x heads of the group) up to which a call comes here
+constexpr int kExtra = 2;      // what a unit costs besides its tiles (its queries), in tiles
 
-template <int kD>
-struct Smem {
-  static constexpr int kPitch = kD * 2 + 16;   // bytes between rows: neighbouring rows start in different banks
-  static constexpr int kK = kKeys * kPitch;
-  static constexpr int kQ = kRowsQ * kPitch;
-  static constexpr int kBytes = kK + kQ + kRowsQ * 8;
+template <int kD, bool kI8, int kN>
+struct Cfg {
+  static constexpr int kStage = KeyTile<kD, kI8>::kBytes;
+  static constexpr int kStages = kStage == 4096 ? 3 : 4;
+  static constexpr int kCtas = 4;
+  static constexpr int kRing = kStage * kStages;
+  static constexpr int kSmem = 1024 + kWarps * kRing;
 };
 
-template <int kD, bool kI8>
-__global__ void __launch_bounds__(kThreads)
-kv_weights_kernel(const __grid_constant__ WeightParams p) {
-  using S = Smem<kD>;
-  constexpr int kSteps = kD / 16, kPieces = kD / 8;   // 16-byte pieces of a bf16 row
-  extern __shared__ __align__(128) uint8_t smem[];
+template <int kD, bool kI8, int kN>
+__global__ void __launch_bounds__(kThreads, (Cfg<kD, kI8, kN>::kCtas))
+kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ WeightParams p) {
+  using C = Cfg<kD, kI8, kN>;
+  using T = KeyTile<kD, kI8>;
+  constexpr int kRows = 8 * kN;
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  __shared__ uint64_t full[kWarps][C::kStages];
   __shared__ int64_t red[kWarps];
-  uint8_t* ks = smem;
-  uint8_t* qs = smem + S::kK;
-  float* row_lse = reinterpret_cast<float*>(qs + S::kQ);     // log2 units; +inf for a row that adds nothing
-  int* row_lim = reinterpret_cast<int*>(row_lse + kRowsQ);
-  int64_t* prefix = reinterpret_cast<int64_t*>(smem + S::kBytes);
+  __shared__ int abort_flag;
+  __shared__ int32_t status[2];
+  int64_t* prefix = reinterpret_cast<int64_t*>(smem + kWarps * C::kRing);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, quad = lane >> 2, t4 = lane & 3;
+  if (tid == 0) {
+    abort_flag = 0;
+    status[0] = status[1] = MQ_OK;
+    for (int i = 0; i < kWarps * C::kStages; ++i) mbar_init(&full[0][0] + i, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
   pdl_launch_dependents();
   pdl_wait();
 
-  // key tiles of the sequences before each one
-  const int n = p.b.n_seq, per = (n + kThreads - 1) / kThreads;
-  int64_t sum = 0;
-  for (int k = 0; k < per; ++k) {
-    const int b = tid * per + k;
-    if (b >= n) break;
-    sum += (kv_seq(p.b, p.c.page_shift, p.max_q, b).n_all + kKeys - 1) / kKeys;
-    prefix[b + 1] = sum;
-  }
-  int64_t inc = sum;
+  // length of a head's stretch of the line (all of a sequence's heads are alike), summed over the sequences before each one
+  auto stretch = [&](const KvSeq& s) -> int { return s.n_all > 0 ? (s.n_all + kTile - 1) / kTile + kExtra : 0; };
+  const int n = p.b.n_seq;
+  {
+    const int per = (n + kThreads - 1) / kThreads;
+    int64_t sum = 0;
+    for (int k = 0; k < per; ++k) {
+      const int b = tid * per + k;
+      if (b >= n) break;
+      sum += (int64_t)stretch(kv_seq(p.b, p.c.page_shift, p.max_q, b)) * p.c.n_kv_heads;
+      prefix[b + 1] = sum;
+    }
+    int64_t inc = sum;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int64_t v = __shfl_up_sync(0xffffffffu, inc, o);
-    if (lane >= o) inc += v;
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t v = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += v;
+    }
+    if (lane == 31) red[warp] = inc;
+    __syncthreads();
+    int64_t off = inc - sum;
+    for (int w = 0; w < warp; ++w) off += red[w];
+    for (int k = 0; k < per; ++k) {
+      const int b = tid * per + k;
+      if (b >= n) break;
+      prefix[b + 1] += off;
+    }
+    if (tid == 0) prefix[0] = 0;
+    __syncthreads();
   }
-  if (lane == 31) red[warp] = inc;
-  __syncthreads();
-  int64_t off = inc - sum;
-  for (int w = 0; w < warp; ++w) off += red[w];
-  for (int k = 0; k < per; ++k) {
-    const int b = tid * per + k;
-    if (b >= n) break;
-    prefix[b + 1] += off;
-  }
-  if (tid == 0) prefix[0] = 0;
-  __syncthreads();
-  const int64_t total = prefix[n] * p.c.n_kv_heads;
-
-  for (int64_t at = blockIdx.x; at < total; at += gridDim.x) {
-    const int g = (int)(at % p.c.n_kv_heads);
-    const int64_t x = at / p.c.n_kv_heads;
-    int lo = 0, hi = n;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (prefix[mid] <= x) lo = mid;
+  const int64_t total = prefix[n];
+  const int64_t share = total >> 31 ? (total + gridDim.x - 1) / gridDim.x : (int64_t)(((uint32_t)total + gridDim.x - 1u) / gridDim.x);
+  int64_t at = min(total, (int64_t)blockIdx.x * share);
+  const int64_t stop = min(total, at + share);
+  const uint32_t ring = kv_smem_u32(smem) + (uint32_t)(warp * C::kRing);
+  uint32_t asked = 0, taken = 0;
+  bool ok = true;
+  while (ok && at < stop) {
+    int b = 0, hi = n;   // prefix[b] <= at < prefix[hi]
+    while (hi - b > 1) {
+      const int mid = (b + hi) >> 1;
+      if (prefix[mid] <= at) b = mid;
       else hi = mid;
     }
-    const KvSeq s = kv_seq(p.b, p.c.page_shift, p.max_q, lo);
-    const int key0 = (int)(x - prefix[lo]) * kKeys, ctx = s.n_all - s.n_new;
-    const int32_t* table = p.b.page_table + (int64_t)lo * p.b.max_pages;
-    const int32_t* perm = p.b.perm ? p.b.perm + s.begin : nullptr;
+    const KvSeq s = kv_seq(p.b, p.c.page_shift, p.max_q, b);
+    const int per_head = stretch(s);
+    const int64_t x = at - prefix[b];
+    const int g = (int)(x >> 31 ? x / per_head : (int64_t)((uint32_t)x / (uint32_t)per_head)), skip = (int)(x - (int64_t)g * per_head);
+    const int len = (int)min((int64_t)(per_head - skip), stop - at);
+    at += len;
+    const int t0 = max(0, skip - kExtra), t1 = max(0, skip + len - kExtra);
+    if (t0 == t1) continue;
+    const int ctx = s.n_all - s.n_new;
+    const int32_t *table = p.b.page_table + (int64_t)b * p.b.max_pages, *perm = p.b.perm ? p.b.perm + s.begin : nullptr;
+    const int first_key = (t0 * kWarps + warp) * 16;
+    const int n_my = min(t1 - t0, s.n_all > first_key ? (s.n_all - first_key + kTile - 1) / kTile : 0);
+    auto page_of = [&](int i) -> int { return i < n_my ? table[(first_key + i * kTile) >> p.c.page_shift] : 0; };
+    auto ask = [&](int i, int page) {
+      if (i >= n_my) return;
+      if (lane == 0) {
+        if ((unsigned)page >= (unsigned)p.c.n_pages) {
+          page = max(p.c.n_pages, 1);   // a page number the map does not have: zeros
+          if (p.status) atomicCAS(p.status, MQ_OK, MQ_ERR_INVALID_ARG);
+        }
+        const int st = (int)(asked % C::kStages), slot = (first_key + i * kTile) & ((1 << p.c.page_shift) - 1);
+        mbar_arrive_expect_tx(&full[warp][st], C::kStage);
+        T::load(ring + (uint32_t)(st * C::kStage), &tmap_k, slot, g, page, &full[warp][st]);
+      }
+      ++asked;
+    };
+    int page_next = page_of(0);
+#pragma unroll
+    for (int i = 0; i < C::kStages - 1; ++i) {
+      const int pg = page_next;
+      page_next = page_of(i + 1);
+      ask(i, pg);
+    }
 
-    // ---- keys to shared memory (bf16; codes of an int8 cache are widened exactly)
-    constexpr int kSrc = kI8 ? kD / 16 : kPieces;   // 16-byte pieces of a cached row
+    // ---- a block of query rows: operands, what turns scores into log2 units, log-sum-exps (log2 units), and sight
+    const int n_rows = s.n_new * p.group.d, blocks = (n_rows + kRows - 1) / kRows;
+    const float base_fac = p.scale * 1.4426950408889634f * (kI8 ? p.c.k_scale[g] : 1.0f);
+    uint32_t qf[kN][kD / 16][2];
+    float fac[kN][2], nl[kN][2];
+    int lim[kN][2], all_see = INT_MAX;   // every row of the block sees the keys below all_see
+    auto rows_of = [&](int row0) {
 #pragma unroll
-    for (int c = 0; c < kKeys * kSrc / kThreads; ++c) {
-      const int idx = c * kThreads + tid, r = idx / kSrc, pc = idx % kSrc, key = key0 + r;
-      int page = -1;
-      if (key < s.n_all) page = table[key >> p.c.page_shift];
-      const bool ok = (unsigned)page < (unsigned)p.c.n_pages;
-      if (!ok && key < s.n_all && p.status) atomicCAS(p.status, MQ_OK, MQ_ERR_INVALID_ARG);
-      const int64_t src = ok ? (int64_t)page * p.c.page_stride + (int64_t)g * p.c.head_stride +
-                                   (int64_t)(key & ((1 << p.c.page_shift) - 1)) * p.c.slot_stride + pc * 16
-                             : 0;
-      if (!kI8) {
-        cp_async16(kv_smem_u32(ks + r * S::kPitch + pc * 16), ok ? p.c.K + src : p.Q, ok ? 16u : 0u);
-      } else {
-        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        if (ok) v = *reinterpret_cast<const uint4*>(p.c.K + src);
-        uint4 a, b;
-        i8x4_to_bf16(v.x, a.x, a.y); i8x4_to_bf16(v.y, a.z, a.w);
-        i8x4_to_bf16(v.z, b.x, b.y); i8x4_to_bf16(v.w, b.z, b.w);
-        *reinterpret_cast<uint4*>(ks + r * S::kPitch + pc * 32) = a;
-        *reinterpret_cast<uint4*>(ks + r * S::kPitch + pc * 32 + 16) = b;
+      for (int nt = 0; nt < kN; ++nt) {
+        const int r = row0 + 8 * nt + quad, tok = r / p.group;
+        load_query<kD, kI8>(p.Q + (int64_t)(s.begin + tok) * p.ldq + (int64_t)(g * p.group.d + r - tok * p.group.d) * (kD * 2), r < n_rows, t4, base_fac, qf[nt], fac[nt]);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int rr = row0 + 8 * nt + 2 * t4 + e, tk = rr / p.group;
+          const bool live = rr < n_rows;
+          const float l = live ? p.lse[(int64_t)(s.begin + tk) * p.n_q_heads + g * p.group.d + rr - tk * p.group.d] : INFINITY;
+          nl[nt][e] = fabsf(l) == INFINITY ? -INFINITY : l * -1.4426950408889634f;   // (a row that sees nothing has -inf and adds nothing)
+          lim[nt][e] = !live ? INT_MIN : perm ? perm[tk] : ctx + tk + 1;
+        }
       }
-    }
-    cp_async_commit();
+      all_see = row0 + kRows > n_rows ? INT_MIN : perm ? ctx : ctx + row0 / p.group + 1;
+    };
+    if (blocks > 0) rows_of(0);
 
-    // ---- query rows that may see any of these keys
-    const int n_rows = s.n_new * p.group;
-    const int first_tok = perm ? 0 : max(0, key0 - ctx);
-    const float scale_log2 = p.scale * 1.4426950408889634f * (kI8 ? p.c.k_scale[g] : 1.0f);
-    float sum0 = 0.0f, sum1 = 0.0f;
-    const int ka = key0 + warp * 16 + quad, kb = ka + 8;
-    uint32_t kf[kSteps][4];
-    bool have_k = false;
-    for (int r0 = first_tok * p.group; r0 < n_rows; r0 += kRowsQ) {
-      __syncthreads();   // the previous block of rows has been read
+    for (int i = 0; i < n_my; ++i) {
+      const int pg = page_next;
+      page_next = page_of(i + C::kStages);
+      ask(i + C::kStages - 1, pg);
+      const int st = (int)(taken % C::kStages), key0 = first_key + i * kTile;
+      // what the two keys of this lane had (asked for before the wait)
+      const int ka = key0 + quad, kb = ka + 8;
+      const int64_t out = (int64_t)b * p.seq_stride + (int64_t)g * p.head_stride;
+      float old_a = 0.0f, old_b = 0.0f;
+      if (t4 == 0 && p.W_in) {
+        if (ka < ctx) old_a = p.W_in[out + ka];
+        if (kb < ctx) old_b = p.W_in[out + kb];
+      }
+      if (!(ok = warp_all(mbar_wait(&full[warp][st], (taken / C::kStages) & 1u, &abort_flag, status, 91)))) break;
+      ++taken;
+      float sum_a = 0.0f, sum_b = 0.0f;
+      for (int blk = 0; blk < blocks; ++blk) {
+        if (blocks > 1) rows_of(blk * kRows);
+        float sc[kN][4];
+        key_scores<kD, kI8, kN>(ring + (uint32_t)(st * C::kStage), lane, qf, sc);
+        const bool masked = key0 + 16 > all_see;
 #pragma unroll
-      for (int c = 0; c < kRowsQ * kPieces / kThreads; ++c) {
-        const int idx = c * kThreads + tid, r = idx / kPieces, pc = idx % kPieces, row = r0 + r;
-        const bool ok = row < n_rows;
-        const uint8_t* src = p.Q;
-        if (ok) src += (int64_t)(s.begin + row / p.group) * p.ldq + (int64_t)(g * p.group + row % p.group) * (kD * 2) + pc * 16;
-        cp_async16(kv_smem_u32(qs + r * S::kPitch + pc * 16), src, ok ? 16u : 0u);
-      }
-      cp_async_commit();
-      if (tid < kRowsQ) {
-        const int row = r0 + tid;
-        float l = INFINITY;
-        int lim = INT_MIN;
-        if (row < n_rows) {
-          const int tok = row / p.group;
-          l = p.lse[(int64_t)(s.begin + tok) * p.n_q_heads + g * p.group + row % p.group] * 1.4426950408889634f;
-          if (l == -INFINITY) l = INFINITY;   // a row that sees nothing
-          lim = perm ? perm[tok] : ctx + tok + 1;
-        }
-        row_lse[tid] = l;
-        row_lim[tid] = lim;
-      }
-      cp_async_wait<0>();
-      __syncthreads();
-      if (!have_k) {
+        for (int nt = 0; nt < kN; ++nt)
 #pragma unroll
-        for (int k = 0; k < kSteps; ++k)
-          ldsm_x4(kv_smem_u32(ks + (warp * 16 + (lane & 15)) * S::kPitch + k * 32 + (lane >> 4) * 16), kf[k]);
-        have_k = true;
+          for (int e = 0; e < 4; ++e) {
+            float v = kv_exp2(fmaf(sc[nt][e], fac[nt][e & 1], nl[nt][e & 1]));
+            if (masked) {
+              const int key = e < 2 ? ka : kb, lm = lim[nt][e & 1];
+              const bool sees = lm != INT_MIN && key < s.n_all && (perm ? key < ctx || perm[key - ctx] <= lm : key < lm);
+              if (!sees) v = 0.0f;
+            }
+            if (e < 2) sum_a += v;
+            else sum_b += v;
+          }
       }
-      const int blocks = (min(kRowsQ, n_rows - r0) + 7) / 8;
-      // all rows of the step see all keys of the tile?
-      const bool masked = key0 + kKeys > (perm ? ctx : ctx + r0 / p.group + 1) || key0 + kKeys > s.n_all;
-      for (int nb = 0; nb < blocks; ++nb) {
-        float c[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int k = 0; k < kSteps; k += 2) {
-          uint32_t b[4];
-          ldsm_x4(kv_smem_u32(qs + (nb * 8 + (lane & 7)) * S::kPitch + k * 32 + (lane >> 3) * 16), b);
-          mma_16816<false>(c, kf[k], b[0], b[1]);
-          mma_16816<false>(c, kf[k + 1], b[2], b[3]);
-        }
-        const int r = nb * 8 + 2 * t4;
-        const float2 l = *reinterpret_cast<const float2*>(row_lse + r);
-        float e[4] = {kv_exp2(fmaf(c[0], scale_log2, -l.x)), kv_exp2(fmaf(c[1], scale_log2, -l.y)),
-                      kv_exp2(fmaf(c[2], scale_log2, -l.x)), kv_exp2(fmaf(c[3], scale_log2, -l.y))};
-        if (masked) {
-          const int2 lim = *reinterpret_cast<const int2*>(row_lim + r);
-          auto sees = [&](int key, int lm) -> bool {
-            if (key >= s.n_all || lm == INT_MIN) return false;
-            return perm ? key < ctx || perm[key - ctx] <= lm : key < lm;
-          };
-          if (!sees(ka, lim.x)) e[0] = 0.0f;
-          if (!sees(ka, lim.y)) e[1] = 0.0f;
-          if (!sees(kb, lim.x)) e[2] = 0.0f;
-          if (!sees(kb, lim.y)) e[3] = 0.0f;
-        } else if (row_lim[r] == INT_MIN || row_lim[r + 1] == INT_MIN) {   // rows behind the last one
-          if (row_lim[r] == INT_MIN) e[0] = e[2] = 0.0f;
-          if (row_lim[r + 1] == INT_MIN) e[1] = e[3] = 0.0f;
-        }
-        sum0 += e[0] + e[1];
-        sum1 += e[2] + e[3];
+      sum_a += __shfl_xor_sync(0xffffffffu, sum_a, 1); sum_a += __shfl_xor_sync(0xffffffffu, sum_a, 2);
+      sum_b += __shfl_xor_sync(0xffffffffu, sum_b, 1); sum_b += __shfl_xor_sync(0xffffffffu, sum_b, 2);
+      if (t4 == 0) {
+        if (ka < s.n_all) p.W_out[out + ka] = old_a + sum_a;
+        if (kb < s.n_all) p.W_out[out + kb] = old_b + sum_b;
       }
+      __syncwarp();   // every lane has read the tile before its slot is asked to be filled again
     }
-    cp_async_wait<0>();   // (a tile that no row sees loads its keys for nothing)
-    sum0 += __shfl_xor_sync(0xffffffffu, sum0, 1); sum0 += __shfl_xor_sync(0xffffffffu, sum0, 2);
-    sum1 += __shfl_xor_sync(0xffffffffu, sum1, 1); sum1 += __shfl_xor_sync(0xffffffffu, sum1, 2);
-    if (t4 == 0) {
-      const int64_t base = (int64_t)lo * p.seq_stride + (int64_t)g * p.head_stride;
-      if (ka < s.n_all) p.W_out[base + ka] = (p.W_in && ka < ctx ? p.W_in[base + ka] : 0.0f) + sum0;
-      if (kb < s.n_all) p.W_out[base + kb] = (p.W_in && kb < ctx ? p.W_in[base + kb] : 0.0f) + sum1;
-    }
-    __syncthreads();   // the keys have been read before the next tile overwrites them
+  }
+  if (!ok) {
+    for (; taken < asked; ++taken) mbar_wait_drain(&full[warp][taken % C::kStages], (taken / C::kStages) & 1u, 20000ull);
+    if (lane == 0 && p.status && atomicCAS(p.status, MQ_OK, MQ_ERR_TIMEOUT) == MQ_OK) p.status[1] = 91;
   }
 }
 
-template <int kD, bool kI8>
+template <int kD, bool kI8, int kN>
 int launch(const WeightParams& p, int64_t most, cudaStream_t st) {
-  using S = Smem<kD>;
-  const size_t smem = S::kBytes + ((size_t)p.b.n_seq + 1) * sizeof(int64_t);
+  using C = Cfg<kD, kI8, kN>;
+  const size_t smem = C::kSmem + ((size_t)p.b.n_seq + 1) * sizeof(int64_t);
   static PerDeviceTable<char> attr_set;
-  if (!ensure_dynamic_smem(attr_set, kv_weights_kernel<kD, kI8>, S::kBytes + (kMaxKvSeqs + 1) * (int)sizeof(int64_t))) return MQ_ERR_CUDA;
-  const int64_t cap = (int64_t)sm_count() * 3;
-  const cudaError_t e = launch_pdl(kv_weights_kernel<kD, kI8>, dim3((unsigned)(most < cap ? most : cap)), dim3(kThreads), smem, st, p);
+  if (!ensure_dynamic_smem(attr_set, kv_weights_kernel<kD, kI8, kN>, C::kSmem + (kMaxKvSeqs + 1) * (int)sizeof(int64_t))) return MQ_ERR_CUDA;
+  CUtensorMap mk;
+  if (!encode_key_tiles(&mk, p.c.K, p.Q, p.c, kD, kI8)) return MQ_ERR_CUDA;
+  const int64_t cap = (int64_t)sm_count() * C::kCtas;
+  const cudaError_t e = launch_pdl(kv_weights_kernel<kD, kI8, kN>, dim3((unsigned)(most < cap ? most : cap)), dim3(kThreads), smem, st, mk, p);
   if (e != cudaSuccess) return cuda_status(e);
   return cuda_status(cudaGetLastError());
 }
@@ -222,15 +230,16 @@ extern "C" int mq_kv_weights(const void* Q, int64_t ldq, const mq_kv_batch* batc
   if (n_q_heads <= 0 || n_q_heads % cache->n_kv_heads) return MQ_ERR_INVALID_ARG;
   if (!(scale > 0.0f) || !std::isfinite(scale)) return MQ_ERR_INVALID_ARG;
   const int64_t reach = (int64_t)batch->max_pages * cache->page_size;
+  const int group = n_q_heads / cache->n_kv_heads;
   if (ldq < (int64_t)n_q_heads * cache->head_dim || w_head_stride < 0 || w_seq_stride < 0) return MQ_ERR_INVALID_ARG;
-  if ((int64_t)batch->max_q * (n_q_heads / cache->n_kv_heads) > (1 << 30)) return MQ_ERR_UNSUPPORTED;
+  if ((int64_t)batch->max_q * group > (1 << 30)) return MQ_ERR_UNSUPPORTED;
   if (batch->n_seq == 0 || reach == 0 || batch->total_q == 0) return MQ_OK;   // (no rows: no weight is added anywhere)
   if (!W_out || !Q || !lse) return MQ_ERR_INVALID_ARG;
-  if ((Q && !kv_aligned16(Q)) || ldq % 8) return MQ_ERR_ALIGNMENT;
+  if (!kv_aligned16(Q) || ldq % 8) return MQ_ERR_ALIGNMENT;
   p.Q = static_cast<const uint8_t*>(Q);
   p.ldq = ldq * 2;
   p.max_q = batch->max_q;
-  p.group = n_q_heads / cache->n_kv_heads;
+  p.group = fast_div(group);
   p.n_q_heads = n_q_heads;
   p.scale = scale;
   p.lse = lse;
@@ -239,12 +248,16 @@ extern "C" int mq_kv_weights(const void* Q, int64_t ldq, const mq_kv_batch* batc
   p.seq_stride = w_seq_stride;
   p.head_stride = w_head_stride;
   p.status = status;
-  const int64_t most = (int64_t)batch->n_seq * cache->n_kv_heads * ((reach + kKeys - 1) / kKeys);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool i8 = (cache->flags & MQ_KV_INT8) != 0;
-  // (a token's heads have to fit into a row tile of the chunk kernel, and its maps need a page)
-  if ((int64_t)batch->max_q * p.group > kFewRows && p.group <= 128 && cache->n_pages > 0)
-    return launch_kv_weights_chunk(p, cache->head_dim, i8, most, st);
-  if (cache->head_dim == 128) return i8 ? launch<128, true>(p, most, st) : launch<128, false>(p, most, st);
-  return i8 ? launch<64, true>(p, most, st) : launch<64, false>(p, most, st);
+  const int64_t rows = (int64_t)batch->max_q * group, units = (int64_t)batch->n_seq * cache->n_kv_heads;
+  // (a token's heads have to fit into a row tile of the chunk kernel)
+  if (rows > kFewRows && group <= 128) return launch_kv_weights_chunk(p, cache->head_dim, i8, units * ((reach + 127) / 128), st);
+  const int64_t most = units * ((reach + kTile - 1) / kTile);
+  if (rows <= 8) {
+    if (cache->head_dim == 128) return i8 ? launch<128, true, 1>(p, most, st) : launch<128, false, 1>(p, most, st);
+    return i8 ? launch<64, true, 1>(p, most, st) : launch<64, false, 1>(p, most, st);
+  }
+  if (cache->head_dim == 128) return i8 ? launch<128, true, 2>(p, most, st) : launch<128, false, 2>(p, most, st);
+  return i8 ? launch<64, true, 2>(p, most, st) : launch<64, false, 2>(p, most, st);
 }

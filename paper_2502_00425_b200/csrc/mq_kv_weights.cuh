@@ -10,7 +10,8 @@ struct WeightParams {
   int64_t ldq;   // bytes
   KvBatchView b;
   KvView c;
-  int max_q, group, n_q_heads;
+  int max_q, n_q_heads;
+  FastDiv group;   // query heads per key/value head
   float scale;
   const float* lse;
   const float* W_in;

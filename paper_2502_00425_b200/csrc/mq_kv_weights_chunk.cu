@@ -99,7 +99,7 @@ kv_weights_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid
   int64_t* red = reinterpret_cast<int64_t*>(xch + 2 * kKeys);
   int64_t* prefix = red + 16;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tid = threadIdx.x;
-  const int tokens = kCols / p.group, block_rows = tokens * p.group;
+  const int tokens = kCols / p.group, block_rows = tokens * p.group.d;
 
   if (tid == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmap_q)) : "memory");
@@ -182,7 +182,7 @@ kv_weights_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid
       const Piece* pc = get_piece(np, ok, 70);
       if (!(ok = warp_all(ok)) || !pc) break;
       const int buf = np & 1, key = pc->key0 + lane * rows;
-      int page = p.c.n_pages;   // outside the map: zeros
+      int page = max(p.c.n_pages, 1);   // a page number the map does not have: zeros
       if (lane < boxes && key < pc->n_all) {
         const int pg = p.b.page_table[(int64_t)pc->b * p.b.max_pages + (key >> shift)];
         if ((unsigned)pg < (unsigned)p.c.n_pages) page = pg;
@@ -285,7 +285,7 @@ kv_weights_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid
         pc.key0 = kb * kKeys;
         pc.n_all = s.n_all;
         pc.ctx = s.n_all - s.n_new;
-        pc.n_rows = s.n_new * p.group;
+        pc.n_rows = s.n_new * p.group.d;
         pc.tile0 = first_tile(p, s, tokens, pc.key0);
         pc.tiles = max(nt - pc.tile0, 1);
         pc.b = b;
@@ -308,7 +308,7 @@ kv_weights_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid
           mbar_arrive_expect_tx(&sh->q_full[qs], (uint32_t)(block_rows * 128 * kHalves));
 #pragma unroll
           for (int h = 0; h < kHalves; ++h)
-            tma_load_3d(smem_u32(q_smem + qs * kTileBytes + h * kHalfBytes), &tmap_q, h * 64, pc.g * p.group, pc.begin + (pc.tile0 + i) * tokens, &sh->q_full[qs]);
+            tma_load_3d(smem_u32(q_smem + qs * kTileBytes + h * kHalfBytes), &tmap_q, h * 64, pc.g * p.group.d, pc.begin + (pc.tile0 + i) * tokens, &sh->q_full[qs]);
         }
         __syncwarp();
       }
@@ -325,12 +325,12 @@ kv_weights_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       tok_of[c] = (c * 32 + lane) / p.group;
-      head_of[c] = (c * 32 + lane) - tok_of[c] * p.group;
+      head_of[c] = (c * 32 + lane) - tok_of[c] * p.group.d;
     }
     for (int np = 0; ok; ++np) {
       const Piece* pc = get_piece(np, ok, 78);
       if (!(ok = warp_all(ok)) || !pc) break;
-      const int tiles = pc->tiles, tile0 = pc->tile0, n_rows = pc->n_rows, begin = pc->begin, g_head = pc->g * p.group;
+      const int tiles = pc->tiles, tile0 = pc->tile0, n_rows = pc->n_rows, begin = pc->begin, g_head = pc->g * p.group.d;
       float l_next[4];
       int rk_next[4];
       auto fetch = [&](int i) {
@@ -390,7 +390,7 @@ kv_weights_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid
         if (!(ok = warp_all(mbar_wait(&sh->s_full[sb], (uint32_t)(t / 4) & 1u, &sh->abort_flag, sh->status, 82)))) break;
         tc_fence_after();
         // columns lo .. hi - 1 count (without perm); with it, columns whose rank is at least kp
-        const int lo = perm ? 0 : (int)max((int64_t)0, min((int64_t)kCols, (int64_t)(key - ctx) * p.group - row0)), hi = n_rows - row0;
+        const int lo = perm ? 0 : (int)max((int64_t)0, min((int64_t)kCols, (int64_t)(key - ctx) * p.group.d - row0)), hi = n_rows - row0;
         float2 acc[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
         const uint32_t s_addr = lane_base + (uint32_t)(sb * kCols);
         uint32_t va[32], vb[32];   // the next 32 columns are on their way while these are summed
@@ -493,8 +493,8 @@ int launch(const WeightParams& p, int64_t most, cudaStream_t st) {
   static PerDeviceTable<char> attr_set;
   if (!ensure_dynamic_smem(attr_set, kv_weights_chunk_kernel<kD, kI8>, C::kSmem + (kMaxKvSeqs + 1) * (int)sizeof(int64_t))) return MQ_ERR_CUDA;
   CUtensorMap mq_{}, mk{};
-  if (!encode_queries(&mq_, p.Q, p.ldq, p.n_q_heads, p.b.total_q, p.group, kCols / p.group * p.group, kD)) return MQ_ERR_CUDA;
-  if (!kI8 && !encode_pages(&mk, p.c.K, p.c, kD, kKeys)) return MQ_ERR_CUDA;
+  if (!encode_queries(&mq_, p.Q, p.ldq, p.n_q_heads, p.b.total_q, p.group.d, kCols / p.group.d * p.group.d, kD)) return MQ_ERR_CUDA;
+  if (!kI8 && !encode_pages(&mk, p.c.K, p.Q, p.c, kD, kKeys)) return MQ_ERR_CUDA;
   const int64_t cap = sm_count();
   const cudaError_t e = launch_pdl(kv_weights_chunk_kernel<kD, kI8>, dim3((unsigned)(most < cap ? most : cap)), dim3(C::kThreads),
                                    C::kSmem + ((size_t)p.b.n_seq + 1) * sizeof(int64_t), st, mq_, mk, p);

@@ -281,6 +281,27 @@ def test_two_streams_with_their_own_workspaces():
         _check(pg, q, new, 8, o.float().cpu().numpy().astype(np.float64), lse.cpu().numpy().astype(np.float64), heads=[0, 7])
 
 
+@pytest.mark.parametrize("new", [[1, 1], [40, 3]])
+def test_a_cache_without_pages_reads_as_zeros(new):
+    """No page exists: every page number is outside the cache (and reported), keys and values are zeros."""
+    K = torch.empty((0, 2, 16, 128), dtype=torch.bfloat16, device=DEV)
+    cache = B.KVCache(K, K.clone())
+    table = torch.zeros((2, 4), dtype=torch.int32, device=DEV)
+    lens = torch.tensor([50, 40], dtype=torch.int32, device=DEV)
+    q = torch.randn((sum(new), 512), device=DEV).to(torch.bfloat16)
+    o, lse = torch.full_like(q, 7.0), torch.zeros((sum(new), 4), device=DEV)
+    ws = B.new_kv_attention_workspace(2, sum(new), max(new), 4, 4, cache)
+    B.mq_kv_attention(q, cu(new), lens, table, cache, 4, max(new), o, ws, lse=lse)
+    w = torch.full((2, 2, 64), 9.0, device=DEV)
+    B.mq_kv_weights(q, cu(new), lens, table, cache, 4, max(new), lse, w)
+    torch.cuda.synchronize()
+    assert B.mq_last_device_status(ws)[0] == B.MQ_ERR_INVALID_ARG
+    assert bool((o == 0).all())
+    counts = torch.cat([torch.arange(n - k + 1, n + 1) for k, n in zip(new, (50, 40))]).double()   # keys that a row sees
+    assert torch.allclose(lse.double().cpu(), counts.log()[:, None].expand(-1, 4), atol=1e-5)
+    assert torch.allclose(w.double().sum(-1).cpu(), torch.tensor([[2.0 * new[0]] * 2, [2.0 * new[1]] * 2]).double() + torch.tensor([[9.0 * 14], [9.0 * 24]]), atol=1e-4)
+
+
 def test_empty_calls_are_no_ops():
     pg = Paged([20], 2, 128, 16)
     ws = B.new_kv_attention_workspace(1, 1, 1, pg.table.shape[1], 4, pg.cache)

@@ -46,6 +46,10 @@ def _weights_case(new, lens, hq, hkv, dim, page, int8, aifs, seed, layout="head"
     ([100], [260], 8, 2, 128, 16, True, True),
     ([300], [700], 7, 1, 128, 64, False, False),
     ([9, 140], [4, 100], 4, 2, 128, 16, False, False),     # fewer keys than rows
+    ([2, 0, 1], [19, 5, 200], 130, 1, 128, 16, False, False),   # more query heads per key/value head than a row tile holds
+    ([1, 2], [130, 66], 150, 1, 64, 16, True, False),
+    ([1, 1, 1, 1], [64, 63, 65, 1], 4, 4, 64, 16, False, False),
+    ([4, 2], [60, 17], 8, 2, 128, 16, True, True),         # a few rows in AIFS order
 ])
 def test_weights(case):
     new, lens, hq, hkv, dim, page, int8, aifs = case
@@ -161,6 +165,8 @@ def _evict(pg, w, budget, n_first, n_last, dst_page, dst_layout="head", same_poo
     ([900, 10], 300, 0, 300, 2, 128, 64, 32, True, True),
     ([1500], 1499, 0, 1, 1, 128, 256, 256, False, True),
     ([100, 0, 50], 0, 0, 0, 2, 128, 16, 16, False, False),            # nothing is kept
+    ([30000, 24576, 24577], 700, 4, 20, 1, 64, 128, 64, True, True),   # more keys than the selection holds in shared memory
+    ([26000], 5000, 0, 0, 2, 64, 256, 32, False, False),
 ])
 def test_evict(lens, budget, first, last, hkv, dim, page, dst_page, int8, ties):
     pg = Paged(lens, hkv, dim, page, int8, "head", 77)
