@@ -58,6 +58,7 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
   __shared__ float ml_s[kWarps][kRows][2];
   __shared__ int64_t red[kWarps];
   int64_t* prefix = reinterpret_cast<int64_t*>(smem + kWarps * C::kRing);
+  KvSeq* seqs = reinterpret_cast<KvSeq*>(prefix + p.sched.b.n_seq + 1);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quad = lane >> 2, t4 = lane & 3;
   if (threadIdx.x == 0) {
     abort_flag = 0;
@@ -67,7 +68,7 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
   pdl_launch_dependents();
   pdl_wait();
   const KvSchedArgs& sc = p.sched;
-  sched_prefix<kThreads>(sc, prefix, red);
+  sched_prefix<kThreads>(sc, prefix, red, seqs);
   const int64_t total = prefix[sc.b.n_seq];
   const int64_t share = sched_share(sc, total, gridDim.x);
   KvRecord rec{};
@@ -77,7 +78,7 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
   uint32_t asked = 0, taken = 0;   // tiles of this warp so far (ring positions and phases run on over units)
   bool ok = true;
   while (at < stop) {
-    const KvUnit u = sched_unit(sc, prefix, at);
+    const KvUnit u = sched_unit(sc, prefix, at, seqs);
     const int len = (int)min((int64_t)(u.tiles + sc.extra - u.skip), stop - at);   // of this range on the line
     const int t0 = max(0, u.skip - sc.extra), t1 = max(0, u.skip + len - sc.extra);
     const int64_t unit_at = at - u.skip;
@@ -90,9 +91,18 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
     // ---- the warp's stream of tiles: tile t holds keys (t * kWarps + warp) * 16 ..; tiles behind the last key are not asked for
     const int first_key = (t0 * kWarps + warp) * 16;
     const int n_my = min(t1 - t0, end > first_key ? (end - first_key + kTile - 1) / kTile : 0);
-    auto page_of = [&](int i) -> int { return i < n_my ? table[(first_key + i * kTile) >> p.cache.page_shift] : 0; };
-    auto ask = [&](int i, int page) {
+    PageWindow pages(table, first_key, p.cache.page_shift, n_my, lane);
+    // query operands (column quad of block nt is row 8 nt + quad of the unit) and scales: asked for here, used below
+    uint32_t qf[kN][kSteps][2];
+#pragma unroll
+    for (int nt = 0; nt < kN; ++nt) {
+      const int r = row0 + 8 * nt + quad, tok = r / sc.group;
+      fetch_query<kD, kI8>(p.Q + (int64_t)(u.s.begin + tok) * p.ldq + (int64_t)(u.g * sc.group.d + r - tok * sc.group.d) * (kD * 2), 8 * nt + quad < n_rows, t4, qf[nt]);
+    }
+    const float k_scale = kI8 ? p.cache.k_scale[u.g] : 1.0f, v_scale = kI8 ? p.cache.v_scale[u.g] : 1.0f;
+    auto ask = [&](int i) {
       if (i >= n_my) return;
+      int page = pages.page(i, lane);
       if (lane == 0) {
         if ((unsigned)page >= (unsigned)p.cache.n_pages) {
           page = max(p.cache.n_pages, 1);   // a page number the maps do not have: zeros
@@ -106,27 +116,16 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
       }
       ++asked;
     };
-    int page_next = page_of(0);
 #pragma unroll
-    for (int i = 0; i < C::kStages - 1; ++i) {
-      const int pg = page_next;
-      page_next = page_of(i + 1);
-      ask(i, pg);
-    }
+    for (int i = 0; i < C::kStages - 1; ++i) ask(i);
 
-    // ---- query fragments (B operand): column quad of block nt is row 8 nt + quad of the unit
-    uint32_t qf[kN][kSteps][2];
     float fac[kN][2];               // scores -> log2 units, rows 2 t4 and 2 t4 + 1 of block nt
-    int lim[kN][2];                 // how far these rows see (below)
+    int lim[kN][2];                 // how far these rows see: without perm, keys below lim; with it, the context and the chunk's
+                                    // rows whose index is at most lim
     const int32_t* perm = sc.b.perm ? sc.b.perm + u.s.begin : nullptr;
-    const float base_fac = p.scale * 1.4426950408889634f * (kI8 ? p.cache.k_scale[u.g] : 1.0f);
 #pragma unroll
     for (int nt = 0; nt < kN; ++nt) {
-      const int r = 8 * nt + quad;
-      const int tok = (row0 + r) / sc.group;
-      load_query<kD, kI8>(p.Q + (int64_t)(u.s.begin + tok) * p.ldq + (int64_t)(u.g * sc.group.d + (row0 + r) - tok * sc.group.d) * (kD * 2), r < n_rows, t4,
-                          base_fac, qf[nt], fac[nt]);
-      // visibility: without perm, keys below lim; with it, the context and the chunk's rows whose index is not larger
+      finish_query<kD, kI8>(t4, p.scale * 1.4426950408889634f * k_scale, qf[nt], fac[nt]);
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const int rr = 8 * nt + 2 * t4 + e, tk = (row0 + rr) / sc.group;
@@ -151,9 +150,7 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
     }
 
     for (int i = 0; i < n_my; ++i) {
-      const int pg = page_next;
-      page_next = page_of(i + C::kStages);
-      ask(i + C::kStages - 1, pg);
+      ask(i + C::kStages - 1);
       const int stage = (int)(taken % C::kStages);
       if (!(ok = warp_all(mbar_wait(&full[warp][stage], (taken / C::kStages) & 1u, &abort_flag, p.status, 90)))) break;
       ++taken;
@@ -337,7 +334,6 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
     __syncthreads();
     const bool whole = t0 == 0 && t1 == u.tiles;
     const int slot = 2 * (int)blockIdx.x + (t0 == 0 ? 1 : 0);
-    const float vsc = kI8 ? p.cache.v_scale[u.g] : 1.0f;
     constexpr int kColThreads = kD / 2;                 // two channels per thread
     const int col = ((int)threadIdx.x % kColThreads) * 2;
     for (int r = (int)threadIdx.x / kColThreads; r < n_rows; r += kThreads / kColThreads) {
@@ -355,14 +351,14 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
       }
       if (whole) {
         const int tk = (row0 + r) / sc.group, tok = u.s.begin + tk, head = u.g * sc.group.d + (row0 + r) - tk * sc.group.d;
-        const float inv = ll == 0.0f ? 0.0f : vsc / ll;
+        const float inv = ll == 0.0f ? 0.0f : v_scale / ll;
         *reinterpret_cast<__nv_bfloat162*>(p.out.O + (int64_t)tok * p.out.ldo + (int64_t)head * kD + col) =
             __floats2bfloat162_rn(x * inv, y * inv);
         if (col == 0 && p.out.lse)
           p.out.lse[(int64_t)tok * p.out.n_q_heads + head] = ll == 0.0f ? -INFINITY : (mm + log2f(ll)) * 0.6931471805599453f;
       } else {
         if (col == 0) p.parts.ml[(int64_t)slot * kRows + r] = make_float2(mm, ll);
-        *reinterpret_cast<float2*>(p.parts.o + ((int64_t)slot * kRows + r) * kD + col) = make_float2(x * vsc, y * vsc);
+        *reinterpret_cast<float2*>(p.parts.o + ((int64_t)slot * kRows + r) * kD + col) = make_float2(x * v_scale, y * v_scale);
       }
     }
     if (t0 == 0 && !whole) {
@@ -485,9 +481,9 @@ kv_combine_kernel(const int pitch, const FastDiv group, const KvParts parts, con
 template <int kD, bool kI8, int kN>
 int launch_decode(const KvAttnArgs& a, int workers, cudaStream_t st) {
   using C = Cfg<kD, kI8, kN>;
-  const size_t smem = C::kSmem + ((size_t)a.sched.b.n_seq + 1) * sizeof(int64_t);
+  const size_t smem = C::kSmem + ((size_t)a.sched.b.n_seq + 1) * (sizeof(int64_t) + sizeof(KvSeq));
   static PerDeviceTable<char> attr_set;
-  if (!ensure_dynamic_smem(attr_set, kv_decode_kernel<kD, kI8, kN>, C::kSmem + (kMaxKvSeqs + 1) * (int)sizeof(int64_t))) return MQ_ERR_CUDA;
+  if (!ensure_dynamic_smem(attr_set, kv_decode_kernel<kD, kI8, kN>, C::kSmem + (kMaxKvSeqs + 1) * (int)(sizeof(int64_t) + sizeof(KvSeq)))) return MQ_ERR_CUDA;
   CUtensorMap mk, mv;
   if (!encode_key_tiles(&mk, a.cache.K, a.Q, a.cache, kD, kI8) || !encode_key_tiles(&mv, a.cache.V, a.Q, a.cache, kD, kI8)) return MQ_ERR_CUDA;
   const cudaError_t e = launch_pdl(kv_decode_kernel<kD, kI8, kN>, dim3((unsigned)workers), dim3(kThreads), smem, st, mk, mv, a);

@@ -41,9 +41,10 @@ __device__ __forceinline__ int sched_blocks(const KvSchedArgs& a, const KvSeq& s
 }
 
 // prefix[b] = length of all units before sequence b; prefix[n_seq] = the whole line.  Called by every thread of a block of kThreads;
-// `red` is shared scratch of kThreads / 32 entries.
+// `red` is shared scratch of kThreads / 32 entries.  `seqs`, if given, is shared memory that keeps the sequences' lengths for
+// sched_unit (a dependent global load per unit costs about as much as a tile).
 template <int kThreads>
-__device__ __forceinline__ void sched_prefix(const KvSchedArgs& a, int64_t* prefix, int64_t* red) {
+__device__ __forceinline__ void sched_prefix(const KvSchedArgs& a, int64_t* prefix, int64_t* red, KvSeq* seqs = nullptr) {
   const int n = a.b.n_seq, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int per = (n + kThreads - 1) / kThreads;
   int64_t sum = 0;
@@ -51,6 +52,7 @@ __device__ __forceinline__ void sched_prefix(const KvSchedArgs& a, int64_t* pref
     const int b = tid * per + k;
     if (b >= n) break;
     const KvSeq s = kv_seq(a.b, a.page_shift, a.max_q, b);
+    if (seqs) seqs[b] = s;
     const int blocks = sched_blocks(a, s);
     int64_t t = 0;
     if (a.b.perm) t = (int64_t)blocks * (blocks ? sched_tiles(a, s, 0) + a.extra : 0);
@@ -83,7 +85,7 @@ struct KvUnit {
   int b, g, rb, tiles, skip;
   KvSeq s;
 };
-__device__ __forceinline__ KvUnit sched_unit(const KvSchedArgs& a, const int64_t* prefix, int64_t at) {
+__device__ __forceinline__ KvUnit sched_unit(const KvSchedArgs& a, const int64_t* prefix, int64_t at, const KvSeq* seqs = nullptr) {
   int lo = 0, hi = a.b.n_seq;   // prefix[lo] <= at < prefix[hi]
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
@@ -92,7 +94,7 @@ __device__ __forceinline__ KvUnit sched_unit(const KvSchedArgs& a, const int64_t
   }
   KvUnit u;
   u.b = lo;
-  u.s = kv_seq(a.b, a.page_shift, a.max_q, lo);
+  u.s = seqs ? seqs[lo] : kv_seq(a.b, a.page_shift, a.max_q, lo);
   const int64_t all = prefix[lo + 1] - prefix[lo], x = at - prefix[lo];
   int64_t y;
   if (all >> 31) {

@@ -47,40 +47,66 @@ inline bool encode_key_tiles(CUtensorMap* map, const void* base, const void* any
 // Query row as column `quad` of a B operand: qf[k] = channels of step k.  fac[e] = what turns the scores of rows 2 t4 + e into
 // log2 units.  An int8 cache takes fp16 queries, brought into range by a power of two per row (they keep all their
 // bits), in the channel order that lets a thread read contiguous codes: step k, position (2 t4, 2 t4 + 1, 2 t4 + 8,
-// 2 t4 + 9) is channel t4 * D/4 + 4 k + 0 .. 3.
+// 2 t4 + 9) is channel t4 * D/4 + 4 k + 0 .. 3.  In two parts, so that the loads can travel while something else is done.
 template <int kD, bool kI8>
-__device__ __forceinline__ void load_query(const uint8_t* q, bool ok, int t4, float base_fac, uint32_t (&qf)[kD / 16][2], float (&fac)[2]) {
-  constexpr int kSteps = kD / 16;
-  if (!kI8) {
+__device__ __forceinline__ void fetch_query(const uint8_t* q, bool ok, int t4, uint32_t (&qf)[kD / 16][2]) {
 #pragma unroll
-    for (int k = 0; k < kSteps; ++k) {
+  for (int k = 0; k < kD / 16; ++k) {
+    if (kI8) {
+      const uint2 w = ok ? *reinterpret_cast<const uint2*>(q + (t4 * (kD / 4) + 4 * k) * 2) : make_uint2(0u, 0u);
+      qf[k][0] = w.x;
+      qf[k][1] = w.y;
+    } else {
       const int c = (k * 16 + 2 * t4) * 2;
       qf[k][0] = ok ? *reinterpret_cast<const uint32_t*>(q + c) : 0u;
       qf[k][1] = ok ? *reinterpret_cast<const uint32_t*>(q + c + 16) : 0u;
     }
-    fac[0] = fac[1] = base_fac;
-  } else {
-    uint2 w[kSteps];
+  }
+}
+template <int kD, bool kI8>
+__device__ __forceinline__ void finish_query(int t4, float base_fac, uint32_t (&qf)[kD / 16][2], float (&fac)[2]) {
+  constexpr int kSteps = kD / 16;
+  fac[0] = fac[1] = base_fac;
+  if (kI8) {
     float m = 0.0f;
 #pragma unroll
-    for (int k = 0; k < kSteps; ++k) {
-      w[k] = ok ? *reinterpret_cast<const uint2*>(q + (t4 * (kD / 4) + 4 * k) * 2) : make_uint2(0u, 0u);
-      m = fmaxf(m, fmaxf(fmaxf(fabsf(kv_bf16_lo(w[k].x)), fabsf(kv_bf16_hi(w[k].x))), fmaxf(fabsf(kv_bf16_lo(w[k].y)), fabsf(kv_bf16_hi(w[k].y)))));
-    }
+    for (int k = 0; k < kSteps; ++k)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) m = fmaxf(m, fmaxf(fabsf(kv_bf16_lo(qf[k][e])), fabsf(kv_bf16_hi(qf[k][e]))));
     m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
     m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
     // the power of two that brings the row's largest magnitude into [1, 2) (an infinity stays one either way)
-    const int e = m > 0.0f && m < INFINITY ? (int)((__float_as_uint(m) >> 23) & 255) - 127 : 0;
-    const float f = exp2f((float)-e), back = base_fac * exp2f((float)e);
+    const int e2 = m > 0.0f && m < INFINITY ? (int)((__float_as_uint(m) >> 23) & 255) - 127 : 0;
+    const float f = exp2f((float)-e2), back = base_fac * exp2f((float)e2);
 #pragma unroll
-    for (int k = 0; k < kSteps; ++k) {
-      qf[k][0] = kv_pack_f16(kv_bf16_lo(w[k].x) * f, kv_bf16_hi(w[k].x) * f);
-      qf[k][1] = kv_pack_f16(kv_bf16_lo(w[k].y) * f, kv_bf16_hi(w[k].y) * f);
-    }
+    for (int k = 0; k < kSteps; ++k)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) qf[k][e] = kv_pack_f16(kv_bf16_lo(qf[k][e]) * f, kv_bf16_hi(qf[k][e]) * f);
     fac[0] = __shfl_sync(0xffffffffu, back, 8 * t4);
     fac[1] = __shfl_sync(0xffffffffu, back, 8 * t4 + 4);
   }
 }
+
+// Pages of a warp's tiles i = 0, 1, .. (the tile's first key is first_key + i * kStreamTile): lane l holds that of tile
+// base + l, so the table is read once per 32 tiles.
+struct PageWindow {
+  const int32_t* table;
+  int first_key, shift, n, base, mine;
+  __device__ __forceinline__ void fetch(int lane) {
+    const int i = base + lane;
+    mine = i < n ? table[(first_key + i * kStreamTile) >> shift] : 0;
+  }
+  __device__ __forceinline__ PageWindow(const int32_t* t, int first, int sh, int tiles, int lane) : table(t), first_key(first), shift(sh), n(tiles), base(0) {
+    fetch(lane);
+  }
+  __device__ __forceinline__ int page(int i, int lane) {   // every lane asks for the same i, in order
+    if (i - base >= 32) {
+      base = i;
+      fetch(lane);
+    }
+    return __shfl_sync(0xffffffffu, mine, i - base);
+  }
+};
 
 // S^T = K Q^T of 16 keys: s[nt] = (key quad, row 2 t4), (quad, 2 t4 + 1), (quad + 8, 2 t4), (quad + 8, 2 t4 + 1) of block nt.
 // Two chains of products each, so that they overlap.

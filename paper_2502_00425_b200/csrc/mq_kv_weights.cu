@@ -105,9 +105,10 @@ kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
     const int32_t *table = p.b.page_table + (int64_t)b * p.b.max_pages, *perm = p.b.perm ? p.b.perm + s.begin : nullptr;
     const int first_key = (t0 * kWarps + warp) * 16;
     const int n_my = min(t1 - t0, s.n_all > first_key ? (s.n_all - first_key + kTile - 1) / kTile : 0);
-    auto page_of = [&](int i) -> int { return i < n_my ? table[(first_key + i * kTile) >> p.c.page_shift] : 0; };
-    auto ask = [&](int i, int page) {
+    PageWindow pages(table, first_key, p.c.page_shift, n_my, lane);
+    auto ask = [&](int i) {
       if (i >= n_my) return;
+      int page = pages.page(i, lane);
       if (lane == 0) {
         if ((unsigned)page >= (unsigned)p.c.n_pages) {
           page = max(p.c.n_pages, 1);   // a page number the map does not have: zeros
@@ -119,13 +120,6 @@ kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
       }
       ++asked;
     };
-    int page_next = page_of(0);
-#pragma unroll
-    for (int i = 0; i < C::kStages - 1; ++i) {
-      const int pg = page_next;
-      page_next = page_of(i + 1);
-      ask(i, pg);
-    }
 
     // ---- a block of query rows: operands, what turns scores into log2 units, log-sum-exps (log2 units), and sight
     const int n_rows = s.n_new * p.group.d, blocks = (n_rows + kRows - 1) / kRows;
@@ -133,28 +127,38 @@ kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
     uint32_t qf[kN][kD / 16][2];
     float fac[kN][2], nl[kN][2];
     int lim[kN][2], all_see = INT_MAX;   // every row of the block sees the keys below all_see
-    auto rows_of = [&](int row0) {
+    auto fetch_rows = [&](int row0) {
 #pragma unroll
       for (int nt = 0; nt < kN; ++nt) {
         const int r = row0 + 8 * nt + quad, tok = r / p.group;
-        load_query<kD, kI8>(p.Q + (int64_t)(s.begin + tok) * p.ldq + (int64_t)(g * p.group.d + r - tok * p.group.d) * (kD * 2), r < n_rows, t4, base_fac, qf[nt], fac[nt]);
+        fetch_query<kD, kI8>(p.Q + (int64_t)(s.begin + tok) * p.ldq + (int64_t)(g * p.group.d + r - tok * p.group.d) * (kD * 2), r < n_rows, t4, qf[nt]);
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const int rr = row0 + 8 * nt + 2 * t4 + e, tk = rr / p.group;
           const bool live = rr < n_rows;
           const float l = live ? p.lse[(int64_t)(s.begin + tk) * p.n_q_heads + g * p.group.d + rr - tk * p.group.d] : INFINITY;
-          nl[nt][e] = fabsf(l) == INFINITY ? -INFINITY : l * -1.4426950408889634f;   // (a row that sees nothing has -inf and adds nothing)
+          nl[nt][e] = l;
           lim[nt][e] = !live ? INT_MIN : perm ? perm[tk] : ctx + tk + 1;
         }
       }
       all_see = row0 + kRows > n_rows ? INT_MIN : perm ? ctx : ctx + row0 / p.group + 1;
     };
-    if (blocks > 0) rows_of(0);
+    auto finish_rows = [&]() {
+#pragma unroll
+      for (int nt = 0; nt < kN; ++nt) {
+        finish_query<kD, kI8>(t4, base_fac, qf[nt], fac[nt]);
+#pragma unroll
+        for (int e = 0; e < 2; ++e)   // (a row that sees nothing has -inf and adds nothing)
+          nl[nt][e] = fabsf(nl[nt][e]) == INFINITY ? -INFINITY : nl[nt][e] * -1.4426950408889634f;
+      }
+    };
+    if (blocks > 0) fetch_rows(0);
+#pragma unroll
+    for (int i = 0; i < C::kStages - 1; ++i) ask(i);
+    if (blocks > 0) finish_rows();
 
     for (int i = 0; i < n_my; ++i) {
-      const int pg = page_next;
-      page_next = page_of(i + C::kStages);
-      ask(i + C::kStages - 1, pg);
+      ask(i + C::kStages - 1);
       const int st = (int)(taken % C::kStages), key0 = first_key + i * kTile;
       // what the two keys of this lane had (asked for before the wait)
       const int ka = key0 + quad, kb = ka + 8;
@@ -168,7 +172,10 @@ kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
       ++taken;
       float sum_a = 0.0f, sum_b = 0.0f;
       for (int blk = 0; blk < blocks; ++blk) {
-        if (blocks > 1) rows_of(blk * kRows);
+        if (blocks > 1) {
+          fetch_rows(blk * kRows);
+          finish_rows();
+        }
         float sc[kN][4];
         key_scores<kD, kI8, kN>(ring + (uint32_t)(st * C::kStage), lane, qf, sc);
         const bool masked = key0 + 16 > all_see;
