@@ -32,8 +32,8 @@ template <int kD, bool kI8, int kN>
 struct Cfg {
   static constexpr int kRows = 8 * kN;
   static constexpr int kStage = 2 * KeyTile<kD, kI8>::kBytes;   // K and V of 16 keys
-  static constexpr int kCtas = kStage == 8192 ? 2 : kN == 1 ? 4 : 3;   // per SM
-  static constexpr int kStages = kStage == 2048 ? 4 : 3;
+  static constexpr int kCtas = kStage == 8192 && kN == 2 ? 2 : 3;   // per SM
+  static constexpr int kStages = kStage == 8192 && kN == 1 ? 2 : kStage == 8192 ? 3 : 4;
   static constexpr int kRing = kStage * kStages;
   static constexpr int kPitch = kD + 4;                  // floats between rows of the warps' results
   static constexpr int kSmem = 1024 + kWarps * kRing;    // (swizzled tiles stand on 1024-byte boundaries)
