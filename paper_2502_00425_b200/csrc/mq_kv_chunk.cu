@@ -66,7 +66,7 @@ struct ChunkCfg {
   static constexpr int kHalves = kD / 64;
   static constexpr int kTileBytes = kHalves * kHalfBytes;
   static constexpr int kThreads = (kI8 ? 16 : 12) * 32;
-  static constexpr int kSmem = 1024 + (2 + 2 * kStages) * kTileBytes + (int)sizeof(ChunkBarriers) + kRing * (int)sizeof(Piece) + 8 * 64 * 4 + 16 * 8;
+  static constexpr int kSmem = 1024 + (2 + 2 * kStages) * kTileBytes + (int)sizeof(ChunkBarriers) + kRing * (int)sizeof(Piece) + 8 * kTile * 4 + 16 * 8;
 };
 
 // B operand whose N (64 channels per block, 128-byte swizzle) is contiguous: blocks `block_bytes` apart, 8-key groups 1024 apart
@@ -87,8 +87,8 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
   uint8_t* v_smem = k_smem + kStages * kTileBytes;
   ChunkBarriers* sh = reinterpret_cast<ChunkBarriers*>(v_smem + kStages * kTileBytes);
   Piece* ring = reinterpret_cast<Piece*>(sh + 1);
-  int32_t* kp_all = reinterpret_cast<int32_t*>(ring + kRing);   // [8 warps][64]
-  int64_t* red = reinterpret_cast<int64_t*>(kp_all + 8 * 64);
+  int32_t* kp_all = reinterpret_cast<int32_t*>(ring + kRing);   // [8 warps][128]
+  int64_t* red = reinterpret_cast<int64_t*>(kp_all + 8 * kTile);
   int64_t* prefix = red + 16;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
@@ -357,14 +357,15 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
           bool hit = false;
           if (all_see < end) {
             // the largest magnitude of the 16-bit halves shows an infinity or NaN
-            uint32_t top = 0u;
+            uint32_t part[4] = {0u, 0u, 0u, 0u};
 #pragma unroll 8
             for (int c = 0; c < kTileBytes / 512; ++c) {
               const uint4 v = *reinterpret_cast<const uint4*>(vt + (c * 32 + lane) * 16);
               uint32_t m4 = __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
               if ((((c * 32 + lane) & 1023) >> 3) >= n_ok) m4 = 0u;
-              top = __vmaxu2(top, m4);
+              part[c & 3] = __vmaxu2(part[c & 3], m4);
             }
+            const uint32_t top = __vmaxu2(__vmaxu2(part[0], part[1]), __vmaxu2(part[2], part[3]));
             hit = __any_sync(0xffffffffu, (top & 0xffffu) >= 0x7f80u || (top >> 16) >= 0x7f80u);
           }
           if (hit || n_ok < kTile) {
@@ -402,7 +403,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
     const int row = quarter * 32 + lane;
     const uint32_t lane_base = tmem_base + ((uint32_t)(quarter * 32) << 16);
     const uint32_t s_base = lane_base + (uint32_t)(grp * 128), o_addr = lane_base + kColO + (uint32_t)(grp * 128);
-    int32_t* kp = kp_all + (warp - 4) * 64;
+    int32_t* kp = kp_all + (warp - 4) * kTile;
     bool ok = true;
     uint32_t cnt = 0;                            // tiles of this group so far
     for (int np = 0; ok; ++np) {
@@ -424,8 +425,27 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
       const float lag_raw = kLag / scale_log2, lift_raw = kI8 ? kLiftChunk / scale_log2 : 0.0f;
       float m_used = -1.0e30f, l_run = 0.0f;   // the exponents' reference (raw units), the sum relative to it
       bool begun = false;                      // the accumulator holds products of this piece
+      // ranks of the keys of the next masked tile, asked for a tile ahead
+      int32_t rank_next[4];
+      auto ask_ranks = [&](int tile) {
+        if (perm && tile < t1 && tile * kTile + kTile > all_see) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const int j = tile * kTile + c * 32 + lane;
+            rank_next[c] = j >= end ? INT_MAX : j < ctx ? -1 : perm[j - ctx];
+          }
+        }
+      };
+      ask_ranks(pc->t0);
       for (int tile = pc->t0; tile < t1 && ok; ++tile, ++cnt) {
         const bool masked = tile * kTile + kTile > all_see;           // (also where the tile passes `end`)
+        if (masked && perm) {
+          __syncwarp();
+#pragma unroll
+          for (int c = 0; c < 4; ++c) kp[c * 32 + lane] = rank_next[c];
+          __syncwarp();
+        }
+        ask_ranks(tile + 1);
         if (!(ok = warp_all(mbar_wait(&sh->s_full[grp], cnt & 1u, &sh->abort_flag, p.status, 59)))) break;
         tc_fence_after();
 #pragma unroll 1
@@ -434,22 +454,12 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
           uint32_t sv[64];
           tmem_ld_x32(s_addr, *reinterpret_cast<uint32_t (*)[32]>(&sv[0]));
           tmem_ld_x32(s_addr + 32u, *reinterpret_cast<uint32_t (*)[32]>(&sv[32]));
-          if (masked && perm) {
-            const int base = tile * kTile + h * 64;
-            __syncwarp();
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-              const int j = base + c * 32 + lane;
-              kp[c * 32 + lane] = j >= end ? INT_MAX : j < ctx ? -1 : perm[j - ctx];
-            }
-            __syncwarp();
-          }
           tmem_wait_ld();
           if (masked) {
             if (perm) {
 #pragma unroll
               for (int e4 = 0; e4 < 64; e4 += 4) {
-                const int4 k4 = *reinterpret_cast<const int4*>(kp + e4);
+                const int4 k4 = *reinterpret_cast<const int4*>(kp + h * 64 + e4);
                 if (k4.x > lim) sv[e4] = 0xff800000u;
                 if (k4.y > lim) sv[e4 + 1] = 0xff800000u;
                 if (k4.z > lim) sv[e4 + 2] = 0xff800000u;
