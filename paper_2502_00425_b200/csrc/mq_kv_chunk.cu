@@ -40,6 +40,25 @@ constexpr float kLag = 8.0f;            // log2 of how far a row's maximum may o
 constexpr float kLiftChunk = 6.0f;
 constexpr int kRing = 8;                // published pieces
 
+// v[k] of lane q of four neighbours <-> v[q] of lane k
+__device__ __forceinline__ void quad_transpose(uint4 (&v)[4], int lane) {
+#pragma unroll
+  for (int o = 1; o < 4; o <<= 1) {
+    const bool up = lane & o;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (k & o) continue;
+      uint4 x = up ? v[k] : v[k | o];
+      x.x = __shfl_xor_sync(0xffffffffu, x.x, o);
+      x.y = __shfl_xor_sync(0xffffffffu, x.y, o);
+      x.z = __shfl_xor_sync(0xffffffffu, x.z, o);
+      x.w = __shfl_xor_sync(0xffffffffu, x.w, o);
+      if (up) v[k] = x;
+      else v[k | o] = x;
+    }
+  }
+}
+
 // What a worker does next on the line: tiles t0 .. t1 - 1 of a unit (t0 == t1: the line's end).
 struct Piece {
   int t0, t1, end, ctx;
@@ -529,6 +548,14 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
       const int head = pc->g * sc.group.d + (pc->row0 + unit_row) - tok * sc.group.d;
       const int64_t out_row = (int64_t)(pc->begin + tok);
       const bool poison = !kI8 && *reinterpret_cast<const volatile int*>(&pc->poison) != 0;
+      // Four neighbouring lanes exchange 16-byte pieces so that they write 64 contiguous bytes of one row after the other (a
+      // lane writing its own row makes every store instruction touch 32 lines: 10 instead of 4 k cycles per piece).
+      const uint8_t* mine = whole ? reinterpret_cast<const uint8_t*>(p.out.O + out_row * p.out.ldo + (int64_t)head * kD)
+                                  : reinterpret_cast<const uint8_t*>(p.parts.o + at_part * kD);
+      uint8_t* dst[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        dst[k] = reinterpret_cast<uint8_t*>(__shfl_sync(0xffffffffu, live ? reinterpret_cast<unsigned long long>(mine) : 0ull, (lane & ~3) | k));
 #pragma unroll 1
       for (int cb = 0; cb < kD; cb += 32) {
         uint32_t a[32];
@@ -554,17 +581,27 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
             }
           }
         }
-        if (live) {
-          if (whole) {
-            __nv_bfloat16* dst = p.out.O + out_row * p.out.ldo + (int64_t)head * kD + cb;
+        if (whole) {
+          uint4 v[4];
 #pragma unroll
-            for (int e = 0; e < 32; e += 8)
-              *reinterpret_cast<uint4*>(dst + e) = make_uint4(kv_pack_bf16(o[e], o[e + 1]), kv_pack_bf16(o[e + 2], o[e + 3]),
-                                                              kv_pack_bf16(o[e + 4], o[e + 5]), kv_pack_bf16(o[e + 6], o[e + 7]));
-          } else {
-            float* part = p.parts.o + at_part * kD + cb;
+          for (int k = 0; k < 4; ++k)
+            v[k] = make_uint4(kv_pack_bf16(o[8 * k], o[8 * k + 1]), kv_pack_bf16(o[8 * k + 2], o[8 * k + 3]), kv_pack_bf16(o[8 * k + 4], o[8 * k + 5]),
+                              kv_pack_bf16(o[8 * k + 6], o[8 * k + 7]));
+          quad_transpose(v, lane);
 #pragma unroll
-            for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(part + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+          for (int k = 0; k < 4; ++k)
+            if (dst[k]) *reinterpret_cast<uint4*>(dst[k] + cb * 2 + (lane & 3) * 16) = v[k];
+        } else {
+#pragma unroll
+          for (int e = 0; e < 32; e += 16) {
+            uint4 v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              v[k] = make_uint4(__float_as_uint(o[e + 4 * k]), __float_as_uint(o[e + 4 * k + 1]), __float_as_uint(o[e + 4 * k + 2]), __float_as_uint(o[e + 4 * k + 3]));
+            quad_transpose(v, lane);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              if (dst[k]) *reinterpret_cast<uint4*>(dst[k] + (cb + e) * 4 + (lane & 3) * 16) = v[k];
           }
         }
       }
