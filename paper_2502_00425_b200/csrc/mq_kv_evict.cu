@@ -34,7 +34,7 @@ struct EvictParams {
 };
 
 __device__ __forceinline__ int evict_len(const EvictParams& p, int b) {
-  return (int)min((int64_t)max(p.kv_len[b], 0), (int64_t)p.max_pages << p.src.page_shift);
+  return (int)min((int64_t)max(__ldcg(p.kv_len + b), 0), (int64_t)p.max_pages << p.src.page_shift);
 }
 
 // Larger weights have larger images; NaN has the smallest, and the two zeros are one.

@@ -1,0 +1,133 @@
+"""A paged key/value cache for one decoder block: the bookkeeping around the library's cache calls.
+
+`PagedKVCache` owns the pool of pages, says which pages hold which sequence, and turns "these sequences get so many new
+tokens" into the device arrays that mq_qk_norm_rope, mq_kv_attention, mq_kv_weights and mq_kv_evict take.  Lengths and
+page lists are kept on the host (that is where a serving program decides); nothing here computes on keys or values.
+"""
+from __future__ import annotations
+
+from dataclasses import dataclass
+from typing import List, Optional, Sequence
+
+import torch
+
+from . import binding as B
+
+
+@dataclass
+class CacheStep:
+    """Device arrays for one step's new rows: the rows of sequence b are cu_q[b] .. cu_q[b + 1] - 1."""
+    new: List[int]
+    cu_q: torch.Tensor        # int32 [n_seq + 1]
+    kv_len: torch.Tensor      # int32 [n_seq], the new keys included
+    slots: torch.Tensor       # int64 [total], where each new row goes
+    pos: torch.Tensor         # int32 [total], token positions in the order of the sequence
+    total: int
+    max_q: int
+
+    def cu_q_host(self, b: int) -> int:
+        return sum(self.new[:b])
+
+
+class PagedKVCache:
+    """n_seq sequences of up to max_len keys in n_pages pages of page_size tokens.  dtype bf16, or int8 with the static scales
+    k_scale, v_scale (float32 [n_kv_heads])."""
+
+    def __init__(self, n_seq: int, n_pages: int, max_len: int, n_kv_heads: int, head_dim: int, page_size: int = 64,
+                 k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None, device="cuda"):
+        dtype = torch.int8 if k_scale is not None else torch.bfloat16
+        shape = (n_pages, n_kv_heads, page_size, head_dim)
+        self.K, self.V = (torch.zeros(shape, dtype=dtype, device=device) for _ in range(2))
+        self.handle = B.KVCache(self.K, self.V, k_scale, v_scale)
+        self.n_seq, self.max_len, self.page_size, self.device = n_seq, max_len, page_size, device
+        self.free = list(range(n_pages))[::-1]
+        self.pages: List[List[int]] = [[] for _ in range(n_seq)]
+        self.lengths = [0] * n_seq       # keys in the cache
+        self.tokens = [0] * n_seq        # tokens seen: the next token's position (eviction does not change it)
+        self.table = torch.full((n_seq, -(-max_len // page_size)), -1, dtype=torch.int32, device=device)
+        self.weights: Optional[torch.Tensor] = None   # accumulated softmax weights, once track_weights() was called
+        self._ws = {}
+
+    def _take(self, n: int) -> List[int]:
+        if n > len(self.free):
+            raise RuntimeError(f"the cache has {len(self.free)} free pages, {n} are needed")
+        return [self.free.pop() for _ in range(n)]
+
+    def _show(self, b: int):
+        row = torch.full((self.table.shape[1],), -1, dtype=torch.int32)
+        row[:len(self.pages[b])] = torch.tensor(self.pages[b], dtype=torch.int32)
+        self.table[b].copy_(row)
+
+    def track_weights(self):
+        """Keeps the softmax weight every key receives (mq_kv_weights), for evict()."""
+        self.weights = torch.zeros((self.n_seq, self.handle.n_kv_heads, self.max_len), device=self.device)
+
+    def extend(self, new: Sequence[int]) -> CacheStep:
+        """Room for new[b] tokens at the end of every sequence b, and the arrays of the step that brings them."""
+        assert len(new) == self.n_seq and min(new) >= 0
+        ps, slots, pos, cu = self.page_size, [], [], [0]
+        for b, n in enumerate(new):
+            if self.lengths[b] + n > self.max_len:
+                raise RuntimeError(f"sequence {b} would have {self.lengths[b] + n} keys, the cache was made for {self.max_len}")
+        need = [max(0, -(-(self.lengths[b] + n) // ps) - len(self.pages[b])) for b, n in enumerate(new)]
+        fresh = self._take(sum(need))
+        for b, n in enumerate(new):
+            if need[b]:
+                self.pages[b] += [fresh.pop() for _ in range(need[b])]
+                self._show(b)
+            slots += [self.pages[b][j // ps] * ps + j % ps for j in range(self.lengths[b], self.lengths[b] + n)]
+            pos += range(self.tokens[b], self.tokens[b] + n)
+            self.lengths[b] += n
+            self.tokens[b] += n
+            cu.append(cu[-1] + n)
+        dev = lambda v, t: torch.tensor(v, dtype=t).to(self.device)
+        return CacheStep(list(new), dev(cu, torch.int32), dev(self.lengths, torch.int32), dev(slots, torch.int64),
+                         dev(pos, torch.int32), cu[-1], max(new))
+
+    def workspace(self, step: CacheStep, n_q_heads: int) -> torch.Tensor:
+        key = (step.total, step.max_q, n_q_heads)
+        if key not in self._ws:
+            self._ws[key] = B.new_kv_attention_workspace(self.n_seq, step.total, step.max_q, self.table.shape[1], n_q_heads,
+                                                         self.handle)
+        return self._ws[key]
+
+    def attend(self, q: torch.Tensor, step: CacheStep, n_q_heads: int, perm: Optional[torch.Tensor] = None,
+               scale: Optional[float] = None) -> torch.Tensor:
+        """Attention of the step's rows over the cache (their keys and values are already stored); adds to the tracked weights."""
+        o = torch.empty_like(q)
+        lse = torch.empty((step.total, n_q_heads), device=q.device)
+        B.mq_kv_attention(q, step.cu_q, step.kv_len, self.table, self.handle, n_q_heads, step.max_q, o, self.workspace(step, n_q_heads),
+                          lse=lse, perm=perm, scale=scale)
+        if self.weights is not None:
+            B.mq_kv_weights(q, step.cu_q, step.kv_len, self.table, self.handle, n_q_heads, step.max_q, lse, self.weights,
+                            w_in=self.weights, perm=perm, scale=scale)
+        return o
+
+    def evict(self, budget: int, n_first: int, n_last: int) -> torch.Tensor:
+        """Cuts every sequence to `budget` keys per head by the tracked weights; returns the kept indices (as mq_kv_evict's
+        `kept`; entries behind a sequence's new length are -1).  The kept rows move to fresh pages, the old ones are freed."""
+        if self.weights is None:
+            raise RuntimeError("track_weights() first")
+        ps = self.page_size
+        after = [min(n, budget) for n in self.lengths]
+        pool = self._take(sum(-(-n // ps) for n in after))
+        fresh = [[pool.pop() for _ in range(-(-n // ps))] for n in after]
+        table = torch.full((self.n_seq, max(1, -(-budget // ps))), -1, dtype=torch.int32)
+        for b, p in enumerate(fresh):
+            table[b, :len(p)] = torch.tensor(p, dtype=torch.int32)
+        kept = torch.full((self.n_seq, self.handle.n_kv_heads, budget), -1, dtype=torch.int32, device=self.device)
+        new_len = torch.empty(self.n_seq, dtype=torch.int32, device=self.device)
+        w_out = torch.zeros((self.n_seq, self.handle.n_kv_heads, budget), device=self.device)
+        B.mq_kv_evict(self.handle, self.table, torch.tensor(self.lengths, dtype=torch.int32).to(self.device), self.weights, budget,
+                      n_first, n_last, self.handle, table.to(self.device), kept, new_len, w_out=w_out)
+        m = min(budget, self.max_len)
+        self.weights.zero_()
+        self.weights[:, :, :m] = w_out[:, :, :m]
+        for b in range(self.n_seq):
+            self.free += self.pages[b]
+            self.pages[b], self.lengths[b] = fresh[b], after[b]
+            self._show(b)
+        return kept
+
+    def status_ok(self) -> bool:
+        return all(B.mq_last_device_status(ws)[0] == B.MQ_OK for ws in self._ws.values())

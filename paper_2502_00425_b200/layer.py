@@ -121,6 +121,9 @@ class W4A8DecoderBlock:
         # True: attention under the unified mask runs as the library's tensor-core kernel (mq_aifs_attention),
         # in AIFS order, straight from the permutation -- no dense mask, no reordering; head_dim must be 128
         self.cuda_attention = shape.head_dim == 128
+        # RMSNorm gains of the query and key heads (float32 [head_dim]), for blocks that norm them; used by forward_cached
+        self.g_q: Optional[torch.Tensor] = None
+        self.g_k: Optional[torch.Tensor] = None
 
     # ---- pieces ------------------------------------------------------------------------
     def aifs(self, embs, is_visuals, tr: BlockTrace) -> torch.Tensor:
@@ -277,6 +280,17 @@ class W4A8DecoderBlock:
         else:
             a = torch.cat([gqa_attention(qr[bd[b]:bd[b + 1]], kr[bd[b]:bd[b + 1]], v[bd[b]:bd[b + 1]], tr.masks[b],
                                          sh.n_q_heads, sh.n_kv_heads) for b in range(n_seq)])
+        x2 = self._behind_attention(x0, a, tr, calibrate)
+        outs = []
+        for b in range(n_seq):
+            out = torch.empty((bd[b + 1] - bd[b], x2.shape[1]), dtype=torch.bfloat16, device=x2.device)
+            B.mq_aifs_reorder(x2[bd[b]:bd[b + 1]], out, None, None, tr.perms[b], None, None, direction=1)
+            outs.append(out)
+        return outs, tr
+
+    def _behind_attention(self, x0, a, tr: BlockTrace, calibrate: bool) -> torch.Tensor:
+        """Output projection, residual, MLP: from the attention's result to the block's."""
+        t = tr.tensors
         t["attn"] = a
         o = self.linear("o_proj", a, tr, calibrate)
         x1 = self._add(x0, o)
@@ -293,11 +307,48 @@ class W4A8DecoderBlock:
         down = self.linear("down_proj", act, tr, calibrate)
         x2 = self._add(x1, down)
         t["resid2"] = x2
-        outs = []
-        for b in range(n_seq):
-            out = torch.empty((bd[b + 1] - bd[b], x2.shape[1]), dtype=torch.bfloat16, device=x2.device)
-            B.mq_aifs_reorder(x2[bd[b]:bd[b + 1]], out, None, None, tr.perms[b], None, None, direction=1)
-            outs.append(out)
+        return x2
+
+    def forward_cached(self, embs, cache, is_visuals=None, calibrate: bool = False):
+        """New tokens of every sequence of a PagedKVCache (one each, a few, or a chunk; empty ones are allowed): lists of
+        bf16 [n_b, hidden] and, where a chunk has visual tokens, uint8 [n_b] (None: text only, no reordering).  Queries and
+        keys are normed (g_q, g_k, if set) and rotated at their positions behind what the cache holds, keys and values
+        are stored, and the rows attend the cached context and, causally in the original order, their chunk.  Returns
+        (outputs in the original order, BlockTrace)."""
+        sh, tr = self.shape, BlockTrace()
+        t = tr.tensors
+        live = [b for b, e in enumerate(embs) if e.shape[0]]
+        if not live:
+            return list(embs), tr
+        step = cache.extend([e.shape[0] for e in embs])
+        perm = None
+        if is_visuals is None:
+            x0 = torch.cat([embs[b] for b in live])
+            tr.seg = B.Segments(torch.empty(0, dtype=torch.int32, device=x0.device), torch.empty(0, dtype=torch.uint8, device=x0.device))
+            pos = step.pos
+        else:
+            x0 = self.aifs([embs[b] for b in live], [is_visuals[b] for b in live], tr)
+            perm = torch.cat(tr.perms)
+            # positions of the rows where they stand now; the cache holds a chunk's keys in the same order
+            starts = torch.cat([torch.full_like(p, step.cu_q_host(b)) for b, p in zip(live, tr.perms)])
+            pos = step.pos[(starts + perm).long()].contiguous()
+        t["emb_u"] = x0
+        h = self._rmsnorm(x0, self.g_attn)
+        q, k, v = self.linear_group(["q_proj", "k_proj", "v_proj"], h, tr, calibrate)
+        qr = torch.empty((step.total, sh.n_q_heads * sh.head_dim), dtype=torch.bfloat16, device=x0.device)
+        B.mq_qk_norm_rope(q, k, pos, sh.n_q_heads, sh.n_kv_heads, qr, gain_q=self.g_q, gain_k=self.g_k, v=v, cache=cache.handle,
+                          slots=step.slots)
+        t["q_rope"] = qr
+        x2 = self._behind_attention(x0, cache.attend(qr, step, sh.n_q_heads, perm), tr, calibrate)
+        outs, at = [], 0
+        for b, n in enumerate(step.new):
+            rows = x2[at:at + n]
+            if n and is_visuals is not None:
+                out = torch.empty((n, x2.shape[1]), dtype=torch.bfloat16, device=x2.device)
+                B.mq_aifs_reorder(rows, out, None, None, tr.perms[live.index(b)], None, None, direction=1)
+                rows = out
+            outs.append(rows)
+            at += n
         return outs, tr
 
     # ---- glue: the library's single-pass kernels, or the torch expressions -------------------------

@@ -302,6 +302,21 @@ def test_a_cache_without_pages_reads_as_zeros(new):
     assert torch.allclose(w.double().sum(-1).cpu(), torch.tensor([[2.0 * new[0]] * 2, [2.0 * new[1]] * 2]).double() + torch.tensor([[9.0 * 14], [9.0 * 24]]), atol=1e-4)
 
 
+@pytest.mark.parametrize("new_most", [1, 20])
+def test_the_most_sequences_of_a_call(new_most):
+    """2048 sequences, some without keys or without new tokens, lengths below and above one tile."""
+    rng = np.random.default_rng(5)
+    new = [int(x) for x in rng.integers(0, new_most + 1, 2048)]
+    lens = [int(x) + n for x, n in zip(rng.integers(0, 70, 2048), new)]
+    pg, q = _inputs(new, lens, 4, 2, 64, 16, False, "head", 50)
+    o, lse = _run(pg, q, new, 4)
+    _check(pg, q, new, 4, o, lse, seqs=set(range(0, 2048, 17)) | {2047}, heads=[0, 3])
+    w = torch.zeros((2048, 2, max(lens)), device=DEV)
+    B.mq_kv_weights(q.to(DEV), cu(new), pg.kv_len, pg.table, pg.cache, 4, max(new), torch.from_numpy(lse.astype(np.float32)).to(DEV), w)
+    sums = w.double().sum(-1).cpu().numpy()
+    assert np.allclose(sums, np.array(new)[:, None] * 2.0 * np.ones((1, 2)), rtol=2e-5, atol=1e-6)   # every row hands out weight 1
+
+
 def test_empty_calls_are_no_ops():
     pg = Paged([20], 2, 128, 16)
     ws = B.new_kv_attention_workspace(1, 1, 1, pg.table.shape[1], 4, pg.cache)
