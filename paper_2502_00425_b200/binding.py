@@ -524,85 +524,83 @@ def _addr(t: Optional[torch.Tensor]):
     return t.data_ptr()
 
 
-# The cache calls are made once per layer and token, so their wrappers are written for few Python steps: one look at a
-# tensor's device gives its address or the refusal, the stream comes as a bare handle, types are compared once each.
+# The cache calls are made once per layer and token, so their wrappers are written for few Python steps: one look at each
+# property of a tensor, the stream as a bare handle.
 _BF16, _F32, _I32, _I64 = torch.bfloat16, torch.float32, torch.int32, torch.int64
+_current_device, _raw_stream = torch.cuda.current_device, torch._C._cuda_getCurrentRawStream
 
 
-def _at(t: torch.Tensor, device: int) -> int:
-    """Device address of t, which must live on CUDA device number `device`."""
+def _elsewhere(t: torch.Tensor, device: int):
+    if not t.is_cuda:
+        raise ValueError("tensor must live on a CUDA device (the library has no CPU path)")
+    raise ValueError(f"tensor on {t.device}, expected cuda:{device}")
+
+
+def _rows(t: torch.Tensor, shape, device: int):
+    """(address, leading dimension) of a bf16 matrix of this shape on this device, rows contiguous."""
+    if t.dtype != _BF16 or t.shape != shape:
+        raise ValueError(f"expected bf16 {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
     if t.get_device() != device:
-        if not t.is_cuda:
-            raise ValueError("tensor must live on a CUDA device (the library has no CPU path)")
-        raise ValueError(f"tensor on {t.device}, expected cuda:{device}")
+        _elsewhere(t, device)
+    pitch, unit = t.stride()
+    if unit != 1 and shape[1] > 1:
+        raise ValueError("rows must be contiguous")
+    return t.data_ptr(), pitch if shape[0] > 1 else max(pitch, shape[1])   # (a single row may carry any stride in torch)
+
+
+def _vec(t: Optional[torch.Tensor], dtype, n: int, device: int):
+    """Address of a contiguous tensor of n elements of this type on this device (None: NULL)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"expected {n} contiguous elements of {dtype}, got {t.dtype} {tuple(t.shape)}")
+    if t.get_device() != device:
+        _elsewhere(t, device)
     return t.data_ptr()
-
-
-def _opt(t: Optional[torch.Tensor], device: int):
-    return None if t is None else _at(t, device)
 
 
 def _kv_call(device: int, fn, where, *args):
     """Runs one library call on the current stream of CUDA device number `device`, made current for it if it is not."""
-    if device == torch.cuda.current_device():
-        status = fn(*args, torch._C._cuda_getCurrentRawStream(device))
+    if device == _current_device():
+        status = fn(*args, _raw_stream(device))
     else:
         with torch.cuda.device(device):
-            status = fn(*args, torch._C._cuda_getCurrentRawStream(device))
+            status = fn(*args, _raw_stream(device))
     if status != MQ_OK:
         raise MqError(status, where)
 
 
-def _pitch(t: torch.Tensor) -> int:
-    """Leading dimension of a row-major matrix (a single row or column may carry any stride in torch)."""
-    rows, cols = t.shape
-    pitch, unit = t.stride()
-    if unit != 1 and cols > 1:
-        raise ValueError("rows must be contiguous")
-    return pitch if rows > 1 else max(pitch, cols)
-
-
 def _kv_batch(cu_q, kv_len, page_table, total_q, max_q, perm, device):
     n_seq, width = page_table.shape
-    if not (cu_q.dtype == kv_len.dtype == page_table.dtype == _I32 and (perm is None or perm.dtype == _I32)):
-        raise ValueError("cu_q, kv_len, page_table and perm are int32")
-    if kv_len.numel() != n_seq or cu_q.numel() != n_seq + 1 or (perm is not None and perm.numel() != total_q):
-        raise ValueError("cu_q [n_seq + 1], kv_len [n_seq], page_table [n_seq, max_pages], perm [rows of q]")
-    if not (cu_q.is_contiguous() and kv_len.is_contiguous() and page_table.is_contiguous() and
-            (perm is None or perm.is_contiguous())):
-        raise ValueError("cu_q, kv_len, page_table and perm must be contiguous")
-    return mq_kv_batch(n_seq, total_q, max_q, width, _at(cu_q, device), _at(kv_len, device), _at(page_table, device),
-                       _opt(perm, device))
+    return mq_kv_batch(n_seq, total_q, max_q, width, _vec(cu_q, _I32, n_seq + 1, device), _vec(kv_len, _I32, n_seq, device),
+                       _vec(page_table, _I32, n_seq * width, device), _vec(perm, _I32, total_q, device))
 
 
 def mq_qk_norm_rope(q, k, pos, n_q_heads, n_kv_heads, q_out, k_out=None, gain_q=None, gain_k=None, eps=1e-6, base=10000.0,
                     half=False, v=None, cache: Optional[KVCache] = None, slots=None):
     """Per-head RMSNorm (where a gain is given), rotary embedding, and the store of K and V into `cache` at `slots`
     (int64 [T], page * page_size + slot; negative: not stored).  See include/mq.h."""
-    T, width = q.shape
-    head_dim = width // n_q_heads
-    kv = (T, n_kv_heads * head_dim)
-    if not (q.dtype == k.dtype == q_out.dtype == _BF16 and pos.dtype == _I32):
-        raise ValueError("q, k and q_out are bf16, pos is int32")
-    if width != n_q_heads * head_dim or k.shape != kv or q_out.shape != q.shape or pos.numel() != T or not pos.is_contiguous():
-        raise ValueError("q, q_out [T, n_q_heads * head_dim], k [T, n_kv_heads * head_dim], pos [T]")
-    if k_out is not None and (k_out.dtype != _BF16 or k_out.shape != kv):
-        raise ValueError("k_out is bf16 of k's shape")
-    for gain in (gain_q, gain_k):
-        if gain is not None and (gain.dtype != _F32 or gain.numel() != head_dim or not gain.is_contiguous()):
-            raise ValueError("gains are float32 [head_dim]")
+    shape = q.shape
+    T, width = shape
+    dim = width // n_q_heads
+    if dim * n_q_heads != width:
+        raise ValueError("q is [T, n_q_heads * head_dim]")
+    kv = (T, n_kv_heads * dim)
     d = q.get_device()
+    pq, ldq = _rows(q, shape, d)
+    pk, ldk = _rows(k, kv, d)
+    po, ldo = _rows(q_out, shape, d)
+    pko, ldko = (None, 0) if k_out is None else _rows(k_out, kv, d)
     if cache is None:
         pv, ldv, pc, ps = None, 0, None, None
     else:
-        if v.dtype != _BF16 or v.shape != kv or slots.dtype != _I64 or slots.numel() != T or not slots.is_contiguous():
-            raise ValueError("v is bf16 of k's shape, slots int64 [T]")
         if cache.index != d:
             raise ValueError(f"the cache is on cuda:{cache.index}, q on {q.device}")
-        pv, ldv, pc, ps = _at(v, d), _pitch(v), cache.ref, _at(slots, d)
-    _kv_call(d, load().mq_qk_norm_rope, "mq_qk_norm_rope", _at(q, d), _pitch(q), _at(k, d), _pitch(k), pv, ldv, T, n_q_heads,
-             n_kv_heads, head_dim, _opt(gain_q, d), _opt(gain_k, d), eps, _at(pos, d), base, MQ_ROPE_HALF if half else 0,
-             _at(q_out, d), _pitch(q_out), _opt(k_out, d), 0 if k_out is None else _pitch(k_out), pc, ps)
+        pv, ldv = _rows(v, kv, d)
+        pc, ps = cache.ref, _vec(slots, _I64, T, d)
+    _kv_call(d, load().mq_qk_norm_rope, "mq_qk_norm_rope", pq, ldq, pk, ldk, pv, ldv, T, n_q_heads, n_kv_heads, dim,
+             _vec(gain_q, _F32, dim, d), _vec(gain_k, _F32, dim, d), eps, _vec(pos, _I32, T, d), base, MQ_ROPE_HALF if half else 0,
+             po, ldo, pko, ldko, pc, ps)
 
 
 def mq_kv_attention_workspace_bytes(n_seq, total_q, max_q, max_pages, n_q_heads, cache: KVCache) -> int:
@@ -623,21 +621,27 @@ def new_kv_attention_workspace(n_seq, total_q, max_q, max_pages, n_q_heads, cach
 
 def mq_kv_attention(q, cu_q, kv_len, page_table, cache: KVCache, n_q_heads, max_q, o, ws, lse=None, perm=None, scale=None):
     """Attention of the new rows q over the paged cache; see include/mq.h.  scale: 1 / sqrt(head_dim) if not given."""
-    total_q, width = q.shape
-    if not (q.dtype == o.dtype == _BF16) or o.shape != q.shape or width != n_q_heads * cache.head_dim:
-        raise ValueError("q and o are bf16 [rows, n_q_heads * head_dim]")
-    if lse is not None and (lse.dtype != _F32 or lse.shape != (total_q, n_q_heads) or not lse.is_contiguous()):
-        raise ValueError("lse is float32 [rows, n_q_heads]")
-    d = cache.index
-    b = _kv_batch(cu_q, kv_len, page_table, total_q, max_q, perm, d)
-    _kv_call(d, load().mq_kv_attention, "mq_kv_attention", _at(q, d), _pitch(q), C.byref(b), cache.ref, n_q_heads,
-             cache.head_dim ** -0.5 if scale is None else scale, _at(o, d), _pitch(o), _opt(lse, d), _at(ws, d), ws.numel())
+    rows = q.shape[0]
+    shape, d = (rows, n_q_heads * cache.head_dim), cache.index
+    pq, ldq = _rows(q, shape, d)
+    po, ldo = _rows(o, shape, d)
+    size = ws.numel()
+    b = _kv_batch(cu_q, kv_len, page_table, rows, max_q, perm, d)
+    _kv_call(d, load().mq_kv_attention, "mq_kv_attention", pq, ldq, C.byref(b), cache.ref, n_q_heads,
+             cache.head_dim ** -0.5 if scale is None else scale, po, ldo, _vec(lse, _F32, rows * n_q_heads, d),
+             _vec(ws, torch.uint8, size, d), size)
 
 
-def _weight_strides(w, n_seq, n_kv_heads):
-    if w.dtype != _F32 or w.dim() != 3 or w.shape[0] != n_seq or w.shape[1] != n_kv_heads or (w.stride(2) != 1 and w.shape[2] > 1):
-        raise ValueError("weights are float32 [n_seq, n_kv_heads, keys] with contiguous rows")
-    return w.stride(0), w.stride(1)
+def _weights(w, n_seq, n_kv_heads, device):
+    """(address, strides) of weights float32 [n_seq, n_kv_heads, keys] with contiguous rows."""
+    if w.dtype != _F32 or w.dim() != 3 or w.shape[0] != n_seq or w.shape[1] != n_kv_heads:
+        raise ValueError("weights are float32 [n_seq, n_kv_heads, keys]")
+    s0, s1, s2 = w.stride()
+    if s2 != 1 and w.shape[2] > 1:
+        raise ValueError("a head's weights must be contiguous")
+    if w.get_device() != device:
+        _elsewhere(w, device)
+    return w.data_ptr(), s0, s1
 
 
 def mq_kv_weights(q, cu_q, kv_len, page_table, cache: KVCache, n_q_heads, max_q, lse, w_out, w_in=None, perm=None, scale=None,
@@ -645,44 +649,34 @@ def mq_kv_weights(q, cu_q, kv_len, page_table, cache: KVCache, n_q_heads, max_q,
     """Adds the softmax weight every key receives from the rows q to w_in (None: zeros) and writes w_out
     (float32 [n_seq, n_kv_heads, >= longest kv_len]; may be w_in).  lse: mq_kv_attention's output for the same rows.
     status: zeroed int32[2] or None."""
-    total_q, width = q.shape
-    if q.dtype != _BF16 or width != n_q_heads * cache.head_dim:
-        raise ValueError("q is bf16 [rows, n_q_heads * head_dim]")
-    if lse.dtype != _F32 or lse.shape != (total_q, n_q_heads) or not lse.is_contiguous():
-        raise ValueError("lse is float32 [rows, n_q_heads]")
-    if status is not None and (status.dtype != _I32 or status.numel() < 2):
-        raise ValueError("status is int32[2]")
+    rows = q.shape[0]
     d = cache.index
-    b = _kv_batch(cu_q, kv_len, page_table, total_q, max_q, perm, d)
-    strides = _weight_strides(w_out, b.n_seq, cache.n_kv_heads)
-    if w_in is not None and (w_in.shape != w_out.shape or _weight_strides(w_in, b.n_seq, cache.n_kv_heads) != strides):
-        raise ValueError("w_in and w_out must have the same shape and strides")
-    _kv_call(d, load().mq_kv_weights, "mq_kv_weights", _at(q, d), _pitch(q), C.byref(b), cache.ref, n_q_heads,
-             cache.head_dim ** -0.5 if scale is None else scale, _at(lse, d), _opt(w_in, d), _at(w_out, d), strides[0], strides[1],
-             _opt(status, d))
+    pq, ldq = _rows(q, (rows, n_q_heads * cache.head_dim), d)
+    b = _kv_batch(cu_q, kv_len, page_table, rows, max_q, perm, d)
+    pw, s0, s1 = _weights(w_out, b.n_seq, cache.n_kv_heads, d)
+    pin = None
+    if w_in is not None:
+        pin, t0, t1 = _weights(w_in, b.n_seq, cache.n_kv_heads, d)
+        if (t0, t1) != (s0, s1) or w_in.shape != w_out.shape:
+            raise ValueError("w_in and w_out must have the same shape and strides")
+    _kv_call(d, load().mq_kv_weights, "mq_kv_weights", pq, ldq, C.byref(b), cache.ref, n_q_heads,
+             cache.head_dim ** -0.5 if scale is None else scale, _vec(lse, _F32, rows * n_q_heads, d), pin, pw, s0, s1,
+             _vec(status, _I32, 2, d))
 
 
 def mq_kv_evict(cache: KVCache, page_table, kv_len, w, budget, n_first, n_last, dst: KVCache, dst_table, kept, new_len, w_out=None):
     """Cuts every sequence to `budget` keys per key/value head by the weights w and copies the kept rows to dst_table's pages
     of `dst` (see include/mq.h).  kept int32 [n_seq, n_kv_heads, budget], new_len int32 [n_seq], w_out float32 like kept."""
     n_seq, width = page_table.shape
-    d = cache.index
-    if not (kv_len.dtype == page_table.dtype == dst_table.dtype == kept.dtype == new_len.dtype == _I32):
-        raise ValueError("page tables, lengths and kept indices are int32")
-    shape = (n_seq, cache.n_kv_heads, budget)
-    if kv_len.numel() != n_seq or new_len.numel() != n_seq or dst_table.shape[0] != n_seq or kept.shape != shape:
-        raise ValueError("kv_len, new_len [n_seq], dst_table [n_seq, pages], kept [n_seq, n_kv_heads, budget]")
-    if w_out is not None and (w_out.dtype != _F32 or w_out.shape != shape or not w_out.is_contiguous()):
-        raise ValueError("w_out is float32 [n_seq, n_kv_heads, budget]")
-    if not (page_table.is_contiguous() and dst_table.is_contiguous() and kv_len.is_contiguous() and kept.is_contiguous() and
-            new_len.is_contiguous()):
-        raise ValueError("page tables, lengths and kept indices must be contiguous")
+    d, n = cache.index, n_seq * cache.n_kv_heads * budget
     if dst.index != d:
         raise ValueError(f"the caches are on cuda:{d} and cuda:{dst.index}")
-    strides = _weight_strides(w, n_seq, cache.n_kv_heads)
-    _kv_call(d, load().mq_kv_evict, "mq_kv_evict", cache.ref, _at(page_table, d), width, _at(kv_len, d), n_seq, _at(w, d),
-             strides[0], strides[1], budget, n_first, n_last, dst.ref, _at(dst_table, d), dst_table.shape[1], _at(kept, d),
-             _at(new_len, d), _opt(w_out, d))
+    if dst_table.shape[0] != n_seq:
+        raise ValueError("dst_table is [n_seq, pages]")
+    pw, s0, s1 = _weights(w, n_seq, cache.n_kv_heads, d)
+    _kv_call(d, load().mq_kv_evict, "mq_kv_evict", cache.ref, _vec(page_table, _I32, n_seq * width, d), width, _vec(kv_len, _I32, n_seq, d),
+             n_seq, pw, s0, s1, budget, n_first, n_last, dst.ref, _vec(dst_table, _I32, dst_table.numel(), d), dst_table.shape[1],
+             _vec(kept, _I32, n, d), _vec(new_len, _I32, n_seq, d), _vec(w_out, _F32, n, d))
 
 
 def mq_last_device_status(ws):
