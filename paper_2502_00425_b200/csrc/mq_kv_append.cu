@@ -8,6 +8,8 @@
 // its heads (they cost as much as two head rows), and the frequencies (doubles) are read once per thread.
 // The angle in turns, pos * theta / (2 pi), is formed and reduced in double: in float32 a position of 100,000 would
 // leave an angle error of 4e-3.
+// 9728 tokens of 32 + 8 heads of 128, 239 MB: 53 us, 4.5 TB/s (68 % of a plain copy); the instructions between the loads
+// and the stores are the bound (sums, conversions and rotation of 8 channels per lane).  32 tokens: 3.4 us.
 #include "mq_kv.cuh"
 
 namespace mq {
@@ -171,8 +173,9 @@ int launch(AppendParams& p, cudaStream_t st) {
   p.n_steps = (rows + per - 1) / per;
   const int sms = sm_count();
   // few tokens: one step per warp, so that the call is one latency long; many: a warp takes a token, or half of one where
-  // that leaves the last warps less to wait for, with four steps in flight
-  const bool wide = (int64_t)p.T * p.n_steps > (int64_t)sms * 64;
+  // that leaves the last warps less to wait for, with four steps in flight.  28 + 4 heads of 128, one step / four steps in
+  // us: 2.9 / 5.9 for 1 token, 4.5 / 6.6 for 128, 6.7 / 6.8 for 256 (18 steps each), 10.1 / 7.4 for 512, 59 / 22 for 4096.
+  const bool wide = (int64_t)p.T * p.n_steps > (int64_t)sms * 32;
   p.chunks = !wide ? p.n_steps : p.n_steps > 8 ? 2 : 1;
   p.per_chunk = (p.n_steps + p.chunks - 1) / p.chunks;
   const int64_t blocks = ((int64_t)p.T * p.chunks + kWarps - 1) / kWarps, most = (int64_t)sms * 4;

@@ -15,14 +15,17 @@
 //   * An int8 cache is read as codes and widened in registers to fp16 exactly (the products' sums do not care in which
 //     order the channels come, so a thread takes contiguous codes); the scales multiply the scores and the result.
 //     Queries are scaled by a power of two per row so that fp16 holds them with all their bits.
+// 64 sequences of 64 to 8192 keys, 8 key/value heads of 128, groups of 4: 78 us in bf16 (449 MB, 5.8 TB/s, 88 % of a plain
+// copy) and 50 us in int8 (225 MB, 4.5 TB/s; widening and the products' instructions hold it, not memory).  One sequence of
+// 3361 keys: 9 us, of which the two launches are half.
 #include "mq_kv_warp.cuh"
 
 namespace mq {
 namespace {
 
 constexpr int kWarps = kStreamWarps, kThreads = kStreamThreads, kTile = kStreamTile;
-constexpr int kExtra = 4;         // what a unit costs besides its tiles, in tiles
-constexpr int kMinLen = 2;        // a worker's least share of the line
+constexpr int kExtra = 4;         // what a unit costs besides its tiles, in tiles (64 ragged int8 sequences: 59 us with 2, 50 with 4, 54 with 8)
+constexpr int kMinLen = 2;        // a worker's least share of the line (one sequence of 3361 keys: 9.0 us with 2, 11.7 with 6)
 // fp16 probabilities reach down to 2^-24 only: with the reference 14 below the maximum they run up to 2^14 instead of 1, and
 // what is lost below is 2^-39 of the largest one (a sum over them stays in float32 either way).
 constexpr float kLiftF16 = 14.0f;
@@ -32,6 +35,8 @@ template <int kD, bool kI8, int kN>
 struct Cfg {
   static constexpr int kRows = 8 * kN;
   static constexpr int kStage = 2 * KeyTile<kD, kI8>::kBytes;   // K and V of 16 keys
+  // three CTAs with two stages of 8 KB (78.4 us in the case above) rather than two with three (79.6 us); 4 KB stages have
+  // room for four
   static constexpr int kCtas = kStage == 8192 && kN == 2 ? 2 : 3;   // per SM
   static constexpr int kStages = kStage == 8192 && kN == 1 ? 2 : kStage == 8192 ? 3 : 4;
   static constexpr int kRing = kStage * kStages;
@@ -496,7 +501,10 @@ int launch_decode(const KvAttnArgs& a, int workers, cudaStream_t st) {
 }
 
 // Which kernel, and how many workers.  Up to kFewRows query rows per key/value head (tokens x heads of the group) take the
-// kernel above in blocks of 8 or 16 rows, more take the 128-row tensor-memory kernel of mq_kv_chunk.cu.
+// kernel above in blocks of 8 or 16 rows, more take the 128-row tensor-memory kernel of mq_kv_chunk.cu.  Both in us, heads
+// of 128, bf16, 4 key/value heads, this kernel / that one: 14 rows over 16 x 8000 keys 56 / 69, 28 rows over 1 x 2000
+// 12 / 19, over 16 x 2000 30 / 31, over 16 x 8000 94 / 68; 56 rows 13 / 19, 47 / 31 and 164 / 68.  The lengths are not known
+// on the host, so the rule is the rows at which the middle is a draw.
 constexpr int kFewRows = 32;
 struct Plan {
   bool chunk;
@@ -537,6 +545,9 @@ cudaError_t launch_join(const KvSchedArgs& a, const KvParts& parts, const KvOutA
 }  // namespace
 
 int launch_kv_combine(const KvSchedArgs& a, const KvParts& parts, const KvOutArgs& out, int workers, int dim, cudaStream_t st) {
+  // Slots of few rows come in long chains (one sequence is spread over all workers): four warps share a row's chain.  With
+  // one warp / four in us, the whole call: one token over 3361 keys 11.6 / 9.0, over 8 x 2000 13.2 / 13.7; a chunk of 40
+  // tokens over 4000 keys (256-row slots) 24 / 39, of 2 x 1024 over 8000 256 / 308.
   const bool few = a.pitch <= 16;
   const cudaError_t e = dim == 128 ? (few ? launch_join<128, 4>(a, parts, out, workers, st) : launch_join<128, 1>(a, parts, out, workers, st))
                                    : (few ? launch_join<64, 4>(a, parts, out, workers, st) : launch_join<64, 1>(a, parts, out, workers, st));
