@@ -540,15 +540,16 @@ int mq_kv_attention(const void* Q, int64_t ldq, const mq_kv_batch* batch, const 
  * The softmax weight that every key received from this call's rows, added to what it had:
  *   W_out[b, g, j] = (W_in[b, g, j] if key j was cached before this chunk, else 0)
  *                    + sum over the chunk's rows i that see j and the query heads h of g of exp(scale * Q[i, h] . K[j, g] - lse[i, h])
- * for j < kv_len[b]; other entries of W_out are left as they were.  lse is mq_kv_attention's output for the same
+ * for j < kv_len[b]; other entries of W_out are left as they were (without rows, total_q = 0, W_in is copied).  lse is mq_kv_attention's output for the same
  * call.  W_in NULL counts as zeros; W_in == W_out accumulates in place.  float32 throughout, and every sum is
- * taken in a fixed order (no atomics).  w_seq_stride, w_head_stride: elements between sequences and heads
- * (w_head_stride at least the longest kv_len; for both arrays).  status: optional device int32[2], zeroed by the caller:
- * MQ_ERR_INVALID_ARG for a page number outside the cache, MQ_ERR_TIMEOUT and the wait's site if a bounded wait expired.
+ * taken in a fixed order (no atomics).  w_seq_stride, w_head_stride: elements between sequences and heads, w_keys:
+ * entries of a head's row (of both arrays); keys at or behind w_keys are neither read nor written.  status: optional
+ * device int32[2], zeroed by the caller: MQ_ERR_INVALID_ARG for a page number outside the cache or a kv_len beyond
+ * w_keys, MQ_ERR_TIMEOUT and the wait's site if a bounded wait expired.
  */
 int mq_kv_weights(const void* Q, int64_t ldq, const mq_kv_batch* batch, const mq_kv_cache* cache, int32_t n_q_heads,
                   float scale, const float* lse, const float* W_in, float* W_out, int64_t w_seq_stride,
-                  int64_t w_head_stride, int32_t* status, void* stream);
+                  int64_t w_head_stride, int32_t w_keys, int32_t* status, void* stream);
 
 /*
  * Eviction: cuts every sequence to at most `budget` keys per key/value head and copies them, in their order, to fresh
@@ -561,12 +562,12 @@ int mq_kv_weights(const void* Q, int64_t ldq, const mq_kv_batch* batch, const mq
  *   dst, dst_table [n_seq][dst_max_pages]: where the kept rows go, row i to slot i of the sequence's new pages; dst
  *            has the type, heads and head_dim of `cache`, and may be the same cache as long as no destination page
  *            is a source page of any sequence.  dst_max_pages * page_size must reach the budget.
- * W: float32 with the strides of mq_kv_weights.  n_first + n_last <= budget (MQ_ERR_INVALID_ARG).  A page number outside
+ * W: float32 with the strides and row length of mq_kv_weights (keys at or behind w_keys count as NaN).  n_first + n_last <= budget (MQ_ERR_INVALID_ARG).  A page number outside
  * the cache reads as zeros, and is not written to.  The page table's max_pages bounds kv_len.
  */
 int mq_kv_evict(const mq_kv_cache* cache, const int32_t* page_table, int32_t max_pages, const int32_t* kv_len,
-                int32_t n_seq, const float* W, int64_t w_seq_stride, int64_t w_head_stride, int32_t budget,
-                int32_t n_first, int32_t n_last, const mq_kv_cache* dst, const int32_t* dst_table,
+                int32_t n_seq, const float* W, int64_t w_seq_stride, int64_t w_head_stride, int32_t w_keys,
+                int32_t budget, int32_t n_first, int32_t n_last, const mq_kv_cache* dst, const int32_t* dst_table,
                 int32_t dst_max_pages, int32_t* kept, int32_t* new_len, float* W_out, void* stream);
 
 /* ---- Measurement and self-test aids (the paper has no counterpart) ------------------------- */

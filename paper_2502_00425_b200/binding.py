@@ -102,8 +102,8 @@ def load(build_if_missing: bool = False):
                                       vp, i64, kvcp, vp, vp]),
         "mq_kv_attention_workspace_bytes": (sz, [kvbp, kvcp, i32]),
         "mq_kv_attention": (C.c_int, [vp, i64, kvbp, kvcp, i32, f32, vp, i64, vp, vp, sz, vp]),
-        "mq_kv_weights": (C.c_int, [vp, i64, kvbp, kvcp, i32, f32, vp, vp, vp, i64, i64, vp, vp]),
-        "mq_kv_evict": (C.c_int, [kvcp, vp, i32, vp, i32, vp, i64, i64, i32, i32, i32, kvcp, vp, i32, vp, vp, vp, vp]),
+        "mq_kv_weights": (C.c_int, [vp, i64, kvbp, kvcp, i32, f32, vp, vp, vp, i64, i64, i32, vp, vp]),
+        "mq_kv_evict": (C.c_int, [kvcp, vp, i32, vp, i32, vp, i64, i64, i32, i32, i32, i32, kvcp, vp, i32, vp, vp, vp, vp]),
         "mq_repack_w4": (C.c_int, [vp, i32, i32, vp, vp]),
         "mq_unpack_w4": (C.c_int, [vp, vp, i32, i32, vp, i64, vp]),
         "mq_aifs_reorder": (C.c_int, [vp, vp, i32, i32, i64, i64, vp, vp, vp, vp, vp, i32, vp]),
@@ -633,7 +633,7 @@ def mq_kv_attention(q, cu_q, kv_len, page_table, cache: KVCache, n_q_heads, max_
 
 
 def _weights(w, n_seq, n_kv_heads, device):
-    """(address, strides) of weights float32 [n_seq, n_kv_heads, keys] with contiguous rows."""
+    """(address, strides, row length) of weights float32 [n_seq, n_kv_heads, keys] with contiguous rows."""
     if w.dtype != _F32 or w.dim() != 3 or w.shape[0] != n_seq or w.shape[1] != n_kv_heads:
         raise ValueError("weights are float32 [n_seq, n_kv_heads, keys]")
     s0, s1, s2 = w.stride()
@@ -641,7 +641,7 @@ def _weights(w, n_seq, n_kv_heads, device):
         raise ValueError("a head's weights must be contiguous")
     if w.get_device() != device:
         _elsewhere(w, device)
-    return w.data_ptr(), s0, s1
+    return w.data_ptr(), s0, s1, w.shape[2]
 
 
 def mq_kv_weights(q, cu_q, kv_len, page_table, cache: KVCache, n_q_heads, max_q, lse, w_out, w_in=None, perm=None, scale=None,
@@ -653,14 +653,14 @@ def mq_kv_weights(q, cu_q, kv_len, page_table, cache: KVCache, n_q_heads, max_q,
     d = cache.index
     pq, ldq = _rows(q, (rows, n_q_heads * cache.head_dim), d)
     b = _kv_batch(cu_q, kv_len, page_table, rows, max_q, perm, d)
-    pw, s0, s1 = _weights(w_out, b.n_seq, cache.n_kv_heads, d)
+    pw, s0, s1, keys = _weights(w_out, b.n_seq, cache.n_kv_heads, d)
     pin = None
     if w_in is not None:
-        pin, t0, t1 = _weights(w_in, b.n_seq, cache.n_kv_heads, d)
+        pin, t0, t1, _ = _weights(w_in, b.n_seq, cache.n_kv_heads, d)
         if (t0, t1) != (s0, s1) or w_in.shape != w_out.shape:
             raise ValueError("w_in and w_out must have the same shape and strides")
     _kv_call(d, load().mq_kv_weights, "mq_kv_weights", pq, ldq, C.byref(b), cache.ref, n_q_heads,
-             cache.head_dim ** -0.5 if scale is None else scale, _vec(lse, _F32, rows * n_q_heads, d), pin, pw, s0, s1,
+             cache.head_dim ** -0.5 if scale is None else scale, _vec(lse, _F32, rows * n_q_heads, d), pin, pw, s0, s1, keys,
              _vec(status, _I32, 2, d))
 
 
@@ -673,9 +673,9 @@ def mq_kv_evict(cache: KVCache, page_table, kv_len, w, budget, n_first, n_last, 
         raise ValueError(f"the caches are on cuda:{d} and cuda:{dst.index}")
     if dst_table.shape[0] != n_seq:
         raise ValueError("dst_table is [n_seq, pages]")
-    pw, s0, s1 = _weights(w, n_seq, cache.n_kv_heads, d)
+    pw, s0, s1, keys = _weights(w, n_seq, cache.n_kv_heads, d)
     _kv_call(d, load().mq_kv_evict, "mq_kv_evict", cache.ref, _vec(page_table, _I32, n_seq * width, d), width, _vec(kv_len, _I32, n_seq, d),
-             n_seq, pw, s0, s1, budget, n_first, n_last, dst.ref, _vec(dst_table, _I32, dst_table.numel(), d), dst_table.shape[1],
+             n_seq, pw, s0, s1, keys, budget, n_first, n_last, dst.ref, _vec(dst_table, _I32, dst_table.numel(), d), dst_table.shape[1],
              _vec(kept, _I32, n, d), _vec(new_len, _I32, n_seq, d), _vec(w_out, _F32, n, d))
 
 

@@ -25,6 +25,7 @@ struct EvictParams {
   int n_seq;
   const float* W;
   int64_t w_seq, w_head;
+  int w_keys;   // entries of a row of W; keys behind it count as NaN
   int budget, n_first, n_last;
   const int32_t* dst_table;
   int dst_max_pages;
@@ -81,13 +82,14 @@ kv_select_kernel(const __grid_constant__ EvictParams p, const int held_most) {
   pdl_wait();
   pdl_launch_dependents();   // (behind the wait: the copy kernel reads lengths and tables before its own)
   const int n = evict_len(p, b), m = min(n, p.budget);
-  const float* w = p.W + (int64_t)b * p.w_seq + (int64_t)g * p.w_head;
+  const float* row = p.W + (int64_t)b * p.w_seq + (int64_t)g * p.w_head;
+  auto w = [&](int j) { return j < p.w_keys ? row[j] : __int_as_float(0x7fffffff); };
   const int64_t out = ((int64_t)b * p.src.n_kv_heads + g) * p.budget;
   if (g == 0 && tid == 0) p.new_len[b] = m;
   if (n <= p.budget) {
     for (int j = tid; j < n; j += kSelThreads) {
       p.kept[out + j] = j;
-      if (p.W_out) p.W_out[out + j] = w[j];
+      if (p.W_out) p.W_out[out + j] = w(j);
     }
     return;
   }
@@ -100,7 +102,7 @@ kv_select_kernel(const __grid_constant__ EvictParams p, const int held_most) {
   for (int j0 = tid; j0 < n; j0 += 4 * kSelThreads) {
     float v[4];
 #pragma unroll
-    for (int c = 0; c < 4; ++c) v[c] = j0 + c * kSelThreads < n ? w[j0 + c * kSelThreads] : 0.0f;
+    for (int c = 0; c < 4; ++c) v[c] = j0 + c * kSelThreads < n ? w(j0 + c * kSelThreads) : 0.0f;
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       const int j = j0 + c * kSelThreads;
@@ -118,7 +120,7 @@ kv_select_kernel(const __grid_constant__ EvictParams p, const int held_most) {
       const uint32_t bins = pass == 0 ? 4096u : 1024u;
       if (pass > 0) {
         for (int j = lo + tid; j < hi; j += kSelThreads) {
-          const uint32_t u = held ? img[j] : image(w[j]);
+          const uint32_t u = held ? img[j] : image(w(j));
           if ((u & known) == prefix) atomicAdd(&hist[(u >> shift) & 1023u], 1u);
         }
         __syncthreads();
@@ -180,7 +182,7 @@ kv_select_kernel(const __grid_constant__ EvictParams p, const int held_most) {
     } else {
 #pragma unroll
       for (int c = 0; c < 4; ++c)
-        if (j0 + c < n) u[c] = image(w[j0 + c]);
+        if (j0 + c < n) u[c] = image(w(j0 + c));
     }
     uint32_t cls = 0u, cnt = 0u;
 #pragma unroll
@@ -199,7 +201,7 @@ kv_select_kernel(const __grid_constant__ EvictParams p, const int held_most) {
       if (k == 1u || (k == 2u && e < need)) {
         const int64_t at = out + a + min(e, need);
         p.kept[at] = j0 + c;
-        if (p.W_out) p.W_out[at] = w[j0 + c];
+        if (p.W_out) p.W_out[at] = w(j0 + c);
       }
       if (k == 1u) ++a;
       if (k == 2u) ++e;
@@ -270,7 +272,7 @@ cudaError_t launch_copy(const EvictParams& p, cudaStream_t st) {
 using namespace mq;
 
 extern "C" int mq_kv_evict(const mq_kv_cache* cache, const int32_t* page_table, int32_t max_pages, const int32_t* kv_len,
-                           int32_t n_seq, const float* W, int64_t w_seq_stride, int64_t w_head_stride, int32_t budget,
+                           int32_t n_seq, const float* W, int64_t w_seq_stride, int64_t w_head_stride, int32_t w_keys, int32_t budget,
                            int32_t n_first, int32_t n_last, const mq_kv_cache* dst, const int32_t* dst_table,
                            int32_t dst_max_pages, int32_t* kept, int32_t* new_len, float* W_out, void* stream) {
   EvictParams p{};
@@ -278,15 +280,15 @@ extern "C" int mq_kv_evict(const mq_kv_cache* cache, const int32_t* page_table, 
   if (rc != MQ_OK) return rc;
   if ((rc = check_kv_cache(dst, &p.dst)) != MQ_OK) return rc;
   if (dst->flags != cache->flags || dst->head_dim != cache->head_dim || dst->n_kv_heads != cache->n_kv_heads) return MQ_ERR_INVALID_ARG;
-  if (n_seq < 0 || max_pages < 0 || dst_max_pages < 0 || budget < 0 || n_first < 0 || n_last < 0 || w_seq_stride < 0 || w_head_stride < 0)
+  if (n_seq < 0 || max_pages < 0 || dst_max_pages < 0 || budget < 0 || n_first < 0 || n_last < 0 || w_seq_stride < 0 || w_head_stride < 0 || w_keys < 0)
     return MQ_ERR_INVALID_ARG;
   if ((int64_t)n_first + n_last > budget || (int64_t)dst_max_pages * dst->page_size < budget) return MQ_ERR_INVALID_ARG;
   if (n_seq > kMaxKvSeqs || cache->n_kv_heads > 65535 || max_pages > (1 << 22) || dst_max_pages > (1 << 22)) return MQ_ERR_UNSUPPORTED;
   if (n_seq == 0) return MQ_OK;
-  if (!kv_len || !new_len || (max_pages > 0 && (!page_table || !W)) || (budget > 0 && (!dst_table || !kept))) return MQ_ERR_INVALID_ARG;
+  if (!kv_len || !new_len || (max_pages > 0 && (!page_table || (w_keys > 0 && !W))) || (budget > 0 && (!dst_table || !kept))) return MQ_ERR_INVALID_ARG;
   p.dim_bytes = cache->head_dim * ((cache->flags & MQ_KV_INT8) ? 1 : 2);
   p.table = page_table; p.max_pages = max_pages; p.kv_len = kv_len; p.n_seq = n_seq;
-  p.W = W; p.w_seq = w_seq_stride; p.w_head = w_head_stride;
+  p.W = W; p.w_seq = w_seq_stride; p.w_head = w_head_stride; p.w_keys = w_keys;
   p.budget = budget; p.n_first = n_first; p.n_last = n_last;
   p.dst_table = dst_table; p.dst_max_pages = dst_max_pages;
   p.kept = kept; p.new_len = new_len; p.W_out = W_out;

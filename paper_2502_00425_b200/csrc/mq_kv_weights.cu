@@ -169,8 +169,8 @@ kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
       const int64_t out = (int64_t)b * p.seq_stride + (int64_t)g * p.head_stride;
       float old_a = 0.0f, old_b = 0.0f;
       if (t4 == 0 && p.W_in) {
-        if (ka < ctx) old_a = p.W_in[out + ka];
-        if (kb < ctx) old_b = p.W_in[out + kb];
+        if (ka < min(ctx, p.w_keys)) old_a = p.W_in[out + ka];
+        if (kb < min(ctx, p.w_keys)) old_b = p.W_in[out + kb];
       }
       if (!(ok = warp_all(mbar_wait(&full[warp][st], (taken / C::kStages) & 1u, &abort_flag, status, 91)))) break;
       ++taken;
@@ -200,8 +200,9 @@ kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
       sum_a += __shfl_xor_sync(0xffffffffu, sum_a, 1); sum_a += __shfl_xor_sync(0xffffffffu, sum_a, 2);
       sum_b += __shfl_xor_sync(0xffffffffu, sum_b, 1); sum_b += __shfl_xor_sync(0xffffffffu, sum_b, 2);
       if (t4 == 0) {
-        if (ka < s.n_all) p.W_out[out + ka] = old_a + sum_a;
-        if (kb < s.n_all) p.W_out[out + kb] = old_b + sum_b;
+        if (ka < min(s.n_all, p.w_keys)) p.W_out[out + ka] = old_a + sum_a;
+        if (kb < min(s.n_all, p.w_keys)) p.W_out[out + kb] = old_b + sum_b;
+        if (max(ka, kb) >= p.w_keys && min(ka, kb) < s.n_all && s.n_all > p.w_keys && p.status) atomicCAS(p.status, MQ_OK, MQ_ERR_INVALID_ARG);
       }
       __syncwarp();   // every lane has read the tile before its slot is asked to be filled again
     }
@@ -219,7 +220,8 @@ int launch(const WeightParams& p, int64_t most, cudaStream_t st) {
   static PerDeviceTable<char> attr_set;
   if (!ensure_dynamic_smem(attr_set, kv_weights_kernel<kD, kI8, kN>, C::kSmem + (kMaxKvSeqs + 1) * (int)sizeof(int64_t))) return MQ_ERR_CUDA;
   CUtensorMap mk;
-  if (!encode_key_tiles(&mk, p.c.K, p.Q, p.c, kD, kI8)) return MQ_ERR_CUDA;
+  // (a cache without pages: any address will do, nothing is read)
+  if (!encode_key_tiles(&mk, p.c.K, reinterpret_cast<const void*>(reinterpret_cast<uintptr_t>(p.W_out) & ~uintptr_t(15)), p.c, kD, kI8)) return MQ_ERR_CUDA;
   const int64_t cap = (int64_t)sm_count() * C::kCtas;
   const cudaError_t e = launch_pdl(kv_weights_kernel<kD, kI8, kN>, dim3((unsigned)(most < cap ? most : cap)), dim3(kThreads), smem, st, mk, p);
   if (e != cudaSuccess) return cuda_status(e);
@@ -233,7 +235,7 @@ using namespace mq;
 
 extern "C" int mq_kv_weights(const void* Q, int64_t ldq, const mq_kv_batch* batch, const mq_kv_cache* cache, int32_t n_q_heads,
                              float scale, const float* lse, const float* W_in, float* W_out, int64_t w_seq_stride,
-                             int64_t w_head_stride, int32_t* status, void* stream) {
+                             int64_t w_head_stride, int32_t w_keys, int32_t* status, void* stream) {
   WeightParams p{};
   int rc = check_kv_cache(cache, &p.c);
   if (rc != MQ_OK) return rc;
@@ -242,10 +244,10 @@ extern "C" int mq_kv_weights(const void* Q, int64_t ldq, const mq_kv_batch* batc
   if (!(scale > 0.0f) || !std::isfinite(scale)) return MQ_ERR_INVALID_ARG;
   const int64_t reach = (int64_t)batch->max_pages * cache->page_size;
   const int group = n_q_heads / cache->n_kv_heads;
-  if (ldq < (int64_t)n_q_heads * cache->head_dim || w_head_stride < 0 || w_seq_stride < 0) return MQ_ERR_INVALID_ARG;
+  if (ldq < (int64_t)n_q_heads * cache->head_dim || w_head_stride < 0 || w_seq_stride < 0 || w_keys < 0) return MQ_ERR_INVALID_ARG;
   if ((int64_t)batch->max_q * group > (1 << 30)) return MQ_ERR_UNSUPPORTED;
-  if (batch->n_seq == 0 || reach == 0 || batch->total_q == 0) return MQ_OK;   // (no rows: no weight is added anywhere)
-  if (!W_out || !Q || !lse) return MQ_ERR_INVALID_ARG;
+  if (batch->n_seq == 0 || reach == 0 || w_keys == 0) return MQ_OK;
+  if (!W_out || (batch->total_q > 0 && (!Q || !lse))) return MQ_ERR_INVALID_ARG;
   if (!kv_aligned16(Q) || ldq % 8) return MQ_ERR_ALIGNMENT;
   p.Q = static_cast<const uint8_t*>(Q);
   p.ldq = ldq * 2;
@@ -258,6 +260,7 @@ extern "C" int mq_kv_weights(const void* Q, int64_t ldq, const mq_kv_batch* batc
   p.W_out = W_out;
   p.seq_stride = w_seq_stride;
   p.head_stride = w_head_stride;
+  p.w_keys = w_keys;
   p.status = status;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool i8 = (cache->flags & MQ_KV_INT8) != 0;

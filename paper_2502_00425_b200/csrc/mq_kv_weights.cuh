@@ -17,6 +17,7 @@ struct WeightParams {
   const float* W_in;
   float* W_out;
   int64_t seq_stride, head_stride;
+  int w_keys;        // entries of a row of W: a sequence with more keys is reported, and keys behind it are left out
   int32_t* status;   // device int32[2] or nullptr
 };
 

@@ -434,7 +434,10 @@ kv_weights_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid
         ok = false;
         break;
       }
-      if (grp == 0 && key < n_all) p.W_out[out] = (p.W_in && key < ctx ? p.W_in[out] : 0.0f) + (sum + xch[(np & 1) * kKeys + r]);
+      if (grp == 0 && key < n_all) {
+        if (key < p.w_keys) p.W_out[out] = (p.W_in && key < ctx ? p.W_in[out] : 0.0f) + (sum + xch[(np & 1) * kKeys + r]);
+        else if (p.status) atomicCAS(p.status, MQ_OK, MQ_ERR_INVALID_ARG);
+      }
       __syncwarp();
       if (lane == 0) mbar_arrive(&sh->piece_empty[np % kRing]);
     }

@@ -31,7 +31,8 @@ class CacheStep:
 
 class PagedKVCache:
     """n_seq sequences of up to max_len keys in n_pages pages of page_size tokens.  dtype bf16, or int8 with the static scales
-    k_scale, v_scale (float32 [n_kv_heads])."""
+    k_scale, v_scale (float32 [n_kv_heads]).  Its calls (and replays of graphs that captured them) follow one another in
+    stream order: they share the workspaces, as they share the keys."""
 
     def __init__(self, n_seq: int, n_pages: int, max_len: int, n_kv_heads: int, head_dim: int, page_size: int = 64,
                  k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None, device="cuda"):
@@ -85,11 +86,18 @@ class PagedKVCache:
                          dev(pos, torch.int32), cu[-1], max(new))
 
     def workspace(self, step: CacheStep, n_q_heads: int) -> torch.Tensor:
-        key = (step.total, step.max_q, n_q_heads)
-        if key not in self._ws:
-            self._ws[key] = B.new_kv_attention_workspace(self.n_seq, step.total, step.max_q, self.table.shape[1], n_q_heads,
-                                                         self.handle)
-        return self._ws[key]
+        """A workspace for the step, from a few sizes (powers of two) that are kept as long as the cache: a captured graph may
+        hold any of them."""
+        need = B.mq_kv_attention_workspace_bytes(self.n_seq, step.total, step.max_q, self.table.shape[1], n_q_heads, self.handle)
+        size = max(1 << 16, 1 << (need - 1).bit_length())
+        if size not in self._ws:
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("run a step of this size once before capturing it: its workspace has to be made first")
+            ws = torch.empty(size, dtype=torch.uint8, device=self.device)
+            with torch.cuda.device(ws.device):
+                B.mq_reset_device_status(ws)
+            self._ws[size] = ws
+        return self._ws[size]
 
     def attend(self, q: torch.Tensor, step: CacheStep, n_q_heads: int, perm: Optional[torch.Tensor] = None,
                scale: Optional[float] = None) -> torch.Tensor:

@@ -243,3 +243,60 @@ def test_odd_weight_pitch():
     pg = Paged([77, 130], 3, 64, 16, False, "head", 81)
     w = torch.rand((2, 3, 131), generator=torch.Generator().manual_seed(1))
     _evict(pg, w, 50, 1, 3, 16)
+
+
+@pytest.mark.parametrize("new,lens,hq", [([1, 1], [90, 30], 4), ([40, 3], [300, 30], 8)])
+def test_weight_rows_shorter_than_a_sequence(new, lens, hq):
+    """Keys behind the row of the weights are neither read nor written, and reported; the others keep their values."""
+    pg, q, qf, perm, lse, mags, scale, group = _weights_case(new, lens, hq, 2, 128, 16, False, False, 90)
+    full = torch.zeros((2, 2, max(lens)), device=DEV)
+    args = (q.to(DEV), cu(new), pg.kv_len, pg.table, pg.cache, hq, max(new), torch.from_numpy(lse).to(DEV))
+    B.mq_kv_weights(*args, full)
+    keys = 37
+    for w_in in (False, True):
+        pool = torch.full((2, 2, 64), 7.0, device=DEV)
+        w = pool[:, :, 10:10 + keys]
+        status = torch.zeros(2, dtype=torch.int32, device=DEV)
+        B.mq_kv_weights(*args, w, w_in=w if w_in else None, status=status)
+        assert status[0].item() == B.MQ_ERR_INVALID_ARG
+        assert bool((pool[:, :, :10] == 7).all()) and bool((pool[:, :, 10 + keys:] == 7).all())
+        for b, n in enumerate(lens):
+            m, ctx = min(n, keys), min(n - new[b], keys)
+            want = full[b, :, :m].clone()
+            if w_in:
+                want[:, :ctx] += 7.0
+            assert torch.equal(w[b, :, :m], want) and bool((w[b, :, m:] == 7).all())
+    status = torch.zeros(2, dtype=torch.int32, device=DEV)
+    B.mq_kv_weights(*args, full, status=status)            # rows of just the longest length are long enough
+    assert status.tolist() == [0, 0]
+
+
+def test_weights_without_rows_copies():
+    pg = Paged([20, 70], 2, 128, 16)
+    w_in = torch.rand((2, 2, 70), device=DEV)
+    none = torch.zeros(3, dtype=torch.int32, device=DEV)
+    q, lse = torch.empty((0, 512), dtype=torch.bfloat16, device=DEV), torch.empty((0, 4), device=DEV)
+    for inp in (w_in, None):
+        w = torch.full((2, 2, 70), 9.0, device=DEV)
+        B.mq_kv_weights(q, none, pg.kv_len, pg.table, pg.cache, 4, 0, lse, w, w_in=inp)
+        for b, n in enumerate(pg.lens):
+            assert torch.equal(w[b, :, :n], w_in[b, :, :n] if inp is not None else torch.zeros((2, n), device=DEV))
+            assert bool((w[b, :, n:] == 9).all())
+
+
+@pytest.mark.parametrize("lens,budget", [([100], 60), ([30000], 500), ([50], 60)])
+def test_evict_with_weight_rows_shorter_than_a_sequence(lens, budget):
+    """Keys behind the row of the weights count as NaN: they stay only where no others are left, or as the last ones."""
+    pg = Paged(lens, 1, 64, 64, False, "head", 91)
+    n, keys = lens[0], 45
+    w = torch.rand((1, 1, 64), generator=torch.Generator().manual_seed(2)).to(DEV)[:, :, :keys]
+    K, V = (torch.zeros((8, 1, 64, 64), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    table = torch.arange(8, dtype=torch.int32, device=DEV)[None]
+    kept = torch.zeros((1, 1, budget), dtype=torch.int32, device=DEV)
+    new_len = torch.zeros(1, dtype=torch.int32, device=DEV)
+    w_out = torch.full((1, 1, budget), 3.0, device=DEV)
+    B.mq_kv_evict(pg.cache, pg.table, pg.kv_len, w, budget, 0, 2, B.KVCache(K, V), table, kept, new_len, w_out=w_out)
+    m = min(n, budget)
+    want = list(range(n)) if n <= budget else list(range(budget - 2)) + [n - 2, n - 1]
+    assert new_len.item() == m and kept[0, 0, :m].tolist() == want
+    assert torch.equal(w_out[0, 0, :keys], w[0, 0]) and bool(torch.isnan(w_out[0, 0, keys:m]).all())

@@ -165,3 +165,25 @@ def test_cache_refusals():
     assert cache.lengths == [0, 0] and len(cache.free) == 3
     with pytest.raises(RuntimeError):
         cache.evict(8, 0, 0)                 # no weights are tracked
+
+
+def test_workspaces_of_a_cache_stay_few_and_are_made_before_a_capture():
+    cache = KC.PagedKVCache(2, 64, 2000, 2, 128, 64, device=DEV)
+    q = lambda n: _emb(n, 3)[:, :512].repeat(1, 2).contiguous()
+    for n in list(range(1, 60, 3)) + [200, 300, 500]:
+        step = cache.extend([n, 1])
+        cache.attend(q(n + 1), step, 8)
+    assert len(cache._ws) <= 6 and cache.status_ok()
+    new = KC.PagedKVCache(1, 4, 200, 2, 128, 64, device=DEV)
+    step, rows = new.extend([1]), q(1)
+    g = torch.cuda.CUDAGraph()
+    with pytest.raises(RuntimeError, match="once before"):
+        with torch.cuda.graph(g):
+            new.attend(rows, step, 8)
+    new.attend(rows, step, 8)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        o = new.attend(rows, step, 8)
+    g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(o, new.attend(rows, step, 8)) and new.status_ok()

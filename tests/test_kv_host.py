@@ -55,9 +55,9 @@ def test_every_entry_point_refuses_a_bad_cache(lib, kw, status):
     b = _batch()
     att = lib.mq_kv_attention(A, 1024, C.byref(b), C.byref(c), 8, 0.1, A, 1024, None, A, 1 << 30, None)
     assert att == want and lib.mq_kv_attention_workspace_bytes(C.byref(b), C.byref(c), 8) == 0
-    assert lib.mq_kv_weights(A, 1024, C.byref(b), C.byref(c), 8, 0.1, A, None, A, 4096, 512, None, None) == want
+    assert lib.mq_kv_weights(A, 1024, C.byref(b), C.byref(c), 8, 0.1, A, None, A, 4096, 512, 448, None, None) == want
     for src, dst in ((c, good), (good, c)):
-        assert lib.mq_kv_evict(C.byref(src), A, 7, A, 2, A, 4096, 512, 64, 0, 0, C.byref(dst), A, 7, A, A, None, None) == want
+        assert lib.mq_kv_evict(C.byref(src), A, 7, A, 2, A, 4096, 512, 448, 64, 0, 0, C.byref(dst), A, 7, A, A, None, None) == want
     if kw.get("dim", 128) == 128 and kw.get("hkv", 4) == 4:
         assert lib.mq_qk_norm_rope(A, 1024, A, 512, A, 512, 5, 8, 4, 128, None, None, 1e-6, A, 1e4, 0, A, 1024, None, 0,
                                    C.byref(c), A, None) == want
@@ -87,23 +87,23 @@ def test_attention_refusals(lib):
 
 
 def test_weights_refusals(lib):
-    def call(q=A, ldq=1024, hq=8, scale=0.1, lse=A, w=A, ss=4096, hs=512, **kw):
-        return lib.mq_kv_weights(q, ldq, C.byref(_batch(**kw)), C.byref(_cache()), hq, scale, lse, None, w, ss, hs, None, None)
+    def call(q=A, ldq=1024, hq=8, scale=0.1, lse=A, w=A, ss=4096, hs=512, wk=448, **kw):
+        return lib.mq_kv_weights(q, ldq, C.byref(_batch(**kw)), C.byref(_cache()), hq, scale, lse, None, w, ss, hs, wk, None, None)
 
-    assert call(hq=6) == call(ldq=512) == call(scale=0.0) == call(ss=-1) == call(hs=-1) == B.MQ_ERR_INVALID_ARG
+    assert call(hq=6) == call(ldq=512) == call(scale=0.0) == call(ss=-1) == call(hs=-1) == call(wk=-1) == B.MQ_ERR_INVALID_ARG
     assert call(q=None) == call(lse=None) == call(w=None) == B.MQ_ERR_INVALID_ARG
     assert call(q=A + 2) == call(ldq=1028) == B.MQ_ERR_ALIGNMENT
-    assert call(n_seq=0, total=0, max_q=0) == call(max_pages=0) == B.MQ_OK
+    assert call(n_seq=0, total=0, max_q=0) == call(max_pages=0) == call(wk=0) == B.MQ_OK
 
 
 def test_evict_refusals(lib):
-    def call(src=None, dst=None, table=A, mp=7, kv=A, n=2, w=A, ss=4096, hs=512, budget=64, first=0, last=0, dt=A, dmp=7, kept=A, nl=A):
-        return lib.mq_kv_evict(C.byref(src or _cache()), table, mp, kv, n, w, ss, hs, budget, first, last, C.byref(dst or _cache()), dt,
+    def call(src=None, dst=None, table=A, mp=7, kv=A, n=2, w=A, ss=4096, hs=512, wk=448, budget=64, first=0, last=0, dt=A, dmp=7, kept=A, nl=A):
+        return lib.mq_kv_evict(C.byref(src or _cache()), table, mp, kv, n, w, ss, hs, wk, budget, first, last, C.byref(dst or _cache()), dt,
                                dmp, kept, nl, None, None)
 
     assert call(dst=_cache(hkv=2)) == call(dst=_cache(dim=64)) == B.MQ_ERR_INVALID_ARG
     assert call(dst=_cache(flags=1, ks=A, vs=A)) == B.MQ_ERR_INVALID_ARG           # another type
-    assert call(budget=-1) == call(first=-1) == call(last=-1) == call(n=-1) == call(mp=-1) == B.MQ_ERR_INVALID_ARG
+    assert call(budget=-1) == call(first=-1) == call(last=-1) == call(n=-1) == call(mp=-1) == call(wk=-1) == B.MQ_ERR_INVALID_ARG
     assert call(first=33, last=32) == B.MQ_ERR_INVALID_ARG                          # more than the budget
     assert call(budget=449) == B.MQ_ERR_INVALID_ARG                                 # 7 pages of 64 hold 448
     assert call(n=5000) == B.MQ_ERR_UNSUPPORTED
