@@ -430,15 +430,14 @@ kv_combine_kernel(const int pitch, const FastDiv group, const KvParts parts, con
       float top = m;
 #pragma unroll
       for (int c = 0; c < kBatch; ++c) top = fmaxf(top, ml[c].x);
-      if (top == -INFINITY) continue;
-      const float back = kv_exp2(m - top);   // (0 while nothing has been seen)
+      // (a reference of -inf: nothing but zeros, or scores that are all NaN, whose sum says so and is kept)
+      const float back = m == -INFINITY ? 0.0f : kv_exp2(m - top);
       l *= back;
 #pragma unroll
       for (int e = 0; e < kPer; ++e) x[e] *= back;
 #pragma unroll
       for (int c = 0; c < kBatch; ++c) {
-        if (ml[c].x == -INFINITY) continue;
-        const float f = kv_exp2(ml[c].x - top);
+        const float f = ml[c].x == -INFINITY ? 0.0f : kv_exp2(ml[c].x - top);
         l = fmaf(f, ml[c].y, l);
 #pragma unroll
         for (int e = 0; e < kPer; ++e) x[e] = fmaf(f, v[c][e], x[e]);
@@ -464,8 +463,7 @@ kv_combine_kernel(const int pitch, const FastDiv group, const KvParts parts, con
 #pragma unroll
     for (int k = 0; k < kWarpsPerRow; ++k) {
       const float mk = part[rr][k][kD];
-      if (mk == -INFINITY) continue;
-      const float f = kv_exp2(mk - m);
+      const float f = mk == -INFINITY ? 0.0f : kv_exp2(mk - m);
       l = fmaf(f, part[rr][k][kD + 1], l);
 #pragma unroll
       for (int e = 0; e < kPer; ++e) x[e] = fmaf(f, part[rr][k][lane * kPer + e], x[e]);

@@ -325,3 +325,22 @@ def test_empty_calls_are_no_ops():
     empty = torch.empty(0, dtype=torch.int32, device=DEV)
     B.mq_kv_attention(q, torch.zeros(1, dtype=torch.int32, device=DEV), empty, empty.view(0, 1), pg.cache, 4, 0, q, ws)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("new,lens,hq,hkv", [([1, 1], [40, 3361], 8, 2), ([3], [900], 8, 2), ([40, 300], [300, 5000], 8, 2), ([9], [12000], 28, 4)])
+def test_a_query_that_is_nan_gives_nan_and_reaches_no_other(int8, new, lens, hq, hkv):
+    """Also where its keys are spread over several workers."""
+    pg, q = _inputs(new, lens, hq, hkv, 128, 64, int8, "head", 61)
+    clean, clean_lse = _run(pg, q, new, hq)
+    bad = [(0, 1), (sum(new) - 1, hq - 1), (sum(new) // 2, 0)]
+    for i, h in bad:
+        q[i, h * 128:(h + 1) * 128] = float("nan")
+    q[0, 0] = float("nan")                                  # a single channel is enough
+    o, lse = _run(pg, q, new, hq)
+    hit = np.zeros((sum(new), hq), bool)
+    for i, h in bad + [(0, 0)]:
+        hit[i, h] = True
+    o, clean = o.reshape(-1, hq, 128), clean.reshape(-1, hq, 128)
+    assert np.isnan(o[hit]).all() and np.isnan(lse[hit]).all()
+    assert np.array_equal(o[~hit], clean[~hit]) and np.array_equal(lse[~hit], clean_lse[~hit])
