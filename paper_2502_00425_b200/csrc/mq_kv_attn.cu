@@ -537,7 +537,10 @@ int check_attention(const mq_kv_batch* batch, const mq_kv_cache* cache, int32_t 
 namespace {
 template <int kD, int kW>
 cudaError_t launch_join(const KvSchedArgs& a, const KvParts& parts, const KvOutArgs& out, int workers, cudaStream_t st) {
-  return launch_pdl(kv_combine_kernel<kD, kW>, dim3((unsigned)workers, (unsigned)(a.pitch * kW * 32 / kJoinThreads)), dim3(kJoinThreads), 0, st,
+  // (a slot has as many rows as a sequence can have, at most)
+  const int64_t rows = (int64_t)a.max_q * a.group.d < a.rows ? (int64_t)a.max_q * a.group.d : a.rows;
+  constexpr int per = kJoinThreads / (kW * 32);
+  return launch_pdl(kv_combine_kernel<kD, kW>, dim3((unsigned)workers, (unsigned)((rows + per - 1) / per)), dim3(kJoinThreads), 0, st,
                     a.pitch, a.group, parts, out);
 }
 }  // namespace

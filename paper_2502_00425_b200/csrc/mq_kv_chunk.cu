@@ -39,6 +39,7 @@ constexpr float kLag = 8.0f;            // log2 of how far a row's maximum may o
 // fp16 probabilities (int8 cache): the reference lies 6 below the maximum, so they run to 2^6, and to 2^14 with the lag
 constexpr float kLiftChunk = 6.0f;
 constexpr int kRing = 8;                // published pieces
+constexpr int kSeqsHeld = 512;          // up to so many sequences have their lengths in shared memory
 
 // v[k] of lane q of four neighbours <-> v[q] of lane k
 __device__ __forceinline__ void quad_transpose(uint4 (&v)[4], int lane) {
@@ -109,6 +110,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
   int32_t* kp_all = reinterpret_cast<int32_t*>(ring + kRing);   // [8 warps][128]
   int64_t* red = reinterpret_cast<int64_t*>(kp_all + 8 * kTile);
   int64_t* prefix = red + 16;
+  KvSeq* seqs = p.sched.b.n_seq <= kSeqsHeld ? reinterpret_cast<KvSeq*>(prefix + p.sched.b.n_seq + 1) : nullptr;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
@@ -137,7 +139,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
   pdl_wait();
   const KvSchedArgs& sc = p.sched;
   tc_fence_before();
-  sched_prefix<C::kThreads>(sc, prefix, red);   // (ends with __syncthreads)
+  sched_prefix<C::kThreads>(sc, prefix, red, seqs);   // (ends with __syncthreads)
   tc_fence_after();
   const uint32_t tmem_base = *reinterpret_cast<volatile uint32_t*>(&sh->tmem_base);
   const int block_rows = sc.rows >> 1;          // rows of a block: whole tokens
@@ -308,7 +310,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
     while (ok) {
       Piece pc{};
       while (at < stop) {
-        const KvUnit u = sched_unit(sc, prefix, at);
+        const KvUnit u = sched_unit(sc, prefix, at, seqs);
         const int len = (int)min((int64_t)(u.tiles + sc.extra - u.skip), stop - at);
         pc.t0 = max(0, u.skip - sc.extra);
         pc.t1 = max(0, u.skip + len - sc.extra);
@@ -360,6 +362,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
     if (lane == 0) p.parts.rec[blockIdx.x] = rec;
   } else if (!kI8 && warp == 3) {
     // ---------------- looks through value tiles that not all rows see in full
+    const int shift = p.cache.page_shift, rows = shift >= 7 ? kTile : 1 << shift;   // (of a box)
     int t = 0;
     bool ok = true;
     for (int np = 0; ok; ++np) {
@@ -373,40 +376,52 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
         if (tile * kTile + kTile > all_see) {
           uint8_t* vt = v_smem + s * kTileBytes;
           const int n_ok = end - tile * kTile;             // rows of the tile that hold keys
+          bool wrote = false;
+          // rows behind the last key: those of its own page hold anything (pages that were not asked for arrived as zeros)
+          const int stale = min(kTile, (n_ok + rows - 1) & ~(rows - 1));
+          if (n_ok < stale) {
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h)
+              for (int c = n_ok * 8 + lane; c < stale * 8; c += 32) *reinterpret_cast<uint4*>(vt + h * kHalfBytes + c * 16) = make_uint4(0u, 0u, 0u, 0u);
+            wrote = true;
+          }
           bool hit = false;
           if (all_see < end) {
-            // the largest magnitude of the 16-bit halves shows an infinity or NaN
+            __syncwarp();
+            // the largest magnitude of the 16-bit halves shows an infinity or NaN (among the rows that not all see)
             uint32_t part[4] = {0u, 0u, 0u, 0u};
+            const int first = max(0, all_see - tile * kTile) * 8;
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h) {
+              const uint4* vh = reinterpret_cast<const uint4*>(vt + h * kHalfBytes);
 #pragma unroll 8
-            for (int c = 0; c < kTileBytes / 512; ++c) {
-              const uint4 v = *reinterpret_cast<const uint4*>(vt + (c * 32 + lane) * 16);
-              uint32_t m4 = __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
-              if ((((c * 32 + lane) & 1023) >> 3) >= n_ok) m4 = 0u;
-              part[c & 3] = __vmaxu2(part[c & 3], m4);
+              for (int c = (first & ~31) + lane; c < kTile * 8; c += 32) {
+                const uint4 v = vh[c];
+                part[0] = __vmaxu2(part[0], v.x & 0x7fff7fffu);
+                part[1] = __vmaxu2(part[1], v.y & 0x7fff7fffu);
+                part[2] = __vmaxu2(part[2], v.z & 0x7fff7fffu);
+                part[3] = __vmaxu2(part[3], v.w & 0x7fff7fffu);
+              }
             }
             const uint32_t top = __vmaxu2(__vmaxu2(part[0], part[1]), __vmaxu2(part[2], part[3]));
             hit = __any_sync(0xffffffffu, (top & 0xffffu) >= 0x7f80u || (top >> 16) >= 0x7f80u);
           }
-          if (hit || n_ok < kTile) {
+          if (hit) {
 #pragma unroll 1
             for (int c = 0; c < kTileBytes / 512; ++c) {
               uint4* at16 = reinterpret_cast<uint4*>(vt + (c * 32 + lane) * 16);
-              uint4 v = make_uint4(0u, 0u, 0u, 0u);
-              if ((((c * 32 + lane) & 1023) >> 3) < n_ok) {
-                if (!hit) continue;
-                v = *at16;
-                uint32_t w[4] = {v.x, v.y, v.z, v.w};
+              const uint4 v = *at16;
+              uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  if ((w[e] & 0x7f80u) == 0x7f80u) w[e] &= 0xffff0000u;
-                  if ((w[e] & 0x7f800000u) == 0x7f800000u) w[e] &= 0xffffu;
-                }
-                v = make_uint4(w[0], w[1], w[2], w[3]);
+              for (int e = 0; e < 4; ++e) {
+                if ((w[e] & 0x7f80u) == 0x7f80u) w[e] &= 0xffff0000u;
+                if ((w[e] & 0x7f800000u) == 0x7f800000u) w[e] &= 0xffffu;
               }
-              *at16 = v;
+              *at16 = make_uint4(w[0], w[1], w[2], w[3]);
             }
-            fence_proxy_async_smem();
+            wrote = true;
           }
+          if (wrote) fence_proxy_async_smem();
           if (hit && !poison) {
             poison = true;
             if (lane == 0) *reinterpret_cast<volatile int*>(&ring[np % kRing].poison) = 1;
@@ -698,14 +713,14 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
 template <int kD, bool kI8>
 int launch(const KvAttnArgs& a, int workers, cudaStream_t st) {
   using C = ChunkCfg<kD, kI8>;
-  static_assert(C::kSmem + (kMaxKvSeqs + 1) * 8 <= 232448, "shared memory of one CTA");
+  static_assert(C::kSmem + (kMaxKvSeqs + 1) * 8 <= 232448 && C::kSmem + (kSeqsHeld + 1) * (8 + (int)sizeof(KvSeq)) <= 232448, "shared memory of one CTA");
   static PerDeviceTable<char> attr_set;
   if (!ensure_dynamic_smem(attr_set, kv_chunk_kernel<kD, kI8>, C::kSmem + (kMaxKvSeqs + 1) * (int)sizeof(int64_t))) return MQ_ERR_CUDA;
   CUtensorMap mq_{}, mk{}, mv{};
   if (!encode_queries(&mq_, a.Q, a.ldq, a.out.n_q_heads, a.sched.b.total_q, a.sched.group.d, a.sched.rows / 2, kD)) return MQ_ERR_CUDA;
   if (!kI8 && (!encode_pages(&mk, a.cache.K, a.Q, a.cache, kD, kTile) || !encode_pages(&mv, a.cache.V, a.Q, a.cache, kD, kTile))) return MQ_ERR_CUDA;
   const cudaError_t e = launch_pdl(kv_chunk_kernel<kD, kI8>, dim3((unsigned)workers), dim3(C::kThreads),
-                                   C::kSmem + ((size_t)a.sched.b.n_seq + 1) * sizeof(int64_t), st, mq_, mk, mv, a);
+                                   C::kSmem + ((size_t)a.sched.b.n_seq + 1) * (sizeof(int64_t) + (a.sched.b.n_seq <= kSeqsHeld ? sizeof(KvSeq) : 0)), st, mq_, mk, mv, a);
   if (e != cudaSuccess) return cuda_status(e);
   return cuda_status(cudaGetLastError());
 }
