@@ -386,11 +386,14 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
 // a unit has few rows and may have tens of pieces (a decode step of one sequence is as long as this chain of loads),
 // one where it has 128 rows and mostly two pieces.  The record holds all that is needed: one dependent load before
 // the pieces.
-constexpr int kJoinThreads = 256;
+// Blocks of 512 threads where a row has one warp: most blocks find nothing to join, and starting them is what they cost (144
+// whole units of 5 tiles: 25.2 us with 256 threads, 22.9 with 512, 24.0 with 1024).  Four warps to a row: 256 (one sequence of 3361 keys 9.3 us, 9.5 with 512).
+template <int kWarpsPerRow>
+constexpr int kJoinThreads = kWarpsPerRow > 1 ? 256 : 512;
 template <int kD, int kWarpsPerRow>
-__global__ void __launch_bounds__(kJoinThreads)
+__global__ void __launch_bounds__(kJoinThreads<kWarpsPerRow>)
 kv_combine_kernel(const int pitch, const FastDiv group, const KvParts parts, const KvOutArgs out) {
-  constexpr int kPer = kD / 32, kRows = kJoinThreads / 32 / kWarpsPerRow;
+  constexpr int kPer = kD / 32, kRows = kJoinThreads<kWarpsPerRow> / 32 / kWarpsPerRow;
   __shared__ float part[kRows][kWarpsPerRow][kD + 2];
   pdl_launch_dependents();
   pdl_wait();
@@ -539,8 +542,8 @@ template <int kD, int kW>
 cudaError_t launch_join(const KvSchedArgs& a, const KvParts& parts, const KvOutArgs& out, int workers, cudaStream_t st) {
   // (a slot has as many rows as a sequence can have, at most)
   const int64_t rows = (int64_t)a.max_q * a.group.d < a.rows ? (int64_t)a.max_q * a.group.d : a.rows;
-  constexpr int per = kJoinThreads / (kW * 32);
-  return launch_pdl(kv_combine_kernel<kD, kW>, dim3((unsigned)workers, (unsigned)((rows + per - 1) / per)), dim3(kJoinThreads), 0, st,
+  constexpr int per = kJoinThreads<kW> / (kW * 32);
+  return launch_pdl(kv_combine_kernel<kD, kW>, dim3((unsigned)workers, (unsigned)((rows + per - 1) / per)), dim3(kJoinThreads<kW>), 0, st,
                     a.pitch, a.group, parts, out);
 }
 }  // namespace
