@@ -335,3 +335,19 @@ def test_far_pages_give_the_same_as_near_ones(int8):
             assert B.mq_last_device_status(ws) == (B.MQ_OK, 0)
             got.append((o, lse, w, kept, K, V))
         assert all(torch.equal(a, b) for a, b in zip(*got)) and bool(torch.isfinite(got[0][0]).all())
+
+
+@pytest.mark.parametrize("new,lens,hq,int8", [([1, 1], [90, 30], 4, False), ([10, 9], [300, 130], 8, False), ([10, 9], [300, 130], 8, True), ([40, 3], [200, 60], 14, False)])
+def test_rows_that_are_nan_stay_with_their_sequence(new, lens, hq, int8):
+    """The rows of the sequence behind lie in the same tile of queries."""
+    pg, q, qf, perm, lse, mags, scale, group = _weights_case(new, lens, hq, 2, 128, 16, int8, False, 96)
+    got = []
+    for bad in (False, True):
+        rows, l = q.clone(), torch.from_numpy(lse.copy())
+        if bad:
+            rows[new[0]:] = float("nan")
+            l[new[0]:] = float("nan")
+        w = torch.zeros((2, 2, max(lens)), device=DEV)
+        B.mq_kv_weights(rows.to(DEV), cu(new), pg.kv_len, pg.table, pg.cache, hq, max(new), l.to(DEV), w)
+        got.append(w)
+    assert torch.equal(got[0][0], got[1][0]) and bool(torch.isnan(got[1][1, :, 0]).all())
