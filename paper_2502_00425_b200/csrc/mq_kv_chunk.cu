@@ -136,6 +136,13 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
     sh->abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  // rows of a query block that no box fills (a group that does not divide 128): zeros, not what the last kernel left there
+  const int unfilled = kBlock - (p.sched.rows >> 1);
+  for (int i = threadIdx.x; i < 2 * kHalves * unfilled * 8; i += C::kThreads) {
+    const int blk = i / (unfilled * 8), r = kBlock - unfilled + (i % (unfilled * 8)) / 8;
+    *reinterpret_cast<uint4*>(q_smem + blk * kHalfBytes + r * 128 + (i & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+  }
+  fence_proxy_async_smem();
   if (warp == 2) {
     tmem_alloc(&sh->tmem_base, 512);
     tmem_relinquish();
@@ -515,7 +522,8 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
 #pragma unroll
           for (int e = 0; e < 64; ++e) mx[e & 3] = fmaxf(mx[e & 3], __uint_as_float(sv[e]));
           const float m_new = fmaxf(m_used, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) - lift_raw);
-          if (__any_sync(0xffffffffu, m_new > m_used + lag_raw)) {
+          // (only rows with a result have a say: what stands in the others is the next sequence's tokens, or nothing)
+          if (__any_sync(0xffffffffu, live && m_new > m_used + lag_raw)) {
             if (begun) {
               // every earlier product must have landed: for the first step the scores behind it say so (their MMAs were issued
               // after those products), for the second the first step's own product has to be waited for

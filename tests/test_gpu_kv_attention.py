@@ -344,3 +344,36 @@ def test_a_query_that_is_nan_gives_nan_and_reaches_no_other(int8, new, lens, hq,
     o, clean = o.reshape(-1, hq, 128), clean.reshape(-1, hq, 128)
     assert np.isnan(o[hit]).all() and np.isnan(lse[hit]).all()
     assert np.array_equal(o[~hit], clean[~hit]) and np.array_equal(lse[~hit], clean_lse[~hit])
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("new,lens,hq,hkv", [([13, 30], [3000, 900], 28, 4), ([36, 20], [2600, 2500], 14, 2), ([50, 17], [3500, 64], 4, 4)])
+def test_results_do_not_depend_on_the_sequence_behind(int8, new, lens, hq, hkv):
+    """The last block of a sequence's rows is filled up with the next sequence's tokens: however large those are, the first
+    sequence keeps its bits."""
+    pg, q = _inputs(new, lens, hq, hkv, 128, 64, int8, "head", 71)
+    first = []
+    for factor in (1.0, 0.0, 3.0, 100.0):
+        rows = q.clone()
+        rows[new[0]:] = (rows[new[0]:].float() * factor).to(torch.bfloat16)
+        o, lse = _run(pg, rows, new, hq)
+        _check(pg, rows, new, hq, o, lse, seqs={0}, heads=[0, hq - 1])
+        first.append((o[:new[0]], lse[:new[0]]))
+    for o, lse in first[1:]:
+        assert np.array_equal(o, first[0][0]) and np.array_equal(lse, first[0][1])
+
+
+def test_results_do_not_depend_on_the_calls_before():
+    """A group of 7 fills 126 of a block's 128 query rows; what other kernels leave in shared memory must not matter."""
+    new, lens, hq = [200, 40], [3000, 1500], 28
+    pg, q = _inputs(new, lens, hq, 4, 128, 64, False, "head", 72)
+    big, qb = _inputs([300], [2000], 8, 2, 128, 64, False, "head", 73, q_scale=200.0)
+    first = _run(pg, q, new, hq)
+    _check(pg, q, new, hq, *first, heads=[0, 27])
+    for scale in (1.0, 50.0, float("nan")):
+        o, lse = _run(big, (qb.float() * scale).to(torch.bfloat16), [300], 8)
+        w = torch.zeros((1, 2, 2000), device=DEV)
+        B.mq_kv_weights((qb.float() * scale).to(torch.bfloat16).to(DEV), cu([300]), big.kv_len, big.table, big.cache, 8, 300,
+                        torch.from_numpy(lse.astype(np.float32)).to(DEV), w)
+        again = _run(pg, q, new, hq)
+        assert np.array_equal(first[0], again[0]) and np.array_equal(first[1], again[1])
