@@ -27,6 +27,8 @@
 // Every wait is bounded (mq_sm100.cuh); an expired one makes all roles leave and sets the status word.
 #include <cuda.h>
 
+#include <cfloat>
+
 #include "mq_kv_sched.cuh"
 #include "mq_kv_tma.cuh"
 
@@ -467,7 +469,11 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
       const int all_see = perm ? ctx : min(end, ctx + (pc->row0 + grp * block_rows) / sc.group + 1);   // of this block
       // live rows: without perm, keys below lim; with it, the context and the chunk's rows whose index is at most lim
       const int lim = perm ? (live ? perm[tok] : INT_MIN) : live ? min(end, ctx + tok + 1) : 0;
-      const float scale_log2 = p.scale * 1.4426950408889634f * (kI8 ? p.cache.k_scale[pc->g] : 1.0f);
+      // The maximum is found before the scale is applied, and a masked score is -inf times it: both want a positive scale. A head
+      // whose static scale is not one (zero where every key was zero) has its scores scaled first.
+      const float given = p.scale * 1.4426950408889634f * (kI8 ? p.cache.k_scale[pc->g] : 1.0f);
+      const bool scale_first = kI8 && !(given >= FLT_MIN);
+      const float scale_log2 = scale_first ? 1.0f : given;
       const float lag_raw = kLag / scale_log2, lift_raw = kI8 ? kLiftChunk / scale_log2 : 0.0f;
       float m_used = -1.0e30f, l_run = 0.0f;   // the exponents' reference (raw units), the sum relative to it
       bool begun = false;                      // the accumulator holds products of this piece
@@ -501,6 +507,10 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
           tmem_ld_x32(s_addr, *reinterpret_cast<uint32_t (*)[32]>(&sv[0]));
           tmem_ld_x32(s_addr + 32u, *reinterpret_cast<uint32_t (*)[32]>(&sv[32]));
           tmem_wait_ld();
+          if (kI8 && scale_first) {
+#pragma unroll
+            for (int e = 0; e < 64; ++e) sv[e] = __float_as_uint(__uint_as_float(sv[e]) * given);
+          }
           if (masked) {
             if (perm) {
 #pragma unroll

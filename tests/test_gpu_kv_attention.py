@@ -377,3 +377,19 @@ def test_results_do_not_depend_on_the_calls_before():
                         torch.from_numpy(lse.astype(np.float32)).to(DEV), w)
         again = _run(pg, q, new, hq)
         assert np.array_equal(first[0], again[0]) and np.array_equal(first[1], again[1])
+
+
+@pytest.mark.parametrize("new,lens", [([1, 2], [40, 300]), ([40, 200], [200, 900]), ([90], [60])])
+@pytest.mark.parametrize("aifs", [False, True])
+@pytest.mark.parametrize("value", [0.0, -0.0125, 1e-42])
+def test_static_scales_that_are_not_positive(value, new, lens, aifs):
+    """Zero (a head whose keys were all zero when its scale was taken: its softmax is uniform over what a row sees), a
+    negative number, and one below the normal range."""
+    pg, q = _inputs(new, lens, 6, 3, 128, 16, True, "head", 74)
+    old = float(pg.k_scale[1])
+    pg.cache.k_scale[1] = value
+    for k in pg.k:
+        k[:, 1] = np.round(k[:, 1] / old) * float(np.float32(value))
+    perm = aifs_perm(np.random.default_rng(4), new) if aifs else None
+    o, lse = _run(pg, q, new, 6, perm)
+    _check(pg, q, new, 6, o, lse, perm)
