@@ -45,8 +45,7 @@ inline bool encode_key_tiles(CUtensorMap* map, const void* base, const void* any
 }
 
 // Query row as column `quad` of a B operand: qf[k] = channels of step k.  fac[e] = what turns the scores of rows 2 t4 + e into
-// log2 units.  An int8 cache takes fp16 queries, brought into range by a power of two per row (they keep all their
-// bits), in the channel order that lets a thread read contiguous codes: step k, position (2 t4, 2 t4 + 1, 2 t4 + 8,
+// log2 units.  An int8 cache takes fp16 queries, brought into range by a power of two per row, in the channel order that lets a thread read contiguous codes: step k, position (2 t4, 2 t4 + 1, 2 t4 + 8,
 // 2 t4 + 9) is channel t4 * D/4 + 4 k + 0 .. 3.  In two parts, so that the loads can travel while something else is done.
 template <int kD, bool kI8>
 __device__ __forceinline__ void fetch_query(const uint8_t* q, bool ok, int t4, uint32_t (&qf)[kD / 16][2]) {
@@ -75,8 +74,10 @@ __device__ __forceinline__ void finish_query(int t4, float base_fac, uint32_t (&
       for (int e = 0; e < 2; ++e) m = fmaxf(m, fmaxf(fabsf(kv_bf16_lo(qf[k][e])), fabsf(kv_bf16_hi(qf[k][e]))));
     m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
     m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
-    // the power of two that brings the row's largest magnitude into [1, 2) (an infinity stays one either way)
-    const int e2 = m > 0.0f && m < INFINITY ? (int)((__float_as_uint(m) >> 23) & 255) - 127 : 0;
+    // the power of two that brings the row's largest magnitude into [2^14, 2^15), the highest that fp16 has room for: the 8
+    // bits of a channel are all kept down to 2^-31 of the largest, and what smaller ones lose is below 2^-39 of it.  (An
+    // infinity stays one either way; the last bound keeps the factor itself finite.)
+    const int e2 = m > 0.0f && m < INFINITY ? max((int)((__float_as_uint(m) >> 23) & 255) - 127 - 14, -126) : 0;
     const float f = exp2f((float)-e2), back = base_fac * exp2f((float)e2);
 #pragma unroll
     for (int k = 0; k < kSteps; ++k)

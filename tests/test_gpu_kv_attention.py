@@ -393,3 +393,29 @@ def test_static_scales_that_are_not_positive(value, new, lens, aifs):
     perm = aifs_perm(np.random.default_rng(4), new) if aifs else None
     o, lse = _run(pg, q, new, 6, perm)
     _check(pg, q, new, 6, o, lse, perm)
+
+
+@pytest.mark.parametrize("new,lens,hq,hkv,dim", [([1, 2], [70, 500], 4, 2, 128), ([1], [2100], 12, 1, 64), ([16], [64], 1, 1, 128)])
+def test_a_query_channel_that_dwarfs_the_others_on_an_int8_cache(new, lens, hq, hkv, dim):
+    """One channel 2^20 times the others, and the keys have nothing there: the small channels alone decide, so they need their
+    bits.  (What fp16 loses of them, 2^-39 of the largest = 2^-19 per channel, is within the tolerance for the sum's own
+    roundings: (D + 8) 2^-23 of sum |q| |k|, with |q| about 1.)  The weights take the same queries."""
+    pg, q = _inputs(new, lens, hq, hkv, dim, 16, True, "head", 75)
+    q[:, ::dim] = 2.0 ** 20
+    pg.K[:, :, :, 0] = 0
+    for k in pg.k:
+        k[:, :, 0] = 0.0
+    o, lse = _run(pg, q, new, hq)
+    _check(pg, q, new, hq, o, lse)
+    w = torch.zeros((len(new), hkv, max(lens)), device=DEV)
+    B.mq_kv_weights(q.to(DEV), cu(new), pg.kv_len, pg.table, pg.cache, hq, max(new), torch.from_numpy(lse.astype(np.float32)).to(DEV), w)
+    qf, group, start = q.double().numpy().reshape(-1, hq, dim), hq // hkv, 0
+    for b, n in enumerate(new):
+        for g in range(hkv):
+            heads = range(g * group, (g + 1) * group)
+            rows = [qf[start:start + n, h] for h in heads]
+            ref = O.weights(rows, pg.k[b][:, g], [lse[start:start + n, h] for h in heads], dim ** -0.5)
+            mag = max(O.attention(r, pg.k[b][:, g], pg.v[b][:, g], dim ** -0.5)[4].max() for r in rows)
+            rel = (dim + 8) * 2.0 ** -23 * mag + 2.0 ** -22 * (mag + np.abs(lse).max()) + 2.0 ** -21 + n * group * 2.0 ** -24
+            assert np.all(np.abs(w[b, g, :lens[b]].double().cpu().numpy() - ref) <= (rel + 2.0 ** -23) * ref + 1e-37)
+        start += n
