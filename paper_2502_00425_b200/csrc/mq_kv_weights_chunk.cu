@@ -39,6 +39,7 @@ struct Barriers {
   uint64_t k_full[2], k_empty[2];
   uint64_t q_full[kQStages], q_empty[kQStages], l_full[kLStages], l_empty[kLStages];   // queries; their log-sum-exps
   uint64_t s_full[4], s_empty[4];
+  uint64_t x_full[kRing];   // the second group's sums of a piece stand in shared memory
   uint64_t drain;
   uint32_t tmem_base;
   int abort_flag;
@@ -51,7 +52,7 @@ struct Cfg {
   static constexpr int kTileBytes = kHalves * kHalfBytes;
   static constexpr int kThreads = (kI8 ? 16 : 12) * 32;
   static constexpr int kSmem = 1024 + (2 + kQStages) * kTileBytes + (int)sizeof(Barriers) + kRing * (int)sizeof(Piece) + kLStages * kCols * 8 +
-                               2 * kKeys * 4 + 16 * 8 + 64;
+                               kRing * kKeys * 4 + 16 * 8 + 64;
 };
 
 // First row tile of the unit of keys key0 ..: without perm the rows before the first key's own see none of them.
@@ -96,8 +97,8 @@ kv_weights_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid
   Piece* ring = reinterpret_cast<Piece*>(sh + 1);
   float* neg_lse = reinterpret_cast<float*>((reinterpret_cast<uintptr_t>(ring + kRing) + 15) & ~uintptr_t(15));   // [stage][col], log2 units
   int32_t* rank = reinterpret_cast<int32_t*>(neg_lse + kLStages * kCols);                                        // [stage][col]
-  float* xch = reinterpret_cast<float*>(rank + kLStages * kCols);                                                // [piece parity][key]
-  int64_t* red = reinterpret_cast<int64_t*>(xch + 2 * kKeys);
+  float* xch = reinterpret_cast<float*>(rank + kLStages * kCols);                                                // [piece][key]
+  int64_t* red = reinterpret_cast<int64_t*>(xch + kRing * kKeys);
   int64_t* prefix = red + 16;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tid = threadIdx.x;
   const int tokens = kCols / p.group, block_rows = tokens * p.group.d;
@@ -105,7 +106,7 @@ kv_weights_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid
   if (tid == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmap_q)) : "memory");
     if (!kI8) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmap_k)) : "memory");
-    for (int i = 0; i < kRing; ++i) { mbar_init(&sh->piece_full[i], 1); mbar_init(&sh->piece_empty[i], 8); }
+    for (int i = 0; i < kRing; ++i) { mbar_init(&sh->piece_full[i], 1); mbar_init(&sh->piece_empty[i], 8); mbar_init(&sh->x_full[i], 4); }
     for (int i = 0; i < 2; ++i) { mbar_init(&sh->k_full[i], kI8 ? 4 : 1); mbar_init(&sh->k_empty[i], 1); }
     for (int i = 0; i < kQStages; ++i) { mbar_init(&sh->q_full[i], 1); mbar_init(&sh->q_empty[i], 1); }
     for (int i = 0; i < kLStages; ++i) { mbar_init(&sh->l_full[i], 1); mbar_init(&sh->l_empty[i], 4); }
@@ -428,15 +429,19 @@ kv_weights_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid
         }
         sum += (acc[0].x + acc[0].y) + (acc[1].x + acc[1].y);
       }
-      // ---- the unit's sums: the second group's first through shared memory
-      if (grp == 1) xch[(np & 1) * kKeys + r] = sum;
-      const bool all_ok = !named_bar_or(1, 256, !ok);
-      if (!all_ok) {
-        ok = false;
+      if (!ok) break;
+      // ---- the unit's sums: the second group's first through shared memory, a slot per published piece (it is written again only
+      // after both groups were done with its piece).  A bounded wait like all others: where one group has given up, the other
+      // must not stay at a barrier for it.
+      if (grp == 1) {
+        xch[np % kRing * kKeys + r] = sum;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh->x_full[np % kRing]);
+      } else if (!(ok = warp_all(mbar_wait(&sh->x_full[np % kRing], (uint32_t)(np / kRing) & 1u, &sh->abort_flag, sh->status, 85)))) {
         break;
       }
       if (grp == 0 && key < n_all) {
-        if (key < p.w_keys) p.W_out[out] = (p.W_in && key < ctx ? p.W_in[out] : 0.0f) + (sum + xch[(np & 1) * kKeys + r]);
+        if (key < p.w_keys) p.W_out[out] = (p.W_in && key < ctx ? p.W_in[out] : 0.0f) + (sum + xch[np % kRing * kKeys + r]);
         else if (p.status) atomicCAS(p.status, MQ_OK, MQ_ERR_INVALID_ARG);
       }
       __syncwarp();

@@ -1,6 +1,7 @@
 """Host-side checks of the key/value-cache entry points (no GPU): refusals before anything is enqueued, workspace sizes,
 and pins of the float64 oracle."""
 import ctypes as C
+import os
 
 import numpy as np
 import pytest
@@ -139,6 +140,17 @@ def test_binding_refuses_mismatched_tensors():
         B.KVCache(K.to(torch.int8), K.to(torch.int8))                               # an int8 cache without scales
     with pytest.raises(ValueError):
         B.KVCache(K, K.clone())                                                     # host memory
+
+
+def test_roles_of_the_cache_kernels_meet_at_bounded_waits_only():
+    """A barrier over some of a CTA's warps (bar.sync / bar.red with a name) has no limit: a warp that gave up on a bounded wait
+    would leave the others at it for good.  The roles of these kernels are ordered by mbarriers, whose waits expire."""
+    src = os.path.join(os.path.dirname(build.__file__), "csrc")
+    names = [f for f in os.listdir(src) if f.startswith("mq_kv")]
+    assert "mq_kv_weights_chunk.cu" in names and "mq_kv_chunk.cu" in names
+    for f in names:
+        text = open(os.path.join(src, f)).read()
+        assert "named_bar" not in text and "bar.sync" not in text and "bar.red" not in text, f
 
 
 # ------------------------------------------------------------------------------------------------ the oracle
