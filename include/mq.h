@@ -557,7 +557,7 @@ int mq_kv_weights(const void* Q, int64_t ldq, const mq_kv_batch* batch, const mq
  *   all of them if n <= budget; else the first n_first and the last n_last keys and, of the others, the
  *   budget - n_first - n_last with the largest W[b, g, j] (of equal ones the lowest j; a NaN counts as lowest).
  *   kept     int32 [n_seq, n_kv_heads, budget]: the kept keys' indices, ascending; entries behind them are left as they were
- *   new_len  int32 [n_seq]: min(n, budget)
+ *   new_len  int32 [n_seq]: min(n, budget); may be kv_len itself (lengths in place), but not overlap it in part
  *   W_out    optional float32 [n_seq, n_kv_heads, budget]: the kept keys' weights (same order)
  *   dst, dst_table [n_seq][dst_max_pages]: where the kept rows go, row i to slot i of the sequence's new pages; dst
  *            has the type, heads and head_dim of `cache`, and may be the same cache as long as no destination page

@@ -82,12 +82,13 @@ kv_select_kernel(const __grid_constant__ EvictParams p, const int held_most) {
   reinterpret_cast<uint4*>(hist)[tid] = make_uint4(0u, 0u, 0u, 0u);
   pdl_wait();
   pdl_launch_dependents();   // (behind the wait: the copy kernel reads lengths and tables before its own)
-  const int n = evict_len(p, b), m = min(n, p.budget);
+  const int n = evict_len(p, b);
   const float* row = p.W + (int64_t)b * p.w_seq + (int64_t)g * p.w_head;
   const int n_w = min(n, p.w_keys);
   auto w = [&](int j) { return j < n_w ? row[j] : __int_as_float(0x7fffffff); };
   const int64_t out = ((int64_t)b * p.src.n_kv_heads + g) * p.budget;
-  if (g == 0 && tid == 0) p.new_len[b] = m;
+  // (kv_len and new_len may be one array: it is written once every head has been selected, by the copy)
+  if (p.budget == 0 && g == 0 && tid == 0) p.new_len[b] = 0;
   if (n <= p.budget) {
     for (int j = tid; j < n; j += kSelThreads) {
       p.kept[out + j] = j;
@@ -229,6 +230,7 @@ kv_copy_kernel(const __grid_constant__ EvictParams p) {
   const int32_t* kept = p.kept + ((int64_t)b * p.src.n_kv_heads + g) * p.budget;
   pdl_launch_dependents();
   pdl_wait();
+  if (blockIdx.x == 0 && g == 0 && threadIdx.x == 0) p.new_len[b] = m;   // (CTAs that read it from here get the same m)
   for (int i0 = blockIdx.x * kPerCta * kCopyRows; i0 < m; i0 += gridDim.x * kPerCta * kCopyRows) {
     uint4 k[kCopyRows], v[kCopyRows];
     int64_t to[kCopyRows];
@@ -288,6 +290,8 @@ extern "C" int mq_kv_evict(const mq_kv_cache* cache, const int32_t* page_table, 
   if (n_seq > kMaxKvSeqs || cache->n_kv_heads > 65535 || max_pages > (1 << 22) || dst_max_pages > (1 << 22)) return MQ_ERR_UNSUPPORTED;
   if (n_seq == 0) return MQ_OK;
   if (!kv_len || !new_len || (max_pages > 0 && (!page_table || (w_keys > 0 && !W))) || (budget > 0 && (!dst_table || !kept))) return MQ_ERR_INVALID_ARG;
+  // lengths in place are fine, as one array; shifted ones would be read after they were written
+  if (kv_len != new_len && kv_len < new_len + n_seq && new_len < kv_len + n_seq) return MQ_ERR_INVALID_ARG;
   p.dim_bytes = cache->head_dim * ((cache->flags & MQ_KV_INT8) ? 1 : 2);
   p.table = page_table; p.max_pages = max_pages; p.kv_len = kv_len; p.n_seq = n_seq;
   p.W = W; p.w_seq = w_seq_stride; p.w_head = w_head_stride; p.w_keys = w_keys;

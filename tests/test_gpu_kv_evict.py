@@ -351,3 +351,28 @@ def test_rows_that_are_nan_stay_with_their_sequence(new, lens, hq, int8):
         B.mq_kv_weights(rows.to(DEV), cu(new), pg.kv_len, pg.table, pg.cache, hq, max(new), l.to(DEV), w)
         got.append(w)
     assert torch.equal(got[0][0], got[1][0]) and bool(torch.isnan(got[1][1, :, 0]).all())
+
+
+@pytest.mark.parametrize("budget", [700, 64, 0])
+def test_evict_with_lengths_in_place(budget):
+    """new_len may be kv_len: no head may see the new length instead of the old one."""
+    rng = np.random.default_rng(8)
+    hkv, dim, page = 8, 64, 16
+    lens = [int(x) for x in rng.integers(1, 1500, 24)] + [0, budget, budget + 1]
+    pg = Paged(lens, hkv, dim, page, True, "head", 97)
+    w = torch.rand((len(lens), hkv, max(lens)), generator=torch.Generator().manual_seed(6)).to(DEV)
+    width = max(1, -(-budget // page))
+    table = torch.arange(len(lens) * width, dtype=torch.int32, device=DEV).view(len(lens), width)
+    K, V = (torch.zeros((len(lens) * width, hkv, page, dim), dtype=torch.int8, device=DEV) for _ in range(2))
+    dst = B.KVCache(K, V, pg.cache.k_scale, pg.cache.v_scale)
+    kept = torch.full((len(lens), hkv, budget), -9, dtype=torch.int32, device=DEV)
+    for _ in range(3):
+        kept.fill_(-9)
+        length = pg.kv_len.clone()
+        B.mq_kv_evict(pg.cache, pg.table, length, w, budget, 2, 3, dst, table, kept, length) if budget else \
+            B.mq_kv_evict(pg.cache, pg.table, length, w, budget, 0, 0, dst, table, kept, length)
+        assert length.tolist() == [min(n, budget) for n in lens]
+        for b, n in enumerate(lens if budget else []):
+            for g in range(hkv):
+                ref = O.keep(w[b, g].cpu().numpy(), n, budget, 2, 3)
+                assert np.array_equal(kept[b, g, :ref.size].cpu().numpy(), ref) and bool((kept[b, g, ref.size:] == -9).all())

@@ -110,6 +110,7 @@ def test_evict_refusals(lib):
     assert call(n=5000) == B.MQ_ERR_UNSUPPORTED
     assert call(table=None) == call(kv=None) == call(w=None) == call(dt=None) == call(kept=None) == call(nl=None) == B.MQ_ERR_INVALID_ARG
     assert call(n=0) == B.MQ_OK
+    assert call(nl=A + 4) == call(nl=A - 4) == B.MQ_ERR_INVALID_ARG                 # lengths that overlap in part
 
 
 def test_norm_rope_refusals(lib):
