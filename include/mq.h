@@ -558,7 +558,8 @@ int mq_kv_weights(const void* Q, int64_t ldq, const mq_kv_batch* batch, const mq
  *   budget - n_first - n_last with the largest W[b, g, j] (of equal ones the lowest j; a NaN counts as lowest).
  *   kept     int32 [n_seq, n_kv_heads, budget]: the kept keys' indices, ascending; entries behind them are left as they were
  *   new_len  int32 [n_seq]: min(n, budget); may be kv_len itself (lengths in place), but not overlap it in part
- *   W_out    optional float32 [n_seq, n_kv_heads, budget]: the kept keys' weights (same order)
+ *   W_out    optional float32 [n_seq, n_kv_heads, budget]: the kept keys' weights (same order); memory apart from W's
+ *            (MQ_ERR_INVALID_ARG)
  *   dst, dst_table [n_seq][dst_max_pages]: where the kept rows go, row i to slot i of the sequence's new pages; dst
  *            has the type, heads and head_dim of `cache`, and may be the same cache as long as no destination page
  *            is a source page of any sequence.  dst_max_pages * page_size must reach the budget.

@@ -292,6 +292,12 @@ extern "C" int mq_kv_evict(const mq_kv_cache* cache, const int32_t* page_table, 
   if (!kv_len || !new_len || (max_pages > 0 && (!page_table || (w_keys > 0 && !W))) || (budget > 0 && (!dst_table || !kept))) return MQ_ERR_INVALID_ARG;
   // lengths in place are fine, as one array; shifted ones would be read after they were written
   if (kv_len != new_len && kv_len < new_len + n_seq && new_len < kv_len + n_seq) return MQ_ERR_INVALID_ARG;
+  // a head's kept weights would replace weights that other heads still have to read
+  if (W_out && W && budget > 0 && w_keys > 0) {
+    const __int128 w_end = (__int128)(n_seq - 1) * w_seq_stride + (__int128)(cache->n_kv_heads - 1) * w_head_stride + w_keys;
+    const __int128 out_end = (__int128)n_seq * cache->n_kv_heads * budget, w0 = reinterpret_cast<intptr_t>(W), o0 = reinterpret_cast<intptr_t>(W_out);
+    if (w0 < o0 + out_end * 4 && o0 < w0 + w_end * 4) return MQ_ERR_INVALID_ARG;
+  }
   p.dim_bytes = cache->head_dim * ((cache->flags & MQ_KV_INT8) ? 1 : 2);
   p.table = page_table; p.max_pages = max_pages; p.kv_len = kv_len; p.n_seq = n_seq;
   p.W = W; p.w_seq = w_seq_stride; p.w_head = w_head_stride; p.w_keys = w_keys;

@@ -110,7 +110,17 @@ def test_evict_refusals(lib):
     assert call(n=5000) == B.MQ_ERR_UNSUPPORTED
     assert call(table=None) == call(kv=None) == call(w=None) == call(dt=None) == call(kept=None) == call(nl=None) == B.MQ_ERR_INVALID_ARG
     assert call(n=0) == B.MQ_OK
+
+
+def test_evict_refuses_outputs_over_its_inputs(lib):
+    """Refused before anything is enqueued (an accepted call would go to a device)."""
+    def call(kv=A, w=0x1000000, nl=A, w_out=None):
+        return lib.mq_kv_evict(C.byref(_cache()), A, 7, kv, 2, w, 4096, 512, 448, 64, 0, 0, C.byref(_cache()), A, 7, A, nl, w_out, None)
+
     assert call(nl=A + 4) == call(nl=A - 4) == B.MQ_ERR_INVALID_ARG                 # lengths that overlap in part
+    # kept weights in the memory of the weights: W ends (2 - 1) * 4096 + 3 * 512 + 448 elements behind its start, W_out 2 * 4 * 64
+    w, w_end, o_len = 0x1000000, (4096 + 3 * 512 + 448) * 4, 2 * 4 * 64 * 4
+    assert call(w_out=w) == call(w_out=w + w_end - 4) == call(w_out=w - o_len + 4) == B.MQ_ERR_INVALID_ARG
 
 
 def test_norm_rope_refusals(lib):
