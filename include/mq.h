@@ -464,7 +464,7 @@ int mq_aifs_attention(const void* Q, int64_t ldq, const void* K, int64_t ldk, co
  * mq_kv_cache describes the pages.  Key s of page p, head g is the row of head_dim contiguous elements at
  * K + p * page_stride + g * head_stride + s * slot_stride (elements), and V alike: both page layouts in use,
  * [page][head][slot][dim] and [page][slot][head][dim], are strides of this form.  Rows must start on 16-byte
- * boundaries (MQ_ERR_ALIGNMENT).  head_dim 64 or 128, page_size a power of two from 16 to 256
+ * boundaries (MQ_ERR_ALIGNMENT); rows of a cache that a call writes to may not overlap (MQ_ERR_INVALID_ARG).  head_dim 64 or 128, page_size a power of two from 16 to 256
  * (MQ_ERR_UNSUPPORTED).  Elements are bf16 or, with MQ_KV_INT8, int8 codes with one static scale per
  * key/value head and tensor (Eq. 2: value = code * scale), k_scale / v_scale device float32 [n_kv_heads].
  *

@@ -44,7 +44,7 @@ inline int check_kv_cache(const mq_kv_cache* c, KvView* out) {
   if (c->n_pages > 0 && (!c->K || !c->V)) return MQ_ERR_INVALID_ARG;
   if (i8 != (c->k_scale != nullptr) || i8 != (c->v_scale != nullptr)) return MQ_ERR_INVALID_ARG;
   const int64_t es = i8 ? 1 : 2;
-  // a row is contiguous and rows never overlap; every row starts on a 16-byte boundary
+  // a row is contiguous, no stride is shorter than a row, and every row starts on a 16-byte boundary
   if (c->slot_stride < c->head_dim || c->head_stride < c->head_dim || c->page_stride < c->head_dim) return MQ_ERR_INVALID_ARG;
   const int64_t lim = (int64_t)1 << 38;
   if (c->slot_stride > lim || c->head_stride > lim || c->page_stride > lim) return MQ_ERR_UNSUPPORTED;
@@ -62,6 +62,28 @@ inline int check_kv_cache(const mq_kv_cache* c, KvView* out) {
   out->k_scale = c->k_scale;
   out->v_scale = c->v_scale;
   return MQ_OK;
+}
+
+// Whether no two of the blocks of `extent` elements that `n` strides and counts span share memory: in the order of their strides,
+// each must step over all that the smaller ones reach.
+inline bool kv_apart(int64_t extent, int n, const int64_t* stride, const int64_t* count) {
+  unsigned done = 0;
+  __int128 reach = extent;
+  for (int i = 0; i < n; ++i) {
+    int k = -1;
+    for (int j = 0; j < n; ++j)
+      if (!(done >> j & 1u) && (k < 0 || stride[j] < stride[k])) k = j;
+    done |= 1u << k;
+    if (count[k] <= 1) continue;
+    if (stride[k] < reach) return false;
+    reach += (__int128)(count[k] - 1) * stride[k];
+  }
+  return true;
+}
+// The rows of a cache that is written to (reading shared rows is harmless).
+inline bool kv_rows_apart(const mq_kv_cache* c) {
+  const int64_t stride[3] = {c->slot_stride, c->head_stride, c->page_stride}, count[3] = {c->page_size, c->n_kv_heads, c->n_pages};
+  return kv_apart(c->head_dim, 3, stride, count);
 }
 
 constexpr int kMaxKvSeqs = 2048;   // sequences of one call: every CTA keeps a prefix over them in shared memory

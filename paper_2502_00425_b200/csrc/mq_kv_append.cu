@@ -204,7 +204,7 @@ extern "C" int mq_qk_norm_rope(const void* Q, int64_t ldq, const void* K, int64_
   if (cache) {
     const int rc = check_kv_cache(cache, &p.c);
     if (rc != MQ_OK) return rc;
-    if (cache->head_dim != head_dim || cache->n_kv_heads != n_kv_heads) return MQ_ERR_INVALID_ARG;
+    if (cache->head_dim != head_dim || cache->n_kv_heads != n_kv_heads || !kv_rows_apart(cache)) return MQ_ERR_INVALID_ARG;
   }
   const int64_t wq = (int64_t)n_q_heads * head_dim, wk = (int64_t)n_kv_heads * head_dim;
   if (ldq < wq || ldk < wk || ldqo < wq || (K_out && ldko < wk) || (cache && ldv < wk)) return MQ_ERR_INVALID_ARG;

@@ -283,7 +283,7 @@ extern "C" int mq_kv_evict(const mq_kv_cache* cache, const int32_t* page_table, 
   int rc = check_kv_cache(cache, &p.src);
   if (rc != MQ_OK) return rc;
   if ((rc = check_kv_cache(dst, &p.dst)) != MQ_OK) return rc;
-  if (dst->flags != cache->flags || dst->head_dim != cache->head_dim || dst->n_kv_heads != cache->n_kv_heads) return MQ_ERR_INVALID_ARG;
+  if (dst->flags != cache->flags || dst->head_dim != cache->head_dim || dst->n_kv_heads != cache->n_kv_heads || !kv_rows_apart(dst)) return MQ_ERR_INVALID_ARG;
   if (n_seq < 0 || max_pages < 0 || dst_max_pages < 0 || budget < 0 || n_first < 0 || n_last < 0 || w_seq_stride < 0 || w_head_stride < 0 || w_keys < 0)
     return MQ_ERR_INVALID_ARG;
   if ((int64_t)n_first + n_last > budget || (int64_t)dst_max_pages * dst->page_size < budget) return MQ_ERR_INVALID_ARG;

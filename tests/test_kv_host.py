@@ -153,6 +153,30 @@ def test_binding_refuses_mismatched_tensors():
         B.KVCache(K, K.clone())                                                     # host memory
 
 
+@pytest.mark.parametrize("kw", [
+    dict(page_stride=128, head_stride=128, slot_stride=128),                                # all rows in one place
+    dict(page_stride=4 * 64 * 128, head_stride=128, slot_stride=256),                       # four heads in room for two
+    dict(page_stride=4 * 64 * 128 - 128, head_stride=64 * 128, slot_stride=128),            # a page's end over the next one's start
+    dict(page_stride=128, head_stride=10 * 128, slot_stride=40 * 128 - 64),
+])
+def test_writers_refuse_a_cache_whose_rows_overlap(lib, kw):
+    c, good = _cache(**kw), _cache()
+    assert lib.mq_qk_norm_rope(A, 1024, A, 512, A, 512, 5, 8, 4, 128, None, None, 1e-6, A, 1e4, 0, A, 1024, None, 0,
+                               C.byref(c), A, None) == B.MQ_ERR_INVALID_ARG
+    assert lib.mq_kv_evict(C.byref(good), A, 7, A, 2, A, 4096, 512, 448, 64, 0, 0, C.byref(c), A, 7, A, A, None, None) == B.MQ_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("kw", [
+    dict(page_stride=128, head_stride=10 * 128, slot_stride=40 * 128),                      # any order of the dimensions
+    dict(page_stride=64 * 160, head_stride=1 << 30, slot_stride=160),
+    dict(page_stride=128, n_pages=1),                                                       # a stride that is never taken
+])
+def test_writers_take_rows_in_any_order(lib, kw):
+    assert lib.mq_qk_norm_rope(A, 1024, A, 512, A, 512, 0, 8, 4, 128, None, None, 1e-6, A, 1e4, 0, A, 1024, None, 0,
+                               C.byref(_cache(**kw)), A, None) == B.MQ_OK                   # no rows: nothing is enqueued
+    assert lib.mq_kv_evict(C.byref(_cache()), A, 7, A, 0, A, 4096, 512, 448, 64, 0, 0, C.byref(_cache(**kw)), A, 7, A, A, None, None) == B.MQ_OK
+
+
 def test_roles_of_the_cache_kernels_meet_at_bounded_waits_only():
     """A barrier over some of a CTA's warps (bar.sync / bar.red with a name) has no limit: a warp that gave up on a bounded wait
     would leave the others at it for good.  The roles of these kernels are ordered by mbarriers, whose waits expire."""
