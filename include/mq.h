@@ -543,7 +543,8 @@ int mq_kv_attention(const void* Q, int64_t ldq, const mq_kv_batch* batch, const 
  * for j < kv_len[b]; other entries of W_out are left as they were (without rows, total_q = 0, W_in is copied).  lse is mq_kv_attention's output for the same
  * call.  W_in NULL counts as zeros; W_in == W_out accumulates in place.  float32 throughout, and every sum is
  * taken in a fixed order (no atomics).  w_seq_stride, w_head_stride: elements between sequences and heads, w_keys:
- * entries of a head's row (of both arrays); keys at or behind w_keys are neither read nor written.  status: optional
+ * entries of a head's row (of both arrays); keys at or behind w_keys are neither read nor written.  Rows may not
+ * overlap (MQ_ERR_INVALID_ARG).  status: optional
  * device int32[2], zeroed by the caller: MQ_ERR_INVALID_ARG for a page number outside the cache or a kv_len beyond
  * w_keys, MQ_ERR_TIMEOUT and the wait's site if a bounded wait expired.
  */

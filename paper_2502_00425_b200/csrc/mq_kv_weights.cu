@@ -248,6 +248,9 @@ extern "C" int mq_kv_weights(const void* Q, int64_t ldq, const mq_kv_batch* batc
   if ((int64_t)batch->max_q * group > (1 << 30)) return MQ_ERR_UNSUPPORTED;
   if (batch->n_seq == 0 || reach == 0 || w_keys == 0) return MQ_OK;
   if (!W_out || (batch->total_q > 0 && (!Q || !lse))) return MQ_ERR_INVALID_ARG;
+  // heads or sequences that share entries of W_out would write them at the same time
+  const int64_t stride[2] = {w_head_stride, w_seq_stride}, count[2] = {cache->n_kv_heads, batch->n_seq};
+  if (!kv_apart(w_keys < reach ? w_keys : reach, 2, stride, count)) return MQ_ERR_INVALID_ARG;
   if (!kv_aligned16(Q) || ldq % 8) return MQ_ERR_ALIGNMENT;
   p.Q = static_cast<const uint8_t*>(Q);
   p.ldq = ldq * 2;

@@ -97,6 +97,15 @@ def test_weights_refusals(lib):
     assert call(n_seq=0, total=0, max_q=0) == call(max_pages=0) == call(wk=0) == B.MQ_OK
 
 
+def test_weights_refuse_rows_that_share_entries(lib):
+    def call(ss, hs, wk, max_pages=7):      # two sequences of four heads, 7 pages of 64 keys
+        return lib.mq_kv_weights(A, 1024, C.byref(_batch(max_pages=max_pages)), C.byref(_cache()), 8, 0.1, A, None, A, ss, hs, wk, None, None)
+
+    assert call(0, 448, 448) == call(4 * 448, 0, 448) == call(0, 0, 448) == B.MQ_ERR_INVALID_ARG     # (expanded tensors)
+    assert call(4 * 448, 447, 448) == call(4 * 448 - 1, 448, 448) == call(448, 2 * 448 - 1, 448) == B.MQ_ERR_INVALID_ARG
+    assert call(4 * 128, 128, 448, max_pages=0) == B.MQ_OK                                           # (nothing to do)
+
+
 def test_evict_refusals(lib):
     def call(src=None, dst=None, table=A, mp=7, kv=A, n=2, w=A, ss=4096, hs=512, wk=448, budget=64, first=0, last=0, dt=A, dmp=7, kept=A, nl=A):
         return lib.mq_kv_evict(C.byref(src or _cache()), table, mp, kv, n, w, ss, hs, wk, budget, first, last, C.byref(dst or _cache()), dt,
