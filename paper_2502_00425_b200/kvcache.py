@@ -47,6 +47,7 @@ class PagedKVCache:
         self.tokens = [0] * n_seq        # tokens seen: the next token's position (eviction does not change it)
         self.table = torch.full((n_seq, -(-max_len // page_size)), -1, dtype=torch.int32, device=device)
         self.weights: Optional[torch.Tensor] = None   # accumulated softmax weights, once track_weights() was called
+        self.weights_status = torch.zeros(2, dtype=torch.int32, device=device)   # of every mq_kv_weights call
         self._ws = {}
 
     def _take(self, n: int) -> List[int]:
@@ -60,7 +61,8 @@ class PagedKVCache:
         self.table[b].copy_(row)
 
     def track_weights(self):
-        """Keeps the softmax weight every key receives (mq_kv_weights), for evict()."""
+        """Keeps the softmax weight every key receives (mq_kv_weights), for evict(); called again, it starts over."""
+        self.weights_status.zero_()
         self.weights = torch.zeros((self.n_seq, self.handle.n_kv_heads, self.max_len), device=self.device)
 
     def extend(self, new: Sequence[int]) -> CacheStep:
@@ -108,7 +110,7 @@ class PagedKVCache:
                           lse=lse, perm=perm, scale=scale)
         if self.weights is not None:
             B.mq_kv_weights(q, step.cu_q, step.kv_len, self.table, self.handle, n_q_heads, step.max_q, lse, self.weights,
-                            w_in=self.weights, perm=perm, scale=scale)
+                            w_in=self.weights, perm=perm, scale=scale, status=self.weights_status)
         return o
 
     def evict(self, budget: int, n_first: int, n_last: int) -> torch.Tensor:
@@ -116,6 +118,8 @@ class PagedKVCache:
         `kept`; entries behind a sequence's new length are -1).  The kept rows move to fresh pages, the old ones are freed."""
         if self.weights is None:
             raise RuntimeError("track_weights() first")
+        if B.mq_last_device_status(self.weights_status)[0] != B.MQ_OK:   # (keys would be dropped for good by them)
+            raise RuntimeError("the accumulated weights are not whole: a call that added to them has failed")
         ps = self.page_size
         after = [min(n, budget) for n in self.lengths]
         pool = self._take(sum(-(-n // ps) for n in after))
@@ -138,4 +142,5 @@ class PagedKVCache:
         return kept
 
     def status_ok(self) -> bool:
-        return all(B.mq_last_device_status(ws)[0] == B.MQ_OK for ws in self._ws.values())
+        """Whether every attention and every accumulation of weights so far went through (waits for the current stream)."""
+        return all(B.mq_last_device_status(s)[0] == B.MQ_OK for s in [*self._ws.values(), self.weights_status])

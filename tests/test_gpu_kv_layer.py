@@ -6,6 +6,7 @@ import pytest
 import torch
 
 from oracle import kv_oracle as O
+from paper_2502_00425_b200 import binding as B
 from paper_2502_00425_b200 import kvcache as KC
 from paper_2502_00425_b200 import layer as LY
 from paper_2502_00425_b200 import synth
@@ -165,6 +166,26 @@ def test_cache_refusals():
     assert cache.lengths == [0, 0] and len(cache.free) == 3
     with pytest.raises(RuntimeError):
         cache.evict(8, 0, 0)                 # no weights are tracked
+
+
+@pytest.mark.parametrize("n_new", [1, 40])
+def test_a_failed_accumulation_of_weights_shows_in_the_status(n_new):
+    cache = KC.PagedKVCache(2, 30, 130, 2, 128, page_size=16)
+    cache.track_weights()
+    q = _emb(2 * n_new, 3)[:, :512].repeat(1, 2).contiguous()
+    cache.attend(q, cache.extend([n_new, n_new]), 8)
+    assert cache.status_ok()
+    cache.weights = torch.zeros((2, 2, 2 * n_new - 1), device=DEV)     # rows too short for what follows: the call leaves keys out and says so
+    cache.attend(q, cache.extend([n_new, n_new]), 8)
+    assert not cache.status_ok()
+    assert all(B.mq_last_device_status(ws)[0] == B.MQ_OK for ws in cache._ws.values())
+    with pytest.raises(RuntimeError, match="not whole"):
+        cache.evict(2, 0, 1)
+    cache.track_weights()                                          # starts over
+    assert cache.status_ok()
+    cache.attend(q, cache.extend([n_new, n_new]), 8)
+    cache.evict(2, 0, 1)
+    assert cache.lengths == [2, 2] and cache.status_ok()
 
 
 def test_workspaces_of_a_cache_stay_few_and_are_made_before_a_capture():
