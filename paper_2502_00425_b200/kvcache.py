@@ -55,6 +55,9 @@ class PagedKVCache:
             raise RuntimeError(f"the cache has {len(self.free)} free pages, {n} are needed")
         return [self.free.pop() for _ in range(n)]
 
+    def _give_back(self, pages: Sequence[int]):
+        self.free += list(pages)[::-1]
+
     def _show(self, b: int):
         row = torch.full((self.table.shape[1],), -1, dtype=torch.int32)
         row[:len(self.pages[b])] = torch.tensor(self.pages[b], dtype=torch.int32)
@@ -122,16 +125,21 @@ class PagedKVCache:
             raise RuntimeError("the accumulated weights are not whole: a call that added to them has failed")
         ps = self.page_size
         after = [min(n, budget) for n in self.lengths]
-        pool = self._take(sum(-(-n // ps) for n in after))
-        fresh = [[pool.pop() for _ in range(-(-n // ps))] for n in after]
-        table = torch.full((self.n_seq, max(1, -(-budget // ps))), -1, dtype=torch.int32)
-        for b, p in enumerate(fresh):
-            table[b, :len(p)] = torch.tensor(p, dtype=torch.int32)
-        kept = torch.full((self.n_seq, self.handle.n_kv_heads, budget), -1, dtype=torch.int32, device=self.device)
-        new_len = torch.empty(self.n_seq, dtype=torch.int32, device=self.device)
-        w_out = torch.zeros((self.n_seq, self.handle.n_kv_heads, budget), device=self.device)
-        B.mq_kv_evict(self.handle, self.table, torch.tensor(self.lengths, dtype=torch.int32).to(self.device), self.weights, budget,
-                      n_first, n_last, self.handle, table.to(self.device), kept, new_len, w_out=w_out)
+        taken = self._take(sum(-(-n // ps) for n in after))
+        try:
+            pool = list(taken)
+            fresh = [[pool.pop() for _ in range(-(-n // ps))] for n in after]
+            table = torch.full((self.n_seq, max(1, -(-budget // ps))), -1, dtype=torch.int32)
+            for b, p in enumerate(fresh):
+                table[b, :len(p)] = torch.tensor(p, dtype=torch.int32)
+            kept = torch.full((self.n_seq, self.handle.n_kv_heads, budget), -1, dtype=torch.int32, device=self.device)
+            new_len = torch.empty(self.n_seq, dtype=torch.int32, device=self.device)
+            w_out = torch.zeros((self.n_seq, self.handle.n_kv_heads, budget), device=self.device)
+            B.mq_kv_evict(self.handle, self.table, torch.tensor(self.lengths, dtype=torch.int32).to(self.device), self.weights, budget,
+                          n_first, n_last, self.handle, table.to(self.device), kept, new_len, w_out=w_out)
+        except BaseException:   # (refused, or no memory for its outputs: nothing has moved)
+            self._give_back(taken)
+            raise
         m = min(budget, self.max_len)
         self.weights.zero_()
         self.weights[:, :, :m] = w_out[:, :, :m]

@@ -1,0 +1,57 @@
+"""PagedKVCache's bookkeeping on the host, with the library's calls replaced: what a step or an eviction that fails leaves behind."""
+import pytest
+import torch
+
+from paper_2502_00425_b200 import binding as B
+from paper_2502_00425_b200 import kvcache as KC
+
+
+class Handle:
+    def __init__(self, K, V, k_scale=None, v_scale=None):
+        self.n_kv_heads, self.head_dim, self.page_size, self.device = K.shape[1], K.shape[3], K.shape[2], K.device
+
+
+@pytest.fixture
+def make(monkeypatch):
+    monkeypatch.setattr(B, "KVCache", Handle)
+    monkeypatch.setattr(B, "mq_last_device_status", lambda ws: (B.MQ_OK, 0))
+    return lambda *args, **kw: KC.PagedKVCache(*args, device="cpu", **kw)
+
+
+def _state(cache):
+    return (list(cache.free), [list(p) for p in cache.pages], list(cache.lengths), list(cache.tokens))
+
+
+def _refuse(*args, **kw):
+    raise B.MqError(B.MQ_ERR_INVALID_ARG, "mq_kv_evict")
+
+
+def test_a_refused_eviction_keeps_its_pages(make, monkeypatch):
+    cache = make(2, 12, 64, 2, 64, page_size=16)
+    cache.track_weights()
+    cache.extend([40, 20])
+    before, weights = _state(cache), cache.weights.clone()
+    monkeypatch.setattr(B, "mq_kv_evict", _refuse)
+    for _ in range(5):                       # (the pool has room for two evictions' pages)
+        with pytest.raises(B.MqError):
+            cache.evict(30, 20, 20)
+        assert _state(cache) == before and torch.equal(cache.weights, weights)
+    with pytest.raises(RuntimeError):        # no memory for the outputs: nothing of the library was called yet
+        monkeypatch.setattr(KC.torch, "zeros", lambda *a, **k: (_ for _ in ()).throw(RuntimeError("out of memory")))
+        cache.evict(30, 2, 2)
+    assert _state(cache) == before
+
+
+def test_an_eviction_moves_to_fresh_pages_and_frees_the_old_ones(make, monkeypatch):
+    calls = []
+    monkeypatch.setattr(B, "mq_kv_evict", lambda *a, **k: calls.append(a))
+    cache = make(2, 10, 64, 2, 64, page_size=16)
+    cache.track_weights()
+    cache.extend([40, 20])
+    old = [list(p) for p in cache.pages]
+    cache.evict(24, 2, 2)
+    assert cache.lengths == [24, 20] and cache.tokens == [40, 20] and len(calls) == 1
+    assert [len(p) for p in cache.pages] == [2, 2] and not set(sum(cache.pages, [])) & set(sum(old, []))
+    assert sorted(cache.free + sum(cache.pages, [])) == list(range(10))
+    for b in range(2):
+        assert cache.table[b, :2].tolist() == cache.pages[b] and bool((cache.table[b, 2:] == -1).all())
