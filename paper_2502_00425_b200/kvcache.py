@@ -49,6 +49,7 @@ class PagedKVCache:
         self.weights: Optional[torch.Tensor] = None   # accumulated softmax weights, once track_weights() was called
         self.weights_status = torch.zeros(2, dtype=torch.int32, device=device)   # of every mq_kv_weights call
         self._ws = {}
+        self._last: Optional[CacheStep] = None        # the step that undo() can take back
 
     def _take(self, n: int) -> List[int]:
         if n > len(self.free):
@@ -58,9 +59,9 @@ class PagedKVCache:
     def _give_back(self, pages: Sequence[int]):
         self.free += list(pages)[::-1]
 
-    def _show(self, b: int):
+    def _show(self, b: int, pages: Sequence[int]):
         row = torch.full((self.table.shape[1],), -1, dtype=torch.int32)
-        row[:len(self.pages[b])] = torch.tensor(self.pages[b], dtype=torch.int32)
+        row[:len(pages)] = torch.tensor(pages, dtype=torch.int32)
         self.table[b].copy_(row)
 
     def track_weights(self):
@@ -69,26 +70,48 @@ class PagedKVCache:
         self.weights = torch.zeros((self.n_seq, self.handle.n_kv_heads, self.max_len), device=self.device)
 
     def extend(self, new: Sequence[int]) -> CacheStep:
-        """Room for new[b] tokens at the end of every sequence b, and the arrays of the step that brings them."""
+        """Room for new[b] tokens at the end of every sequence b, and the arrays of the step that brings them.  Where it raises,
+        the cache is as it was."""
         assert len(new) == self.n_seq and min(new) >= 0
         ps, slots, pos, cu = self.page_size, [], [], [0]
         for b, n in enumerate(new):
             if self.lengths[b] + n > self.max_len:
                 raise RuntimeError(f"sequence {b} would have {self.lengths[b] + n} keys, the cache was made for {self.max_len}")
         need = [max(0, -(-(self.lengths[b] + n) // ps) - len(self.pages[b])) for b, n in enumerate(new)]
-        fresh = self._take(sum(need))
-        for b, n in enumerate(new):
-            if need[b]:
-                self.pages[b] += [fresh.pop() for _ in range(need[b])]
-                self._show(b)
-            slots += [self.pages[b][j // ps] * ps + j % ps for j in range(self.lengths[b], self.lengths[b] + n)]
-            pos += range(self.tokens[b], self.tokens[b] + n)
-            self.lengths[b] += n
-            self.tokens[b] += n
-            cu.append(cu[-1] + n)
-        dev = lambda v, t: torch.tensor(v, dtype=t).to(self.device)
-        return CacheStep(list(new), dev(cu, torch.int32), dev(self.lengths, torch.int32), dev(slots, torch.int64),
-                         dev(pos, torch.int32), cu[-1], max(new))
+        taken = self._take(sum(need))
+        try:
+            fresh, pages = list(taken), []
+            lengths, tokens = [m + n for m, n in zip(self.lengths, new)], [m + n for m, n in zip(self.tokens, new)]
+            for b, n in enumerate(new):
+                pages.append(self.pages[b] + [fresh.pop() for _ in range(need[b])])
+                slots += [pages[b][j // ps] * ps + j % ps for j in range(self.lengths[b], lengths[b])]
+                pos += range(self.tokens[b], tokens[b])
+                cu.append(cu[-1] + n)
+            dev = lambda v, t: torch.tensor(v, dtype=t).to(self.device)
+            step = CacheStep(list(new), dev(cu, torch.int32), dev(lengths, torch.int32), dev(slots, torch.int64),
+                             dev(pos, torch.int32), cu[-1], max(new))
+            for b in range(self.n_seq):
+                if need[b]:
+                    self._show(b, pages[b])   # (entries behind a sequence's last key are not read)
+        except BaseException:
+            self._give_back(taken)
+            raise
+        self.pages, self.lengths, self.tokens, self._last = pages, lengths, tokens, step
+        return step
+
+    def undo(self, step: CacheStep):
+        """Takes back the last extend(), for a step that could not be finished: its keys no longer count and its pages are free
+        again.  Only the last step can be undone, and not behind an eviction.  (What attend() added to the tracked weights of
+        earlier keys stays.)"""
+        if step is not self._last:
+            raise RuntimeError("only the last step can be undone")
+        self._last = None
+        for b in range(self.n_seq):
+            self.lengths[b] -= step.new[b]
+            self.tokens[b] -= step.new[b]
+            keep = -(-self.lengths[b] // self.page_size)
+            self.free += self.pages[b][keep:]
+            del self.pages[b][keep:]
 
     def workspace(self, step: CacheStep, n_q_heads: int) -> torch.Tensor:
         """A workspace for the step, from a few sizes (powers of two) that are kept as long as the cache: a captured graph may
@@ -107,14 +130,25 @@ class PagedKVCache:
     def attend(self, q: torch.Tensor, step: CacheStep, n_q_heads: int, perm: Optional[torch.Tensor] = None,
                scale: Optional[float] = None) -> torch.Tensor:
         """Attention of the step's rows over the cache (their keys and values are already stored); adds to the tracked weights."""
+        o, lse = self.attention(q, step, n_q_heads, perm, scale)
+        self.accumulate(q, lse, step, n_q_heads, perm, scale)
+        return o
+
+    def attention(self, q: torch.Tensor, step: CacheStep, n_q_heads: int, perm: Optional[torch.Tensor] = None,
+                  scale: Optional[float] = None):
+        """The attention alone: its result and the log-sum-exps."""
         o = torch.empty_like(q)
         lse = torch.empty((step.total, n_q_heads), device=q.device)
         B.mq_kv_attention(q, step.cu_q, step.kv_len, self.table, self.handle, n_q_heads, step.max_q, o, self.workspace(step, n_q_heads),
                           lse=lse, perm=perm, scale=scale)
+        return o, lse
+
+    def accumulate(self, q: torch.Tensor, lse: torch.Tensor, step: CacheStep, n_q_heads: int, perm: Optional[torch.Tensor] = None,
+                   scale: Optional[float] = None):
+        """Adds to the tracked weights, if there are any, what the step's rows gave (with attention()'s arguments)."""
         if self.weights is not None:
             B.mq_kv_weights(q, step.cu_q, step.kv_len, self.table, self.handle, n_q_heads, step.max_q, lse, self.weights,
                             w_in=self.weights, perm=perm, scale=scale, status=self.weights_status)
-        return o
 
     def evict(self, budget: int, n_first: int, n_last: int) -> torch.Tensor:
         """Cuts every sequence to `budget` keys per head by the tracked weights; returns the kept indices (as mq_kv_evict's
@@ -146,7 +180,8 @@ class PagedKVCache:
         for b in range(self.n_seq):
             self.free += self.pages[b]
             self.pages[b], self.lengths[b] = fresh[b], after[b]
-            self._show(b)
+            self._show(b, fresh[b])
+        self._last = None
         return kept
 
     def status_ok(self) -> bool:

@@ -314,13 +314,20 @@ class W4A8DecoderBlock:
         bf16 [n_b, hidden] and, where a chunk has visual tokens, uint8 [n_b] (None: text only, no reordering).  Queries and
         keys are normed (g_q, g_k, if set) and rotated at their positions behind what the cache holds, keys and values
         are stored, and the rows attend the cached context and, causally in the original order, their chunk.  Returns
-        (outputs in the original order, BlockTrace)."""
-        sh, tr = self.shape, BlockTrace()
-        t = tr.tensors
+        (outputs in the original order, BlockTrace).  Where it raises, the cache holds what it held before."""
         live = [b for b, e in enumerate(embs) if e.shape[0]]
         if not live:
-            return list(embs), tr
+            return list(embs), BlockTrace()
         step = cache.extend([e.shape[0] for e in embs])
+        try:
+            return self._cached_step(embs, cache, step, live, is_visuals, calibrate)
+        except BaseException:
+            cache.undo(step)
+            raise
+
+    def _cached_step(self, embs, cache, step, live, is_visuals, calibrate: bool):
+        sh, tr = self.shape, BlockTrace()
+        t = tr.tensors
         perm = None
         if is_visuals is None:
             x0 = torch.cat([embs[b] for b in live])
@@ -339,7 +346,8 @@ class W4A8DecoderBlock:
         B.mq_qk_norm_rope(q, k, pos, sh.n_q_heads, sh.n_kv_heads, qr, gain_q=self.g_q, gain_k=self.g_k, v=v, cache=cache.handle,
                           slots=step.slots)
         t["q_rope"] = qr
-        x2 = self._behind_attention(x0, cache.attend(qr, step, sh.n_q_heads, perm), tr, calibrate)
+        a, lse = cache.attention(qr, step, sh.n_q_heads, perm)
+        x2 = self._behind_attention(x0, a, tr, calibrate)
         outs, at = [], 0
         for b, n in enumerate(step.new):
             rows = x2[at:at + n]
@@ -349,6 +357,7 @@ class W4A8DecoderBlock:
                 rows = out
             outs.append(rows)
             at += n
+        cache.accumulate(qr, lse, step, sh.n_q_heads, perm)   # (last: it cannot be taken back)
         return outs, tr
 
     # ---- glue: the library's single-pass kernels, or the torch expressions -------------------------

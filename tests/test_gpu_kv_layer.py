@@ -208,3 +208,33 @@ def test_workspaces_of_a_cache_stay_few_and_are_made_before_a_capture():
     g.replay()
     torch.cuda.synchronize()
     assert torch.equal(o, new.attend(rows, step, 8)) and new.status_ok()
+
+
+@pytest.mark.parametrize("images", [False, True])
+def test_a_step_that_fails_leaves_the_cache_as_it_was(images, monkeypatch):
+    """An error behind the attention, and one in it: the same call made again gives what it gives without the failures."""
+    blk = _block(9)
+    vis = (lambda *ns: [torch.tensor([0] + [1] * (n - 1), dtype=torch.uint8, device=DEV) for n in ns]) if images else (lambda *ns: None)
+    steps = [([_emb(70, 1), _emb(24, 2)], vis(70, 24)), ([_emb(20, 3), _emb(9, 4)], vis(20, 9)), ([_emb(1, 5), _emb(1, 6)], vis(1, 1))]
+    blk.forward_cached(*steps[0][:1], KC.PagedKVCache(2, 30, 200, 2, 128, 16), steps[0][1], calibrate=True)
+    got = []
+    for fail in (False, True):
+        cache = KC.PagedKVCache(2, 30, 200, 2, 128, 16)
+        cache.track_weights()
+        outs = []
+        for embs, v in steps:
+            if fail:
+                before = (list(cache.free), [list(p) for p in cache.pages], list(cache.lengths), list(cache.tokens), cache.weights.clone())
+                for where, name in ((blk, "_behind_attention"), (LY.B, "mq_kv_attention"), (LY.B, "mq_qk_norm_rope"), (LY.B, "mq_kv_weights")):
+                    with monkeypatch.context() as m:
+                        def fails(*a, **k):
+                            raise RuntimeError("out of memory")
+                        m.setattr(where, name, fails)
+                        with pytest.raises(RuntimeError, match="out of memory"):
+                            blk.forward_cached(embs, cache, v)
+                    assert before[:4] == (cache.free, cache.pages, cache.lengths, cache.tokens) and torch.equal(cache.weights, before[4])
+            outs += blk.forward_cached(embs, cache, v)[0]
+        got.append((outs, cache))
+    (a, ca), (b, cb) = got
+    assert all(torch.equal(x, y) for x, y in zip(a, b)) and ca.pages == cb.pages and ca.lengths == cb.lengths
+    assert torch.equal(ca.weights, cb.weights) and bool((ca.weights > 0).any()) and ca.status_ok() and cb.status_ok()

@@ -55,3 +55,60 @@ def test_an_eviction_moves_to_fresh_pages_and_frees_the_old_ones(make, monkeypat
     assert sorted(cache.free + sum(cache.pages, [])) == list(range(10))
     for b in range(2):
         assert cache.table[b, :2].tolist() == cache.pages[b] and bool((cache.table[b, 2:] == -1).all())
+
+
+def test_an_extension_that_fails_changes_nothing(make, monkeypatch):
+    cache = make(2, 12, 100, 2, 64, page_size=16)
+    cache.extend([40, 20])
+    before = _state(cache)
+    for name, at in (("tensor", 1), ("tensor", 3), ("tensor", 5), ("full", 1), ("full", 2)):
+        real, count = getattr(torch, name), [0]
+
+        def fails(*args, **kw):
+            count[0] += 1
+            if count[0] == at:
+                raise RuntimeError("out of memory")
+            return real(*args, **kw)
+
+        with monkeypatch.context() as m:
+            m.setattr(KC.torch, name, fails)
+            with pytest.raises(RuntimeError, match="out of memory"):
+                cache.extend([30, 30])
+        assert _state(cache) == before
+    step = cache.extend([30, 30])
+    assert cache.lengths == [70, 50] and step.kv_len.tolist() == [70, 50] and step.total == 60
+
+
+def test_a_step_is_undone(make):
+    cache = make(3, 12, 100, 2, 64, page_size=16)
+    first = cache.extend([40, 16, 0])
+    before = _state(cache)
+    for new in ([1, 1, 1], [30, 0, 17], [8, 8, 8], [0, 0, 1]):
+        step = cache.extend(new)
+        arrays = [step.cu_q, step.kv_len, step.slots, step.pos]
+        cache.undo(step)
+        assert _state(cache) == before
+        again = cache.extend(new)            # the same pages and positions
+        assert all(torch.equal(a, b) for a, b in zip(arrays, [again.cu_q, again.kv_len, again.slots, again.pos]))
+        for b in range(3):
+            n = len(cache.pages[b])
+            assert cache.table[b, :n].tolist() == cache.pages[b]
+        with pytest.raises(RuntimeError):
+            cache.undo(step)                 # not the last one
+        cache.undo(again)
+        with pytest.raises(RuntimeError):
+            cache.undo(again)
+    with pytest.raises(RuntimeError):
+        cache.undo(first)
+    assert _state(cache) == before
+
+
+def test_a_step_is_not_undone_behind_an_eviction(make, monkeypatch):
+    monkeypatch.setattr(B, "mq_kv_evict", lambda *a, **k: None)
+    cache = make(1, 10, 64, 2, 64, page_size=16)
+    cache.track_weights()
+    step = cache.extend([40])
+    cache.evict(40, 0, 0)
+    with pytest.raises(RuntimeError):
+        cache.undo(step)
+    assert cache.lengths == [40]
