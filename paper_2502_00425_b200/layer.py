@@ -311,7 +311,8 @@ class W4A8DecoderBlock:
 
     def forward_cached(self, embs, cache, is_visuals=None, calibrate: bool = False):
         """New tokens of every sequence of a PagedKVCache (one each, a few, or a chunk; empty ones are allowed): lists of
-        bf16 [n_b, hidden] and, where a chunk has visual tokens, uint8 [n_b] (None: text only, no reordering).  Queries and
+        bf16 [n_b, hidden] and, where a chunk has visual tokens, uint8 [n_b] (None for a chunk of text, or for all of them: no
+        reordering then).  Queries and
         keys are normed (g_q, g_k, if set) and rotated at their positions behind what the cache holds, keys and values
         are stored, and the rows attend the cached context and, causally in the original order, their chunk.  Returns
         (outputs in the original order, BlockTrace).  Where it raises, the cache holds what it held before."""
@@ -334,7 +335,8 @@ class W4A8DecoderBlock:
             tr.seg = B.Segments(torch.empty(0, dtype=torch.int32, device=x0.device), torch.empty(0, dtype=torch.uint8, device=x0.device))
             pos = step.pos
         else:
-            x0 = self.aifs([embs[b] for b in live], [is_visuals[b] for b in live], tr)
+            text = lambda e: torch.zeros(e.shape[0], dtype=torch.uint8, device=e.device)
+            x0 = self.aifs([embs[b] for b in live], [text(embs[b]) if is_visuals[b] is None else is_visuals[b] for b in live], tr)
             perm = torch.cat(tr.perms)
             # positions of the rows where they stand now; the cache holds a chunk's keys in the same order
             starts = torch.cat([torch.full_like(p, step.cu_q_host(b)) for b, p in zip(live, tr.perms)])

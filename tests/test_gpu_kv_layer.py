@@ -238,3 +238,19 @@ def test_a_step_that_fails_leaves_the_cache_as_it_was(images, monkeypatch):
     (a, ca), (b, cb) = got
     assert all(torch.equal(x, y) for x, y in zip(a, b)) and ca.pages == cb.pages and ca.lengths == cb.lengths
     assert torch.equal(ca.weights, cb.weights) and bool((ca.weights > 0).any()) and ca.status_ok() and cb.status_ok()
+
+
+def test_turns_of_text_beside_turns_with_images():
+    """None in place of a chunk's modalities: text only, as zeros say."""
+    blk = _block(5)
+    embs = [_emb(40, 1), _emb(24, 2), _emb(1, 3)]
+    vis = torch.tensor([0] * 3 + [1] * 30 + [0] * 7, dtype=torch.uint8, device=DEV)
+    blk.forward_cached(embs, KC.PagedKVCache(3, 20, 100, 2, 128, 16), [vis] + [torch.zeros(e.shape[0], dtype=torch.uint8, device=DEV) for e in embs[1:]],
+                       calibrate=True)
+    got = []
+    for text in (None, torch.zeros):
+        is_vis = [vis] + [None if text is None else text(e.shape[0], dtype=torch.uint8, device=DEV) for e in embs[1:]]
+        cache = KC.PagedKVCache(3, 20, 100, 2, 128, 16)
+        got.append((blk.forward_cached(embs, cache, is_vis)[0], cache.K.clone(), cache.V.clone()))
+        assert cache.status_ok()
+    assert all(torch.equal(a, b) for a, b in zip(got[0][0], got[1][0])) and torch.equal(got[0][1], got[1][1]) and torch.equal(got[0][2], got[1][2])
