@@ -40,7 +40,8 @@ class PagedKVCache:
         shape = (n_pages, n_kv_heads, page_size, head_dim)
         self.K, self.V = (torch.zeros(shape, dtype=dtype, device=device) for _ in range(2))
         self.handle = B.KVCache(self.K, self.V, k_scale, v_scale)
-        self.n_seq, self.max_len, self.page_size, self.device = n_seq, max_len, page_size, device
+        self.n_seq, self.max_len, self.page_size = n_seq, max_len, page_size
+        device = self.device = self.K.device      # (with its number: "cuda" would follow the current device)
         self.free = list(range(n_pages))[::-1]
         self.pages: List[List[int]] = [[] for _ in range(n_seq)]
         self.lengths = [0] * n_seq       # keys in the cache
@@ -155,7 +156,7 @@ class PagedKVCache:
         `kept`; entries behind a sequence's new length are -1).  The kept rows move to fresh pages, the old ones are freed."""
         if self.weights is None:
             raise RuntimeError("track_weights() first")
-        if B.mq_last_device_status(self.weights_status)[0] != B.MQ_OK:   # (keys would be dropped for good by them)
+        if not self._ok(self.weights_status):   # (keys would be dropped for good by them)
             raise RuntimeError("the accumulated weights are not whole: a call that added to them has failed")
         ps = self.page_size
         after = [min(n, budget) for n in self.lengths]
@@ -186,4 +187,9 @@ class PagedKVCache:
 
     def status_ok(self) -> bool:
         """Whether every attention and every accumulation of weights so far went through (waits for the current stream)."""
-        return all(B.mq_last_device_status(s)[0] == B.MQ_OK for s in [*self._ws.values(), self.weights_status])
+        return all(self._ok(s) for s in [*self._ws.values(), self.weights_status])
+
+    @staticmethod
+    def _ok(status: torch.Tensor) -> bool:
+        with torch.cuda.device_of(status):      # (in the order of the calls, which run on its device's stream)
+            return B.mq_last_device_status(status)[0] == B.MQ_OK

@@ -112,3 +112,24 @@ def test_a_step_is_not_undone_behind_an_eviction(make, monkeypatch):
     with pytest.raises(RuntimeError):
         cache.undo(step)
     assert cache.lengths == [40]
+
+
+def test_a_cache_stays_on_the_device_it_was_made_on(make, monkeypatch):
+    """Not on whichever is current when a step's arrays are made, or when its status is read."""
+    cache = make(1, 10, 64, 2, 64, page_size=16)
+    assert cache.device == cache.K.device == cache.table.device and isinstance(cache.device, torch.device)
+    seen = []
+
+    class Current:
+        def __init__(self, tensor):
+            self.tensor = tensor
+
+        def __enter__(self):
+            seen.append(self.tensor)
+
+        def __exit__(self, *exc):
+            seen.append(None)
+
+    monkeypatch.setattr(KC.torch.cuda, "device_of", Current)
+    monkeypatch.setattr(B, "mq_last_device_status", lambda ws: (B.MQ_OK if seen and seen[-1] is ws else B.MQ_ERR_CUDA, 0))
+    assert cache.status_ok()
