@@ -527,7 +527,8 @@ def _addr(t: Optional[torch.Tensor]):
 # The cache calls are made once per layer and token, so their wrappers are written for few Python steps: one look at each
 # property of a tensor, the stream as a bare handle.
 _BF16, _F32, _I32, _I64 = torch.bfloat16, torch.float32, torch.int32, torch.int64
-_current_device, _raw_stream = torch.cuda.current_device, torch._C._cuda_getCurrentRawStream
+_current_device = torch.cuda.current_device
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # (a torch without CUDA has none; every tensor is refused there)
 
 
 def _elsewhere(t: torch.Tensor, device: int):

@@ -231,3 +231,13 @@ def test_attention_entry_point_validates(lib):
     assert call(q=A + 2) == B.MQ_ERR_ALIGNMENT
     assert call(ldq=516) == B.MQ_ERR_ALIGNMENT
     assert call(wsb=1024) == B.MQ_ERR_WORKSPACE
+
+
+def test_the_package_imports_on_a_torch_without_cuda():
+    """The bare stream handle is not part of a torch built without CUDA; the host-only parts have to import all the same."""
+    import subprocess
+    import sys
+    code = ("import torch; hasattr(torch._C, '_cuda_getCurrentRawStream') and delattr(torch._C, '_cuda_getCurrentRawStream'); "
+            "from paper_2502_00425_b200 import binding, build, kvcache, layer, synth; print(binding.MQ_OK)")
+    done = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True)
+    assert done.returncode == 0 and done.stdout.strip() == "0", done.stderr
