@@ -143,3 +143,37 @@ def test_far_offsets_of_a_large_pool():
     o = torch.empty((1, hkv * dim), dtype=torch.bfloat16, device=DEV)
     B.mq_kv_attention(x[1:] * 30, torch.tensor([0, 1], dtype=torch.int32, device=DEV), one, table, cache, hkv, 1, o, ws)
     assert torch.equal(o[0], x[1])
+
+
+@pytest.mark.parametrize("int8", [False, True])
+def test_far_rows_of_keys_and_of_values_are_told_apart(int8):
+    """K and V share one allocation at different offsets, their last pages behind 2^32 bytes, and hold different things."""
+    hkv, dim, page = 2, 128, 16
+    es = 1 if int8 else 2
+    rows = hkv * page * dim
+    stride = (1 << 21) // es                           # elements between pages: 2 MiB
+    n_pages = 2100                                     # the last page starts behind 4.4e9 bytes
+    dt = torch.int8 if int8 else torch.bfloat16
+    pool = torch.empty((n_pages - 1) * stride + 2 * rows, dtype=dt, device=DEV)
+    K, V = (pool.as_strided((n_pages, hkv, page, dim), (stride, page * dim, dim, 1), off) for off in (0, rows))
+    scales = [torch.full((hkv,), s, device=DEV) for s in (0.05, 0.03)] if int8 else [None, None]
+    slots = torch.tensor([3, (n_pages - 1) * page + 5, 2049 * page + 15], dtype=torch.int64, device=DEV)
+    for p in (0, 2049, n_pages - 1):
+        K[p], V[p] = 77, 78
+    g = torch.Generator().manual_seed(3)
+    k, v = (torch.randn((3, hkv * dim), generator=g).to(torch.bfloat16).to(DEV) for _ in range(2))
+    out = torch.empty_like(k)
+    B.mq_qk_norm_rope(k, k, torch.zeros(3, dtype=torch.int32, device=DEV), hkv, hkv, out, v=v, cache=B.KVCache(K, V, *scales), slots=slots)
+    torch.cuda.synchronize()                           # position 0: the rotation is the identity
+    for t, slot in enumerate(slots.tolist()):
+        for view, x, s in ((K, k, scales[0]), (V, v, scales[1])):
+            want = x[t].view(hkv, dim)
+            if int8:
+                inv = 1.0 / s.cpu()                    # the stored code: round_half_even(y * (1 / scale)), both in float32
+                want = (want.float().cpu() * inv[:, None]).round().clamp(-128, 127).to(torch.int8).to(DEV)
+            assert torch.equal(view[slot // page, :, slot % page], want)
+    for view, fill in ((K, 77), (V, 78)):
+        for p in (0, 2049, n_pages - 1):
+            mask = torch.ones(page, dtype=torch.bool, device=DEV)
+            mask[[s % page for s in slots.tolist() if s // page == p]] = False
+            assert bool((view[p][:, mask] == fill).all())
