@@ -84,7 +84,7 @@ class PagedKVCache:
             fresh, pages = list(taken), []
             lengths, tokens = [m + n for m, n in zip(self.lengths, new)], [m + n for m, n in zip(self.tokens, new)]
             for b, n in enumerate(new):
-                pages.append(self.pages[b] + [fresh.pop() for _ in range(need[b])])
+                pages.append(self.pages[b] + [fresh.pop() for _ in range(need[b])] if need[b] else self.pages[b])
                 slots += [pages[b][j // ps] * ps + j % ps for j in range(self.lengths[b], lengths[b])]
                 pos += range(self.tokens[b], tokens[b])
                 cu.append(cu[-1] + n)
