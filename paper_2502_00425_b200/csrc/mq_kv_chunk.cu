@@ -72,7 +72,7 @@ struct Piece {
   int t0, t1, end, ctx;
   int row0, n_rows;       // query rows of the unit
   int all_see;            // every row of the unit sees the keys below
-  int b, g, begin, n_all;
+  int b, g, begin;
   int whole;              // the piece is the whole unit
   int n_parts;            // of the unit, if this is its first piece
   int poison;             // values were taken out of its tiles
@@ -339,7 +339,6 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
         pc.b = u.b;
         pc.g = u.g;
         pc.begin = u.s.begin;
-        pc.n_all = u.s.n_all;
         pc.whole = pc.t0 == 0 && pc.t1 == u.tiles;
         if (pc.t0 == 0 && !pc.whole) {
           pc.n_parts = (int)((unit_at + sc.extra + u.tiles - 1) / share) - (int)blockIdx.x + 1;
