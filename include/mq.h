@@ -466,7 +466,7 @@ int mq_aifs_attention(const void* Q, int64_t ldq, const void* K, int64_t ldk, co
  * [page][head][slot][dim] and [page][slot][head][dim], are strides of this form.  Rows must start on 16-byte
  * boundaries (MQ_ERR_ALIGNMENT); rows of a cache that a call writes to may not overlap (MQ_ERR_INVALID_ARG).  head_dim 64 or 128, page_size a power of two from 16 to 256
  * (MQ_ERR_UNSUPPORTED).  Elements are bf16 or, with MQ_KV_INT8, int8 codes with one static scale per
- * key/value head and tensor (Eq. 2: value = code * scale), k_scale / v_scale device float32 [n_kv_heads].
+ * key/value head and tensor (Eq. 2: value = code * scale), k_scale / v_scale device float32 [n_kv_heads], finite.
  *
  * mq_kv_batch describes the new tokens: rows cu_q[b] .. cu_q[b + 1] - 1 of the query matrix belong to sequence b,
  * kv_len[b] counts its keys INCLUDING the new ones (they are already in the cache, at its end).  All four arrays are
@@ -510,7 +510,8 @@ typedef struct mq_kv_batch {
  * Q_out (may be Q) receives the query heads and K_out (may be K, or NULL) the key heads, rounded once to bf16.
  * With a cache, key and value row t go to slot slots[t] = page * page_size + slot of it: bf16, or
  * sat_int8(round_half_even(y * (1 / scale))) of the unrounded y and of V.  Rows whose slot is outside the cache
- * (padding: -1) are not stored.  Two rows with one slot leave either of them there.
+ * (padding: -1) are not stored.  Rows of one call want slots of their own: where two have the same one, its heads
+ * may hold pieces of either.
  *   Q [T, n_q_heads * head_dim], K, V [T, n_kv_heads * head_dim] (leading dimensions in elements, 16-byte rows)
  *   gain_q, gain_k  device float32 [head_dim] or NULL, 16-byte aligned;  pos device int32 [T]
  *   cache NULL: V and slots are ignored and K_out is required.  cache->head_dim / n_kv_heads must match.
@@ -554,7 +555,8 @@ int mq_kv_weights(const void* Q, int64_t ldq, const mq_kv_batch* batch, const mq
 
 /*
  * Eviction: cuts every sequence to at most `budget` keys per key/value head and copies them, in their order, to fresh
- * pages.  Of sequence b with n = kv_len[b] keys, a head keeps
+ * pages.  "First", "last" and "order" are those of the cache: where a chunk was stored in AIFS order, its visual tokens
+ * come first, whatever stood before them in the prompt.  Of sequence b with n = kv_len[b] keys, a head keeps
  *   all of them if n <= budget; else the first n_first and the last n_last keys and, of the others, the
  *   budget - n_first - n_last with the largest W[b, g, j] (of equal ones the lowest j; a NaN counts as lowest).
  *   kept     int32 [n_seq, n_kv_heads, budget]: the kept keys' indices, ascending; entries behind them are left as they were

@@ -1,5 +1,5 @@
 // Shared pieces of the key/value-cache kernels (mq_kv_*.cu): the device view of a paged cache, argument checks of
-// the two descriptors, and the few warp-level tensor-core instructions (mma.sync, ldmatrix, cp.async) that the
+// the two descriptors, and the few warp-level tensor-core instructions (mma.sync, ldmatrix, movmatrix) that the
 // kernels with few query rows use.
 #pragma once
 
@@ -122,7 +122,8 @@ __device__ __forceinline__ KvSeq kv_seq(const KvBatchView& v, int page_shift, in
 }
 
 // Division of 0 <= n < 2^31 by a divisor known on the host: n * m >> 31 + l with l = ceil(log2 d), m = ceil(2^(31 + l) / d)
-// (m < 2^32, and the quotient is exact for n < 2^31).  A runtime division is some 40 dependent instructions, which
+// (m < 2^32, and the quotient is exact for n < 2^31: Granlund and Montgomery, "Division by invariant integers using
+// multiplication", 1994).  A runtime division is some 40 dependent instructions, which
 // counts in kernels that last a few microseconds.
 struct FastDiv {
   uint32_t m;

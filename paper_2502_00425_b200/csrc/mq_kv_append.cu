@@ -8,8 +8,10 @@
 // its heads (they cost as much as two head rows), and the frequencies (doubles) are read once per thread.
 // The angle in turns, pos * theta / (2 pi), is formed and reduced in double: in float32 a position of 100,000 would
 // leave an angle error of 4e-3.
-// 9728 tokens of 32 + 8 heads of 128, 239 MB: 53 us, 4.5 TB/s (68 % of a plain copy); the instructions between the loads
-// and the stores are the bound (sums, conversions and rotation of 8 channels per lane).  32 tokens: 3.4 us.
+// 9728 tokens of 32 + 8 heads of 128, 239 MB: 53 us, 4.5 TB/s (68 % of a plain copy).  39 M warp instructions (sums, conversions,
+// rotation) are 35 us of issue by themselves, as long as the bytes take; issue is busy for 68 % of the cycles in which an SM
+// has work, the rest are fixed latencies and the shuffles' and conversions' results (7 warps to a scheduler), and 11 % of the
+// time an SM has none (start, last round).  Into an int8 cache: 6 us more.  32 tokens: 3.4 us.
 #include "mq_kv.cuh"
 
 namespace mq {
@@ -40,10 +42,10 @@ __global__ void __launch_bounds__(kWarps * 32, kU > 1 ? 4 : 2)
 qk_norm_rope_kernel(const __grid_constant__ AppendParams p) {
   constexpr int kLanes = kD / 8;        // lanes per head row
   constexpr int kRows = 32 / kLanes;    // head rows per step
-  // byte offsets of a lane's two runs of four channels
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int sub = lane % kLanes, sel = lane / kLanes;
+  // byte offsets of a lane's two runs of four channels
   const int off0 = kHalf ? sub * 8 : sub * 16, off1 = kHalf ? kD + sub * 8 : sub * 16 + 8;
   double turns[4];
 #pragma unroll

@@ -11,13 +11,16 @@
 //   * Both products are taken transposed, S^T = K Q^T and O^T = V^T P^T: the 16 keys, and 16 channels, are the rows of the
 //     instruction's tile and the query rows its 8 columns, so a group of up to 8 heads wastes nothing.  P^T changes from
 //     the layout of a result to that of an operand by an 8 x 8 transpose in registers.
-//   * The exponents are taken relative to the running maximum, the accumulator is rescaled only when a row's maximum moved.
+//   * The exponents are taken relative to the running maximum, the accumulator is rescaled only when a row's maximum moved.  The
+//     probabilities are rounded once, to the values' type, as operands of mma.sync have to be; the sums take them unrounded.
 //   * An int8 cache is read as codes and widened in registers to fp16 exactly (the products' sums do not care in which
 //     order the channels come, so a thread takes contiguous codes); the scales multiply the scores and the result.
 //     Queries are scaled by a power of two per row: fp16 then holds all bits of channels down to 2^-31 of the row's largest.
 // 64 sequences of 64 to 8192 keys, 8 key/value heads of 128, groups of 4: 78 us in bf16 (449 MB, 5.8 TB/s, 88 % of a plain
-// copy) and 50 us in int8 (225 MB, 4.5 TB/s; widening and the products' instructions hold it, not memory).  One sequence of
-// 3361 keys: 9 us, of which the two launches are half.
+// copy) and 50 us in int8 (225 MB, 4.5 TB/s).  There 446 warp instructions go with 16 keys, all counted; issue is busy for 54 %
+// of the cycles in which an SM has work (integer pipe 47 %), three warps to a scheduler wait most for the fixed latencies
+// of their own chains, and 13 % of the time an SM has no work (start, and ranges that end early).  Two blocks of 8 rows
+// spill 132 bytes in int8.  One sequence of 3361 keys: 9 us, of which the two launches are half.
 #include "mq_kv_warp.cuh"
 
 namespace mq {

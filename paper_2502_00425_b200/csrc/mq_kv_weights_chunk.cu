@@ -8,8 +8,9 @@
 // and adds exponentials; nothing is exchanged until the two groups of four warps, which take turns at the row tiles, add
 // their sums at the unit's end.  Four score buffers fill tensor memory.  Every key is written once, in one order of
 // summation.  Bound by the exponentials (128 x 128 of them cost the special-function pipe twice what the product costs
-// the tensor pipe): chunks of 900 and 1024 tokens over 9092 and 3024 keys, 32 / 8 heads of 128 (85 GFLOP): 162 us, 115 without the
-// exponentials, 99 for products and loads alone; 640 units over 148 CTAs are 5 for some and 4.3 on average.
+// the tensor pipe): chunks of 900 and 1024 tokens over 9092 and 3024 keys, 32 / 8 heads of 128 (85 GFLOP): 159 us, 115 without the
+// exponentials, 99 for products and loads alone; 640 units over 148 CTAs are 5 for some and 4.3 on average.  All forms
+// spill 24 to 28 bytes.
 // A persistent CTA per SM takes the units whose start lies in its share of the line of all row tiles.
 #include <cuda.h>
 

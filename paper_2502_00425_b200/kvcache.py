@@ -153,7 +153,9 @@ class PagedKVCache:
 
     def evict(self, budget: int, n_first: int, n_last: int) -> torch.Tensor:
         """Cuts every sequence to `budget` keys per head by the tracked weights; returns the kept indices (as mq_kv_evict's
-        `kept`; entries behind a sequence's new length are -1).  The kept rows move to fresh pages, the old ones are freed."""
+        `kept`; entries behind a sequence's new length are -1).  The kept rows move to fresh pages, the old ones are freed.  The
+        first n_first and last n_last keys are those of the cache: a chunk stored in AIFS order (forward_cached with images) has its
+        visual tokens in front, so n_first keeps these rather than the text that stood before them."""
         if self.weights is None:
             raise RuntimeError("track_weights() first")
         if not self._ok(self.weights_status):   # (keys would be dropped for good by them)
