@@ -542,7 +542,7 @@ int mq_kv_attention(const void* Q, int64_t ldq, const mq_kv_batch* batch, const 
  *   W_out[b, g, j] = (W_in[b, g, j] if key j was cached before this chunk, else 0)
  *                    + sum over the chunk's rows i that see j and the query heads h of g of exp(scale * Q[i, h] . K[j, g] - lse[i, h])
  * for j < kv_len[b]; other entries of W_out are left as they were (without rows, total_q = 0, W_in is copied).  lse is mq_kv_attention's output for the same
- * call.  W_in NULL counts as zeros; W_in == W_out accumulates in place.  float32 throughout, and every sum is
+ * call.  W_in NULL counts as zeros; W_in == W_out accumulates in place (else their rows share nothing).  float32 throughout, and every sum is
  * taken in a fixed order (no atomics).  w_seq_stride, w_head_stride: elements between sequences and heads, w_keys:
  * entries of a head's row (of both arrays); keys at or behind w_keys are neither read nor written.  Rows may not
  * overlap (MQ_ERR_INVALID_ARG).  status: optional
