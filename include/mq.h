@@ -523,6 +523,30 @@ int mq_qk_norm_rope(const void* Q, int64_t ldq, const void* K, int64_t ldk, cons
                     int64_t ldko, const mq_kv_cache* cache, const int64_t* slots, void* stream);
 
 /*
+ * The same pass for heads that rotate in part, and for rotary embeddings scaled for longer contexts than they were made for: of
+ * every query and key head the first rotary_dim channels rotate, in pairs (2i, 2i + 1), or (i, i + rotary_dim / 2) with MQ_ROPE_HALF,
+ * pair i by pos[t] * theta[i] radians (formed and reduced in double precision) and times amp; the channels behind them pass,
+ * normed where there is a gain.  Everything else as mq_qk_norm_rope, which is this with rotary_dim = head_dim,
+ * theta[i] = base^(-2i / head_dim) and amp = 1.
+ *   theta       HOST array of rotary_dim / 2 doubles, read during the call (a captured graph keeps what it held then); at most
+ *               1e6 in magnitude, finite.  Scalings by a factor f divide theta by f, for all pairs or, by parts, for those that
+ *               turn seldom within the original context.
+ *   rotary_dim  0 .. head_dim, a multiple of 8 (MQ_ERR_UNSUPPORTED)
+ *   amp         finite (the temperature that some scalings put on the embedding)
+ */
+typedef struct mq_rope {
+  const double* theta; /* host */
+  int32_t rotary_dim;
+  uint32_t flags; /* MQ_ROPE_HALF */
+  float amp;
+} mq_rope;
+int mq_qk_norm_rope_scaled(const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V, int64_t ldv, int32_t T,
+                           int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, const float* gain_q,
+                           const float* gain_k, float eps, const int32_t* pos, const mq_rope* rope, void* Q_out,
+                           int64_t ldqo, void* K_out, int64_t ldko, const mq_kv_cache* cache, const int64_t* slots,
+                           void* stream);
+
+/*
  * Attention of the new tokens over the paged cache:
  *   O[i, h] = sum_j P[i, j] V[j, g(h)],  P[i, :] = softmax over the keys j that row i sees of scale * Q[i, h] . K[j, g(h)],
  *   lse[i, h] = log of the softmax's denominator: log sum_j exp(scale * Q . K)     (optional, float32 [total_q, n_q_heads])

@@ -76,6 +76,33 @@ def norm_rope(x, gain, eps, pos, base, half):
     return y, mag
 
 
+def rope_theta(r, base, factor=1.0, original=0, fast=32.0, slow=1.0):
+    """Radians per position of the r / 2 pairs; with an original context, pairs between `slow` and `fast` turns in it are scaled in
+    proportion, those above stay."""
+    out = []
+    for i in range(r // 2):
+        t = base ** (-2.0 * i / r)
+        wavelength = 2 * np.pi / t
+        keep = 0.0 if not original else np.clip((original / wavelength - slow) / (fast - slow), 0.0, 1.0)
+        out.append(keep * t + (1 - keep) * t / factor)
+    return np.array(out)
+
+
+def norm_rope_scaled(x, gain, eps, pos, theta, half, amp):
+    """norm_rope of the first 2 len(theta) channels with given frequencies, times amp; the others are normed only."""
+    x = np.asarray(x, np.float64)
+    if gain is not None:
+        x = x / np.sqrt((x ** 2).mean(-1, keepdims=True) + eps) * np.asarray(gain, np.float64)
+    r = 2 * len(theta)
+    y, mag = x.copy(), np.abs(x)
+    for i, t in enumerate(theta):
+        a, b = (i, i + r // 2) if half else (2 * i, 2 * i + 1)
+        z = (x[..., a] + 1j * x[..., b]) * (amp * np.exp(1j * np.asarray(pos, np.float64) * t))[:, None]
+        y[..., a], y[..., b] = z.real, z.imag
+        mag[..., a] = mag[..., b] = abs(amp) * (np.abs(x[..., a]) + np.abs(x[..., b]))
+    return y, mag
+
+
 def keep(w, n, budget, n_first, n_last):
     """Indices (ascending) of the keys one head keeps of its n keys with weights w [n]."""
     if n <= budget:

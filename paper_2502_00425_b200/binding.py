@@ -8,6 +8,7 @@ tensor is not on a CUDA device the call raises.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 from typing import Optional
 
@@ -60,6 +61,10 @@ class mq_kv_batch(C.Structure):
                 ("cu_q", C.c_void_p), ("kv_len", C.c_void_p), ("page_table", C.c_void_p), ("perm", C.c_void_p)]
 
 
+class mq_rope(C.Structure):
+    _fields_ = [("theta", C.POINTER(C.c_double)), ("rotary_dim", C.c_int32), ("flags", C.c_uint32), ("amp", C.c_float)]
+
+
 def lib_path() -> str:
     return os.path.join(os.path.dirname(os.path.abspath(__file__)), _LIB_NAME)
 
@@ -100,6 +105,8 @@ def load(build_if_missing: bool = False):
         "mq_aifs_attention": (C.c_int, [vp, i64, vp, i64, vp, i64, vp, vp, i32, i32, i32, i32, vp, i64, vp, sz, vp, vp]),
         "mq_qk_norm_rope": (C.c_int, [vp, i64, vp, i64, vp, i64, i32, i32, i32, i32, vp, vp, f32, vp, f32, C.c_uint32, vp, i64,
                                       vp, i64, kvcp, vp, vp]),
+        "mq_qk_norm_rope_scaled": (C.c_int, [vp, i64, vp, i64, vp, i64, i32, i32, i32, i32, vp, vp, f32, vp, C.POINTER(mq_rope), vp, i64,
+                                             vp, i64, kvcp, vp, vp]),
         "mq_kv_attention_workspace_bytes": (sz, [kvbp, kvcp, i32]),
         "mq_kv_attention": (C.c_int, [vp, i64, kvbp, kvcp, i32, f32, vp, i64, vp, vp, sz, vp]),
         "mq_kv_weights": (C.c_int, [vp, i64, kvbp, kvcp, i32, f32, vp, vp, vp, i64, i64, i32, vp, vp]),
@@ -142,7 +149,7 @@ EXPORTED = ["mq_version", "mq_status_string", "mq_workspace_bytes", "mq_w4_layou
             "mq_ubench_mma_i8", "mq_selftest_bounded_wait", "mq_ubench_expand", "mq_calibrate_static_scales_bits",
             "mq_w8_layout_bytes", "mq_pack_w8", "mq_fwht_quant_bits", "mq_kron_quant_i8", "mq_glue_rmsnorm", "mq_glue_rope",
             "mq_glue_swiglu", "mq_glue_residual_add", "mq_aifs_attention_workspace_bytes", "mq_aifs_attention",
-            "mq_qk_norm_rope", "mq_kv_attention_workspace_bytes", "mq_kv_attention", "mq_kv_weights", "mq_kv_evict"]
+            "mq_qk_norm_rope", "mq_qk_norm_rope_scaled", "mq_kv_attention_workspace_bytes", "mq_kv_attention", "mq_kv_weights", "mq_kv_evict"]
 
 
 def status_string(status: int) -> str:
@@ -577,10 +584,40 @@ def _kv_batch(cu_q, kv_len, page_table, total_q, max_q, perm, device):
                        _vec(page_table, _I32, n_seq * width, device), _vec(perm, _I32, total_q, device))
 
 
+class Rope:
+    """A rotary embedding of the first rotary_dim channels of every head (mq_rope), made once and used for every call.
+
+    theta: radians per position of each of the rotary_dim / 2 pairs; if not given, base^(-2i / rotary_dim), scaled for contexts
+    `factor` times as long: all pairs alike, or, with the length of the `original` context, by parts (Peng et al., "YaRN: Efficient
+    Context Window Extension of Large Language Models", 2023): pairs that make more than `fast` turns in it stay, those with fewer than `slow` are divided by the
+    factor, between them in proportion.  amp multiplies sine and cosine (that method takes 0.1 ln(factor) + 1)."""
+
+    def __init__(self, rotary_dim: int, base: float = 10000.0, half: bool = False, factor: float = 1.0, original: int = 0, fast: float = 32.0,
+                 slow: float = 1.0, amp: float = 1.0, theta=None):
+        if rotary_dim < 0 or rotary_dim % 2:
+            raise ValueError("rotary_dim is even and not negative")
+        if theta is None:
+            if not (base > 1.0 and factor > 0.0 and original >= 0 and (not original or fast > slow)):
+                raise ValueError("base > 1, factor > 0, original >= 0 and fast > slow are wanted")
+            theta = [base ** (-2.0 * i / rotary_dim) for i in range(rotary_dim // 2)]
+            if not original:
+                theta = [t / factor for t in theta]
+            elif factor != 1.0:
+                ramp = [min(1.0, max(0.0, (original * t / (2 * math.pi) - slow) / (fast - slow))) for t in theta]
+                theta = [t * (r + (1.0 - r) / factor) for t, r in zip(theta, ramp)]
+        theta = [float(t) for t in theta]
+        if len(theta) != rotary_dim // 2:
+            raise ValueError(f"theta has {len(theta)} entries, {rotary_dim // 2} are wanted")
+        self.theta, self.rotary_dim, self.half, self.amp = theta, rotary_dim, bool(half), float(amp)
+        self._array = (C.c_double * max(1, len(theta)))(*theta)
+        self.c = mq_rope(C.cast(self._array, C.POINTER(C.c_double)), rotary_dim, MQ_ROPE_HALF if half else 0, amp)
+        self.ref = C.byref(self.c)
+
+
 def mq_qk_norm_rope(q, k, pos, n_q_heads, n_kv_heads, q_out, k_out=None, gain_q=None, gain_k=None, eps=1e-6, base=10000.0,
-                    half=False, v=None, cache: Optional[KVCache] = None, slots=None):
+                    half=False, v=None, cache: Optional[KVCache] = None, slots=None, rope: Optional[Rope] = None):
     """Per-head RMSNorm (where a gain is given), rotary embedding, and the store of K and V into `cache` at `slots`
-    (int64 [T], page * page_size + slot; negative: not stored).  See include/mq.h."""
+    (int64 [T], page * page_size + slot; negative: not stored).  With `rope`, base and half are its own.  See include/mq.h."""
     shape = q.shape
     T, width = shape
     dim = width // n_q_heads
@@ -599,9 +636,19 @@ def mq_qk_norm_rope(q, k, pos, n_q_heads, n_kv_heads, q_out, k_out=None, gain_q=
             raise ValueError(f"the cache is on cuda:{cache.index}, q on {q.device}")
         pv, ldv = _rows(v, kv, d)
         pc, ps = cache.ref, _vec(slots, _I64, T, d)
-    _kv_call(d, load().mq_qk_norm_rope, "mq_qk_norm_rope", pq, ldq, pk, ldk, pv, ldv, T, n_q_heads, n_kv_heads, dim,
-             _vec(gain_q, _F32, dim, d), _vec(gain_k, _F32, dim, d), eps, _vec(pos, _I32, T, d), base, MQ_ROPE_HALF if half else 0,
-             po, ldo, pko, ldko, pc, ps)
+    if rope is None:
+        _kv_call(d, load().mq_qk_norm_rope, "mq_qk_norm_rope", pq, ldq, pk, ldk, pv, ldv, T, n_q_heads, n_kv_heads, dim,
+                 _vec(gain_q, _F32, dim, d), _vec(gain_k, _F32, dim, d), eps, _vec(pos, _I32, T, d), base, MQ_ROPE_HALF if half else 0,
+                 po, ldo, pko, ldko, pc, ps)
+    else:
+        _kv_call(d, load().mq_qk_norm_rope_scaled, "mq_qk_norm_rope_scaled", pq, ldq, pk, ldk, pv, ldv, T, n_q_heads, n_kv_heads, dim,
+                 _vec(gain_q, _F32, dim, d), _vec(gain_k, _F32, dim, d), eps, _vec(pos, _I32, T, d), rope.ref, po, ldo, pko, ldko, pc, ps)
+
+
+def mq_qk_norm_rope_scaled(q, k, pos, n_q_heads, n_kv_heads, q_out, rope: Rope, k_out=None, gain_q=None, gain_k=None, eps=1e-6, v=None,
+                           cache: Optional[KVCache] = None, slots=None):
+    """mq_qk_norm_rope with a rotary embedding of a part of the head, or scaled for a longer context.  See include/mq.h."""
+    mq_qk_norm_rope(q, k, pos, n_q_heads, n_kv_heads, q_out, k_out, gain_q, gain_k, eps, v=v, cache=cache, slots=slots, rope=rope)
 
 
 def mq_kv_attention_workspace_bytes(n_seq, total_q, max_q, max_pages, n_q_heads, cache: KVCache) -> int:

@@ -1,5 +1,6 @@
 // Norm of every query and key head, rotary embedding and the store into the paged cache, in one pass:
-//   n = x / sqrt(mean(x^2) + eps) * gain;   y = n rotated by pos * base^(-2i / D);   Q_out, K_out, cache <- y, V
+//   n = x / sqrt(mean(x^2) + eps) * gain;   y = n rotated by pos * theta_i;   Q_out, K_out, cache <- y, V
+// theta_i = base^(-2i / D) over the whole head, or given frequencies over its first channels (mq_qk_norm_rope_scaled).
 // The pass is bound by its bytes (each of q, k, v read once and written once).  A head row of D channels is held by
 // D / 8 lanes, so the sum of squares is a shuffle over those lanes and a row never leaves registers; a lane's 8 channels
 // are four pairs: 16 contiguous bytes, or for pairs (i, i + D/2) two runs of 8 bytes, so that no pair crosses lanes.
@@ -11,7 +12,8 @@
 // 9728 tokens of 32 + 8 heads of 128, 239 MB: 53 us, 4.5 TB/s (68 % of a plain copy).  39 M warp instructions (sums, conversions,
 // rotation) are 35 us of issue by themselves, as long as the bytes take; issue is busy for 68 % of the cycles in which an SM
 // has work, the rest are fixed latencies and the shuffles' and conversions' results (7 warps to a scheduler), and 11 % of the
-// time an SM has none (start, last round).  Into an int8 cache: 6 us more.  32 tokens: 3.4 us.
+// time an SM has none (start, last round).  Into an int8 cache: 6 us more.  32 tokens: 3.4 us.  Half of the head rotated, in pairs
+// (i, i + 32): 60 us call to call where the whole head takes 55; the lanes of what passes read two neighbouring runs.
 #include "mq_kv.cuh"
 
 namespace mq {
@@ -31,6 +33,8 @@ struct AppendParams {
   const int64_t* slots;
   int has_cache;
   KvView c;
+  int rot_pairs;             // pairs of a head that rotate, a multiple of 4; the channels behind them pass
+  float amp;                 // of the rotated pairs
   double turns[64];          // theta_i / (2 pi)
 };
 
@@ -45,8 +49,12 @@ qk_norm_rope_kernel(const __grid_constant__ AppendParams p) {
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int sub = lane % kLanes, sel = lane / kLanes;
-  // byte offsets of a lane's two runs of four channels
-  const int off0 = kHalf ? sub * 8 : sub * 16, off1 = kHalf ? kD + sub * 8 : sub * 16 + 8;
+  // byte offsets of a lane's two runs of four channels.  Pairs (i, i + R/2) of the first R channels: the first R/8 lanes hold the runs
+  // that belong together, the others two neighbouring runs of what passes.
+  const int pair_lanes = p.rot_pairs >> 2;
+  const bool rotates = sub < pair_lanes;
+  const int off0 = !kHalf ? sub * 16 : rotates ? sub * 8 : pair_lanes * 16 + (sub - pair_lanes) * 16;
+  const int off1 = kHalf && rotates ? (sub + pair_lanes) * 8 : off0 + 8;
   double turns[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) turns[e] = p.turns[4 * sub + e];
@@ -86,6 +94,8 @@ qk_norm_rope_kernel(const __grid_constant__ AppendParams p) {
         for (int e = 0; e < 4; ++e) {
           const double rev = pos * turns[e];
           sincospif(2.0f * (float)(rev - rint(rev)), &sn[e], &cs[e]);
+          sn[e] *= p.amp;
+          cs[e] *= p.amp;
         }
         const int64_t page = slot >> p.c.page_shift;
         stored = slot >= 0 && page < p.c.n_pages;
@@ -120,7 +130,7 @@ qk_norm_rope_kernel(const __grid_constant__ AppendParams p) {
             for (int e = 0; e < 4; ++e) { a[e] *= r * ga[e]; b[e] *= r * gb[e]; }
           }
         }
-        if (is_q || is_k) {
+        if ((is_q || is_k) && rotates) {   // (what passes must not meet its neighbour, as 0 times an infinity)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float y = fmaf(-b[e], sn[e], a[e] * cs[e]);
@@ -188,21 +198,11 @@ int launch(AppendParams& p, cudaStream_t st) {
   return cuda_status(cudaGetLastError());
 }
 
-}  // namespace
-}  // namespace mq
-
-using namespace mq;
-
-extern "C" int mq_qk_norm_rope(const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V, int64_t ldv,
-                               int32_t T, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, const float* gain_q,
-                               const float* gain_k, float eps, const int32_t* pos, float base, uint32_t flags, void* Q_out,
-                               int64_t ldqo, void* K_out, int64_t ldko, const mq_kv_cache* cache, const int64_t* slots,
-                               void* stream) {
-  if (T < 0 || n_q_heads <= 0 || n_kv_heads <= 0 || head_dim <= 0 || (flags & ~MQ_ROPE_HALF)) return MQ_ERR_INVALID_ARG;
-  if (!(eps >= 0.0f) || !std::isfinite(eps) || !(base > 1.0f) || !std::isfinite(base)) return MQ_ERR_INVALID_ARG;
-  if (head_dim != 64 && head_dim != 128) return MQ_ERR_UNSUPPORTED;
+// What both entry points have in common; the rotation stands in p already.
+int append(AppendParams& p, const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V, int64_t ldv, int32_t T, int32_t n_q_heads,
+           int32_t n_kv_heads, int32_t head_dim, const float* gain_q, const float* gain_k, float eps, const int32_t* pos, bool half, void* Q_out,
+           int64_t ldqo, void* K_out, int64_t ldko, const mq_kv_cache* cache, const int64_t* slots, void* stream) {
   if (n_q_heads > 65536 || n_kv_heads > 65536) return MQ_ERR_UNSUPPORTED;
-  AppendParams p{};
   if (cache) {
     const int rc = check_kv_cache(cache, &p.c);
     if (rc != MQ_OK) return rc;
@@ -223,16 +223,62 @@ extern "C" int mq_qk_norm_rope(const void* Q, int64_t ldq, const void* K, int64_
   p.T = T; p.n_q = n_q_heads; p.n_kv = n_kv_heads;
   p.gain_q = gain_q; p.gain_k = gain_k; p.eps = eps; p.pos = pos; p.slots = slots;
   p.has_cache = cache != nullptr;
-  // powers of one ratio, in long double: 64 roundings of 2^-64 (one pow instead of 64, which took longer than the launch)
-  const long double ratio = powl((long double)base, -2.0L / head_dim);
-  long double turn = 1.0L / 6.283185307179586476925286766559L;
-  for (int i = 0; i < head_dim / 2; ++i, turn *= ratio) p.turns[i] = (double)turn;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const bool half = flags & MQ_ROPE_HALF, i8 = cache && (cache->flags & MQ_KV_INT8);
+  const bool i8 = cache && (cache->flags & MQ_KV_INT8);
   if (head_dim == 128) {
     if (half) return i8 ? launch<128, true, true>(p, st) : launch<128, true, false>(p, st);
     return i8 ? launch<128, false, true>(p, st) : launch<128, false, false>(p, st);
   }
   if (half) return i8 ? launch<64, true, true>(p, st) : launch<64, true, false>(p, st);
   return i8 ? launch<64, false, true>(p, st) : launch<64, false, false>(p, st);
+}
+
+constexpr long double kTurn = 1.0L / 6.283185307179586476925286766559L;
+
+}  // namespace
+}  // namespace mq
+
+using namespace mq;
+
+extern "C" int mq_qk_norm_rope(const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V, int64_t ldv, int32_t T,
+                               int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, const float* gain_q,
+                               const float* gain_k, float eps, const int32_t* pos, float base, uint32_t flags, void* Q_out,
+                               int64_t ldqo, void* K_out, int64_t ldko, const mq_kv_cache* cache, const int64_t* slots,
+                               void* stream) {
+  if (T < 0 || n_q_heads <= 0 || n_kv_heads <= 0 || head_dim <= 0 || (flags & ~MQ_ROPE_HALF)) return MQ_ERR_INVALID_ARG;
+  if (!(eps >= 0.0f) || !std::isfinite(eps) || !(base > 1.0f) || !std::isfinite(base)) return MQ_ERR_INVALID_ARG;
+  if (head_dim != 64 && head_dim != 128) return MQ_ERR_UNSUPPORTED;
+  AppendParams p{};
+  p.rot_pairs = head_dim / 2;
+  p.amp = 1.0f;
+  if (T > 0) {
+    // powers of one ratio, in long double: 64 roundings of 2^-64 (one pow instead of 64, which took longer than the launch)
+    const long double ratio = powl((long double)base, -2.0L / head_dim);
+    long double turn = kTurn;
+    for (int i = 0; i < head_dim / 2; ++i, turn *= ratio) p.turns[i] = (double)turn;
+  }
+  return append(p, Q, ldq, K, ldk, V, ldv, T, n_q_heads, n_kv_heads, head_dim, gain_q, gain_k, eps, pos, flags & MQ_ROPE_HALF, Q_out, ldqo, K_out,
+                ldko, cache, slots, stream);
+}
+
+extern "C" int mq_qk_norm_rope_scaled(const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V, int64_t ldv, int32_t T,
+                                      int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, const float* gain_q,
+                                      const float* gain_k, float eps, const int32_t* pos, const mq_rope* rope, void* Q_out,
+                                      int64_t ldqo, void* K_out, int64_t ldko, const mq_kv_cache* cache, const int64_t* slots,
+                                      void* stream) {
+  if (T < 0 || n_q_heads <= 0 || n_kv_heads <= 0 || head_dim <= 0 || !rope || (rope->flags & ~MQ_ROPE_HALF)) return MQ_ERR_INVALID_ARG;
+  if (!(eps >= 0.0f) || !std::isfinite(eps) || !std::isfinite(rope->amp)) return MQ_ERR_INVALID_ARG;
+  if (head_dim != 64 && head_dim != 128) return MQ_ERR_UNSUPPORTED;
+  const int r = rope->rotary_dim;
+  if (r < 0 || r > head_dim || (r > 0 && !rope->theta)) return MQ_ERR_INVALID_ARG;
+  if (r % 8) return MQ_ERR_UNSUPPORTED;
+  AppendParams p{};
+  p.rot_pairs = r / 2;
+  p.amp = rope->amp;
+  for (int i = 0; i < r / 2; ++i) {
+    if (!(std::fabs(rope->theta[i]) <= 1.0e6)) return MQ_ERR_INVALID_ARG;
+    p.turns[i] = (double)((long double)rope->theta[i] * kTurn);
+  }
+  return append(p, Q, ldq, K, ldk, V, ldv, T, n_q_heads, n_kv_heads, head_dim, gain_q, gain_k, eps, pos, rope->flags & MQ_ROPE_HALF, Q_out, ldqo,
+                K_out, ldko, cache, slots, stream);
 }

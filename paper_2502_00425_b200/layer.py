@@ -124,6 +124,9 @@ class W4A8DecoderBlock:
         # RMSNorm gains of the query and key heads (float32 [head_dim]), for blocks that norm them; used by forward_cached
         self.g_q: Optional[torch.Tensor] = None
         self.g_k: Optional[torch.Tensor] = None
+        # rotary embedding of a part of the head, or scaled for a longer context (None: the whole head, pairs (2i, 2i + 1), base
+        # 10000); used by forward_cached
+        self.rope: Optional[B.Rope] = None
 
     # ---- pieces ------------------------------------------------------------------------
     def aifs(self, embs, is_visuals, tr: BlockTrace) -> torch.Tensor:
@@ -313,7 +316,7 @@ class W4A8DecoderBlock:
         """New tokens of every sequence of a PagedKVCache (one each, a few, or a chunk; empty ones are allowed): lists of
         bf16 [n_b, hidden] and, where a chunk has visual tokens, uint8 [n_b] (None for a chunk of text, or for all of them: no
         reordering then).  Queries and
-        keys are normed (g_q, g_k, if set) and rotated at their positions behind what the cache holds, keys and values
+        keys are normed (g_q, g_k, if set) and rotated (by `rope`, if set) at their positions behind what the cache holds, keys and values
         are stored, and the rows attend the cached context and, causally in the original order, their chunk.  Returns
         (outputs in the original order, BlockTrace).  Where it raises, the cache holds what it held before."""
         live = [b for b, e in enumerate(embs) if e.shape[0]]
@@ -346,7 +349,7 @@ class W4A8DecoderBlock:
         q, k, v = self.linear_group(["q_proj", "k_proj", "v_proj"], h, tr, calibrate)
         qr = torch.empty((step.total, sh.n_q_heads * sh.head_dim), dtype=torch.bfloat16, device=x0.device)
         B.mq_qk_norm_rope(q, k, pos, sh.n_q_heads, sh.n_kv_heads, qr, gain_q=self.g_q, gain_k=self.g_k, v=v, cache=cache.handle,
-                          slots=step.slots)
+                          slots=step.slots, rope=self.rope)
         t["q_rope"] = qr
         a, lse = cache.attention(qr, step, sh.n_q_heads, perm)
         x2 = self._behind_attention(x0, a, tr, calibrate)

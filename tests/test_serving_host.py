@@ -1,0 +1,74 @@
+"""Host-side checks (no GPU) of the calls around a serving step: refusals before anything is enqueued, and pins of their oracle."""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+
+from oracle import kv_oracle as O
+from paper_2502_00425_b200 import binding as B
+from paper_2502_00425_b200 import build
+
+A = 0x10000   # a fake, aligned device address: validation must come before it is used
+
+
+@pytest.fixture(scope="module")
+def lib():
+    build.build_library()
+    return B.load()
+
+
+def _cache(K=A, V=A, page_stride=4 * 64 * 128, head_stride=64 * 128, slot_stride=128, n_pages=10, page=64, hkv=4, dim=128, flags=0,
+           ks=None, vs=None):
+    return B.mq_kv_cache(K, V, page_stride, head_stride, slot_stride, n_pages, page, hkv, dim, flags, ks, vs)
+
+
+# ------------------------------------------------------------------------------------------------ rotary embedding
+def test_rotary_refusals(lib):
+    theta = (C.c_double * 64)(*[0.5] * 64)
+    rope = lambda rot=64, flags=0, amp=1.0, theta=theta: B.mq_rope(C.cast(theta, C.POINTER(C.c_double)) if theta else None, rot, flags, amp)
+
+    def call(r=None, T=5, hq=8, hkv=4, dim=128, eps=1e-6, q=A, ldq=1024, pos=A, qo=A, slots=A, cache=None, none=False):
+        r = rope() if r is None else r
+        return lib.mq_qk_norm_rope_scaled(q, ldq, A, hkv * dim, A, hkv * dim, T, hq, hkv, dim, None, None, eps, pos, None if none else C.byref(r),
+                                          qo, hq * dim, None, 0, C.byref(cache or _cache()), slots, None)
+
+    assert call(none=True) == B.MQ_ERR_INVALID_ARG
+    assert call(rope(rot=-8)) == call(rope(rot=136)) == call(rope(flags=2)) == call(rope(theta=None)) == B.MQ_ERR_INVALID_ARG
+    assert call(rope(rot=68)) == B.MQ_ERR_UNSUPPORTED
+    for bad in (math.nan, math.inf, -2e6):
+        assert call(rope(theta=(C.c_double * 64)(*[0.5] * 31 + [bad] + [0.5] * 32))) == B.MQ_ERR_INVALID_ARG
+    assert call(rope(rot=32, theta=(C.c_double * 64)(*[0.5] * 31 + [math.nan] + [0.5] * 32)), q=None) == B.MQ_ERR_INVALID_ARG
+    assert call(rope(amp=math.inf)) == call(rope(amp=math.nan)) == call(eps=-1.0) == call(T=-1) == call(hq=0) == B.MQ_ERR_INVALID_ARG
+    assert call(dim=96) == B.MQ_ERR_UNSUPPORTED
+    assert call(q=None) == call(pos=None) == call(qo=None) == call(slots=None) == call(ldq=512) == B.MQ_ERR_INVALID_ARG
+    assert call(q=A + 2) == call(ldq=1028) == B.MQ_ERR_ALIGNMENT
+    assert call(cache=_cache(dim=64)) == call(cache=_cache(hkv=2)) == B.MQ_ERR_INVALID_ARG
+    assert call(T=0) == call(rope(rot=0, theta=None), T=0) == B.MQ_OK
+
+
+def test_frequencies_of_the_binding():
+    for kw in (dict(), dict(factor=4.0), dict(factor=4.0, original=32768), dict(factor=2.0, original=100, fast=8.0, slow=2.0)):
+        got = np.array(B.Rope(64, **kw).theta)
+        want = O.rope_theta(64, 10000.0, **kw)
+        assert np.all(np.abs(got - want) <= 2.0 ** -48 * want)
+    by_parts, plain = B.Rope(128, factor=8.0, original=4096).theta, B.Rope(128).theta
+    assert by_parts[0] == plain[0] and by_parts[-1] == plain[-1] / 8.0       # many turns: kept; less than one: divided
+    assert all(p / 8.0 <= t <= p for t, p in zip(by_parts, plain))
+    assert B.Rope(4, theta=[1, 2]).theta == [1.0, 2.0]
+    for bad in (dict(rotary_dim=7), dict(rotary_dim=-2), dict(rotary_dim=8, theta=[1.0]), dict(rotary_dim=8, base=0.5),
+                dict(rotary_dim=8, factor=0.0), dict(rotary_dim=8, original=4096, fast=1.0, slow=1.0)):
+        with pytest.raises(ValueError):
+            B.Rope(**bad)
+
+
+def test_rotary_oracle_reduces_to_the_whole_head():
+    rng = np.random.default_rng(0)
+    x, pos, gain = rng.standard_normal((5, 3, 16)), np.arange(5) * 7, rng.standard_normal(16)
+    for half in (False, True):
+        y, mag = O.norm_rope(x, gain, 1e-6, pos, 10000.0, half)
+        y2, mag2 = O.norm_rope_scaled(x, gain, 1e-6, pos, O.rope_theta(16, 10000.0), half, 1.0)
+        assert np.allclose(y, y2, rtol=0, atol=1e-13) and np.allclose(mag, mag2, rtol=1e-13)
+        y3, _ = O.norm_rope_scaled(x[..., :8], None, 0, pos, O.rope_theta(8, 10000.0), half, 2.0)
+        y4, _ = O.norm_rope_scaled(x, None, 0, pos, O.rope_theta(8, 10000.0), half, 2.0)
+        assert np.array_equal(y3, y4[..., :8]) and np.array_equal(y4[..., 8:], x[..., 8:])
