@@ -598,6 +598,30 @@ int mq_kv_evict(const mq_kv_cache* cache, const int32_t* page_table, int32_t max
                 int32_t budget, int32_t n_first, int32_t n_last, const mq_kv_cache* dst, const int32_t* dst_table,
                 int32_t dst_max_pages, int32_t* kept, int32_t* new_len, float* W_out, void* stream);
 
+/* ---- Sampling ----------------------------------------------------------------------------------
+ *
+ * The next token of every row of logits X [B, V] (bf16, or float32 with MQ_SAMPLE_F32; leading dimension in elements, any
+ * alignment of the type), from one given random number per row.  With w_i = exp((x_i - max) / T) and the order "larger x first, of
+ * equal ones the lower index":
+ *   top_k   keeps the first top_k of the order (<= 0 or >= V: all);
+ *   top_p   keeps, of those, the ones before which less than top_p of their mass lies (>= 1 or NaN: all; <= 0: the first);
+ *   min_p   keeps those with w_i >= min_p (<= 0 or NaN: all; above 1 counts as 1);
+ * the first of the order is always kept.  token[r] is the first kept index, in the order of the vocabulary, at which the running sum of the
+ * kept weights exceeds u[r] times their total (u in [0, 1); what lies outside counts as its nearest).  T <= 0 or NaN: the
+ * first of the order.  NaN and -infinity logits are never kept; where every logit is one, token is -1.  Where a logit is +infinity, all
+ * others weigh nothing.
+ *   temperature, u   device float32 [B];  top_k device int32 [B], top_p, min_p device float32 [B], each may be NULL (all kept)
+ *   token            device int32 [B]
+ *   logp             optional device float32 [B]: log of the kept, renormalised probability of the token (0 if T <= 0, -inf if none)
+ *   kept             optional device int32 [B]: how many were kept
+ * Weights are fixed-point numbers with 43 bits behind the point and their sums whole numbers: results do not depend on any order of
+ * execution.  V at most 2^20, B at most 2^24 (MQ_ERR_UNSUPPORTED).  One kernel; no workspace.
+ */
+#define MQ_SAMPLE_F32 1u
+int mq_sample(const void* logits, int64_t ld, int32_t B, int32_t V, uint32_t flags, const float* temperature,
+              const int32_t* top_k, const float* top_p, const float* min_p, const float* u, int32_t* token, float* logp,
+              int32_t* kept, void* stream);
+
 /* ---- Measurement and self-test aids (the paper has no counterpart) ------------------------- */
 
 /*

@@ -28,6 +28,7 @@ MQ_FLAG_W8 = 8
 MQ_NOALLOC_WS_BYTES = 4 << 20
 MQ_KV_INT8 = 1
 MQ_ROPE_HALF = 1
+MQ_SAMPLE_F32 = 1
 MQ_W_TILE_N, MQ_W_TILE_K = 128, 128
 TEXT, VISUAL = 0, 1
 
@@ -110,6 +111,7 @@ def load(build_if_missing: bool = False):
         "mq_kv_attention_workspace_bytes": (sz, [kvbp, kvcp, i32]),
         "mq_kv_attention": (C.c_int, [vp, i64, kvbp, kvcp, i32, f32, vp, i64, vp, vp, sz, vp]),
         "mq_kv_weights": (C.c_int, [vp, i64, kvbp, kvcp, i32, f32, vp, vp, vp, i64, i64, i32, vp, vp]),
+        "mq_sample": (C.c_int, [vp, i64, i32, i32, C.c_uint32, vp, vp, vp, vp, vp, vp, vp, vp, vp]),
         "mq_kv_evict": (C.c_int, [kvcp, vp, i32, vp, i32, vp, i64, i64, i32, i32, i32, i32, kvcp, vp, i32, vp, vp, vp, vp]),
         "mq_repack_w4": (C.c_int, [vp, i32, i32, vp, vp]),
         "mq_unpack_w4": (C.c_int, [vp, vp, i32, i32, vp, i64, vp]),
@@ -149,7 +151,7 @@ EXPORTED = ["mq_version", "mq_status_string", "mq_workspace_bytes", "mq_w4_layou
             "mq_ubench_mma_i8", "mq_selftest_bounded_wait", "mq_ubench_expand", "mq_calibrate_static_scales_bits",
             "mq_w8_layout_bytes", "mq_pack_w8", "mq_fwht_quant_bits", "mq_kron_quant_i8", "mq_glue_rmsnorm", "mq_glue_rope",
             "mq_glue_swiglu", "mq_glue_residual_add", "mq_aifs_attention_workspace_bytes", "mq_aifs_attention",
-            "mq_qk_norm_rope", "mq_qk_norm_rope_scaled", "mq_kv_attention_workspace_bytes", "mq_kv_attention", "mq_kv_weights", "mq_kv_evict"]
+            "mq_qk_norm_rope", "mq_qk_norm_rope_scaled", "mq_kv_attention_workspace_bytes", "mq_kv_attention", "mq_kv_weights", "mq_kv_evict", "mq_sample"]
 
 
 def status_string(status: int) -> str:
@@ -725,6 +727,24 @@ def mq_kv_evict(cache: KVCache, page_table, kv_len, w, budget, n_first, n_last, 
     _kv_call(d, load().mq_kv_evict, "mq_kv_evict", cache.ref, _vec(page_table, _I32, n_seq * width, d), width, _vec(kv_len, _I32, n_seq, d),
              n_seq, pw, s0, s1, keys, budget, n_first, n_last, dst.ref, _vec(dst_table, _I32, dst_table.numel(), d), dst_table.shape[1],
              _vec(kept, _I32, n, d), _vec(new_len, _I32, n_seq, d), _vec(w_out, _F32, n, d))
+
+
+def mq_sample(logits, temperature, u, token, top_k=None, top_p=None, min_p=None, logp=None, kept=None):
+    """The next token of every row of logits ([B, V], bf16 or float32, contiguous rows of any pitch) from the random numbers u (float32 [B] in
+    [0, 1)): temperature, top_p, min_p float32 [B], top_k int32 [B]; token int32 [B], logp float32 [B], kept int32 [B].  See
+    include/mq.h."""
+    if logits.dim() != 2 or logits.dtype not in (_BF16, _F32):
+        raise ValueError(f"expected bf16 or float32 logits [B, V], got {logits.dtype} {tuple(logits.shape)}")
+    rows, vocab = logits.shape
+    pitch, unit = logits.stride()
+    if unit != 1 and vocab > 1:
+        raise ValueError("rows must be contiguous")
+    if not logits.is_cuda:
+        raise ValueError("tensor must live on a CUDA device (the library has no CPU path)")
+    d = logits.get_device()
+    _kv_call(d, load().mq_sample, "mq_sample", logits.data_ptr(), pitch if rows > 1 else max(pitch, vocab), rows, vocab,
+             MQ_SAMPLE_F32 if logits.dtype == _F32 else 0, _vec(temperature, _F32, rows, d), _vec(top_k, _I32, rows, d), _vec(top_p, _F32, rows, d),
+             _vec(min_p, _F32, rows, d), _vec(u, _F32, rows, d), _vec(token, _I32, rows, d), _vec(logp, _F32, rows, d), _vec(kept, _I32, rows, d))
 
 
 def mq_last_device_status(ws):

@@ -1,0 +1,228 @@
+"""mq_sample against the float64 definition.
+
+Tokens and counts have to be equal: a weight of the call is off by at most 2^-44 of the largest one and 2^-45 of itself (fixed point and a
+double exponential), so sums over V <= 2^19 tokens are off by less than 2^-25 of the largest weight in the worst case and about 2^-34 as
+roundings add up, which a random border (top_p, u) comes near to once in some 2^20 rows; the constructed cases sum exactly.  logp is one float32 rounding (2^-24, relative) of a logarithm whose argument is off by 2^-30 at most.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle.sample_oracle import sample
+from paper_2502_00425_b200 import binding as B
+
+from kv_util import DEV
+
+pytestmark = pytest.mark.gpu
+
+
+def _run(x, t, u, k=None, p=None, mp=None):
+    n = x.shape[0]
+    dev = lambda v, dt: None if v is None else torch.tensor(np.broadcast_to(np.asarray(v), (n,)).copy(), dtype=dt, device=DEV)
+    token, kept = (torch.full((n + 1,), 77, dtype=torch.int32, device=DEV) for _ in range(2))
+    logp = torch.full((n + 1,), 77.0, device=DEV)
+    B.mq_sample(x, dev(t, torch.float32), dev(u, torch.float32), token[:n], top_k=dev(k, torch.int32), top_p=dev(p, torch.float32),
+                min_p=dev(mp, torch.float32), logp=logp[:n], kept=kept[:n])
+    torch.cuda.synchronize()
+    assert int(token[n]) == 77 and float(logp[n]) == 77.0 and int(kept[n]) == 77
+    return token[:n].tolist(), logp[:n].double().tolist(), kept[:n].tolist()
+
+
+def _check(x, t, u, k=None, p=None, mp=None):
+    got = _run(x, t, u, k, p, mp)
+    host = x.float().cpu().numpy()
+    at = lambda v, r, off: off if v is None else np.broadcast_to(np.asarray(v), (x.shape[0],))[r]
+    for r, (token, logp, kept) in enumerate(zip(*got)):
+        want, lp, keep = sample(host[r], at(t, r, 0), at(u, r, 0), at(k, r, 0), at(p, r, 1.0), at(mp, r, 0.0))
+        assert (token, kept) == (want, keep.size), (r, token, kept, want, keep.size)
+        assert logp == lp or abs(logp - lp) <= 2.0 ** -24 * abs(lp) + 2.0 ** -30, (r, logp, lp)
+    return got
+
+
+def _logits(rng, n, v, bf16, peaks=40):
+    x = rng.standard_normal((n, v)) * 2
+    for r in range(n):
+        at = rng.integers(0, v, min(v, peaks))
+        x[r, at] += 8 + 3 * rng.standard_normal(at.size)
+    t = torch.from_numpy(x.astype(np.float32))
+    return (t.to(torch.bfloat16) if bf16 else t).to(DEV)
+
+
+@pytest.mark.parametrize("v", [1, 2, 7, 33, 1000, 4095, 4096, 9999, 20001, 131072])
+@pytest.mark.parametrize("bf16", [False, True])
+def test_every_filter(v, bf16):
+    rng = np.random.default_rng(v)
+    n = 24
+    x = _logits(rng, n, v, bf16)
+    t = rng.uniform(0.4, 1.6, n).astype(np.float32)
+    u = rng.random(n).astype(np.float32)
+    k = np.where(np.arange(n) % 3 == 0, rng.integers(1, v + 2, n), rng.integers(1, 60, n))
+    p, mp = rng.uniform(0.1, 0.98, n).astype(np.float32), rng.uniform(1e-4, 0.3, n).astype(np.float32)
+    _check(x, t, u)
+    _check(x, t, u, k=k)
+    _check(x, t, u, p=p)
+    _check(x, t, u, mp=mp)
+    _check(x, t, u, k=k, p=p, mp=mp)
+    _check(x, np.where(np.arange(n) % 2, 0.0, t), u, k=np.where(np.arange(n) % 4 < 2, k, 0), p=np.where(np.arange(n) % 5 < 3, p, 1.0), mp=mp)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_flat_rows(bf16):
+    """Thousands of tokens are kept: nothing fits into a list."""
+    rng = np.random.default_rng(1)
+    n, v = 8, 100003
+    x = (torch.from_numpy(rng.standard_normal((n, v)).astype(np.float32) * 0.5).to(torch.bfloat16 if bf16 else torch.float32)).to(DEV)
+    u = rng.random(n).astype(np.float32)
+    for kw in (dict(), dict(p=0.9), dict(p=0.5), dict(k=30000), dict(k=30000, p=0.95), dict(k=50000, p=0.3, mp=0.2), dict(mp=0.1)):
+        _check(x, 1.0, u, **kw)
+    _check(x, 30.0, u, k=20000)        # a temperature that makes it flatter still
+    _check(x, 0.02, u, p=0.9)          # and ones that leave few
+    _check(x, 0.0005, u, k=500)
+
+
+@pytest.mark.parametrize("v", [5000, 60000])
+def test_equal_logits_are_cut_by_index(v):
+    x = torch.full((4, v), 1.5, device=DEV)
+    u = np.array([0.0, 0.25, 0.5, 0.99999994], np.float32)
+    tok, _, kept = _check(x, 0.7, u)
+    assert tok[0] == 0 and tok[2] == v // 2 and tok[3] == v - 1 and kept == [v] * 4
+    tok, _, kept = _check(x, 0.7, u, k=v - 3)
+    assert kept == [v - 3] * 4 and max(tok) < v - 3
+    _, _, kept = _check(x, 0.7, u, p=0.5)
+    assert kept == [v // 2] * 4
+    _, _, kept = _check(x, 0.7, u, p=0.25, k=4 * (v // 8))
+    assert kept == [v // 8] * 4
+    _check(x, 0.7, u, mp=1.0)
+    y = x.clone()                      # two values, the larger at every third column
+    y[:, ::3] = 2.5
+    n3 = -(-v // 3)
+    for k in (n3 - 1, n3, n3 + 1, n3 + 1000, v - 1):
+        _check(y, 1.0, u, k=k)
+    _check(y, 1.0, u, p=0.9)
+    _check(y, 0.5, u, p=0.2, k=n3 + 7)
+    z = y.clone()
+    z[:, 1::3] = -0.0
+    z[:, 2::3] = 0.0                   # one value, two bit patterns
+    _check(z, 1.0, u, k=n3 + 501)
+
+
+def test_masked_rows_nans_and_infinities():
+    rng = np.random.default_rng(2)
+    v, inf, nan = 30011, float("inf"), float("nan")
+    x = _logits(rng, 10, v, False)
+    x[0] = -inf
+    x[1] = nan
+    x[2, 100:] = -inf
+    x[3, :-1] = nan
+    x[4, ::2] = -inf
+    x[5, 77] = inf
+    x[6, 5:2000:7] = inf
+    x[7, 1000:20000] = torch.finfo(torch.float32).min
+    x[8] = torch.finfo(torch.float32).min
+    x[9, :] = -inf
+    x[9, 12345] = torch.finfo(torch.float32).min
+    u = rng.random(10).astype(np.float32)
+    for kw in (dict(), dict(k=200), dict(k=5000), dict(p=0.8), dict(mp=0.05), dict(k=20000, p=0.9, mp=0.001)):
+        tok, lp, kept = _check(x, 0.9, u, **kw)
+        assert tok[:2] == [-1, -1] and kept[:2] == [0, 0] and lp[0] == -np.inf and tok[3] == v - 1 and tok[5] == 77 and tok[9] == 12345
+    tok, _, _ = _check(x, 0.0, u)
+    assert tok[0] == -1 and tok[5] == 77 and tok[6] == 5 and tok[8] == 0
+    w = x.to(torch.bfloat16)
+    _check(w, 0.9, u, p=0.8, k=7000)
+
+
+def test_extreme_parameters():
+    rng = np.random.default_rng(3)
+    n, v = 6, 12000
+    x = _logits(rng, n, v, False)
+    u = rng.random(n).astype(np.float32)
+    nan, inf = float("nan"), float("inf")
+    for t in (nan, -1.0, 0.0):
+        tok, lp, kept = _check(x, t, u, k=5)
+        assert tok == x.argmax(1).tolist() and lp == [0.0] * n and kept == [1] * n
+    _check(x, 1e-30, u, p=0.9)
+    _check(x, 1e-42, u, k=300)
+    tok, _, kept = _check(x, inf, u)
+    assert kept == [v] * n and tok == [int(np.float64(a) * v) for a in u]      # every token alike
+    _check(x, inf, u, k=5000)
+    base = _run(x, 1.0, u)
+    for kw in (dict(k=0), dict(k=-3), dict(k=v), dict(k=v + 5), dict(p=1.0), dict(p=1.5), dict(p=nan), dict(mp=0.0), dict(mp=-1.0), dict(mp=nan)):
+        assert _run(x, 1.0, u, **kw) == base
+    for kw in (dict(p=0.0), dict(p=-1.0), dict(p=1e-30), dict(k=1), dict(mp=5.0)):
+        tok, _, kept = _run(x, 1.0, u, **kw)
+        assert tok == x.argmax(1).tolist() and kept == [1] * n
+    low, high = _run(x, 1.0, np.zeros(n, np.float32))[0], _run(x, 1.0, np.full(n, 0.99999994, np.float32))[0]
+    assert _run(x, 1.0, np.full(n, -2.0))[0] == _run(x, 1.0, np.full(n, nan))[0] == low and _run(x, 1.0, np.full(n, 7.0))[0] == high
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_strides_and_offsets(bf16):
+    """Rows that start anywhere in a 16-byte piece, poison around them."""
+    rng = np.random.default_rng(4)
+    v, dt = 10007, torch.bfloat16 if bf16 else torch.float32
+    for pad, off in ((0, 0), (1, 0), (1, 1), (5, 3), (24, 7)):
+        buf = torch.full((5, v + pad + off), float("inf"), dtype=dt, device=DEV)
+        x = buf[:, off:off + v]
+        x.copy_(_logits(rng, 5, v, bf16))
+        _check(x, 0.8, rng.random(5).astype(np.float32), k=300, p=0.9)
+        _check(x, 0.8, rng.random(5).astype(np.float32))
+    _check(buf[2:3, off:off + v], 0.8, np.float32([0.3]), p=0.9)
+
+
+def test_rows_too_long_to_be_staged():
+    rng = np.random.default_rng(5)
+    x = _logits(rng, 2, 1 << 19, False)
+    u = rng.random(2).astype(np.float32)
+    for kw in (dict(), dict(k=50), dict(p=0.9), dict(k=100000, p=0.99)):
+        _check(x, 0.8, u, **kw)
+    y = _logits(rng, 1, (1 << 20) - 5, True)
+    _check(y, 1.0, u[:1], p=0.9, k=1000)
+
+
+def test_sorted_rows():
+    v = 40000
+    x = torch.stack([torch.linspace(-20, 20, v), torch.linspace(20, -20, v), torch.linspace(-1e4, 1e4, v), torch.linspace(3e38, -3e38, v)]).to(DEV)
+    u = np.array([0.1, 0.6, 0.9, 0.3], np.float32)
+    for kw in (dict(), dict(k=64), dict(k=9000), dict(p=0.95), dict(k=9000, p=0.5), dict(mp=0.01)):
+        _check(x, 1.0, u, **kw)
+
+
+def test_captured_and_on_another_stream():
+    rng = np.random.default_rng(6)
+    n, v = 5, 9000
+    x = torch.empty((n, v), device=DEV)
+    t, u = torch.full((n,), 0.9, device=DEV), torch.empty(n, device=DEV)
+    token = torch.empty(n, dtype=torch.int32, device=DEV)
+    p = torch.full((n,), 0.9, device=DEV)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        B.mq_sample(x.zero_(), t, u.zero_(), token, top_p=p)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.mq_sample(x, t, u, token, top_p=p)
+    for _ in range(3):
+        x.copy_(_logits(rng, n, v, False))
+        u.copy_(torch.from_numpy(rng.random(n).astype(np.float32)))
+        graph.replay()
+        torch.cuda.synchronize()
+        host = x.cpu().numpy()
+        assert token.tolist() == [sample(host[r], 0.9, float(u[r]), top_p=0.9)[0] for r in range(n)]
+
+
+def test_no_rows_and_many_rows():
+    _run(torch.empty((0, 100), device=DEV), 1.0, 0.5)
+    rng = np.random.default_rng(7)
+    x = _logits(rng, 700, 300, True, peaks=5)
+    _check(x, 0.9, rng.random(700).astype(np.float32), k=20, p=0.9)
+
+
+def test_the_drawn_tokens_have_their_probabilities():
+    """20000 even steps of u: each token's share is its probability to one step."""
+    v, n = 50, 20000
+    x = torch.linspace(-3, 3, v, device=DEV).roll(13)
+    tok, _, _ = _run(x.expand(n, v).contiguous(), 1.0, (np.arange(n) / n).astype(np.float32))
+    prob = torch.softmax(x.double(), 0).cpu().numpy()
+    share = np.bincount(tok, minlength=v) / n
+    assert np.all(np.abs(share - prob) <= 1.0 / n + 2.0 ** -23)

@@ -6,6 +6,7 @@ import numpy as np
 import pytest
 
 from oracle import kv_oracle as O
+from oracle import sample_oracle as S
 from paper_2502_00425_b200 import binding as B
 from paper_2502_00425_b200 import build
 
@@ -72,3 +73,30 @@ def test_rotary_oracle_reduces_to_the_whole_head():
         y3, _ = O.norm_rope_scaled(x[..., :8], None, 0, pos, O.rope_theta(8, 10000.0), half, 2.0)
         y4, _ = O.norm_rope_scaled(x, None, 0, pos, O.rope_theta(8, 10000.0), half, 2.0)
         assert np.array_equal(y3, y4[..., :8]) and np.array_equal(y4[..., 8:], x[..., 8:])
+
+
+# ------------------------------------------------------------------------------------------------ sampling
+def test_sample_refusals(lib):
+    def call(x=A, ld=1000, n=4, v=1000, flags=1, t=A, u=A, token=A):
+        return lib.mq_sample(x, ld, n, v, flags, t, None, None, None, u, token, None, None, None)
+
+    assert call(n=-1) == call(v=0) == call(v=-5) == call(ld=999) == call(flags=2) == B.MQ_ERR_INVALID_ARG
+    assert call(x=None) == call(t=None) == call(u=None) == call(token=None) == B.MQ_ERR_INVALID_ARG
+    assert call(v=(1 << 20) + 1, ld=1 << 21) == call(n=(1 << 24) + 1) == B.MQ_ERR_UNSUPPORTED
+    assert call(x=A + 2) == call(x=A + 1, flags=0) == B.MQ_ERR_ALIGNMENT
+    assert call(n=0) == call(n=0, x=None) == B.MQ_OK
+
+
+def test_sample_oracle_by_hand():
+    x = np.log([4.0, 2.0, 1.0, 1.0])
+    for u, want in ((0.0, 0), (0.49, 0), (0.5, 1), (0.74, 1), (0.75, 2), (0.88, 3)):
+        assert S.sample(x, 1.0, u)[0] == want
+    assert S.sample(x, 1.0, 0.6, top_k=2)[2].tolist() == [0, 1] and S.sample(x, 1.0, 0.7, top_k=2)[0] == 1
+    assert S.sample(x, 1.0, 0.0, top_p=0.5)[2].tolist() == [0]               # exactly half lies before the second
+    assert S.sample(x, 1.0, 0.0, top_p=0.51)[2].tolist() == [0, 1] and S.sample(x, 1.0, 0.0, top_p=0.9)[2].tolist() == [0, 1, 2, 3]
+    assert S.sample(x, 1.0, 0.0, top_k=2, top_p=0.7)[2].tolist() == [0, 1]   # of the first two, two thirds lie before the second
+    assert S.sample(x, 1.0, 0.0, top_k=2, top_p=0.6)[2].tolist() == [0]
+    assert S.sample(x, 0.5, 0.0, min_p=0.25)[2].tolist() == [0, 1]           # weights 1, 1/4, 1/16
+    assert S.sample(np.array([1.0, 3.0, 3.0]), 0.0, 0.9)[0] == 1
+    assert S.sample(np.array([np.nan, -np.inf]), 1.0, 0.9)[0] == -1
+    assert abs(S.sample(x, 1.0, 0.5)[1] - np.log(0.25)) < 1e-15
