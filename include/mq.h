@@ -598,6 +598,32 @@ int mq_kv_evict(const mq_kv_cache* cache, const int32_t* page_table, int32_t max
                 int32_t budget, int32_t n_first, int32_t n_last, const mq_kv_cache* dst, const int32_t* dst_table,
                 int32_t dst_max_pages, int32_t* kept, int32_t* new_len, float* W_out, void* stream);
 
+/*
+ * A step's bookkeeping on the GPU, from the lengths that the sequences ask for: pages are taken and given back, and the arrays that the
+ * calls above want are built.  mq_kv_state is what lives on the device between steps:
+ *   kv_len      [n_seq] keys of every sequence;  seen [n_seq] tokens it has seen (the next one's position; eviction leaves it)
+ *   page_table  [n_seq][max_pages];  borrowed [n_seq] or NULL: so many first entries of a row are pages of another sequence (all of them full):
+ *               they are read only, and do not go back to the free list with this one
+ *   free_pages  [n_pages], of which the first *n_free are free pages: a stack, its top at the end
+ * The step: sequence b keeps its first min(keep[b], kv_len[b]) keys (keep NULL: all; 0 ends it, and its next token is at position 0) and
+ * gets new_len[b] more.  Pages that no key needs any more go back to the free list first, in the order of sequence and entry, the
+ * first of them on top; then pages are taken from the top in the same order.  A step that takes back what another one added leaves free list
+ * and lengths as they were.  borrowed[b] shrinks to the whole pages that are kept; inside its borrowed pages a sequence can be cut
+ * at whole pages only.  Table entries behind a sequence's last page are left as they were.
+ *   cu_q   int32 [n_seq + 1]: the step's rows of sequence b are cu_q[b] .. cu_q[b + 1] - 1
+ *   slots  int64 [max_rows]: where they go (mq_qk_norm_rope), pos int32 [max_rows]: their positions; -1 and 0 behind the last row
+ * A step that cannot be made changes nothing and has no rows (cu_q all 0, slots -1); status (optional, int32[2], zeroed by the caller)
+ * then says MQ_ERR_INVALID_ARG and 1: a length that is negative or does not fit the table, or a cut inside a borrowed page, 2: more than
+ * max_rows rows, 3: more free pages than n_pages; or MQ_ERR_WORKSPACE and 4: not enough free pages.  page_size as of a cache; n_seq <= 2048, max_pages
+ * at most 2^22.  No two arrays may overlap.
+ */
+typedef struct mq_kv_state {
+  int32_t n_seq, max_pages, page_size, n_pages;
+  int32_t *kv_len, *seen, *page_table, *borrowed, *free_pages, *n_free; /* device */
+} mq_kv_state;
+int mq_kv_plan(const mq_kv_state* state, const int32_t* new_len, const int32_t* keep, int32_t max_rows, int32_t* cu_q, int64_t* slots,
+               int32_t* pos, int32_t* status, void* stream);
+
 /* ---- Sampling ----------------------------------------------------------------------------------
  *
  * The next token of every row of logits X [B, V] (bf16, or float32 with MQ_SAMPLE_F32; leading dimension in elements, any

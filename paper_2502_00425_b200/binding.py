@@ -66,6 +66,11 @@ class mq_rope(C.Structure):
     _fields_ = [("theta", C.POINTER(C.c_double)), ("rotary_dim", C.c_int32), ("flags", C.c_uint32), ("amp", C.c_float)]
 
 
+class mq_kv_state(C.Structure):
+    _fields_ = [("n_seq", C.c_int32), ("max_pages", C.c_int32), ("page_size", C.c_int32), ("n_pages", C.c_int32), ("kv_len", C.c_void_p),
+                ("seen", C.c_void_p), ("page_table", C.c_void_p), ("borrowed", C.c_void_p), ("free_pages", C.c_void_p), ("n_free", C.c_void_p)]
+
+
 def lib_path() -> str:
     return os.path.join(os.path.dirname(os.path.abspath(__file__)), _LIB_NAME)
 
@@ -111,6 +116,7 @@ def load(build_if_missing: bool = False):
         "mq_kv_attention_workspace_bytes": (sz, [kvbp, kvcp, i32]),
         "mq_kv_attention": (C.c_int, [vp, i64, kvbp, kvcp, i32, f32, vp, i64, vp, vp, sz, vp]),
         "mq_kv_weights": (C.c_int, [vp, i64, kvbp, kvcp, i32, f32, vp, vp, vp, i64, i64, i32, vp, vp]),
+        "mq_kv_plan": (C.c_int, [C.POINTER(mq_kv_state), vp, vp, i32, vp, vp, vp, vp, vp]),
         "mq_sample": (C.c_int, [vp, i64, i32, i32, C.c_uint32, vp, vp, vp, vp, vp, vp, vp, vp, vp]),
         "mq_kv_evict": (C.c_int, [kvcp, vp, i32, vp, i32, vp, i64, i64, i32, i32, i32, i32, kvcp, vp, i32, vp, vp, vp, vp]),
         "mq_repack_w4": (C.c_int, [vp, i32, i32, vp, vp]),
@@ -151,7 +157,7 @@ EXPORTED = ["mq_version", "mq_status_string", "mq_workspace_bytes", "mq_w4_layou
             "mq_ubench_mma_i8", "mq_selftest_bounded_wait", "mq_ubench_expand", "mq_calibrate_static_scales_bits",
             "mq_w8_layout_bytes", "mq_pack_w8", "mq_fwht_quant_bits", "mq_kron_quant_i8", "mq_glue_rmsnorm", "mq_glue_rope",
             "mq_glue_swiglu", "mq_glue_residual_add", "mq_aifs_attention_workspace_bytes", "mq_aifs_attention",
-            "mq_qk_norm_rope", "mq_qk_norm_rope_scaled", "mq_kv_attention_workspace_bytes", "mq_kv_attention", "mq_kv_weights", "mq_kv_evict", "mq_sample"]
+            "mq_qk_norm_rope", "mq_qk_norm_rope_scaled", "mq_kv_attention_workspace_bytes", "mq_kv_attention", "mq_kv_weights", "mq_kv_evict", "mq_sample", "mq_kv_plan"]
 
 
 def status_string(status: int) -> str:
@@ -727,6 +733,32 @@ def mq_kv_evict(cache: KVCache, page_table, kv_len, w, budget, n_first, n_last, 
     _kv_call(d, load().mq_kv_evict, "mq_kv_evict", cache.ref, _vec(page_table, _I32, n_seq * width, d), width, _vec(kv_len, _I32, n_seq, d),
              n_seq, pw, s0, s1, keys, budget, n_first, n_last, dst.ref, _vec(dst_table, _I32, dst_table.numel(), d), dst_table.shape[1],
              _vec(kept, _I32, n, d), _vec(new_len, _I32, n_seq, d), _vec(w_out, _F32, n, d))
+
+
+class KVState:
+    """Handle of a paged cache's bookkeeping on the GPU (mq_kv_state), all int32: kv_len, seen [n_seq], page_table [n_seq, pages], free_pages
+    [n_pages] of which the first n_free [1] are free, and optionally borrowed [n_seq].  The tensors are kept alive by the handle."""
+
+    def __init__(self, kv_len, seen, page_table, free_pages, n_free, page_size, borrowed=None):
+        n, width = page_table.shape
+        d = page_table.get_device()
+        if not page_table.is_cuda:
+            raise ValueError("tensor must live on a CUDA device (the library has no CPU path)")
+        self.tensors = (kv_len, seen, page_table, free_pages, n_free, borrowed)
+        self.index, self.n_seq = d, n
+        self.c = mq_kv_state(n, width, page_size, free_pages.numel(), _vec(kv_len, _I32, n, d), _vec(seen, _I32, n, d),
+                             _vec(page_table, _I32, n * width, d), _vec(borrowed, _I32, n, d), _vec(free_pages, _I32, free_pages.numel(), d),
+                             _vec(n_free, _I32, 1, d))
+        self.ref = C.byref(self.c)
+
+
+def mq_kv_plan(state: KVState, new_len, cu_q, slots, pos, status=None, keep=None):
+    """One step's pages, cumulative row counts (cu_q int32 [n_seq + 1]), slots (int64 [max_rows]) and positions (int32 [max_rows]) from the rows
+    that every sequence brings (new_len int32 [n_seq]) and the keys it keeps (keep int32 [n_seq], None: all).  status: zeroed int32[2] or
+    None.  See include/mq.h."""
+    d, n, rows = state.index, state.n_seq, slots.numel()
+    _kv_call(d, load().mq_kv_plan, "mq_kv_plan", state.ref, _vec(new_len, _I32, n, d), _vec(keep, _I32, n, d), rows, _vec(cu_q, _I32, n + 1, d),
+             _vec(slots, _I64, rows, d), _vec(pos, _I32, rows, d), _vec(status, _I32, 2, d))
 
 
 def mq_sample(logits, temperature, u, token, top_k=None, top_p=None, min_p=None, logp=None, kept=None):

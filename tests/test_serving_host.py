@@ -6,6 +6,7 @@ import numpy as np
 import pytest
 
 from oracle import kv_oracle as O
+from oracle import plan_oracle as P
 from oracle import sample_oracle as S
 from paper_2502_00425_b200 import binding as B
 from paper_2502_00425_b200 import build
@@ -100,3 +101,29 @@ def test_sample_oracle_by_hand():
     assert S.sample(np.array([1.0, 3.0, 3.0]), 0.0, 0.9)[0] == 1
     assert S.sample(np.array([np.nan, -np.inf]), 1.0, 0.9)[0] == -1
     assert abs(S.sample(x, 1.0, 0.5)[1] - np.log(0.25)) < 1e-15
+
+
+# ------------------------------------------------------------------------------------------------ bookkeeping
+def test_plan_refusals(lib):
+    def call(n=4, width=7, page=64, pages=100, kv=A, seen=A, table=A, borrowed=None, free=A, n_free=A, new=A, keep=None, rows=10, cu=A, slots=A,
+             pos=A, none=False):
+        s = B.mq_kv_state(n, width, page, pages, kv, seen, table, borrowed, free, n_free)
+        return lib.mq_kv_plan(None if none else C.byref(s), new, keep, rows, cu, slots, pos, None, None)
+
+    assert call(none=True) == call(n=-1) == call(width=-1) == call(pages=-1) == call(rows=-1) == call(page=0) == B.MQ_ERR_INVALID_ARG
+    assert call(n=2049) == call(width=(1 << 22) + 1) == call(page=48) == call(page=8) == call(page=512) == call(rows=(1 << 30) + 1) == B.MQ_ERR_UNSUPPORTED
+    for name in ("kv", "seen", "table", "free", "n_free", "new", "cu", "slots", "pos"):
+        assert call(**{name: None}) == B.MQ_ERR_INVALID_ARG
+
+
+def test_plan_oracle_by_hand():
+    state = dict(kv_len=[5, 0], seen=[9, 0], borrowed=[0, 0], table=[[3, 5, -1], [-1, -1, -1]], free=[4, 2, 1, 0], n_pages=6)
+    assert P.plan(state, [4, 3], None, 8, 4) == ([0, 4, 7], [21, 22, 23, 0, 4, 5, 6, -1], [9, 10, 11, 12, 0, 1, 2, 0])
+    assert state["table"] == [[3, 5, 0], [1, -1, -1]] and state["free"] == [4, 2] and state["kv_len"] == [9, 3]
+    assert P.plan(state, [0, 0], [5, 0], 0, 4) == ([0, 0, 0], [], [])
+    assert state["free"] == [4, 2, 1, 0] and state["seen"] == [9, 0]
+    state["borrowed"] = [1, 0]
+    assert P.plan(state, [1, 0], [0, 0], 1, 4) == ([0, 1, 1], [20], [0])      # its own page 5 goes back and comes again; page 3 is not its own
+    assert state["free"] == [4, 2, 1, 0] and state["borrowed"] == [0, 0]
+    with pytest.raises(P.Refused):
+        P.plan(state, [12, 12], None, 24, 4)
