@@ -562,6 +562,22 @@ int mq_kv_attention(const void* Q, int64_t ldq, const mq_kv_batch* batch, const 
                     float scale, void* O, int64_t ldo, float* lse, void* ws, size_t ws_bytes, void* stream);
 
 /*
+ * The same attention where sequences share a long prefix: many questions about one image, one document.  Sequence b has its first
+ * shared_len[b] keys in the pages of sequence leader[b], the first of its group (leader[b] == b there); a group's sequences stand side
+ * by side in the batch.  Every sequence's page list names the shared pages as well, so the result is mq_kv_attention's (up to the order of its
+ * float32 sums), but the shared keys are read, and multiplied with all rows of the group, once.  Shared are whole pages, at most as
+ * many as every sequence of the group with new rows has cached in front of them; what is left, and groups with fewer than two such
+ * sequences, or whose leaders do not say what is written here, every sequence reads by itself.  Shared pages are taken from the first
+ * sequence's list.
+ *   leader, shared_len  device int32 [n_seq];  n_seq <= 1024, total_q * n_q_heads <= 2^30
+ * ws as for mq_kv_attention, of mq_kv_attention_shared_workspace_bytes(): it holds a float32 result per query row and key list.
+ */
+size_t mq_kv_attention_shared_workspace_bytes(const mq_kv_batch* batch, const mq_kv_cache* cache, int32_t n_q_heads);
+int mq_kv_attention_shared(const void* Q, int64_t ldq, const mq_kv_batch* batch, const int32_t* leader, const int32_t* shared_len,
+                           const mq_kv_cache* cache, int32_t n_q_heads, float scale, void* O, int64_t ldo, float* lse, void* ws,
+                           size_t ws_bytes, void* stream);
+
+/*
  * The softmax weight that every key received from this call's rows, added to what it had:
  *   W_out[b, g, j] = (W_in[b, g, j] if key j was cached before this chunk, else 0)
  *                    + sum over the chunk's rows i that see j and the query heads h of g of exp(scale * Q[i, h] . K[j, g] - lse[i, h])

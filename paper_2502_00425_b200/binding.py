@@ -115,6 +115,8 @@ def load(build_if_missing: bool = False):
                                              vp, i64, kvcp, vp, vp]),
         "mq_kv_attention_workspace_bytes": (sz, [kvbp, kvcp, i32]),
         "mq_kv_attention": (C.c_int, [vp, i64, kvbp, kvcp, i32, f32, vp, i64, vp, vp, sz, vp]),
+        "mq_kv_attention_shared_workspace_bytes": (sz, [kvbp, kvcp, i32]),
+        "mq_kv_attention_shared": (C.c_int, [vp, i64, kvbp, vp, vp, kvcp, i32, f32, vp, i64, vp, vp, sz, vp]),
         "mq_kv_weights": (C.c_int, [vp, i64, kvbp, kvcp, i32, f32, vp, vp, vp, i64, i64, i32, vp, vp]),
         "mq_kv_plan": (C.c_int, [C.POINTER(mq_kv_state), vp, vp, i32, vp, vp, vp, vp, vp]),
         "mq_sample": (C.c_int, [vp, i64, i32, i32, C.c_uint32, vp, vp, vp, vp, vp, vp, vp, vp, vp]),
@@ -157,7 +159,8 @@ EXPORTED = ["mq_version", "mq_status_string", "mq_workspace_bytes", "mq_w4_layou
             "mq_ubench_mma_i8", "mq_selftest_bounded_wait", "mq_ubench_expand", "mq_calibrate_static_scales_bits",
             "mq_w8_layout_bytes", "mq_pack_w8", "mq_fwht_quant_bits", "mq_kron_quant_i8", "mq_glue_rmsnorm", "mq_glue_rope",
             "mq_glue_swiglu", "mq_glue_residual_add", "mq_aifs_attention_workspace_bytes", "mq_aifs_attention",
-            "mq_qk_norm_rope", "mq_qk_norm_rope_scaled", "mq_kv_attention_workspace_bytes", "mq_kv_attention", "mq_kv_weights", "mq_kv_evict", "mq_sample", "mq_kv_plan"]
+            "mq_qk_norm_rope", "mq_qk_norm_rope_scaled", "mq_kv_attention_workspace_bytes", "mq_kv_attention", "mq_kv_weights", "mq_kv_evict", "mq_sample", "mq_kv_plan",
+            "mq_kv_attention_shared_workspace_bytes", "mq_kv_attention_shared"]
 
 
 def status_string(status: int) -> str:
@@ -686,6 +689,37 @@ def mq_kv_attention(q, cu_q, kv_len, page_table, cache: KVCache, n_q_heads, max_
     _kv_call(d, load().mq_kv_attention, "mq_kv_attention", pq, ldq, C.byref(b), cache.ref, n_q_heads,
              cache.head_dim ** -0.5 if scale is None else scale, po, ldo, _vec(lse, _F32, rows * n_q_heads, d),
              _vec(ws, torch.uint8, size, d), size)
+
+
+def mq_kv_attention_shared_workspace_bytes(n_seq, total_q, max_q, max_pages, n_q_heads, cache: KVCache) -> int:
+    b = mq_kv_batch(n_seq, total_q, max_q, max_pages, 1, 1, 1, None)   # the arrays are not read for the size
+    return int(load().mq_kv_attention_shared_workspace_bytes(C.byref(b), C.byref(cache.c), n_q_heads))
+
+
+def new_kv_attention_shared_workspace(n_seq, total_q, max_q, max_pages, n_q_heads, cache: KVCache) -> torch.Tensor:
+    """Allocates (with torch) and clears a workspace for mq_kv_attention_shared calls up to these bounds."""
+    with torch.cuda.device(cache.device):
+        n = mq_kv_attention_shared_workspace_bytes(n_seq, total_q, max_q, max_pages, n_q_heads, cache)
+        if n == 0:
+            raise MqError(MQ_ERR_INVALID_ARG, "mq_kv_attention_shared_workspace_bytes")
+        ws = torch.empty(n, dtype=torch.uint8, device=cache.device)
+        _check(load().mq_reset_device_status(_ptr(ws), _stream()), "mq_reset_device_status")
+    return ws
+
+
+def mq_kv_attention_shared(q, cu_q, kv_len, page_table, leader, shared_len, cache: KVCache, n_q_heads, max_q, o, ws, lse=None, perm=None,
+                           scale=None):
+    """mq_kv_attention for sequences that share their first shared_len[b] keys with sequence leader[b] (int32 [n_seq]): the shared keys are
+    read once per group.  See include/mq.h."""
+    rows = q.shape[0]
+    shape, d = (rows, n_q_heads * cache.head_dim), cache.index
+    pq, ldq = _rows(q, shape, d)
+    po, ldo = _rows(o, shape, d)
+    size = ws.numel()
+    b = _kv_batch(cu_q, kv_len, page_table, rows, max_q, perm, d)
+    _kv_call(d, load().mq_kv_attention_shared, "mq_kv_attention_shared", pq, ldq, C.byref(b), _vec(leader, _I32, b.n_seq, d),
+             _vec(shared_len, _I32, b.n_seq, d), cache.ref, n_q_heads, cache.head_dim ** -0.5 if scale is None else scale, po, ldo,
+             _vec(lse, _F32, rows * n_q_heads, d), _vec(ws, torch.uint8, size, d), size)
 
 
 def _weights(w, n_seq, n_kv_heads, device):

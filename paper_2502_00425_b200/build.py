@@ -11,7 +11,8 @@ ROOT = os.path.dirname(PKG_DIR)
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libmq.so")
 SOURCES = ["mq_api.cu", "mq_fwht_quant.cu", "mq_pack.cu", "mq_aifs.cu", "mq_gemm.cu", "mq_noalloc.cu", "mq_rms.cu", "mq_gemv.cu", "mq_dynquant.cu", "mq_probe.cu", "mq_kron.cu", "mq_glue.cu", "mq_attn.cu", "mq_kv_append.cu",
-           "mq_kv_attn.cu", "mq_kv_chunk.cu", "mq_kv_weights.cu", "mq_kv_weights_chunk.cu", "mq_kv_evict.cu", "mq_sample.cu", "mq_kv_plan.cu"]
+           "mq_kv_attn.cu", "mq_kv_chunk.cu", "mq_kv_weights.cu", "mq_kv_weights_chunk.cu", "mq_kv_evict.cu", "mq_sample.cu", "mq_kv_plan.cu",
+           "mq_kv_shared.cu"]
 
 
 def _nvcc() -> str:
@@ -33,7 +34,7 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
     """Compile csrc/*.cu into paper_2502_00425_b200/libmq.so; returns its path."""
     if not force and not _stale():
         return LIB_PATH
-    cmd = [_nvcc(), "-shared", "-Xcompiler", "-fPIC", "-std=c++17", "-O3", "-lineinfo",
+    cmd = [_nvcc(), "-t", "0", "-shared", "-Xcompiler", "-fPIC", "-std=c++17", "-O3", "-lineinfo",
            "-gencode", "arch=compute_100a,code=sm_100a",
            "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-o", LIB_PATH]
     if verbose:

@@ -52,7 +52,7 @@ constexpr int decode_ctas(int dim, bool i8, int n) {
                     : (i8 ? (n == 1 ? Cfg<64, true, 1>::kCtas : Cfg<64, true, 2>::kCtas) : (n == 1 ? Cfg<64, false, 1>::kCtas : Cfg<64, false, 2>::kCtas));
 }
 
-template <int kD, bool kI8, int kN>
+template <int kD, bool kI8, int kN, KvMode kMode>
 __global__ void __launch_bounds__(kThreads, (Cfg<kD, kI8, kN>::kCtas))
 kv_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ KvAttnArgs p) {
   using C = Cfg<kD, kI8, kN>;
@@ -67,6 +67,7 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
   __shared__ int64_t red[kWarps];
   int64_t* prefix = reinterpret_cast<int64_t*>(smem + kWarps * C::kRing);
   KvSeq* seqs = reinterpret_cast<KvSeq*>(prefix + p.sched.b.n_seq + 1);
+  int* page0 = reinterpret_cast<int*>(seqs + p.sched.b.n_seq);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quad = lane >> 2, t4 = lane & 3;
   if (threadIdx.x == 0) {
     abort_flag = 0;
@@ -76,7 +77,8 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
   pdl_launch_dependents();
   pdl_wait();
   const KvSchedArgs& sc = p.sched;
-  sched_prefix<kThreads>(sc, prefix, red, seqs);
+  sched_prefix<kThreads, kMode>(sc, prefix, red, seqs, page0);
+  kv_clear_refs<kMode>(p.whole);
   const int64_t total = prefix[sc.b.n_seq];
   const int64_t share = sched_share(sc, total, gridDim.x);
   KvRecord rec{};
@@ -86,15 +88,15 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
   uint32_t asked = 0, taken = 0;   // tiles of this warp so far (ring positions and phases run on over units)
   bool ok = true;
   while (at < stop) {
-    const KvUnit u = sched_unit(sc, prefix, at, seqs);
+    const KvUnit u = sched_unit<kMode>(sc, prefix, at, seqs);
     const int len = (int)min((int64_t)(u.tiles + sc.extra - u.skip), stop - at);   // of this range on the line
     const int t0 = max(0, u.skip - sc.extra), t1 = max(0, u.skip + len - sc.extra);
     const int64_t unit_at = at - u.skip;
     at += len;
     if (t0 == t1) continue;   // the range ends before the unit's first tile
-    const int end = sched_end(sc, u.s, u.rb), ctx = u.s.n_all - u.s.n_new;
+    const int end = sched_end<kMode>(sc, u.s, u.rb), ctx = kMode == kPrefix ? end : u.s.n_all - u.s.n_new;
     const int row0 = u.rb * kRows, n_rows = min(kRows, u.s.n_new * sc.group.d - row0);
-    const int32_t* table = sc.b.page_table + (int64_t)u.b * sc.b.max_pages;
+    const int32_t* table = sc.b.page_table + (int64_t)u.b * sc.b.max_pages + (kMode == kOwn ? page0[u.b] : 0);
 
     // ---- the warp's stream of tiles: tile t holds keys (t * kWarps + warp) * 16 ..; tiles behind the last key are not asked for
     const int first_key = (t0 * kWarps + warp) * 16;
@@ -130,17 +132,17 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
     float fac[kN][2];               // scores -> log2 units, rows 2 t4 and 2 t4 + 1 of block nt
     int lim[kN][2];                 // how far these rows see: without perm, keys below lim; with it, the context and the chunk's
                                     // rows whose index is at most lim
-    const int32_t* perm = sc.b.perm ? sc.b.perm + u.s.begin : nullptr;
+    const int32_t* perm = kMode != kPrefix && sc.b.perm ? sc.b.perm + u.s.begin : nullptr;
 #pragma unroll
     for (int nt = 0; nt < kN; ++nt) {
       finish_query<kD, kI8>(t4, p.scale * 1.4426950408889634f * k_scale, qf[nt], fac[nt]);
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const int rr = 8 * nt + 2 * t4 + e, tk = (row0 + rr) / sc.group;
-        lim[nt][e] = rr >= n_rows ? INT_MIN : perm ? perm[tk] : ctx + tk + 1;
+        lim[nt][e] = rr >= n_rows ? INT_MIN : kMode == kPrefix ? end : perm ? perm[tk] : ctx + tk + 1;
       }
     }
-    const int all_see = perm ? ctx : min(end, ctx + row0 / sc.group + 1);   // every row of the unit sees the keys below
+    const int all_see = kMode == kPrefix ? end : perm ? ctx : min(end, ctx + row0 / sc.group + 1);   // every row of the unit sees the keys below
     auto sees = [&](int key, int lm) -> bool {
       if (key >= end || lm == INT_MIN) return false;
       if (!perm) return key < lm;
@@ -342,6 +344,12 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
     __syncthreads();
     const bool whole = t0 == 0 && t1 == u.tiles;
     const int slot = 2 * (int)blockIdx.x + (t0 == 0 ? 1 : 0);
+    int n_parts = 0;
+    if (t0 == 0 && !whole) {
+      // the pieces end with the worker whose range holds the unit's last tile
+      const int64_t last = unit_at + sc.extra + u.tiles - 1;
+      n_parts = (last >> 31 ? (int)(last / share) : (int)((uint32_t)last / (uint32_t)share)) - (int)blockIdx.x + 1;
+    }
     constexpr int kColThreads = kD / 2;                 // two channels per thread
     const int col = ((int)threadIdx.x % kColThreads) * 2;
     for (int r = (int)threadIdx.x / kColThreads; r < n_rows; r += kThreads / kColThreads) {
@@ -357,8 +365,14 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
         const float2 v = *reinterpret_cast<const float2*>(reinterpret_cast<const float*>(smem) + (w * kRows + r) * C::kPitch + col);
         if (f != 0.0f) { x = fmaf(f, v.x, x); y = fmaf(f, v.y, y); }
       }
-      if (whole) {
-        const int tk = (row0 + r) / sc.group, tok = u.s.begin + tk, head = u.g * sc.group.d + (row0 + r) - tk * sc.group.d;
+      const int tk = (row0 + r) / sc.group, tok = u.s.begin + tk, head = u.g * sc.group.d + (row0 + r) - tk * sc.group.d;
+      if (kMode != kPlain && t0 == 0 && col == 0)
+        p.whole.ref[(int64_t)tok * p.out.n_q_heads + head] = KvRowRef{(int)blockIdx.x, n_parts, r, kMode == kOwn && page0[u.b] > 0};
+      if (whole && kMode != kPlain) {
+        const int64_t at_row = (int64_t)tok * p.out.n_q_heads + head;
+        if (col == 0) p.whole.ml[at_row] = make_float2(mm, ll);
+        *reinterpret_cast<float2*>(p.whole.o + at_row * kD + col) = make_float2(x * v_scale, y * v_scale);
+      } else if (whole) {
         const float inv = ll == 0.0f ? 0.0f : v_scale / ll;
         *reinterpret_cast<__nv_bfloat162*>(p.out.O + (int64_t)tok * p.out.ldo + (int64_t)head * kD + col) =
             __floats2bfloat162_rn(x * inv, y * inv);
@@ -369,10 +383,8 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
         *reinterpret_cast<float2*>(p.parts.o + ((int64_t)slot * kRows + r) * kD + col) = make_float2(x * v_scale, y * v_scale);
       }
     }
-    if (t0 == 0 && !whole) {
-      // the pieces end with the worker whose range holds the unit's last tile
-      const int64_t last = unit_at + sc.extra + u.tiles - 1;
-      rec.n_parts = (last >> 31 ? (int)(last / share) : (int)((uint32_t)last / (uint32_t)share)) - (int)blockIdx.x + 1;
+    if (n_parts) {
+      rec.n_parts = n_parts;
       rec.begin = u.s.begin; rec.row0 = row0; rec.n_rows = n_rows; rec.g = u.g;
     }
     fence_proxy_async_smem();   // (the rings are next written by TMA)
@@ -382,7 +394,7 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
     for (; taken < asked; ++taken) mbar_wait_drain(&full[warp][taken % C::kStages], (taken / C::kStages) & 1u, 20000ull);
     rec = KvRecord{};
   }
-  if (threadIdx.x == 0) p.parts.rec[blockIdx.x] = rec;
+  if (kMode == kPlain && threadIdx.x == 0) p.parts.rec[blockIdx.x] = rec;
 }
 
 // Joins the pieces of the units that are split.  kWarps warps share a row and take every kWarps-th piece: four where
@@ -487,22 +499,28 @@ kv_combine_kernel(const int pitch, const FastDiv group, const KvParts parts, con
     out.lse[(int64_t)tok * out.n_q_heads + head] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
 }
 
-template <int kD, bool kI8, int kN>
+template <int kD, bool kI8, int kN, KvMode kMode>
 int launch_decode(const KvAttnArgs& a, int workers, cudaStream_t st) {
   using C = Cfg<kD, kI8, kN>;
-  const size_t smem = C::kSmem + ((size_t)a.sched.b.n_seq + 1) * (sizeof(int64_t) + sizeof(KvSeq));
+  const size_t smem = C::kSmem + ((size_t)a.sched.b.n_seq + 1) * (sizeof(int64_t) + kSeqBytes<kMode>);
   static PerDeviceTable<char> attr_set;
-  if (!ensure_dynamic_smem(attr_set, kv_decode_kernel<kD, kI8, kN>, C::kSmem + (kMaxKvSeqs + 1) * (int)(sizeof(int64_t) + sizeof(KvSeq)))) return MQ_ERR_CUDA;
+  if (!ensure_dynamic_smem(attr_set, kv_decode_kernel<kD, kI8, kN, kMode>, C::kSmem + (kMaxKvSeqs + 1) * (int)(sizeof(int64_t) + sizeof(KvSeq)))) return MQ_ERR_CUDA;
   CUtensorMap mk, mv;
   if (!encode_key_tiles(&mk, a.cache.K, a.Q, a.cache, kD, kI8) || !encode_key_tiles(&mv, a.cache.V, a.Q, a.cache, kD, kI8)) return MQ_ERR_CUDA;
-  const cudaError_t e = launch_pdl(kv_decode_kernel<kD, kI8, kN>, dim3((unsigned)workers), dim3(kThreads), smem, st, mk, mv, a);
+  const cudaError_t e = launch_pdl(kv_decode_kernel<kD, kI8, kN, kMode>, dim3((unsigned)workers), dim3(kThreads), smem, st, mk, mv, a);
   if (e != cudaSuccess) return cuda_status(e);
   return cuda_status(cudaGetLastError());
 }
-template <int kD, bool kI8>
-int launch_decode(const KvAttnArgs& a, int workers, cudaStream_t st) {
-  return a.sched.rows == 8 ? launch_decode<kD, kI8, 1>(a, workers, st) : launch_decode<kD, kI8, 2>(a, workers, st);
+template <int kD, bool kI8, int kN>
+int launch_decode(const KvAttnArgs& a, KvMode mode, int workers, cudaStream_t st) {
+  return mode == kPlain ? launch_decode<kD, kI8, kN, kPlain>(a, workers, st)
+         : mode == kPrefix ? launch_decode<kD, kI8, kN, kPrefix>(a, workers, st) : launch_decode<kD, kI8, kN, kOwn>(a, workers, st);
 }
+template <int kD, bool kI8>
+int launch_decode(const KvAttnArgs& a, KvMode mode, int workers, cudaStream_t st) {
+  return a.sched.rows == 8 ? launch_decode<kD, kI8, 1>(a, mode, workers, st) : launch_decode<kD, kI8, 2>(a, mode, workers, st);
+}
+static_assert(kMaxSharedSeqs * (8 + kSeqBytes<kOwn>) <= kMaxKvSeqs * (8 + (int)sizeof(KvSeq)), "the limit above holds for all modes");
 
 // Which kernel, and how many workers.  Up to kFewRows query rows per key/value head (tokens x heads of the group) take the
 // kernel above in blocks of 8 or 16 rows, more take the 128-row tensor-memory kernel of mq_kv_chunk.cu.  Both in us, heads
@@ -510,25 +528,43 @@ int launch_decode(const KvAttnArgs& a, int workers, cudaStream_t st) {
 // 12 / 19, over 16 x 2000 30 / 31, over 16 x 8000 94 / 68; 56 rows 13 / 19, 47 / 31 and 164 / 68.  The lengths are not known
 // on the host, so the rule is the rows at which the middle is a draw.
 constexpr int kFewRows = 32;
-struct Plan {
-  bool chunk;
-  int workers, rows, pitch, tile, extra;
-};
-Plan attn_plan(const mq_kv_batch* b, const mq_kv_cache* c, int group) {
-  Plan p{};
+}  // namespace
+
+KvPlan kv_plan_attention(const mq_kv_batch* b, const mq_kv_cache* c, int group, int64_t n_lists, int64_t max_q) {
+  KvPlan p{};
   // (a token's heads have to fit into a block of that kernel)
-  p.chunk = (int64_t)b->max_q * group > kFewRows && group <= 128;
+  p.chunk = max_q * group > kFewRows && group <= 128;
   if (p.chunk) kv_chunk_shape(group, &p.rows, &p.pitch, &p.tile, &p.extra);
-  else p.rows = p.pitch = (int64_t)b->max_q * group <= 8 ? 8 : 16, p.tile = kTile, p.extra = kExtra;
-  const int64_t blocks = ((int64_t)b->max_q * group + p.rows - 1) / p.rows;
+  else p.rows = p.pitch = max_q * group <= 8 ? 8 : 16, p.tile = kTile, p.extra = kExtra;
+  const int64_t blocks = (max_q * group + p.rows - 1) / p.rows;
   const int64_t tiles = (((int64_t)b->max_pages * c->page_size) + p.tile - 1) / p.tile;
-  const int64_t most = (int64_t)b->n_seq * c->n_kv_heads * blocks * (tiles > 0 ? tiles : 1);
+  const int64_t most = n_lists * c->n_kv_heads * blocks * (tiles > 0 ? tiles : 1);
   const int64_t cap = (int64_t)sm_count() * (p.chunk ? 1 : decode_ctas(c->head_dim, (c->flags & MQ_KV_INT8) != 0, p.rows / 8));
   p.workers = (int)(most < cap ? (most > 0 ? most : 1) : cap);
   return p;
 }
 
-int check_attention(const mq_kv_batch* batch, const mq_kv_cache* cache, int32_t n_q_heads, KvBatchView* bv, KvView* cv) {
+void kv_set_plan(KvAttnArgs* a, const KvPlan& p, const mq_kv_cache* cache, int max_q, int group) {
+  a->sched.page_shift = a->cache.page_shift;
+  a->sched.max_q = max_q;
+  a->sched.group = fast_div(group);
+  a->sched.by_rows = fast_div(p.rows);
+  a->sched.n_kv = cache->n_kv_heads;
+  a->sched.rows = p.rows;
+  a->sched.pitch = p.pitch;
+  a->sched.tile = p.tile;
+  a->sched.tile_shift = 31 - __builtin_clz((unsigned)p.tile);
+  a->sched.extra = p.extra;
+  a->sched.min_len = p.chunk ? p.extra + 2 : kMinLen;
+}
+
+int launch_kv_lines(const KvAttnArgs& a, const KvPlan& p, KvMode mode, int dim, bool i8, cudaStream_t st) {
+  if (p.chunk) return launch_kv_chunk(a, mode, dim, i8, p.workers, st);
+  if (dim == 128) return i8 ? launch_decode<128, true>(a, mode, p.workers, st) : launch_decode<128, false>(a, mode, p.workers, st);
+  return i8 ? launch_decode<64, true>(a, mode, p.workers, st) : launch_decode<64, false>(a, mode, p.workers, st);
+}
+
+int check_kv_attention(const mq_kv_batch* batch, const mq_kv_cache* cache, int32_t n_q_heads, KvBatchView* bv, KvView* cv) {
   int rc = check_kv_cache(cache, cv);
   if (rc != MQ_OK) return rc;
   if ((rc = check_kv_batch(batch, bv)) != MQ_OK) return rc;
@@ -537,8 +573,6 @@ int check_attention(const mq_kv_batch* batch, const mq_kv_cache* cache, int32_t 
   if ((int64_t)batch->max_q * (n_q_heads / cache->n_kv_heads) > (1 << 30)) return MQ_ERR_UNSUPPORTED;
   return MQ_OK;
 }
-
-}  // namespace
 
 namespace {
 template <int kD, int kW>
@@ -569,15 +603,15 @@ using namespace mq;
 extern "C" size_t mq_kv_attention_workspace_bytes(const mq_kv_batch* batch, const mq_kv_cache* cache, int32_t n_q_heads) {
   KvBatchView bv;
   KvView cv;
-  if (check_attention(batch, cache, n_q_heads, &bv, &cv) != MQ_OK) return 0;
-  const Plan p = attn_plan(batch, cache, n_q_heads / cache->n_kv_heads);
+  if (check_kv_attention(batch, cache, n_q_heads, &bv, &cv) != MQ_OK) return 0;
+  const KvPlan p = kv_plan_attention(batch, cache, n_q_heads / cache->n_kv_heads, batch->n_seq, batch->max_q);
   return kStatusBytes + kv_parts_bytes(p.workers, p.pitch, cache->head_dim);
 }
 
 extern "C" int mq_kv_attention(const void* Q, int64_t ldq, const mq_kv_batch* batch, const mq_kv_cache* cache, int32_t n_q_heads,
                                float scale, void* O, int64_t ldo, float* lse, void* ws, size_t ws_bytes, void* stream) {
   KvAttnArgs a{};
-  const int rc = check_attention(batch, cache, n_q_heads, &a.sched.b, &a.cache);
+  const int rc = check_kv_attention(batch, cache, n_q_heads, &a.sched.b, &a.cache);
   if (rc != MQ_OK) return rc;
   if (!(scale > 0.0f) || !std::isfinite(scale)) return MQ_ERR_INVALID_ARG;
   const int64_t width = (int64_t)n_q_heads * cache->head_dim;
@@ -585,21 +619,11 @@ extern "C" int mq_kv_attention(const void* Q, int64_t ldq, const mq_kv_batch* ba
   if (batch->n_seq == 0 || batch->total_q == 0 || batch->max_q == 0) return MQ_OK;
   if (!Q || !O || !ws) return MQ_ERR_INVALID_ARG;
   if (!kv_aligned16(Q) || !kv_aligned16(O) || ldq % 8 || ldo % 8 || (reinterpret_cast<uintptr_t>(ws) & 255u)) return MQ_ERR_ALIGNMENT;
-  const Plan p = attn_plan(batch, cache, n_q_heads / cache->n_kv_heads);
+  const KvPlan p = kv_plan_attention(batch, cache, n_q_heads / cache->n_kv_heads, batch->n_seq, batch->max_q);
   if (ws_bytes < kStatusBytes + kv_parts_bytes(p.workers, p.pitch, cache->head_dim)) return MQ_ERR_WORKSPACE;
   a.Q = static_cast<const uint8_t*>(Q);
   a.ldq = ldq * 2;
-  a.sched.page_shift = a.cache.page_shift;
-  a.sched.max_q = batch->max_q;
-  a.sched.group = fast_div(n_q_heads / cache->n_kv_heads);
-  a.sched.by_rows = fast_div(p.rows);
-  a.sched.n_kv = cache->n_kv_heads;
-  a.sched.rows = p.rows;
-  a.sched.pitch = p.pitch;
-  a.sched.tile = p.tile;
-  a.sched.tile_shift = 31 - __builtin_clz((unsigned)p.tile);
-  a.sched.extra = p.extra;
-  a.sched.min_len = p.chunk ? p.extra + 2 : kMinLen;
+  kv_set_plan(&a, p, cache, batch->max_q, n_q_heads / cache->n_kv_heads);
   a.out.O = static_cast<__nv_bfloat16*>(O);
   a.out.ldo = ldo;
   a.out.lse = lse;
@@ -608,11 +632,7 @@ extern "C" int mq_kv_attention(const void* Q, int64_t ldq, const mq_kv_batch* ba
   a.scale = scale;
   a.status = static_cast<int32_t*>(ws);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const bool i8 = (cache->flags & MQ_KV_INT8) != 0;
-  int e;
-  if (p.chunk) e = launch_kv_chunk(a, cache->head_dim, i8, p.workers, st);
-  else if (cache->head_dim == 128) e = i8 ? launch_decode<128, true>(a, p.workers, st) : launch_decode<128, false>(a, p.workers, st);
-  else e = i8 ? launch_decode<64, true>(a, p.workers, st) : launch_decode<64, false>(a, p.workers, st);
+  const int e = launch_kv_lines(a, p, kPlain, cache->head_dim, (cache->flags & MQ_KV_INT8) != 0, st);
   if (e != MQ_OK) return e;
   return launch_kv_combine(a.sched, a.parts, a.out, p.workers, cache->head_dim, st);
 }

@@ -74,7 +74,9 @@ struct Piece {
   int t0, t1, end, ctx;
   int row0, n_rows;       // query rows of the unit
   int all_see;            // every row of the unit sees the keys below
-  int b, g, begin;
+  const int32_t* table;   // page of the piece's first key
+  int g, begin;
+  int more;               // kOwn: the rows see shared keys, too
   int whole;              // the piece is the whole unit
   int n_parts;            // of the unit, if this is its first piece
   int poison;             // values were taken out of its tiles
@@ -103,7 +105,7 @@ __device__ __forceinline__ uint64_t desc_n_major(uint32_t addr, uint32_t block_b
   return (uint64_t)((addr >> 4) & 0x3FFFu) | ((uint64_t)(block_bytes >> 4) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
 }
 
-template <int kD, bool kI8>
+template <int kD, bool kI8, KvMode kMode>
 __global__ void __launch_bounds__(ChunkCfg<kD, kI8>::kThreads, 1)
 kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
                 const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ KvAttnArgs p) {
@@ -119,7 +121,8 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
   int32_t* kp_all = reinterpret_cast<int32_t*>(ring + kRing);   // [8 warps][128]
   int64_t* red = reinterpret_cast<int64_t*>(kp_all + 8 * kTile);
   int64_t* prefix = red + 16;
-  KvSeq* seqs = p.sched.b.n_seq <= kSeqsHeld ? reinterpret_cast<KvSeq*>(prefix + p.sched.b.n_seq + 1) : nullptr;
+  KvSeq* seqs = kMode != kPlain || p.sched.b.n_seq <= kSeqsHeld ? reinterpret_cast<KvSeq*>(prefix + p.sched.b.n_seq + 1) : nullptr;
+  int* page0 = reinterpret_cast<int*>(seqs + p.sched.b.n_seq);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
@@ -155,7 +158,8 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
   pdl_wait();
   const KvSchedArgs& sc = p.sched;
   tc_fence_before();
-  sched_prefix<C::kThreads>(sc, prefix, red, seqs);   // (ends with __syncthreads)
+  kv_clear_refs<kMode>(p.whole);
+  sched_prefix<C::kThreads, kMode>(sc, prefix, red, seqs, page0);   // (ends with __syncthreads)
   tc_fence_after();
   const uint32_t tmem_base = *reinterpret_cast<volatile uint32_t*>(&sh->tmem_base);
   const int block_rows = sc.rows >> 1;          // rows of a block: whole tokens
@@ -179,7 +183,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
     for (int np = 0; ok; ++np) {
       const Piece* pc = get_piece(np, ok, 50);
       if (!(ok = warp_all(ok)) || !pc) break;
-      const int32_t* table = sc.b.page_table + (int64_t)pc->b * sc.b.max_pages;
+      const int32_t* table = pc->table;
       const int t1 = pc->t1, end = pc->end, g = pc->g, outside = max(p.cache.n_pages, 1);   // (a page number the map does not have)
       auto page_of = [&](int tile) -> int {
         const int key = tile * kTile + lane * rows;
@@ -326,19 +330,20 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
     while (ok) {
       Piece pc{};
       while (at < stop) {
-        const KvUnit u = sched_unit(sc, prefix, at, seqs);
+        const KvUnit u = sched_unit<kMode>(sc, prefix, at, seqs);
         const int len = (int)min((int64_t)(u.tiles + sc.extra - u.skip), stop - at);
         pc.t0 = max(0, u.skip - sc.extra);
         pc.t1 = max(0, u.skip + len - sc.extra);
         const int64_t unit_at = at - u.skip;
         at += len;
         if (pc.t0 >= pc.t1) continue;
-        pc.end = sched_end(sc, u.s, u.rb);
-        pc.ctx = u.s.n_all - u.s.n_new;
+        pc.end = sched_end<kMode>(sc, u.s, u.rb);
+        pc.ctx = kMode == kPrefix ? pc.end : u.s.n_all - u.s.n_new;
         pc.row0 = u.rb * sc.rows;
         pc.n_rows = min(sc.rows, u.s.n_new * group - pc.row0);
-        pc.all_see = sc.b.perm ? pc.ctx : min(pc.end, pc.ctx + pc.row0 / sc.group + 1);
-        pc.b = u.b;
+        pc.all_see = kMode == kPrefix || sc.b.perm ? pc.ctx : min(pc.end, pc.ctx + pc.row0 / sc.group + 1);
+        pc.table = sc.b.page_table + (int64_t)u.b * sc.b.max_pages + (kMode == kOwn ? page0[u.b] : 0);
+        pc.more = kMode == kOwn && page0[u.b] > 0;
         pc.g = u.g;
         pc.begin = u.s.begin;
         pc.whole = pc.t0 == 0 && pc.t1 == u.tiles;
@@ -374,7 +379,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
     if (!ok)
       for (int k = 0; k < 2; ++k)
         if (nq[k]) mbar_wait_drain(&sh->q_full[k], (uint32_t)(nq[k] - 1) & 1u, 20000ull);
-    if (lane == 0) p.parts.rec[blockIdx.x] = rec;
+    if (kMode == kPlain && lane == 0) p.parts.rec[blockIdx.x] = rec;
   } else if (!kI8 && warp == 3) {
     // ---------------- looks through value tiles that not all rows see in full
     const int shift = p.cache.page_shift, rows = shift >= 7 ? kTile : 1 << shift;   // (of a box)
@@ -465,11 +470,11 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
       }
       const bool live = row < block_rows && unit_row < pc->n_rows;
       const int ctx = pc->ctx, end = pc->end, t1 = pc->t1;
-      const int32_t* perm = sc.b.perm ? sc.b.perm + pc->begin : nullptr;
+      const int32_t* perm = kMode != kPrefix && sc.b.perm ? sc.b.perm + pc->begin : nullptr;
       const int tok = live ? (pc->row0 + unit_row) / sc.group : 0;
-      const int all_see = perm ? ctx : min(end, ctx + (pc->row0 + grp * block_rows) / sc.group + 1);   // of this block
+      const int all_see = kMode == kPrefix ? end : perm ? ctx : min(end, ctx + (pc->row0 + grp * block_rows) / sc.group + 1);   // of this block
       // live rows: without perm, keys below lim; with it, the context and the chunk's rows whose index is at most lim
-      const int lim = perm ? (live ? perm[tok] : INT_MIN) : live ? min(end, ctx + tok + 1) : 0;
+      const int lim = kMode == kPrefix ? (live ? end : 0) : perm ? (live ? perm[tok] : INT_MIN) : live ? min(end, ctx + tok + 1) : 0;
       // The maximum is found before the scale is applied, and a masked score is -inf times it: both want a positive scale. A head
       // whose static scale is not one (zero where every key was zero) has its scores scaled first.
       const float given = p.scale * 1.4426950408889634f * (kI8 ? p.cache.k_scale[pc->g] : 1.0f);
@@ -580,17 +585,18 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
       if (ok) ok = warp_all(mbar_wait(&sh->pv_done[2 * grp + 1], (cnt - 1) & 1u, &sh->abort_flag, p.status, 63));
       if (!ok) break;
       tc_fence_after();
-      const bool whole = pc->whole != 0;
+      const bool whole = pc->whole != 0, bf16_out = whole && kMode == kPlain;
       const float vsc = kI8 ? p.cache.v_scale[pc->g] : 1.0f;
-      const float w = whole ? (l_run != 0.0f ? vsc / l_run : 0.0f) : vsc;
+      const float w = bf16_out ? (l_run != 0.0f ? vsc / l_run : 0.0f) : vsc;
       const int64_t at_part = (int64_t)(2 * (int)blockIdx.x + (pc->t0 == 0 ? 1 : 0)) * kPitch + unit_row;
       const int head = pc->g * sc.group.d + (pc->row0 + unit_row) - tok * sc.group.d;
-      const int64_t out_row = (int64_t)(pc->begin + tok);
+      const int64_t out_row = (int64_t)(pc->begin + tok), at_row = out_row * p.out.n_q_heads + head;
+      if (kMode != kPlain && live && pc->t0 == 0) p.whole.ref[at_row] = KvRowRef{(int)blockIdx.x, pc->n_parts, unit_row, pc->more};
       const bool poison = !kI8 && *reinterpret_cast<const volatile int*>(&pc->poison) != 0;
       // Four neighbouring lanes exchange 16-byte pieces so that they write 64 contiguous bytes of one row after the other (a
       // lane writing its own row makes every store instruction touch 32 lines: 10 instead of 4 k cycles per piece).
-      const uint8_t* mine = whole ? reinterpret_cast<const uint8_t*>(p.out.O + out_row * p.out.ldo + (int64_t)head * kD)
-                                  : reinterpret_cast<const uint8_t*>(p.parts.o + at_part * kD);
+      const uint8_t* mine = bf16_out ? reinterpret_cast<const uint8_t*>(p.out.O + out_row * p.out.ldo + (int64_t)head * kD)
+                            : reinterpret_cast<const uint8_t*>(whole ? p.whole.o + at_row * kD : p.parts.o + at_part * kD);
       uint8_t* dst[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k)
@@ -609,7 +615,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
           for (int key = first; key < last; ++key) {
             const bool sees = key < ctx || (perm ? perm[key - ctx] <= lim : key < lim);
             if (!sees) continue;
-            const int pg = sc.b.page_table[(int64_t)pc->b * sc.b.max_pages + (key >> p.cache.page_shift)];
+            const int pg = pc->table[key >> p.cache.page_shift];
             if ((unsigned)pg >= (unsigned)p.cache.n_pages) continue;
             const uint16_t* vr = reinterpret_cast<const uint16_t*>(p.cache.V + (int64_t)pg * p.cache.page_stride + (int64_t)pc->g * p.cache.head_stride +
                                                                   (int64_t)(key & ((1 << p.cache.page_shift) - 1)) * p.cache.slot_stride) + cb;
@@ -620,7 +626,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
             }
           }
         }
-        if (whole) {
+        if (bf16_out) {
           uint4 v[4];
 #pragma unroll
           for (int k = 0; k < 4; ++k)
@@ -647,7 +653,8 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
       if (live) {
         const float m = l_run != 0.0f ? m_used * scale_log2 : -INFINITY;
         if (!whole) p.parts.ml[at_part] = make_float2(m, l_run);
-        else if (p.out.lse) p.out.lse[out_row * p.out.n_q_heads + head] = l_run != 0.0f ? (m + log2f(l_run)) * 0.6931471805599453f : -INFINITY;
+        else if (kMode != kPlain) p.whole.ml[at_row] = make_float2(m, l_run);
+        else if (p.out.lse) p.out.lse[at_row] = l_run != 0.0f ? (m + log2f(l_run)) * 0.6931471805599453f : -INFINITY;
       }
       tc_fence_before();   // the accumulator has been read before the next piece's first product replaces it
       __syncwarp();
@@ -664,7 +671,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
     for (int np = 0; ok; ++np) {
       const Piece* pc = get_piece(np, ok, 65);
       if (!(ok = warp_all(ok)) || !pc) break;
-      const int32_t* table = sc.b.page_table + (int64_t)pc->b * sc.b.max_pages;
+      const int32_t* table = pc->table;
       const int t1 = pc->t1, end = pc->end;
       const int64_t head_off = (int64_t)pc->g * p.cache.head_stride;
       auto row_of = [&](int tile) -> int64_t {   // byte offset of this thread's row, -1 where it reads as zeros
@@ -734,19 +741,28 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
   }
 }
 
-template <int kD, bool kI8>
+template <int kD, bool kI8, KvMode kMode>
 int launch(const KvAttnArgs& a, int workers, cudaStream_t st) {
   using C = ChunkCfg<kD, kI8>;
-  static_assert(C::kSmem + (kMaxKvSeqs + 1) * 8 <= 232448 && C::kSmem + (kSeqsHeld + 1) * (8 + (int)sizeof(KvSeq)) <= 232448, "shared memory of one CTA");
+  constexpr int kHeld = kMode == kPlain ? kSeqsHeld : kMaxSharedSeqs, kPerSeq = (int)sizeof(int64_t) + kSeqBytes<kMode>;
+  constexpr int kMost = kMode != kPlain ? (kMaxSharedSeqs + 1) * kPerSeq
+                        : (kMaxKvSeqs + 1) * 8 > (kSeqsHeld + 1) * kPerSeq ? (kMaxKvSeqs + 1) * 8 : (kSeqsHeld + 1) * kPerSeq;
+  static_assert(C::kSmem + kMost <= 232448, "shared memory of one CTA");
   static PerDeviceTable<char> attr_set;
-  if (!ensure_dynamic_smem(attr_set, kv_chunk_kernel<kD, kI8>, C::kSmem + (kMaxKvSeqs + 1) * (int)sizeof(int64_t))) return MQ_ERR_CUDA;
+  if (!ensure_dynamic_smem(attr_set, kv_chunk_kernel<kD, kI8, kMode>, C::kSmem + kMost)) return MQ_ERR_CUDA;
   CUtensorMap mq_{}, mk{}, mv{};
   if (!encode_queries(&mq_, a.Q, a.ldq, a.out.n_q_heads, a.sched.b.total_q, a.sched.group.d, a.sched.rows / 2, kD)) return MQ_ERR_CUDA;
   if (!kI8 && (!encode_pages(&mk, a.cache.K, a.Q, a.cache, kD, kTile) || !encode_pages(&mv, a.cache.V, a.Q, a.cache, kD, kTile))) return MQ_ERR_CUDA;
-  const cudaError_t e = launch_pdl(kv_chunk_kernel<kD, kI8>, dim3((unsigned)workers), dim3(C::kThreads),
-                                   C::kSmem + ((size_t)a.sched.b.n_seq + 1) * (sizeof(int64_t) + (a.sched.b.n_seq <= kSeqsHeld ? sizeof(KvSeq) : 0)), st, mq_, mk, mv, a);
+  const size_t seqs = (size_t)a.sched.b.n_seq + 1;
+  const cudaError_t e = launch_pdl(kv_chunk_kernel<kD, kI8, kMode>, dim3((unsigned)workers), dim3(C::kThreads),
+                                   C::kSmem + seqs * (a.sched.b.n_seq <= kHeld ? kPerSeq : sizeof(int64_t)), st, mq_, mk, mv, a);
   if (e != cudaSuccess) return cuda_status(e);
   return cuda_status(cudaGetLastError());
+}
+template <int kD, bool kI8>
+int launch(const KvAttnArgs& a, KvMode mode, int workers, cudaStream_t st) {
+  return mode == kPlain ? launch<kD, kI8, kPlain>(a, workers, st)
+         : mode == kPrefix ? launch<kD, kI8, kPrefix>(a, workers, st) : launch<kD, kI8, kOwn>(a, workers, st);
 }
 
 }  // namespace
@@ -759,9 +775,9 @@ void kv_chunk_shape(int group, int* rows, int* pitch, int* tile, int* extra) {
   *extra = kExtraTiles;
 }
 
-int launch_kv_chunk(const KvAttnArgs& a, int dim, bool i8, int workers, cudaStream_t st) {
-  if (dim == 128) return i8 ? launch<128, true>(a, workers, st) : launch<128, false>(a, workers, st);
-  return i8 ? launch<64, true>(a, workers, st) : launch<64, false>(a, workers, st);
+int launch_kv_chunk(const KvAttnArgs& a, KvMode mode, int dim, bool i8, int workers, cudaStream_t st) {
+  if (dim == 128) return i8 ? launch<128, true>(a, mode, workers, st) : launch<128, false>(a, mode, workers, st);
+  return i8 ? launch<64, true>(a, mode, workers, st) : launch<64, false>(a, mode, workers, st);
 }
 
 }  // namespace mq

@@ -8,11 +8,17 @@
 // unit's tiles whole writes its output; otherwise it leaves a partial result (exponent reference, sum, unnormalised
 // output) in its slot and the combine kernel joins the slots in the order of the keys: no atomics, the result does
 // not depend on timing.
+//
+// Sequences that share a prefix (mq_kv_attention_shared) go over two lines, each with the same kernels: kPrefix has one unit line per group of
+// sequences, all of whose rows see all shared keys; kOwn has every sequence's keys behind them.  Both leave their results, whole or
+// in pieces, in the workspace, with a reference per row that says where, and one kernel joins them.
 #pragma once
 
 #include "mq_kv.cuh"
 
 namespace mq {
+
+enum KvMode { kPlain, kPrefix, kOwn };
 
 struct KvSchedArgs {
   KvBatchView b;
@@ -24,38 +30,90 @@ struct KvSchedArgs {
   int tile, tile_shift;   // keys of a tile (a power of two)
   int extra;       // a unit's cost besides its tiles, in tiles
   int min_len;     // a worker's range is at least this long (fewer workers for little work)
+  const int32_t *leader, *shared_len;   // kPrefix, kOwn: of every sequence, the first of its group and the keys shared with it
 };
 
 // Keys [0, end) that row block rb of a sequence may see any of, and the tiles that hold them (at least one: a unit that
 // sees nothing still has to write its zeros).  (Rows of a sequence, tokens x group, are below 2^30.)
+template <KvMode kMode = kPlain>
 __device__ __forceinline__ int sched_end(const KvSchedArgs& a, const KvSeq& s, int rb) {
-  if (a.b.perm) return s.n_all;
+  if (kMode == kPrefix || a.b.perm) return s.n_all;
   const int last = min((rb * a.rows + a.rows - 1) / a.group, s.n_new - 1);
   return max(0, min(s.n_all, s.n_all - s.n_new + last + 1));
 }
+template <KvMode kMode = kPlain>
 __device__ __forceinline__ int sched_tiles(const KvSchedArgs& a, const KvSeq& s, int rb) {
-  return max(1, (sched_end(a, s, rb) + a.tile - 1) >> a.tile_shift);
+  return max(1, (sched_end<kMode>(a, s, rb) + a.tile - 1) >> a.tile_shift);
 }
 __device__ __forceinline__ int sched_blocks(const KvSchedArgs& a, const KvSeq& s) {
   return (s.n_new * a.group.d + a.rows - 1) / a.by_rows;
 }
 
+// Shared memory of a sequence besides its place on the line: lengths, and for the lines of shared prefixes two numbers more
+template <KvMode kMode>
+constexpr int kSeqBytes = (int)sizeof(KvSeq) + (kMode == kPlain ? 0 : 8);
+constexpr int kMaxSharedSeqs = 1024;   // sequences of a call with shared prefixes: all of them are held in shared memory
+
+// What the groups share, and what follows from it for the line: seqs[b] becomes the group's rows and shared keys (kPrefix, at its
+// first sequence; the others have no rows) or the sequence with its own keys only, which begin at page page0[b] of its list (kOwn).  A
+// group shares whole pages, no more keys than any of its sequences with rows has cached, and nothing if it has fewer than two of
+// those or its sequences do not stand side by side behind the first.  `prefix` is scratch here.
+template <int kThreads, KvMode kMode>
+__device__ __forceinline__ void sched_groups(const KvSchedArgs& a, int64_t* prefix, KvSeq* seqs, int* page0) {
+  const int n = a.b.n_seq;
+  int* keys = page0 + n;                             // of the group that begins at b
+  int2* group = reinterpret_cast<int2*>(prefix);     // its sequences with rows, the last of them
+  for (int b = threadIdx.x; b < n; b += kThreads) {
+    seqs[b] = kv_seq(a.b, a.page_shift, a.max_q, b);
+    keys[b] = INT_MAX;
+    group[b] = make_int2(0, b);
+  }
+  __syncthreads();
+  for (int b = threadIdx.x; b < n; b += kThreads) {
+    const int l = a.leader[b];
+    if (l < 0 || l > b) continue;
+    if (a.leader[l] != l || (l < b && a.leader[b - 1] != l)) atomicMin(&keys[l], 0);
+    else if (seqs[b].n_new > 0) {
+      atomicMin(&keys[l], max(0, min(a.shared_len[b], seqs[b].n_all - seqs[b].n_new)));
+      atomicAdd(&group[l].x, 1);
+      atomicMax(&group[l].y, b);
+    }
+  }
+  __syncthreads();
+  for (int b = threadIdx.x; b < n; b += kThreads) {
+    const int l = a.leader[b];
+    const int pages = l >= 0 && l <= b && group[l].x > 1 ? keys[l] >> a.page_shift : 0;
+    page0[b] = kMode == kOwn ? pages : 0;
+    if (kMode == kOwn) {
+      seqs[b].n_all = max(0, seqs[b].n_all - (pages << a.page_shift));
+    } else if (l == b && pages > 0) {
+      const KvSeq last = kv_seq(a.b, a.page_shift, a.max_q, group[b].y);
+      seqs[b].n_new = last.begin + last.n_new - seqs[b].begin;
+      seqs[b].n_all = pages << a.page_shift;
+    } else {
+      seqs[b].n_new = 0;
+    }
+  }
+  __syncthreads();
+}
+
 // prefix[b] = length of all units before sequence b; prefix[n_seq] = the whole line.  Called by every thread of a block of kThreads;
 // `red` is shared scratch of kThreads / 32 entries.  `seqs`, if given, is shared memory that keeps the sequences' lengths for
 // sched_unit (a dependent global load per unit costs about as much as a tile).
-template <int kThreads>
-__device__ __forceinline__ void sched_prefix(const KvSchedArgs& a, int64_t* prefix, int64_t* red, KvSeq* seqs = nullptr) {
+template <int kThreads, KvMode kMode = kPlain>
+__device__ __forceinline__ void sched_prefix(const KvSchedArgs& a, int64_t* prefix, int64_t* red, KvSeq* seqs = nullptr, int* page0 = nullptr) {
+  if (kMode != kPlain) sched_groups<kThreads, kMode>(a, prefix, seqs, page0);
   const int n = a.b.n_seq, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int per = (n + kThreads - 1) / kThreads;
   int64_t sum = 0;
   for (int k = 0; k < per; ++k) {
     const int b = tid * per + k;
     if (b >= n) break;
-    const KvSeq s = kv_seq(a.b, a.page_shift, a.max_q, b);
-    if (seqs) seqs[b] = s;
+    const KvSeq s = kMode != kPlain ? seqs[b] : kv_seq(a.b, a.page_shift, a.max_q, b);
+    if (kMode == kPlain && seqs) seqs[b] = s;
     const int blocks = sched_blocks(a, s);
     int64_t t = 0;
-    if (a.b.perm) t = (int64_t)blocks * (blocks ? sched_tiles(a, s, 0) + a.extra : 0);
+    if (kMode == kPrefix || a.b.perm) t = (int64_t)blocks * (blocks ? sched_tiles<kMode>(a, s, 0) + a.extra : 0);
     else
       for (int rb = 0; rb < blocks; ++rb) t += sched_tiles(a, s, rb) + a.extra;
     sum += t * a.n_kv;
@@ -85,6 +143,7 @@ struct KvUnit {
   int b, g, rb, tiles, skip;
   KvSeq s;
 };
+template <KvMode kMode = kPlain>
 __device__ __forceinline__ KvUnit sched_unit(const KvSchedArgs& a, const int64_t* prefix, int64_t at, const KvSeq* seqs = nullptr) {
   int lo = 0, hi = a.b.n_seq;   // prefix[lo] <= at < prefix[hi]
   while (hi - lo > 1) {
@@ -106,9 +165,9 @@ __device__ __forceinline__ KvUnit sched_unit(const KvSchedArgs& a, const int64_t
     u.g = (int)((uint32_t)x / per_head);
     y = (uint32_t)x - (uint32_t)u.g * per_head;
   }
-  u.tiles = sched_tiles(a, u.s, 0);
+  u.tiles = sched_tiles<kMode>(a, u.s, 0);
   u.rb = 0;
-  if (a.b.perm) {
+  if (kMode == kPrefix || a.b.perm) {
     if (y >= u.tiles + a.extra) u.rb = (int)(y / (u.tiles + a.extra));
     y -= (int64_t)u.rb * (u.tiles + a.extra);
   } else {
@@ -164,6 +223,21 @@ struct KvOutArgs {
   int n_q_heads;
 };
 
+// Results of the lines of shared prefixes, which the join turns into the output.  Row = token x query heads + head.
+struct __align__(16) KvRowRef {
+  int worker;    // its first piece is in slot 2 worker + 1, the next ones in 2 (worker + 1), ..
+  int n_parts;   // 0: not in pieces, but in KvWhole; -1: the row belongs to no sequence
+  int row;       // of a slot
+  int more;      // kOwn: the row has a result over shared keys, too
+};
+struct KvWhole {
+  KvRowRef* ref;     // [rows]
+  KvRowRef* clear;   // kPrefix: the references of the other line, set to "no sequence" before it runs
+  int64_t n_rows;
+  float2* ml;        // [rows]
+  float* o;          // [rows][D], unnormalised
+};
+
 // joins the pieces of split units
 int launch_kv_combine(const KvSchedArgs& a, const KvParts& parts, const KvOutArgs& out, int workers, int dim, cudaStream_t st);
 
@@ -177,9 +251,28 @@ struct KvAttnArgs {
   KvParts parts;
   float scale;
   int32_t* status;
+  KvWhole whole;     // kPrefix, kOwn
 };
 
+// How a call's work is divided: which kernel, its units, its workers
+struct KvPlan {
+  bool chunk;
+  int workers, rows, pitch, tile, extra;
+};
+// n_lists lists of keys, each for at most max_q tokens
+KvPlan kv_plan_attention(const mq_kv_batch* b, const mq_kv_cache* c, int group, int64_t n_lists, int64_t max_q);
+void kv_set_plan(KvAttnArgs* a, const KvPlan& p, const mq_kv_cache* cache, int max_q, int group);
+int launch_kv_lines(const KvAttnArgs& a, const KvPlan& p, KvMode mode, int dim, bool i8, cudaStream_t st);
+int check_kv_attention(const mq_kv_batch* batch, const mq_kv_cache* cache, int32_t n_q_heads, KvBatchView* bv, KvView* cv);
+
+template <KvMode kMode>
+__device__ __forceinline__ void kv_clear_refs(const KvWhole& w) {
+  if (kMode == kPrefix)
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < w.n_rows; i += (int64_t)gridDim.x * blockDim.x)
+      w.clear[i] = KvRowRef{0, -1, 0, 0};
+}
+
 void kv_chunk_shape(int group, int* rows, int* pitch, int* tile, int* extra);
-int launch_kv_chunk(const KvAttnArgs& a, int dim, bool i8, int workers, cudaStream_t st);
+int launch_kv_chunk(const KvAttnArgs& a, KvMode mode, int dim, bool i8, int workers, cudaStream_t st);
 
 }  // namespace mq

@@ -127,3 +127,23 @@ def test_plan_oracle_by_hand():
     assert state["free"] == [4, 2, 1, 0] and state["borrowed"] == [0, 0]
     with pytest.raises(P.Refused):
         P.plan(state, [12, 12], None, 24, 4)
+
+
+# ------------------------------------------------------------------------------------------------ attention behind a shared prefix
+def test_shared_attention_refusals(lib):
+    def call(q=A, ldq=1024, hq=8, scale=0.1, o=A, ldo=1024, ws=A, wsb=1 << 40, leader=A, shared=A, cache=None, n_seq=2, total=5, max_q=4,
+             max_pages=7, cu=A, kv=A, table=A):
+        b = B.mq_kv_batch(n_seq, total, max_q, max_pages, cu, kv, table, None)
+        return lib.mq_kv_attention_shared(q, ldq, C.byref(b), leader, shared, C.byref(cache or _cache()), hq, scale, o, ldo, None, ws, wsb, None)
+
+    assert call(n_seq=-1) == call(max_q=6) == call(cu=None) == call(table=None) == call(hq=7) == B.MQ_ERR_INVALID_ARG
+    assert call(leader=None) == call(shared=None) == call(q=None) == call(o=None) == call(ws=None) == B.MQ_ERR_INVALID_ARG
+    assert call(n_seq=1025) == call(total=1 << 28, max_q=1, hq=8) == call(cache=_cache(dim=96)) == B.MQ_ERR_UNSUPPORTED
+    for bad in (0.0, -1.0, float("nan"), float("inf")):
+        assert call(scale=bad) == B.MQ_ERR_INVALID_ARG
+    assert call(ldq=1016) == call(ldo=512) == B.MQ_ERR_INVALID_ARG
+    assert call(q=A + 2) == call(o=A + 8) == call(ldq=1028) == call(ws=A + 16) == B.MQ_ERR_ALIGNMENT
+    size = lambda n=2, total=5, max_q=4: lib.mq_kv_attention_shared_workspace_bytes(C.byref(B.mq_kv_batch(n, total, max_q, 7, A, A, A, None)), C.byref(_cache()), 8)
+    assert size() > 2 * 5 * 8 * 128 * 4 and call(wsb=size() - 1) == B.MQ_ERR_WORKSPACE
+    assert size(n=1025) == size(max_q=6) == 0
+    assert call(n_seq=0, total=0, max_q=0) == call(total=0, max_q=0) == B.MQ_OK     # nothing to do
