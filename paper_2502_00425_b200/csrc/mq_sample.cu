@@ -6,16 +6,20 @@
 //
 // All three filters cut the order at one place, so the work is to find that place without sorting.
 //   * A row belongs to a cluster of up to 8 CTAs; each stages its slice in shared memory (a row too long for that is read again from L2), so the
-//     logits come from HBM once.  What the CTAs have to agree on (maximum, histograms, sums) goes through distributed shared memory.
+//     logits come from HBM once.  What the CTAs have to agree on goes through distributed shared memory.
 //   * Weights are fixed-point numbers of 43 bits behind the point, from exponentials in double: their sums are whole numbers, the same in
 //     any order, and a border between two tokens of a hundred thousand falls where 64-bit arithmetic puts it (float32 sums of such a
 //     row are off by as much as a token's weight).
-//   * The cut is narrowed down by histograms of 16 bins over (max - x), each thread counting (or weighing) in bins of its own, until what can
-//     hold it fits into a list of 2048; mostly the whole kept set does, and one CTA finishes on the sorted list.  Large kept sets are summed
-//     by warps over contiguous ranges, and only the range the random number falls into is walked.
-//   * Logits that do not separate by (max - x), as thousands of equal ones, are narrowed by their bits, and ties cut by index.
+//   * While the slice arrives, every thread keeps the maximum of each 4 pieces of 16 bytes that it looks at.  A histogram of these maxima says from
+//     which value on there are at least k elements (as many groups have one); the few elements above it are gathered, 15 of 16
+//     groups unseen, and one CTA finishes on the list.  Top-p does the same with the mass above two such values.
+//   * Where what is kept does not fit into a list, passes that sum mass and count above several values at once narrow the place of the cut
+//     down until its neighbourhood fits; equal logits by the thousand are cut by index.  The kept weights are then summed by warps over
+//     contiguous ranges, and only the range that the random number falls into is walked.
+#include <cfloat>
 #include <climits>
 #include <cmath>
+#include <type_traits>
 
 #include <cuda_bf16.h>
 
@@ -25,21 +29,25 @@ namespace mq {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kBins = 16;
-constexpr int kCap = 2048;            // candidates of a list
+constexpr int kCap = 1024;            // candidates of a list
 constexpr int kMaxCluster = 8;
-constexpr int kItems = kBins + 1;     // what a CTA tells the others at once
+constexpr int kGroup = 4;             // pieces of 16 bytes whose maximum is kept
+constexpr int kBars = 1024;           // bars of the histogram of these: eight to a unit, from -64 on
+constexpr int kPairs = 256;           // a list of up to so many is compared pair by pair instead of sorted
+constexpr int kShort = 96, kLong = 640;   // candidates that a nucleus is looked for in, and the largest k that the bars serve
+constexpr int kEdges = 7;             // values that a narrowing pass sums above
+constexpr int kItems = 2 * (kEdges + 1) > kWarps + 1 ? 2 * (kEdges + 1) : kWarps + 1;   // what a CTA tells the others at once
 constexpr int kPoint = 43;            // bits behind the point of a weight: 2^20 of them stay below 2^63
 constexpr int kMaxVocab = 1 << 20;
-constexpr int kTable = 64;            // 2^(j / kTable)
-constexpr uint32_t kKeyNegInf = 0x007fffffu;
-constexpr int kStageMax = 190 * 1024; // bytes of a staged slice
+constexpr int kTable = 128;           // 2^(j / kTable)
+constexpr int kSmemMax = 216 * 1024;  // dynamic shared memory of a CTA (what a block may have, less what is static)
+constexpr int kListBytes = 2 * kCap * 8;
 
 struct SampleArgs {
   const void* x;
   int64_t ld;
   int V, per;          // columns, and those of a CTA
-  int staged, slice_bytes;
+  int staged, maxima_bytes;
   const float *temperature, *top_p, *min_p, *u;
   const int32_t* top_k;
   int32_t* token;
@@ -47,11 +55,15 @@ struct SampleArgs {
   int32_t* kept;
 };
 
+// Floats (no NaN, no -0) in their order as whole numbers, and back
 __device__ __forceinline__ uint32_t order_key(float x) {
   const uint32_t b = __float_as_uint(x);
   return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
+// x + 64 rounded down compares with a bar's edge as x does
+__device__ __forceinline__ int bar_of(float x) { return max(0, min(kBars - 1, (int)floorf(__fadd_rd(x, 64.0f) * 8.0f))); }
+__device__ __forceinline__ float bar_edge(int b) { return (float)b * 0.125f - 64.0f; }
 
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
@@ -66,52 +78,32 @@ __device__ __forceinline__ uint32_t cluster_size() {
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-__device__ __forceinline__ void peer_store(const void* mine, uint32_t rank, uint64_t v) {
+// what stands in the place of `mine` in another CTA of the cluster
+template <typename T>
+__device__ __forceinline__ T peer_load(const T* mine, uint32_t rank) {
   uint32_t a = static_cast<uint32_t>(__cvta_generic_to_shared(mine)), r;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
-  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(r), "l"(v) : "memory");
+  if (sizeof(T) == 8) {
+    uint64_t v;
+    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(r) : "memory");
+    return (T)v;
+  }
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(r) : "memory");
+  return (T)v;
 }
 
-// an element's place: kept are keys above `key`, and of the equal ones those up to `idx`
-struct Cut {
-  uint32_t key;
-  int idx;
-  __device__ __forceinline__ bool keeps(uint32_t k, int i) const { return k > key || (k == key && i <= idx); }
-};
+__device__ __forceinline__ uint64_t warp_sum(uint64_t v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
 
-// A range of the order, as the histograms narrow it down: digits of y = (max - x) c first, bits of the key then
-struct Bracket {
-  float c;             // y = (m - x) c
-  float scale;         // 0: every y;  else floor(min(y, 15) scale) == prefix
-  int prefix;
-  uint32_t klo, khi;
-  bool by_key;
-  __device__ __forceinline__ float y_of(float m, float x) const { return x == m ? 0.0f : fminf((m - x) * c, 15.0f); }
-  __device__ __forceinline__ bool holds(float y, uint32_t key) const {
-    return (scale == 0.0f || (int)(y * scale) == prefix) && (!by_key || (key >= klo && key <= khi));
-  }
-  __device__ __forceinline__ int shift() const { return max(0, 28 - __clz((int)(khi - klo))); }
-  __device__ __forceinline__ int bin(float y, uint32_t key) const {
-    if (by_key) return (int)((khi - key) >> shift());
-    return scale == 0.0f ? (int)y : (int)(y * scale * 16.0f) - prefix * 16;
-  }
-  // the part that bin d is; false: it is one key, and cannot be divided
-  __device__ __forceinline__ bool narrow(int d, uint32_t key_max) {
-    if (by_key) {
-      const int sh = shift();
-      khi -= (uint32_t)d << sh;
-      if (khi - klo >= (1u << sh)) klo = khi - ((1u << sh) - 1u);
-      return klo < khi;
-    }
-    if (scale == 0.0f) { scale = 1.0f; prefix = d; }
-    else { scale *= 16.0f; prefix = prefix * 16 + d; }
-    if (prefix == 15 || scale > 60000.0f) {   // the open end, or digits that float32 does not have
-      by_key = true;
-      klo = kKeyNegInf + 1u;
-      khi = key_max;
-    }
-    return true;
-  }
+// Where the order is cut: larger elements are kept, and of those equal to `value` the ones up to column idx
+struct Cut {
+  float value;
+  int idx;
+  __device__ __forceinline__ bool keeps(float x, int i) const { return x > value || (x == value && i <= idx); }
 };
 
 template <typename T>
@@ -119,13 +111,17 @@ struct Row {
   static constexpr int kE = 16 / (int)sizeof(T);   // elements of a 16-byte piece
   const T* x;          // the row
   const uint8_t* smem; // its staged slice
+  float* maxima;       // [group][thread] of this thread's pieces
   int i0, i1;          // columns of this CTA
   int lead;            // elements of the first piece in front of column i0
   int pieces;
   bool staged;
 
   __device__ __forceinline__ float widen(T v) const;
-  __device__ __forceinline__ static float clean(float v) { return v == v ? v + 0.0f : -INFINITY; }   // (NaN: never; -0 is 0)
+  // NaN: never; -0 is 0; +infinity is the largest number (of bf16, where the logits are that: its bits can be cut off)
+  static constexpr float kMost = sizeof(T) == 4 ? FLT_MAX : 3.3895313892515355e38f;
+  __device__ __forceinline__ static float clean(float v) { return v == v ? fminf(v + 0.0f, kMost) : -INFINITY; }
+  __device__ __forceinline__ static bool odd(float v) { return !(v <= kMost) || __float_as_uint(v) == 0x80000000u; }
   // columns i0 - lead + kE v ..; those that are not this CTA's read as -inf
   __device__ __forceinline__ void global(int v, float (&out)[kE]) const {
     const int first = i0 - lead + v * kE;
@@ -176,317 +172,274 @@ __device__ __forceinline__ uint4 Row<__nv_bfloat16>::pack(const float (&in)[8]) 
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// exp(-(m - x) / T) as a fixed-point number.  2^t by a table of 2^(j / 64) and the exponential's series on |f| <= 1/128 (the
-// first term left out is below 2^-53 of the sum); the sum with 2^(52 - kPoint) leaves the rounded number in the low bits.
+// exp((x - m) / T) as a fixed-point number: 2^(d c) = 2^r 2^f with r = d c rounded to multiples of 1 / kTable, 2^r from a table and
+// the exponent's bits, 2^f by the exponential's series (the first term left out is below 2^-49).  The sum with 512 leaves the rounded number in the low bits of a
+// double whose upper bits are always the same: sums over such patterns are sums of weights once these bits are taken off, once per
+// term.  No branches, so that the chains of several elements overlap; what is far down is lifted to `low`, whose weight rounds to 0.
+constexpr uint64_t kBias = 0x4080000000000000ull;   // the bits of 512.0
 struct Weight {
   double m, c;            // c = log2(e) / T
-  float top;
+  float low;
   const double* table;
-  __device__ __forceinline__ uint64_t operator()(float x) const {
-    if (x == top) return 1ull << kPoint;
-    const double t = (m - (double)x) * c;           // >= 0
-    if (!(t < 60.0)) return 0ull;                   // (also an infinite gap times a factor of zero)
-    const double magic = 6755399441055744.0 / kTable;   // 1.5 * 2^52 / kTable: adding it rounds to multiples of 1 / kTable
-    const double a = magic - t;
-    const double f = (magic - a) - t;               // 2^-t = 2^(-round) 2^f
-    const int n = (int)(uint32_t)__double_as_longlong(a);   // -round(t * kTable), in the low bits
-    const double z = f * 0.69314718055994530942;
-    double p = fma(z, 1.0 / 120.0, 1.0 / 24.0);
-    p = fma(p, z, 1.0 / 6.0);
-    p = fma(p, z, 0.5);
-    p = fma(p, z, 1.0);
-    p = fma(p, z, 1.0);
-    const double s = table[n & (kTable - 1)] * p;   // in (0.99, 2)
-    const double w = __longlong_as_double(__double_as_longlong(s) + ((int64_t)(n >> 6) << 52));
-    return (uint64_t)__double_as_longlong(w + 512.0) & ((1ull << 52) - 1ull);
+  __device__ __forceinline__ uint64_t biased(float x) const {
+    const double d = (double)fmaxf(x, low) - m;            // <= 0
+    const double magic = 6755399441055744.0 / kTable;      // 1.5 * 2^52 / kTable: adding it rounds to multiples of 1 / kTable
+    const double a = fma(d, c, magic);
+    const double f = fma(d, c, magic - a);
+    const int n = (int)(uint32_t)__double_as_longlong(a);  // round(d c kTable), in the low bits
+    double p = fma(f, 9.618129107628477232e-3, 5.550410866482157995e-2);   // ln(2)^k / k!
+    p = fma(p, f, 2.402265069591007123e-1);
+    p = fma(p, f, 6.931471805599453094e-1);
+    p = fma(p, f, 1.0);
+    const double s = table[n & (kTable - 1)];
+    const double scaled = __hiloint2double(__double2hiint(s) + ((n & ~(kTable - 1)) << 13), __double2loint(s));
+    return (uint64_t)__double_as_longlong(fma(scaled, p, 512.0));
   }
+  __device__ __forceinline__ uint64_t operator()(float x) const { return biased(x) - kBias; }
 };
-static_assert(kTable == 64 && kPoint == 43, "the shifts above");
+static_assert(kPoint == 43 && kTable == 128, "512 = 2^(52 - kPoint); 2^13 = 2^20 / kTable");
 
 template <typename Tx>
 struct Smem {
-  uint64_t exch[2][kMaxCluster][kItems];
+  uint64_t exch[2][kItems];             // what the others fetch
+  uint64_t warp_part[kItems][kWarps];
   uint64_t warp_sum[kWarps];
-  uint64_t tot[kItems];
+  uint32_t bars[kBars];
+  uint32_t scan[kWarps];
   double table[kTable];
-  uint32_t n_list, n_bin;
+  uint32_t n_list;
+  int edge[2];
   int found;
 };
+
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_constant__ SampleArgs p) {
   constexpr int kE = Row<T>::kE;
   extern __shared__ __align__(16) uint8_t dyn[];
-  uint64_t* bins = reinterpret_cast<uint64_t*>(dyn);                   // [kBins][kThreads]
-  uint64_t *list = bins, *part = bins + kCap;                          // (the same memory, when the bins are done with)
-  static_assert(kBins * kThreads == 2 * kCap, "the lists take the bins' place");
+  uint64_t *list = reinterpret_cast<uint64_t*>(dyn), *part = list + kCap;
   __shared__ Smem<T> sh;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const uint32_t rank = cluster_rank(), n_cta = cluster_size();
   const int row = blockIdx.x / n_cta;
   if (tid < kTable) sh.table[tid] = exp2((double)tid / kTable);
+  for (int k = tid; k < kBars; k += kThreads) sh.bars[k] = 0u;
   pdl_launch_dependents();
   pdl_wait();
 
   Row<T> r;
   r.x = static_cast<const T*>(p.x) + (int64_t)row * p.ld;
-  r.smem = dyn + kBins * kThreads * 8;
+  r.maxima = reinterpret_cast<float*>(dyn + kListBytes);
+  r.smem = dyn + kListBytes + p.maxima_bytes;
   r.i0 = min(p.V, (int)rank * p.per);
   r.i1 = min(p.V, r.i0 + p.per);
   r.lead = (int)((reinterpret_cast<uintptr_t>(r.x + r.i0) & 15u) / sizeof(T));
   r.pieces = r.i1 > r.i0 ? (r.i1 - r.i0 + r.lead + kE - 1) / kE : 0;
   r.staged = p.staged != 0;
 
-  int parity = 0;
-  // Every CTA's n items (thread i of it holds item i) to all of them; sh.exch[parity ^ 1] afterwards
-  auto exchange = [&](int n, uint64_t item) {
-    if (tid < n)
-      for (uint32_t q = 0; q < n_cta; ++q) peer_store(&sh.exch[parity][rank][tid], q, item);
-    cluster_sync();
-    parity ^= 1;
-  };
-  auto got = [&](uint32_t cta, int i) { return sh.exch[parity ^ 1][cta][i]; };
-
-  // ---- the slice into shared memory, and the row's maximum
+  // ---- the slice into shared memory, the row's maximum, and the histogram of the groups' maxima
+  const int n_groups = (r.pieces + kThreads * kGroup - 1) / (kThreads * kGroup);
+  auto whole = [&](int v) { return r.column(v) >= r.i0 && r.column(v) + kE <= r.i1; };
+  if (r.staged) {
+    // all copies of a thread are on their way before it looks at the first; a quarter of them is waited for at a time
+    const uint32_t dst = static_cast<uint32_t>(__cvta_generic_to_shared(r.smem));
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      for (int g = n_groups * q / 4; g < n_groups * (q + 1) / 4; ++g)
+#pragma unroll
+        for (int k = 0; k < kGroup; ++k) {
+          const int v = (g * kGroup + k) * kThreads + tid;
+          if (v < r.pieces && whole(v))
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + (uint32_t)v * 16u), "l"(r.x + r.column(v)) : "memory");
+        }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+  }
+  const float temp = p.temperature[row], u = p.u[row];
+  const int want_k = p.top_k ? p.top_k[row] : 0;
+  const float want_p = p.top_p ? p.top_p[row] : 1.0f, min_p = p.min_p ? p.min_p[row] : 0.0f;
+  __syncthreads();   // the bars are zero
   float top = -INFINITY;
-  constexpr int kU = 8;
-  for (int v0 = tid; v0 < r.pieces; v0 += kThreads * kU) {
-    float x[kU][kE];
+  auto look = [&](int g) {
+    float most = -INFINITY;
 #pragma unroll
-    for (int k = 0; k < kU; ++k)
-      if (v0 + k * kThreads < r.pieces) r.global(v0 + k * kThreads, x[k]);
+    for (int k = 0; k < kGroup; ++k) {
+      const int v = (g * kGroup + k) * kThreads + tid;
+      if (v >= r.pieces) break;
+      float x[kE];
+      if (!r.staged || !whole(v)) {
+        r.global(v, x);
+        if (r.staged) *reinterpret_cast<uint4*>(const_cast<uint8_t*>(r.smem) + (size_t)v * 16) = r.pack(x);
+      } else {
+        r.unpack(*reinterpret_cast<const uint4*>(r.smem + (size_t)v * 16), x);
+        bool odd = false;
 #pragma unroll
-    for (int k = 0; k < kU; ++k)
-      if (v0 + k * kThreads < r.pieces) {
-        if (r.staged) *reinterpret_cast<uint4*>(const_cast<uint8_t*>(r.smem) + (size_t)(v0 + k * kThreads) * 16) = r.pack(x[k]);
+        for (int e = 0; e < kE; ++e) odd |= Row<T>::odd(x[e]);
+        if (odd) {
 #pragma unroll
-        for (int e = 0; e < kE; ++e) top = fmaxf(top, x[k][e]);
+          for (int e = 0; e < kE; ++e) x[e] = Row<T>::clean(x[e]);
+          *reinterpret_cast<uint4*>(const_cast<uint8_t*>(r.smem) + (size_t)v * 16) = r.pack(x);
+        }
       }
+#pragma unroll
+      for (int e = 0; e < kE; ++e) most = fmaxf(most, x[e]);
+    }
+    r.maxima[g * kThreads + tid] = most;
+    top = fmaxf(top, most);
+    if (most > -63.875f) atomicAdd(&sh.bars[bar_of(most)], 1u);
+  };
+  if (r.staged) {
+    asm volatile("cp.async.wait_group 3;" ::: "memory");
+    for (int g = 0; g < n_groups / 4; ++g) look(g);
+    asm volatile("cp.async.wait_group 2;" ::: "memory");
+    for (int g = n_groups / 4; g < n_groups * 2 / 4; ++g) look(g);
+    asm volatile("cp.async.wait_group 1;" ::: "memory");
+    for (int g = n_groups * 2 / 4; g < n_groups * 3 / 4; ++g) look(g);
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    for (int g = n_groups * 3 / 4; g < n_groups; ++g) look(g);
+  } else {
+    for (int g = 0; g < n_groups; ++g) look(g);
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  if (lane == 0) sh.warp_sum[warp] = order_key(top);
-  __syncthreads();
-  uint64_t best = sh.warp_sum[0];
-  for (int w = 1; w < kWarps; ++w) best = max(best, sh.warp_sum[w]);
-  exchange(1, best);
-  for (uint32_t q = 0; q < n_cta; ++q) best = max(best, got(q, 0));
-  const uint32_t key_max = (uint32_t)best;
+  int turn = 0;   // which half of `exch` is written next
+  if (lane == 0) sh.exch[turn][warp] = order_key(top);
+  cluster_sync();
+  // every warp fetches what all warps of all CTAs found
+  uint32_t key_max = 0u;
+  for (int k = lane; k < (int)n_cta * kWarps; k += 32) key_max = max(key_max, (uint32_t)peer_load(&sh.exch[turn][k % kWarps], k / kWarps));
+  key_max = __reduce_max_sync(0xffffffffu, key_max);
+  turn ^= 1;
   top = key_value(key_max);
 
-  const float temp = p.temperature[row];
-  if (key_max <= kKeyNegInf) {   // nothing to choose from
+  // Every thread gets the sum over all CTAs (and their warps) of each of n <= kItems numbers; sh.exch[turn ^ 1] keeps the CTA's own.  An
+  // entry of `exch` is written again two sums later, when every CTA has passed the barrier behind its last reading.
+  auto sum_all = [&](auto items, uint64_t* v) {
+    constexpr int n = decltype(items)::value;
+#pragma unroll
+    for (int k = 0; k < n; ++k) {
+      const uint64_t s = warp_sum(v[k]);
+      if (lane == 0) sh.warp_part[k][warp] = s;
+    }
+    __syncthreads();
+    if (tid < n) {
+      uint64_t s = 0ull;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) s += sh.warp_part[tid][w];
+      sh.exch[turn][tid] = s;
+    }
+    cluster_sync();
+    // lane k adds up number k, from one CTA after the other
+    uint64_t s = 0ull;
+    if (lane < n)
+      for (uint32_t q = 0; q < n_cta; ++q) s += peer_load(&sh.exch[turn][lane], q);
+#pragma unroll
+    for (int k = 0; k < n; ++k) v[k] = __shfl_sync(0xffffffffu, s, k);
+    turn ^= 1;
+  };
+
+  if (!(top > -INFINITY)) {      // nothing to choose from
     if (rank == 0 && tid == 0) {
       p.token[row] = -1;
       if (p.logp) p.logp[row] = -INFINITY;
       if (p.kept) p.kept[row] = 0;
     }
+    cluster_sync();              // (a CTA stays until the others have fetched from it)
     return;
   }
   if (!(temp > 0.0f)) {          // the first of the order
     int first = INT_MAX;
-    for (int v = tid; v < r.pieces; v += kThreads) {
-      float x[kE];
-      r.get(v, x);
+    for (int g = 0; g < n_groups; ++g) {
+      if (r.maxima[g * kThreads + tid] != top) continue;
+      for (int v = g * kGroup * kThreads + tid; v < min(r.pieces, (g + 1) * kGroup * kThreads); v += kThreads) {
+        float x[kE];
+        r.get(v, x);
 #pragma unroll
-      for (int e = kE - 1; e >= 0; --e)
-        if (x[e] == top) first = min(first, r.column(v) + e);
+        for (int e = kE - 1; e >= 0; --e)
+          if (x[e] == top) first = min(first, r.column(v) + e);
+      }
     }
     first = __reduce_min_sync(0xffffffffu, first);
-    if (lane == 0) sh.warp_sum[warp] = (uint64_t)first;
-    __syncthreads();
-    best = sh.warp_sum[0];
-    for (int w = 1; w < kWarps; ++w) best = min(best, sh.warp_sum[w]);
-    exchange(1, best);
-    if (rank == 0 && tid == 0) {
-      for (uint32_t q = 0; q < n_cta; ++q) best = min(best, got(q, 0));
-      p.token[row] = (int32_t)best;
-      if (p.logp) p.logp[row] = 0.0f;
-      if (p.kept) p.kept[row] = 1;
+    if (lane == 0) sh.exch[turn][warp] = (uint64_t)first;
+    cluster_sync();
+    if (rank == 0 && warp == 0) {
+      for (int k = lane; k < (int)n_cta * kWarps; k += 32) first = min(first, (int)peer_load(&sh.exch[turn][k % kWarps], k / kWarps));
+      first = __reduce_min_sync(0xffffffffu, first);
+      if (lane == 0) {
+        p.token[row] = first;
+        if (p.logp) p.logp[row] = 0.0f;
+        if (p.kept) p.kept[row] = 1;
+      }
     }
+    cluster_sync();
     return;
   }
 
   Weight weight;
   weight.m = (double)top;
-  weight.top = top;
+  // exp(-40) and less rounds to 0.  Where T is below a step of x, the number below the maximum has that already: no larger factor is needed, and
+  // none is taken, so that d c stays in a double's range.
+  const float next = fmaxf(key_value(key_max - 1u), -FLT_MAX);
+  weight.low = fmaxf(fminf(top - 40.0f * temp, next), -FLT_MAX);
   weight.c = 1.4426950408889634074 / (double)temp;
+  if (next < top) weight.c = fmin(weight.c, 58.0 / ((double)top - (double)next));
   weight.table = sh.table;
-  const int want_k = p.top_k ? p.top_k[row] : 0;
-  const float want_p = p.top_p ? p.top_p[row] : 1.0f, min_p = p.min_p ? p.min_p[row] : 0.0f, u = p.u[row];
   const bool by_k = want_k > 0 && want_k < p.V, by_p = want_p < 1.0f, by_min = min_p > 0.0f;
   // w >= min_p is x >= m - T ln(1 / min_p): the smallest float32 that is
-  uint32_t key_min = kKeyNegInf + 1u;
-  if (by_min) {
-    const float t = __double2float_ru((double)top + (double)temp * log((double)min_p));
-    key_min = min(key_max, max(key_min, order_key(t + 0.0f)));
-  }
+  float x_min = -FLT_MAX;
+  if (by_min) x_min = fmaxf(x_min, fminf(top, __double2float_ru((double)top + (double)temp * log((double)min_p)) + 0.0f));
 
-  // ---- kept elements, a warp's contiguous range at a time: `value` of every one, summed; and the first column at which the
-  // running sum exceeds `at(total)` (known to the CTA that holds it; *owner tells it)
-  auto column_of = [&](auto value, auto at, uint64_t* total, uint64_t* count, bool* owner) -> int {
-    const int a = (int)((int64_t)r.pieces * warp / kWarps), b = (int)((int64_t)r.pieces * (warp + 1) / kWarps);
-    uint64_t sum = 0;
-    uint32_t n = 0;
-    for (int v = a + lane; v < b; v += 32) {
-      float x[kE];
-      r.get(v, x);
-#pragma unroll
-      for (int e = 0; e < kE; ++e) {
-        uint64_t g;
-        if (value(x[e], r.column(v) + e, &g)) { sum += g; ++n; }
-      }
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    n = __reduce_add_sync(0xffffffffu, n);
-    __syncthreads();
+  // floor(u total), and the least whole number that is not below p total
+  auto share_of = [](float f, uint64_t total, bool up) -> uint64_t {
+    f = f > 0.0f ? fminf(f, 0.99999994f) : 0.0f;
+    const uint64_t F = (uint64_t)((double)f * 18446744073709551616.0);
+    return __umul64hi(F, total) + (up && F * total != 0ull ? 1ull : 0ull);
+  };
+  auto mass_goal = [&](uint64_t all) { return max(1ull, (unsigned long long)share_of(want_p, all, true)); };
+  auto write = [&](int token, uint64_t w, uint64_t total, int kept) {
+    p.token[row] = token;
+    if (p.logp) p.logp[row] = (float)log((double)w / (double)total);
+    if (p.kept) p.kept[row] = kept;
+  };
+
+  // ---- the elements from `least` on and below `below` that `base` keeps, as (key, index) into the first CTA's list; how many they are, or
+  // -1 if too many.  Behind it no CTA needs another one's memory.
+  auto gather = [&](float least, float below, const Cut& base) -> int {
     if (tid == 0) sh.n_list = 0;
     __syncthreads();
-    if (lane == 0) {
-      sh.warp_sum[warp] = sum;
-      atomicAdd(&sh.n_list, n);
-    }
-    __syncthreads();
-    exchange(kWarps + 1, tid < kWarps ? sh.warp_sum[tid] : (uint64_t)sh.n_list);
-    uint64_t all = 0, cnt = 0;
-    for (uint32_t q = 0; q < n_cta; ++q) {
-      for (int w = 0; w < kWarps; ++w) all += got(q, w);
-      cnt += got(q, kWarps);
-    }
-    *total = all;
-    *count = cnt;
-    uint64_t left = at(all);
-    int in_warp = -1;
-    *owner = false;
-    for (uint32_t q = 0; q < n_cta && in_warp < 0; ++q)
-      for (int w = 0; w < kWarps; ++w) {
-        const uint64_t s = got(q, w);
-        if (left < s) {
-          in_warp = w;
-          *owner = q == rank;
-          break;
-        }
-        left -= s;
-      }
-    if (!*owner) return -1;
-    // the range, cut among all warps; then the part it falls into, 32 pieces at a time
-    const int ra = (int)((int64_t)r.pieces * in_warp / kWarps), rb = (int)((int64_t)r.pieces * (in_warp + 1) / kWarps);
-    const int pa = ra + (int)((int64_t)(rb - ra) * warp / kWarps), pb = ra + (int)((int64_t)(rb - ra) * (warp + 1) / kWarps);
-    sum = 0;
-    for (int v = pa + lane; v < pb; v += 32) {
-      float x[kE];
-      r.get(v, x);
-#pragma unroll
-      for (int e = 0; e < kE; ++e) {
-        uint64_t g;
-        if (value(x[e], r.column(v) + e, &g)) sum += g;
-      }
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (tid == 0) sh.found = -1;
-    if (lane == 0) sh.warp_sum[warp] = sum;
-    __syncthreads();
-    uint64_t before = 0;
-    for (int w = 0; w < warp; ++w) before += sh.warp_sum[w];
-    if (left >= before && left - before < sum) {
-      left -= before;
-      for (int v0 = pa; v0 < pb; v0 += 32) {
-        const int v = v0 + lane;
+    for (int g = 0; g < n_groups; ++g) {
+      if (!(r.maxima[g * kThreads + tid] >= least)) continue;
+      for (int v = g * kGroup * kThreads + tid; v < min(r.pieces, (g + 1) * kGroup * kThreads); v += kThreads) {
         float x[kE];
-        uint64_t mine = 0;
-        if (v < pb) {
-          r.get(v, x);
+        r.get(v, x);
 #pragma unroll
-          for (int e = 0; e < kE; ++e) {
-            uint64_t g;
-            if (value(x[e], r.column(v) + e, &g)) mine += g;
+        for (int e = 0; e < kE; ++e)
+          if (x[e] >= least && x[e] < below && base.keeps(x[e], r.column(v) + e)) {
+            const uint32_t at = atomicAdd(&sh.n_list, 1u);
+            if (at < (uint32_t)kCap) part[at] = (uint64_t)order_key(x[e]) << 32 | (uint32_t)~(r.column(v) + e);
           }
-        }
-        uint64_t inc = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const uint64_t y = __shfl_up_sync(0xffffffffu, inc, o);
-          if (lane >= o) inc += y;
-        }
-        const bool here = left >= inc - mine && left < inc;
-        if (here) {
-          uint64_t run = inc - mine;
-#pragma unroll
-          for (int e = 0; e < kE; ++e) {
-            uint64_t g;
-            if (value(x[e], r.column(v) + e, &g)) {
-              if (run <= left && left < run + g) sh.found = r.column(v) + e;
-              run += g;
-            }
-          }
-        }
-        if (__any_sync(0xffffffffu, here)) break;
-        left -= __shfl_sync(0xffffffffu, inc, 31);
       }
     }
     __syncthreads();
-    return sh.found;
-  };
-
-  // ---- a histogram of the kept elements of a bracket, over all CTAs: sh.tot
-  auto histogram = [&](const Bracket& br, const Cut& base, bool mass) {
-    for (int b = 0; b < kBins; ++b) bins[b * kThreads + tid] = 0ull;
-    for (int v = tid; v < r.pieces; v += kThreads) {
-      float x[kE];
-      r.get(v, x);
-#pragma unroll
-      for (int e = 0; e < kE; ++e) {
-        const uint32_t key = order_key(x[e]);
-        const float y = br.y_of(top, x[e]);
-        if (base.keeps(key, r.column(v) + e) && br.holds(y, key)) bins[br.bin(y, key) * kThreads + tid] += mass ? weight(x[e]) : 1ull;
-      }
-    }
-    __syncthreads();
-    for (int b = warp; b < kBins; b += kWarps) {
-      uint64_t s = 0;
-      for (int k = lane; k < kThreads; k += 32) s += bins[b * kThreads + k];
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-      if (lane == 0) sh.tot[b] = s;
-    }
-    __syncthreads();
-    exchange(kBins, tid < kBins ? sh.tot[tid] : 0ull);
-    if (tid < kBins) {
-      uint64_t s = 0;
-      for (uint32_t q = 0; q < n_cta; ++q) s += got(q, tid);
-      sh.tot[tid] = s;
-    }
-    __syncthreads();
-  };
-
-  // ---- the elements that `pick` names, as (key, index) into the first CTA's list; how many they are, or -1 if too many
-  auto gather = [&](auto pick) -> int {
-    if (tid == 0) sh.n_list = 0;
-    __syncthreads();
-    for (int v = tid; v < r.pieces; v += kThreads) {
-      float x[kE];
-      r.get(v, x);
-#pragma unroll
-      for (int e = 0; e < kE; ++e)
-        if (pick(x[e], order_key(x[e]), r.column(v) + e)) {
-          const uint32_t at = atomicAdd(&sh.n_list, 1u);
-          if (at < (uint32_t)kCap) part[at] = (uint64_t)order_key(x[e]) << 32 | (uint32_t)~(r.column(v) + e);
-        }
-    }
-    __syncthreads();
-    const uint32_t mine = sh.n_list;
-    exchange(1, mine);
-    uint64_t n = 0, at = 0;
-    for (uint32_t q = 0; q < n_cta; ++q) {
-      if (q == rank) at = n;
-      n += got(q, 0);
-    }
-    if (n > (uint64_t)kCap) return -1;
-    for (uint32_t k = tid; k < mine; k += kThreads) peer_store(&list[at + k], 0, part[k]);
+    if (tid == 0) sh.exch[turn][0] = min(sh.n_list, (uint32_t)kCap + 1u);
     cluster_sync();
-    return (int)n;
+    uint32_t to = lane < (int)n_cta ? (uint32_t)peer_load(&sh.exch[turn][0], lane) : 0u;   // elements up to this lane's CTA
+    turn ^= 1;
+#pragma unroll
+    for (int o = 1; o < kMaxCluster; o <<= 1) {
+      const uint32_t y = __shfl_up_sync(0xffffffffu, to, o);
+      if (lane >= o) to += y;
+    }
+    const uint32_t n = __shfl_sync(0xffffffffu, to, kMaxCluster - 1);
+    if (rank == 0 && n <= (uint32_t)kCap) {
+      for (uint32_t q = 0, at = 0; q < n_cta; ++q) {
+        const uint32_t end = __shfl_sync(0xffffffffu, to, q);
+        for (uint32_t k = at + tid; k < end; k += kThreads) list[k] = peer_load(&part[k - at], q);
+        at = end;
+      }
+    }
+    cluster_sync();
+    return n <= (uint32_t)kCap ? (int)n : -1;
   };
 
   // sorts a[0 .. n) in shared memory, largest first (a has room for the next power of two)
@@ -540,39 +493,79 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     for (int k0 = 0; k0 < n; k0 += kThreads) c += __syncthreads_count(k0 + tid < n && pred(k0 + tid));
     return c;
   };
-
-  // u and p of a total: floor(u total), and the least whole number that is not below p total
-  auto share_of = [](float f, uint64_t total, bool up) -> uint64_t {
-    f = f > 0.0f ? fminf(f, 0.99999994f) : 0.0f;
-    const uint64_t F = (uint64_t)((double)f * 18446744073709551616.0);
-    return __umul64hi(F, total) + (up && F * total != 0ull ? 1ull : 0ull);
-  };
-  auto write = [&](int token, uint64_t w, uint64_t total, int kept) {
-    p.token[row] = token;
-    if (p.logp) p.logp[row] = (float)log((double)w / (double)total);
-    if (p.kept) p.kept[row] = kept;
-  };
+  auto value_of = [](uint64_t entry) { return key_value((uint32_t)(entry >> 32)); };
+  auto index_of = [](uint64_t entry) { return (int)~(uint32_t)entry; };
 
   // ---- the first CTA finishes on a list that holds every kept element; S1's mass is `mass` or, with k, that of the list's first k
   auto finish_list = [&](int n, int k, uint64_t mass) {
     if (rank != 0) return;
+    if (n <= kPairs) {
+      // every pair compared, `share` neighbouring threads to an element
+      int share = 1;
+      while (share < 32 && n * share * 2 <= kThreads) share *= 2;
+      const int j = tid / share, s0 = tid % share;
+      const bool live = j < n;
+      const uint64_t a = live ? list[j] : 0ull;
+      if (tid < n) part[tid] = weight(value_of(list[tid]));
+      __syncthreads();
+      const uint64_t w = live ? part[j] : 0ull;
+      auto sum_share = [&](uint64_t v) {
+        for (int o = 1; o < share; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        return v;
+      };
+      auto sum_block = [&](uint64_t v) {   // of every element's own v
+        v = warp_sum(s0 == 0 ? v : 0ull);
+        __syncthreads();
+        if (lane == 0) sh.warp_sum[warp] = v;
+        __syncthreads();
+        v = 0ull;
+#pragma unroll
+        for (int q = 0; q < kWarps; ++q) v += sh.warp_sum[q];
+        return v;
+      };
+      uint64_t before = 0ull;
+      uint32_t place = 0u;
+      for (int i = s0; i < n; i += share) {
+        const bool first = list[i] > a;
+        before += first ? part[i] : 0ull;
+        place += first ? 1u : 0u;
+      }
+      before = sum_share(before);
+      for (int o = 1; o < share; o <<= 1) place += __shfl_xor_sync(0xffffffffu, place, o);
+      bool keep = live && (k <= 0 || place < (uint32_t)k);
+      if (by_p) {
+        const uint64_t all = k > 0 ? sum_block(keep ? w : 0ull) : mass;
+        keep = keep && before < mass_goal(all);
+      }
+      if (by_min) keep = keep && (place == 0u || value_of(a) >= x_min);
+      uint64_t* kept_w = list + kCap / 2;       // weights of the kept ones, 0 of the others
+      if (live && s0 == 0) kept_w[j] = keep ? w : 0ull;
+      const uint64_t total = sum_block(keep ? w : 0ull);
+      const int kept = __syncthreads_count(keep && s0 == 0);
+      uint64_t run = 0ull;                      // of those with a lower index
+      for (int i = s0; i < n; i += share) run += (uint32_t)list[i] > (uint32_t)a ? kept_w[i] : 0ull;
+      run = sum_share(run);
+      const uint64_t goal = share_of(u, total, false);
+      if (keep && s0 == 0 && run <= goal && goal - run < w) write(index_of(a), w, total, kept);
+      return;
+    }
     sort_desc(list, n);
     if (k > 0) n = min(n, k);
-    for (int j = tid; j < n; j += kThreads) part[j] = weight(key_value((uint32_t)(list[j] >> 32)));
+    for (int j = tid; j < n; j += kThreads) part[j] = weight(value_of(list[j]));
     __syncthreads();
     int cut = n;
     if (by_p || by_min) {
       const uint64_t all = scan(part, n);
       if (by_p) {
-        const uint64_t goal = max(1ull, (unsigned long long)share_of(want_p, k > 0 ? all : mass, true));
+        const uint64_t goal = mass_goal(k > 0 ? all : mass);
         cut = min(cut, count_if(n, [&](int j) { return (j ? part[j - 1] : 0ull) < goal; }));
       }
-      if (by_min) cut = min(cut, count_if(n, [&](int j) { return (uint32_t)(list[j] >> 32) >= key_min; }));
+      if (by_min) cut = min(cut, count_if(n, [&](int j) { return value_of(list[j]) >= x_min; }));
       cut = max(cut, 1);
     }
     __syncthreads();
-    // in index order: (~index, place in the list), sorted largest first
-    for (int j = tid; j < cut; j += kThreads) part[j] = (list[j] & 0xffffffffull) << 32 | (list[j] >> 32);
+    // in index order: (~index, key), sorted largest first
+    for (int j = tid; j < cut; j += kThreads) part[j] = list[j] << 32 | list[j] >> 32;
     sort_desc(part, cut);
     for (int j = tid; j < cut; j += kThreads) list[j] = weight(key_value((uint32_t)part[j]));
     __syncthreads();
@@ -581,100 +574,321 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     if (tid == 0) write((int)~(uint32_t)(part[j] >> 32), list[j] - (j ? list[j - 1] : 0ull), total, cut);
   };
 
-  // ---- where the order is cut: elements are kept as long as less than `goal` (count or mass; p's share of the mass, if goal is 0) lies before
-  // them.  1: *base is the cut.  0: nothing is cut off.  -1: all is done, on a list.
-  auto find_cut = [&](Cut* base, bool mass, uint64_t goal) -> int {
-    Bracket br;
-    br.c = mass ? (float)weight.c : 1.4426950408889634f;
-    br.scale = 0.0f;
-    br.prefix = 0;
-    br.by_key = false;
-    br.klo = kKeyNegInf + 1u;
-    br.khi = key_max;
-    uint64_t above = 0, all = 0;
-    const Cut from = *base;
-    for (int level = 0;; ++level) {
-      histogram(br, from, mass);
-      if (level == 0) {
-        for (int b = 0; b < kBins; ++b) all += sh.tot[b];
-        if (mass) goal = max(1ull, (unsigned long long)share_of(want_p, all, true));
-        if (all < goal) return 0;
+  // ---- mass and count of the elements from each of E descending values on (those that `base` keeps, where there is one), and of all
+  auto sums_from = [&](auto edges, auto with_mass, auto with_base, const float* at, const Cut& base, uint64_t* mass, uint64_t* count) {
+    constexpr int E = decltype(edges)::value;
+    constexpr bool kMass = decltype(with_mass)::value, kBase = decltype(with_base)::value;
+    uint64_t m[E + 1];
+    uint32_t c[E + 1];
+    float edge[E + 1];
+#pragma unroll
+    for (int k = 0; k <= E; ++k) {
+      m[k] = 0ull;
+      c[k] = 0u;
+      edge[k] = k < E ? at[k] : -FLT_MAX;
+    }
+    for (int v = tid; v < r.pieces; v += kThreads) {
+      float x[kE];
+      r.get(v, x);
+#pragma unroll
+      for (int e = 0; e < kE; ++e) {
+        const uint64_t w = kMass ? weight.biased(x[e]) : 0ull;
+        if (kBase && !base.keeps(x[e], r.column(v) + e)) x[e] = -INFINITY;
+#pragma unroll
+        for (int k = 0; k <= E; ++k)
+          if (x[e] >= edge[k]) {
+            if (kMass) m[k] += w;
+            ++c[k];
+          }
       }
-      int d = 0;
-      while (d < kBins - 1 && above + sh.tot[d] < goal) above += sh.tot[d++];
-      const uint64_t in_bin = sh.tot[d];
-      const Bracket was = br;
-      const bool divisible = br.narrow(d, key_max);
-      if (level == 0 && (mass || above + in_bin <= (uint64_t)kCap)) {
-        // everything down to this bin
-        const int n = gather([&](float x, uint32_t key, int i) { return from.keeps(key, i) && was.bin(was.y_of(top, x), key) <= d; });
-        if (n >= 0) {
-          finish_list(n, mass ? 0 : (int)goal, all);
-          return -1;
+    }
+    uint64_t v[2 * (E + 1)];
+#pragma unroll
+    for (int k = 0; k <= E; ++k) {
+      v[2 * k] = m[k] - (kMass ? c[k] * kBias : 0ull);
+      v[2 * k + 1] = c[k];
+    }
+    sum_all(std::integral_constant<int, 2 * (E + 1)>(), v);
+#pragma unroll
+    for (int k = 0; k <= E; ++k) {
+      mass[k] = kMass ? v[2 * k] : v[2 * k + 1];
+      count[k] = v[2 * k + 1];
+    }
+  };
+  
+
+  // ---- kept elements, a warp's contiguous range at a time: weights (or ones) summed, and the first column at which the running sum exceeds
+  // `at(total)`: known to the CTA that holds it, -1 elsewhere
+  auto column_of = [&](auto as_weights, auto all_kept, const Cut& base, bool equal_only, auto at, uint64_t* total, uint64_t* count) -> int {
+    constexpr bool kW = decltype(as_weights)::value, kAll = decltype(all_kept)::value;
+    auto term = [&](float x, int i, uint32_t* n) -> uint64_t {
+      const uint64_t w = kW ? weight.biased(x) - kBias : 1ull;
+      const bool it = kAll ? x > -INFINITY : base.keeps(x, i) && (!equal_only || x == base.value);
+      *n += it ? 1u : 0u;
+      return it ? w : 0ull;
+    };
+    const int a = (int)((int64_t)r.pieces * warp / kWarps), b = (int)((int64_t)r.pieces * (warp + 1) / kWarps);
+    uint64_t sum = 0;
+    uint32_t n = 0;
+    for (int v = a + lane; v < b; v += 32) {
+      float x[kE];
+      r.get(v, x);
+#pragma unroll
+      for (int e = 0; e < kE; ++e) sum += term(x[e], r.column(v) + e, &n);
+    }
+    sum = warp_sum(sum);
+    n = __reduce_add_sync(0xffffffffu, n);
+    if (tid == 0) sh.n_list = 0;
+    __syncthreads();
+    if (lane == 0) {
+      sh.exch[turn][warp] = sum;
+      atomicAdd(&sh.n_list, n);
+    }
+    __syncthreads();
+    if (tid == 0) sh.exch[turn][kWarps] = sh.n_list;
+    cluster_sync();
+    // the sums of all ranges, two to a lane, and the counts
+    static_assert(kMaxCluster * kWarps == 64, "two ranges to a lane");
+    uint64_t s0 = 0ull, s1 = 0ull, cnt = 0ull;
+    if (2 * lane < (int)n_cta * kWarps) {
+      s0 = peer_load(&sh.exch[turn][(2 * lane) % kWarps], 2 * lane / kWarps);
+      s1 = peer_load(&sh.exch[turn][(2 * lane + 1) % kWarps], 2 * lane / kWarps);
+    }
+    if (lane < (int)n_cta) cnt = peer_load(&sh.exch[turn][kWarps], lane);
+    turn ^= 1;
+    *count = warp_sum(cnt);
+    uint64_t inc = s0 + s1;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint64_t y = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += y;
+    }
+    *total = __shfl_sync(0xffffffffu, inc, 31);
+    uint64_t left = at(*total);
+    const uint64_t before = inc - s0 - s1;
+    const bool first = left >= before && left - before < s0, second = left >= before + s0 && left < inc;
+    const unsigned vote = __ballot_sync(0xffffffffu, first || second);
+    int range = -1;
+    if (vote) {
+      const int l = __ffs(vote) - 1;
+      range = 2 * l + (__shfl_sync(0xffffffffu, (int)second, l) ? 1 : 0);
+      left -= __shfl_sync(0xffffffffu, second ? before + s0 : before, l);
+    }
+    cluster_sync();   // (the others' sums have been read)
+    if (range < 0 || range / kWarps != (int)rank) return -1;
+    // the range, cut among all warps; then the part it falls into, 32 pieces at a time
+    const int in_warp = range % kWarps;
+    const int ra = (int)((int64_t)r.pieces * in_warp / kWarps), rb = (int)((int64_t)r.pieces * (in_warp + 1) / kWarps);
+    const int pa = ra + (int)((int64_t)(rb - ra) * warp / kWarps), pb = ra + (int)((int64_t)(rb - ra) * (warp + 1) / kWarps);
+    sum = 0;
+    for (int v = pa + lane; v < pb; v += 32) {
+      float x[kE];
+      r.get(v, x);
+#pragma unroll
+      for (int e = 0; e < kE; ++e) sum += term(x[e], r.column(v) + e, &n);
+    }
+    sum = warp_sum(sum);
+    if (tid == 0) sh.found = -1;
+    if (lane == 0) sh.warp_sum[warp] = sum;
+    __syncthreads();
+    uint64_t front = 0;
+    for (int w = 0; w < warp; ++w) front += sh.warp_sum[w];
+    if (left >= front && left - front < sum) {
+      left -= front;
+      for (int v0 = pa; v0 < pb; v0 += 32) {
+        const int v = v0 + lane;
+        float x[kE];
+        uint64_t g[kE], mine = 0;
+#pragma unroll
+        for (int e = 0; e < kE; ++e) g[e] = 0ull;
+        if (v < pb) {
+          r.get(v, x);
+#pragma unroll
+          for (int e = 0; e < kE; ++e) {
+            g[e] = term(x[e], r.column(v) + e, &n);
+            mine += g[e];
+          }
         }
+        uint64_t upto = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const uint64_t y = __shfl_up_sync(0xffffffffu, upto, o);
+          if (lane >= o) upto += y;
+        }
+        uint64_t run = upto - mine;
+        const bool here = left >= run && left < upto;
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+          if (here && run <= left && left - run < g[e]) sh.found = r.column(v) + e;
+          run += g[e];
+        }
+        if (__any_sync(0xffffffffu, here)) break;
+        left -= __shfl_sync(0xffffffffu, upto, 31);
       }
-      const int n = !mass && in_bin > (uint64_t)kCap ? -1
-                    : gather([&](float x, uint32_t key, int i) { return from.keeps(key, i) && br.holds(br.y_of(top, x), key); });
-      if (n >= 0) {
-        uint64_t word = 0;
+    }
+    __syncthreads();
+    return sh.found;
+  };
+  using Yes = std::integral_constant<bool, true>;
+  using No = std::integral_constant<bool, false>;
+
+
+  // ---- where the order is cut: elements are kept as long as less than `goal` (of mass or count) lies before them.  Less than
+  // that (above, above_n elements) lies from `hi` on.  1: *base is the cut.  0: all together are less.  -1: all is done, on a list.
+  auto find_cut = [&](Cut* base, bool mass, uint64_t goal, uint64_t all, float hi, uint64_t above, uint64_t above_n) -> int {
+    const Cut from = *base;
+    uint32_t klo = order_key(-FLT_MAX), khi = order_key(hi);
+    uint64_t lo_n = ~0ull;     // elements from klo on
+    for (int level = 0;; ++level) {
+      // Seven values between, downwards: some times T below the maximum first, then evenly, and in the end evenly among the numbers
+      // that there are.  (Of few numbers between, some come twice.)
+      float at[kEdges];
+      const float lo = key_value(klo);
+      const float far[kEdges] = {1.0f, 2.0f, 3.5f, 5.0f, 7.0f, 10.0f, 15.0f};
+      const bool even = level > 0 && level < 6 && lo > -1.0e6f && khi - klo > 64u;
+#pragma unroll
+      for (int k = 0; k < kEdges; ++k) {
+        const float h = fminf(hi, top), v = level == 0 ? top - temp * far[k] : lo + (h - lo) * (0.125f * (float)(kEdges - k));
+        at[k] = level == 0 || even ? fminf(fmaxf(v, lo), h) : key_value(klo + (uint32_t)((uint64_t)(khi - klo) * (kEdges - k) / (kEdges + 1)));
+      }
+      uint64_t m[kEdges + 1], c[kEdges + 1];
+      if (!mass) sums_from(std::integral_constant<int, kEdges>(), No(), No(), at, from, m, c);
+      else if (from.value >= -FLT_MAX) sums_from(std::integral_constant<int, kEdges>(), Yes(), Yes(), at, from, m, c);
+      else sums_from(std::integral_constant<int, kEdges>(), Yes(), No(), at, from, m, c);
+      if (level == 0) {
+        if (m[kEdges] < goal) return 0;
+        lo_n = c[kEdges];
+      }
+      int k = 0;
+#pragma unroll
+      for (int e = 0; e < kEdges; ++e)
+        if (k == e && m[e] < goal) {
+          const uint32_t key = order_key(at[e]);
+          if (key <= khi) { khi = key; above = m[e]; above_n = c[e]; }
+          ++k;
+        }
+#pragma unroll
+      for (int e = 0; e < kEdges; ++e)
+        if (k == e && order_key(at[e]) >= klo) { klo = order_key(at[e]); lo_n = c[e]; }
+      hi = key_value(khi);
+      if (lo_n <= (uint64_t)kCap) {
+        const int n = gather(key_value(klo), INFINITY, from);
+        finish_list(n, mass ? 0 : (int)goal, all);
+        return -1;
+      }
+      if (lo_n - above_n <= (uint64_t)kCap) {
+        const int n = gather(key_value(klo), hi, from);
         if (rank == 0) {
           sort_desc(list, n);
-          for (int j = tid; j < n; j += kThreads) part[j] = mass ? weight(key_value((uint32_t)(list[j] >> 32))) : 1ull;
+          for (int j = tid; j < n; j += kThreads) part[j] = mass ? weight(value_of(list[j])) : 1ull;
           __syncthreads();
           scan(part, n);
-          const int m = count_if(n, [&](int j) { return above + (j ? part[j - 1] : 0ull) < goal; });
-          word = list[max(m, 1) - 1];
+          const int kept = count_if(n, [&](int j) { return above + (j ? part[j - 1] : 0ull) < goal; });
+          if (tid == 0) sh.exch[turn][0] = list[max(kept, 1) - 1];
         }
-        exchange(1, word);
-        word = got(0, 0);
-        base->key = (uint32_t)(word >> 32);
-        base->idx = (int)~(uint32_t)word;
+        cluster_sync();
+        const uint64_t word = peer_load(&sh.exch[turn][0], 0);
+        turn ^= 1;
+        *base = Cut{value_of(word), index_of(word)};
         return 1;
       }
-      if (!divisible) {   // thousands of equal logits: the first of them by index
-        const uint32_t key = br.khi;
-        const uint64_t g = mass ? weight(key_value(key)) : 1ull, ties = g ? (goal - above + g - 1) / g : 1ull;
+      if (khi - klo <= 1u) {   // thousands of equal logits: the first of them by index
+        base->value = key_value(klo);
+        const uint64_t g = mass ? weight(base->value) : 1ull, ties = g ? (goal - above + g - 1ull) / g : 1ull;
         uint64_t total, count;
-        bool owner;
-        const int i = column_of([&](float x, int c, uint64_t* one) { *one = 1ull; return order_key(x) == key && from.keeps(key, c); },
-                                [&](uint64_t t) { return min(ties, t) - 1; }, &total, &count, &owner);
-        exchange(1, owner ? (uint64_t)(i + 1) : 0ull);
-        uint64_t at = 0;
-        for (uint32_t q = 0; q < n_cta; ++q) at |= got(q, 0);
-        base->key = key;
-        base->idx = (int)at - 1;
+        // (those that `from` keeps: its own cut may lie among them)
+        const Cut equal{base->value, from.value == base->value ? from.idx : INT_MAX};
+        const int i = column_of(No(), No(), equal, true, [&](uint64_t t) { return min(ties, t) - 1ull; }, &total, &count);
+        if (tid == 0) sh.exch[turn][0] = (uint64_t)(i + 1);
+        cluster_sync();
+        uint32_t one = lane < (int)n_cta ? (uint32_t)peer_load(&sh.exch[turn][0], lane) : 0u;
+        turn ^= 1;
+        base->idx = (int)__reduce_max_sync(0xffffffffu, one) - 1;
         return 1;
       }
     }
   };
 
-  Cut base{kKeyNegInf, INT_MIN};   // (columns in front of a slice are -inf with an index below 0)
-  if (by_k && find_cut(&base, false, (uint64_t)want_k) < 0) return;
-  if (by_p && find_cut(&base, true, 0ull) < 0) return;
-  if (by_min && key_min > base.key) base = Cut{key_min - 1u, INT_MIN};
+  Cut base{-INFINITY, INT_MIN};   // (columns in front of a slice are -inf with an index below 0)
+  const float least = key_value(order_key(x_min) - 1u);
   if (by_min && !by_k && !by_p) {
-    const int n = gather([&](float, uint32_t key, int i) { return base.keeps(key, i); });
+    const int n = gather(x_min, INFINITY, base);
     if (n >= 0) {
       finish_list(n, 0, 0ull);
       return;
     }
   }
+  const bool short_k = by_k && want_k <= kLong;
+  uint64_t all = 0ull, above = 0ull, above_n = 0ull;
+  float hi = INFINITY;
+  if (short_k || (by_p && !by_k)) {
+    // From which value on there are enough: as many groups have a maximum there.  Thread t has the bar t below the maximum's.
+    const int bar = bar_of(top) - tid;
+    uint32_t n = 0u;
+    if (bar > 0)
+      for (uint32_t q = 0; q < n_cta; ++q) n += peer_load(&sh.bars[bar], q);
+    uint32_t inc = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t y = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += y;
+    }
+    if (lane == 31) sh.scan[warp] = inc;
+    if (tid < 2) sh.edge[tid] = 0;
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) inc += sh.scan[w];
+    const uint32_t want[2] = {(uint32_t)(short_k ? want_k : kShort), (uint32_t)kLong};
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      if (bar > 0 && inc >= want[k] && inc - n < want[k]) sh.edge[k] = bar;
+    __syncthreads();
+    float e0 = sh.edge[0] > 0 ? bar_edge(sh.edge[0]) : INFINITY, from = e0;
+    uint64_t list_n = 0ull;
+    if (!short_k) {
+      const float at[2] = {e0, sh.edge[1] > 0 ? bar_edge(sh.edge[1]) : INFINITY};
+      uint64_t m[3], c[3];
+      sums_from(std::integral_constant<int, 2>(), Yes(), No(), at, base, m, c);
+      all = m[2];
+      const uint64_t goal = mass_goal(all);
+      const int k = m[0] >= goal ? 0 : 1;
+      from = m[k] >= goal ? at[k] : INFINITY;
+      list_n = c[k];
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        if (at[e] < hi && m[e] < goal) { hi = at[e]; above = m[e]; above_n = c[e]; }
+    }
+    if (from < INFINITY && list_n <= (uint64_t)kCap) {
+      const int n_list = gather(from, INFINITY, base);
+      if (n_list >= 0) {
+        finish_list(n_list, short_k ? want_k : 0, all);
+        return;
+      }
+    }
+  }
+  const float end = key_value(key_max + 1u);
+  if (by_k && find_cut(&base, false, (uint64_t)want_k, 0ull, end, 0ull, 0ull) < 0) return;
+  if (by_p) {
+    if (by_k) {   // the mass of the first k
+      const float at[1] = {top};
+      uint64_t m[2], c[2];
+      if (base.value >= -FLT_MAX) sums_from(std::integral_constant<int, 1>(), Yes(), Yes(), at, base, m, c);
+      else sums_from(std::integral_constant<int, 1>(), Yes(), No(), at, base, m, c);
+      all = m[1];
+    }
+    if (find_cut(&base, true, mass_goal(all), all, hi < INFINITY ? hi : end, above, above_n) < 0) return;
+  }
+  if (by_min && least > base.value) base = Cut{least, INT_MIN};
   uint64_t total, count;
-  bool owner;
-  const int i = column_of([&](float x, int c, uint64_t* g) {
-                            if (!base.keeps(order_key(x), c)) return false;
-                            *g = weight(x);
-                            return true;
-                          },
-                          [&](uint64_t t) { return share_of(u, t, false); }, &total, &count, &owner);
-  if (owner && tid == 0 && i >= 0) write(i, weight(Row<T>::clean(r.widen(r.x[i]))), total, (int)count);
+  auto goal_of = [&](uint64_t t) { return share_of(u, t, false); };
+  const int i = base.value >= -FLT_MAX ? column_of(Yes(), No(), base, false, goal_of, &total, &count) : column_of(Yes(), Yes(), base, false, goal_of, &total, &count);
+  if (i >= 0 && tid == 0) write(i, weight(Row<T>::clean(r.widen(r.x[i]))), total, (int)count);
 }
 
 template <typename T>
-int launch(const SampleArgs& a, int B, int cluster, cudaStream_t st) {
-  const int smem = kBins * kThreads * 8 + (a.staged ? a.slice_bytes : 0);
+int launch(const SampleArgs& a, int B, int cluster, int slice_bytes, cudaStream_t st) {
+  const int smem = kListBytes + a.maxima_bytes + (a.staged ? slice_bytes : 0);
   static PerDeviceTable<char> attr_set;
-  if (!ensure_dynamic_smem(attr_set, sample_kernel<T>, kBins * kThreads * 8 + kStageMax)) return MQ_ERR_CUDA;
+  if (!ensure_dynamic_smem(attr_set, sample_kernel<T>, kSmemMax)) return MQ_ERR_CUDA;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)B * (unsigned)cluster);
   cfg.blockDim = dim3(kThreads);
@@ -714,9 +928,9 @@ extern "C" int mq_sample(const void* logits, int64_t ld, int32_t B, int32_t V, u
   int cluster = 1;
   while (cluster < kMaxCluster && V / (cluster * 2) >= 2048) cluster *= 2;
   a.per = ((V + cluster - 1) / cluster + 63) / 64 * 64;
-  a.slice_bytes = a.per * es + 16;   // (the slice may start inside a 16-byte piece)
-  a.slice_bytes = (a.slice_bytes + 15) / 16 * 16;
-  a.staged = a.slice_bytes <= kStageMax;
+  const int slice_bytes = a.per * es + 16;   // (a slice may start inside a 16-byte piece)
+  a.maxima_bytes = (slice_bytes / 16 + kThreads * kGroup - 1) / (kThreads * kGroup) * kThreads * 4;
+  a.staged = kListBytes + a.maxima_bytes + slice_bytes <= kSmemMax;
   a.temperature = temperature;
   a.top_k = top_k;
   a.top_p = top_p;
@@ -726,5 +940,5 @@ extern "C" int mq_sample(const void* logits, int64_t ld, int32_t B, int32_t V, u
   a.logp = logp;
   a.kept = kept;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  return es == 4 ? launch<float>(a, B, cluster, st) : launch<__nv_bfloat16>(a, B, cluster, st);
+  return es == 4 ? launch<float>(a, B, cluster, slice_bytes, st) : launch<__nv_bfloat16>(a, B, cluster, slice_bytes, st);
 }
