@@ -5,14 +5,14 @@
 //   index order at which the running sum of the kept weights exceeds u times their total.
 //
 // All three filters cut the order at one place, so the work is to find that place without sorting.
-//   * A row belongs to a cluster of up to 8 CTAs; each stages its slice in shared memory (a row too long for that is read again from L2), so the
-//     logits come from HBM once.  What the CTAs have to agree on goes through distributed shared memory.
+//   * A row belongs to a cluster of up to 8 CTAs.  Its logits come from HBM once: the rows that are worked on stay in L2, and what a pass needs
+//     again is read from there.  What the CTAs have to agree on goes through distributed shared memory.
 //   * Weights are fixed-point numbers of 43 bits behind the point, from exponentials in double: their sums are whole numbers, the same in
 //     any order, and a border between two tokens of a hundred thousand falls where 64-bit arithmetic puts it (float32 sums of such a
 //     row are off by as much as a token's weight).
-//   * While the slice arrives, every thread keeps the maximum of each 4 pieces of 16 bytes that it looks at.  A histogram of these maxima says from
-//     which value on there are at least k elements (as many groups have one); the few elements above it are gathered, 15 of 16
-//     groups unseen, and one CTA finishes on the list.  Top-p does the same with the mass above two such values.
+//   * In the first pass every thread keeps the maximum of each 4 pieces of 16 bytes that it looks at.  A histogram of these maxima says from
+//     which value on there are at least k elements (as many groups have one); the few elements above it are gathered, nearly all
+//     groups unseen, and one CTA finishes on the list.  Top-p does the same with two such values, if what lies above one of them has enough mass.
 //   * Where what is kept does not fit into a list, passes that sum mass and count above several values at once narrow the place of the cut
 //     down until its neighbourhood fits; equal logits by the thousand are cut by index.  The kept weights are then summed by warps over
 //     contiguous ranges, and only the range that the random number falls into is walked.
@@ -39,15 +39,14 @@ constexpr int kEdges = 7;             // values that a narrowing pass sums above
 constexpr int kItems = 2 * (kEdges + 1) > kWarps + 1 ? 2 * (kEdges + 1) : kWarps + 1;   // what a CTA tells the others at once
 constexpr int kPoint = 43;            // bits behind the point of a weight: 2^20 of them stay below 2^63
 constexpr int kMaxVocab = 1 << 20;
-constexpr int kTable = 128;           // 2^(j / kTable)
-constexpr int kSmemMax = 216 * 1024;  // dynamic shared memory of a CTA (what a block may have, less what is static)
+constexpr int kTable = 1024;          // 2^(j / kTable)
 constexpr int kListBytes = 2 * kCap * 8;
+constexpr int kMaximaMost = (kMaxVocab / kMaxCluster / 4 + kThreads * kGroup) / kGroup * 4;
 
 struct SampleArgs {
   const void* x;
   int64_t ld;
   int V, per;          // columns, and those of a CTA
-  int staged, maxima_bytes;
   const float *temperature, *top_p, *min_p, *u;
   const int32_t* top_k;
   int32_t* token;
@@ -110,18 +109,17 @@ template <typename T>
 struct Row {
   static constexpr int kE = 16 / (int)sizeof(T);   // elements of a 16-byte piece
   const T* x;          // the row
-  const uint8_t* smem; // its staged slice
   float* maxima;       // [group][thread] of this thread's pieces
   int i0, i1;          // columns of this CTA
   int lead;            // elements of the first piece in front of column i0
   int pieces;
-  bool staged;
+  bool odd;            // the row has a NaN, an infinity or a -0 somewhere
 
   __device__ __forceinline__ float widen(T v) const;
   // NaN: never; -0 is 0; +infinity is the largest number (of bf16, where the logits are that: its bits can be cut off)
   static constexpr float kMost = sizeof(T) == 4 ? FLT_MAX : 3.3895313892515355e38f;
   __device__ __forceinline__ static float clean(float v) { return v == v ? fminf(v + 0.0f, kMost) : -INFINITY; }
-  __device__ __forceinline__ static bool odd(float v) { return !(v <= kMost) || __float_as_uint(v) == 0x80000000u; }
+  __device__ __forceinline__ static bool is_odd(float v) { return !(v <= kMost) || __float_as_uint(v) == 0x80000000u; }   // (-infinity needs no change)
   // columns i0 - lead + kE v ..; those that are not this CTA's read as -inf
   __device__ __forceinline__ void global(int v, float (&out)[kE]) const {
     const int first = i0 - lead + v * kE;
@@ -132,15 +130,15 @@ struct Row {
 #pragma unroll
       for (int e = 0; e < kE; ++e) out[e] = first + e >= i0 && first + e < i1 ? widen(x[first + e]) : -INFINITY;
     }
-#pragma unroll
-    for (int e = 0; e < kE; ++e) out[e] = clean(out[e]);
   }
   __device__ __forceinline__ void unpack(const uint4& q, float (&out)[kE]) const;
-  __device__ __forceinline__ uint4 pack(const float (&in)[kE]) const;
   __device__ __forceinline__ int column(int v) const { return i0 - lead + v * kE; }
   __device__ __forceinline__ void get(int v, float (&out)[kE]) const {
-    if (staged) unpack(*reinterpret_cast<const uint4*>(smem + (size_t)v * 16), out);
-    else global(v, out);
+    global(v, out);
+    if (odd) {
+#pragma unroll
+      for (int e = 0; e < kE; ++e) out[e] = clean(out[e]);
+    }
   }
 };
 template <>
@@ -148,10 +146,6 @@ __device__ __forceinline__ float Row<float>::widen(float v) const { return v; }
 template <>
 __device__ __forceinline__ void Row<float>::unpack(const uint4& q, float (&out)[4]) const {
   out[0] = __uint_as_float(q.x); out[1] = __uint_as_float(q.y); out[2] = __uint_as_float(q.z); out[3] = __uint_as_float(q.w);
-}
-template <>
-__device__ __forceinline__ uint4 Row<float>::pack(const float (&in)[4]) const {
-  return make_uint4(__float_as_uint(in[0]), __float_as_uint(in[1]), __float_as_uint(in[2]), __float_as_uint(in[3]));
 }
 template <>
 __device__ __forceinline__ float Row<__nv_bfloat16>::widen(__nv_bfloat16 v) const { return __bfloat162float(v); }
@@ -164,16 +158,8 @@ __device__ __forceinline__ void Row<__nv_bfloat16>::unpack(const uint4& q, float
     out[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
   }
 }
-template <>
-__device__ __forceinline__ uint4 Row<__nv_bfloat16>::pack(const float (&in)[8]) const {   // (values that came from bf16: exact)
-  uint32_t w[4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) w[e] = (__float_as_uint(in[2 * e]) >> 16) | (__float_as_uint(in[2 * e + 1]) & 0xffff0000u);
-  return make_uint4(w[0], w[1], w[2], w[3]);
-}
-
 // exp((x - m) / T) as a fixed-point number: 2^(d c) = 2^r 2^f with r = d c rounded to multiples of 1 / kTable, 2^r from a table and
-// the exponent's bits, 2^f by the exponential's series (the first term left out is below 2^-49).  The sum with 512 leaves the rounded number in the low bits of a
+// the exponent's bits, 2^f by the exponential's series (the first term left out is below 2^-37 of the sum, and as often above as below 0).  The sum with 512 leaves the rounded number in the low bits of a
 // double whose upper bits are always the same: sums over such patterns are sums of weights once these bits are taken off, once per
 // term.  No branches, so that the chains of several elements overlap; what is far down is lifted to `low`, whose weight rounds to 0.
 constexpr uint64_t kBias = 0x4080000000000000ull;   // the bits of 512.0
@@ -187,17 +173,14 @@ struct Weight {
     const double a = fma(d, c, magic);
     const double f = fma(d, c, magic - a);
     const int n = (int)(uint32_t)__double_as_longlong(a);  // round(d c kTable), in the low bits
-    double p = fma(f, 9.618129107628477232e-3, 5.550410866482157995e-2);   // ln(2)^k / k!
-    p = fma(p, f, 2.402265069591007123e-1);
-    p = fma(p, f, 6.931471805599453094e-1);
-    p = fma(p, f, 1.0);
+    const double p = fma(fma(f, 2.402265069591007123e-1, 6.931471805599453094e-1), f, 1.0);   // ln(2)^k / k!
     const double s = table[n & (kTable - 1)];
-    const double scaled = __hiloint2double(__double2hiint(s) + ((n & ~(kTable - 1)) << 13), __double2loint(s));
+    const double scaled = __hiloint2double(__double2hiint(s) + ((n & ~(kTable - 1)) << 10), __double2loint(s));
     return (uint64_t)__double_as_longlong(fma(scaled, p, 512.0));
   }
   __device__ __forceinline__ uint64_t operator()(float x) const { return biased(x) - kBias; }
 };
-static_assert(kPoint == 43 && kTable == 128, "512 = 2^(52 - kPoint); 2^13 = 2^20 / kTable");
+static_assert(kPoint == 43 && kTable == 1024, "512 = 2^(52 - kPoint); 2^10 = 2^20 / kTable");
 
 template <typename Tx>
 struct Smem {
@@ -207,14 +190,14 @@ struct Smem {
   uint32_t bars[kBars];
   uint32_t scan[kWarps];
   double table[kTable];
-  uint32_t n_list;
+  uint32_t n_list, n_back;
   int edge[2];
   int found;
 };
 
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_constant__ SampleArgs p) {
+__global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_constant__ SampleArgs p) {
   constexpr int kE = Row<T>::kE;
   extern __shared__ __align__(16) uint8_t dyn[];
   uint64_t *list = reinterpret_cast<uint64_t*>(dyn), *part = list + kCap;
@@ -222,7 +205,6 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const uint32_t rank = cluster_rank(), n_cta = cluster_size();
   const int row = blockIdx.x / n_cta;
-  if (tid < kTable) sh.table[tid] = exp2((double)tid / kTable);
   for (int k = tid; k < kBars; k += kThreads) sh.bars[k] = 0u;
   pdl_launch_dependents();
   pdl_wait();
@@ -230,85 +212,67 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   Row<T> r;
   r.x = static_cast<const T*>(p.x) + (int64_t)row * p.ld;
   r.maxima = reinterpret_cast<float*>(dyn + kListBytes);
-  r.smem = dyn + kListBytes + p.maxima_bytes;
   r.i0 = min(p.V, (int)rank * p.per);
   r.i1 = min(p.V, r.i0 + p.per);
   r.lead = (int)((reinterpret_cast<uintptr_t>(r.x + r.i0) & 15u) / sizeof(T));
   r.pieces = r.i1 > r.i0 ? (r.i1 - r.i0 + r.lead + kE - 1) / kE : 0;
-  r.staged = p.staged != 0;
+  r.odd = false;
 
-  // ---- the slice into shared memory, the row's maximum, and the histogram of the groups' maxima
+  // ---- the row's maximum, and the histogram of the groups' maxima
   const int n_groups = (r.pieces + kThreads * kGroup - 1) / (kThreads * kGroup);
-  auto whole = [&](int v) { return r.column(v) >= r.i0 && r.column(v) + kE <= r.i1; };
-  if (r.staged) {
-    // all copies of a thread are on their way before it looks at the first; a quarter of them is waited for at a time
-    const uint32_t dst = static_cast<uint32_t>(__cvta_generic_to_shared(r.smem));
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      for (int g = n_groups * q / 4; g < n_groups * (q + 1) / 4; ++g)
-#pragma unroll
-        for (int k = 0; k < kGroup; ++k) {
-          const int v = (g * kGroup + k) * kThreads + tid;
-          if (v < r.pieces && whole(v))
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + (uint32_t)v * 16u), "l"(r.x + r.column(v)) : "memory");
-        }
-      asm volatile("cp.async.commit_group;" ::: "memory");
-    }
-  }
   const float temp = p.temperature[row], u = p.u[row];
   const int want_k = p.top_k ? p.top_k[row] : 0;
   const float want_p = p.top_p ? p.top_p[row] : 1.0f, min_p = p.min_p ? p.min_p[row] : 0.0f;
   __syncthreads();   // the bars are zero
   float top = -INFINITY;
-  auto look = [&](int g) {
-    float most = -INFINITY;
+  bool odd = false;
+  constexpr int kAhead = 2;   // groups whose loads are on their way
+  for (int g0 = 0; g0 < n_groups; g0 += kAhead) {
+    float x[kAhead][kGroup][kE];
 #pragma unroll
-    for (int k = 0; k < kGroup; ++k) {
-      const int v = (g * kGroup + k) * kThreads + tid;
-      if (v >= r.pieces) break;
-      float x[kE];
-      if (!r.staged || !whole(v)) {
-        r.global(v, x);
-        if (r.staged) *reinterpret_cast<uint4*>(const_cast<uint8_t*>(r.smem) + (size_t)v * 16) = r.pack(x);
-      } else {
-        r.unpack(*reinterpret_cast<const uint4*>(r.smem + (size_t)v * 16), x);
-        bool odd = false;
+    for (int a = 0; a < kAhead; ++a)
 #pragma unroll
-        for (int e = 0; e < kE; ++e) odd |= Row<T>::odd(x[e]);
-        if (odd) {
+      for (int k = 0; k < kGroup; ++k) {
+        const int v = ((g0 + a) * kGroup + k) * kThreads + tid;
+        if (v < r.pieces) r.global(v, x[a][k]);
+        else
 #pragma unroll
-          for (int e = 0; e < kE; ++e) x[e] = Row<T>::clean(x[e]);
-          *reinterpret_cast<uint4*>(const_cast<uint8_t*>(r.smem) + (size_t)v * 16) = r.pack(x);
-        }
+          for (int e = 0; e < kE; ++e) x[a][k][e] = -INFINITY;
       }
 #pragma unroll
-      for (int e = 0; e < kE; ++e) most = fmaxf(most, x[e]);
+    for (int a = 0; a < kAhead; ++a) {
+      if (g0 + a >= n_groups) break;
+      float most = -INFINITY;
+      bool any = false;
+#pragma unroll
+      for (int k = 0; k < kGroup; ++k)
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+          any |= Row<T>::is_odd(x[a][k][e]);
+          most = fmaxf(most, x[a][k][e]);   // (the number, where one of the two is NaN)
+        }
+      odd |= any;
+      if (any) most = fminf(most + 0.0f, Row<T>::kMost);
+      r.maxima[(g0 + a) * kThreads + tid] = most;
+      top = fmaxf(top, most);
+      if (most > -63.875f) atomicAdd(&sh.bars[bar_of(most)], 1u);
     }
-    r.maxima[g * kThreads + tid] = most;
-    top = fmaxf(top, most);
-    if (most > -63.875f) atomicAdd(&sh.bars[bar_of(most)], 1u);
-  };
-  if (r.staged) {
-    asm volatile("cp.async.wait_group 3;" ::: "memory");
-    for (int g = 0; g < n_groups / 4; ++g) look(g);
-    asm volatile("cp.async.wait_group 2;" ::: "memory");
-    for (int g = n_groups / 4; g < n_groups * 2 / 4; ++g) look(g);
-    asm volatile("cp.async.wait_group 1;" ::: "memory");
-    for (int g = n_groups * 2 / 4; g < n_groups * 3 / 4; ++g) look(g);
-    asm volatile("cp.async.wait_group 0;" ::: "memory");
-    for (int g = n_groups * 3 / 4; g < n_groups; ++g) look(g);
-  } else {
-    for (int g = 0; g < n_groups; ++g) look(g);
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
   int turn = 0;   // which half of `exch` is written next
-  if (lane == 0) sh.exch[turn][warp] = order_key(top);
+  odd = __any_sync(0xffffffffu, odd);
+  if (lane == 0) sh.exch[turn][warp] = order_key(top) | (odd ? 1ull << 32 : 0ull);
   cluster_sync();
   // every warp fetches what all warps of all CTAs found
   uint32_t key_max = 0u;
-  for (int k = lane; k < (int)n_cta * kWarps; k += 32) key_max = max(key_max, (uint32_t)peer_load(&sh.exch[turn][k % kWarps], k / kWarps));
+  for (int k = lane; k < (int)n_cta * kWarps; k += 32) {
+    const uint64_t found = peer_load(&sh.exch[turn][k % kWarps], k / kWarps);
+    key_max = max(key_max, (uint32_t)found);
+    odd |= found >> 32 != 0ull;
+  }
   key_max = __reduce_max_sync(0xffffffffu, key_max);
+  r.odd = __any_sync(0xffffffffu, odd);
   turn ^= 1;
   top = key_value(key_max);
 
@@ -375,6 +339,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     return;
   }
 
+  for (int j = tid; j < kTable; j += kThreads) sh.table[j] = exp2((double)j * (1.0 / kTable));
+  __syncthreads();
   Weight weight;
   weight.m = (double)top;
   // exp(-40) and less rounds to 0.  Where T is below a step of x, the number below the maximum has that already: no larger factor is needed, and
@@ -384,6 +350,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   weight.c = 1.4426950408889634074 / (double)temp;
   if (next < top) weight.c = fmin(weight.c, 58.0 / ((double)top - (double)next));
   weight.table = sh.table;
+  const bool low_is_0 = weight.low > -FLT_MAX;   // -infinity, lifted to it, weighs nothing either
   const bool by_k = want_k > 0 && want_k < p.V, by_p = want_p < 1.0f, by_min = min_p > 0.0f;
   // w >= min_p is x >= m - T ln(1 / min_p): the smallest float32 that is
   float x_min = -FLT_MAX;
@@ -400,6 +367,29 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     p.token[row] = token;
     if (p.logp) p.logp[row] = (float)log((double)w / (double)total);
     if (p.kept) p.kept[row] = kept;
+  };
+
+  // The first CTA's list: the entries that every CTA has at the front (or the back) of its part, n_q of them in lane q; how many they are.
+  // Called by all behind the barrier that says they are there; followed by one.
+  auto fetch = [&](uint32_t n_q, int to, bool back) -> uint32_t {
+#pragma unroll
+    for (int o = 1; o < kMaxCluster; o <<= 1) {
+      const uint32_t y = __shfl_up_sync(0xffffffffu, n_q, o);
+      if (lane >= o) n_q += y;
+    }
+    uint32_t end[kMaxCluster];
+#pragma unroll
+    for (int q = 0; q < kMaxCluster; ++q) end[q] = __shfl_sync(0xffffffffu, n_q, q);
+    const uint32_t n = end[kMaxCluster - 1];
+    if (rank == 0 && to + n <= (uint32_t)kCap)
+      for (uint32_t k = tid; k < n; k += kThreads) {
+        uint32_t q = 0, at = 0;
+#pragma unroll
+        for (int i = 0; i < kMaxCluster - 1; ++i)
+          if (k >= end[i]) { q = i + 1; at = end[i]; }
+        list[to + k] = peer_load(&part[back ? kCap - 1 - (k - at) : k - at], q);
+      }
+    return n;
   };
 
   // ---- the elements from `least` on and below `below` that `base` keeps, as (key, index) into the first CTA's list; how many they are, or
@@ -423,21 +413,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     __syncthreads();
     if (tid == 0) sh.exch[turn][0] = min(sh.n_list, (uint32_t)kCap + 1u);
     cluster_sync();
-    uint32_t to = lane < (int)n_cta ? (uint32_t)peer_load(&sh.exch[turn][0], lane) : 0u;   // elements up to this lane's CTA
+    const uint32_t mine = lane < (int)n_cta ? (uint32_t)peer_load(&sh.exch[turn][0], lane) : 0u;
     turn ^= 1;
-#pragma unroll
-    for (int o = 1; o < kMaxCluster; o <<= 1) {
-      const uint32_t y = __shfl_up_sync(0xffffffffu, to, o);
-      if (lane >= o) to += y;
-    }
-    const uint32_t n = __shfl_sync(0xffffffffu, to, kMaxCluster - 1);
-    if (rank == 0 && n <= (uint32_t)kCap) {
-      for (uint32_t q = 0, at = 0; q < n_cta; ++q) {
-        const uint32_t end = __shfl_sync(0xffffffffu, to, q);
-        for (uint32_t k = at + tid; k < end; k += kThreads) list[k] = peer_load(&part[k - at], q);
-        at = end;
-      }
-    }
+    const uint32_t n = fetch(mine, 0, false);
     cluster_sync();
     return n <= (uint32_t)kCap ? (int)n : -1;
   };
@@ -842,33 +820,82 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     for (int k = 0; k < 2; ++k)
       if (bar > 0 && inc >= want[k] && inc - n < want[k]) sh.edge[k] = bar;
     __syncthreads();
-    float e0 = sh.edge[0] > 0 ? bar_edge(sh.edge[0]) : INFINITY, from = e0;
-    uint64_t list_n = 0ull;
-    if (!short_k) {
-      const float at[2] = {e0, sh.edge[1] > 0 ? bar_edge(sh.edge[1]) : INFINITY};
-      uint64_t m[3], c[3];
-      sums_from(std::integral_constant<int, 2>(), Yes(), No(), at, base, m, c);
-      all = m[2];
-      const uint64_t goal = mass_goal(all);
-      const int k = m[0] >= goal ? 0 : 1;
-      from = m[k] >= goal ? at[k] : INFINITY;
-      list_n = c[k];
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-        if (at[e] < hi && m[e] < goal) { hi = at[e]; above = m[e]; above_n = c[e]; }
-    }
-    if (from < INFINITY && list_n <= (uint64_t)kCap) {
-      const int n_list = gather(from, INFINITY, base);
+    const float e0 = sh.edge[0] > 0 ? bar_edge(sh.edge[0]) : INFINITY;
+    if (short_k) {
+      const int n_list = e0 < INFINITY ? gather(e0, INFINITY, base) : -1;
       if (n_list >= 0) {
-        finish_list(n_list, short_k ? want_k : 0, all);
+        finish_list(n_list, want_k, 0ull);
         return;
+      }
+    } else {
+      // the mass of all; then the candidates with theirs, those from e0 on at the front of the part, those from e1 on at its back
+      const float e1 = sh.edge[1] > 0 ? bar_edge(sh.edge[1]) : INFINITY, least_e = fminf(e0, e1);
+      uint64_t m[3] = {0ull, 0ull, 0ull};
+      uint32_t terms = 0u;
+      for (int v0 = tid; v0 < r.pieces; v0 += 2 * kThreads) {
+        float x[2][kE];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          if (v0 + k * kThreads < r.pieces) r.get(v0 + k * kThreads, x[k]);
+          else
+#pragma unroll
+            for (int e = 0; e < kE; ++e) x[k][e] = -INFINITY;
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int e = 0; e < kE; ++e) m[0] += weight.biased(x[k][e]);
+        terms += 2 * kE;
+      }
+      m[0] -= terms * kBias;
+      if (tid == 0) sh.n_list = sh.n_back = 0u;
+      __syncthreads();
+      for (int g = 0; g < n_groups; ++g) {
+        if (!(r.maxima[g * kThreads + tid] >= least_e)) continue;
+        for (int v = g * kGroup * kThreads + tid; v < min(r.pieces, (g + 1) * kGroup * kThreads); v += kThreads) {
+          float x[kE];
+          r.get(v, x);
+#pragma unroll
+          for (int e = 0; e < kE; ++e)
+            if (x[e] >= least_e) {
+              const uint64_t w = weight(x[e]), entry = (uint64_t)order_key(x[e]) << 32 | (uint32_t)~(r.column(v) + e);
+              const bool high = x[e] >= e0;
+              const uint32_t at = atomicAdd(high ? &sh.n_list : &sh.n_back, 1u);
+              if (at < (uint32_t)kCap / 2) part[high ? at : kCap - 1 - at] = entry;
+              m[1] += high ? w : 0ull;
+              m[2] += w;
+            }
+        }
+      }
+      __syncthreads();
+      const uint32_t lists = min(sh.n_list, (uint32_t)kCap) | min(sh.n_back, (uint32_t)kCap) << 16;
+      // (more than half a part: too many, as kCap + 1 says to the sum)
+      const uint32_t front = lists & 0xffffu, behind = lists >> 16;
+      uint64_t v[5] = {m[0], m[1], m[2], tid == 0 ? (front <= kCap / 2 ? front : kCap + 1) : 0ull, tid == 0 ? (behind <= kCap / 2 ? behind : kCap + 1) : 0ull};
+      sum_all(std::integral_constant<int, 5>(), v);
+      all = v[0];
+      if (low_is_0) {
+        const uint64_t goal = mass_goal(all);
+        const int which = v[1] >= goal && v[3] <= (uint64_t)kCap ? 1 : v[2] >= goal && v[3] + v[4] <= (uint64_t)kCap ? 2 : 0;
+        if (which) {
+          const uint32_t n_front = lane < (int)n_cta ? (uint32_t)peer_load(&sh.exch[turn ^ 1][3], lane) : 0u;
+          const uint32_t n_behind = lane < (int)n_cta && which == 2 ? (uint32_t)peer_load(&sh.exch[turn ^ 1][4], lane) : 0u;
+          uint32_t n = fetch(n_front, 0, false);
+          if (which == 2) n += fetch(n_behind, (int)n, true);
+          cluster_sync();
+          finish_list((int)n, 0, all);
+          return;
+        }
+        // (counts that were cut off are not used)
+        if (e0 < hi && v[1] < goal && v[3] <= (uint64_t)kCap) { hi = e0; above = v[1]; above_n = v[3]; }
+        if (e1 < hi && v[2] < goal && v[3] + v[4] <= (uint64_t)kCap) { hi = e1; above = v[2]; above_n = v[3] + v[4]; }
       }
     }
   }
   const float end = key_value(key_max + 1u);
   if (by_k && find_cut(&base, false, (uint64_t)want_k, 0ull, end, 0ull, 0ull) < 0) return;
   if (by_p) {
-    if (by_k) {   // the mass of the first k
+    if (by_k || !low_is_0) {   // the mass of the first k
       const float at[1] = {top};
       uint64_t m[2], c[2];
       if (base.value >= -FLT_MAX) sums_from(std::integral_constant<int, 1>(), Yes(), Yes(), at, base, m, c);
@@ -885,10 +912,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
 }
 
 template <typename T>
-int launch(const SampleArgs& a, int B, int cluster, int slice_bytes, cudaStream_t st) {
-  const int smem = kListBytes + a.maxima_bytes + (a.staged ? slice_bytes : 0);
+int launch(const SampleArgs& a, int B, int cluster, int smem, cudaStream_t st) {
+  // (the maxima: up to 32 groups for 2^17 columns of float32)
   static PerDeviceTable<char> attr_set;
-  if (!ensure_dynamic_smem(attr_set, sample_kernel<T>, kSmemMax)) return MQ_ERR_CUDA;
+  if (!ensure_dynamic_smem(attr_set, sample_kernel<T>, kListBytes + kMaximaMost)) return MQ_ERR_CUDA;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)B * (unsigned)cluster);
   cfg.blockDim = dim3(kThreads);
@@ -929,8 +956,7 @@ extern "C" int mq_sample(const void* logits, int64_t ld, int32_t B, int32_t V, u
   while (cluster < kMaxCluster && V / (cluster * 2) >= 2048) cluster *= 2;
   a.per = ((V + cluster - 1) / cluster + 63) / 64 * 64;
   const int slice_bytes = a.per * es + 16;   // (a slice may start inside a 16-byte piece)
-  a.maxima_bytes = (slice_bytes / 16 + kThreads * kGroup - 1) / (kThreads * kGroup) * kThreads * 4;
-  a.staged = kListBytes + a.maxima_bytes + slice_bytes <= kSmemMax;
+  const int maxima = (slice_bytes / 16 + kThreads * kGroup - 1) / (kThreads * kGroup) * kThreads * 4;
   a.temperature = temperature;
   a.top_k = top_k;
   a.top_p = top_p;
@@ -940,5 +966,5 @@ extern "C" int mq_sample(const void* logits, int64_t ld, int32_t B, int32_t V, u
   a.logp = logp;
   a.kept = kept;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  return es == 4 ? launch<float>(a, B, cluster, slice_bytes, st) : launch<__nv_bfloat16>(a, B, cluster, slice_bytes, st);
+  return es == 4 ? launch<float>(a, B, cluster, kListBytes + maxima, st) : launch<__nv_bfloat16>(a, B, cluster, kListBytes + maxima, st);
 }
