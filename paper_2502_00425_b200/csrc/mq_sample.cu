@@ -29,13 +29,13 @@ namespace mq {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kCap = 1024;            // candidates of a list
+constexpr int kCap = 2048;            // candidates of a list
 constexpr int kMaxCluster = 8;
 constexpr int kGroup = 4;             // pieces of 16 bytes whose maximum is kept
 constexpr int kBars = 1024;           // bars of the histogram of these: eight to a unit, from -64 on
 constexpr int kPairs = 256;           // a list of up to so many is compared pair by pair instead of sorted
-constexpr int kShort = 96, kLong = 640;   // candidates that a nucleus is looked for in, and the largest k that the bars serve
-constexpr int kEdges = 7;             // values that a narrowing pass sums above
+constexpr int kShort = 96, kLong = 1280;  // candidates that a nucleus is looked for in, and the largest k that the groups' bars serve
+constexpr int kEdges = 4;             // values that a narrowing pass sums above
 constexpr int kItems = 2 * (kEdges + 1) > kWarps + 1 ? 2 * (kEdges + 1) : kWarps + 1;   // what a CTA tells the others at once
 constexpr int kPoint = 43;            // bits behind the point of a weight: 2^20 of them stay below 2^63
 constexpr int kMaxVocab = 1 << 20;
@@ -189,6 +189,8 @@ struct Smem {
   uint64_t warp_sum[kWarps];
   uint32_t bars[kBars];
   uint32_t scan[kWarps];
+  uint32_t cum[kThreads];               // of the bars from the maximum's downwards
+  float mass[kThreads];
   double table[kTable];
   uint32_t n_list, n_back;
   int edge[2];
@@ -275,6 +277,24 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
   r.odd = __any_sync(0xffffffffu, odd);
   turn ^= 1;
   top = key_value(key_max);
+
+  // fn(x, column of x[0]) for the pieces from, from + step, .. below `to`, several of which are loaded at once (from L2); lanes without a
+  // piece get -infinity
+  auto pieces_of = [&](int from, int to, int step, auto fn) {
+    constexpr int kU = 16 / kE;
+    for (int v0 = from; __any_sync(0xffffffffu, v0 < to); v0 += step * kU) {
+      float x[kU][kE];
+#pragma unroll
+      for (int k = 0; k < kU; ++k) {
+        if (v0 + k * step < to) r.get(v0 + k * step, x[k]);
+        else
+#pragma unroll
+          for (int e = 0; e < kE; ++e) x[k][e] = -INFINITY;
+      }
+#pragma unroll
+      for (int k = 0; k < kU; ++k) fn(x[k], r.column(v0 + k * step));
+    }
+  };
 
   // Every thread gets the sum over all CTAs (and their warps) of each of n <= kItems numbers; sh.exch[turn ^ 1] keeps the CTA's own.  An
   // entry of `exch` is written again two sums later, when every CTA has passed the barrier behind its last reading.
@@ -565,13 +585,11 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
       c[k] = 0u;
       edge[k] = k < E ? at[k] : -FLT_MAX;
     }
-    for (int v = tid; v < r.pieces; v += kThreads) {
-      float x[kE];
-      r.get(v, x);
+    pieces_of(tid, r.pieces, kThreads, [&](float (&x)[kE], int column) {
 #pragma unroll
       for (int e = 0; e < kE; ++e) {
         const uint64_t w = kMass ? weight.biased(x[e]) : 0ull;
-        if (kBase && !base.keeps(x[e], r.column(v) + e)) x[e] = -INFINITY;
+        if (kBase && !base.keeps(x[e], column + e)) x[e] = -INFINITY;
 #pragma unroll
         for (int k = 0; k <= E; ++k)
           if (x[e] >= edge[k]) {
@@ -579,7 +597,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
             ++c[k];
           }
       }
-    }
+    });
     uint64_t v[2 * (E + 1)];
 #pragma unroll
     for (int k = 0; k <= E; ++k) {
@@ -608,12 +626,10 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
     const int a = (int)((int64_t)r.pieces * warp / kWarps), b = (int)((int64_t)r.pieces * (warp + 1) / kWarps);
     uint64_t sum = 0;
     uint32_t n = 0;
-    for (int v = a + lane; v < b; v += 32) {
-      float x[kE];
-      r.get(v, x);
+    pieces_of(a + lane, b, 32, [&](float (&x)[kE], int column) {
 #pragma unroll
-      for (int e = 0; e < kE; ++e) sum += term(x[e], r.column(v) + e, &n);
-    }
+      for (int e = 0; e < kE; ++e) sum += term(x[e], column + e, &n);
+    });
     sum = warp_sum(sum);
     n = __reduce_add_sync(0xffffffffu, n);
     if (tid == 0) sh.n_list = 0;
@@ -659,12 +675,10 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
     const int ra = (int)((int64_t)r.pieces * in_warp / kWarps), rb = (int)((int64_t)r.pieces * (in_warp + 1) / kWarps);
     const int pa = ra + (int)((int64_t)(rb - ra) * warp / kWarps), pb = ra + (int)((int64_t)(rb - ra) * (warp + 1) / kWarps);
     sum = 0;
-    for (int v = pa + lane; v < pb; v += 32) {
-      float x[kE];
-      r.get(v, x);
+    pieces_of(pa + lane, pb, 32, [&](float (&x)[kE], int column) {
 #pragma unroll
-      for (int e = 0; e < kE; ++e) sum += term(x[e], r.column(v) + e, &n);
-    }
+      for (int e = 0; e < kE; ++e) sum += term(x[e], column + e, &n);
+    });
     sum = warp_sum(sum);
     if (tid == 0) sh.found = -1;
     if (lane == 0) sh.warp_sum[warp] = sum;
@@ -711,51 +725,125 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
   using No = std::integral_constant<bool, false>;
 
 
-  // ---- where the order is cut: elements are kept as long as less than `goal` (of mass or count) lies before them.  Less than
-  // that (above, above_n elements) lies from `hi` on.  1: *base is the cut.  0: all together are less.  -1: all is done, on a list.
-  auto find_cut = [&](Cut* base, bool mass, uint64_t goal, uint64_t all, float hi, uint64_t above, uint64_t above_n) -> int {
+  // ---- the bars of all CTAs, from the maximum's (bar `high`) downwards: sh.cum[t] of the bars high .. high - t
+  const int high = bar_of(top);
+  auto add_bars = [&]() {
+    uint32_t n = 0u;
+    if (high - tid > 0)
+      for (uint32_t q = 0; q < n_cta; ++q) n += peer_load(&sh.bars[high - tid], q);
+    uint32_t inc = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t y = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += y;
+    }
+    if (lane == 31) sh.scan[warp] = inc;
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) inc += sh.scan[w];
+    sh.cum[tid] = inc;
+    __syncthreads();
+  };
+  // the bar whose end reaches `want`; kThreads: none
+  auto bar_with = [&](uint64_t want) -> int {
+    const int t = count_if(kThreads, [&](int k) { return (uint64_t)sh.cum[k] < want; });
+    return high - t > 0 ? t : kThreads;
+  };
+  auto edge_of = [&](int t) { return t < kThreads ? bar_edge(high - t) : INFINITY; };
+  // The bars once more, of all elements instead of the groups' maxima
+  bool of_elements = false;
+  auto count_elements = [&]() {
+    if (of_elements) return;
+    of_elements = true;
+    cluster_sync();
+    for (int k = tid; k < kBars; k += kThreads) sh.bars[k] = 0u;
+    __syncthreads();
+    const float from = fmaxf(bar_edge(max(1, high - kThreads + 1)), bar_edge(1));
+    pieces_of(tid, r.pieces, kThreads, [&](float (&x)[kE], int) {
+#pragma unroll
+      for (int e = 0; e < kE; ++e)
+        if (x[e] >= from) atomicAdd(&sh.bars[bar_of(x[e])], 1u);
+    });
+    cluster_sync();
+    add_bars();
+  };
+
+  // ---- where the order is cut: elements are kept as long as less than `goal` (of mass or count) lies before them.  1: *base is the
+  // cut.  0: all together are less.  -1: all is done, on a list.
+  auto find_cut = [&](Cut* base, bool mass, uint64_t goal, uint64_t all) -> int {
     const Cut from = *base;
-    uint32_t klo = order_key(-FLT_MAX), khi = order_key(hi);
-    uint64_t lo_n = ~0ull;     // elements from klo on
-    for (int level = 0;; ++level) {
-      // Seven values between, downwards: some times T below the maximum first, then evenly, and in the end evenly among the numbers
-      // that there are.  (Of few numbers between, some come twice.)
-      float at[kEdges];
-      const float lo = key_value(klo);
-      const float far[kEdges] = {1.0f, 2.0f, 3.5f, 5.0f, 7.0f, 10.0f, 15.0f};
-      const bool even = level > 0 && level < 6 && lo > -1.0e6f && khi - klo > 64u;
-#pragma unroll
-      for (int k = 0; k < kEdges; ++k) {
-        const float h = fminf(hi, top), v = level == 0 ? top - temp * far[k] : lo + (h - lo) * (0.125f * (float)(kEdges - k));
-        at[k] = level == 0 || even ? fminf(fmaxf(v, lo), h) : key_value(klo + (uint32_t)((uint64_t)(khi - klo) * (kEdges - k) / (kEdges + 1)));
-      }
-      uint64_t m[kEdges + 1], c[kEdges + 1];
-      if (!mass) sums_from(std::integral_constant<int, kEdges>(), No(), No(), at, from, m, c);
-      else if (from.value >= -FLT_MAX) sums_from(std::integral_constant<int, kEdges>(), Yes(), Yes(), at, from, m, c);
-      else sums_from(std::integral_constant<int, kEdges>(), Yes(), No(), at, from, m, c);
-      if (level == 0) {
-        if (m[kEdges] < goal) return 0;
-        lo_n = c[kEdges];
-      }
-      int k = 0;
-#pragma unroll
-      for (int e = 0; e < kEdges; ++e)
-        if (k == e && m[e] < goal) {
-          const uint32_t key = order_key(at[e]);
-          if (key <= khi) { khi = key; above = m[e]; above_n = c[e]; }
-          ++k;
+    // less than the goal (above, above_n elements) lies from khi on, and no less from klo on (lo_n elements)
+    uint32_t klo = order_key(-FLT_MAX), khi = key_max + 1u;
+    uint64_t above = 0ull, above_n = 0ull, lo_n = ~0ull;
+    count_elements();
+    int near;       // the bar that the goal lies in, or about where it lies
+    bool known = false;
+    if (!mass) {
+      near = bar_with(goal);
+      known = near < kThreads;   // (exactly: no pass is needed)
+      if (known) {
+        klo = order_key(edge_of(near));
+        lo_n = sh.cum[near];
+        if (near > 0) {
+          khi = order_key(edge_of(near - 1));
+          above = above_n = sh.cum[near - 1];
         }
+      }
+    } else {
+      // (a bar's elements weigh about as much as its middle)
+      const float mine = (float)(sh.cum[tid] - (tid ? sh.cum[tid - 1] : 0u)) * exp2f(fminf((bar_edge(high - tid) + 0.0625f - top) * (float)weight.c, 0.0f));
+      float inc = mine;
 #pragma unroll
-      for (int e = 0; e < kEdges; ++e)
-        if (k == e && order_key(at[e]) >= klo) { klo = order_key(at[e]); lo_n = c[e]; }
-      hi = key_value(khi);
+      for (int o = 1; o < 32; o <<= 1) {
+        const float y = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += y;
+      }
+      if (lane == 31) sh.mass[warp] = inc;
+      __syncthreads();
+      for (int w = 0; w < warp; ++w) inc += sh.mass[w];
+      near = __syncthreads_count(inc < (float)goal * (1.0f / (float)(1ull << kPoint)));
+      if (near > high - 3) near = kThreads;
+    }
+    for (int level = 0;; ++level) {
+      if (!known) {
+        // Values between, downwards: edges of bars, or some times T below the maximum, first; then evenly, and in the end evenly among the
+        // numbers that there are.  (Of few numbers between, some come twice.)
+        float at[kEdges];
+        const float lo = key_value(klo), h = fminf(key_value(khi), top);
+        const bool even = level > 0 && level < 6 && lo > -1.0e6f && khi - klo > 64u;
+#pragma unroll
+        for (int k = 0; k < kEdges; ++k) {
+          const float first = near < kThreads ? bar_edge(high - near + 2 - k) : top - temp * (2.0f * (float)(1 << k));
+          const float v = level == 0 ? first : lo + (h - lo) * ((float)(kEdges - k) / (float)(kEdges + 1));
+          at[k] = level == 0 || even ? fminf(fmaxf(v, lo), h) : key_value(klo + (uint32_t)((uint64_t)(khi - klo) * (kEdges - k) / (kEdges + 1)));
+        }
+        uint64_t m[kEdges + 1], c[kEdges + 1];
+        if (!mass) sums_from(std::integral_constant<int, kEdges>(), No(), No(), at, from, m, c);
+        else if (from.value >= -FLT_MAX) sums_from(std::integral_constant<int, kEdges>(), Yes(), Yes(), at, from, m, c);
+        else sums_from(std::integral_constant<int, kEdges>(), Yes(), No(), at, from, m, c);
+        if (level == 0) {
+          if (m[kEdges] < goal) return 0;
+          lo_n = c[kEdges];
+        }
+        int k = 0;
+#pragma unroll
+        for (int e = 0; e < kEdges; ++e)
+          if (k == e && m[e] < goal) {
+            const uint32_t key = order_key(at[e]);
+            if (key <= khi) { khi = key; above = m[e]; above_n = c[e]; }
+            ++k;
+          }
+#pragma unroll
+        for (int e = 0; e < kEdges; ++e)
+          if (k == e && order_key(at[e]) >= klo) { klo = order_key(at[e]); lo_n = c[e]; }
+      }
+      known = false;
       if (lo_n <= (uint64_t)kCap) {
         const int n = gather(key_value(klo), INFINITY, from);
         finish_list(n, mass ? 0 : (int)goal, all);
         return -1;
       }
       if (lo_n - above_n <= (uint64_t)kCap) {
-        const int n = gather(key_value(klo), hi, from);
+        const int n = gather(key_value(klo), key_value(khi), from);
         if (rank == 0) {
           sort_desc(list, n);
           for (int j = tid; j < n; j += kThreads) part[j] = mass ? weight(value_of(list[j])) : 1ull;
@@ -779,12 +867,69 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
         const int i = column_of(No(), No(), equal, true, [&](uint64_t t) { return min(ties, t) - 1ull; }, &total, &count);
         if (tid == 0) sh.exch[turn][0] = (uint64_t)(i + 1);
         cluster_sync();
-        uint32_t one = lane < (int)n_cta ? (uint32_t)peer_load(&sh.exch[turn][0], lane) : 0u;
+        const uint32_t one = lane < (int)n_cta ? (uint32_t)peer_load(&sh.exch[turn][0], lane) : 0u;
         turn ^= 1;
         base->idx = (int)__reduce_max_sync(0xffffffffu, one) - 1;
         return 1;
       }
     }
+  };
+
+  // ---- top-p: the mass of all that `base` keeps, and the candidates with theirs, those from e0 on at the front of the part, those from e1 on
+  // at its back.  True: one of the two was enough, and all is done.
+  auto nucleus = [&](auto with_base, const Cut& base, float e0, float e1, uint64_t* all) -> bool {
+    constexpr bool kBase = decltype(with_base)::value;
+    uint64_t m[3] = {0ull, 0ull, 0ull};
+    uint32_t terms = 0u;
+    pieces_of(tid, r.pieces, kThreads, [&](float (&x)[kE], int column) {
+#pragma unroll
+      for (int e = 0; e < kE; ++e) {
+        const uint64_t w = weight.biased(x[e]);
+        const bool it = !kBase || base.keeps(x[e], column + e);
+        if (it) {
+          m[0] += w;
+          if (kBase) ++terms;
+        }
+      }
+      if (!kBase) terms += kE;
+    });
+    m[0] -= terms * kBias;
+    if (tid == 0) sh.n_list = sh.n_back = 0u;
+    __syncthreads();
+    const float low = fminf(e0, e1);
+    for (int g = 0; g < n_groups; ++g) {
+      if (!(r.maxima[g * kThreads + tid] >= low)) continue;
+      for (int v = g * kGroup * kThreads + tid; v < min(r.pieces, (g + 1) * kGroup * kThreads); v += kThreads) {
+        float x[kE];
+        r.get(v, x);
+#pragma unroll
+        for (int e = 0; e < kE; ++e)
+          if (x[e] >= low && (!kBase || base.keeps(x[e], r.column(v) + e))) {
+            const uint64_t w = weight(x[e]), entry = (uint64_t)order_key(x[e]) << 32 | (uint32_t)~(r.column(v) + e);
+            const bool front = x[e] >= e0;
+            const uint32_t at = atomicAdd(front ? &sh.n_list : &sh.n_back, 1u);
+            if (at < (uint32_t)kCap / 2) part[front ? at : kCap - 1 - at] = entry;
+            m[1] += front ? w : 0ull;
+            m[2] += w;
+          }
+      }
+    }
+    __syncthreads();
+    // (more than half a part is too many, and says so in the sums)
+    auto number = [&](uint32_t n) { return tid == 0 ? (uint64_t)(n <= (uint32_t)kCap / 2 ? n : (uint32_t)kCap + 1u) : 0ull; };
+    uint64_t v[5] = {m[0], m[1], m[2], number(sh.n_list), number(sh.n_back)};
+    sum_all(std::integral_constant<int, 5>(), v);
+    *all = v[0];
+    const uint64_t goal = mass_goal(v[0]);
+    const int which = v[1] >= goal && v[3] <= (uint64_t)kCap ? 1 : v[2] >= goal && v[3] + v[4] <= (uint64_t)kCap ? 2 : 0;
+    if (!which) return false;
+    const uint32_t n_front = lane < (int)n_cta ? (uint32_t)peer_load(&sh.exch[turn ^ 1][3], lane) : 0u;
+    const uint32_t n_back = lane < (int)n_cta && which == 2 ? (uint32_t)peer_load(&sh.exch[turn ^ 1][4], lane) : 0u;
+    uint32_t n = fetch(n_front, 0, false);
+    if (which == 2) n += fetch(n_back, (int)n, true);
+    cluster_sync();
+    finish_list((int)n, 0, v[0]);
+    return true;
   };
 
   Cut base{-INFINITY, INT_MIN};   // (columns in front of a slice are -inf with an index below 0)
@@ -797,112 +942,21 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
     }
   }
   const bool short_k = by_k && want_k <= kLong;
-  uint64_t all = 0ull, above = 0ull, above_n = 0ull;
-  float hi = INFINITY;
-  if (short_k || (by_p && !by_k)) {
-    // From which value on there are enough: as many groups have a maximum there.  Thread t has the bar t below the maximum's.
-    const int bar = bar_of(top) - tid;
-    uint32_t n = 0u;
-    if (bar > 0)
-      for (uint32_t q = 0; q < n_cta; ++q) n += peer_load(&sh.bars[bar], q);
-    uint32_t inc = n;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const uint32_t y = __shfl_up_sync(0xffffffffu, inc, o);
-      if (lane >= o) inc += y;
-    }
-    if (lane == 31) sh.scan[warp] = inc;
-    if (tid < 2) sh.edge[tid] = 0;
-    __syncthreads();
-    for (int w = 0; w < warp; ++w) inc += sh.scan[w];
-    const uint32_t want[2] = {(uint32_t)(short_k ? want_k : kShort), (uint32_t)kLong};
-#pragma unroll
-    for (int k = 0; k < 2; ++k)
-      if (bar > 0 && inc >= want[k] && inc - n < want[k]) sh.edge[k] = bar;
-    __syncthreads();
-    const float e0 = sh.edge[0] > 0 ? bar_edge(sh.edge[0]) : INFINITY;
-    if (short_k) {
-      const int n_list = e0 < INFINITY ? gather(e0, INFINITY, base) : -1;
-      if (n_list >= 0) {
-        finish_list(n_list, want_k, 0ull);
-        return;
-      }
-    } else {
-      // the mass of all; then the candidates with theirs, those from e0 on at the front of the part, those from e1 on at its back
-      const float e1 = sh.edge[1] > 0 ? bar_edge(sh.edge[1]) : INFINITY, least_e = fminf(e0, e1);
-      uint64_t m[3] = {0ull, 0ull, 0ull};
-      uint32_t terms = 0u;
-      for (int v0 = tid; v0 < r.pieces; v0 += 2 * kThreads) {
-        float x[2][kE];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          if (v0 + k * kThreads < r.pieces) r.get(v0 + k * kThreads, x[k]);
-          else
-#pragma unroll
-            for (int e = 0; e < kE; ++e) x[k][e] = -INFINITY;
-        }
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-          for (int e = 0; e < kE; ++e) m[0] += weight.biased(x[k][e]);
-        terms += 2 * kE;
-      }
-      m[0] -= terms * kBias;
-      if (tid == 0) sh.n_list = sh.n_back = 0u;
-      __syncthreads();
-      for (int g = 0; g < n_groups; ++g) {
-        if (!(r.maxima[g * kThreads + tid] >= least_e)) continue;
-        for (int v = g * kGroup * kThreads + tid; v < min(r.pieces, (g + 1) * kGroup * kThreads); v += kThreads) {
-          float x[kE];
-          r.get(v, x);
-#pragma unroll
-          for (int e = 0; e < kE; ++e)
-            if (x[e] >= least_e) {
-              const uint64_t w = weight(x[e]), entry = (uint64_t)order_key(x[e]) << 32 | (uint32_t)~(r.column(v) + e);
-              const bool high = x[e] >= e0;
-              const uint32_t at = atomicAdd(high ? &sh.n_list : &sh.n_back, 1u);
-              if (at < (uint32_t)kCap / 2) part[high ? at : kCap - 1 - at] = entry;
-              m[1] += high ? w : 0ull;
-              m[2] += w;
-            }
-        }
-      }
-      __syncthreads();
-      const uint32_t lists = min(sh.n_list, (uint32_t)kCap) | min(sh.n_back, (uint32_t)kCap) << 16;
-      // (more than half a part: too many, as kCap + 1 says to the sum)
-      const uint32_t front = lists & 0xffffu, behind = lists >> 16;
-      uint64_t v[5] = {m[0], m[1], m[2], tid == 0 ? (front <= kCap / 2 ? front : kCap + 1) : 0ull, tid == 0 ? (behind <= kCap / 2 ? behind : kCap + 1) : 0ull};
-      sum_all(std::integral_constant<int, 5>(), v);
-      all = v[0];
-      if (low_is_0) {
-        const uint64_t goal = mass_goal(all);
-        const int which = v[1] >= goal && v[3] <= (uint64_t)kCap ? 1 : v[2] >= goal && v[3] + v[4] <= (uint64_t)kCap ? 2 : 0;
-        if (which) {
-          const uint32_t n_front = lane < (int)n_cta ? (uint32_t)peer_load(&sh.exch[turn ^ 1][3], lane) : 0u;
-          const uint32_t n_behind = lane < (int)n_cta && which == 2 ? (uint32_t)peer_load(&sh.exch[turn ^ 1][4], lane) : 0u;
-          uint32_t n = fetch(n_front, 0, false);
-          if (which == 2) n += fetch(n_behind, (int)n, true);
-          cluster_sync();
-          finish_list((int)n, 0, all);
-          return;
-        }
-        // (counts that were cut off are not used)
-        if (e0 < hi && v[1] < goal && v[3] <= (uint64_t)kCap) { hi = e0; above = v[1]; above_n = v[3]; }
-        if (e1 < hi && v[2] < goal && v[3] + v[4] <= (uint64_t)kCap) { hi = e1; above = v[2]; above_n = v[3] + v[4]; }
-      }
+  if (short_k || (by_p && !by_k)) add_bars();   // as many elements as groups have a maximum there
+  if (short_k) {
+    const float edge = edge_of(bar_with((uint64_t)want_k));
+    const int n = edge < INFINITY ? gather(edge, INFINITY, base) : -1;
+    if (n >= 0) {
+      finish_list(n, want_k, 0ull);
+      return;
     }
   }
-  const float end = key_value(key_max + 1u);
-  if (by_k && find_cut(&base, false, (uint64_t)want_k, 0ull, end, 0ull, 0ull) < 0) return;
+  if (by_k && find_cut(&base, false, (uint64_t)want_k, 0ull) < 0) return;
   if (by_p) {
-    if (by_k || !low_is_0) {   // the mass of the first k
-      const float at[1] = {top};
-      uint64_t m[2], c[2];
-      if (base.value >= -FLT_MAX) sums_from(std::integral_constant<int, 1>(), Yes(), Yes(), at, base, m, c);
-      else sums_from(std::integral_constant<int, 1>(), Yes(), No(), at, base, m, c);
-      all = m[1];
-    }
-    if (find_cut(&base, true, mass_goal(all), all, hi < INFINITY ? hi : end, above, above_n) < 0) return;
+    const float e0 = edge_of(bar_with(kShort)), e1 = edge_of(bar_with(kLong));
+    uint64_t all;
+    const bool done = base.value >= -FLT_MAX || !low_is_0 ? nucleus(Yes(), base, e0, e1, &all) : nucleus(No(), base, e0, e1, &all);
+    if (done || find_cut(&base, true, mass_goal(all), all) < 0) return;
   }
   if (by_min && least > base.value) base = Cut{least, INT_MIN};
   uint64_t total, count;
