@@ -54,15 +54,22 @@ struct SampleArgs {
   int32_t* kept;
 };
 
-// Floats (no NaN, no -0) in their order as whole numbers, and back
+// Floats (no NaN; -0 as 0) in their order as whole numbers, and back
 __device__ __forceinline__ uint32_t order_key(float x) {
-  const uint32_t b = __float_as_uint(x);
+  const uint32_t b = __float_as_uint(x + 0.0f);
   return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
 // x + 64 rounded down compares with a bar's edge as x does
 __device__ __forceinline__ int bar_of(float x) { return max(0, min(kBars - 1, (int)floorf(__fadd_rd(x, 64.0f) * 8.0f))); }
 __device__ __forceinline__ float bar_edge(int b) { return (float)b * 0.125f - 64.0f; }
+
+// The larger one; NaN if one of them is
+__device__ __forceinline__ float max_or_nan(float a, float b) {
+  float m;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
+  return m;
+}
 
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
@@ -113,17 +120,18 @@ struct Row {
   int i0, i1;          // columns of this CTA
   int lead;            // elements of the first piece in front of column i0
   int pieces;
-  bool odd;            // the row has a NaN, an infinity or a -0 somewhere
+  int w0, wn;          // pieces w0 .. w0 + wn - 1 have no other columns
+  bool odd;            // the row has a NaN or +infinity somewhere
 
   __device__ __forceinline__ float widen(T v) const;
-  // NaN: never; -0 is 0; +infinity is the largest number (of bf16, where the logits are that: its bits can be cut off)
+  // NaN: never; +infinity is the largest number of the type
   static constexpr float kMost = sizeof(T) == 4 ? FLT_MAX : 3.3895313892515355e38f;
-  __device__ __forceinline__ static float clean(float v) { return v == v ? fminf(v + 0.0f, kMost) : -INFINITY; }
-  __device__ __forceinline__ static bool is_odd(float v) { return !(v <= kMost) || __float_as_uint(v) == 0x80000000u; }   // (-infinity needs no change)
+  __device__ __forceinline__ static float clean(float v) { return v == v ? fminf(v, kMost) : -INFINITY; }
+
   // columns i0 - lead + kE v ..; those that are not this CTA's read as -inf
   __device__ __forceinline__ void global(int v, float (&out)[kE]) const {
     const int first = i0 - lead + v * kE;
-    if (first >= i0 && first + kE <= i1) {
+    if ((unsigned)(v - w0) < (unsigned)wn) {
       const uint4 q = __ldg(reinterpret_cast<const uint4*>(x + first));
       unpack(q, out);
     } else {
@@ -219,6 +227,8 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
   r.lead = (int)((reinterpret_cast<uintptr_t>(r.x + r.i0) & 15u) / sizeof(T));
   r.pieces = r.i1 > r.i0 ? (r.i1 - r.i0 + r.lead + kE - 1) / kE : 0;
   r.odd = false;
+  r.w0 = r.lead ? 1 : 0;
+  r.wn = max(0, (r.i1 - r.i0 + r.lead) / kE - r.w0);
 
   // ---- the row's maximum, and the histogram of the groups' maxima
   const int n_groups = (r.pieces + kThreads * kGroup - 1) / (kThreads * kGroup);
@@ -245,16 +255,18 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
     for (int a = 0; a < kAhead; ++a) {
       if (g0 + a >= n_groups) break;
       float most = -INFINITY;
-      bool any = false;
 #pragma unroll
       for (int k = 0; k < kGroup; ++k)
 #pragma unroll
-        for (int e = 0; e < kE; ++e) {
-          any |= Row<T>::is_odd(x[a][k][e]);
-          most = fmaxf(most, x[a][k][e]);   // (the number, where one of the two is NaN)
-        }
-      odd |= any;
-      if (any) most = fminf(most + 0.0f, Row<T>::kMost);
+        for (int e = 0; e < kE; ++e) most = max_or_nan(most, x[a][k][e]);
+      if (!(most <= Row<T>::kMost)) {
+        odd = true;
+        most = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < kGroup; ++k)
+#pragma unroll
+          for (int e = 0; e < kE; ++e) most = fmaxf(most, Row<T>::clean(x[a][k][e]));
+      }
       r.maxima[(g0 + a) * kThreads + tid] = most;
       top = fmaxf(top, most);
       if (most > -63.875f) atomicAdd(&sh.bars[bar_of(most)], 1u);
@@ -618,19 +630,27 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
   auto column_of = [&](auto as_weights, auto all_kept, const Cut& base, bool equal_only, auto at, uint64_t* total, uint64_t* count) -> int {
     constexpr bool kW = decltype(as_weights)::value, kAll = decltype(all_kept)::value;
     auto term = [&](float x, int i, uint32_t* n) -> uint64_t {
-      const uint64_t w = kW ? weight.biased(x) - kBias : 1ull;
-      const bool it = kAll ? x > -INFINITY : base.keeps(x, i) && (!equal_only || x == base.value);
+      const uint64_t w = kW ? weight(x) : 1ull;
+      const bool it = kAll || (base.keeps(x, i) && (!equal_only || x == base.value));
       *n += it ? 1u : 0u;
       return it ? w : 0ull;
     };
     const int a = (int)((int64_t)r.pieces * warp / kWarps), b = (int)((int64_t)r.pieces * (warp + 1) / kWarps);
     uint64_t sum = 0;
-    uint32_t n = 0;
+    uint32_t n = 0, terms = 0;
     pieces_of(a + lane, b, 32, [&](float (&x)[kE], int column) {
 #pragma unroll
-      for (int e = 0; e < kE; ++e) sum += term(x[e], column + e, &n);
+      for (int e = 0; e < kE; ++e) {
+        if (kW && kAll) {   // (-infinity weighs nothing: all can be summed)
+          sum += weight.biased(x[e]);
+          n += x[e] > -INFINITY ? 1u : 0u;
+        } else {
+          sum += term(x[e], column + e, &n);
+        }
+      }
+      if (kW && kAll) terms += kE;
     });
-    sum = warp_sum(sum);
+    sum = warp_sum(sum - terms * kBias);
     n = __reduce_add_sync(0xffffffffu, n);
     if (tid == 0) sh.n_list = 0;
     __syncthreads();
@@ -961,7 +981,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
   if (by_min && least > base.value) base = Cut{least, INT_MIN};
   uint64_t total, count;
   auto goal_of = [&](uint64_t t) { return share_of(u, t, false); };
-  const int i = base.value >= -FLT_MAX ? column_of(Yes(), No(), base, false, goal_of, &total, &count) : column_of(Yes(), Yes(), base, false, goal_of, &total, &count);
+  const int i = base.value >= -FLT_MAX || !low_is_0 ? column_of(Yes(), No(), base, false, goal_of, &total, &count) : column_of(Yes(), Yes(), base, false, goal_of, &total, &count);
   if (i >= 0 && tid == 0) write(i, weight(Row<T>::clean(r.widen(r.x[i]))), total, (int)count);
 }
 
