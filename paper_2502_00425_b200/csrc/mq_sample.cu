@@ -33,10 +33,10 @@ constexpr int kCap = 2048;            // candidates of a list
 constexpr int kMaxCluster = 8;
 constexpr int kGroup = 4;             // pieces of 16 bytes whose maximum is kept
 constexpr int kBars = 1024;           // bars of the histogram of these: eight to a unit, from -64 on
-constexpr int kPairs = 256;           // a list of up to so many is compared pair by pair instead of sorted
+constexpr int kPairs = 256;           // a list of up to so many is compared pair by pair
 constexpr int kShort = 96, kLong = 1280;  // candidates that a nucleus is looked for in, and the largest k that the groups' bars serve
-constexpr int kEdges = 4;             // values that a narrowing pass sums above
-constexpr int kItems = 2 * (kEdges + 1) > kWarps + 1 ? 2 * (kEdges + 1) : kWarps + 1;   // what a CTA tells the others at once
+constexpr int kEdges = 3;             // values that a narrowing pass sums above
+constexpr int kItems = 2 * kEdges > kWarps + 1 ? 2 * kEdges : kWarps + 1;   // what a CTA tells the others at once
 constexpr int kPoint = 43;            // bits behind the point of a weight: 2^20 of them stay below 2^63
 constexpr int kMaxVocab = 1 << 20;
 constexpr int kTable = 1024;          // 2^(j / kTable)
@@ -203,6 +203,7 @@ struct Smem {
   uint32_t n_list, n_back;
   int edge[2];
   int found;
+  uint64_t front, entry;
 };
 
 
@@ -308,6 +309,27 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
     }
   };
 
+  // fn(x, column) for the elements from `least` on; groups without one are not looked at
+  auto elements_from = [&](float least, auto fn) {
+    for (int g = 0; g < n_groups; ++g) {
+      if (!(r.maxima[g * kThreads + tid] >= least)) continue;
+      float x[kGroup][kE];
+#pragma unroll
+      for (int k = 0; k < kGroup; ++k) {
+        const int v = (g * kGroup + k) * kThreads + tid;
+        if (v < r.pieces) r.get(v, x[k]);
+        else
+#pragma unroll
+          for (int e = 0; e < kE; ++e) x[k][e] = -INFINITY;
+      }
+#pragma unroll
+      for (int k = 0; k < kGroup; ++k)
+#pragma unroll
+        for (int e = 0; e < kE; ++e)
+          if (x[k][e] >= least) fn(x[k][e], r.column((g * kGroup + k) * kThreads + tid) + e);
+    }
+  };
+
   // Every thread gets the sum over all CTAs (and their warps) of each of n <= kItems numbers; sh.exch[turn ^ 1] keeps the CTA's own.  An
   // entry of `exch` is written again two sums later, when every CTA has passed the barrier behind its last reading.
   auto sum_all = [&](auto items, uint64_t* v) {
@@ -345,16 +367,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
   }
   if (!(temp > 0.0f)) {          // the first of the order
     int first = INT_MAX;
-    for (int g = 0; g < n_groups; ++g) {
-      if (r.maxima[g * kThreads + tid] != top) continue;
-      for (int v = g * kGroup * kThreads + tid; v < min(r.pieces, (g + 1) * kGroup * kThreads); v += kThreads) {
-        float x[kE];
-        r.get(v, x);
-#pragma unroll
-        for (int e = kE - 1; e >= 0; --e)
-          if (x[e] == top) first = min(first, r.column(v) + e);
-      }
-    }
+    elements_from(top, [&](float, int i) { first = min(first, i); });
     first = __reduce_min_sync(0xffffffffu, first);
     if (lane == 0) sh.exch[turn][warp] = (uint64_t)first;
     cluster_sync();
@@ -429,19 +442,12 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
   auto gather = [&](float least, float below, const Cut& base) -> int {
     if (tid == 0) sh.n_list = 0;
     __syncthreads();
-    for (int g = 0; g < n_groups; ++g) {
-      if (!(r.maxima[g * kThreads + tid] >= least)) continue;
-      for (int v = g * kGroup * kThreads + tid; v < min(r.pieces, (g + 1) * kGroup * kThreads); v += kThreads) {
-        float x[kE];
-        r.get(v, x);
-#pragma unroll
-        for (int e = 0; e < kE; ++e)
-          if (x[e] >= least && x[e] < below && base.keeps(x[e], r.column(v) + e)) {
-            const uint32_t at = atomicAdd(&sh.n_list, 1u);
-            if (at < (uint32_t)kCap) part[at] = (uint64_t)order_key(x[e]) << 32 | (uint32_t)~(r.column(v) + e);
-          }
+    elements_from(least, [&](float x, int i) {
+      if (x < below && base.keeps(x, i)) {
+        const uint32_t at = atomicAdd(&sh.n_list, 1u);
+        if (at < (uint32_t)kCap) part[at] = (uint64_t)order_key(x) << 32 | (uint32_t)~i;
       }
-    }
+    });
     __syncthreads();
     if (tid == 0) sh.exch[turn][0] = min(sh.n_list, (uint32_t)kCap + 1u);
     cluster_sync();
@@ -452,50 +458,79 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
     return n <= (uint32_t)kCap ? (int)n : -1;
   };
 
-  // sorts a[0 .. n) in shared memory, largest first (a has room for the next power of two)
-  auto sort_desc = [&](uint64_t* a, int n) {
-    int size = 2;
-    while (size < n) size <<= 1;
-    for (int k = n + tid; k < size; k += kThreads) a[k] = 0ull;
-    __syncthreads();
-    for (int len = 2; len <= size; len <<= 1)
-      for (int half = len >> 1; half > 0; half >>= 1) {
-        for (int k = tid; k < size / 2; k += kThreads) {
-          const int i = ((k & ~(half - 1)) << 1) | (k & (half - 1)), j = i | half;
-          const uint64_t x = a[i], y = a[j];
-          if ((x < y) == ((i & len) == 0)) {
-            a[i] = y;
-            a[j] = x;
-          }
-        }
-        __syncthreads();
+  // Of the n entries of a[] (all different), taken from the largest on: the one at which the running sum of weight_of(place) reaches `goal`
+  // (1 .. the sum of all).  Eight bits at a time, from the first bit on in which they differ, by a histogram of those that have the bits
+  // in front, until a bin holds one.  Called by the whole CTA.
+  auto entry_at = [&](const uint64_t* a, int n, uint64_t goal, auto weight_of) -> uint64_t {
+    unsigned long long* bin = reinterpret_cast<unsigned long long*>(sh.bars);   // (which have been read)
+    uint32_t* number = sh.bars + 2 * kThreads;
+    static_assert(kBars >= 3 * kThreads, "two numbers per bin");
+    uint64_t most = 0ull, least_one = ~0ull;
+    for (int k = tid; k < n; k += kThreads)
+      if (weight_of(k)) {
+        most = max(most, a[k]);
+        least_one = min(least_one, a[k]);
       }
-  };
-  // a[k] <- sum of a[0 .. k], k < n
-  auto scan = [&](uint64_t* a, int n) -> uint64_t {
-    const int per = (n + kThreads - 1) / kThreads, k0 = min(n, tid * per), k1 = min(n, k0 + per);
-    uint64_t s = 0;
-    for (int k = k0; k < k1; ++k) s += a[k];
-    uint64_t inc = s;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const uint64_t y = __shfl_up_sync(0xffffffffu, inc, o);
-      if (lane >= o) inc += y;
+    for (int o = 16; o > 0; o >>= 1) {
+      most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+      least_one = min(least_one, __shfl_xor_sync(0xffffffffu, least_one, o));
     }
     __syncthreads();
-    if (lane == 31) sh.warp_sum[warp] = inc;
+    if (lane == 0) {
+      sh.warp_part[0][warp] = most;
+      sh.warp_part[1][warp] = least_one;
+    }
     __syncthreads();
-    uint64_t run = inc - s, all = 0;
+#pragma unroll
     for (int w = 0; w < kWarps; ++w) {
-      if (w < warp) run += sh.warp_sum[w];
-      all += sh.warp_sum[w];
+      most = max(most, sh.warp_part[0][w]);
+      least_one = min(least_one, sh.warp_part[1][w]);
     }
-    for (int k = k0; k < k1; ++k) {
-      run += a[k];
-      a[k] = run;
+    int pos = 64 - __clzll((long long)(most ^ least_one));   // bits from pos on are known
+    uint64_t head = pos < 64 ? most >> pos : 0ull;
+    while (pos > 0) {
+      const int to = max(0, pos - 8);
+      __syncthreads();
+      bin[tid] = 0ull;
+      number[tid] = 0u;
+      __syncthreads();
+      for (int k = tid; k < n; k += kThreads) {
+        const uint64_t v = a[k], w = weight_of(k);
+        if (w && (pos == 64 || v >> pos == head)) {
+          const int d = (int)(v >> to) & ((1 << (pos - to)) - 1);
+          atomicAdd(&bin[d], (unsigned long long)w);
+          atomicAdd(&number[d], 1u);
+        }
+      }
+      __syncthreads();
+      const uint64_t mine = bin[255 - tid];
+      uint64_t inc = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint64_t y = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += y;
+      }
+      if (lane == 31) sh.warp_sum[warp] = inc;
+      __syncthreads();
+      for (int w = 0; w < warp; ++w) inc += sh.warp_sum[w];
+      if (inc >= goal && inc - mine < goal) {
+        sh.found = 255 - tid;
+        sh.front = inc - mine;
+      }
+      __syncthreads();
+      const int d = sh.found;
+      head = head << (pos - to) | (uint64_t)d;
+      goal -= sh.front;
+      pos = to;
+      if (number[d] == 1u && pos > 0) {
+        for (int k = tid; k < n; k += kThreads)
+          if (a[k] >> pos == head && weight_of(k)) sh.entry = a[k];
+        __syncthreads();
+        return sh.entry;
+      }
     }
-    __syncthreads();
-    return all;
+    return head;
   };
   // how many k < n satisfy `pred` (every thread calls)
   auto count_if = [&](int n, auto pred) -> int {
@@ -559,71 +594,75 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
       if (keep && s0 == 0 && run <= goal && goal - run < w) write(index_of(a), w, total, kept);
       return;
     }
-    sort_desc(list, n);
-    if (k > 0) n = min(n, k);
+    // the cut, entry by entry; then the index, among those that are kept
+    uint64_t cut = 0ull;             // the last entry that is kept
+    auto sum_list = [&](auto weight_of) {
+      uint64_t v = 0ull;
+      for (int j = tid; j < n; j += kThreads) v += weight_of(j);
+      v = warp_sum(v);
+      __syncthreads();
+      if (lane == 0) sh.warp_sum[warp] = v;
+      __syncthreads();
+      v = 0ull;
+#pragma unroll
+      for (int q = 0; q < kWarps; ++q) v += sh.warp_sum[q];
+      return v;
+    };
     for (int j = tid; j < n; j += kThreads) part[j] = weight(value_of(list[j]));
     __syncthreads();
-    int cut = n;
-    if (by_p || by_min) {
-      const uint64_t all = scan(part, n);
-      if (by_p) {
-        const uint64_t goal = mass_goal(k > 0 ? all : mass);
-        cut = min(cut, count_if(n, [&](int j) { return (j ? part[j - 1] : 0ull) < goal; }));
-      }
-      if (by_min) cut = min(cut, count_if(n, [&](int j) { return value_of(list[j]) >= x_min; }));
-      cut = max(cut, 1);
+    auto kept_weight = [&](int j) { return list[j] >= cut ? part[j] : 0ull; };
+    if (k > 0 && k < n) cut = entry_at(list, n, (uint64_t)k, [](int) { return 1ull; });
+    if (by_p) {
+      const uint64_t goal = mass_goal(k > 0 ? sum_list(kept_weight) : mass);
+      cut = max(cut, entry_at(list, n, goal, [&](int j) { return part[j]; }));
     }
+    if (by_min) cut = max(cut, (uint64_t)order_key(x_min) << 32);
+    const uint64_t total = sum_list(kept_weight), kept = sum_list([&](int j) { return list[j] >= cut ? 1ull : 0ull; });
+    // (index order is that of the entries' lower halves, downwards)
+    uint64_t* by_index = part;
     __syncthreads();
-    // in index order: (~index, key), sorted largest first
-    for (int j = tid; j < cut; j += kThreads) part[j] = list[j] << 32 | list[j] >> 32;
-    sort_desc(part, cut);
-    for (int j = tid; j < cut; j += kThreads) list[j] = weight(key_value((uint32_t)part[j]));
+    for (int j = tid; j < n; j += kThreads) list[j] = list[j] >= cut ? list[j] << 32 | list[j] >> 32 : 0ull;
     __syncthreads();
-    const uint64_t total = scan(list, cut), goal = share_of(u, total, false);
-    const int j = count_if(cut, [&](int i) { return list[i] <= goal; });
-    if (tid == 0) write((int)~(uint32_t)(part[j] >> 32), list[j] - (j ? list[j - 1] : 0ull), total, cut);
+    const uint64_t found = entry_at(list, n, share_of(u, total, false) + 1ull, [&](int j) { return list[j] ? by_index[j] : 0ull; });
+    if (tid == 0) write((int)~(uint32_t)(found >> 32), weight(key_value((uint32_t)found)), total, (int)kept);
   };
 
-  // ---- mass and count of the elements from each of E descending values on (those that `base` keeps, where there is one), and of all
-  auto sums_from = [&](auto edges, auto with_mass, auto with_base, const float* at, const Cut& base, uint64_t* mass, uint64_t* count) {
-    constexpr int E = decltype(edges)::value;
+  // ---- mass (or count) and count of the elements from each of the values on, of those that `base` keeps where there is one
+  auto sums_from = [&](auto with_mass, auto with_base, const float (&at)[kEdges], const Cut& base, uint64_t (&mass)[kEdges], uint64_t (&count)[kEdges]) {
     constexpr bool kMass = decltype(with_mass)::value, kBase = decltype(with_base)::value;
-    uint64_t m[E + 1];
-    uint32_t c[E + 1];
-    float edge[E + 1];
+    uint64_t m[kEdges];
+    uint32_t c[kEdges];
 #pragma unroll
-    for (int k = 0; k <= E; ++k) {
+    for (int k = 0; k < kEdges; ++k) {
       m[k] = 0ull;
       c[k] = 0u;
-      edge[k] = k < E ? at[k] : -FLT_MAX;
     }
     pieces_of(tid, r.pieces, kThreads, [&](float (&x)[kE], int column) {
 #pragma unroll
       for (int e = 0; e < kE; ++e) {
         const uint64_t w = kMass ? weight.biased(x[e]) : 0ull;
-        if (kBase && !base.keeps(x[e], column + e)) x[e] = -INFINITY;
+        const bool it = !kBase || base.keeps(x[e], column + e);
 #pragma unroll
-        for (int k = 0; k <= E; ++k)
-          if (x[e] >= edge[k]) {
-            if (kMass) m[k] += w;
-            ++c[k];
-          }
+        for (int k = 0; k < kEdges; ++k) {
+          const bool in = it && x[e] >= at[k];
+          if (kMass) m[k] += in ? w : 0ull;
+          c[k] += in ? 1u : 0u;
+        }
       }
     });
-    uint64_t v[2 * (E + 1)];
+    uint64_t v[2 * kEdges];
 #pragma unroll
-    for (int k = 0; k <= E; ++k) {
+    for (int k = 0; k < kEdges; ++k) {
       v[2 * k] = m[k] - (kMass ? c[k] * kBias : 0ull);
       v[2 * k + 1] = c[k];
     }
-    sum_all(std::integral_constant<int, 2 * (E + 1)>(), v);
+    sum_all(std::integral_constant<int, 2 * kEdges>(), v);
 #pragma unroll
-    for (int k = 0; k <= E; ++k) {
-      mass[k] = kMass ? v[2 * k] : v[2 * k + 1];
+    for (int k = 0; k < kEdges; ++k) {
+      mass[k] = v[2 * k + (kMass ? 0 : 1)];
       count[k] = v[2 * k + 1];
     }
   };
-  
 
   // ---- kept elements, a warp's contiguous range at a time: weights (or ones) summed, and the first column at which the running sum exceeds
   // `at(total)`: known to the CTA that holds it, -1 elsewhere
@@ -819,9 +858,14 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
       }
       if (lane == 31) sh.mass[warp] = inc;
       __syncthreads();
-      for (int w = 0; w < warp; ++w) inc += sh.mass[w];
-      near = __syncthreads_count(inc < (float)goal * (1.0f / (float)(1ull << kPoint)));
-      if (near > high - 3) near = kThreads;
+      float total = 0.0f;
+      for (int w = 0; w < kWarps; ++w) {
+        if (w < warp) inc += sh.mass[w];
+        total += sh.mass[w];
+      }
+      // (in proportion to what all of them weigh)
+      near = __syncthreads_count(inc < total * ((float)goal / (float)all));
+      if (near > high - 2) near = kThreads;
     }
     for (int level = 0;; ++level) {
       if (!known) {
@@ -832,18 +876,15 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
         const bool even = level > 0 && level < 6 && lo > -1.0e6f && khi - klo > 64u;
 #pragma unroll
         for (int k = 0; k < kEdges; ++k) {
-          const float first = near < kThreads ? bar_edge(high - near + 2 - k) : top - temp * (2.0f * (float)(1 << k));
+          const float first = near < kThreads ? bar_edge(high - near + 1 - k) : k == kEdges - 1 ? -FLT_MAX : top - temp * (4.0f + 8.0f * (float)k);
           const float v = level == 0 ? first : lo + (h - lo) * ((float)(kEdges - k) / (float)(kEdges + 1));
           at[k] = level == 0 || even ? fminf(fmaxf(v, lo), h) : key_value(klo + (uint32_t)((uint64_t)(khi - klo) * (kEdges - k) / (kEdges + 1)));
         }
-        uint64_t m[kEdges + 1], c[kEdges + 1];
-        if (!mass) sums_from(std::integral_constant<int, kEdges>(), No(), No(), at, from, m, c);
-        else if (from.value >= -FLT_MAX) sums_from(std::integral_constant<int, kEdges>(), Yes(), Yes(), at, from, m, c);
-        else sums_from(std::integral_constant<int, kEdges>(), Yes(), No(), at, from, m, c);
-        if (level == 0) {
-          if (m[kEdges] < goal) return 0;
-          lo_n = c[kEdges];
-        }
+        uint64_t m[kEdges], c[kEdges];
+        if (!mass) sums_from(No(), No(), at, from, m, c);
+        else if (from.value >= -FLT_MAX) sums_from(Yes(), Yes(), at, from, m, c);
+        else sums_from(Yes(), No(), at, from, m, c);
+        if (!mass && level == 0 && m[kEdges - 1] < goal) return 0;   // (of all)
         int k = 0;
 #pragma unroll
         for (int e = 0; e < kEdges; ++e)
@@ -865,12 +906,10 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
       if (lo_n - above_n <= (uint64_t)kCap) {
         const int n = gather(key_value(klo), key_value(khi), from);
         if (rank == 0) {
-          sort_desc(list, n);
+          // the last one before which less than the goal lies: where the running sum reaches it
           for (int j = tid; j < n; j += kThreads) part[j] = mass ? weight(value_of(list[j])) : 1ull;
-          __syncthreads();
-          scan(part, n);
-          const int kept = count_if(n, [&](int j) { return above + (j ? part[j - 1] : 0ull) < goal; });
-          if (tid == 0) sh.exch[turn][0] = list[max(kept, 1) - 1];
+          const uint64_t last = entry_at(list, n, goal - above, [&](int j) { return part[j]; });
+          if (tid == 0) sh.exch[turn][0] = last;
         }
         cluster_sync();
         const uint64_t word = peer_load(&sh.exch[turn][0], 0);
@@ -916,24 +955,15 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
     m[0] -= terms * kBias;
     if (tid == 0) sh.n_list = sh.n_back = 0u;
     __syncthreads();
-    const float low = fminf(e0, e1);
-    for (int g = 0; g < n_groups; ++g) {
-      if (!(r.maxima[g * kThreads + tid] >= low)) continue;
-      for (int v = g * kGroup * kThreads + tid; v < min(r.pieces, (g + 1) * kGroup * kThreads); v += kThreads) {
-        float x[kE];
-        r.get(v, x);
-#pragma unroll
-        for (int e = 0; e < kE; ++e)
-          if (x[e] >= low && (!kBase || base.keeps(x[e], r.column(v) + e))) {
-            const uint64_t w = weight(x[e]), entry = (uint64_t)order_key(x[e]) << 32 | (uint32_t)~(r.column(v) + e);
-            const bool front = x[e] >= e0;
-            const uint32_t at = atomicAdd(front ? &sh.n_list : &sh.n_back, 1u);
-            if (at < (uint32_t)kCap / 2) part[front ? at : kCap - 1 - at] = entry;
-            m[1] += front ? w : 0ull;
-            m[2] += w;
-          }
-      }
-    }
+    elements_from(fminf(e0, e1), [&](float x, int i) {
+      if (kBase && !base.keeps(x, i)) return;
+      const uint64_t w = weight(x);
+      const bool front = x >= e0;
+      const uint32_t at = atomicAdd(front ? &sh.n_list : &sh.n_back, 1u);
+      if (at < (uint32_t)kCap / 2) part[front ? at : kCap - 1 - at] = (uint64_t)order_key(x) << 32 | (uint32_t)~i;
+      m[1] += front ? w : 0ull;
+      m[2] += w;
+    });
     __syncthreads();
     // (more than half a part is too many, and says so in the sums)
     auto number = [&](uint32_t n) { return tid == 0 ? (uint64_t)(n <= (uint32_t)kCap / 2 ? n : (uint32_t)kCap + 1u) : 0ull; };
