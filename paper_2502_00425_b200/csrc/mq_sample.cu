@@ -34,7 +34,8 @@ constexpr int kMaxCluster = 8;
 constexpr int kGroup = 4;             // pieces of 16 bytes whose maximum is kept
 constexpr int kBars = 1024;           // bars of the histogram of these: eight to a unit, from -64 on
 constexpr int kPairs = 256;           // a list of up to so many is compared pair by pair
-constexpr int kShort = 96, kLong = 1280;  // candidates that a nucleus is looked for in, and the largest k that the groups' bars serve
+constexpr int kShort = 160;           // candidates that a nucleus is looked for in first
+constexpr int kLong = 1280;           // the largest k that the groups' bars serve
 constexpr int kEdges = 3;             // values that a narrowing pass sums above
 constexpr int kItems = 2 * kEdges > kWarps + 1 ? 2 * kEdges : kWarps + 1;   // what a CTA tells the others at once
 constexpr int kPoint = 43;            // bits behind the point of a weight: 2^20 of them stay below 2^63
@@ -60,8 +61,10 @@ __device__ __forceinline__ uint32_t order_key(float x) {
   return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
-// x + 64 rounded down compares with a bar's edge as x does
-__device__ __forceinline__ int bar_of(float x) { return max(0, min(kBars - 1, (int)floorf(__fadd_rd(x, 64.0f) * 8.0f))); }
+// floor(8 x) + 512, at most the last bar (x >= -64): the sum with 1.5 * 2^20, rounded down, has it in its low bits
+__device__ __forceinline__ int bar_of(float x) {
+  return (int)(__float_as_uint(__fadd_rd(fminf(x, 63.875f), 1572864.0f)) - __float_as_uint(1572864.0f)) + kBars / 2;
+}
 __device__ __forceinline__ float bar_edge(int b) { return (float)b * 0.125f - 64.0f; }
 
 // The larger one; NaN if one of them is
@@ -81,6 +84,8 @@ __device__ __forceinline__ uint32_t cluster_size() {
   asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
   return r;
 }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
@@ -200,7 +205,7 @@ struct Smem {
   uint32_t cum[kThreads];               // of the bars from the maximum's downwards
   float mass[kThreads];
   double table[kTable];
-  uint32_t n_list, n_back;
+  uint32_t n_list;
   int edge[2];
   int found;
   uint64_t front, entry;
@@ -208,7 +213,7 @@ struct Smem {
 
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_constant__ SampleArgs p) {
+__global__ void __launch_bounds__(kThreads, 4) sample_kernel(const __grid_constant__ SampleArgs p) {
   constexpr int kE = Row<T>::kE;
   extern __shared__ __align__(16) uint8_t dyn[];
   uint64_t *list = reinterpret_cast<uint64_t*>(dyn), *part = list + kCap;
@@ -278,7 +283,10 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
   int turn = 0;   // which half of `exch` is written next
   odd = __any_sync(0xffffffffu, odd);
   if (lane == 0) sh.exch[turn][warp] = order_key(top) | (odd ? 1ull << 32 : 0ull);
-  cluster_sync();
+  cluster_arrive();
+  if (temp > 0.0f)   // (while the others arrive)
+    for (int j = tid; j < kTable; j += kThreads) sh.table[j] = exp2((double)j * (1.0 / kTable));
+  cluster_wait();
   // every warp fetches what all warps of all CTAs found
   uint32_t key_max = 0u;
   for (int k = lane; k < (int)n_cta * kWarps; k += 32) {
@@ -384,8 +392,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
     return;
   }
 
-  for (int j = tid; j < kTable; j += kThreads) sh.table[j] = exp2((double)j * (1.0 / kTable));
-  __syncthreads();
+  __syncthreads();               // the table stands
   Weight weight;
   weight.m = (double)top;
   // exp(-40) and less rounds to 0.  Where T is below a step of x, the number below the maximum has that already: no larger factor is needed, and
@@ -414,9 +421,9 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
     if (p.kept) p.kept[row] = kept;
   };
 
-  // The first CTA's list: the entries that every CTA has at the front (or the back) of its part, n_q of them in lane q; how many they are.
-  // Called by all behind the barrier that says they are there; followed by one.
-  auto fetch = [&](uint32_t n_q, int to, bool back) -> uint32_t {
+  // The first CTA's list: the entries of every CTA's part, n_q of them in lane q; how many they are.  Called by all behind the barrier that says
+  // they are there; followed by one.
+  auto fetch = [&](uint32_t n_q) -> uint32_t {
 #pragma unroll
     for (int o = 1; o < kMaxCluster; o <<= 1) {
       const uint32_t y = __shfl_up_sync(0xffffffffu, n_q, o);
@@ -426,13 +433,13 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
 #pragma unroll
     for (int q = 0; q < kMaxCluster; ++q) end[q] = __shfl_sync(0xffffffffu, n_q, q);
     const uint32_t n = end[kMaxCluster - 1];
-    if (rank == 0 && to + n <= (uint32_t)kCap)
+    if (rank == 0 && n <= (uint32_t)kCap)
       for (uint32_t k = tid; k < n; k += kThreads) {
         uint32_t q = 0, at = 0;
 #pragma unroll
         for (int i = 0; i < kMaxCluster - 1; ++i)
           if (k >= end[i]) { q = i + 1; at = end[i]; }
-        list[to + k] = peer_load(&part[back ? kCap - 1 - (k - at) : k - at], q);
+        list[k] = peer_load(&part[k - at], q);
       }
     return n;
   };
@@ -453,7 +460,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
     cluster_sync();
     const uint32_t mine = lane < (int)n_cta ? (uint32_t)peer_load(&sh.exch[turn][0], lane) : 0u;
     turn ^= 1;
-    const uint32_t n = fetch(mine, 0, false);
+    const uint32_t n = fetch(mine);
     cluster_sync();
     return n <= (uint32_t)kCap ? (int)n : -1;
   };
@@ -785,7 +792,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
 
 
   // ---- the bars of all CTAs, from the maximum's (bar `high`) downwards: sh.cum[t] of the bars high .. high - t
-  const int high = bar_of(top);
+  const int high = bar_of(fmaxf(top, -64.0f));
   auto add_bars = [&]() {
     uint32_t n = 0u;
     if (high - tid > 0)
@@ -934,11 +941,10 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
     }
   };
 
-  // ---- top-p: the mass of all that `base` keeps, and the candidates with theirs, those from e0 on at the front of the part, those from e1 on
-  // at its back.  True: one of the two was enough, and all is done.
-  auto nucleus = [&](auto with_base, const Cut& base, float e0, float e1, uint64_t* all) -> bool {
+  // ---- top-p: the mass of all that `base` keeps, and the candidates, those from `edge` on, with theirs.  True: that was enough, and all is done.
+  auto nucleus = [&](auto with_base, const Cut& base, float edge, uint64_t* all) -> bool {
     constexpr bool kBase = decltype(with_base)::value;
-    uint64_t m[3] = {0ull, 0ull, 0ull};
+    uint64_t m[2] = {0ull, 0ull};
     uint32_t terms = 0u;
     pieces_of(tid, r.pieces, kThreads, [&](float (&x)[kE], int column) {
 #pragma unroll
@@ -953,30 +959,20 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
       if (!kBase) terms += kE;
     });
     m[0] -= terms * kBias;
-    if (tid == 0) sh.n_list = sh.n_back = 0u;
+    if (tid == 0) sh.n_list = 0u;
     __syncthreads();
-    elements_from(fminf(e0, e1), [&](float x, int i) {
+    elements_from(edge, [&](float x, int i) {
       if (kBase && !base.keeps(x, i)) return;
-      const uint64_t w = weight(x);
-      const bool front = x >= e0;
-      const uint32_t at = atomicAdd(front ? &sh.n_list : &sh.n_back, 1u);
-      if (at < (uint32_t)kCap / 2) part[front ? at : kCap - 1 - at] = (uint64_t)order_key(x) << 32 | (uint32_t)~i;
-      m[1] += front ? w : 0ull;
-      m[2] += w;
+      const uint32_t at = atomicAdd(&sh.n_list, 1u);
+      if (at < (uint32_t)kCap) part[at] = (uint64_t)order_key(x) << 32 | (uint32_t)~i;
+      m[1] += weight(x);
     });
     __syncthreads();
-    // (more than half a part is too many, and says so in the sums)
-    auto number = [&](uint32_t n) { return tid == 0 ? (uint64_t)(n <= (uint32_t)kCap / 2 ? n : (uint32_t)kCap + 1u) : 0ull; };
-    uint64_t v[5] = {m[0], m[1], m[2], number(sh.n_list), number(sh.n_back)};
-    sum_all(std::integral_constant<int, 5>(), v);
+    uint64_t v[3] = {m[0], m[1], tid == 0 ? (uint64_t)min(sh.n_list, (uint32_t)kCap + 1u) : 0ull};
+    sum_all(std::integral_constant<int, 3>(), v);
     *all = v[0];
-    const uint64_t goal = mass_goal(v[0]);
-    const int which = v[1] >= goal && v[3] <= (uint64_t)kCap ? 1 : v[2] >= goal && v[3] + v[4] <= (uint64_t)kCap ? 2 : 0;
-    if (!which) return false;
-    const uint32_t n_front = lane < (int)n_cta ? (uint32_t)peer_load(&sh.exch[turn ^ 1][3], lane) : 0u;
-    const uint32_t n_back = lane < (int)n_cta && which == 2 ? (uint32_t)peer_load(&sh.exch[turn ^ 1][4], lane) : 0u;
-    uint32_t n = fetch(n_front, 0, false);
-    if (which == 2) n += fetch(n_back, (int)n, true);
+    if (v[1] < mass_goal(v[0]) || v[2] > (uint64_t)kCap) return false;
+    const uint32_t n = fetch(lane < (int)n_cta ? (uint32_t)peer_load(&sh.exch[turn ^ 1][2], lane) : 0u);
     cluster_sync();
     finish_list((int)n, 0, v[0]);
     return true;
@@ -1003,9 +999,9 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
   }
   if (by_k && find_cut(&base, false, (uint64_t)want_k, 0ull) < 0) return;
   if (by_p) {
-    const float e0 = edge_of(bar_with(kShort)), e1 = edge_of(bar_with(kLong));
+    const float edge = edge_of(bar_with(kShort));
     uint64_t all;
-    const bool done = base.value >= -FLT_MAX || !low_is_0 ? nucleus(Yes(), base, e0, e1, &all) : nucleus(No(), base, e0, e1, &all);
+    const bool done = base.value >= -FLT_MAX || !low_is_0 ? nucleus(Yes(), base, edge, &all) : nucleus(No(), base, edge, &all);
     if (done || find_cut(&base, true, mass_goal(all), all) < 0) return;
   }
   if (by_min && least > base.value) base = Cut{least, INT_MIN};
