@@ -28,15 +28,18 @@
 namespace mq {
 namespace {
 
+// (a step that the compiler makes a call of has its operands in local memory, and takes four times as long)
+#define MQ_INLINE __attribute__((always_inline))
+
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kCap = 2048;            // candidates of a list
 constexpr int kMaxCluster = 8;
 constexpr int kGroup = 4;             // pieces of 16 bytes whose maximum is kept
-constexpr int kBars = 1024;           // bars of the histogram of these: eight to a unit, from -64 on
+constexpr int kBars = 1024;           // bars of a histogram: of these, eight to a unit, from -64 on; of all elements, 32 to a unit, up to the maximum's
 constexpr int kPairs = 256;           // a list of up to so many is compared pair by pair
 constexpr int kShort = 160;           // candidates that a nucleus is looked for in first
 constexpr int kLong = 1280;           // the largest k that the groups' bars serve
-constexpr int kEdges = 3;             // values that a narrowing pass sums above
+constexpr int kEdges = 2;             // values that a narrowing pass sums above
 constexpr int kItems = 2 * kEdges > kWarps + 1 ? 2 * kEdges : kWarps + 1;   // what a CTA tells the others at once
 constexpr int kPoint = 43;            // bits behind the point of a weight: 2^20 of them stay below 2^63
 constexpr int kMaxVocab = 1 << 20;
@@ -61,11 +64,11 @@ __device__ __forceinline__ uint32_t order_key(float x) {
   return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
-// floor(8 x) + 512, at most the last bar (x >= -64): the sum with 1.5 * 2^20, rounded down, has it in its low bits
-__device__ __forceinline__ int bar_of(float x) {
-  return (int)(__float_as_uint(__fadd_rd(fminf(x, 63.875f), 1572864.0f)) - __float_as_uint(1572864.0f)) + kBars / 2;
-}
-__device__ __forceinline__ float bar_edge(int b) { return (float)b * 0.125f - 64.0f; }
+// floor(x * 2^23 / 2^e) for a small |x|: the sum with 1.5 * 2^e, rounded down, has it in its low bits
+__device__ __forceinline__ int floor_bits(float x, float magic) { return (int)(__float_as_uint(__fadd_rd(x, magic)) - __float_as_uint(magic)); }
+// floor(8 x) + 512, at most the last bar (x >= -64); floor(32 x)
+__device__ __forceinline__ int bar_of(float x) { return floor_bits(fminf(x, 63.875f), 1572864.0f) + kBars / 2; }
+__device__ __forceinline__ int fine_of(float x) { return floor_bits(fminf(x, 63.96875f), 393216.0f); }
 
 // The larger one; NaN if one of them is
 __device__ __forceinline__ float max_or_nan(float a, float b) {
@@ -102,6 +105,14 @@ __device__ __forceinline__ T peer_load(const T* mine, uint32_t rank) {
   uint32_t v;
   asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(r) : "memory");
   return (T)v;
+}
+
+__device__ __forceinline__ uint4 peer_load4(const uint32_t* mine, uint32_t rank) {
+  uint32_t a = static_cast<uint32_t>(__cvta_generic_to_shared(mine)), r;
+  uint4 v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
+  asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(r) : "memory");
+  return v;
 }
 
 __device__ __forceinline__ uint64_t warp_sum(uint64_t v) {
@@ -200,10 +211,10 @@ struct Smem {
   uint64_t exch[2][kItems];             // what the others fetch
   uint64_t warp_part[kItems][kWarps];
   uint64_t warp_sum[kWarps];
-  uint32_t bars[kBars];
+  alignas(16) uint32_t bars[kBars];
   uint32_t scan[kWarps];
-  uint32_t cum[kThreads];               // of the bars from the maximum's downwards
-  float mass[kThreads];
+  uint32_t cum[kBars];                  // of the bars from the maximum's downwards
+  float mass[kWarps];
   double table[kTable];
   uint32_t n_list;
   int edge[2];
@@ -301,7 +312,7 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const __grid_consta
 
   // fn(x, column of x[0]) for the pieces from, from + step, .. below `to`, several of which are loaded at once (from L2); lanes without a
   // piece get -infinity
-  auto pieces_of = [&](int from, int to, int step, auto fn) {
+  auto pieces_of = [&](int from, int to, int step, auto fn) MQ_INLINE {
     constexpr int kU = 16 / kE;
     for (int v0 = from; __any_sync(0xffffffffu, v0 < to); v0 += step * kU) {
       float x[kU][kE];
@@ -318,7 +329,7 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const __grid_consta
   };
 
   // fn(x, column) for the elements from `least` on; groups without one are not looked at
-  auto elements_from = [&](float least, auto fn) {
+  auto elements_from = [&](float least, auto fn) MQ_INLINE {
     for (int g = 0; g < n_groups; ++g) {
       if (!(r.maxima[g * kThreads + tid] >= least)) continue;
       float x[kGroup][kE];
@@ -340,7 +351,7 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const __grid_consta
 
   // Every thread gets the sum over all CTAs (and their warps) of each of n <= kItems numbers; sh.exch[turn ^ 1] keeps the CTA's own.  An
   // entry of `exch` is written again two sums later, when every CTA has passed the barrier behind its last reading.
-  auto sum_all = [&](auto items, uint64_t* v) {
+  auto sum_all = [&](auto items, uint64_t* v) MQ_INLINE {
     constexpr int n = decltype(items)::value;
 #pragma unroll
     for (int k = 0; k < n; ++k) {
@@ -423,7 +434,7 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const __grid_consta
 
   // The first CTA's list: the entries of every CTA's part, n_q of them in lane q; how many they are.  Called by all behind the barrier that says
   // they are there; followed by one.
-  auto fetch = [&](uint32_t n_q) -> uint32_t {
+  auto fetch = [&](uint32_t n_q) MQ_INLINE -> uint32_t {
 #pragma unroll
     for (int o = 1; o < kMaxCluster; o <<= 1) {
       const uint32_t y = __shfl_up_sync(0xffffffffu, n_q, o);
@@ -446,7 +457,7 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const __grid_consta
 
   // ---- the elements from `least` on and below `below` that `base` keeps, as (key, index) into the first CTA's list; how many they are, or
   // -1 if too many.  Behind it no CTA needs another one's memory.
-  auto gather = [&](float least, float below, const Cut& base) -> int {
+  auto gather = [&](float least, float below, const Cut& base) MQ_INLINE -> int {
     if (tid == 0) sh.n_list = 0;
     __syncthreads();
     elements_from(least, [&](float x, int i) {
@@ -468,10 +479,11 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const __grid_consta
   // Of the n entries of a[] (all different), taken from the largest on: the one at which the running sum of weight_of(place) reaches `goal`
   // (1 .. the sum of all).  Eight bits at a time, from the first bit on in which they differ, by a histogram of those that have the bits
   // in front, until a bin holds one.  Called by the whole CTA.
-  auto entry_at = [&](const uint64_t* a, int n, uint64_t goal, auto weight_of) -> uint64_t {
-    unsigned long long* bin = reinterpret_cast<unsigned long long*>(sh.bars);   // (which have been read)
-    uint32_t* number = sh.bars + 2 * kThreads;
-    static_assert(kBars >= 3 * kThreads, "two numbers per bin");
+  auto entry_at = [&](const uint64_t* a, int n, uint64_t goal, auto weight_of) MQ_INLINE -> uint64_t {
+    // (The bars have been read.  A bin's sum is two words, the carry taken from what the lower one was: many entries may share a bin, and a 64-bit sum
+    // in shared memory is a loop then.)
+    uint32_t *low = sh.bars, *upper = low + kThreads, *number = upper + kThreads;
+    static_assert(kBars >= 3 * kThreads, "three words per bin");
     uint64_t most = 0ull, least_one = ~0ull;
     for (int k = tid; k < n; k += kThreads)
       if (weight_of(k)) {
@@ -499,19 +511,19 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const __grid_consta
     while (pos > 0) {
       const int to = max(0, pos - 8);
       __syncthreads();
-      bin[tid] = 0ull;
-      number[tid] = 0u;
+      low[tid] = upper[tid] = number[tid] = 0u;
       __syncthreads();
       for (int k = tid; k < n; k += kThreads) {
         const uint64_t v = a[k], w = weight_of(k);
         if (w && (pos == 64 || v >> pos == head)) {
           const int d = (int)(v >> to) & ((1 << (pos - to)) - 1);
-          atomicAdd(&bin[d], (unsigned long long)w);
+          const uint32_t was = atomicAdd(&low[d], (uint32_t)w), more = (uint32_t)(w >> 32) + (was + (uint32_t)w < was ? 1u : 0u);
+          if (more) atomicAdd(&upper[d], more);
           atomicAdd(&number[d], 1u);
         }
       }
       __syncthreads();
-      const uint64_t mine = bin[255 - tid];
+      const uint64_t mine = (uint64_t)upper[255 - tid] << 32 | low[255 - tid];
       uint64_t inc = mine;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -549,7 +561,7 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const __grid_consta
   auto index_of = [](uint64_t entry) { return (int)~(uint32_t)entry; };
 
   // ---- the first CTA finishes on a list that holds every kept element; S1's mass is `mass` or, with k, that of the list's first k
-  auto finish_list = [&](int n, int k, uint64_t mass) {
+  auto finish_list = [&](int n, int k, uint64_t mass) MQ_INLINE {
     if (rank != 0) return;
     if (n <= kPairs) {
       // every pair compared, `share` neighbouring threads to an element
@@ -635,7 +647,7 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const __grid_consta
   };
 
   // ---- mass (or count) and count of the elements from each of the values on, of those that `base` keeps where there is one
-  auto sums_from = [&](auto with_mass, auto with_base, const float (&at)[kEdges], const Cut& base, uint64_t (&mass)[kEdges], uint64_t (&count)[kEdges]) {
+  auto sums_from = [&](auto with_mass, auto with_base, const float (&at)[kEdges], const Cut& base, uint64_t (&mass)[kEdges], uint64_t (&count)[kEdges]) MQ_INLINE {
     constexpr bool kMass = decltype(with_mass)::value, kBase = decltype(with_base)::value;
     uint64_t m[kEdges];
     uint32_t c[kEdges];
@@ -673,7 +685,7 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const __grid_consta
 
   // ---- kept elements, a warp's contiguous range at a time: weights (or ones) summed, and the first column at which the running sum exceeds
   // `at(total)`: known to the CTA that holds it, -1 elsewhere
-  auto column_of = [&](auto as_weights, auto all_kept, const Cut& base, bool equal_only, auto at, uint64_t* total, uint64_t* count) -> int {
+  auto column_of = [&](auto as_weights, auto all_kept, const Cut& base, bool equal_only, auto at, uint64_t* total, uint64_t* count) MQ_INLINE -> int {
     constexpr bool kW = decltype(as_weights)::value, kAll = decltype(all_kept)::value;
     auto term = [&](float x, int i, uint32_t* n) -> uint64_t {
       const uint64_t w = kW ? weight(x) : 1ull;
@@ -791,61 +803,132 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const __grid_consta
   using No = std::integral_constant<bool, false>;
 
 
-  // ---- the bars of all CTAs, from the maximum's (bar `high`) downwards: sh.cum[t] of the bars high .. high - t
-  const int high = bar_of(fmaxf(top, -64.0f));
-  auto add_bars = [&]() {
-    uint32_t n = 0u;
-    if (high - tid > 0)
-      for (uint32_t q = 0; q < n_cta; ++q) n += peer_load(&sh.bars[high - tid], q);
-    uint32_t inc = n;
+  // ---- the bars of all CTAs, from the maximum's downwards: sh.cum[t] of the first t + 1.  n_bars of them, `first` is the maximum's
+  int high = 0, n_bars = 0;
+  float per_unit = 8.0f;
+  auto edge_of = [&](int t) { return t < n_bars ? (float)(high - t) * (1.0f / per_unit) : INFINITY; };
+  auto add_bars = [&](auto each, int first) MQ_INLINE {   // each: bars of a thread
+    constexpr int kPer = decltype(each)::value;
+    uint32_t n[kPer], sum = 0u;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) n[k] = 0u;
+    if (kPer == 4) {   // (16 bytes at a time: first is one less than a multiple of four)
+      for (uint32_t q = 0; q < n_cta; ++q) {
+        const uint4 b = peer_load4(&sh.bars[first - 3 - 4 * tid], q);
+        n[0] += b.w; n[1 % kPer] += b.z; n[2 % kPer] += b.y; n[3 % kPer] += b.x;
+      }
+    } else if (first >= tid) {
+      for (uint32_t q = 0; q < n_cta; ++q) n[0] += peer_load(&sh.bars[first - tid], q);
+    }
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) sum += n[k];
+    uint32_t inc = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const uint32_t y = __shfl_up_sync(0xffffffffu, inc, o);
       if (lane >= o) inc += y;
     }
+    __syncthreads();
     if (lane == 31) sh.scan[warp] = inc;
     __syncthreads();
+    inc -= sum;
     for (int w = 0; w < warp; ++w) inc += sh.scan[w];
-    sh.cum[tid] = inc;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      inc += n[k];
+      sh.cum[tid * kPer + k] = inc;
+    }
     __syncthreads();
   };
-  // the bar whose end reaches `want`; kThreads: none
-  auto bar_with = [&](uint64_t want) -> int {
-    const int t = count_if(kThreads, [&](int k) { return (uint64_t)sh.cum[k] < want; });
-    return high - t > 0 ? t : kThreads;
+  // the groups' maxima, 32 units down from the largest: as many elements as groups have a maximum there
+  auto add_groups = [&]() {
+    const int bar = bar_of(fmaxf(top, -64.0f));
+    high = bar - kBars / 2;
+    n_bars = min(kThreads, bar);   // (bar 0 takes what is far down)
+    per_unit = 8.0f;
+    add_bars(std::integral_constant<int, 1>(), bar);
   };
-  auto edge_of = [&](int t) { return t < kThreads ? bar_edge(high - t) : INFINITY; };
-  // The bars once more, of all elements instead of the groups' maxima
+  // all elements, 32 units down
   bool of_elements = false;
   auto count_elements = [&]() {
     if (of_elements) return;
     of_elements = true;
-    cluster_sync();
+    cluster_sync();   // (the groups' bars have been read)
     for (int k = tid; k < kBars; k += kThreads) sh.bars[k] = 0u;
     __syncthreads();
-    const float from = fmaxf(bar_edge(max(1, high - kThreads + 1)), bar_edge(1));
+    high = fine_of(fmaxf(top, -64.0f));
+    n_bars = kBars;
+    per_unit = 32.0f;
+    const float from = fmaxf(edge_of(kBars - 1), -64.0f);
     pieces_of(tid, r.pieces, kThreads, [&](float (&x)[kE], int) {
 #pragma unroll
       for (int e = 0; e < kE; ++e)
-        if (x[e] >= from) atomicAdd(&sh.bars[bar_of(x[e])], 1u);
+        if (x[e] >= from) atomicAdd(&sh.bars[fine_of(x[e]) - high + kBars - 1], 1u);
     });
+    n_bars = max(0, min(kBars, high + 64 * 32 + 1));   // (none below -64)
     cluster_sync();
-    add_bars();
+    add_bars(std::integral_constant<int, kBars / kThreads>(), kBars - 1);
+  };
+  // the first bar at whose end there are `want`; n_bars: none
+  auto bar_with = [&](uint64_t want) -> int { return count_if(n_bars, [&](int k) { return (uint64_t)sh.cum[k] < want; }); };
+
+  // ---- top-p: the candidates, those from `edge` on that `base` keeps, with their mass; *all, the mass of S1, is added up from `own` on the way, *have
+  // is theirs.
+  // True: they hold all that is kept, and all is done.
+  auto candidates = [&](const Cut& base, float edge, uint64_t own, uint64_t* all, uint64_t* have) MQ_INLINE -> bool {
+    uint64_t mass = 0ull;
+    if (tid == 0) sh.n_list = 0u;
+    __syncthreads();
+    elements_from(edge, [&](float x, int i) {
+      if (!base.keeps(x, i)) return;
+      const uint32_t at = atomicAdd(&sh.n_list, 1u);
+      if (at < (uint32_t)kCap) part[at] = (uint64_t)order_key(x) << 32 | (uint32_t)~i;
+      mass += weight(x);
+    });
+    __syncthreads();
+    uint64_t v[3] = {own, mass, tid == 0 ? (uint64_t)min(sh.n_list, (uint32_t)kCap + 1u) : 0ull};
+    sum_all(std::integral_constant<int, 3>(), v);
+    *all += v[0];
+    *have = v[1];
+    if (v[1] < mass_goal(*all) || v[2] > (uint64_t)kCap) return false;
+    const uint32_t n = fetch(lane < (int)n_cta ? (uint32_t)peer_load(&sh.exch[turn ^ 1][2], lane) : 0u);
+    cluster_sync();
+    finish_list((int)n, 0, *all);
+    return true;
+  };
+  // this thread's part of the mass of all that `base` keeps
+  auto mass_of = [&](auto with_base, const Cut& base) MQ_INLINE -> uint64_t {
+    constexpr bool kBase = decltype(with_base)::value;
+    uint64_t m = 0ull;
+    uint32_t terms = 0u;
+    pieces_of(tid, r.pieces, kThreads, [&](float (&x)[kE], int column) {
+#pragma unroll
+      for (int e = 0; e < kE; ++e) {
+        const uint64_t w = weight.biased(x[e]);
+        if (!kBase || base.keeps(x[e], column + e)) {
+          m += w;
+          if (kBase) ++terms;
+        }
+      }
+      if (!kBase) terms += kE;
+    });
+    return m - terms * kBias;
   };
 
-  // ---- where the order is cut: elements are kept as long as less than `goal` (of mass or count) lies before them.  1: *base is the
+  // ---- where the order is cut: elements are kept as long as less than `goal` (of mass or count) lies before them.  From `known_edge` on (if not
+  // infinite), known_mass is known to lie, less than the goal.  1: *base is the
   // cut.  0: all together are less.  -1: all is done, on a list.
-  auto find_cut = [&](Cut* base, bool mass, uint64_t goal, uint64_t all) -> int {
+  auto find_cut = [&](Cut* base, bool mass, uint64_t goal, uint64_t all, float known_edge, uint64_t known_mass) MQ_INLINE -> int {
     const Cut from = *base;
     // less than the goal (above, above_n elements) lies from khi on, and no less from klo on (lo_n elements)
     uint32_t klo = order_key(-FLT_MAX), khi = key_max + 1u;
     uint64_t above = 0ull, above_n = 0ull, lo_n = ~0ull;
     count_elements();
-    int near;       // the bar that the goal lies in, or about where it lies
     bool known = false;
+    int listed = -1;           // entries of the list, where it holds what lies from klo on below khi
     if (!mass) {
-      near = bar_with(goal);
-      known = near < kThreads;   // (exactly: no pass is needed)
+      const int near = bar_with(goal);   // (the counts are exact: no pass is needed)
+      known = near < n_bars;
       if (known) {
         klo = order_key(edge_of(near));
         lo_n = sh.cum[near];
@@ -855,9 +938,19 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const __grid_consta
         }
       }
     } else {
-      // (a bar's elements weigh about as much as its middle)
-      const float mine = (float)(sh.cum[tid] - (tid ? sh.cum[tid - 1] : 0u)) * exp2f(fminf((bar_edge(high - tid) + 0.0625f - top) * (float)weight.c, 0.0f));
-      float inc = mine;
+      // A bar's elements weigh about as much as its middle: that says in which bar the goal lies, as the few heavy ones, of which it would be
+      // too rough, are known.  One pass sums what lies above that bar and puts its elements on a list; where the exact sums say otherwise,
+      // the search below finds it.
+      const int t0 = known_edge < INFINITY ? high - (int)(known_edge * 32.0f) : -1;   // (up to this bar)
+      float sum = 0.0f, w4[4];
+      static_assert(kBars == 4 * kThreads, "four bars to a thread");
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int t = 4 * tid + k;
+        w4[k] = t <= t0 ? 0.0f : (float)(sh.cum[t] - (t ? sh.cum[t - 1] : 0u)) * exp2f(fminf((((float)(high - t) + 0.5f) * (1.0f / 32.0f) - top) * (float)weight.c, 0.0f));
+        sum += w4[k];
+      }
+      float inc = sum;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const float y = __shfl_up_sync(0xffffffffu, inc, o);
@@ -865,26 +958,68 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const __grid_consta
       }
       if (lane == 31) sh.mass[warp] = inc;
       __syncthreads();
-      float total = 0.0f;
-      for (int w = 0; w < kWarps; ++w) {
-        if (w < warp) inc += sh.mass[w];
-        total += sh.mass[w];
+      inc -= sum;
+      for (int w = 0; w < warp; ++w) inc += sh.mass[w];
+      const float want = (float)(goal - known_mass) * (1.0f / (float)(1ull << kPoint));
+      int near = 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        inc += w4[k];
+        near += __syncthreads_count(inc < want);
       }
-      // (in proportion to what all of them weigh)
-      near = __syncthreads_count(inc < total * ((float)goal / (float)all));
-      if (near > high - 2) near = kThreads;
+      if (near + 1 < n_bars && sh.cum[near + 1] <= (uint32_t)kCap) {   // (a bar more, as the guess may be one too few)
+        uint64_t have;
+        if (candidates(from, edge_of(near + 1), 0ull, &all, &have)) return -1;
+      } else if (near < n_bars) {
+        const float e_lo = edge_of(near), e_hi = near > 0 ? edge_of(near - 1) : INFINITY;
+        const bool fits = sh.cum[near] - (near > 0 ? sh.cum[near - 1] : 0u) <= (uint32_t)kCap;
+        uint64_t m[2] = {0ull, 0ull};
+        uint32_t c = 0u;
+        if (tid == 0) sh.n_list = 0u;
+        __syncthreads();
+        pieces_of(tid, r.pieces, kThreads, [&](float (&x)[kE], int column) {
+#pragma unroll
+          for (int e = 0; e < kE; ++e) {
+            const uint64_t w = weight.biased(x[e]);
+            if (x[e] >= e_hi) {
+              m[0] += w;
+              ++c;
+            } else if (x[e] >= e_lo && from.keeps(x[e], column + e)) {
+              m[1] += w - kBias;
+              const uint32_t at = atomicAdd(&sh.n_list, 1u);
+              if (at < (uint32_t)kCap) part[at] = (uint64_t)order_key(x[e]) << 32 | (uint32_t)~(column + e);
+            }
+          }
+        });
+        __syncthreads();
+        // (what `from` cuts off lies below e_hi, or the goal would not be reached there)
+        uint64_t v[4] = {m[0] - c * kBias, m[1], c, tid == 0 ? (uint64_t)sh.n_list : 0ull};
+        sum_all(std::integral_constant<int, 4>(), v);
+        const bool right = from.value < e_hi && v[0] < goal && v[0] + v[1] >= goal;
+        if (right) {
+          klo = order_key(e_lo);
+          lo_n = v[2] + v[3];
+          above = v[0];
+          above_n = v[2];
+          if (near > 0) khi = order_key(e_hi);
+        }
+        known = right;
+        if (right && fits) {
+          listed = (int)fetch(lane < (int)n_cta ? (uint32_t)peer_load(&sh.exch[turn ^ 1][3], lane) : 0u);
+          cluster_sync();
+        }
+      }
     }
     for (int level = 0;; ++level) {
       if (!known) {
-        // Values between, downwards: edges of bars, or some times T below the maximum, first; then evenly, and in the end evenly among the
-        // numbers that there are.  (Of few numbers between, some come twice.)
+        // Values between, downwards: some times T below the maximum and all, where nothing is known; else evenly, and in the end evenly among
+        // the numbers that there are.  (Of few numbers between, some come twice.)
         float at[kEdges];
         const float lo = key_value(klo), h = fminf(key_value(khi), top);
-        const bool even = level > 0 && level < 6 && lo > -1.0e6f && khi - klo > 64u;
+        const bool even = level < 8 && lo > -1.0e6f && khi - klo > 64u;
 #pragma unroll
         for (int k = 0; k < kEdges; ++k) {
-          const float first = near < kThreads ? bar_edge(high - near + 1 - k) : k == kEdges - 1 ? -FLT_MAX : top - temp * (4.0f + 8.0f * (float)k);
-          const float v = level == 0 ? first : lo + (h - lo) * ((float)(kEdges - k) / (float)(kEdges + 1));
+          const float v = lo_n == ~0ull && level == 0 ? (k == 0 ? top - 8.0f * temp : -FLT_MAX) : lo + (h - lo) * ((float)(kEdges - k) / (float)(kEdges + 1));
           at[k] = level == 0 || even ? fminf(fmaxf(v, lo), h) : key_value(klo + (uint32_t)((uint64_t)(khi - klo) * (kEdges - k) / (kEdges + 1)));
         }
         uint64_t m[kEdges], c[kEdges];
@@ -905,17 +1040,17 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const __grid_consta
           if (k == e && order_key(at[e]) >= klo) { klo = order_key(at[e]); lo_n = c[e]; }
       }
       known = false;
-      if (lo_n <= (uint64_t)kCap) {
+      if (listed < 0 && lo_n <= (uint64_t)kCap) {
         const int n = gather(key_value(klo), INFINITY, from);
         finish_list(n, mass ? 0 : (int)goal, all);
         return -1;
       }
       if (lo_n - above_n <= (uint64_t)kCap) {
-        const int n = gather(key_value(klo), key_value(khi), from);
+        if (listed < 0) listed = gather(key_value(klo), key_value(khi), from);
+        // the last one before which less than the goal lies: where the running sum reaches it
         if (rank == 0) {
-          // the last one before which less than the goal lies: where the running sum reaches it
-          for (int j = tid; j < n; j += kThreads) part[j] = mass ? weight(value_of(list[j])) : 1ull;
-          const uint64_t last = entry_at(list, n, goal - above, [&](int j) { return part[j]; });
+          for (int j = tid; j < listed; j += kThreads) part[j] = mass ? weight(value_of(list[j])) : 1ull;
+          const uint64_t last = entry_at(list, listed, goal - above, [&](int j) { return part[j]; });
           if (tid == 0) sh.exch[turn][0] = last;
         }
         cluster_sync();
@@ -941,43 +1076,6 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const __grid_consta
     }
   };
 
-  // ---- top-p: the mass of all that `base` keeps, and the candidates, those from `edge` on, with theirs.  True: that was enough, and all is done.
-  auto nucleus = [&](auto with_base, const Cut& base, float edge, uint64_t* all) -> bool {
-    constexpr bool kBase = decltype(with_base)::value;
-    uint64_t m[2] = {0ull, 0ull};
-    uint32_t terms = 0u;
-    pieces_of(tid, r.pieces, kThreads, [&](float (&x)[kE], int column) {
-#pragma unroll
-      for (int e = 0; e < kE; ++e) {
-        const uint64_t w = weight.biased(x[e]);
-        const bool it = !kBase || base.keeps(x[e], column + e);
-        if (it) {
-          m[0] += w;
-          if (kBase) ++terms;
-        }
-      }
-      if (!kBase) terms += kE;
-    });
-    m[0] -= terms * kBias;
-    if (tid == 0) sh.n_list = 0u;
-    __syncthreads();
-    elements_from(edge, [&](float x, int i) {
-      if (kBase && !base.keeps(x, i)) return;
-      const uint32_t at = atomicAdd(&sh.n_list, 1u);
-      if (at < (uint32_t)kCap) part[at] = (uint64_t)order_key(x) << 32 | (uint32_t)~i;
-      m[1] += weight(x);
-    });
-    __syncthreads();
-    uint64_t v[3] = {m[0], m[1], tid == 0 ? (uint64_t)min(sh.n_list, (uint32_t)kCap + 1u) : 0ull};
-    sum_all(std::integral_constant<int, 3>(), v);
-    *all = v[0];
-    if (v[1] < mass_goal(v[0]) || v[2] > (uint64_t)kCap) return false;
-    const uint32_t n = fetch(lane < (int)n_cta ? (uint32_t)peer_load(&sh.exch[turn ^ 1][2], lane) : 0u);
-    cluster_sync();
-    finish_list((int)n, 0, v[0]);
-    return true;
-  };
-
   Cut base{-INFINITY, INT_MIN};   // (columns in front of a slice are -inf with an index below 0)
   const float least = key_value(order_key(x_min) - 1u);
   if (by_min && !by_k && !by_p) {
@@ -988,7 +1086,7 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const __grid_consta
     }
   }
   const bool short_k = by_k && want_k <= kLong;
-  if (short_k || (by_p && !by_k)) add_bars();   // as many elements as groups have a maximum there
+  if (short_k || (by_p && !by_k)) add_groups();
   if (short_k) {
     const float edge = edge_of(bar_with((uint64_t)want_k));
     const int n = edge < INFINITY ? gather(edge, INFINITY, base) : -1;
@@ -997,12 +1095,14 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const __grid_consta
       return;
     }
   }
-  if (by_k && find_cut(&base, false, (uint64_t)want_k, 0ull) < 0) return;
+  if (by_k && find_cut(&base, false, (uint64_t)want_k, 0ull, INFINITY, 0ull) < 0) return;
   if (by_p) {
     const float edge = edge_of(bar_with(kShort));
-    uint64_t all;
-    const bool done = base.value >= -FLT_MAX || !low_is_0 ? nucleus(Yes(), base, edge, &all) : nucleus(No(), base, edge, &all);
-    if (done || find_cut(&base, true, mass_goal(all), all) < 0) return;
+    uint64_t all = 0ull, have;
+    const uint64_t own = base.value >= -FLT_MAX || !low_is_0 ? mass_of(Yes(), base) : mass_of(No(), base);
+    const bool done = candidates(base, edge, own, &all, &have);
+    const bool short_of = have < mass_goal(all);   // (else they were too many)
+    if (done || find_cut(&base, true, mass_goal(all), all, short_of ? edge : INFINITY, short_of ? have : 0ull) < 0) return;
   }
   if (by_min && least > base.value) base = Cut{least, INT_MIN};
   uint64_t total, count;
