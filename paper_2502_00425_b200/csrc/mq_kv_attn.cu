@@ -74,11 +74,9 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
     for (int i = 0; i < kWarps * C::kStages; ++i) mbar_init(&full[0][0] + i, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  pdl_launch_dependents();
-  pdl_wait();
+  kv_begin<kMode>(p.whole);
   const KvSchedArgs& sc = p.sched;
   sched_prefix<kThreads, kMode>(sc, prefix, red, seqs, page0);
-  kv_clear_refs<kMode>(p.whole);
   const int64_t total = prefix[sc.b.n_seq];
   const int64_t share = sched_share(sc, total, gridDim.x);
   KvRecord rec{};
@@ -395,6 +393,7 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
     rec = KvRecord{};
   }
   if (kMode == kPlain && threadIdx.x == 0) p.parts.rec[blockIdx.x] = rec;
+  kv_end<kMode>();
 }
 
 // Joins the pieces of the units that are split.  kWarps warps share a row and take every kWarps-th piece: four where

@@ -154,11 +154,9 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
     tmem_alloc(&sh->tmem_base, 512);
     tmem_relinquish();
   }
-  pdl_launch_dependents();
-  pdl_wait();
+  kv_begin<kMode>(p.whole);
   const KvSchedArgs& sc = p.sched;
   tc_fence_before();
-  kv_clear_refs<kMode>(p.whole);
   sched_prefix<C::kThreads, kMode>(sc, prefix, red, seqs, page0);   // (ends with __syncthreads)
   tc_fence_after();
   const uint32_t tmem_base = *reinterpret_cast<volatile uint32_t*>(&sh->tmem_base);
@@ -739,6 +737,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
     tc_fence_after();
     tmem_dealloc(tmem_base, 512);
   }
+  kv_end<kMode>();
 }
 
 template <int kD, bool kI8, KvMode kMode>

@@ -61,27 +61,39 @@ constexpr int kMaxSharedSeqs = 1024;   // sequences of a call with shared prefix
 template <int kThreads, KvMode kMode>
 __device__ __forceinline__ void sched_groups(const KvSchedArgs& a, int64_t* prefix, KvSeq* seqs, int* page0) {
   const int n = a.b.n_seq;
+  int mine = -1;                                     // keys that this thread's first sequence can share (-1: it has no rows)
   int* keys = page0 + n;                             // of the group that begins at b
   int2* group = reinterpret_cast<int2*>(prefix);     // its sequences with rows, the last of them
-  for (int b = threadIdx.x; b < n; b += kThreads) {
-    seqs[b] = kv_seq(a.b, a.page_shift, a.max_q, b);
+  for (int b = threadIdx.x; b < n; b += kThreads) {  // (all loads at once; the leader waits in page0's place)
+    const int l = a.leader[b], shared = a.shared_len[b];
+    const KvSeq s = kv_seq(a.b, a.page_shift, a.max_q, b);
+    seqs[b] = s;
+    page0[b] = l;
     keys[b] = INT_MAX;
     group[b] = make_int2(0, b);
+    if (b == threadIdx.x) mine = s.n_new > 0 ? max(0, min(shared, s.n_all - s.n_new)) : -1;
   }
   __syncthreads();
   for (int b = threadIdx.x; b < n; b += kThreads) {
-    const int l = a.leader[b];
+    const int l = page0[b];
     if (l < 0 || l > b) continue;
-    if (a.leader[l] != l || (l < b && a.leader[b - 1] != l)) atomicMin(&keys[l], 0);
-    else if (seqs[b].n_new > 0) {
-      atomicMin(&keys[l], max(0, min(a.shared_len[b], seqs[b].n_all - seqs[b].n_new)));
+    if (page0[l] != l || (l < b && page0[b - 1] != l)) {
+      atomicMin(&keys[l], 0);
+      continue;
+    }
+    if (b != threadIdx.x) {
+      const KvSeq s = seqs[b];
+      mine = s.n_new > 0 ? max(0, min(a.shared_len[b], s.n_all - s.n_new)) : -1;
+    }
+    if (mine >= 0) {
+      atomicMin(&keys[l], mine);
       atomicAdd(&group[l].x, 1);
       atomicMax(&group[l].y, b);
     }
   }
   __syncthreads();
   for (int b = threadIdx.x; b < n; b += kThreads) {
-    const int l = a.leader[b];
+    const int l = page0[b];
     const int pages = l >= 0 && l <= b && group[l].x > 1 ? keys[l] >> a.page_shift : 0;
     page0[b] = kMode == kOwn ? pages : 0;
     if (kMode == kOwn) {
@@ -265,11 +277,27 @@ void kv_set_plan(KvAttnArgs* a, const KvPlan& p, const mq_kv_cache* cache, int m
 int launch_kv_lines(const KvAttnArgs& a, const KvPlan& p, KvMode mode, int dim, bool i8, cudaStream_t st);
 int check_kv_attention(const mq_kv_batch* batch, const mq_kv_cache* cache, int32_t n_q_heads, KvBatchView* bv, KvView* cv);
 
+// The two lines run side by side: kOwn is launched behind kPrefix, but neither reads what the other writes, and where kPrefix leaves SMs idle
+// kOwn begins at once.  For that kPrefix lets it start only when the kernel before both has completed (its own wait is over) and the
+// references are cleared; kOwn then waits for nothing at its start, and at its end for kPrefix, so that the join, which waits for kOwn, has
+// both.
 template <KvMode kMode>
-__device__ __forceinline__ void kv_clear_refs(const KvWhole& w) {
-  if (kMode == kPrefix)
+__device__ __forceinline__ void kv_begin(const KvWhole& w) {
+  if (kMode == kPrefix) {
+    pdl_wait();
     for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < w.n_rows; i += (int64_t)gridDim.x * blockDim.x)
       w.clear[i] = KvRowRef{0, -1, 0, 0};
+    __threadfence();
+    __syncthreads();
+    pdl_launch_dependents();
+  } else {
+    pdl_launch_dependents();
+    if (kMode == kPlain) pdl_wait();
+  }
+}
+template <KvMode kMode>
+__device__ __forceinline__ void kv_end() {
+  if (kMode == kOwn) pdl_wait();
 }
 
 void kv_chunk_shape(int group, int* rows, int* pitch, int* tile, int* extra);
