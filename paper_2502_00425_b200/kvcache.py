@@ -3,6 +3,9 @@
 `PagedKVCache` owns the pool of pages, says which pages hold which sequence, and turns "these sequences get so many new
 tokens" into the device arrays that mq_qk_norm_rope, mq_kv_attention, mq_kv_weights and mq_kv_evict take.  Lengths and
 page lists are kept on the host (that is where a serving program decides); nothing here computes on keys or values.
+
+`DeviceKVCache` keeps lengths, page lists and free pages on the GPU instead (mq_kv_plan), so that whole steps can be captured in a graph
+and replayed, lets sequences end and begin again, and shares prefixes between them (mq_kv_attention_shared).
 """
 from __future__ import annotations
 
@@ -27,6 +30,18 @@ class CacheStep:
 
     def cu_q_host(self, b: int) -> int:
         return sum(self.new[:b])
+
+
+def _workspace(cache, need: int) -> torch.Tensor:
+    size = max(1 << 16, 1 << (need - 1).bit_length())
+    if size not in cache._ws:
+        if torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("run a step of this size once before capturing it: its workspace has to be made first")
+        ws = torch.empty(size, dtype=torch.uint8, device=cache.device)
+        with torch.cuda.device(ws.device):
+            B.mq_reset_device_status(ws)
+        cache._ws[size] = ws
+    return cache._ws[size]
 
 
 class PagedKVCache:
@@ -117,16 +132,7 @@ class PagedKVCache:
     def workspace(self, step: CacheStep, n_q_heads: int) -> torch.Tensor:
         """A workspace for the step, from a few sizes (powers of two) that are kept as long as the cache: a captured graph may
         hold any of them."""
-        need = B.mq_kv_attention_workspace_bytes(self.n_seq, step.total, step.max_q, self.table.shape[1], n_q_heads, self.handle)
-        size = max(1 << 16, 1 << (need - 1).bit_length())
-        if size not in self._ws:
-            if torch.cuda.is_current_stream_capturing():
-                raise RuntimeError("run a step of this size once before capturing it: its workspace has to be made first")
-            ws = torch.empty(size, dtype=torch.uint8, device=self.device)
-            with torch.cuda.device(ws.device):
-                B.mq_reset_device_status(ws)
-            self._ws[size] = ws
-        return self._ws[size]
+        return _workspace(self, B.mq_kv_attention_workspace_bytes(self.n_seq, step.total, step.max_q, self.table.shape[1], n_q_heads, self.handle))
 
     def attend(self, q: torch.Tensor, step: CacheStep, n_q_heads: int, perm: Optional[torch.Tensor] = None,
                scale: Optional[float] = None) -> torch.Tensor:
@@ -195,3 +201,146 @@ class PagedKVCache:
     def _ok(status: torch.Tensor) -> bool:
         with torch.cuda.device_of(status):      # (in the order of the calls, which run on its device's stream)
             return B.mq_last_device_status(status)[0] == B.MQ_OK
+
+
+class DeviceKVCache:
+    """A paged cache for one decoder block whose bookkeeping lives on the GPU: every step (extend) is one call on the stream, nothing waits,
+    and a captured step goes on from whatever the cache holds when it is replayed.  What cannot be done (no free page, a sequence
+    beyond the pages that max_len needs) makes a step without rows, and shows in status_ok().  Arguments as PagedKVCache's; it accumulates no weights and
+    evicts nothing.  Its calls, and replays of graphs that captured them, follow one another in stream order."""
+
+    def __init__(self, n_seq: int, n_pages: int, max_len: int, n_kv_heads: int, head_dim: int, page_size: int = 64,
+                 k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None, device="cuda"):
+        dtype = torch.int8 if k_scale is not None else torch.bfloat16
+        self.K, self.V = (torch.zeros((n_pages, n_kv_heads, page_size, head_dim), dtype=dtype, device=device) for _ in range(2))
+        self.handle = B.KVCache(self.K, self.V, k_scale, v_scale)
+        self.n_seq, self.max_len, self.page_size = n_seq, max_len, page_size
+        device = self.device = self.K.device
+        ints = lambda *shape: torch.zeros(shape, dtype=torch.int32, device=device)
+        self.table = ints(n_seq, -(-max_len // page_size)).fill_(-1)
+        self.kv_len, self.seen, self.borrowed, self.shared_len = (ints(n_seq) for _ in range(4))
+        self.leader = torch.arange(n_seq, dtype=torch.int32, device=device)
+        self.free = torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=device)
+        self.n_free = torch.full((1,), n_pages, dtype=torch.int32, device=device)
+        self.plan_status = ints(2)
+        self.state = B.KVState(self.kv_len, self.seen, self.table, self.free, self.n_free, page_size, borrowed=self.borrowed)
+        self.leaders = list(range(n_seq))   # as `leader` says
+        self._lent = [0] * n_seq            # keys that others have from a sequence
+        self._ws = {}
+        self._numbers = {}                  # small device arrays, by what they hold
+        self._captured = set()              # those that a graph may hold
+        self._last: Optional[CacheStep] = None
+
+    def _ints(self, values: Sequence[int]) -> torch.Tensor:
+        key = tuple(values)
+        capturing = torch.cuda.is_current_stream_capturing()
+        if key not in self._numbers:
+            if capturing:
+                raise RuntimeError("make a step of these sizes once before capturing it: its arrays have to be made first")
+            if len(self._numbers) >= 256:
+                self._numbers = {k: v for k, v in self._numbers.items() if k in self._captured}
+            self._numbers[key] = torch.tensor(key, dtype=torch.int32).to(self.device)
+        if capturing:
+            self._captured.add(key)
+        return self._numbers[key]
+
+    def _plan(self, new: torch.Tensor, keep: Optional[torch.Tensor], rows: int):
+        cu = torch.empty(self.n_seq + 1, dtype=torch.int32, device=self.device)
+        slots, pos = (torch.empty(rows, dtype=t, device=self.device) for t in (torch.int64, torch.int32))
+        B.mq_kv_plan(self.state, new, cu, slots, pos, self.plan_status, keep=keep)
+        return cu, slots, pos
+
+    def extend(self, new: Sequence[int], keep: Optional[Sequence[int]] = None) -> CacheStep:
+        """Room for new[b] tokens at the end of every sequence b, of which keep[b] keys stay (None: all of every sequence; 0 ends one, and what
+        it gets is a new one), and the arrays of the step that brings them."""
+        assert len(new) == self.n_seq and min(new) >= 0
+        if keep is not None and any(k < n for k, n in zip(keep, self._lent)):
+            raise RuntimeError("a sequence keeps what others borrow from it")
+        total = sum(new)
+        cu, slots, pos = self._plan(self._ints(new), None if keep is None else self._ints(keep), total)
+        self._last = CacheStep(list(new), cu, self.kv_len, slots, pos, total, max(new))
+        return self._last
+
+    def undo(self, step: CacheStep):
+        """Takes back the last extend(): its rows no longer count and their pages are free again."""
+        if step is not self._last:
+            raise RuntimeError("only the last step can be undone")
+        self._last = None
+        got = step.cu_q[1:] - step.cu_q[:-1]          # (none, if the step could not be made)
+        self._plan(self._ints([0] * self.n_seq), self.kv_len - got, 0)
+
+    def share(self, src: int, first: int, count: int) -> int:
+        """Sequences first .. first + count - 1, which are empty, begin with the whole pages of sequence src, which stay its own (it cannot be
+        released before them).  They stand behind src or its other borrowers.  Returns the number of keys they have then; what src has
+        behind its last whole page they get by extend().  Waits for the stream."""
+        to = range(first, first + count)
+        if self.leaders[src] != src or first <= src or any(self.leaders[b] != src for b in range(src, first)):
+            raise RuntimeError("borrowers stand directly behind the sequence they borrow from")
+        if count < 1 or first + count > self.n_seq or any(self.leaders[b] != b for b in to):
+            raise RuntimeError("not that many sequences of their own")
+        lengths = self.lengths()
+        if any(lengths[b] for b in to) or any(b in self.leaders[:b] + self.leaders[b + 1:] for b in to):
+            raise RuntimeError("a sequence that borrows pages is empty, and lends none")
+        pages = lengths[src] // self.page_size
+        rows = slice(first, first + count)
+        self.table[rows] = self.table[src]
+        for array, value in ((self.borrowed, pages), (self.kv_len, pages * self.page_size), (self.shared_len, pages * self.page_size),
+                             (self.leader, src)):
+            array[rows] = value
+        self.seen[rows] = self.seen[src] - (lengths[src] - pages * self.page_size)
+        self.shared_len[src] = 1 << 30                # (as far as the others go)
+        self.leaders[first:first + count] = [src] * count
+        self._lent[src] = max(self._lent[src], pages * self.page_size)
+        self._last = None
+        return pages * self.page_size
+
+    def release(self, sequences: Sequence[int]):
+        """Ends sequences: their own pages are free again."""
+        left = [l for b, l in enumerate(self.leaders) if l != b and b not in sequences]
+        if any(b in left for b in sequences):
+            raise RuntimeError("a sequence cannot end before those that borrow its pages")
+        self._plan(self._ints([0] * self.n_seq), self._ints([0 if b in sequences else 1 << 30 for b in range(self.n_seq)]), 0)
+        for b in sequences:
+            self.leaders[b] = b
+            self._lent[b] = 0
+        for b in range(self.n_seq):
+            if self._lent[b] and b not in self.leaders[:b] + self.leaders[b + 1:]:
+                self._lent[b] = 0
+        self.leader.copy_(torch.tensor(self.leaders, dtype=torch.int32))
+        for b in sequences:
+            self.shared_len[b] = 0
+        self._last = None
+
+    def lengths(self) -> List[int]:
+        """Keys of every sequence (waits for the stream)."""
+        return self.kv_len.tolist()
+
+    @property
+    def _groups(self) -> bool:
+        return any(l != b for b, l in enumerate(self.leaders))
+
+    def workspace(self, step: CacheStep, n_q_heads: int) -> torch.Tensor:
+        """As PagedKVCache.workspace()."""
+        size_of = B.mq_kv_attention_shared_workspace_bytes if self._groups else B.mq_kv_attention_workspace_bytes
+        return _workspace(self, size_of(self.n_seq, step.total, step.max_q, self.table.shape[1], n_q_heads, self.handle))
+
+    def attention(self, q: torch.Tensor, step: CacheStep, n_q_heads: int, perm: Optional[torch.Tensor] = None,
+                  scale: Optional[float] = None):
+        """Attention of the step's rows over the cache (their keys and values are already stored), what a group shares being read once for
+        all of it: the result and the log-sum-exps."""
+        o = torch.empty_like(q)
+        lse = torch.empty((step.total, n_q_heads), device=q.device)
+        ws = self.workspace(step, n_q_heads)
+        if self._groups:
+            B.mq_kv_attention_shared(q, step.cu_q, step.kv_len, self.table, self.leader, self.shared_len, self.handle, n_q_heads, step.max_q, o,
+                                     ws, lse=lse, perm=perm, scale=scale)
+        else:
+            B.mq_kv_attention(q, step.cu_q, step.kv_len, self.table, self.handle, n_q_heads, step.max_q, o, ws, lse=lse, perm=perm, scale=scale)
+        return o, lse
+
+    def accumulate(self, q, lse, step, n_q_heads, perm=None, scale=None):
+        """(This cache keeps no weights.)"""
+
+    def status_ok(self) -> bool:
+        """Whether every step could be made and every attention went through (waits for the current stream)."""
+        return all(PagedKVCache._ok(s) for s in [*self._ws.values(), self.plan_status])

@@ -313,7 +313,7 @@ class W4A8DecoderBlock:
         return x2
 
     def forward_cached(self, embs, cache, is_visuals=None, calibrate: bool = False):
-        """New tokens of every sequence of a PagedKVCache (one each, a few, or a chunk; empty ones are allowed): lists of
+        """New tokens of every sequence of a PagedKVCache or DeviceKVCache (one each, a few, or a chunk; empty ones are allowed): lists of
         bf16 [n_b, hidden] and, where a chunk has visual tokens, uint8 [n_b] (None for a chunk of text, or for all of them: no
         reordering then).  Queries and
         keys are normed (g_q, g_k, if set) and rotated (by `rope`, if set) at their positions behind what the cache holds, keys and values
@@ -392,6 +392,53 @@ class W4A8DecoderBlock:
     def device_status_ok(self) -> bool:
         return (all(B.mq_last_device_status(ws)[0] == B.MQ_OK for ws in self._ws.values())
                 and all(int(status[0]) == B.MQ_OK for _, status in self._attn_ws.values()))
+
+
+class W4A8Head:
+    """What follows the last block of a decoder: RMSNorm, the W4A8 linear to the vocabulary with float32 logits, and the next tokens from
+    them (mq_sample).  The linear's N is a multiple of 16; the vocabulary may be smaller.  Rows are text."""
+
+    def __init__(self, weights: LinearWeights, gain: torch.Tensor, vocab: Optional[int] = None):
+        self.w, self.gain, self.vocab = weights, gain, weights.N if vocab is None else vocab
+        if not 0 < self.vocab <= weights.N:
+            raise ValueError(f"a vocabulary of {self.vocab} in a linear of {weights.N}")
+        empty = lambda t: torch.empty(0, dtype=t, device=gain.device)
+        self._seg = B.Segments(empty(torch.int32), empty(torch.uint8))
+        self._ws: Dict[int, torch.Tensor] = {}     # by the number of rows; kept, as a captured graph may hold any of them
+
+    def logits(self, x: torch.Tensor) -> torch.Tensor:
+        """float32 [rows, vocab] of the last block's output, bf16 [rows, hidden]."""
+        T, w = x.shape[0], self.w
+        if T == 0:
+            return torch.empty((0, self.vocab), device=x.device)
+        if T not in self._ws:
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("run this many rows once before capturing them: their workspace has to be made first")
+            self._ws[T] = B.new_workspace(T, w.K, w.N, w.rot_block, device=x.device)
+        h = torch.empty_like(x)
+        B.mq_glue_rmsnorm(x, self.gain, h)
+        y = torch.empty((T, w.N), device=x.device)
+        B.mq_w4a8_msq_linear(h, self._seg, w.s_vis, w.s_txt, w.layout, w.s_w, y, self._ws[T], w.N, rot_block=w.rot_block, bias=w.bias)
+        return y[:, :self.vocab]
+
+    def next_tokens(self, x: torch.Tensor, temperature: torch.Tensor, u: torch.Tensor, top_k=None, top_p=None, min_p=None, logp=None,
+                    kept=None) -> torch.Tensor:
+        """The next token of every row (int32), by mq_sample's parameters and one random number per row."""
+        token = torch.empty(x.shape[0], dtype=torch.int32, device=x.device)
+        B.mq_sample(self.logits(x), temperature, u, token, top_k=top_k, top_p=top_p, min_p=min_p, logp=logp, kept=kept)
+        return token
+
+    def device_status_ok(self) -> bool:
+        return all(B.mq_last_device_status(ws)[0] == B.MQ_OK for ws in self._ws.values())
+
+
+def random_head(hidden: int, vocab: int, seed: int, device="cuda") -> W4A8Head:
+    """A head with random valid weight bytes and scales, as random_block()."""
+    g = torch.Generator(device="cpu").manual_seed(seed)
+    N = -(-vocab // 16) * 16
+    lay = torch.randint(0, 256, (B.mq_w4_layout_bytes(N, hidden),), dtype=torch.uint8, generator=g).to(device)
+    w = LinearWeights(lay, (torch.rand(N, generator=g) * 0.002 + 0.0005).to(device), hidden, N, s_vis=0.03, s_txt=0.03)
+    return W4A8Head(w, torch.ones(hidden, device=device), vocab)
 
 
 def random_block(shape: LayerShape, seed: int, device="cuda") -> W4A8DecoderBlock:

@@ -4,12 +4,14 @@ import math
 
 import numpy as np
 import pytest
+import torch
 
 from oracle import kv_oracle as O
 from oracle import plan_oracle as P
 from oracle import sample_oracle as S
 from paper_2502_00425_b200 import binding as B
 from paper_2502_00425_b200 import build
+from paper_2502_00425_b200 import kvcache as KC
 
 A = 0x10000   # a fake, aligned device address: validation must come before it is used
 
@@ -147,3 +149,101 @@ def test_shared_attention_refusals(lib):
     assert size() > 2 * 5 * 8 * 128 * 4 and call(wsb=size() - 1) == B.MQ_ERR_WORKSPACE
     assert size(n=1025) == size(max_q=6) == 0
     assert call(n_seq=0, total=0, max_q=0) == call(total=0, max_q=0) == B.MQ_OK     # nothing to do
+
+
+# ------------------------------------------------------------------------------------------------ the cache whose bookkeeping is on the GPU
+class _State:
+    def __init__(self, kv_len, seen, table, free, n_free, page, borrowed=None):
+        self.t = dict(kv_len=kv_len, seen=seen, table=table, free=free, n_free=n_free, borrowed=borrowed)
+        self.page = page
+
+
+def _plan(state, new, cu, slots, pos, status=None, keep=None):
+    """mq_kv_plan on the CPU, by the oracle."""
+    t = state.t
+    host = {k: t[k].tolist() for k in ("kv_len", "seen", "borrowed", "table")}
+    host.update(free=t["free"][:int(t["n_free"])].tolist(), n_pages=len(t["free"]))
+    try:
+        got = P.plan(host, new.tolist(), None if keep is None else keep.tolist(), len(slots), state.page)
+    except P.Refused as e:
+        cu.zero_(), slots.fill_(-1), pos.zero_()
+        status[:] = torch.tensor([B.MQ_ERR_WORKSPACE, e.args[0]])
+        return
+    for to, v in zip((cu, slots, pos), got):
+        to[:] = torch.tensor(v, dtype=to.dtype)
+    for k in ("kv_len", "seen", "borrowed", "table"):
+        t[k][:] = torch.tensor(host[k], dtype=torch.int32)
+    t["free"][:len(host["free"])] = torch.tensor(host["free"], dtype=torch.int32)
+    t["n_free"][0] = len(host["free"])
+
+
+class _Handle:
+    def __init__(self, K, V, k_scale=None, v_scale=None):
+        self.n_kv_heads, self.head_dim, self.page_size, self.device = K.shape[1], K.shape[3], K.shape[2], K.device
+
+
+@pytest.fixture
+def make(monkeypatch):
+    monkeypatch.setattr(B, "KVCache", _Handle)
+    monkeypatch.setattr(B, "KVState", _State)
+    monkeypatch.setattr(B, "mq_kv_plan", _plan)
+    monkeypatch.setattr(B, "mq_last_device_status", lambda ws: (int(ws[0]), 0))
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    return lambda *args, **kw: KC.DeviceKVCache(*args, device="cpu", **kw)
+
+
+def _pages(cache, b):
+    return cache.table[b, :-(-int(cache.kv_len[b]) // cache.page_size)].tolist()
+
+
+def test_steps_of_the_device_cache_and_their_undoing(make):
+    cache = make(3, 12, 100, 2, 64, page_size=16)
+    step = cache.extend([20, 0, 33])
+    assert step.cu_q.tolist() == [0, 20, 20, 53] and step.total == 53 and step.max_q == 33 and step.cu_q_host(2) == 20
+    assert cache.lengths() == [20, 0, 33] and int(cache.n_free) == 7 and step.pos.tolist() == list(range(20)) + list(range(33))
+    free = cache.free[:7].tolist()
+    again = cache.extend([1, 40, 1])
+    cache.undo(again)
+    assert cache.lengths() == [20, 0, 33] and cache.free[:int(cache.n_free)].tolist() == free and cache.seen.tolist() == [20, 0, 33]
+    for s in (step, again):
+        with pytest.raises(RuntimeError):
+            cache.undo(s)
+    assert cache.status_ok()
+    refused = cache.extend([93, 0, 0])                       # behind the seven pages of max_len: no rows, nothing changes
+    assert refused.cu_q.tolist() == [0] * 4 and set(refused.slots.tolist()) == {-1} and cache.lengths() == [20, 0, 33]
+    cache.undo(refused)
+    assert cache.lengths() == [20, 0, 33] and not cache.status_ok()
+    cache.extend([5, 1, 1], keep=[10, 9, 0])
+    assert cache.lengths() == [15, 1, 1] and cache.seen.tolist() == [15, 1, 1]
+
+
+def test_sharing_in_the_device_cache(make):
+    cache = make(6, 40, 200, 2, 64, page_size=16)
+    cache.extend([70, 0, 0, 0, 30, 0])
+    assert cache.share(0, 1, 2) == 64
+    assert cache.lengths() == [70, 64, 64, 0, 30, 0] and cache.seen.tolist() == [70, 64, 64, 0, 30, 0]
+    assert _pages(cache, 1) == _pages(cache, 0)[:4] and cache.leaders == [0, 0, 0, 3, 4, 5] == cache.leader.tolist()
+    assert cache.share(0, 3, 1) == 64
+    for src, first, count in ((1, 4, 1), (4, 3, 1), (0, 5, 1), (4, 5, 2), (4, 5, 0), (0, 4, 1)):
+        with pytest.raises(RuntimeError):
+            cache.share(src, first, count)
+    before = int(cache.n_free)
+    cache.extend([1, 6, 7, 20, 0, 0])
+    assert cache.lengths() == [71, 70, 71, 84, 30, 0] and before - int(cache.n_free) == 4
+    assert all(_pages(cache, b)[4:] and not set(_pages(cache, b)[4:]) & set(_pages(cache, 0)) for b in (1, 2, 3))
+    for call in (lambda: cache.release([0]), lambda: cache.release([0, 1]), lambda: cache.extend([0] * 6, keep=[60] + [1 << 30] * 5)):
+        with pytest.raises(RuntimeError):
+            call()
+    cache.release([1, 3])
+    assert cache.lengths() == [71, 0, 71, 0, 30, 0] and cache.leaders == [0, 1, 0, 3, 4, 5] and cache.borrowed.tolist() == [0, 0, 4, 0, 0, 0]
+    cache.release([0, 2])
+    assert int(cache.n_free) == 40 - 2 and cache.leader.tolist() == list(range(6)) and not cache._groups
+    cache.extend([0] * 6, keep=[0] * 6)
+    assert int(cache.n_free) == 40 and sorted(cache.free.tolist()) == list(range(40)) and cache.status_ok()
+
+
+def test_numbers_of_the_device_cache_stay_few(make):
+    cache = make(2, 1000, 4000, 2, 64, page_size=16)
+    for n in range(600):
+        cache.extend([n % 300, 0], keep=[n % 7, n])
+    assert len(cache._numbers) <= 256
