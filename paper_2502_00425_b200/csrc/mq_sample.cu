@@ -32,6 +32,7 @@ namespace {
 #define MQ_INLINE __attribute__((always_inline))
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kCtas = 4;              // to an SM (256 x 150001, top-k 50: 66 us, 76 with 3)
 constexpr int kCap = 2048;            // candidates of a list
 constexpr int kMaxCluster = 8;
 constexpr int kGroup = 4;             // pieces of 16 bytes whose maximum is kept
@@ -224,10 +225,11 @@ struct Smem {
 
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 4) sample_kernel(const __grid_constant__ SampleArgs p) {
+__global__ void __launch_bounds__(kThreads, kCtas) sample_kernel(const __grid_constant__ SampleArgs p) {
   constexpr int kE = Row<T>::kE;
   extern __shared__ __align__(16) uint8_t dyn[];
   uint64_t *list = reinterpret_cast<uint64_t*>(dyn), *part = list + kCap;
+  uint32_t* fine = reinterpret_cast<uint32_t*>(dyn);   // bars of all elements, where the list comes later
   __shared__ Smem<T> sh;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const uint32_t rank = cluster_rank(), n_cta = cluster_size();
@@ -807,18 +809,18 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const __grid_consta
   int high = 0, n_bars = 0;
   float per_unit = 8.0f;
   auto edge_of = [&](int t) { return t < n_bars ? (float)(high - t) * (1.0f / per_unit) : INFINITY; };
-  auto add_bars = [&](auto each, int first) MQ_INLINE {   // each: bars of a thread
+  auto add_bars = [&](auto each, const uint32_t* bars, int first) MQ_INLINE {   // each: bars of a thread
     constexpr int kPer = decltype(each)::value;
     uint32_t n[kPer], sum = 0u;
 #pragma unroll
     for (int k = 0; k < kPer; ++k) n[k] = 0u;
     if (kPer == 4) {   // (16 bytes at a time: first is one less than a multiple of four)
       for (uint32_t q = 0; q < n_cta; ++q) {
-        const uint4 b = peer_load4(&sh.bars[first - 3 - 4 * tid], q);
+        const uint4 b = peer_load4(bars + first - 3 - 4 * tid, q);
         n[0] += b.w; n[1 % kPer] += b.z; n[2 % kPer] += b.y; n[3 % kPer] += b.x;
       }
     } else if (first >= tid) {
-      for (uint32_t q = 0; q < n_cta; ++q) n[0] += peer_load(&sh.bars[first - tid], q);
+      for (uint32_t q = 0; q < n_cta; ++q) n[0] += peer_load(bars + first - tid, q);
     }
 #pragma unroll
     for (int k = 0; k < kPer; ++k) sum += n[k];
@@ -846,28 +848,36 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const __grid_consta
     high = bar - kBars / 2;
     n_bars = min(kThreads, bar);   // (bar 0 takes what is far down)
     per_unit = 8.0f;
-    add_bars(std::integral_constant<int, 1>(), bar);
+    add_bars(std::integral_constant<int, 1>(), sh.bars, bar);
   };
-  // all elements, 32 units down
-  bool of_elements = false;
-  auto count_elements = [&]() {
-    if (of_elements) return;
-    of_elements = true;
-    cluster_sync();   // (the groups' bars have been read)
-    for (int k = tid; k < kBars; k += kThreads) sh.bars[k] = 0u;
+  // all elements, 32 units down (for top-p alone as far as there is some weight): counted along with another pass, or by one of their own
+  const int fine_high = fine_of(fmaxf(top, -64.0f));
+  const float fine_from = fmaxf(fmaxf((float)(fine_high - kBars + 1) * (1.0f / 32.0f), -64.0f), by_k ? -64.0f : top - 20.0f * temp);
+  int fine_state = 0;   // 1: counted, by all CTAs; 2: added up
+  auto count_fine = [&](float x) {
+    if (x >= fine_from) atomicAdd(&fine[fine_of(x) - fine_high + kBars - 1], 1u);
+  };
+  auto clear_fine = [&]() {
     __syncthreads();
-    high = fine_of(fmaxf(top, -64.0f));
-    n_bars = kBars;
-    per_unit = 32.0f;
-    const float from = fmaxf(edge_of(kBars - 1), -64.0f);
-    pieces_of(tid, r.pieces, kThreads, [&](float (&x)[kE], int) {
+    for (int k = tid; k < kBars; k += kThreads) fine[k] = 0u;
+    __syncthreads();
+  };
+  auto add_elements = [&]() {
+    if (fine_state == 0) {
+      clear_fine();
+      pieces_of(tid, r.pieces, kThreads, [&](float (&x)[kE], int) {
 #pragma unroll
-      for (int e = 0; e < kE; ++e)
-        if (x[e] >= from) atomicAdd(&sh.bars[fine_of(x[e]) - high + kBars - 1], 1u);
-    });
-    n_bars = max(0, min(kBars, high + 64 * 32 + 1));   // (none below -64)
-    cluster_sync();
-    add_bars(std::integral_constant<int, kBars / kThreads>(), kBars - 1);
+        for (int e = 0; e < kE; ++e) count_fine(x[e]);
+      });
+      cluster_sync();
+    }
+    if (fine_state < 2) {
+      high = fine_high;
+      n_bars = max(0, min(kBars, fine_high + 64 * 32 + 1));   // (none below -64)
+      per_unit = 32.0f;
+      add_bars(std::integral_constant<int, kBars / kThreads>(), fine, kBars - 1);
+    }
+    fine_state = 2;
   };
   // the first bar at whose end there are `want`; n_bars: none
   auto bar_with = [&](uint64_t want) -> int { return count_if(n_bars, [&](int k) { return (uint64_t)sh.cum[k] < want; }); };
@@ -896,9 +906,11 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const __grid_consta
     finish_list((int)n, 0, *all);
     return true;
   };
-  // this thread's part of the mass of all that `base` keeps
+  // this thread's part of the mass of all that `base` keeps; the elements are counted along
   auto mass_of = [&](auto with_base, const Cut& base) MQ_INLINE -> uint64_t {
     constexpr bool kBase = decltype(with_base)::value;
+    const bool counting = fine_state == 0;
+    if (counting) clear_fine();
     uint64_t m = 0ull;
     uint32_t terms = 0u;
     pieces_of(tid, r.pieces, kThreads, [&](float (&x)[kE], int column) {
@@ -909,6 +921,7 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const __grid_consta
           m += w;
           if (kBase) ++terms;
         }
+        if (counting) count_fine(x[e]);
       }
       if (!kBase) terms += kE;
     });
@@ -916,18 +929,21 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const __grid_consta
   };
 
   // ---- where the order is cut: elements are kept as long as less than `goal` (of mass or count) lies before them.  From `known_edge` on (if not
-  // infinite), known_mass is known to lie, less than the goal.  1: *base is the
+  // infinite), known_mass is known to lie, less than the goal.  *all is the mass of all, or becomes, for a
+  // count and a later top-p, the mass of what is kept (0: not found on the way).  1: *base is the
   // cut.  0: all together are less.  -1: all is done, on a list.
-  auto find_cut = [&](Cut* base, bool mass, uint64_t goal, uint64_t all, float known_edge, uint64_t known_mass) MQ_INLINE -> int {
+  auto find_cut = [&](Cut* base, bool mass, uint64_t goal, uint64_t* all, float known_edge, uint64_t known_mass) MQ_INLINE -> int {
     const Cut from = *base;
     // less than the goal (above, above_n elements) lies from khi on, and no less from klo on (lo_n elements)
     uint32_t klo = order_key(-FLT_MAX), khi = key_max + 1u;
     uint64_t above = 0ull, above_n = 0ull, lo_n = ~0ull;
-    count_elements();
+    add_elements();
     bool known = false;
     int listed = -1;           // entries of the list, where it holds what lies from klo on below khi
+    int near, pass = -1;       // pass: the bar whose elements are listed while what lies above is summed
+    uint64_t mass_above = 0ull;
     if (!mass) {
-      const int near = bar_with(goal);   // (the counts are exact: no pass is needed)
+      near = bar_with(goal);   // (the counts are exact)
       known = near < n_bars;
       if (known) {
         klo = order_key(edge_of(near));
@@ -936,6 +952,7 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const __grid_consta
           khi = order_key(edge_of(near - 1));
           above = above_n = sh.cum[near - 1];
         }
+        if (by_p && lo_n > (uint64_t)kCap && lo_n - above_n <= (uint64_t)kCap) pass = near;
       }
     } else {
       // A bar's elements weigh about as much as its middle: that says in which bar the goal lies, as the few heavy ones, of which it would be
@@ -961,7 +978,7 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const __grid_consta
       inc -= sum;
       for (int w = 0; w < warp; ++w) inc += sh.mass[w];
       const float want = (float)(goal - known_mass) * (1.0f / (float)(1ull << kPoint));
-      int near = 0;
+      near = 0;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         inc += w4[k];
@@ -969,45 +986,49 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const __grid_consta
       }
       if (near + 1 < n_bars && sh.cum[near + 1] <= (uint32_t)kCap) {   // (a bar more, as the guess may be one too few)
         uint64_t have;
-        if (candidates(from, edge_of(near + 1), 0ull, &all, &have)) return -1;
+        if (candidates(from, edge_of(near + 1), 0ull, all, &have)) return -1;
       } else if (near < n_bars) {
-        const float e_lo = edge_of(near), e_hi = near > 0 ? edge_of(near - 1) : INFINITY;
-        const bool fits = sh.cum[near] - (near > 0 ? sh.cum[near - 1] : 0u) <= (uint32_t)kCap;
-        uint64_t m[2] = {0ull, 0ull};
-        uint32_t c = 0u;
-        if (tid == 0) sh.n_list = 0u;
-        __syncthreads();
-        pieces_of(tid, r.pieces, kThreads, [&](float (&x)[kE], int column) {
+        pass = near;
+      }
+    }
+    if (pass >= 0) {
+      const float e_lo = edge_of(near), e_hi = near > 0 ? edge_of(near - 1) : INFINITY;
+      const bool fits = sh.cum[near] - (near > 0 ? sh.cum[near - 1] : 0u) <= (uint32_t)kCap;
+      uint64_t m[2] = {0ull, 0ull};
+      uint32_t c = 0u;
+      if (tid == 0) sh.n_list = 0u;
+      __syncthreads();
+      pieces_of(tid, r.pieces, kThreads, [&](float (&x)[kE], int column) {
 #pragma unroll
-          for (int e = 0; e < kE; ++e) {
-            const uint64_t w = weight.biased(x[e]);
-            if (x[e] >= e_hi) {
-              m[0] += w;
-              ++c;
-            } else if (x[e] >= e_lo && from.keeps(x[e], column + e)) {
-              m[1] += w - kBias;
-              const uint32_t at = atomicAdd(&sh.n_list, 1u);
-              if (at < (uint32_t)kCap) part[at] = (uint64_t)order_key(x[e]) << 32 | (uint32_t)~(column + e);
-            }
+        for (int e = 0; e < kE; ++e) {
+          const uint64_t w = weight.biased(x[e]);
+          if (x[e] >= e_hi) {
+            m[0] += w;
+            ++c;
+          } else if (x[e] >= e_lo && from.keeps(x[e], column + e)) {
+            m[1] += w - kBias;
+            const uint32_t at = atomicAdd(&sh.n_list, 1u);
+            if (at < (uint32_t)kCap) part[at] = (uint64_t)order_key(x[e]) << 32 | (uint32_t)~(column + e);
           }
-        });
-        __syncthreads();
-        // (what `from` cuts off lies below e_hi, or the goal would not be reached there)
-        uint64_t v[4] = {m[0] - c * kBias, m[1], c, tid == 0 ? (uint64_t)sh.n_list : 0ull};
-        sum_all(std::integral_constant<int, 4>(), v);
-        const bool right = from.value < e_hi && v[0] < goal && v[0] + v[1] >= goal;
-        if (right) {
-          klo = order_key(e_lo);
-          lo_n = v[2] + v[3];
-          above = v[0];
-          above_n = v[2];
-          if (near > 0) khi = order_key(e_hi);
         }
-        known = right;
-        if (right && fits) {
-          listed = (int)fetch(lane < (int)n_cta ? (uint32_t)peer_load(&sh.exch[turn ^ 1][3], lane) : 0u);
-          cluster_sync();
-        }
+      });
+      __syncthreads();
+      // (what `from` cuts off lies below e_hi, or the goal would not be reached there)
+      uint64_t v[4] = {m[0] - c * kBias, m[1], c, tid == 0 ? (uint64_t)sh.n_list : 0ull};
+      sum_all(std::integral_constant<int, 4>(), v);
+      const bool right = !mass || (from.value < e_hi && v[0] < goal && v[0] + v[1] >= goal);
+      mass_above = v[0];
+      if (right && mass) {
+        klo = order_key(e_lo);
+        lo_n = v[2] + v[3];
+        above = v[0];
+        above_n = v[2];
+        if (near > 0) khi = order_key(e_hi);
+      }
+      known = right;
+      if (right && fits) {
+        listed = (int)fetch(lane < (int)n_cta ? (uint32_t)peer_load(&sh.exch[turn ^ 1][3], lane) : 0u);
+        cluster_sync();
       }
     }
     for (int level = 0;; ++level) {
@@ -1042,7 +1063,7 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const __grid_consta
       known = false;
       if (listed < 0 && lo_n <= (uint64_t)kCap) {
         const int n = gather(key_value(klo), INFINITY, from);
-        finish_list(n, mass ? 0 : (int)goal, all);
+        finish_list(n, mass ? 0 : (int)goal, *all);
         return -1;
       }
       if (lo_n - above_n <= (uint64_t)kCap) {
@@ -1051,10 +1072,21 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const __grid_consta
         if (rank == 0) {
           for (int j = tid; j < listed; j += kThreads) part[j] = mass ? weight(value_of(list[j])) : 1ull;
           const uint64_t last = entry_at(list, listed, goal - above, [&](int j) { return part[j]; });
-          if (tid == 0) sh.exch[turn][0] = last;
+          uint64_t kept = 0ull;
+          if (pass >= 0 && !mass)
+            for (int j = tid; j < listed; j += kThreads) kept += list[j] >= last ? weight(value_of(list[j])) : 0ull;
+          kept = warp_sum(kept);
+          if (lane == 0) sh.warp_part[2][warp] = kept;
+          __syncthreads();
+          if (tid == 0) {
+            for (int w = 1; w < kWarps; ++w) kept += sh.warp_part[2][w];
+            sh.exch[turn][0] = last;
+            sh.exch[turn][1] = mass_above + kept;
+          }
         }
         cluster_sync();
         const uint64_t word = peer_load(&sh.exch[turn][0], 0);
+        if (pass >= 0 && !mass) *all = peer_load(&sh.exch[turn][1], 0);
         turn ^= 1;
         *base = Cut{value_of(word), index_of(word)};
         return 1;
@@ -1095,14 +1127,16 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const __grid_consta
       return;
     }
   }
-  if (by_k && find_cut(&base, false, (uint64_t)want_k, 0ull, INFINITY, 0ull) < 0) return;
+  uint64_t all = 0ull;
+  if (by_k && find_cut(&base, false, (uint64_t)want_k, &all, INFINITY, 0ull) < 0) return;
   if (by_p) {
     const float edge = edge_of(bar_with(kShort));
-    uint64_t all = 0ull, have;
-    const uint64_t own = base.value >= -FLT_MAX || !low_is_0 ? mass_of(Yes(), base) : mass_of(No(), base);
-    const bool done = candidates(base, edge, own, &all, &have);
+    uint64_t own = 0ull, have;
+    if (all == 0ull) own = base.value >= -FLT_MAX || !low_is_0 ? mass_of(Yes(), base) : mass_of(No(), base);
+    if (candidates(base, edge, own, &all, &have)) return;
+    if (fine_state == 0) fine_state = 1;
     const bool short_of = have < mass_goal(all);   // (else they were too many)
-    if (done || find_cut(&base, true, mass_goal(all), all, short_of ? edge : INFINITY, short_of ? have : 0ull) < 0) return;
+    if (find_cut(&base, true, mass_goal(all), &all, short_of ? edge : INFINITY, short_of ? have : 0ull) < 0) return;
   }
   if (by_min && least > base.value) base = Cut{least, INT_MIN};
   uint64_t total, count;
@@ -1151,9 +1185,10 @@ extern "C" int mq_sample(const void* logits, int64_t ld, int32_t B, int32_t V, u
   a.x = logits;
   a.ld = ld;
   a.V = V;
-  // as many CTAs to a row as have 2048 columns each
+  // as many CTAs to a row as have 2048 columns each while all of them run at once; else as have 6144 (256 rows of 32000 with filters as in
+  // use: 75 us with four CTAs, 103 with eight, 83 with two; 64 rows: 41 with eight, 44 with four)
   int cluster = 1;
-  while (cluster < kMaxCluster && V / (cluster * 2) >= 2048) cluster *= 2;
+  while (cluster < kMaxCluster && V / (cluster * 2) >= ((int64_t)B * cluster * 2 <= sm_count() * kCtas ? 2048 : 6144)) cluster *= 2;
   a.per = ((V + cluster - 1) / cluster + 63) / 64 * 64;
   const int slice_bytes = a.per * es + 16;   // (a slice may start inside a 16-byte piece)
   const int maxima = (slice_bytes / 16 + kThreads * kGroup - 1) / (kThreads * kGroup) * kThreads * 4;
