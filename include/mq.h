@@ -650,14 +650,14 @@ int mq_kv_plan(const mq_kv_state* state, const int32_t* new_len, const int32_t* 
  *   min_p   keeps those with w_i >= min_p (<= 0 or NaN: all; above 1 counts as 1);
  * the first of the order is always kept.  token[r] is the first kept index, in the order of the vocabulary, at which the running sum of the
  * kept weights exceeds u[r] times their total (u in [0, 1); what lies outside counts as its nearest).  T <= 0 or NaN: the
- * first of the order.  NaN and -infinity logits are never kept; where every logit is one, token is -1.  Where a logit is +infinity, all
- * others weigh nothing.
+ * first of the order.  NaN and -infinity logits are never kept; where every logit is one, token is -1.  +infinity
+ * counts as the largest finite number of the type.
  *   temperature, u   device float32 [B];  top_k device int32 [B], top_p, min_p device float32 [B], each may be NULL (all kept)
  *   token            device int32 [B]
  *   logp             optional device float32 [B]: log of the kept, renormalised probability of the token (0 if T <= 0, -inf if none)
  *   kept             optional device int32 [B]: how many were kept
- * Weights are fixed-point numbers with 43 bits behind the point and their sums whole numbers: results do not depend on any order of
- * execution.  V at most 2^20, B at most 2^24 (MQ_ERR_UNSUPPORTED).  One kernel; no workspace.
+ * Weights are fixed-point numbers with 43 bits behind the point (off by 2^-44 of the largest weight and 2^-37 of themselves at most; below
+ * 2^-44 they are zero) and their sums whole numbers: results do not depend on any order of execution.  V at most 2^20, B at most 2^24 (MQ_ERR_UNSUPPORTED).  One kernel; no workspace.
  */
 #define MQ_SAMPLE_F32 1u
 int mq_sample(const void* logits, int64_t ld, int32_t B, int32_t V, uint32_t flags, const float* temperature,

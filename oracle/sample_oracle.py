@@ -2,12 +2,12 @@
 import numpy as np
 
 
-def sample(x, temperature, u, top_k=0, top_p=1.0, min_p=0.0):
+def sample(x, temperature, u, top_k=0, top_p=1.0, min_p=0.0, most=float(np.finfo(np.float32).max)):
     """(token, log probability, kept indices ascending) of one row x [V]; token -1 where nothing can be kept.
 
-    Parameters are the float32 / int32 values of the call.
+    Parameters are the float32 / int32 values of the call; most: the largest finite number of x's type, which +infinity counts as.
     """
-    x = np.where(np.isnan(x), -np.inf, np.asarray(x, np.float64)) + 0.0
+    x = np.where(np.isnan(x), -np.inf, np.minimum(np.asarray(x, np.float64), most)) + 0.0
     t, p, mp, u = (float(np.float32(v)) for v in (temperature, top_p, min_p, u))
     order = np.argsort(-x, kind="stable")
     order = order[x[order] > -np.inf]

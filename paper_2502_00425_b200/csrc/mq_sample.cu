@@ -32,7 +32,10 @@ namespace {
 #define MQ_INLINE __attribute__((always_inline))
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kCtas = 4;              // to an SM (256 x 150001, top-k 50: 66 us, 76 with 3)
+// CTAs to an SM.  float32: 256 x 150001, top-k 50: 66 us, 76 with 3.  bf16, whose pieces are twice as many elements in registers: 64 x 131072
+// with filters as in use 67 us, 72 with 4; 1 x 131072, greedy, 6.8 us, 7.9 with 4 (256 x 150001 loses by it: 175 us, 168 with 4)
+template <typename T>
+constexpr int kCtas = sizeof(T) == 4 ? 4 : 3;
 constexpr int kCap = 2048;            // candidates of a list
 constexpr int kMaxCluster = 8;
 constexpr int kGroup = 4;             // pieces of 16 bytes whose maximum is kept
@@ -225,7 +228,7 @@ struct Smem {
 
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads, kCtas) sample_kernel(const __grid_constant__ SampleArgs p) {
+__global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid_constant__ SampleArgs p) {
   constexpr int kE = Row<T>::kE;
   extern __shared__ __align__(16) uint8_t dyn[];
   uint64_t *list = reinterpret_cast<uint64_t*>(dyn), *part = list + kCap;
@@ -315,7 +318,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) sample_kernel(const __grid_co
   // fn(x, column of x[0]) for the pieces from, from + step, .. below `to`, several of which are loaded at once (from L2); lanes without a
   // piece get -infinity
   auto pieces_of = [&](int from, int to, int step, auto fn) MQ_INLINE {
-    constexpr int kU = 16 / kE;
+    constexpr int kU = 8 / kE;   // (code counts: most of it runs once per CTA, from L2.  256 x 150001, flat rows: 407 us, 427 with twice as many)
     for (int v0 = from; __any_sync(0xffffffffu, v0 < to); v0 += step * kU) {
       float x[kU][kE];
 #pragma unroll
@@ -343,11 +346,17 @@ __global__ void __launch_bounds__(kThreads, kCtas) sample_kernel(const __grid_co
 #pragma unroll
           for (int e = 0; e < kE; ++e) x[k][e] = -INFINITY;
       }
+      // (which they are first, then one after the other: fn once per element in line would be code that a warp reads from L2 as it goes)
+      uint32_t hits = 0u;
 #pragma unroll
       for (int k = 0; k < kGroup; ++k)
 #pragma unroll
-        for (int e = 0; e < kE; ++e)
-          if (x[k][e] >= least) fn(x[k][e], r.column((g * kGroup + k) * kThreads + tid) + e);
+        for (int e = 0; e < kE; ++e) hits |= x[k][e] >= least ? 1u << (k * kE + e) : 0u;
+      while (hits) {
+        const int bit = __ffs((int)hits) - 1, i = r.column((g * kGroup + bit / kE) * kThreads + tid) + bit % kE;
+        hits &= hits - 1u;
+        fn(Row<T>::clean(r.widen(r.x[i])), i);
+      }
     }
   };
 
@@ -964,7 +973,9 @@ __global__ void __launch_bounds__(kThreads, kCtas) sample_kernel(const __grid_co
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const int t = 4 * tid + k;
-        w4[k] = t <= t0 ? 0.0f : (float)(sh.cum[t] - (t ? sh.cum[t - 1] : 0u)) * exp2f(fminf((((float)(high - t) + 0.5f) * (1.0f / 32.0f) - top) * (float)weight.c, 0.0f));
+        // (bf16 numbers from 4 on are multiples of a bar's width, and lie at its lower edge)
+        const float edge = (float)(high - t) * (1.0f / 32.0f), at = sizeof(T) == 2 && fabsf(edge) >= 4.0f ? edge : edge + 1.0f / 64.0f;
+        w4[k] = t <= t0 ? 0.0f : (float)(sh.cum[t] - (t ? sh.cum[t - 1] : 0u)) * exp2f(fminf((at - top) * (float)weight.c, 0.0f));
         sum += w4[k];
       }
       float inc = sum;
@@ -1188,7 +1199,7 @@ extern "C" int mq_sample(const void* logits, int64_t ld, int32_t B, int32_t V, u
   // as many CTAs to a row as have 2048 columns each while all of them run at once; else as have 6144 (256 rows of 32000 with filters as in
   // use: 75 us with four CTAs, 103 with eight, 83 with two; 64 rows: 41 with eight, 44 with four)
   int cluster = 1;
-  while (cluster < kMaxCluster && V / (cluster * 2) >= ((int64_t)B * cluster * 2 <= sm_count() * kCtas ? 2048 : 6144)) cluster *= 2;
+  while (cluster < kMaxCluster && V / (cluster * 2) >= ((int64_t)B * cluster * 2 <= sm_count() * (es == 4 ? kCtas<float> : kCtas<__nv_bfloat16>) ? 2048 : 6144)) cluster *= 2;
   a.per = ((V + cluster - 1) / cluster + 63) / 64 * 64;
   const int slice_bytes = a.per * es + 16;   // (a slice may start inside a 16-byte piece)
   const int maxima = (slice_bytes / 16 + kThreads * kGroup - 1) / (kThreads * kGroup) * kThreads * 4;

@@ -1,8 +1,9 @@
 """mq_sample against the float64 definition.
 
-Tokens and counts have to be equal: a weight of the call is off by at most 2^-44 of the largest one and 2^-45 of itself (fixed point and a
-double exponential), so sums over V <= 2^19 tokens are off by less than 2^-25 of the largest weight in the worst case and about 2^-34 as
-roundings add up, which a random border (top_p, u) comes near to once in some 2^20 rows; the constructed cases sum exactly.  logp is one float32 rounding (2^-24, relative) of a logarithm whose argument is off by 2^-30 at most.
+Tokens and counts have to be equal: a weight of the call is off by at most 2^-44 of the largest one and 2^-37 of itself (fixed point; a table
+and a cubic in double), so a border (top_p, u) lies within 2^-36 of its place relative to the total, plus V 2^-44 of the largest weight in the worst
+case.  A random border comes that near to a token's edge once in 2^36 / tokens rows (some 2^19 rows for 10^5 tokens); the constructed
+cases sum exactly.  logp is one float32 rounding (2^-24, relative) of a logarithm whose argument is off by 2^-30 at most.
 """
 import numpy as np
 import pytest
