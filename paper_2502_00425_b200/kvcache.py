@@ -207,11 +207,18 @@ class DeviceKVCache:
     """A paged cache for one decoder block whose bookkeeping lives on the GPU: every step (extend) is one call on the stream, nothing waits,
     and a captured step goes on from whatever the cache holds when it is replayed.  What cannot be done (no free page, a sequence
     beyond the pages that max_len needs) makes a step without rows, and shows in status_ok().  Arguments as PagedKVCache's; it accumulates no weights and
-    evicts nothing.  Its calls, and replays of graphs that captured them, follow one another in stream order."""
+    evicts nothing.  Its calls, and replays of graphs that captured them, follow one another in stream order; a graph holds the groups of
+    its time, and is captured anew after share() or release().
+
+    shared_from: where a step's groups have at least so many numbers (keys and values, times channels) to read again, they are read once by
+    mq_kv_attention_shared; below, the repeated reads come out of L2 faster than two lines of work and their join (one new token each, 8
+    heads of 128, bf16: 32 sequences over 1024 shared keys, 65 million, 23.7 us against 21.0, over 2048 24.1 against 29.0; 8 over 4096 21.5
+    against 17.9, over 8192 26.5 against 29.5; int8 the same in numbers)."""
 
     def __init__(self, n_seq: int, n_pages: int, max_len: int, n_kv_heads: int, head_dim: int, page_size: int = 64,
-                 k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None, device="cuda"):
+                 k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None, device="cuda", shared_from: int = 100_000_000):
         dtype = torch.int8 if k_scale is not None else torch.bfloat16
+        self.shared_from = shared_from
         self.K, self.V = (torch.zeros((n_pages, n_kv_heads, page_size, head_dim), dtype=dtype, device=device) for _ in range(2))
         self.handle = B.KVCache(self.K, self.V, k_scale, v_scale)
         self.n_seq, self.max_len, self.page_size = n_seq, max_len, page_size
@@ -225,7 +232,7 @@ class DeviceKVCache:
         self.plan_status = ints(2)
         self.state = B.KVState(self.kv_len, self.seen, self.table, self.free, self.n_free, page_size, borrowed=self.borrowed)
         self.leaders = list(range(n_seq))   # as `leader` says
-        self._lent = [0] * n_seq            # keys that others have from a sequence
+        self._lent = [0] * n_seq            # keys that others have from a sequence, or that it has from another
         self._ws = {}
         self._numbers = {}                  # small device arrays, by what they hold
         self._captured = set()              # those that a graph may hold
@@ -252,10 +259,10 @@ class DeviceKVCache:
 
     def extend(self, new: Sequence[int], keep: Optional[Sequence[int]] = None) -> CacheStep:
         """Room for new[b] tokens at the end of every sequence b, of which keep[b] keys stay (None: all of every sequence; 0 ends one, and what
-        it gets is a new one), and the arrays of the step that brings them."""
+        it gets is a new one; what is lent or borrowed stays until release()), and the arrays of the step that brings them."""
         assert len(new) == self.n_seq and min(new) >= 0
         if keep is not None and any(k < n for k, n in zip(keep, self._lent)):
-            raise RuntimeError("a sequence keeps what others borrow from it")
+            raise RuntimeError("a sequence keeps what others borrow from it, and what it has borrowed")
         total = sum(new)
         cu, slots, pos = self._plan(self._ints(new), None if keep is None else self._ints(keep), total)
         self._last = CacheStep(list(new), cu, self.kv_len, slots, pos, total, max(new))
@@ -291,11 +298,16 @@ class DeviceKVCache:
         self.shared_len[src] = 1 << 30                # (as far as the others go)
         self.leaders[first:first + count] = [src] * count
         self._lent[src] = max(self._lent[src], pages * self.page_size)
+        self._lent[first:first + count] = [pages * self.page_size] * count
         self._last = None
         return pages * self.page_size
 
     def release(self, sequences: Sequence[int]):
-        """Ends sequences: their own pages are free again."""
+        """Ends sequences: their own pages are free again.  Not while a stream is captured."""
+        if torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("sequences are not released while a stream is captured")
+        if any(not 0 <= b < self.n_seq for b in sequences):
+            raise RuntimeError("no such sequence")
         left = [l for b, l in enumerate(self.leaders) if l != b and b not in sequences]
         if any(b in left for b in sequences):
             raise RuntimeError("a sequence cannot end before those that borrow its pages")
@@ -304,7 +316,7 @@ class DeviceKVCache:
             self.leaders[b] = b
             self._lent[b] = 0
         for b in range(self.n_seq):
-            if self._lent[b] and b not in self.leaders[:b] + self.leaders[b + 1:]:
+            if self.leaders[b] == b and b not in self.leaders[:b] + self.leaders[b + 1:]:
                 self._lent[b] = 0
         self.leader.copy_(torch.tensor(self.leaders, dtype=torch.int32))
         for b in sequences:
@@ -315,23 +327,31 @@ class DeviceKVCache:
         """Keys of every sequence (waits for the stream)."""
         return self.kv_len.tolist()
 
-    @property
-    def _groups(self) -> bool:
-        return any(l != b for b, l in enumerate(self.leaders))
+    def _shares(self, step: CacheStep) -> bool:
+        if self.n_seq > 1024:             # (the shared form's limit; every sequence's pages are in its own row as well)
+            return False
+        rows, keys = {}, {}
+        for b, l in enumerate(self.leaders):
+            if step.new[b]:
+                rows[l] = rows.get(l, 0) + 1
+                if l != b:
+                    keys[l] = min(keys.get(l, self.max_len), self._lent[b])
+        numbers = 2 * self.handle.n_kv_heads * self.handle.head_dim
+        return any(rows[l] > 1 for l in keys) and sum((rows[l] - 1) * k for l, k in keys.items()) * numbers >= self.shared_from
 
     def workspace(self, step: CacheStep, n_q_heads: int) -> torch.Tensor:
         """As PagedKVCache.workspace()."""
-        size_of = B.mq_kv_attention_shared_workspace_bytes if self._groups else B.mq_kv_attention_workspace_bytes
+        size_of = B.mq_kv_attention_shared_workspace_bytes if self._shares(step) else B.mq_kv_attention_workspace_bytes
         return _workspace(self, size_of(self.n_seq, step.total, step.max_q, self.table.shape[1], n_q_heads, self.handle))
 
     def attention(self, q: torch.Tensor, step: CacheStep, n_q_heads: int, perm: Optional[torch.Tensor] = None,
                   scale: Optional[float] = None):
         """Attention of the step's rows over the cache (their keys and values are already stored), what a group shares being read once for
-        all of it: the result and the log-sum-exps."""
+        all of it where that is faster: the result and the log-sum-exps."""
         o = torch.empty_like(q)
         lse = torch.empty((step.total, n_q_heads), device=q.device)
         ws = self.workspace(step, n_q_heads)
-        if self._groups:
+        if self._shares(step):
             B.mq_kv_attention_shared(q, step.cu_q, step.kv_len, self.table, self.leader, self.shared_len, self.handle, n_q_heads, step.max_q, o,
                                      ws, lse=lse, perm=perm, scale=scale)
         else:

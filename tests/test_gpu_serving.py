@@ -69,7 +69,7 @@ def _calibrated(blk):
 def test_shared_prompt_and_answers(int8):
     blk = _calibrated(_block())
     scales = (torch.full((2,), 0.02, device=DEV), torch.full((2,), 0.05, device=DEV)) if int8 else (None, None)
-    cache = KC.DeviceKVCache(5, 60, 300, 2, 128, 16, *scales)
+    cache = KC.DeviceKVCache(5, 60, 300, 2, 128, 16, *scales, shared_from=0)
     prompt = _emb(90, 1)
     none = _emb(0, 1)
     _, tr = blk.forward_cached([prompt, none, none, none, _emb(7, 2)], cache)      # one prompt, and a stranger
@@ -100,7 +100,7 @@ def test_shared_prompt_and_answers(int8):
 
 def test_image_turns_behind_a_shared_prompt():
     blk = _calibrated(_block(3, rope=False))
-    cache = KC.DeviceKVCache(3, 40, 300, 2, 128, 32)
+    cache = KC.DeviceKVCache(3, 40, 300, 2, 128, 32, shared_from=0)
     vis = lambda *runs: torch.cat([torch.full((n,), v, dtype=torch.uint8) for v, n in runs]).to(DEV)
     _, tr = blk.forward_cached([_emb(70, 1), _emb(0, 1), _emb(0, 1)], cache, [vis((0, 10), (1, 50), (0, 10)), None, None])
     _check_attention(cache, tr, [70, 0, 0], tr.perms)
@@ -150,7 +150,7 @@ def test_a_captured_step_goes_on_by_itself():
     us = [torch.from_numpy(rng.random(n).astype(np.float32)).to(DEV) for _ in range(steps + 1)]
     out = []
     for captured in (False, True):
-        cache = KC.DeviceKVCache(n, 60, 200, 2, 128, 16)
+        cache = KC.DeviceKVCache(n, 60, 200, 2, 128, 16, shared_from=0)
         blk.forward_cached([_emb(60, 1), _emb(0, 1), _emb(0, 1), _emb(19, 2)], cache)
         cache.share(0, 1, 2)
         blk.forward_cached([_emb(0, 1), _emb(4, 3), _emb(9, 4), _emb(0, 1)], cache)

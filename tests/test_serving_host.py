@@ -231,13 +231,16 @@ def test_sharing_in_the_device_cache(make):
     cache.extend([1, 6, 7, 20, 0, 0])
     assert cache.lengths() == [71, 70, 71, 84, 30, 0] and before - int(cache.n_free) == 4
     assert all(_pages(cache, b)[4:] and not set(_pages(cache, b)[4:]) & set(_pages(cache, 0)) for b in (1, 2, 3))
-    for call in (lambda: cache.release([0]), lambda: cache.release([0, 1]), lambda: cache.extend([0] * 6, keep=[60] + [1 << 30] * 5)):
+    most = 1 << 30
+    for call in (lambda: cache.release([0]), lambda: cache.release([0, 1]), lambda: cache.extend([0] * 6, keep=[60] + [most] * 5),
+                 lambda: cache.extend([0] * 6, keep=[most, 0] + [most] * 4), lambda: cache.extend([0] * 6, keep=[most, 48] + [most] * 4),
+                 lambda: cache.release([-1]), lambda: cache.release([6])):
         with pytest.raises(RuntimeError):
             call()
     cache.release([1, 3])
     assert cache.lengths() == [71, 0, 71, 0, 30, 0] and cache.leaders == [0, 1, 0, 3, 4, 5] and cache.borrowed.tolist() == [0, 0, 4, 0, 0, 0]
     cache.release([0, 2])
-    assert int(cache.n_free) == 40 - 2 and cache.leader.tolist() == list(range(6)) and not cache._groups
+    assert int(cache.n_free) == 40 - 2 and cache.leader.tolist() == list(range(6)) and cache.leaders == list(range(6))
     cache.extend([0] * 6, keep=[0] * 6)
     assert int(cache.n_free) == 40 and sorted(cache.free.tolist()) == list(range(40)) and cache.status_ok()
 
@@ -247,3 +250,24 @@ def test_numbers_of_the_device_cache_stay_few(make):
     for n in range(600):
         cache.extend([n % 300, 0], keep=[n % 7, n])
     assert len(cache._numbers) <= 256
+
+
+def test_the_shared_form_is_called_where_it_saves_enough(make):
+    cache = make(6, 40, 200, 2, 64, page_size=16)        # 256 numbers to a key
+    cache.extend([70, 0, 0, 40, 0, 0])
+    cache.share(0, 1, 2)
+    cache.share(3, 4, 2)
+    step = cache.extend([1] * 6)
+    for new, numbers in (([1] * 6, (2 * 64 + 2 * 32) * 256), ([0, 1, 1, 0, 0, 0], 64 * 256), ([1, 0, 1, 1, 0, 0], 64 * 256), ([0, 1, 0, 1, 0, 0], None),
+                         ([1, 0, 0, 1, 0, 0], None)):
+        step.new = new
+        for limit, shared in ((0, True), (numbers or 0, True), ((numbers or 0) + 1, False)):
+            cache.shared_from = limit
+            assert cache._shares(step) == (shared and numbers is not None)
+    cache.shared_from = 0
+    cache.release([1, 2, 4, 5])
+    assert not cache._shares(cache.extend([1] * 6))
+    wide = make(1025, 1100, 32, 1, 64, page_size=16, shared_from=0)
+    wide.extend([20] + [0] * 1024)
+    wide.share(0, 1, 2)
+    assert not wide._shares(wide.extend([1] * 1025))
