@@ -74,6 +74,27 @@ __device__ __forceinline__ int floor_bits(float x, float magic) { return (int)(_
 __device__ __forceinline__ int bar_of(float x) { return floor_bits(fminf(x, 63.875f), 1572864.0f) + kBars / 2; }
 __device__ __forceinline__ int fine_of(float x) { return floor_bits(fminf(x, 63.96875f), 393216.0f); }
 
+// An entry of a list: the key of a logit (16 bits say it of a bf16 number), then the index, downwards.  As many bits as can differ: a list is
+// searched by 8 of them at a time.
+constexpr int kIndexBits = 20;
+constexpr uint32_t kIndexMask = (1u << kIndexBits) - 1u;
+template <typename T>
+__device__ __forceinline__ uint64_t entry_of(float x, int i) {
+  return (uint64_t)(order_key(x) >> (sizeof(T) == 2 ? 16 : 0)) << kIndexBits | ((uint32_t)~i & kIndexMask);
+}
+__device__ __forceinline__ int entry_index(uint64_t e) { return (int)(~(uint32_t)e & kIndexMask); }
+template <typename T>
+__device__ __forceinline__ float entry_value(uint64_t e) {
+  const uint32_t k = (uint32_t)(e >> kIndexBits);
+  return key_value(sizeof(T) == 4 ? k : k << 16 | (k & 0x8000u ? 0u : 0xffffu));
+}
+// the first entry whose value is not below x
+template <typename T>
+__device__ __forceinline__ uint64_t first_entry(float x) {
+  const uint32_t k = order_key(x);
+  return (uint64_t)(sizeof(T) == 4 ? k : k & 0x80000000u ? (k + 0xffffu) >> 16 : k >> 16) << kIndexBits;
+}
+
 // The larger one; NaN if one of them is
 __device__ __forceinline__ float max_or_nan(float a, float b) {
   float m;
@@ -474,7 +495,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
     elements_from(least, [&](float x, int i) {
       if (x < below && base.keeps(x, i)) {
         const uint32_t at = atomicAdd(&sh.n_list, 1u);
-        if (at < (uint32_t)kCap) part[at] = (uint64_t)order_key(x) << 32 | (uint32_t)~i;
+        if (at < (uint32_t)kCap) part[at] = entry_of<T>(x, i);
       }
     });
     __syncthreads();
@@ -495,30 +516,28 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
     // in shared memory is a loop then.)
     uint32_t *low = sh.bars, *upper = low + kThreads, *number = upper + kThreads;
     static_assert(kBars >= 3 * kThreads, "three words per bin");
-    uint64_t most = 0ull, least_one = ~0ull;
+    uint64_t any = 0ull, both = ~0ull;
     for (int k = tid; k < n; k += kThreads)
       if (weight_of(k)) {
-        most = max(most, a[k]);
-        least_one = min(least_one, a[k]);
+        any |= a[k];
+        both &= a[k];
       }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
-      least_one = min(least_one, __shfl_xor_sync(0xffffffffu, least_one, o));
-    }
+    any = (uint64_t)__reduce_or_sync(0xffffffffu, (uint32_t)(any >> 32)) << 32 | __reduce_or_sync(0xffffffffu, (uint32_t)any);
+    both = (uint64_t)__reduce_and_sync(0xffffffffu, (uint32_t)(both >> 32)) << 32 | __reduce_and_sync(0xffffffffu, (uint32_t)both);
     __syncthreads();
     if (lane == 0) {
-      sh.warp_part[0][warp] = most;
-      sh.warp_part[1][warp] = least_one;
+      sh.warp_part[0][warp] = any;
+      sh.warp_part[1][warp] = both;
     }
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
-      most = max(most, sh.warp_part[0][w]);
-      least_one = min(least_one, sh.warp_part[1][w]);
+      any |= sh.warp_part[0][w];
+      both &= sh.warp_part[1][w];
     }
-    int pos = 64 - __clzll((long long)(most ^ least_one));   // bits from pos on are known
-    uint64_t head = pos < 64 ? most >> pos : 0ull;
+    uint64_t open = any & ~both;   // bits in which entries differ; the others need no search
+    int pos = 64 - __clzll((long long)open);
+    uint64_t head = pos < 64 ? any >> pos : 0ull;   // the entry's bits from pos on
     while (pos > 0) {
       const int to = max(0, pos - 8);
       __syncthreads();
@@ -550,9 +569,11 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
       }
       __syncthreads();
       const int d = sh.found;
-      head = head << (pos - to) | (uint64_t)d;
+      open &= (1ull << to) - 1ull;
+      const int next = 64 - __clzll((long long)open);
+      head = (head << (pos - to) | (uint64_t)d) << (to - next) | (any >> next & ((1ull << (to - next)) - 1ull));
       goal -= sh.front;
-      pos = to;
+      pos = next;
       if (number[d] == 1u && pos > 0) {
         for (int k = tid; k < n; k += kThreads)
           if (a[k] >> pos == head && weight_of(k)) sh.entry = a[k];
@@ -568,8 +589,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
     for (int k0 = 0; k0 < n; k0 += kThreads) c += __syncthreads_count(k0 + tid < n && pred(k0 + tid));
     return c;
   };
-  auto value_of = [](uint64_t entry) { return key_value((uint32_t)(entry >> 32)); };
-  auto index_of = [](uint64_t entry) { return (int)~(uint32_t)entry; };
+  auto value_of = [](uint64_t entry) { return entry_value<T>(entry); };
 
   // ---- the first CTA finishes on a list that holds every kept element; S1's mass is `mass` or, with k, that of the list's first k
   auto finish_list = [&](int n, int k, uint64_t mass) MQ_INLINE {
@@ -618,10 +638,10 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
       const uint64_t total = sum_block(keep ? w : 0ull);
       const int kept = __syncthreads_count(keep && s0 == 0);
       uint64_t run = 0ull;                      // of those with a lower index
-      for (int i = s0; i < n; i += share) run += (uint32_t)list[i] > (uint32_t)a ? kept_w[i] : 0ull;
+      for (int i = s0; i < n; i += share) run += ((uint32_t)list[i] & kIndexMask) > ((uint32_t)a & kIndexMask) ? kept_w[i] : 0ull;
       run = sum_share(run);
       const uint64_t goal = share_of(u, total, false);
-      if (keep && s0 == 0 && run <= goal && goal - run < w) write(index_of(a), w, total, kept);
+      if (keep && s0 == 0 && run <= goal && goal - run < w) write(entry_index(a), w, total, kept);
       return;
     }
     // the cut, entry by entry; then the index, among those that are kept
@@ -646,15 +666,15 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
       const uint64_t goal = mass_goal(k > 0 ? sum_list(kept_weight) : mass);
       cut = max(cut, entry_at(list, n, goal, [&](int j) { return part[j]; }));
     }
-    if (by_min) cut = max(cut, (uint64_t)order_key(x_min) << 32);
+    if (by_min) cut = max(cut, first_entry<T>(x_min));
     const uint64_t total = sum_list(kept_weight), kept = sum_list([&](int j) { return list[j] >= cut ? 1ull : 0ull; });
-    // (index order is that of the entries' lower halves, downwards)
+    // (the index in front: its order is that of the entries' lowest bits, downwards)
     uint64_t* by_index = part;
     __syncthreads();
-    for (int j = tid; j < n; j += kThreads) list[j] = list[j] >= cut ? list[j] << 32 | list[j] >> 32 : 0ull;
+    for (int j = tid; j < n; j += kThreads) list[j] = list[j] >= cut ? (list[j] & kIndexMask) << 32 | list[j] >> kIndexBits : 0ull;
     __syncthreads();
     const uint64_t found = entry_at(list, n, share_of(u, total, false) + 1ull, [&](int j) { return list[j] ? by_index[j] : 0ull; });
-    if (tid == 0) write((int)~(uint32_t)(found >> 32), weight(key_value((uint32_t)found)), total, (int)kept);
+    if (tid == 0) write(entry_index(found >> 32), weight(value_of(found << kIndexBits)), total, (int)kept);
   };
 
   // ---- mass (or count) and count of the elements from each of the values on, of those that `base` keeps where there is one
@@ -901,7 +921,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
     elements_from(edge, [&](float x, int i) {
       if (!base.keeps(x, i)) return;
       const uint32_t at = atomicAdd(&sh.n_list, 1u);
-      if (at < (uint32_t)kCap) part[at] = (uint64_t)order_key(x) << 32 | (uint32_t)~i;
+      if (at < (uint32_t)kCap) part[at] = entry_of<T>(x, i);
       mass += weight(x);
     });
     __syncthreads();
@@ -951,6 +971,9 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
     int listed = -1;           // entries of the list, where it holds what lies from klo on below khi
     int near, pass = -1;       // pass: the bar whose elements are listed while what lies above is summed
     uint64_t mass_above = 0ull;
+    float* upto = reinterpret_cast<float*>(sh.bars);   // the guessed mass of each bar and those above it (the groups' bars have been read)
+    const float kUnit = 1.0f / (float)(1ull << kPoint);
+    float want = 0.0f;
     if (!mass) {
       near = bar_with(goal);   // (the counts are exact)
       known = near < n_bars;
@@ -973,8 +996,10 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const int t = 4 * tid + k;
-        // (bf16 numbers from 4 on are multiples of a bar's width, and lie at its lower edge)
-        const float edge = (float)(high - t) * (1.0f / 32.0f), at = sizeof(T) == 2 && fabsf(edge) >= 4.0f ? edge : edge + 1.0f / 64.0f;
+        // (the numbers of a bar begin at its lower edge, and bf16's are up to its width apart: their middle is half a step lower)
+        const float edge = (float)(high - t) * (1.0f / 32.0f);
+        const float step = sizeof(T) == 2 ? fminf(__uint_as_float(__float_as_uint(edge) & 0x7f800000u) * (1.0f / 128.0f), 1.0f / 32.0f) : 0.0f;
+        const float at = edge + 0.5f * (1.0f / 32.0f - step);
         w4[k] = t <= t0 ? 0.0f : (float)(sh.cum[t] - (t ? sh.cum[t - 1] : 0u)) * exp2f(fminf((at - top) * (float)weight.c, 0.0f));
         sum += w4[k];
       }
@@ -988,13 +1013,14 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
       __syncthreads();
       inc -= sum;
       for (int w = 0; w < warp; ++w) inc += sh.mass[w];
-      const float want = (float)(goal - known_mass) * (1.0f / (float)(1ull << kPoint));
-      near = 0;
+      want = (float)(goal - known_mass) * kUnit;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         inc += w4[k];
-        near += __syncthreads_count(inc < want);
+        upto[4 * tid + k] = inc;
       }
+      __syncthreads();
+      near = count_if(kBars, [&](int t) { return upto[t] < want; });
       if (near + 1 < n_bars && sh.cum[near + 1] <= (uint32_t)kCap) {   // (a bar more, as the guess may be one too few)
         uint64_t have;
         if (candidates(from, edge_of(near + 1), 0ull, all, &have)) return -1;
@@ -1002,7 +1028,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
         pass = near;
       }
     }
-    if (pass >= 0) {
+    for (int tries = 0; pass >= 0; ++tries) {
       const float e_lo = edge_of(near), e_hi = near > 0 ? edge_of(near - 1) : INFINITY;
       const bool fits = sh.cum[near] - (near > 0 ? sh.cum[near - 1] : 0u) <= (uint32_t)kCap;
       uint64_t m[2] = {0ull, 0ull};
@@ -1010,37 +1036,61 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
       if (tid == 0) sh.n_list = 0u;
       __syncthreads();
       pieces_of(tid, r.pieces, kThreads, [&](float (&x)[kE], int column) {
+        uint32_t hits = 0u;
 #pragma unroll
         for (int e = 0; e < kE; ++e) {
           const uint64_t w = weight.biased(x[e]);
           if (x[e] >= e_hi) {
             m[0] += w;
             ++c;
-          } else if (x[e] >= e_lo && from.keeps(x[e], column + e)) {
-            m[1] += w - kBias;
-            const uint32_t at = atomicAdd(&sh.n_list, 1u);
-            if (at < (uint32_t)kCap) part[at] = (uint64_t)order_key(x[e]) << 32 | (uint32_t)~(column + e);
+          } else if (x[e] >= e_lo) {
+            hits |= 1u << e;
           }
+        }
+        while (hits) {   // (one after the other, as above)
+          const int i = column + __ffs((int)hits) - 1;
+          hits &= hits - 1u;
+          const float v = Row<T>::clean(r.widen(r.x[i]));
+          if (!from.keeps(v, i)) continue;
+          m[1] += weight(v);
+          const uint32_t at = atomicAdd(&sh.n_list, 1u);
+          if (at < (uint32_t)kCap) part[at] = entry_of<T>(v, i);
         }
       });
       __syncthreads();
       // (what `from` cuts off lies below e_hi, or the goal would not be reached there)
       uint64_t v[4] = {m[0] - c * kBias, m[1], c, tid == 0 ? (uint64_t)sh.n_list : 0ull};
       sum_all(std::integral_constant<int, 4>(), v);
-      const bool right = !mass || (from.value < e_hi && v[0] < goal && v[0] + v[1] >= goal);
       mass_above = v[0];
-      if (right && mass) {
+      const bool exact = mass && from.value < e_hi;      // (else `from` cuts among what was summed)
+      const bool low = exact && v[0] + v[1] < goal, over = exact && v[0] >= goal, right = !mass || (exact && !low && !over);
+      if (over) {
+        klo = order_key(e_hi);
+        lo_n = v[2];
+      } else if (low) {
+        khi = order_key(e_lo);
+        above = v[0] + v[1];
+        above_n = v[2] + v[3];
+      } else if (exact) {
         klo = order_key(e_lo);
         lo_n = v[2] + v[3];
         above = v[0];
         above_n = v[2];
         if (near > 0) khi = order_key(e_hi);
       }
+      if ((low || over) && tries < 2) {
+        // the sums say how far off the guess was there, which is most likely what it is off a few bars further, too
+        want = low ? upto[near] + (float)(goal - above) * kUnit : upto[near - 1] - (float)(v[0] - goal) * kUnit;
+        const int at = count_if(kBars, [&](int t) { return upto[t] < want; });
+        near = low ? max(at, near + 1) : min(at, near - 1);
+        if (near < n_bars) continue;
+      }
       known = right;
       if (right && fits) {
         listed = (int)fetch(lane < (int)n_cta ? (uint32_t)peer_load(&sh.exch[turn ^ 1][3], lane) : 0u);
         cluster_sync();
       }
+      break;
     }
     for (int level = 0;; ++level) {
       if (!known) {
@@ -1099,7 +1149,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
         const uint64_t word = peer_load(&sh.exch[turn][0], 0);
         if (pass >= 0 && !mass) *all = peer_load(&sh.exch[turn][1], 0);
         turn ^= 1;
-        *base = Cut{value_of(word), index_of(word)};
+        *base = Cut{value_of(word), entry_index(word)};
         return 1;
       }
       if (khi - klo <= 1u) {   // thousands of equal logits: the first of them by index
