@@ -181,6 +181,16 @@ struct Row {
     }
   }
   __device__ __forceinline__ void unpack(const uint4& q, float (&out)[kE]) const;
+  // the same in its own bits
+  __device__ __forceinline__ uint32_t bits_of(int i) const;
+  __device__ __forceinline__ uint4 raw(int v) const {
+    const int first = i0 - lead + v * kE;
+    if ((unsigned)(v - w0) < (unsigned)wn) return __ldg(reinterpret_cast<const uint4*>(x + first));
+    uint32_t w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = sizeof(T) == 4 ? bits_of(first + e) : bits_of(first + 2 * e) | bits_of(first + 2 * e + 1) << 16;
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
   __device__ __forceinline__ int column(int v) const { return i0 - lead + v * kE; }
   __device__ __forceinline__ void get(int v, float (&out)[kE]) const {
     global(v, out);
@@ -192,6 +202,12 @@ struct Row {
 };
 template <>
 __device__ __forceinline__ float Row<float>::widen(float v) const { return v; }
+template <>
+__device__ __forceinline__ uint32_t Row<float>::bits_of(int i) const { return i >= i0 && i < i1 ? __float_as_uint(x[i]) : 0xff800000u; }
+template <>
+__device__ __forceinline__ uint32_t Row<__nv_bfloat16>::bits_of(int i) const {
+  return i >= i0 && i < i1 ? (uint32_t)__bfloat16_as_ushort(x[i]) : 0xff80u;
+}
 template <>
 __device__ __forceinline__ void Row<float>::unpack(const uint4& q, float (&out)[4]) const {
   out[0] = __uint_as_float(q.x); out[1] = __uint_as_float(q.y); out[2] = __uint_as_float(q.z); out[3] = __uint_as_float(q.w);
@@ -336,21 +352,24 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
   turn ^= 1;
   top = key_value(key_max);
 
-  // fn(x, column of x[0]) for the pieces from, from + step, .. below `to`, several of which are loaded at once (from L2); lanes without a
-  // piece get -infinity
+  // fn(x, column of x[0]) for the pieces from, from + step, .. below `to`, the next of which is loaded on the way (from L2); lanes without a
+  // piece get -infinity.  One piece at a time: most of this code runs a few times per CTA and is itself read from L2 (256 x 150001, flat rows: 412 us,
+  // 430 with two pieces on their way, 420 with two worked on at once, 427 with four)
   auto pieces_of = [&](int from, int to, int step, auto fn) MQ_INLINE {
-    constexpr int kU = 8 / kE;   // (code counts: most of it runs once per CTA, from L2.  256 x 150001, flat rows: 407 us, 427 with twice as many)
-    for (int v0 = from; __any_sync(0xffffffffu, v0 < to); v0 += step * kU) {
-      float x[kU][kE];
+    uint4 next = make_uint4(0u, 0u, 0u, 0u);
+    if (from < to) next = r.raw(from);
+#pragma unroll 1
+    for (int v = from; __any_sync(0xffffffffu, v < to); v += step) {
+      float x[kE];
+      r.unpack(next, x);
+      if (v + step < to) next = r.raw(v + step);
+      if (r.odd)
 #pragma unroll
-      for (int k = 0; k < kU; ++k) {
-        if (v0 + k * step < to) r.get(v0 + k * step, x[k]);
-        else
+        for (int e = 0; e < kE; ++e) x[e] = r.clean(x[e]);
+      if (v >= to)
 #pragma unroll
-          for (int e = 0; e < kE; ++e) x[k][e] = -INFINITY;
-      }
-#pragma unroll
-      for (int k = 0; k < kU; ++k) fn(x[k], r.column(v0 + k * step));
+        for (int e = 0; e < kE; ++e) x[e] = -INFINITY;
+      fn(x, r.column(v));
     }
   };
 
@@ -1032,7 +1051,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
       const float e_lo = edge_of(near), e_hi = near > 0 ? edge_of(near - 1) : INFINITY;
       const bool fits = sh.cum[near] - (near > 0 ? sh.cum[near - 1] : 0u) <= (uint32_t)kCap;
       uint64_t m[2] = {0ull, 0ull};
-      uint32_t c = 0u;
+      uint32_t c = 0u, c1 = 0u;
       if (tid == 0) sh.n_list = 0u;
       __syncthreads();
       pieces_of(tid, r.pieces, kThreads, [&](float (&x)[kE], int column) {
@@ -1043,23 +1062,22 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
           if (x[e] >= e_hi) {
             m[0] += w;
             ++c;
-          } else if (x[e] >= e_lo) {
+          } else if (x[e] >= e_lo && from.keeps(x[e], column + e)) {
+            m[1] += w;
             hits |= 1u << e;
           }
         }
-        while (hits) {   // (one after the other, as above)
+        if (hits == 0u) return;
+        c1 += (uint32_t)__popc(hits);
+        uint32_t at = atomicAdd(&sh.n_list, (uint32_t)__popc(hits));
+        for (; hits; hits &= hits - 1u, ++at) {   // (one after the other, as above)
           const int i = column + __ffs((int)hits) - 1;
-          hits &= hits - 1u;
-          const float v = Row<T>::clean(r.widen(r.x[i]));
-          if (!from.keeps(v, i)) continue;
-          m[1] += weight(v);
-          const uint32_t at = atomicAdd(&sh.n_list, 1u);
-          if (at < (uint32_t)kCap) part[at] = entry_of<T>(v, i);
+          if (at < (uint32_t)kCap) part[at] = entry_of<T>(Row<T>::clean(r.widen(r.x[i])), i);
         }
       });
       __syncthreads();
       // (what `from` cuts off lies below e_hi, or the goal would not be reached there)
-      uint64_t v[4] = {m[0] - c * kBias, m[1], c, tid == 0 ? (uint64_t)sh.n_list : 0ull};
+      uint64_t v[4] = {m[0] - c * kBias, m[1] - c1 * kBias, c, tid == 0 ? (uint64_t)sh.n_list : 0ull};
       sum_all(std::integral_constant<int, 4>(), v);
       mass_above = v[0];
       const bool exact = mass && from.value < e_hi;      // (else `from` cuts among what was summed)
