@@ -261,6 +261,8 @@ struct Smem {
   int edge[2];
   int found;
   uint64_t front, entry;
+  uint64_t range_mass[kWarps];          // what a pass has summed of each warp's range of columns, and how many elements that were
+  uint32_t range_n[kWarps];
 };
 
 
@@ -735,7 +737,10 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
 
   // ---- kept elements, a warp's contiguous range at a time: weights (or ones) summed, and the first column at which the running sum exceeds
   // `at(total)`: known to the CTA that holds it, -1 elsewhere
-  auto column_of = [&](auto as_weights, auto all_kept, const Cut& base, bool equal_only, auto at, uint64_t* total, uint64_t* count) MQ_INLINE -> int {
+  // (`listed` >= 0: range_mass and range_n have those above all entries of this CTA's list, which has `listed` of them)
+  auto first_piece = [&](int w) { return (int)((int64_t)r.pieces * w / kWarps); };
+  auto column_of = [&](auto as_weights, auto all_kept, const Cut& base, bool equal_only, const uint64_t* entries, int listed, auto at, uint64_t* total,
+                       uint64_t* count) MQ_INLINE -> int {
     constexpr bool kW = decltype(as_weights)::value, kAll = decltype(all_kept)::value;
     auto term = [&](float x, int i, uint32_t* n) -> uint64_t {
       const uint64_t w = kW ? weight(x) : 1ull;
@@ -743,21 +748,32 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
       *n += it ? 1u : 0u;
       return it ? w : 0ull;
     };
-    const int a = (int)((int64_t)r.pieces * warp / kWarps), b = (int)((int64_t)r.pieces * (warp + 1) / kWarps);
+    const int a = first_piece(warp), b = first_piece(warp + 1);
     uint64_t sum = 0;
     uint32_t n = 0, terms = 0;
-    pieces_of(a + lane, b, 32, [&](float (&x)[kE], int column) {
-#pragma unroll
-      for (int e = 0; e < kE; ++e) {
-        if (kW && kAll) {   // (-infinity weighs nothing: all can be summed)
-          sum += weight.biased(x[e]);
-          n += x[e] > -INFINITY ? 1u : 0u;
-        } else {
-          sum += term(x[e], column + e, &n);
-        }
+    if (kW && !kAll && listed >= 0) {
+      for (int k = lane; k < listed; k += 32) {
+        const int i = entry_index(entries[k]), piece = (i - r.i0 + r.lead) / kE;
+        if (piece >= a && piece < b) sum += term(entry_value<T>(entries[k]), i, &n);
       }
-      if (kW && kAll) terms += kE;
-    });
+      if (lane == 0) {
+        sum += sh.range_mass[warp];
+        n += sh.range_n[warp];
+      }
+    } else {
+      pieces_of(a + lane, b, 32, [&](float (&x)[kE], int column) {
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+          if (kW && kAll) {   // (-infinity weighs nothing: all can be summed)
+            sum += weight.biased(x[e]);
+            n += x[e] > -INFINITY ? 1u : 0u;
+          } else {
+            sum += term(x[e], column + e, &n);
+          }
+        }
+        if (kW && kAll) terms += kE;
+      });
+    }
     sum = warp_sum(sum - terms * kBias);
     n = __reduce_add_sync(0xffffffffu, n);
     if (tid == 0) sh.n_list = 0;
@@ -980,6 +996,9 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
   // infinite), known_mass is known to lie, less than the goal.  *all is the mass of all, or becomes, for a
   // count and a later top-p, the mass of what is kept (0: not found on the way).  1: *base is the
   // cut.  0: all together are less.  -1: all is done, on a list.
+  float few_edge = INFINITY;      // finite: the mass from it on is few_mass
+  uint64_t few_mass = 0ull;
+  int own_list = -1, in_ranges = -1;   // entries of this CTA's list; the same, once they and the ranges' sums say what is kept
   auto find_cut = [&](Cut* base, bool mass, uint64_t goal, uint64_t* all, float known_edge, uint64_t known_mass) MQ_INLINE -> int {
     const Cut from = *base;
     // less than the goal (above, above_n elements) lies from khi on, and no less from klo on (lo_n elements)
@@ -1050,11 +1069,15 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
     for (int tries = 0; pass >= 0; ++tries) {
       const float e_lo = edge_of(near), e_hi = near > 0 ? edge_of(near - 1) : INFINITY;
       const bool fits = sh.cum[near] - (near > 0 ? sh.cum[near - 1] : 0u) <= (uint32_t)kCap;
-      uint64_t m[2] = {0ull, 0ull};
+      // (on the way, for the top-p behind: the mass of as few as its candidates are)
+      const int t_few = mass ? n_bars : bar_with(kShort);
+      const bool sum_few = !mass && t_few < near;
+      const float e_few = sum_few ? edge_of(t_few) : INFINITY;
+      uint64_t m[2] = {0ull, 0ull}, few = 0ull;
       uint32_t c = 0u, c1 = 0u;
       if (tid == 0) sh.n_list = 0u;
       __syncthreads();
-      pieces_of(tid, r.pieces, kThreads, [&](float (&x)[kE], int column) {
+      pieces_of(first_piece(warp) + lane, first_piece(warp + 1), 32, [&](float (&x)[kE], int column) {   // (a warp's range, as in column_of)
         uint32_t hits = 0u;
 #pragma unroll
         for (int e = 0; e < kE; ++e) {
@@ -1062,6 +1085,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
           if (x[e] >= e_hi) {
             m[0] += w;
             ++c;
+            few += x[e] >= e_few ? w : 0ull;
           } else if (x[e] >= e_lo && from.keeps(x[e], column + e)) {
             m[1] += w;
             hits |= 1u << e;
@@ -1077,8 +1101,20 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
       });
       __syncthreads();
       // (what `from` cuts off lies below e_hi, or the goal would not be reached there)
-      uint64_t v[4] = {m[0] - c * kBias, m[1] - c1 * kBias, c, tid == 0 ? (uint64_t)sh.n_list : 0ull};
-      sum_all(std::integral_constant<int, 4>(), v);
+      uint64_t v[5] = {m[0] - c * kBias, m[1] - c1 * kBias, c, tid == 0 ? (uint64_t)sh.n_list : 0ull, few};
+      if (mass) {
+        const uint64_t of_warp = warp_sum(v[0]);
+        const uint32_t n_warp = __reduce_add_sync(0xffffffffu, c);
+        if (lane == 0) {
+          sh.range_mass[warp] = of_warp;
+          sh.range_n[warp] = n_warp;
+        }
+      }
+      sum_all(std::integral_constant<int, 5>(), v);
+      if (sum_few) {
+        few_edge = e_few;
+        few_mass = v[4] - sh.cum[t_few] * kBias;
+      }
       mass_above = v[0];
       const bool exact = mass && from.value < e_hi;      // (else `from` cuts among what was summed)
       const bool low = exact && v[0] + v[1] < goal, over = exact && v[0] >= goal, right = !mass || (exact && !low && !over);
@@ -1105,6 +1141,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
       }
       known = right;
       if (right && fits) {
+        own_list = (int)sh.n_list;
         listed = (int)fetch(lane < (int)n_cta ? (uint32_t)peer_load(&sh.exch[turn ^ 1][3], lane) : 0u);
         cluster_sync();
       }
@@ -1147,6 +1184,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
       }
       if (lo_n - above_n <= (uint64_t)kCap) {
         if (listed < 0) listed = gather(key_value(klo), key_value(khi), from);
+        else if (mass) in_ranges = own_list;
         // the last one before which less than the goal lies: where the running sum reaches it
         if (rank == 0) {
           for (int j = tid; j < listed; j += kThreads) part[j] = mass ? weight(value_of(list[j])) : 1ull;
@@ -1176,7 +1214,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
         uint64_t total, count;
         // (those that `from` keeps: its own cut may lie among them)
         const Cut equal{base->value, from.value == base->value ? from.idx : INT_MAX};
-        const int i = column_of(No(), No(), equal, true, [&](uint64_t t) { return min(ties, t) - 1ull; }, &total, &count);
+        const int i = column_of(No(), No(), equal, true, part, -1, [&](uint64_t t) { return min(ties, t) - 1ull; }, &total, &count);
         if (tid == 0) sh.exch[turn][0] = (uint64_t)(i + 1);
         cluster_sync();
         const uint32_t one = lane < (int)n_cta ? (uint32_t)peer_load(&sh.exch[turn][0], lane) : 0u;
@@ -1209,18 +1247,26 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
   uint64_t all = 0ull;
   if (by_k && find_cut(&base, false, (uint64_t)want_k, &all, INFINITY, 0ull) < 0) return;
   if (by_p) {
-    const float edge = edge_of(bar_with(kShort));
-    uint64_t own = 0ull, have;
-    if (all == 0ull) own = base.value >= -FLT_MAX || !low_is_0 ? mass_of(Yes(), base) : mass_of(No(), base);
-    if (candidates(base, edge, own, &all, &have)) return;
-    if (fine_state == 0) fine_state = 1;
+    float edge = few_edge;
+    uint64_t have = few_mass;
+    if (!(edge < INFINITY && have < mass_goal(all))) {   // (else the few are known to be too few)
+      edge = edge_of(bar_with(kShort));
+      uint64_t own = 0ull;
+      if (all == 0ull) own = base.value >= -FLT_MAX || !low_is_0 ? mass_of(Yes(), base) : mass_of(No(), base);
+      if (candidates(base, edge, own, &all, &have)) return;
+      if (fine_state == 0) fine_state = 1;
+    }
     const bool short_of = have < mass_goal(all);   // (else they were too many)
     if (find_cut(&base, true, mass_goal(all), &all, short_of ? edge : INFINITY, short_of ? have : 0ull) < 0) return;
   }
-  if (by_min && least > base.value) base = Cut{least, INT_MIN};
+  if (by_min && least > base.value) {
+    base = Cut{least, INT_MIN};
+    in_ranges = -1;
+  }
   uint64_t total, count;
   auto goal_of = [&](uint64_t t) { return share_of(u, t, false); };
-  const int i = base.value >= -FLT_MAX || !low_is_0 ? column_of(Yes(), No(), base, false, goal_of, &total, &count) : column_of(Yes(), Yes(), base, false, goal_of, &total, &count);
+  const int i = base.value >= -FLT_MAX || !low_is_0 ? column_of(Yes(), No(), base, false, rank == 0 ? list : part, in_ranges, goal_of, &total, &count)
+                                                               : column_of(Yes(), Yes(), base, false, part, -1, goal_of, &total, &count);
   if (i >= 0 && tid == 0) write(i, weight(Row<T>::clean(r.widen(r.x[i]))), total, (int)count);
 }
 
