@@ -254,7 +254,7 @@ struct Smem {
   uint64_t warp_sum[kWarps];
   alignas(16) uint32_t bars[kBars];
   uint32_t scan[kWarps];
-  uint32_t cum[kBars];                  // of the bars from the maximum's downwards
+  alignas(16) uint32_t cum[kBars];      // of the bars from the maximum's downwards
   float mass[kWarps];
   double table[kTable];
   uint32_t n_list;
@@ -277,6 +277,10 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
   const uint32_t rank = cluster_rank(), n_cta = cluster_size();
   const int row = blockIdx.x / n_cta;
   for (int k = tid; k < kBars; k += kThreads) sh.bars[k] = 0u;
+  // (2^(a / 32) and 2^(b / 1024), of whose products the table consists: 256 x 32000 rows 64.5 us, 65.3 with an exponential for every entry)
+  double* roots = reinterpret_cast<double*>(sh.cum);
+  static_assert(kTable == 32 * 32 && sizeof(sh.cum) >= 64 * sizeof(double), "two times 32 roots");
+  if (tid < 64) roots[tid] = exp2((double)(tid & 31) * (tid < 32 ? 1.0 / 32.0 : 1.0 / 1024.0));
   pdl_launch_dependents();
   pdl_wait();
 
@@ -340,7 +344,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
   if (lane == 0) sh.exch[turn][warp] = order_key(top) | (odd ? 1ull << 32 : 0ull);
   cluster_arrive();
   if (temp > 0.0f)   // (while the others arrive)
-    for (int j = tid; j < kTable; j += kThreads) sh.table[j] = exp2((double)j * (1.0 / kTable));
+    for (int j = tid; j < kTable; j += kThreads) sh.table[j] = roots[j / 32] * roots[32 + j % 32];
   cluster_wait();
   // every warp fetches what all warps of all CTAs found
   uint32_t key_max = 0u;
