@@ -227,3 +227,66 @@ def test_the_drawn_tokens_have_their_probabilities():
     prob = torch.softmax(x.double(), 0).cpu().numpy()
     share = np.bincount(tok, minlength=v) / n
     assert np.all(np.abs(share - prob) <= 1.0 / n + 2.0 ** -23)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("t", [0.03, 0.2, 1.0, 4.0])
+def test_logits_that_crowd_in_a_corner_of_their_interval(bf16, t):
+    """The mass of 1/32 wide intervals is first guessed from how many logits they have: here they lie at an end of theirs, or in a few of them."""
+    rng = np.random.default_rng(int(100 * t))
+    n, v = 6, 60013
+    x = rng.standard_normal((n, v)) * np.array([0.3, 1.0, 2.0, 3.0, 0.1, 1.5])[:, None]
+    low = np.floor(x * 32) / 32
+    x = np.where(np.arange(n)[:, None] % 3 == 0, low + 1 / 33, np.where(np.arange(n)[:, None] % 3 == 1, low + 1e-4 * rng.random((n, v)), x))
+    x[2] = np.round(x[2])
+    x[5] -= 40.0
+    x = torch.from_numpy(x.astype(np.float32))
+    x = (x.to(torch.bfloat16) if bf16 else x).to(DEV)
+    u, p = rng.random(n).astype(np.float32), rng.uniform(0.3, 0.97, n).astype(np.float32)
+    k = rng.integers(3000, v, n)
+    for kw in (dict(p=p), dict(p=p, k=k), dict(p=p, mp=0.3), dict(p=p, k=k, mp=0.02), dict(k=k)):
+        _check(x, t, u, **kw)
+    _check(x, t, np.float32(0.99999994), p=0.99, k=v - 1)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_many_short_rows(bf16):
+    rng = np.random.default_rng(11)
+    n, v = 6000, 37
+    x = _logits(rng, n, v, bf16, peaks=4)
+    u, t = rng.random(n).astype(np.float32), rng.uniform(0.3, 2.0, n).astype(np.float32)
+    _check(x, t, u, k=rng.integers(0, 50, n), p=rng.uniform(0.2, 1.2, n).astype(np.float32), mp=rng.uniform(-0.1, 0.2, n).astype(np.float32))
+
+
+def test_rows_further_apart_than_32_bits():
+    rng = np.random.default_rng(12)
+    v, pitch = 20011, (1 << 31) + 8
+    buf = torch.empty(2 * pitch + v, dtype=torch.bfloat16, device=DEV)
+    x = buf.as_strided((3, v), (pitch, 1))
+    x.copy_(_logits(rng, 3, v, True))
+    _check(x, 0.8, rng.random(3).astype(np.float32), k=4000, p=0.9)
+    del x, buf
+    torch.cuda.empty_cache()
+
+
+def test_two_calls_at_once():
+    rng = np.random.default_rng(13)
+    n, v = 40, 50021
+    x, y = _logits(rng, n, v, False), (torch.from_numpy(rng.standard_normal((n, v)).astype(np.float32)) * 0.5).to(DEV)
+    t, u, p = (torch.full((n,), f, device=DEV) for f in (0.9, 0.37, 0.95))
+    alone = []
+    for z in (x, y):
+        token = torch.empty(n, dtype=torch.int32, device=DEV)
+        B.mq_sample(z, t, u, token, top_p=p)
+        alone.append(token)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[torch.empty(n, dtype=torch.int32, device=DEV) for _ in range(8)] for _ in range(2)]
+    torch.cuda.synchronize()
+    for i in range(8):
+        for k, z in enumerate((x, y)):
+            with torch.cuda.stream(streams[k]):
+                B.mq_sample(z, t, u, got[k][i], top_p=p)
+    torch.cuda.synchronize()
+    for k in range(2):
+        assert all(torch.equal(g, alone[k]) for g in got[k])
