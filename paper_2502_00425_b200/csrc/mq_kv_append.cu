@@ -28,13 +28,12 @@ struct AppendParams {
   int n_steps;               // steps of 32 lanes per token
   int chunks, per_chunk;     // parts that a token's steps are cut into, and the steps of a part
   const float *gain_q, *gain_k;
-  float eps;
+  float eps, amp;            // amp: of the rotated pairs
   const int32_t* pos;
   const int64_t* slots;
   int has_cache;
-  KvView c;
   int rot_pairs;             // pairs of a head that rotate, a multiple of 4; the channels behind them pass
-  float amp;                 // of the rotated pairs
+  KvView c;
   double turns[64];          // theta_i / (2 pi)
 };
 
