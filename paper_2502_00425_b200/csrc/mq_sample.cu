@@ -16,6 +16,9 @@
 //   * Where what is kept does not fit into a list, passes that sum mass and count above several values at once narrow the place of the cut
 //     down until its neighbourhood fits; equal logits by the thousand are cut by index.  The kept weights are then summed by warps over
 //     contiguous ranges, and only the range that the random number falls into is walked.
+// Bound by latency for few rows: a greedy row of 131072 takes 5.4 us, one with a few candidates 11 - 15 (some 15 steps with a cluster barrier of 1.5 us
+// each), one that keeps thousands 27 - 45, a pass from L2 4 - 10 us each.  256 x 150001 float32: greedy 46 us, 3.4 TB/s, as the first pass of
+// a row and the steps behind it do not overlap within its cluster; top-k 65, unfiltered 97, top-p 206.
 #include <cfloat>
 #include <climits>
 #include <cmath>
