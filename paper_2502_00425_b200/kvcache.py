@@ -328,7 +328,7 @@ class DeviceKVCache:
         return self.kv_len.tolist()
 
     def _shares(self, step: CacheStep) -> bool:
-        if self.n_seq > 1024:             # (the shared form's limit; every sequence's pages are in its own row as well)
+        if self.n_seq > 1024 or not any(self._lent):   # (the shared form's limit; every sequence's pages are in its own row as well)
             return False
         rows, keys = {}, {}
         for b, l in enumerate(self.leaders):
@@ -341,7 +341,10 @@ class DeviceKVCache:
 
     def workspace(self, step: CacheStep, n_q_heads: int) -> torch.Tensor:
         """As PagedKVCache.workspace()."""
-        size_of = B.mq_kv_attention_shared_workspace_bytes if self._shares(step) else B.mq_kv_attention_workspace_bytes
+        return self._attention_workspace(step, n_q_heads, self._shares(step))
+
+    def _attention_workspace(self, step: CacheStep, n_q_heads: int, shares: bool) -> torch.Tensor:
+        size_of = B.mq_kv_attention_shared_workspace_bytes if shares else B.mq_kv_attention_workspace_bytes
         return _workspace(self, size_of(self.n_seq, step.total, step.max_q, self.table.shape[1], n_q_heads, self.handle))
 
     def attention(self, q: torch.Tensor, step: CacheStep, n_q_heads: int, perm: Optional[torch.Tensor] = None,
@@ -350,8 +353,9 @@ class DeviceKVCache:
         all of it where that is faster: the result and the log-sum-exps."""
         o = torch.empty_like(q)
         lse = torch.empty((step.total, n_q_heads), device=q.device)
-        ws = self.workspace(step, n_q_heads)
-        if self._shares(step):
+        shares = self._shares(step)
+        ws = self._attention_workspace(step, n_q_heads, shares)
+        if shares:
             B.mq_kv_attention_shared(q, step.cu_q, step.kv_len, self.table, self.leader, self.shared_len, self.handle, n_q_heads, step.max_q, o,
                                      ws, lse=lse, perm=perm, scale=scale)
         else:

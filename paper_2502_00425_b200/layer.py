@@ -396,7 +396,8 @@ class W4A8DecoderBlock:
 
 class W4A8Head:
     """What follows the last block of a decoder: RMSNorm, the W4A8 linear to the vocabulary with float32 logits, and the next tokens from
-    them (mq_sample).  The linear's N is a multiple of 16; the vocabulary may be smaller.  Rows are text."""
+    them (mq_sample).  The linear's N is a multiple of 16; the vocabulary may be smaller.  Rows are text.  Calls, and replays of graphs that
+    captured them, follow one another in stream order: those of as many rows share a workspace."""
 
     def __init__(self, weights: LinearWeights, gain: torch.Tensor, vocab: Optional[int] = None):
         self.w, self.gain, self.vocab = weights, gain, weights.N if vocab is None else vocab
