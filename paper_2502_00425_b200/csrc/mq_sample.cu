@@ -261,7 +261,6 @@ struct Smem {
   float mass[kWarps];
   double table[kTable];
   uint32_t n_list;
-  int edge[2];
   int found;
   uint64_t front, entry;
   uint64_t range_mass[kWarps];          // what a pass has summed of each warp's range of columns, and how many elements that were
@@ -1069,9 +1068,12 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
       if (near + 1 < n_bars && sh.cum[near + 1] <= (uint32_t)kCap) {   // (a bar more, as the guess may be one too few)
         uint64_t have;
         if (candidates(from, edge_of(near + 1), 0ull, all, &have)) return -1;
-      } else if (near < n_bars) {
-        pass = near;
+        khi = order_key(edge_of(near + 1));   // (they were too few)
+        above = have;
+        above_n = sh.cum[near + 1];
+        near += 2;
       }
+      if (near < n_bars) pass = near;
     }
     for (int tries = 0; pass >= 0; ++tries) {
       const float e_lo = edge_of(near), e_hi = near > 0 ? edge_of(near - 1) : INFINITY;
