@@ -361,7 +361,7 @@ def _plain_shared(s):
         top = torch.where(top > -math.inf, top, 0.0)
         e0, e1 = torch.exp(s0 - top), torch.exp(s1 - top)
         z = e0.sum(-1, keepdim=True) + e1.sum(-1, keepdim=True)
-        o = torch.matmul(e0.flatten(1, 3), v0).view(*e0.shape[:4], d) + torch.matmul(e1.flatten(2, 3), v1).view(*e1.shape[:4], d)
+        o = torch.matmul(e0.view(hkv, -1, e0.shape[-1]), v0).view(*e0.shape[:4], d) + torch.matmul(e1.flatten(2, 3), v1).view(*e1.shape[:4], d)
         o, lse = o / z.clamp(min=1e-30), torch.log(z[..., 0]) + top[..., 0]
         out.append(o.permute(1, 3, 0, 2, 4)[b, j].reshape(-1, hq * d))
         lses.append(lse.permute(1, 3, 0, 2)[b, j].reshape(-1, hq))
