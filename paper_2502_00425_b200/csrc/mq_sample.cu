@@ -27,6 +27,7 @@
 #include <cuda_bf16.h>
 
 #include "mq_common.cuh"
+#include "mq_sample_order.h"
 
 namespace mq {
 namespace {
@@ -47,6 +48,7 @@ constexpr int kPairs = 256;           // a list of up to so many is compared pai
 constexpr int kShort = 160;           // candidates that a nucleus is looked for in first
 constexpr int kLong = 1280;           // the largest k that the groups' bars serve
 constexpr int kEdges = 2;             // values that a narrowing pass sums above
+constexpr int kLevels = 32;           // more than a narrowing takes: a bound, so that no rows whatever can keep a kernel in it
 constexpr int kItems = 2 * kEdges > kWarps + 1 ? 2 * kEdges : kWarps + 1;   // what a CTA tells the others at once
 constexpr int kPoint = 43;            // bits behind the point of a weight: 2^20 of them stay below 2^63
 constexpr int kMaxVocab = 1 << 20;
@@ -66,11 +68,8 @@ struct SampleArgs {
 };
 
 // Floats (no NaN; -0 as 0) in their order as whole numbers, and back
-__device__ __forceinline__ uint32_t order_key(float x) {
-  const uint32_t b = __float_as_uint(x + 0.0f);
-  return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
-}
-__device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
+__device__ __forceinline__ uint32_t order_key(float x) { return order_of_bits(__float_as_uint(x)); }
+__device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(bits_of_order(k)); }
 // floor(x * 2^23 / 2^e) for a small |x|: the sum with 1.5 * 2^e, rounded down, has it in its low bits
 __device__ __forceinline__ int floor_bits(float x, float magic) { return (int)(__float_as_uint(__fadd_rd(x, magic)) - __float_as_uint(magic)); }
 // floor(8 x) + 512, at most the last bar (x >= -64); floor(32 x)
@@ -89,13 +88,13 @@ __device__ __forceinline__ int entry_index(uint64_t e) { return (int)(~(uint32_t
 template <typename T>
 __device__ __forceinline__ float entry_value(uint64_t e) {
   const uint32_t k = (uint32_t)(e >> kIndexBits);
-  return key_value(sizeof(T) == 4 ? k : k << 16 | (k & 0x8000u ? 0u : 0xffffu));
+  return key_value(sizeof(T) == 4 ? k : k << 16);
 }
 // the first entry whose value is not below x
 template <typename T>
 __device__ __forceinline__ uint64_t first_entry(float x) {
   const uint32_t k = order_key(x);
-  return (uint64_t)(sizeof(T) == 4 ? k : k & 0x80000000u ? (k + 0xffffu) >> 16 : k >> 16) << kIndexBits;
+  return (uint64_t)(sizeof(T) == 4 ? k : (k + 0xffffu) >> 16) << kIndexBits;
 }
 
 // The larger one; NaN if one of them is
@@ -1156,7 +1155,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
       }
       break;
     }
-    for (int level = 0;; ++level) {
+    for (int level = 0;; ++level) {   // (from level 8 on the interval shrinks to a third of its places each time: 21 more at most)
       if (!known) {
         // Values between, downwards: some times T below the maximum and all, where nothing is known; else evenly, and in the end evenly among
         // the numbers that there are.  (Of few numbers between, some come twice.)
@@ -1166,7 +1165,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
 #pragma unroll
         for (int k = 0; k < kEdges; ++k) {
           const float v = lo_n == ~0ull && level == 0 ? (k == 0 ? top - 8.0f * temp : -FLT_MAX) : lo + (h - lo) * ((float)(kEdges - k) / (float)(kEdges + 1));
-          at[k] = level == 0 || even ? fminf(fmaxf(v, lo), h) : key_value(klo + (uint32_t)((uint64_t)(khi - klo) * (kEdges - k) / (kEdges + 1)));
+          at[k] = level == 0 || even ? fminf(fmaxf(v, lo), h) : key_value(order_between(klo, khi, k, kEdges));
         }
         uint64_t m[kEdges], c[kEdges];
         if (!mass) sums_from(No(), No(), at, from, m, c);
@@ -1217,7 +1216,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
         *base = Cut{value_of(word), entry_index(word)};
         return 1;
       }
-      if (khi - klo <= 1u) {   // thousands of equal logits: the first of them by index
+      if (khi - klo <= 1u || level >= kLevels) {   // thousands of equal logits: the first of them by index
         base->value = key_value(klo);
         const uint64_t g = mass ? weight(base->value) : 1ull, ties = g ? (goal - above + g - 1ull) / g : 1ull;
         uint64_t total, count;

@@ -290,3 +290,20 @@ def test_two_calls_at_once():
     torch.cuda.synchronize()
     for k in range(2):
         assert all(torch.equal(g, alone[k]) for g in got[k])
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_equal_logits_beside_zero(bf16):
+    """Thousands of the smallest numbers below and above zero, and of zeros of both signs, under a larger one."""
+    v, tiny = 5001, 2.0 ** -133 if bf16 else 2.0 ** -149
+    x = torch.full((5, v), 0.0, dtype=torch.bfloat16 if bf16 else torch.float32)
+    x[0], x[1], x[2] = -tiny, tiny, -0.0
+    x[3, ::2], x[3, 1::2] = -tiny, 0.0
+    x[4, ::3], x[4, 1::3], x[4, 2::3] = -tiny, -0.0, tiny
+    assert float(x[0, 0]) == -tiny
+    x[:, 3000] = 1.0
+    x, u = x.to(DEV), np.array([0.1, 0.9, 0.5, 0.99999994, 0.3], np.float32)
+    for kw in (dict(k=50), dict(k=4000), dict(p=0.5), dict(k=4500, p=0.7), dict(mp=0.3), dict(mp=0.5), dict(k=4000, p=0.5, mp=0.3)):
+        _check(x, 1.0, u, **kw)
+    tok, _, kept = _check(x[:, :2900], 1.0, u, k=2500)
+    assert kept == [2500] * 5
