@@ -919,9 +919,11 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
     per_unit = 8.0f;
     add_bars(std::integral_constant<int, 1>(), sh.bars, bar);
   };
-  // all elements, 32 units down (for top-p alone as far as there is some weight): counted along with another pass, or by one of their own
+  // all elements, 32 units down (for top-p alone as far as there is some weight): counted along with another pass, or by one of their own.
+  // Whole bars, fine_high down to fine_low: a bar counted in part would make a list of its elements longer than is known.
   const int fine_high = fine_of(fmaxf(top, -64.0f));
-  const float fine_from = fmaxf(fmaxf((float)(fine_high - kBars + 1) * (1.0f / 32.0f), -64.0f), by_k ? -64.0f : top - 20.0f * temp);
+  const int fine_low = max(fine_high - kBars + 1, fine_of(by_k ? -64.0f : fmaxf(top - 20.0f * temp, -64.0f)));
+  const float fine_from = (float)fine_low * (1.0f / 32.0f);
   int fine_state = 0;   // 1: counted, by all CTAs; 2: added up
   auto count_fine = [&](float x) {
     if (x >= fine_from) atomicAdd(&fine[fine_of(x) - fine_high + kBars - 1], 1u);
@@ -942,7 +944,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
     }
     if (fine_state < 2) {
       high = fine_high;
-      n_bars = max(0, min(kBars, fine_high + 64 * 32 + 1));   // (none below -64)
+      n_bars = fine_high - fine_low + 1;
       per_unit = 32.0f;
       add_bars(std::integral_constant<int, kBars / kThreads>(), fine, kBars - 1);
     }
@@ -1076,7 +1078,6 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
     }
     for (int tries = 0; pass >= 0; ++tries) {
       const float e_lo = edge_of(near), e_hi = near > 0 ? edge_of(near - 1) : INFINITY;
-      const bool fits = sh.cum[near] - (near > 0 ? sh.cum[near - 1] : 0u) <= (uint32_t)kCap;
       // (on the way, for the top-p behind: the mass of as few as its candidates are)
       const int t_few = mass ? n_bars : bar_with(kShort);
       const bool sum_few = !mass && t_few < near;
@@ -1148,7 +1149,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
         if (near < n_bars) continue;
       }
       known = right;
-      if (right && fits) {
+      if (right && v[3] <= (uint64_t)kCap) {
         own_list = (int)sh.n_list;
         listed = (int)fetch(lane < (int)n_cta ? (uint32_t)peer_load(&sh.exch[turn ^ 1][3], lane) : 0u);
         cluster_sync();

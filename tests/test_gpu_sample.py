@@ -307,3 +307,47 @@ def test_equal_logits_beside_zero(bf16):
         _check(x, 1.0, u, **kw)
     tok, _, kept = _check(x[:, :2900], 1.0, u, k=2500)
     assert kept == [2500] * 5
+
+
+def _check_within_rounding(x, t, u, p):
+    """top-p where single tokens weigh as little as the roundings of all weights together: with e = V 2^-44 (of the largest weight) + 2^-37 of the
+    sum, running sums are off by e and borders by as much again, so the cut and the token lie where the exact sums are within 2 e of
+    their borders.  The token's weight is off by 2^-44 + 2^-37 of itself, the total by e, the logarithm is rounded by 2^-24."""
+    got = _run(x, t, u, p=p)
+    host = x.double().cpu().numpy()
+    for r, (token, logp, kept) in enumerate(zip(*got)):
+        temp, want_p, draw = (float(np.float32(a[r])) for a in (t, p, u))
+        w = np.exp((host[r] - host[r].max()) / temp)
+        order = np.argsort(-host[r], kind="stable")
+        run = np.concatenate([[0.0], np.cumsum(w[order])])
+        e = w.size * 2.0 ** -44 + 2.0 ** -37 * run[-1]
+        assert 1 <= kept <= w.size and run[kept - 1] < want_p * run[-1] + 2 * e and run[kept] >= want_p * run[-1] - 2 * e, (r, kept)
+        cols = np.sort(order[:kept])
+        run = np.concatenate([[0.0], np.cumsum(w[cols])])
+        j = int(np.searchsorted(cols, token))
+        assert j < cols.size and cols[j] == token, (r, token)
+        assert run[j] <= draw * run[-1] + 2 * e and run[j + 1] >= draw * run[-1] - 2 * e, (r, token, run[j], draw * run[-1])
+        lp = np.log(w[token] / run[-1])
+        assert abs(logp - lp) <= 2.0 ** -24 * abs(lp) + 2 * (2.0 ** -44 / w[token] + 2.0 ** -37 + e / run[-1]), (r, logp, lp)
+    return got
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("v,t,mid,dev", [(150001, 1.01, -20.2, 0.5), (150001, 1.0, -20.0, 0.5), (150001, 1.01, -20.3, 0.05), (150001, 1.01, -20.215, 0.001),
+                                         (60013, 0.5, -10.0, 0.3), (60013, 0.503, -10.05, 0.02), (40009, 3.3, -66.0, 1.0), (1 << 20, 1.003, -20.05, 0.4)])
+def test_top_p_that_ends_far_below_the_largest(bf16, v, t, mid, dev):
+    """One token has nearly all of the mass, thousands lie near 20 T below it, and the nucleus ends among them: the bars of 1/32 that are counted end
+    there as well, at an edge of one (T = 1, 0.5) or in its middle."""
+    rng = np.random.default_rng(v + int(1000 * t))
+    rows = 3 if v > 1000000 else 8
+    x = (mid + dev * rng.standard_normal((rows, v))).astype(np.float32)
+    x[:, 7] = 0.0
+    x[1] += 70.0                        # (beyond the bars' upper end)
+    x[2] += np.float32(5.0 / 64)        # (the limit elsewhere in its bar)
+    x = torch.from_numpy(x).to(torch.bfloat16 if bf16 else torch.float32)
+    tail = 1.0 - 1.0 / np.exp((x[0].double().numpy() - float(x[0].max())) / t).sum()      # what is not the largest one's
+    share = np.array([0.5, 0.3, 0.6, 0.01, 0.9, 0.99, 0.97, 0.2])[:rows]                  # of it, within the nucleus
+    p = (1.0 - tail * (1.0 - share)).astype(np.float32)
+    u = np.array([0.99999994, 1 - tail / 3, 0.5, 1 - tail / 2, tail / 1000, 1 - tail / 4, 1 - tail / 5, 0.0])[:rows].astype(np.float32)
+    _check_within_rounding(x.to(DEV), np.full(rows, t, np.float32), u, p)
+    _check_within_rounding(x.to(DEV), np.full(rows, t, np.float32), u, np.full(rows, 0.99999994, np.float32))
