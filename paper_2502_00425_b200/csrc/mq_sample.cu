@@ -954,9 +954,10 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
   auto bar_with = [&](uint64_t want) -> int { return count_if(n_bars, [&](int k) { return (uint64_t)sh.cum[k] < want; }); };
 
   // ---- top-p: the candidates, those from `edge` on that `base` keeps, with their mass; *all, the mass of S1, is added up from `own` on the way, *have
-  // is theirs.
-  // True: they hold all that is kept, and all is done.
-  auto candidates = [&](const Cut& base, float edge, uint64_t own, uint64_t* all, uint64_t* have) MQ_INLINE -> bool {
+  // is theirs, *have_n how many they are.
+  // kDone: they hold all that is kept, and all is done.  kTooFew: the nucleus goes on behind them.  kTooMany: it does not, but they fill more than a list.
+  enum Found { kDone, kTooFew, kTooMany };
+  auto candidates = [&](const Cut& base, float edge, uint64_t own, uint64_t* all, uint64_t* have, uint64_t* have_n) MQ_INLINE -> Found {
     uint64_t mass = 0ull;
     if (tid == 0) sh.n_list = 0u;
     __syncthreads();
@@ -967,15 +968,17 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
       mass += weight(x);
     });
     __syncthreads();
-    uint64_t v[3] = {own, mass, tid == 0 ? (uint64_t)min(sh.n_list, (uint32_t)kCap + 1u) : 0ull};
+    uint64_t v[3] = {own, mass, tid == 0 ? (uint64_t)sh.n_list : 0ull};
     sum_all(std::integral_constant<int, 3>(), v);
     *all += v[0];
     *have = v[1];
-    if (v[1] < mass_goal(*all) || v[2] > (uint64_t)kCap) return false;
+    *have_n = v[2];
+    if (v[1] < mass_goal(*all)) return kTooFew;
+    if (v[2] > (uint64_t)kCap) return kTooMany;
     const uint32_t n = fetch(lane < (int)n_cta ? (uint32_t)peer_load(&sh.exch[turn ^ 1][2], lane) : 0u);
     cluster_sync();
     finish_list((int)n, 0, *all);
-    return true;
+    return kDone;
   };
   // this thread's part of the mass of all that `base` keeps; the elements are counted along
   auto mass_of = [&](auto with_base, const Cut& base) MQ_INLINE -> uint64_t {
@@ -1067,12 +1070,15 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
       __syncthreads();
       near = count_if(kBars, [&](int t) { return upto[t] < want; });
       if (near + 1 < n_bars && sh.cum[near + 1] <= (uint32_t)kCap) {   // (a bar more, as the guess may be one too few)
-        uint64_t have;
-        if (candidates(from, edge_of(near + 1), 0ull, all, &have)) return -1;
-        khi = order_key(edge_of(near + 1));   // (they were too few)
-        above = have;
-        above_n = sh.cum[near + 1];
-        near += 2;
+        uint64_t have, have_n;
+        const Found found = candidates(from, edge_of(near + 1), 0ull, all, &have, &have_n);
+        if (found == kDone) return -1;
+        if (found == kTooFew) {
+          khi = order_key(edge_of(near + 1));
+          above = have;
+          above_n = have_n;
+          near += 2;
+        }
       }
       if (near < n_bars) pass = near;
     }
@@ -1262,7 +1268,8 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
       edge = edge_of(bar_with(kShort));
       uint64_t own = 0ull;
       if (all == 0ull) own = base.value >= -FLT_MAX || !low_is_0 ? mass_of(Yes(), base) : mass_of(No(), base);
-      if (candidates(base, edge, own, &all, &have)) return;
+      uint64_t have_n;
+      if (candidates(base, edge, own, &all, &have, &have_n) == kDone) return;
       if (fine_state == 0) fine_state = 1;
     }
     const bool short_of = have < mass_goal(all);   // (else they were too many)

@@ -351,3 +351,24 @@ def test_top_p_that_ends_far_below_the_largest(bf16, v, t, mid, dev):
     u = np.array([0.99999994, 1 - tail / 3, 0.5, 1 - tail / 2, tail / 1000, 1 - tail / 4, 1 - tail / 5, 0.0])[:rows].astype(np.float32)
     _check_within_rounding(x.to(DEV), np.full(rows, t, np.float32), u, p)
     _check_within_rounding(x.to(DEV), np.full(rows, t, np.float32), u, np.full(rows, 0.99999994, np.float32))
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("t", [0.05, 0.1, 0.3])
+def test_a_nucleus_of_some_hundreds_behind_a_wrong_guess(bf16, t):
+    """40 logits at one end of every interval of 1/32: they weigh less, or more, than their interval's middle, so the place of the nucleus's end is first
+    guessed some intervals off, where a list of all above still fits; down to intervals that lie 20 T below the largest."""
+    rng = np.random.default_rng(int(1000 * t))
+    rows, v = 24, 9001
+    x = np.full((rows, v), -90.0)
+    for r in range(rows):
+        at = rng.permutation(v)[:40 * 45].reshape(45, 40)
+        for b in range(45):
+            x[r, at[b]] = 2.0 - (b + 1) / 32 + (1 / 512 if r % 2 else 1 / 32 - 1 / 512)
+    x = torch.from_numpy(x.astype(np.float32))
+    x = (x.to(torch.bfloat16) if bf16 else x).to(DEV)
+    u = rng.random(rows).astype(np.float32)
+    p = np.concatenate([rng.uniform(0.3, 0.99, rows - 6), [0.995, 0.999, 0.9995, 0.9999, 0.99999, 0.999999]]).astype(np.float32)
+    _check(x, t, u, p=p)
+    _check(x, t, u, p=p, k=rng.integers(1300, 1700, rows))
+    _check(x, t, u, p=p, mp=np.full(rows, 1e-4, np.float32))
