@@ -1241,7 +1241,6 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
   };
 
   Cut base{-INFINITY, INT_MIN};   // (columns in front of a slice are -inf with an index below 0)
-  const float least = key_value(order_key(x_min) - 1u);
   if (by_min && !by_k && !by_p) {
     const int n = gather(x_min, INFINITY, base);
     if (n >= 0) {
@@ -1275,8 +1274,8 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
     const bool short_of = have < mass_goal(all);   // (else they were too many)
     if (find_cut(&base, true, mass_goal(all), &all, short_of ? edge : INFINITY, short_of ? have : 0ull) < 0) return;
   }
-  if (by_min && least > base.value) {
-    base = Cut{least, INT_MIN};
+  if (by_min && x_min > fmaxf(base.value, -FLT_MAX)) {   // (on the cut's own value the cut's column decides)
+    base = Cut{x_min, INT_MAX};
     in_ranges = -1;
   }
   uint64_t total, count;

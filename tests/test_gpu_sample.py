@@ -372,3 +372,20 @@ def test_a_nucleus_of_some_hundreds_behind_a_wrong_guess(bf16, t):
     _check(x, t, u, p=p)
     _check(x, t, u, p=p, k=rng.integers(1300, 1700, rows))
     _check(x, t, u, p=p, mp=np.full(rows, 1e-4, np.float32))
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_min_p_beside_a_cut_among_equal_logits(bf16):
+    """The first filters cut among thousands of equal logits whose weight is, within a rounding of the border, what min-p asks for: one float32 below
+    the border all of them go, on it or above none."""
+    v = 9001
+    x = torch.full((1, v), -1.0, dtype=torch.bfloat16 if bf16 else torch.float32, device=DEV)
+    x[0, 4321] = 0.0
+    at = float(np.float32(np.exp(-1.0)))
+    assert at > np.exp(-1.0)            # (so that the border lies above -1, by less than a float32 of logits)
+    below = float(np.nextafter(np.float32(at), np.float32(0)))
+    for kw in (dict(p=0.5), dict(k=5000), dict(k=5000, p=0.7), dict()):
+        tok, _, kept = _check(x, 1.0, np.float32([0.7]), mp=at, **kw)
+        assert (tok, kept) == ([4321], [1])
+        _, _, kept = _check(x, 1.0, np.float32([0.7]), mp=below, **kw)
+        assert kept[0] > 2048
