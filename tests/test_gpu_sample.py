@@ -389,3 +389,21 @@ def test_min_p_beside_a_cut_among_equal_logits(bf16):
         assert (tok, kept) == ([4321], [1])
         _, _, kept = _check(x, 1.0, np.float32([0.7]), mp=below, **kw)
         assert kept[0] > 2048
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("v", [100, 2049, 30000])
+def test_min_p_of_one_keeps_the_largest(bf16, v):
+    """Of rows of zeros of either sign all are kept, and so are all that are as large as the largest."""
+    dtype, tiny = (torch.bfloat16, 2.0 ** -133) if bf16 else (torch.float32, 2.0 ** -149)
+    x = torch.zeros((5, v), dtype=dtype)
+    x[1] = -0.0
+    x[2, ::2] = -0.0
+    x[3, 1::2] = -tiny
+    x[4] = torch.finfo(dtype).min
+    u = np.array([0.0, 0.99999994, 0.6, 0.3, 0.9], np.float32)
+    for mp in (1.0, 5.0):
+        _, _, kept = _check(x.to(DEV), 0.8, u, mp=mp)
+        assert kept == [v, v, v, -(-v // 2), v]
+        for kw in (dict(k=v - 1), dict(p=0.75), dict(k=v // 2, p=0.5)):
+            _check(x[[0, 1, 2, 4]].to(DEV), 0.8, u[:4], mp=mp, **kw)
