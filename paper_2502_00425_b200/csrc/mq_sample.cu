@@ -467,11 +467,12 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
   // exp(-40) and less rounds to 0.  Where T is below a step of x, the number below the maximum has that already: no larger factor is needed, and
   // none is taken, so that d c stays in a double's range.
   const float next = fmaxf(key_value(key_max - 1u), -FLT_MAX);
-  weight.low = fmaxf(fminf(top - 40.0f * temp, next), -FLT_MAX);
+  // (rounded down: to the nearest, 40 T of 1.3 steps would be one, whose weight is not 0)
+  weight.low = fmaxf(fminf(__fsub_rd(top, __fmul_ru(40.0f, temp)), next), -FLT_MAX);
   weight.c = 1.4426950408889634074 / (double)temp;
   if (next < top) weight.c = fmin(weight.c, 58.0 / ((double)top - (double)next));
   weight.table = sh.table;
-  const bool low_is_0 = weight.low > -FLT_MAX;   // -infinity, lifted to it, weighs nothing either
+  const bool low_is_0 = weight(weight.low) == 0ull;   // -infinity, lifted to it, weighs nothing either
   const bool by_k = want_k > 0 && want_k < p.V, by_p = want_p < 1.0f, by_min = min_p > 0.0f;
   // w >= min_p is x >= m - T ln(1 / min_p): the smallest float32 that is
   float x_min = -FLT_MAX;

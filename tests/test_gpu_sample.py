@@ -407,3 +407,21 @@ def test_min_p_of_one_keeps_the_largest(bf16, v):
         assert kept == [v, v, v, -(-v // 2), v]
         for kw in (dict(k=v - 1), dict(p=0.75), dict(k=v // 2, p=0.5)):
             _check(x[[0, 1, 2, 4]].to(DEV), 0.8, u[:4], mp=mp, **kw)
+
+
+@pytest.mark.parametrize("top", [300.0, 1.0, 0.75, -5.5, 2.0 ** 20])
+def test_masked_logits_weigh_nothing_at_any_temperature(top):
+    """Temperatures at which 40 T is 1/4 to 6 steps of a float32 at the largest logit, the others masked or far below: none of their 2^17 has a share."""
+    v = 1 << 17
+    step = 2.0 ** (np.floor(np.log2(abs(top))) - 23)
+    t = (np.linspace(0.25, 6, 47) * step / 40).astype(np.float32)
+    x = torch.full((1, v), -float("inf"), device=DEV)
+    x[0, 3] = top
+    y = torch.full((1, v), -2.0 ** 21, device=DEV)
+    y[0, 3] = top
+    n = t.size
+    for row, kept_all in ((x, 1), (y, v)):
+        for kw in (dict(), dict(p=0.99999994), dict(k=v - 1), dict(k=v - 1, p=0.9999)):
+            tok, lp, kept = _run(row.expand(n, v).contiguous(), t, np.full(n, 0.99999994, np.float32), **kw)
+            assert tok == [3] * n and lp == [0.0] * n, (kw, tok, lp)
+            assert kept == [1 if "p" in kw else min(kept_all, kw.get("k", v))] * n, (kw, kept)
