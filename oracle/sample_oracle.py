@@ -23,7 +23,7 @@ def sample(x, temperature, u, top_k=0, top_p=1.0, min_p=0.0, most=float(np.finfo
     if p < 1:
         before = np.concatenate([[0.0], np.cumsum(w)[:-1]])
         n = min(n, int((before < p * w.sum()).sum()))
-    if mp > 0:
+    if mp > 0 and not np.isinf(t):      # (every weight is 1 there, and min_p at most 1)
         n = min(n, int((gap[:n] >= t * np.log(min(mp, 1.0))).sum()))
     n = max(n, 1)
     kept = np.sort(order[:n])

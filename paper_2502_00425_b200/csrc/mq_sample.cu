@@ -473,7 +473,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
   if (next < top) weight.c = fmin(weight.c, 58.0 / ((double)top - (double)next));
   weight.table = sh.table;
   const bool low_is_0 = weight(weight.low) == 0ull;   // -infinity, lifted to it, weighs nothing either
-  const bool by_k = want_k > 0 && want_k < p.V, by_p = want_p < 1.0f, by_min = min_p > 0.0f;
+  const bool by_k = want_k > 0 && want_k < p.V, by_p = want_p < 1.0f, by_min = min_p > 0.0f && temp < INFINITY;   // (at an infinite T all weigh 1)
   // w >= min_p is x >= m - T ln(1 / min_p): the smallest float32 that is
   float x_min = -FLT_MAX;
   if (by_min) x_min = fmaxf(x_min, fminf(top, __double2float_ru((double)top + (double)temp * log((double)min_p)) + 0.0f));

@@ -425,3 +425,14 @@ def test_masked_logits_weigh_nothing_at_any_temperature(top):
             tok, lp, kept = _run(row.expand(n, v).contiguous(), t, np.full(n, 0.99999994, np.float32), **kw)
             assert tok == [3] * n and lp == [0.0] * n, (kw, tok, lp)
             assert kept == [1 if "p" in kw else min(kept_all, kw.get("k", v))] * n, (kw, kept)
+
+
+@pytest.mark.parametrize("v", [300, 20000])
+def test_infinite_temperature_beside_min_p(v):
+    """Every weight is 1, which is no less than any min_p."""
+    x = _logits(np.random.default_rng(v), 3, v, False)
+    x[1, ::2] = -float("inf")
+    for mp in (1.0, 7.0, 0.3):
+        tok, _, kept = _run(x, float("inf"), np.float32([0.25, 0.5, 0.75]), mp=mp)
+        assert kept == [v, v // 2, v] and tok == [v // 4, v // 2 + 1, 3 * (v // 4)]
+        assert _run(x, float("inf"), np.float32([0.25, 0.5, 0.75]), mp=mp, k=100)[2] == [100] * 3
