@@ -77,7 +77,9 @@ __device__ __forceinline__ void sched_groups(const KvSchedArgs& a, int64_t* pref
   for (int b = threadIdx.x; b < n; b += kThreads) {
     const int l = page0[b];
     if (l < 0 || l > b) continue;
-    if (page0[l] != l || (l < b && page0[b - 1] != l)) {
+    // (rows in front of its neighbour's: a cu_q that decreases.  The group's rows are counted from the first one's to the last one's, which could be
+    // fewer than none.)
+    if (page0[l] != l || (l < b && (page0[b - 1] != l || seqs[b].begin < seqs[b - 1].begin))) {
       atomicMin(&keys[l], 0);
       continue;
     }

@@ -300,3 +300,30 @@ def test_two_streams_with_their_own_workspaces():
     torch.cuda.synchronize()
     for (_, o, _), (w, _) in zip(bufs, want):
         assert np.array_equal(o.double().cpu().numpy(), w)
+
+
+@pytest.mark.parametrize("n_heads", [2, 16])
+def test_row_counts_that_decrease_share_nothing(n_heads):
+    """A cu_q that is not one: every sequence reads by itself what mq_kv_attention reads for it, and the call ends as soon."""
+    pg = Groups([(160, [1, 30, 5, 77, 8])], 2, 64, 16, seed=17)
+    dev = lambda v: torch.tensor(v, dtype=torch.int32, device=DEV)
+    for rows, cu_q in ((12, [10, 12, 2, 4, 4, 7]), (12, [8, 9, 6, 7, 2, 3]), (12, [12, 0, 0, 1, 1, 1]), (12, [5, 6, 6, 7, 8, 3]),
+                       (12, [900, -4, 2, 3, 1 << 30, 11]), (12, [0, 6, 10, 3, 4, 5]), (700, [690, 692, 2, 4, 4, 7]), (700, [699, 0, 600, 601, 100, 102])):
+        q = _queries([rows], n_heads, 64, seed=18).to(DEV)
+        ws = B.new_kv_attention_workspace(5, rows, 2, pg.table.shape[1], n_heads, pg.cache)
+        wss = B.new_kv_attention_shared_workspace(5, rows, 2, pg.table.shape[1], n_heads, pg.cache)
+        a, b = (torch.full((rows, n_heads * 64), 7.0, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+        B.mq_kv_attention(q, dev(cu_q), pg.kv_len, pg.table, pg.cache, n_heads, 2, a, ws)
+        B.mq_kv_attention_shared(q, dev(cu_q), pg.kv_len, pg.table, pg.d_leader, pg.d_shared, pg.cache, n_heads, 2, b, wss)
+        torch.cuda.synchronize()
+        assert B.mq_last_device_status(wss) == B.mq_last_device_status(ws) == (B.MQ_OK, 0)
+        begin = [min(max(c, 0), rows) for c in cu_q[:-1]]
+        spans = [(lo, min(min(max(hi, lo), rows) - lo, 2)) for lo, hi in zip(begin, cu_q[1:])]
+        owned = [sum(lo <= r < lo + n for lo, n in spans) for r in range(rows)]
+        assert max(owned) == 1
+        most = float(pg.V[pg.V == pg.V].abs().max())         # of a value, and so of a result and of the sums of absolute values
+        for r in range(rows):
+            if owned[r]:                                     # (each within two roundings to bf16 and a probability's, besides float32 sums)
+                assert float((a[r].float() - b[r].float()).abs().max()) <= 2 * (2.0 ** -8 + 2.0 ** -8 + 2.0 ** -10) * most, (cu_q, r)
+            else:
+                assert bool((a[r] == 7.0).all()) and bool((b[r] == 7.0).all())
