@@ -231,7 +231,9 @@ class DeviceKVCache:
         self.n_free = torch.full((1,), n_pages, dtype=torch.int32, device=device)
         self.plan_status = ints(2)
         self.state = B.KVState(self.kv_len, self.seen, self.table, self.free, self.n_free, page_size, borrowed=self.borrowed)
-        self.leaders = list(range(n_seq))   # as `leader` says
+        self.leaders = list(range(n_seq))   # whose pages a sequence begins with: its own, or those it borrows
+        self._heads = list(range(n_seq))    # as `leader` says: of every sequence, the first of those that are read together
+        self._ended = [False] * n_seq       # released, and without rows since
         self._lent = [0] * n_seq            # keys that others have from a sequence, or that it has from another
         self._ws = {}
         self._numbers = {}                  # small device arrays, by what they hold
@@ -251,6 +253,21 @@ class DeviceKVCache:
             self._captured.add(key)
         return self._numbers[key]
 
+    def _group(self, ended: List[bool]):
+        """Neighbours that begin with the same pages are read together, whichever of them is the first (the pages are in every one's list); one that has
+        ended parts them only when it gets rows again, as a sequence of its own."""
+        heads, last = list(range(self.n_seq)), None
+        for b in range(self.n_seq):
+            if ended[b]:
+                continue
+            if last is not None and self.leaders[b] == self.leaders[last]:
+                heads[last + 1:b + 1] = [heads[last]] * (b - last)
+            last = b
+        if heads != self._heads:
+            self.leader.copy_(self._ints(heads))
+            self._heads = heads
+        self._ended = ended
+
     def _plan(self, new: torch.Tensor, keep: Optional[torch.Tensor], rows: int):
         cu = torch.empty(self.n_seq + 1, dtype=torch.int32, device=self.device)
         slots, pos = (torch.empty(rows, dtype=t, device=self.device) for t in (torch.int64, torch.int32))
@@ -263,6 +280,8 @@ class DeviceKVCache:
         assert len(new) == self.n_seq and min(new) >= 0
         if keep is not None and any(k < n for k, n in zip(keep, self._lent)):
             raise RuntimeError("a sequence keeps what others borrow from it, and what it has borrowed")
+        if any(n and e for n, e in zip(new, self._ended)):
+            self._group([e and not n for n, e in zip(new, self._ended)])
         total = sum(new)
         cu, slots, pos = self._plan(self._ints(new), None if keep is None else self._ints(keep), total)
         self._last = CacheStep(list(new), cu, self.kv_len, slots, pos, total, max(new))
@@ -291,14 +310,14 @@ class DeviceKVCache:
         pages = lengths[src] // self.page_size
         rows = slice(first, first + count)
         self.table[rows] = self.table[src]
-        for array, value in ((self.borrowed, pages), (self.kv_len, pages * self.page_size), (self.shared_len, pages * self.page_size),
-                             (self.leader, src)):
+        for array, value in ((self.borrowed, pages), (self.kv_len, pages * self.page_size), (self.shared_len, pages * self.page_size)):
             array[rows] = value
         self.seen[rows] = self.seen[src] - (lengths[src] - pages * self.page_size)
         self.shared_len[src] = 1 << 30                # (as far as the others go)
         self.leaders[first:first + count] = [src] * count
         self._lent[src] = max(self._lent[src], pages * self.page_size)
         self._lent[first:first + count] = [pages * self.page_size] * count
+        self._group([e and b not in to for b, e in enumerate(self._ended)])
         self._last = None
         return pages * self.page_size
 
@@ -318,7 +337,7 @@ class DeviceKVCache:
         for b in range(self.n_seq):
             if self.leaders[b] == b and b not in self.leaders[:b] + self.leaders[b + 1:]:
                 self._lent[b] = 0
-        self.leader.copy_(torch.tensor(self.leaders, dtype=torch.int32))
+        self._group([e or b in sequences for b, e in enumerate(self._ended)])
         for b in sequences:
             self.shared_len[b] = 0
         self._last = None
@@ -331,13 +350,13 @@ class DeviceKVCache:
         if self.n_seq > 1024 or not any(self._lent):   # (the shared form's limit; every sequence's pages are in its own row as well)
             return False
         rows, keys = {}, {}
-        for b, l in enumerate(self.leaders):
+        for b, h in enumerate(self._heads):
             if step.new[b]:
-                rows[l] = rows.get(l, 0) + 1
-                if l != b:
-                    keys[l] = min(keys.get(l, self.max_len), self._lent[b])
+                rows[h] = rows.get(h, 0) + 1
+                if self.leaders[b] != b:
+                    keys[h] = min(keys.get(h, self.max_len), self._lent[b])
         numbers = 2 * self.handle.n_kv_heads * self.handle.head_dim
-        return any(rows[l] > 1 for l in keys) and sum((rows[l] - 1) * k for l, k in keys.items()) * numbers >= self.shared_from
+        return any(rows[h] > 1 for h in keys) and sum((rows[h] - 1) * k for h, k in keys.items()) * numbers >= self.shared_from
 
     def workspace(self, step: CacheStep, n_q_heads: int) -> torch.Tensor:
         """As PagedKVCache.workspace()."""

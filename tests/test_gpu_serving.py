@@ -215,3 +215,33 @@ def test_a_step_of_new_sizes_is_not_captured():
     with pytest.raises(RuntimeError, match="once before"):
         with torch.cuda.graph(g):
             cache.extend([1, 1])
+
+
+@pytest.mark.parametrize("int8", [False, True])
+def test_answers_that_end_one_after_another(int8, monkeypatch):
+    """Questions about one prompt, of which some end and leave their places empty or to new sequences: the others go on reading the shared keys once."""
+    blk = _calibrated(_block(7))
+    scales = (torch.full((2,), 0.02, device=DEV), torch.full((2,), 0.05, device=DEV)) if int8 else (None, None)
+    cache = KC.DeviceKVCache(7, 80, 300, 2, 128, 16, *scales, shared_from=0)
+    groups = []
+    call = B.mq_kv_attention_shared
+    monkeypatch.setattr(B, "mq_kv_attention_shared", lambda *a, **k: (groups.append(a[4].tolist()), call(*a, **k))[1])
+    none = _emb(0, 1)
+    blk.forward_cached([_emb(90, 1)] + [none] * 6, cache)
+    assert cache.share(0, 1, 6) == 80
+
+    def step(rows, seed):
+        _, tr = blk.forward_cached([_emb(n, seed + b) for b, n in enumerate(rows)], cache)
+        _check_attention(cache, tr, rows)
+        return groups[-1]
+
+    assert step([0, 5, 3, 9, 1, 2, 4], 10) == [0] * 7
+    cache.release([2])
+    assert step([1, 1, 0, 1, 1, 1, 1], 20) == [0] * 7
+    cache.release([4, 5])
+    assert step([1, 1, 0, 1, 0, 0, 1], 30) == [0] * 7
+    assert step([0, 1, 20, 1, 0, 0, 1], 40) == [0, 0, 2, 3, 3, 3, 3]          # a new sequence in place 2
+    assert step([1, 1, 1, 1, 7, 0, 1], 50) == [0, 0, 2, 3, 4, 5, 6]           # and in place 4
+    cache.release([2, 4])
+    assert step([1, 1, 0, 1, 0, 0, 1], 60) == [0] * 7
+    assert cache.status_ok() and blk.device_status_ok()

@@ -271,3 +271,31 @@ def test_the_shared_form_is_called_where_it_saves_enough(make):
     wide.extend([20] + [0] * 1024)
     wide.share(0, 1, 2)
     assert not wide._shares(wide.extend([1] * 1025))
+
+
+def test_an_answer_that_ends_leaves_the_others_their_sharing(make):
+    cache = make(8, 80, 200, 2, 64, page_size=16, shared_from=0)
+    cache.extend([70] + [0] * 6 + [5])
+    cache.share(0, 1, 6)
+    step = cache.extend([1] * 8)
+    cache.release([2])                                        # nobody parts the group as long as the place is empty
+    assert cache.leader.tolist() == [0, 0, 0, 0, 0, 0, 0, 7] and cache.leaders == [0, 0, 2, 0, 0, 0, 0, 7]
+    step = cache.extend([1, 1, 0, 1, 1, 1, 1, 1])
+    saved = lambda step: [limit for limit in (5, 4, 3, 2, 1) if not setattr(cache, "shared_from", limit * 64 * 256) and cache._shares(step)]
+    assert saved(step)[0] == 5                                # (64 keys of 256 numbers for five of six)
+    cache.release([4, 6])
+    assert cache.leader.tolist() == [0, 0, 0, 0, 0, 0, 6, 7]
+    step = cache.extend([1, 0, 9, 1, 0, 1, 0, 0])             # place 2 taken by a sequence of its own: two groups, read by what both sides' pages are
+    assert cache.leader.tolist() == [0, 0, 2, 3, 3, 3, 6, 7] and cache.lengths()[:6] == [73, 66, 9, 67, 0, 67]
+    assert cache.shared_len.tolist()[3:6] == [64, 0, 64] and _pages(cache, 3)[:4] == _pages(cache, 0)[:4] == _pages(cache, 5)[:4]
+    assert saved(step) == [1] and saved(cache.extend([1, 1, 1, 1, 0, 1, 0, 0]))[0] == 2
+    assert saved(cache.extend([1, 0, 1, 0, 0, 1, 0, 0])) == []                               # one of each group: nothing is read twice
+    assert saved(cache.extend([0] * 8)) == []
+    cache.release([2])
+    assert cache.leader.tolist() == [0, 0, 0, 0, 0, 0, 6, 7]
+    cache.release([0, 1, 3, 5])
+    assert cache.leader.tolist() == list(range(8)) and cache.lengths() == [0] * 7 + [7] and cache.status_ok()
+    assert not cache._shares(cache.extend([1] * 8))
+    assert not any(cache._ended)
+    cache.extend([0] * 8, keep=[0] * 8)
+    assert int(cache.n_free) == 80
