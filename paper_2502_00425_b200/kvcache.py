@@ -248,7 +248,9 @@ class DeviceKVCache:
                 raise RuntimeError("make a step of these sizes once before capturing it: its arrays have to be made first")
             if len(self._numbers) >= 256:
                 self._numbers = {k: v for k, v in self._numbers.items() if k in self._captured}
-            self._numbers[key] = torch.tensor(key, dtype=torch.int32).to(self.device)
+            # (from pinned memory, which torch does not hand out again before the copy is done: a copy from other memory waits for all that is queued)
+            pinned = torch.tensor(key, dtype=torch.int32, pin_memory=self.device.type == "cuda")
+            self._numbers[key] = pinned.to(self.device, non_blocking=True)
         if capturing:
             self._captured.add(key)
         return self._numbers[key]

@@ -245,3 +245,20 @@ def test_answers_that_end_one_after_another(int8, monkeypatch):
     cache.release([2, 4])
     assert step([1, 1, 0, 1, 0, 0, 1], 60) == [0] * 7
     assert cache.status_ok() and blk.device_status_ok()
+
+
+def test_a_step_of_new_lengths_waits_for_nothing():
+    """Lengths that were never asked for go to the GPU behind what is queued, and the host goes on."""
+    cache = KC.DeviceKVCache(16, 200, 400, 2, 128, 16)
+    lengths, rng = [0] * 16, np.random.default_rng(12)
+    for _ in range(3):                                  # (the first rounds make the pinned memory)
+        torch.cuda.synchronize()
+        done = torch.cuda.Event()
+        torch.cuda._sleep(200_000_000)                  # some 0.1 s
+        done.record()
+        for _ in range(4):
+            new, keep = rng.integers(0, 3, 16).tolist(), rng.integers(0, 9, 16).tolist()
+            cache.extend(new, keep)
+            lengths = [min(k, l) + a for k, l, a in zip(keep, lengths, new)]
+        ahead = not done.query()
+    assert ahead and cache.lengths() == lengths and cache.status_ok()
