@@ -251,9 +251,12 @@ class DeviceKVCache:
             # (from pinned memory, which torch does not hand out again before the copy is done: a copy from other memory waits for all that is queued)
             pinned = torch.tensor(key, dtype=torch.int32, pin_memory=self.device.type == "cuda")
             self._numbers[key] = pinned.to(self.device, non_blocking=True)
+        numbers = self._numbers[key]
         if capturing:
             self._captured.add(key)
-        return self._numbers[key]
+        elif numbers.is_cuda:               # (it may be dropped while a stream that did not make it has yet to read it)
+            numbers.record_stream(torch.cuda.current_stream(self.device))
+        return numbers
 
     def _group(self, ended: List[bool]):
         """Neighbours that begin with the same pages are read together, whichever of them is the first (the pages are in every one's list); one that has

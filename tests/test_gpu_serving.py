@@ -262,3 +262,21 @@ def test_a_step_of_new_lengths_waits_for_nothing():
             lengths = [min(k, l) + a for k, l, a in zip(keep, lengths, new)]
         ahead = not done.query()
     assert ahead and cache.lengths() == lengths and cache.status_ok()
+
+
+def test_lengths_stay_until_another_stream_has_read_them():
+    """Lengths made on one stream and read on another one, which is behind: they are dropped from the cache, and their memory is asked for, in between."""
+    cache = KC.DeviceKVCache(16, 200, 400, 2, 128, 16)
+    cache.extend([3] * 16)
+    cache.extend([0] * 16, keep=[0] * 16)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200_000_000)
+        cache.extend([3] * 16)                                  # (the arrays that the default stream made)
+        for i in range(300):
+            cache.extend([0] * 16, keep=[1 << 30] * 15 + [1000 + i])
+    assert (3,) * 16 not in cache._numbers
+    taken = [torch.full((16,), 2, dtype=torch.int32, device=DEV) for _ in range(400)]
+    torch.cuda.synchronize()
+    assert cache.lengths() == [3] * 16 and cache.status_ok() and len(taken) == 400
