@@ -300,7 +300,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
   const int n_groups = (r.pieces + kThreads * kGroup - 1) / (kThreads * kGroup);
   const float temp = p.temperature[row], u = p.u[row];
   const int want_k = p.top_k ? p.top_k[row] : 0;
-  const float want_p = p.top_p ? p.top_p[row] : 1.0f, min_p = p.min_p ? p.min_p[row] : 0.0f;
+  const float want_p = p.top_p ? p.top_p[row] : 1.0f, min_p = p.min_p && temp < INFINITY ? p.min_p[row] : 0.0f;   // (at an infinite T all weigh 1)
   __syncthreads();   // the bars are zero
   float top = -INFINITY;
   bool odd = false;
@@ -472,8 +472,8 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) sample_kernel(const __grid
   weight.c = 1.4426950408889634074 / (double)temp;
   if (next < top) weight.c = fmin(weight.c, 58.0 / ((double)top - (double)next));
   weight.table = sh.table;
-  const bool low_is_0 = weight(weight.low) == 0ull;   // -infinity, lifted to it, weighs nothing either
-  const bool by_k = want_k > 0 && want_k < p.V, by_p = want_p < 1.0f, by_min = min_p > 0.0f && temp < INFINITY;   // (at an infinite T all weigh 1)
+  const bool low_is_0 = weight.low > -FLT_MAX;   // -infinity, lifted to it, weighs nothing either
+  const bool by_k = want_k > 0 && want_k < p.V, by_p = want_p < 1.0f, by_min = min_p > 0.0f;
   // w >= min_p is x >= m - T ln(1 / min_p): the smallest float32 that is
   float x_min = -FLT_MAX;
   if (by_min) x_min = fmaxf(x_min, fminf(top, __double2float_ru((double)top + (double)temp * log((double)min_p)) + 0.0f));
