@@ -567,8 +567,8 @@ int mq_kv_attention(const void* Q, int64_t ldq, const mq_kv_batch* batch, const 
  * by side in the batch.  Every sequence's page list names the shared pages as well, so the result is mq_kv_attention's (up to the order of its
  * float32 sums), but the shared keys are read, and multiplied with all rows of the group, once.  Shared are whole pages, at most as
  * many as every sequence of the group with new rows has cached in front of them; what is left, and groups with fewer than two such
- * sequences, or whose leaders do not say what is written here, every sequence reads by itself.  Shared pages are taken from the first
- * sequence's list.
+ * sequences, or whose leaders or row counts (cu_q does not decrease) are not what is written here, every sequence reads by itself.
+ * Shared pages are taken from the first sequence's list.
  *   leader, shared_len  device int32 [n_seq];  n_seq <= 1024, total_q * n_q_heads <= 2^30
  * ws as for mq_kv_attention, of mq_kv_attention_shared_workspace_bytes(): it holds a float32 result per query row and key list.
  */
@@ -650,7 +650,7 @@ int mq_kv_plan(const mq_kv_state* state, const int32_t* new_len, const int32_t* 
  *   min_p   keeps those with w_i >= min_p (<= 0 or NaN: all; above 1 counts as 1);
  * the first of the order is always kept.  token[r] is the first kept index, in the order of the vocabulary, at which the running sum of the
  * kept weights exceeds u[r] times their total (u in [0, 1); what lies outside counts as its nearest).  T <= 0 or NaN: the
- * first of the order.  NaN and -infinity logits are never kept; where every logit is one, token is -1.  +infinity
+ * first of the order; T infinite: all weigh 1.  NaN and -infinity logits are never kept; where every logit is one, token is -1.  +infinity
  * counts as the largest finite number of the type.
  *   temperature, u   device float32 [B];  top_k device int32 [B], top_p, min_p device float32 [B], each may be NULL (all kept)
  *   token            device int32 [B]

@@ -13,7 +13,7 @@
 // rotation) are 35 us of issue by themselves, as long as the bytes take; issue is busy for 68 % of the cycles in which an SM
 // has work, the rest are fixed latencies and the shuffles' and conversions' results (7 warps to a scheduler), and 11 % of the
 // time an SM has none (start, last round).  Into an int8 cache: 6 us more.  32 tokens: 3.4 us.  Half of the head rotated, in pairs
-// (i, i + 32): 60 us call to call where the whole head takes 55; the lanes of what passes read two neighbouring runs.
+// (i, i + 32): 60 us call to call where the whole head takes 55; the lanes of what passes read two neighbouring runs, and its 64 registers spill 16 bytes.
 #include "mq_kv.cuh"
 
 namespace mq {

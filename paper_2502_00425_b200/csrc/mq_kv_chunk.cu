@@ -24,7 +24,7 @@
 // 2048 tokens behind 32768 keys, 28 / 4 heads of 128 (992 GFLOP): 825 us in a short run, 1.2 PFLOP/s (72 % of the measured GEMM
 // rate), and 960 to 990 us in a long one, under the power cap.  A tile of 256 rows takes some 3700 cycles: 2 x 1300 of softmax per group, the rest the products that the
 // two groups cannot hide for one another; the products alone would take 661 us, the softmax without exponentials 764.  Over an int8
-// cache 16 warps share the registers, 128 a thread, which spills 72 bytes.  Six turns of 40 to 701 tokens in AIFS order: 83 us, of which 51 at this rate.  A call of a few tiles is 5 us of start (work line, page
+// cache 16 warps share the registers, 128 a thread, which spills 80 bytes (with a shared prefix 120 - 128 on its line, 252 on the other).  Six turns of 40 to 701 tokens in AIFS order: 83 us, of which 51 at this rate.  A call of a few tiles is 5 us of start (work line, page
 // table, first tiles), its tiles, 2 us of results and the join.
 // Every wait is bounded (mq_sm100.cuh); an expired one makes all roles leave and sets the status word.
 #include <cuda.h>

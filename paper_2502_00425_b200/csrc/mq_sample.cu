@@ -16,9 +16,10 @@
 //   * Where what is kept does not fit into a list, passes that sum mass and count above several values at once narrow the place of the cut
 //     down until its neighbourhood fits; equal logits by the thousand are cut by index.  The kept weights are then summed by warps over
 //     contiguous ranges, and only the range that the random number falls into is walked.
-// Bound by latency for few rows: a greedy row of 131072 takes 5.4 us, one with a few candidates 11 - 15 (some 15 steps with a cluster barrier of 1.5 us
-// each), one that keeps thousands 27 - 45, a pass from L2 4 - 10 us each.  256 x 150001 float32: greedy 46 us, 3.4 TB/s, as the first pass of
-// a row and the steps behind it do not overlap within its cluster; top-k 65, unfiltered 97, top-p 206.
+// Bound by latency for few rows: a greedy row of 131072 takes 5.5 us, one with a few candidates 11 - 14 (three cluster barriers, as all
+// rows that end on their first list or keep everything, and some 14 of the block, the last of them in one CTA alone), one that keeps thousands
+// 27 - 44 (seven to nine cluster barriers and three or four passes from L2 of 4 - 10 us each).  256 x 150001 float32: greedy 46 us,
+// 3.4 TB/s, as the first pass of a row and the steps behind it do not overlap within its cluster; top-k 65, unfiltered 97, top-p 204.
 #include <cfloat>
 #include <climits>
 #include <cmath>
@@ -37,7 +38,7 @@ namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 // CTAs to an SM.  float32: 256 x 150001, top-k 50: 66 us, 76 with 3.  bf16, whose pieces are twice as many elements in registers: 64 x 131072
-// with filters as in use 67 us, 72 with 4; 1 x 131072, greedy, 6.8 us, 7.9 with 4 (256 x 150001 loses by it: 175 us, 168 with 4)
+// with filters as in use 67 us, 72 with 4; 1 x 131072, greedy, 6.8 us, 7.9 with 4 (256 x 150001 loses by it: 175 us, 168 with 4; an earlier form's times)
 template <typename T>
 constexpr int kCtas = sizeof(T) == 4 ? 4 : 3;
 constexpr int kCap = 2048;            // candidates of a list

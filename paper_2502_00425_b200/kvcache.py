@@ -211,9 +211,12 @@ class DeviceKVCache:
     its time, and is captured anew after share() or release().
 
     shared_from: where a step's groups have at least so many numbers (keys and values, times channels) to read again, they are read once by
-    mq_kv_attention_shared; below, the repeated reads come out of L2 faster than two lines of work and their join (one new token each, 8
-    heads of 128, bf16: 32 sequences over 1024 shared keys, 65 million, 23.7 us against 21.0, over 2048 24.1 against 29.0; 8 over 4096 21.5
-    against 17.9, over 8192 26.5 against 29.5; int8 the same in numbers)."""
+    mq_kv_attention_shared; below, the repeated reads come out of L2 faster than two lines of work and their join.  One new token each, bf16,
+    shared against not: 28 / 4 heads of 128, 32 sequences over 2048 keys (65 million) 21.1 us against 21.7, over 3360 (106) 28.3 against 27.6, over
+    4096 (130) 28.6 against 30.4, over 6144 (195) 31.0 against 38.6; 32 / 8 heads, 4 over 16384 (101) 28.5 against 31.9, 8 over 8192 (117) 28.5
+    against 29.1, 64 over 1024 (132) 35.8 against 35.5, over 2048 (264) 36.7 against 51.6.  So between 65 and 130 million it depends on the sizes, and the
+    choice is up to 6 % off.  Steps of several tokens gain earlier (four each, 28 / 4 heads, 32 sequences over 2048 keys: 37.7 against 50.6): where they are
+    usual, half of this number is better."""
 
     def __init__(self, n_seq: int, n_pages: int, max_len: int, n_kv_heads: int, head_dim: int, page_size: int = 64,
                  k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None, device="cuda", shared_from: int = 100_000_000):
