@@ -272,6 +272,8 @@ class DeviceKVCache:
                 heads[last + 1:b + 1] = [heads[last]] * (b - last)
             last = b
         if heads != self._heads:
+            if torch.cuda.is_current_stream_capturing():   # (the host would know of groups that the GPU has only once the graph is replayed)
+                raise RuntimeError("make a step of these sizes once before capturing it: a sequence begins again in it")
             self.leader.copy_(self._ints(heads))
             self._heads = heads
         self._ended = ended

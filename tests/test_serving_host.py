@@ -299,3 +299,24 @@ def test_an_answer_that_ends_leaves_the_others_their_sharing(make):
     assert not any(cache._ended)
     cache.extend([0] * 8, keep=[0] * 8)
     assert int(cache.n_free) == 80
+
+
+def test_groups_do_not_change_in_a_capture(make, monkeypatch):
+    cache = make(4, 40, 200, 2, 64, page_size=16)
+    cache.extend([40, 0, 0, 0])
+    cache.share(0, 1, 3)
+    cache.extend([0, 1, 1, 1])
+    cache.release([2])
+    for row in ([1, 1, 3, 1], [0, 0, 2, 3], [0, 0, 0, 0]):          # (the arrays are there)
+        cache._ints(row)
+    with monkeypatch.context() as m:
+        m.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+        with pytest.raises(RuntimeError, match="once before"):
+            cache.extend([1, 1, 3, 1])
+        assert cache.leader.tolist() == [0, 0, 0, 0] == cache._heads and cache.lengths() == [40, 33, 0, 33]
+    cache.extend([1, 1, 3, 1])
+    assert cache.leader.tolist() == [0, 0, 2, 3] == cache._heads
+    with monkeypatch.context() as m:
+        m.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+        cache.extend([1, 1, 3, 1])
+    assert cache.lengths() == [42, 35, 6, 35] and cache.status_ok()
